@@ -8,3 +8,11 @@ from .binding import (  # noqa: F401
     GPGA_OBJ_LOGISTIC, GPGA_OBJ_QUADRATIC, GPGA_TOPO_EXP, GPGA_TOPO_GRID, GPGA_TOPO_NONE,
     GPGA_TOPO_RING, GPGA_TOPO_SPARSE, GPGA_TOPO_STATIC_EXP, GPGA_X0_PER_NODE_NORMAL, GPGA_X0_SHARED_NORMAL,
     GPGA_X0_ZERO, Gpga, GpgaError, lib)
+
+
+def __getattr__(name):
+    """The token-block operators, loaded on first use (they need torch)."""
+    if name in ("embedding_forward", "embedding_backward", "dropout", "layer_norm_forward", "layer_norm_backward"):
+        from . import token_ops
+        return globals().setdefault(name, getattr(token_ops, name))
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

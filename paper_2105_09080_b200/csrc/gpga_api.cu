@@ -12,6 +12,7 @@
 #include "gpga_loss.cuh"
 #include "gpga_shard.cuh"
 #include "gpga_tile.cuh"
+#include "gpga_token.cuh"
 
 using namespace gpga;
 
@@ -63,6 +64,15 @@ struct gpga_ctx {
 };
 
 static thread_local std::string g_create_error;
+
+int32_t gpga::token_error(int32_t code, const char* text) noexcept
+{
+    try {
+        g_create_error = text;
+    } catch (...) {   // no memory for the text: the status stands
+    }
+    return code;
+}
 
 namespace {
 
