@@ -13,23 +13,40 @@ __device__ __forceinline__ int64_t token_at(const void* tokens, bool is64, int64
 }
 
 // ---- lookup -----------------------------------------------------------------------------------------
-template <class T, bool TVEC, bool OVEC>
+// TPR lanes take a stretch of NC * TPR chunks of one row.  VEC: the rows of the table and of out are aligned.
+template <class T, bool VEC, int TPR, int NC>
 __global__ void __launch_bounds__(256) lookup_kernel(const LookupParams p)
 {
-    const uint32_t chunks = (uint32_t)(p.d + kChunk - 1) / kChunk;
-    const uint64_t g = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-    if (g >= (uint64_t)p.nodes * p.rows * chunks) return;
-    const uint32_t row = (uint32_t)(g / chunks), chunk = (uint32_t)(g - (uint64_t)row * chunks);
-    const uint32_t node = row / p.rows;
-    const int col = (int)chunk * kChunk;
+    const uint32_t node = blockIdx.y, chunks = p.chunks.d;
+    const uint32_t g = blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+    const uint32_t t = divide(g, p.stretches);
+    if (t >= p.rows) return;
+    const uint32_t first = (g - t * p.stretches.d) * (NC * TPR);
+    const int lane = threadIdx.x % TPR;
+    const int64_t row = (int64_t)node * p.rows + t;
     const int64_t token = token_at(p.tokens, p.tokens64, row);
-    float v[8] = {};
-    if (token >= 0 && token < (int64_t)p.vocab) {
-        param8(p.table + node * p.node_ldt + token * p.ldt, col, p.d, TVEC, v);
+    const bool named = token >= 0 && token < (int64_t)p.vocab;
+    const float* table = p.table + node * p.node_ldt;
+    const Span span = span_of<float>(table, p.ldt, p.vocab, p.d);
+    const float* from = table + (named ? token : 0) * p.ldt;
+    Raw8<float, VEC> raw[NC];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] *= p.scale;
+    for (int c = 0; c < NC; ++c)
+        if (!VEC || first + c * TPR + lane < chunks) raw[c].load_cached(from, (int)(first + c * TPR + lane) * kChunk, p.d, span);
+    RowStore<T, VEC, TPR> store;
+    T* out = static_cast<T*>(p.out) + row * p.ldo;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        const uint32_t base = first + c * TPR;
+        if (base >= chunks) break;
+        f32x2_t v[4];
+        if (!VEC || base + lane < chunks) {
+            raw[c].get(v);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = named ? mul2(v[j], both(p.scale)) : both(0.f);
+        }
+        store.store(out, (int)(base + lane) * kChunk, p.d, v, lane, group_mask<TPR>(), c + 1 == NC || base + TPR >= chunks);
     }
-    store8<T, OVEC>(static_cast<T*>(p.out) + (int64_t)row * p.ldo, col, p.d, v);
 }
 
 // ---- gradient: sort -----------------------------------------------------------------------------------
@@ -56,7 +73,7 @@ GradLayout grad_layout(int64_t nodes, int64_t rows, int64_t d, int64_t vocab)
     L.tile = tile_entries(nodes, rows);
     L.tiles = (uint32_t)((rows + L.tile - 1) / L.tile);
     L.words = (uint32_t)((vocab + 31) / 32);
-    L.dpad = (int32_t)((d + 3) / 4 * 4);
+    L.dpad = (int32_t)((d + 7) / 8 * 8);
     L.key_off = 0;
     L.pos_off = L.key_off + up(nodes * rows * 4);
     L.bit_off = L.pos_off + up(nodes * rows * 4);
@@ -216,35 +233,6 @@ struct SumParams {
     bool accumulate, gvec;   // gvec: 128-bit accesses to grad
 };
 
-// Column of element j of a thread: eight adjacent ones, or eight that are TX apart where rows are not aligned
-// (a warp then reads adjacent elements).
-template <bool VEC, int TX>
-__device__ __forceinline__ int column(int c0, int tx, int j) { return VEC ? c0 + tx * 8 + j : c0 + j * TX + tx; }
-
-template <class T, bool VEC, int TX> struct Entry;
-template <class T, int TX> struct Entry<T, true, TX> {
-    Raw8<T, true> raw;
-    __device__ __forceinline__ void load(const T* row, int c0, int tx, int d)
-    {
-        if (c0 + tx * 8 < d) raw.load(row, c0 + tx * 8, d);
-    }
-    __device__ __forceinline__ void get(float* v) const { raw.get(v); }
-};
-template <class T, int TX> struct Entry<T, false, TX> {
-    T e[8];
-    __device__ __forceinline__ void load(const T* row, int c0, int tx, int d)
-    {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (c0 + j * TX + tx < d) e[j] = row[c0 + j * TX + tx];
-    }
-    __device__ __forceinline__ void get(float* v) const
-    {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = to_f32(e[j]);
-    }
-};
-
 // The sorted entries are cut into tiles of p.tile; TX threads walk a tile's entries over 8 TX columns and keep the
 // running sum of one token.  A token whose entries all lie in the tile is written to its row of grad; one that
 // comes from the tile before or goes on into the next leaves a partial sum (slot 0: came from before, slot 1:
@@ -252,64 +240,66 @@ template <class T, int TX> struct Entry<T, false, TX> {
 template <class T, bool VEC, int TX>
 __device__ __forceinline__ void sum_tile(const SumParams& p, uint32_t node, uint32_t tile, int c0, int tx)
 {
-    constexpr int U = 8;
+    constexpr int U = VEC && sizeof(T) == 2 ? 8 : 4;   // entries whose loads are in flight together
+    constexpr int LANES = TX < 32 ? TX : 32;
     const uint32_t* keys = p.keys + (int64_t)node * p.count;
     const uint32_t* pos = p.pos + (int64_t)node * p.count;
     const T* dout = static_cast<const T*>(p.dout) + (int64_t)node * p.node_rows * p.ldo;
+    const Span span = span_of<T>(dout, p.ldo, p.node_rows, p.d);
     const uint32_t begin = tile * p.tile, end = min(begin + p.tile, p.count);
     float* part = p.part + ((int64_t)node * p.tiles + tile) * 2 * p.dpad;
     const uint32_t none = 0xFFFFFFFFu;
     const uint32_t prev = begin ? keys[begin - 1] : none, next = end < p.count ? keys[end] : none;
-    const unsigned group = TX >= 32 ? 0xFFFFFFFFu : ((1u << (TX & 31)) - 1u) << ((threadIdx.x & 31) / TX * TX);
-    float acc[8] = {};
+    const unsigned group = group_mask<TX>();
+    const int c = c0 + tx * 8;
+    f32x2_t acc[4] = {both(0.f), both(0.f), both(0.f), both(0.f)};
     uint32_t cur = keys[begin];
     bool from_before = cur == prev;
     auto flush = [&](bool goes_on) {
         if (cur >= p.vocab) return;
         if (from_before || goes_on) {
             float* to = part + (from_before ? 0 : p.dpad);
-            if constexpr (VEC) {
-                const int c = c0 + tx * 8;
-                if (c < p.d) {
-                    *reinterpret_cast<float4*>(to + c) = make_float4(acc[0], acc[1], acc[2], acc[3]);
-                    *reinterpret_cast<float4*>(to + c + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (column<VEC, TX>(c0, tx, j) < p.d) to[column<VEC, TX>(c0, tx, j)] = acc[j];
+            if (c < p.dpad) {
+                *reinterpret_cast<float4*>(to + c) = join4(acc[0], acc[1]);
+                *reinterpret_cast<float4*>(to + c + 4) = join4(acc[2], acc[3]);
             }
             return;
         }
         float* to = p.grad + node * p.node_ldg + (int64_t)cur * p.ldg;
-        if (VEC && p.gvec) {
-            const int c = c0 + tx * 8;
-            if (c < p.d) {
-                float4 a = make_float4(acc[0] * p.scale, acc[1] * p.scale, acc[2] * p.scale, acc[3] * p.scale);
-                float4 b = make_float4(acc[4] * p.scale, acc[5] * p.scale, acc[6] * p.scale, acc[7] * p.scale);
-                float4* t4 = reinterpret_cast<float4*>(to + c);
-                if (p.accumulate) a = add4(t4[0], a), b = add4(t4[1], b);
-                __stcs(t4, a);
-                __stcs(t4 + 1, b);
-            }
-        } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int c = column<VEC, TX>(c0, tx, j);
-                if (c < p.d) to[c] = (p.accumulate ? to[c] : 0.f) + acc[j] * p.scale;
+        for (int j = 0; j < 4; ++j) acc[j] = mul2(acc[j], both(p.scale));
+        if (p.gvec) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (c + 4 * h < p.d) {
+                    float4 a = join4(acc[2 * h], acc[2 * h + 1]);
+                    float4* at = reinterpret_cast<float4*>(to + c) + h;
+                    if (p.accumulate) a = add4(*at, a);
+                    __stcs(at, a);
+                }
+        } else {
+            if (p.accumulate) {
+                Raw8<float, false> old;
+                f32x2_t v[4];
+                old.load(to, c, p.d, span_of<float>(to, 0, 1, p.d));
+                old.get(v);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[j] = add2(v[j], acc[j]);
             }
+            RowStore<float, false, LANES> store;
+            store.store(to, c, p.d, acc, tx % LANES, group, true);
         }
     };
     for (uint32_t e0 = begin; e0 < end; e0 += U) {
-        const uint32_t own_e = min(e0 + (tx & 7), end - 1);
+        const uint32_t own_e = min(e0 + (tx & (U - 1)), end - 1);
         const uint32_t own_key = keys[own_e], own_pos = pos[own_e];
         uint32_t k[U];
-        Entry<T, VEC, TX> raw[U];
+        Raw8<T, VEC> raw[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            k[u] = __shfl_sync(group, own_key, u, 8);
-            const uint32_t at = __shfl_sync(group, own_pos, u, 8);
-            if (e0 + u < end && k[u] < p.vocab) raw[u].load(dout + (int64_t)at * p.ldo, c0, tx, p.d);
+            k[u] = __shfl_sync(group, own_key, u, U);
+            const uint32_t at = __shfl_sync(group, own_pos, u, U);
+            if (e0 + u < end && k[u] < p.vocab && (!VEC || c < p.d)) raw[u].load(dout + (int64_t)at * p.ldo, c, p.d, span);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -319,13 +309,13 @@ __device__ __forceinline__ void sum_tile(const SumParams& p, uint32_t node, uint
                     cur = k[u];
                     from_before = false;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+                    for (int j = 0; j < 4; ++j) acc[j] = both(0.f);
                 }
-                if (cur < p.vocab) {
-                    float v[8];
+                if (cur < p.vocab && c < p.d) {
+                    f32x2_t v[4];
                     raw[u].get(v);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) acc[j] += v[j];
+                    for (int j = 0; j < 4; ++j) acc[j] = add2(acc[j], v[j]);
                 }
             }
         }
@@ -471,20 +461,32 @@ cudaError_t sums_of(const SumParams& p, uint32_t nodes, cudaStream_t s)
 
 bool aligned(const void* p, int64_t ld, int size) { return (((uintptr_t)p) & 15u) == 0 && (ld * size) % 16 == 0; }
 
-template <class T>
-cudaError_t lookup_of(const LookupParams& p, cudaStream_t s)
+template <class T, bool VEC, int TPR, int NC>
+cudaError_t lookup_as(LookupParams& p, cudaStream_t s)
 {
-    const uint64_t total = (uint64_t)p.nodes * p.rows * ((p.d + kChunk - 1) / kChunk);
-    if (!total) return cudaSuccess;
-    const unsigned grid = (unsigned)((total + 255) / 256);
-    const bool full = p.d % 8 == 0;
-    const bool tvec = full && aligned(p.table, p.ldt, 4) && p.node_ldt % 4 == 0;
-    const bool ovec = full && aligned(p.out, p.ldo, sizeof(T));
-    if (tvec && ovec) lookup_kernel<T, true, true><<<grid, 256, 0, s>>>(p);
-    else if (tvec) lookup_kernel<T, true, false><<<grid, 256, 0, s>>>(p);
-    else if (ovec) lookup_kernel<T, false, true><<<grid, 256, 0, s>>>(p);
-    else lookup_kernel<T, false, false><<<grid, 256, 0, s>>>(p);
+    p.stretches = make_divisor((p.chunks.d + NC * TPR - 1) / (NC * TPR));
+    const uint64_t groups = (uint64_t)p.rows * p.stretches.d;
+    lookup_kernel<T, VEC, TPR, NC><<<dim3((unsigned)((groups + 256 / TPR - 1) / (256 / TPR)), p.nodes), 256, 0, s>>>(p);
     return cudaGetLastError();
+}
+
+template <class T, bool VEC>
+cudaError_t lookup_by_width(LookupParams& p, cudaStream_t s)
+{
+    const uint32_t chunks = p.chunks.d;
+    return chunks <= 8    ? lookup_as<T, VEC, 8, 1>(p, s)
+           : chunks <= 32 ? lookup_as<T, VEC, 32, 1>(p, s)
+           : chunks <= 64 ? lookup_as<T, VEC, 32, 2>(p, s)
+                          : lookup_as<T, VEC, 32, 4>(p, s);
+}
+
+template <class T>
+cudaError_t lookup_of(LookupParams p, cudaStream_t s)
+{
+    if (!p.rows) return cudaSuccess;
+    p.chunks = make_divisor((uint32_t)(p.d + kChunk - 1) / kChunk);
+    const bool vec = p.d % kChunk == 0 && aligned(p.table, p.ldt, 4) && p.node_ldt % 4 == 0 && aligned(p.out, p.ldo, sizeof(T));
+    return vec ? lookup_by_width<T, true>(p, s) : lookup_by_width<T, false>(p, s);
 }
 
 }  // namespace

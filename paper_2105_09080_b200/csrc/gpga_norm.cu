@@ -9,134 +9,360 @@ namespace {
 
 constexpr int kSMs = 148;
 
-// ---- sums over the TPR threads of a row -------------------------------------------------------------
-// TPR <= 32: lanes of one warp (the other groups of the warp may have left).  Wider: the whole block, through
-// shared memory; `part` holds 32 floats per call site and round, so that one barrier per sum is enough.
-template <int TPR>
-__device__ __forceinline__ float row_sum(float v, float* part)
+// Chunk c of a thread.  A group of at most 32 threads takes neighbouring chunks call by call; in wider groups every
+// warp has NC * 32 neighbouring chunks, so that only its two ends meet other warps' columns.
+template <int TPR, int NC>
+__device__ __forceinline__ uint32_t chunk_of(int c)
 {
-    if constexpr (TPR <= 32) {
-        const unsigned mask = TPR == 32 ? 0xFFFFFFFFu : ((1u << (TPR & 31)) - 1u) << ((threadIdx.x & 31) / TPR * TPR);
+    if (TPR <= 32) return threadIdx.x % TPR + c * TPR;
+    return (threadIdx.x % TPR / 32 * NC + c) * 32 + threadIdx.x % 32;
+}
+// First chunk of the lanes that share a store with this thread, for its chunk c.
+template <int TPR, int NC>
+__device__ __forceinline__ uint32_t first_chunk_of(int c)
+{
+    return TPR <= 32 ? c * TPR : (threadIdx.x % TPR / 32 * NC + c) * 32;
+}
+__host__ __device__ constexpr int lanes_of(int tpr) { return tpr < 32 ? tpr : 32; }
+
+
+// Sums of M values over the TPR threads of a group; every thread gets them all.  In a warp, M values take M - 1
+// shuffles to halve down to one per lane (a lane gives away the half it does not keep), the remaining steps on that
+// one, and M to hand the sums round: 17 for M = 8 instead of 40.  Wider groups go on through shared memory: one
+// barrier; `part` ([warps][M], on 16 bytes) may be used again by the next call but one.
+template <int TPR, int M>
+__device__ __forceinline__ void group_sums(float* v, float* part)
+{
+    constexpr int L = lanes_of(TPR);
+    const unsigned mask = group_mask<TPR>();
+    const int lane = threadIdx.x % L;
+    int o = L / 2;
 #pragma unroll
-        for (int o = TPR / 2; o > 0; o >>= 1) v += __shfl_xor_sync(mask, v, o);
-        return v;
-    } else {
-        v = warp_sum_f(v);
-        if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+    for (int m = M / 2; m >= 1; m /= 2, o /= 2) {
+        const bool upper = lane & o;
+#pragma unroll
+        for (int i = 0; i < m; ++i) {
+            const float give = upper ? v[i] : v[i + m], keep = upper ? v[i + m] : v[i];
+            v[i] = keep + __shfl_xor_sync(mask, give, o);
+        }
+    }
+#pragma unroll
+    for (; o >= 1; o /= 2) v[0] += __shfl_xor_sync(mask, v[0], o);
+    // lane l now has value l / (L / M)
+    if constexpr (TPR > 32) {
+        const int warp = threadIdx.x / 32;
+        if (lane % (L / M) == 0) part[warp * M + lane / (L / M)] = v[0];
         __syncthreads();
-        float s = 0.f;
+        const int w0 = threadIdx.x / TPR * (TPR / 32);
+        if constexpr (M >= 4) {
+            f32x2_t sum[M / 2];
 #pragma unroll
-        for (int w = 0; w < TPR / 32; ++w) s += part[w];
-        return s;
+            for (int w = 0; w < TPR / 32; ++w)
+#pragma unroll
+                for (int i = 0; i < M / 4; ++i) {
+                    const float4 q = reinterpret_cast<const float4*>(part)[(w0 + w) * (M / 4) + i];
+                    sum[2 * i] = w ? add2(sum[2 * i], pack2(q.x, q.y)) : pack2(q.x, q.y);
+                    sum[2 * i + 1] = w ? add2(sum[2 * i + 1], pack2(q.z, q.w)) : pack2(q.z, q.w);
+                }
+#pragma unroll
+            for (int i = 0; i < M; ++i) v[i] = element(sum, i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < M; ++i) v[i] = 0.f;
+#pragma unroll
+            for (int w = 0; w < TPR / 32; ++w)
+#pragma unroll
+                for (int i = 0; i < M; ++i) v[i] += part[(w0 + w) * M + i];
+        }
+    } else if constexpr (M > 1) {
+        const float mine = v[0];
+#pragma unroll
+        for (int i = 0; i < M; ++i) v[i] = __shfl_sync(mask, mine, i * (L / M), L);
     }
 }
 
 // ---- dropout ----------------------------------------------------------------------------------------
-template <class T, bool VEC>
-__global__ void __launch_bounds__(256) dropout_kernel(const DropoutParams p)
+// Both tensors dense and aligned: U chunks per thread, 256 apart, their loads in flight together.
+template <class T, int U>
+__global__ void __launch_bounds__(256) dropout_dense_kernel(const DropoutParams p)
 {
-    const uint32_t chunks = (uint32_t)(p.d + kChunk - 1) / kChunk;
-    const uint64_t total = (uint64_t)p.nodes * p.rows * chunks;
-    const uint64_t g = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-    if (g >= total) return;
-    const uint32_t row = (uint32_t)(g / chunks), chunk = (uint32_t)(g - (uint64_t)row * chunks);
-    const uint32_t node = row / p.rows, t = row - node * p.rows;
-    const int col = (int)chunk * kChunk;
-    Raw8<T, VEC> raw;
-    float v[8];
-    raw.load(static_cast<const T*>(p.x) + (int64_t)row * p.ldx, col, p.d);
-    raw.get(v);
-    drop8(p.mask, t, node, chunks, chunk, v);
-    store8<T, VEC>(static_cast<T*>(p.y) + (int64_t)row * p.ldy, col, p.d, v);
+    const uint32_t node = blockIdx.y, total = p.rows * p.chunks.d;
+    const T* x = static_cast<const T*>(p.x) + (int64_t)node * total * kChunk;
+    T* y = static_cast<T*>(p.y) + (int64_t)node * total * kChunk;
+    const uint32_t f0 = blockIdx.x * (256 * U) + threadIdx.x;   // the host keeps total + 256 U below 2^32
+    Raw8<T, true> raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (f0 + u * 256 < total) raw[u].load(x + (int64_t)f0 * kChunk, u * 256 * kChunk, p.d, Span());
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (f0 + u * 256 >= total) return;
+        f32x2_t v[4];
+        raw[u].get(v);
+        drop8(p.mask, f0 + u * 256, node, v);
+        store8<T>(y + (int64_t)f0 * kChunk + u * 256 * kChunk, v);
+    }
+}
+
+// Otherwise TPR lanes take a stretch of NC * TPR chunks of one row.
+template <class T, bool VEC, int TPR, int NC>
+__global__ void __launch_bounds__(256) dropout_rows_kernel(const DropoutParams p)
+{
+    const uint32_t node = blockIdx.y, chunks = p.chunks.d;
+    const uint32_t g = blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+    const uint32_t t = divide(g, p.stretches);
+    if (t >= p.rows) return;
+    const uint32_t first = (g - t * p.stretches.d) * (NC * TPR);
+    const int lane = threadIdx.x % TPR;
+    const int64_t row = (int64_t)node * p.rows + t;
+    const T* x = static_cast<const T*>(p.x) + row * p.ldx;
+    T* y = static_cast<T*>(p.y) + row * p.ldy;
+    const Span span = span_of<T>(p.x, p.ldx, (int64_t)p.nodes * p.rows, p.d);
+    Raw8<T, VEC> raw[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+        if (!VEC || first + c * TPR + lane < chunks) raw[c].load(x, (int)(first + c * TPR + lane) * kChunk, p.d, span);
+    RowStore<T, VEC, TPR> store;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        const uint32_t base = first + c * TPR, chunk = base + lane;
+        if (base >= chunks) break;
+        f32x2_t v[4];
+        if (!VEC || chunk < chunks) {
+            raw[c].get(v);
+            drop8(p.mask, t * chunks + chunk, node, v);
+        }
+        store.store(y, (int)chunk * kChunk, p.d, v, lane, group_mask<TPR>(), c + 1 == NC || base + TPR >= chunks);
+    }
 }
 
 // ---- layer norm, forward ----------------------------------------------------------------------------
-// z = residual + dropout(x) of one chunk in fp32.
-template <class T, bool VEC>
-__device__ __forceinline__ void mix8(const NormForwardParams& p, const Raw8<T, VEC>& rx, const Raw8<T, VEC>& rr, uint32_t t,
-                                     uint32_t node, uint32_t chunks, uint32_t chunk, float* v)
+// (z - mean) rstd w + b
+__device__ __forceinline__ void scale8(const f32x2_t* v, float mean, float rstd, const f32x2_t* w, const f32x2_t* b, f32x2_t* y)
 {
-    rx.get(v);
-    if (p.mask.threshold) drop8(p.mask, t, node, chunks, chunk, v);
-    if (p.residual) {
-        float r[8];
-        rr.get(r);
+    const f32x2_t m = both(mean), s = both(rstd);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += r[j];
+    for (int j = 0; j < 4; ++j) y[j] = fma2(mul2(sub2(v[j], m), s), w[j], b[j]);
+}
+
+__device__ __forceinline__ f32x2_t sum4(const f32x2_t* v) { return add2(add2(v[0], v[1]), add2(v[2], v[3])); }
+
+// Sum of (v - mean)^2 over the first n of eight columns.
+__device__ __forceinline__ f32x2_t squares8(const f32x2_t* v, float mean, int n)
+{
+    const f32x2_t m = both(mean);
+    f32x2_t e[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) e[j] = sub2(v[j], m);
+    keep_first(e, n);
+    f32x2_t s = mul2(e[0], e[0]);
+#pragma unroll
+    for (int j = 1; j < 4; ++j) s = fma2(e[j], e[j], s);
+    return s;
+}
+
+// s / n for a row's mean: one multiplication by fl(1 / n), corrected by the exact remainder.  (A constant row's mean is
+// exact this way, as by a division, which takes several times the instructions.)
+__device__ __forceinline__ float mean_of(float s, float n, float inv_n)
+{
+    const float m = s * inv_n;
+    const float fixed = fmaf(fmaf(-m, n, s), inv_n, m);
+    return fabsf(fixed) <= 3.4e38f ? fixed : m;   // an infinite sum has no remainder
+}
+
+// Statistics of R rows that a group of TPR threads holds in registers (columns and rows that are not there: zero).  The
+// variance is a second pass over the registers, so that nothing cancels.  FULL: every chunk is there.
+template <bool FULL, bool VEC, int TPR, int NC, int R>
+__device__ __forceinline__ void row_statistics(const f32x2_t (*v)[NC][4], int d, float eps, float* part, float* mean, float* rstd)
+{
+    const float n = (float)d, inv_n = 1.f / n;
+    float s[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        f32x2_t sum = sum4(v[r][0]);
+#pragma unroll
+        for (int c = 1; c < NC; ++c) sum = add2(sum, sum4(v[r][c]));
+        s[r] = sum2(sum);
     }
+    group_sums<TPR, R>(s, part);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        mean[r] = mean_of(s[r], n, inv_n);
+        f32x2_t sum = both(0.f);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int col = chunk_of<TPR, NC>(c) * kChunk;
+            if (FULL || col < d) sum = add2(sum, squares8(v[r][c], mean[r], VEC ? 8 : d - col));
+        }
+        s[r] = sum2(sum);
+    }
+    group_sums<TPR, R>(s, part + 32 * R);
+#pragma unroll
+    for (int r = 0; r < R; ++r) rstd[r] = rsqrtf(fmaf(s[r], inv_n, eps));   // within 2 ulp
 }
 
-template <class T, bool VEC>
-__device__ __forceinline__ void norm_store8(const NormForwardParams& p, int64_t row, uint32_t node, int col, const float* v,
-                                            float mean, float rstd)
+// z = residual + dropout(x) of R rows from row t of a node on, in fp32; zero where there is no row or chunk.  The
+// branches are the same for the whole launch and stand outside the loops.
+template <class T, bool FULL, bool VEC, int TPR, int NC, int R>
+__device__ __forceinline__ void load_mixed(const NormForwardParams& p, uint32_t node, uint32_t t, f32x2_t (*v)[NC][4])
 {
-    float w[8], b[8], y[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) w[j] = 1.f, b[j] = 0.f;
-    if (p.weight) param8(p.weight + node * p.ldw, col, p.d, p.wvec, w);
-    if (p.bias) param8(p.bias + node * p.ldw, col, p.d, p.wvec, b);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = fmaf((v[j] - mean) * rstd, w[j], b[j]);
-    if (p.z) store8<T, VEC>(static_cast<T*>(p.z) + row * p.ldz, col, p.d, v);
-    store8<T, VEC>(static_cast<T*>(p.y) + row * p.ldy, col, p.d, y);
-}
-
-// TPR threads per row, NC chunks of eight columns per thread: the row stays in registers between the mean,
-// the variance (a second pass over the registers, so no cancellation) and the output.
-template <class T, bool VEC, int TPR, int NC>
-__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) norm_forward_kernel(const NormForwardParams p)
-{
-    constexpr int BLOCK = TPR < 128 ? 128 : TPR, RPB = BLOCK / TPR;
-    __shared__ float part[2][32];
-    const int lane = threadIdx.x % TPR;
-    const uint32_t row = blockIdx.x * RPB + threadIdx.x / TPR;
-    if (row >= p.nodes * p.rows) return;   // whole groups only; with TPR > 32 a block is one row
-    const uint32_t node = row / p.rows, t = row - node * p.rows;
     const uint32_t chunks = (uint32_t)(p.d + kChunk - 1) / kChunk;
-    const T* x = static_cast<const T*>(p.x) + (int64_t)row * p.ldx;
-    const T* r = static_cast<const T*>(p.residual) + (p.residual ? (int64_t)row * p.ldr : 0);
-    Raw8<T, VEC> rx[NC], rr[NC];
+    const int64_t all = (int64_t)p.nodes * p.rows, row0 = (int64_t)node * p.rows + t;
+    const Span sx = span_of<T>(p.x, p.ldx, all, p.d), sr = span_of<T>(p.residual, p.ldr, all, p.d);
+    Raw8<T, VEC> rx[R][NC], rr[R][NC];
+    const T* x = static_cast<const T*>(p.x) + row0 * p.ldx;
+    const T* res = static_cast<const T*>(p.residual) + (p.residual ? row0 * p.ldr : 0);
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-        const uint32_t chunk = lane + c * TPR;
-        if (chunk < chunks) {
-            rx[c].load(x, chunk * kChunk, p.d);
-            if (p.residual) rr[c].load(r, chunk * kChunk, p.d);
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+            if (FULL || (t + r < p.rows && chunk_of<TPR, NC>(c) < chunks)) rx[r][c].load(x + r * p.ldx, chunk_of<TPR, NC>(c) * kChunk, p.d, sx);
+    if (p.residual)
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                if (FULL || (t + r < p.rows && chunk_of<TPR, NC>(c) < chunks))
+                    rr[r][c].load(res + r * p.ldr, chunk_of<TPR, NC>(c) * kChunk, p.d, sr);
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            if (FULL || (t + r < p.rows && chunk_of<TPR, NC>(c) < chunks)) rx[r][c].get(v[r][c]);
+            else
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[r][c][j] = both(0.f);
         }
+    if (p.mask.on)
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) drop8(p.mask, (t + r) * chunks + chunk_of<TPR, NC>(c), node, v[r][c]);
+    if (p.residual)
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                if (FULL || (t + r < p.rows && chunk_of<TPR, NC>(c) < chunks)) {
+                    f32x2_t e[4];
+                    rr[r][c].get(e);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[r][c][j] = add2(v[r][c][j], e[j]);
+                }
+}
+
+// Everything aligned, weight and bias there: a group of TPR threads takes R rows, NC chunks of eight columns per
+// thread, all loads first.  FULL: the block's rows and every thread's chunks are all there, nothing is tested.
+template <class T, bool FULL, int TPR, int NC, int R>
+__device__ __forceinline__ void norm_forward(const NormForwardParams& p, float* part)
+{
+    constexpr int G = (TPR < 128 ? 128 : TPR) / TPR;
+    const uint32_t node = blockIdx.y, chunks = (uint32_t)p.d / kChunk;
+    const uint32_t t = (blockIdx.x * G + threadIdx.x / TPR) * R;
+    const int64_t row0 = (int64_t)node * p.rows + t;
+    f32x2_t v[R][NC][4];
+    load_mixed<T, FULL, true, TPR, NC, R>(p, node, t, v);
+    float mean[R], rstd[R];
+    row_statistics<FULL, true, TPR, NC, R>(v, p.d, p.eps, part, mean, rstd);
+    if (threadIdx.x % TPR == 0)
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (FULL || t + r < p.rows) {
+                p.mean[row0 + r] = mean[r];
+                p.rstd[row0 + r] = rstd[r];
+            }
+    if (p.z) {
+        T* z = static_cast<T*>(p.z) + row0 * p.ldz;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                if (FULL || (t + r < p.rows && chunk_of<TPR, NC>(c) < chunks)) store8<T>(z + r * p.ldz + chunk_of<TPR, NC>(c) * kChunk, v[r][c]);
     }
-    float v[NC][8];
-    float sum = 0.f;
+    T* y = static_cast<T*>(p.y) + row0 * p.ldy;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        const uint32_t chunk = lane + c * TPR;
-        if (chunk < chunks) {
-            mix8<T, VEC>(p, rx[c], rr[c], t, node, chunks, chunk, v[c]);
+        const uint32_t chunk = chunk_of<TPR, NC>(c);
+        if (!FULL && chunk >= chunks) continue;
+        f32x2_t w[4], b[4];
+        param8(p.weight + node * p.ldw, chunk * kChunk, p.d, true, w);
+        param8(p.bias + node * p.ldw, chunk * kChunk, p.d, true, b);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum += v[c][j];   // columns from d on are zero
-        }
-    }
-    const float mean = row_sum<TPR>(sum, part[0]) / (float)p.d;
-    float sq = 0.f;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-        const int col = (lane + c * TPR) * kChunk;
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (VEC ? col < p.d : col + j < p.d) {
-                const float e = v[c][j] - mean;
-                sq = fmaf(e, e, sq);
+        for (int r = 0; r < R; ++r)
+            if (FULL || t + r < p.rows) {
+                f32x2_t out[4];
+                scale8(v[r][c], mean[r], rstd[r], w, b, out);
+                store8<T>(y + r * p.ldy + chunk * kChunk, out);
             }
     }
-    const float var = row_sum<TPR>(sq, part[1]) / (float)p.d;
-    const float rstd = 1.f / sqrtf(var + p.eps);
-    if (lane == 0) {
-        p.mean[row] = mean;
-        p.rstd[row] = rstd;
+}
+
+template <class T, int TPR, int NC, int R>
+__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) norm_forward_kernel(const NormForwardParams p)
+{
+    constexpr int G = (TPR < 128 ? 128 : TPR) / TPR;
+    __shared__ __align__(16) float part[2 * 32 * R];
+    if (p.d == TPR * NC * kChunk && (blockIdx.x + 1) * (G * R) <= p.rows) norm_forward<T, true, TPR, NC, R>(p, part);
+    else norm_forward<T, false, TPR, NC, R>(p, part);
+}
+
+// Otherwise: the same per row, by blocks that take every gridDim.x-th set of rows of one node.  The node's weight and
+// bias (one and zero where there is none), which might have to be cut as well, are laid out in shared memory once per
+// block, each chunk's two halves in planes of their own (no bank conflicts).
+template <class T, bool VEC, int TPR, int NC, int R>
+__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, 512 / (TPR < 128 ? 128 : TPR)) norm_forward_odd_kernel(const NormForwardParams p)
+{
+    constexpr int BLOCK = TPR < 128 ? 128 : TPR, G = BLOCK / TPR, LANES = lanes_of(TPR);
+    extern __shared__ float4 params[];   // weight, bias: two planes of `chunks` each
+    __shared__ __align__(16) float part[2 * 32 * R];
+    const int lane = threadIdx.x % LANES;
+    const uint32_t node = blockIdx.y;
+    const uint32_t chunks = (uint32_t)(p.d + kChunk - 1) / kChunk;
+    for (uint32_t col = threadIdx.x; col < chunks * kChunk; col += BLOCK) {
+        const bool in = col < (uint32_t)p.d;
+        float* at = reinterpret_cast<float*>(params + (col >> 2 & 1) * chunks + (col >> 3)) + (col & 3);
+        at[0] = !in ? 0.f : p.weight ? p.weight[node * p.ldw + col] : 1.f;
+        at[8 * chunks] = in && p.bias ? p.bias[node * p.ldw + col] : 0.f;
     }
+    __syncthreads();
+    // all groups of a block go round equally often (barriers inside)
+    for (uint32_t t0 = blockIdx.x * (G * R); t0 < p.rows; t0 += gridDim.x * (G * R)) {
+        const uint32_t t = t0 + threadIdx.x / TPR * R;
+        const int64_t row0 = (int64_t)node * p.rows + t;
+        f32x2_t v[R][NC][4];
+        load_mixed<T, false, VEC, TPR, NC, R>(p, node, t, v);
+        float mean[R], rstd[R];
+        row_statistics<false, VEC, TPR, NC, R>(v, p.d, p.eps, part, mean, rstd);
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-        const uint32_t chunk = lane + c * TPR;
-        if (chunk < chunks) norm_store8<T, VEC>(p, row, node, chunk * kChunk, v[c], mean, rstd);
+        for (int r = 0; r < R; ++r) {
+            if (t + r >= p.rows) continue;
+            if (threadIdx.x % TPR == 0) {
+                p.mean[row0 + r] = mean[r];
+                p.rstd[row0 + r] = rstd[r];
+            }
+            T* y = static_cast<T*>(p.y) + (row0 + r) * p.ldy;
+            T* z = static_cast<T*>(p.z) + (p.z ? (row0 + r) * p.ldz : 0);
+            RowStore<T, VEC, LANES> to_y, to_z;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const uint32_t first = first_chunk_of<TPR, NC>(c), chunk = chunk_of<TPR, NC>(c);
+                if (first >= chunks) break;
+                const bool last = c + 1 == NC || first + LANES >= chunks;
+                if (p.z) to_z.store(z, chunk * kChunk, p.d, v[r][c], lane, group_mask<TPR>(), last);
+                f32x2_t out[4];
+                if (chunk < chunks) {
+                    f32x2_t w[4], b[4];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const float4 qw = params[h * chunks + chunk], qb = params[(2 + h) * chunks + chunk];
+                        w[2 * h] = pack2(qw.x, qw.y); w[2 * h + 1] = pack2(qw.z, qw.w);
+                        b[2 * h] = pack2(qb.x, qb.y); b[2 * h + 1] = pack2(qb.z, qb.w);
+                    }
+                    scale8(v[r][c], mean[r], rstd[r], w, b, out);
+                }
+                to_y.store(y, chunk * kChunk, p.d, out, lane, group_mask<TPR>(), last);
+            }
+        }
     }
 }
 
@@ -144,153 +370,200 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) norm_forward_kernel(con
 template <class T, bool VEC>
 __global__ void __launch_bounds__(1024) norm_forward_wide_kernel(const NormForwardParams p)
 {
-    __shared__ float part[2][32];
+    __shared__ __align__(16) float part[2][32];
     const uint32_t row = blockIdx.x;
     const uint32_t node = row / p.rows, t = row - node * p.rows;
     const uint32_t chunks = (uint32_t)(p.d + kChunk - 1) / kChunk;
     const T* x = static_cast<const T*>(p.x) + (int64_t)row * p.ldx;
     const T* r = static_cast<const T*>(p.residual) + (p.residual ? (int64_t)row * p.ldr : 0);
-    auto chunk_of = [&](uint32_t chunk, float* v) {
+    const int64_t all = (int64_t)p.nodes * p.rows;
+    const Span sx = span_of<T>(p.x, p.ldx, all, p.d), sr = span_of<T>(p.residual, p.ldr, all, p.d);
+    auto chunk_at = [&](uint32_t chunk, f32x2_t* v) {
         Raw8<T, VEC> rx, rr;
-        rx.load(x, chunk * kChunk, p.d);
-        if (p.residual) rr.load(r, chunk * kChunk, p.d);
-        mix8<T, VEC>(p, rx, rr, t, node, chunks, chunk, v);
+        rx.load(x, chunk * kChunk, p.d, sx);
+        if (p.residual) rr.load(r, chunk * kChunk, p.d, sr);
+        rx.get(v);
+        drop8(p.mask, t * chunks + chunk, node, v);
+        if (p.residual) {
+            f32x2_t e[4];
+            rr.get(e);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = add2(v[j], e[j]);
+        }
     };
-    float v[8];
-    float sum = 0.f;
+    f32x2_t v[4];
+    float sum[1] = {0.f};
     for (uint32_t chunk = threadIdx.x; chunk < chunks; chunk += 1024) {
-        chunk_of(chunk, v);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum += v[j];
+        chunk_at(chunk, v);
+        sum[0] += sum2(sum4(v));
     }
-    const float mean = row_sum<1024>(sum, part[0]) / (float)p.d;
-    float sq = 0.f;
+    group_sums<1024, 1>(sum, part[0]);
+    const float mean = mean_of(sum[0], (float)p.d, 1.f / (float)p.d);
+    float sq[1] = {0.f};
     for (uint32_t chunk = threadIdx.x; chunk < chunks; chunk += 1024) {
-        chunk_of(chunk, v);
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if ((int)chunk * kChunk + j < p.d) sq = fmaf(v[j] - mean, v[j] - mean, sq);
+        chunk_at(chunk, v);
+        sq[0] += sum2(squares8(v, mean, VEC ? 8 : p.d - (int)chunk * kChunk));
     }
-    const float rstd = 1.f / sqrtf(row_sum<1024>(sq, part[1]) / (float)p.d + p.eps);
+    group_sums<1024, 1>(sq, part[1]);
+    const float rstd = rsqrtf(sq[0] / (float)p.d + p.eps);   // within 2 ulp
     if (threadIdx.x == 0) {
         p.mean[row] = mean;
         p.rstd[row] = rstd;
     }
-    for (uint32_t chunk = threadIdx.x; chunk < chunks; chunk += 1024) {
-        chunk_of(chunk, v);
-        norm_store8<T, VEC>(p, row, node, chunk * kChunk, v, mean, rstd);
+    T* y = static_cast<T*>(p.y) + (int64_t)row * p.ldy;
+    T* z = static_cast<T*>(p.z) + (p.z ? (int64_t)row * p.ldz : 0);
+    const int lane = threadIdx.x & 31;
+    for (uint32_t first = threadIdx.x - lane; first < chunks; first += 1024) {
+        const uint32_t chunk = first + lane;
+        f32x2_t out[4];
+        if (chunk < chunks) {
+            f32x2_t w[4], b[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = both(1.f), b[j] = both(0.f);
+            if (p.weight) param8(p.weight + node * p.ldw, chunk * kChunk, p.d, p.wvec, w);
+            if (p.bias) param8(p.bias + node * p.ldw, chunk * kChunk, p.d, p.wvec, b);
+            chunk_at(chunk, v);
+            scale8(v, mean, rstd, w, b, out);
+        }
+        RowStore<T, VEC, 32> to_y, to_z;
+        if (p.z) to_z.store(z, chunk * kChunk, p.d, v, lane, 0xFFFFFFFFu, true);
+        to_y.store(y, chunk * kChunk, p.d, out, lane, 0xFFFFFFFFu, true);
     }
 }
 
 // ---- layer norm, backward ---------------------------------------------------------------------------
-// g = rstd (h - mean(h) - xh mean(h xh)) + dz of one chunk, h = w dy and xh = (z - mean) rstd given.
-template <class T, bool VEC>
-__device__ __forceinline__ void grad_store8(const NormBackwardParams& p, int64_t row, uint32_t t, uint32_t node, uint32_t chunks,
-                                            uint32_t chunk, const float* h, const float* xh, float rstd, float mh, float mhx)
+// g = rstd (w dy - mean(h) - xh mean(h xh)) of one chunk, xh = (z - mean) rstd.
+__device__ __forceinline__ void grad8(const f32x2_t* z, const f32x2_t* dy, const f32x2_t* w, float mean, float rstd, float mh, float mhx,
+                                      f32x2_t* g)
 {
-    const int col = chunk * kChunk;
-    float g[8];
+    const f32x2_t m = both(mean), s = both(rstd), a = both(-mh), c = both(-mhx);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) g[j] = rstd * (h[j] - mh - xh[j] * mhx);
-    if (p.dz) {
-        Raw8<T, VEC> raw;
-        float e[8];
-        raw.load(static_cast<const T*>(p.dz) + row * p.lddz, col, p.d);
-        raw.get(e);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) g[j] += e[j];
-    }
-    store8<T, VEC>(static_cast<T*>(p.dres) + row * p.lddres, col, p.d, g);
-    if (p.dx) {
-        drop8(p.mask, t, node, chunks, chunk, g);
-        store8<T, VEC>(static_cast<T*>(p.dx) + row * p.lddx, col, p.d, g);
-    }
+    for (int j = 0; j < 4; ++j) g[j] = mul2(s, fma2(mul2(sub2(z[j], m), s), c, fma2(dy[j], w[j], a)));
 }
 
-// A block takes every splits-th group of rows of one node; each thread keeps the column sums of its chunks
-// (dw += dy xh, db += dy) in registers and the block leaves one pair of rows of partial sums.
-template <class T, bool VEC, int TPR, int NC>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_backward_kernel(const NormBackwardParams p)
+// A block takes every splits-th set of rows of one node, R rows per group of TPR threads at a time: their loads are
+// in flight together and their 2 R row sums share the shuffles and the barrier.  Each thread has the same NC chunks of
+// columns in every row and so keeps the column sums (dw += dy xh, db += dy) in registers; the block leaves one pair of
+// rows of partial sums.
+template <class T, bool VEC, int TPR, int NC, int R>
+__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 512 ? 512 / (TPR < 128 ? 128 : TPR) : 1)
+norm_backward_kernel(const NormBackwardParams p)
 {
-    constexpr int BLOCK = TPR < 256 ? 256 : TPR, RPB = BLOCK / TPR;
-    __shared__ float part[2][RPB > 1 ? RPB : 1][32];
-    extern __shared__ float sums[];   // 2 x d, only when RPB > 1
-    const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+    constexpr int BLOCK = TPR < 128 ? 128 : TPR, G = BLOCK / TPR, LANES = lanes_of(TPR);
+    __shared__ __align__(16) float part[2][BLOCK / 32 * 2 * R];
+    __shared__ float sums[G > 1 ? 2 * TPR * NC * 8 : 1];
+    const int sub = threadIdx.x / TPR, lane = threadIdx.x % LANES;
     const uint32_t node = blockIdx.y;
     const uint32_t chunks = (uint32_t)(p.d + kChunk - 1) / kChunk;
-    float dw[NC][8], db[NC][8];
+    const int64_t all = (int64_t)p.nodes * p.rows, row0 = (int64_t)node * p.rows;
+    const Span sz = span_of<T>(p.z, p.ldz, all, p.d), sy = span_of<T>(p.dy, p.lddy, all, p.d), se = span_of<T>(p.dz, p.lddz, all, p.d);
+    f32x2_t w[NC][4], dw[NC][4], db[NC][4];
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
+    for (int c = 0; c < NC; ++c) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) dw[c][j] = db[c][j] = 0.f;
-
-    for (uint32_t t0 = blockIdx.x * RPB; t0 < p.rows; t0 += gridDim.x * RPB) {
-        const uint32_t t = t0 + sub;
-        const bool live = t < p.rows;
-        const int64_t row = (int64_t)node * p.rows + t;
-        if (TPR <= 32 && !live) continue;
-        Raw8<T, VEC> rz[NC], rdy[NC];
+        for (int j = 0; j < 4; ++j) dw[c][j] = db[c][j] = both(0.f), w[c][j] = both(1.f);
+        const uint32_t chunk = chunk_of<TPR, NC>(c);
+        if (p.weight && chunk < chunks) param8(p.weight + node * p.ldw, chunk * kChunk, p.d, p.wvec, w[c]);
+    }
+    const float inv_d = 1.f / (float)p.d;
+    int buf = 0;
+    for (uint32_t t0 = blockIdx.x * (G * R); t0 < p.rows; t0 += gridDim.x * (G * R), buf ^= 1) {
+        const uint32_t t = t0 + sub * R;
+        const int64_t row = row0 + t;
+        Raw8<T, VEC> rz[R][NC], ry[R][NC], re[R][NC];
+        float mean[R], rstd[R];
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const uint32_t chunk = lane + c * TPR;
-            if (chunk < chunks) {
-                rz[c].load(static_cast<const T*>(p.z) + row * p.ldz, chunk * kChunk, p.d);
-                rdy[c].load(static_cast<const T*>(p.dy) + row * p.lddy, chunk * kChunk, p.d);
-            }
-        }
-        const float mean = p.mean[row], rstd = p.rstd[row];
-        float s1 = 0.f, s2 = 0.f;
-        float xh[NC][8], h[NC][8];
+        for (int r = 0; r < R; ++r) {
+            mean[r] = rstd[r] = 0.f;
+            if (t + r >= p.rows) continue;
+            mean[r] = p.mean[row + r];
+            rstd[r] = p.rstd[row + r];
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const uint32_t chunk = lane + c * TPR;
-            if (chunk < chunks) {
-                float w[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) w[j] = 1.f;
-                if (p.weight) param8(p.weight + node * p.ldw, chunk * kChunk, p.d, p.wvec, w);
-                rz[c].get(xh[c]);
-                rdy[c].get(h[c]);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    // columns from d on have dy = 0 and so add nothing anywhere
-                    xh[c][j] = (xh[c][j] - mean) * rstd;
-                    db[c][j] += h[c][j];
-                    dw[c][j] = fmaf(h[c][j], xh[c][j], dw[c][j]);
-                    h[c][j] *= w[j];
-                    s1 += h[c][j];
-                    s2 = fmaf(h[c][j], xh[c][j], s2);
+            for (int c = 0; c < NC; ++c) {
+                const uint32_t chunk = chunk_of<TPR, NC>(c);
+                if (!VEC || chunk < chunks) {
+                    rz[r][c].load(static_cast<const T*>(p.z) + (row + r) * p.ldz, chunk * kChunk, p.d, sz);
+                    ry[r][c].load(static_cast<const T*>(p.dy) + (row + r) * p.lddy, chunk * kChunk, p.d, sy);
+                    if (p.dz) re[r][c].load(static_cast<const T*>(p.dz) + (row + r) * p.lddz, chunk * kChunk, p.d, se);
                 }
             }
         }
-        const float mh = row_sum<TPR>(s1, part[0][0]) / (float)p.d;
-        const float mhx = row_sum<TPR>(s2, part[1][0]) / (float)p.d;
-        if (TPR > 32) __syncthreads();   // part is reused by the next row
+        float s[2 * R];
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const uint32_t chunk = lane + c * TPR;
-            if (chunk < chunks) grad_store8<T, VEC>(p, row, t, node, chunks, chunk, h[c], xh[c], rstd, mh, mhx);
+        for (int r = 0; r < R; ++r) {
+            f32x2_t s1 = both(0.f), s2 = both(0.f);
+            const f32x2_t m = both(mean[r]), q = both(rstd[r]);
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                if (chunk_of<TPR, NC>(c) >= chunks || t + r >= p.rows) continue;
+                f32x2_t z[4], dy[4];
+                rz[r][c].get(z);
+                ry[r][c].get(dy);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    // columns from d on have dy = 0 and so add nothing
+                    const f32x2_t xh = mul2(sub2(z[j], m), q), h = mul2(dy[j], w[c][j]);
+                    db[c][j] = add2(db[c][j], dy[j]);
+                    dw[c][j] = fma2(dy[j], xh, dw[c][j]);
+                    s1 = add2(s1, h);
+                    s2 = fma2(h, xh, s2);
+                }
+            }
+            s[2 * r] = sum2(s1);
+            s[2 * r + 1] = sum2(s2);
+        }
+        group_sums<TPR, 2 * R>(s, part[buf]);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (t + r >= p.rows) continue;
+            T* dres = static_cast<T*>(p.dres) + (row + r) * p.lddres;
+            T* dx = static_cast<T*>(p.dx) + (p.dx ? (row + r) * p.lddx : 0);
+            RowStore<T, VEC, LANES> to_res, to_x;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const uint32_t first = first_chunk_of<TPR, NC>(c), chunk = chunk_of<TPR, NC>(c);
+                if (first >= chunks) break;
+                const bool last = c + 1 == NC || first + LANES >= chunks;
+                f32x2_t g[4];
+                if (chunk < chunks) {
+                    f32x2_t z[4], dy[4];
+                    rz[r][c].get(z);
+                    ry[r][c].get(dy);
+                    grad8(z, dy, w[c], mean[r], rstd[r], s[2 * r] * inv_d, s[2 * r + 1] * inv_d, g);
+                    if (p.dz) {
+                        f32x2_t e[4];
+                        re[r][c].get(e);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) g[j] = add2(g[j], e[j]);
+                    }
+                }
+                to_res.store(dres, chunk * kChunk, p.d, g, lane, group_mask<TPR>(), last);
+                if (p.dx) {
+                    if (chunk < chunks) drop8(p.mask, (t + r) * chunks + chunk, node, g);
+                    to_x.store(dx, chunk * kChunk, p.d, g, lane, group_mask<TPR>(), last);
+                }
+            }
         }
     }
     if (!p.dweight && !p.dbias) return;
 
-    // the block's sums: its groups of rows one after the other, then out
-    if constexpr (RPB > 1) {
-        for (int s = 0; s < RPB; ++s) {
-            if (s) __syncthreads();
-            if (sub == s)
+    // the block's sums: its groups one after the other, then out
+    if constexpr (G > 1) {
+        constexpr int D = TPR * NC * 8;
+        for (int g = 0; g < G; ++g) {
+            if (g) __syncthreads();
+            if (sub == g)
 #pragma unroll
                 for (int c = 0; c < NC; ++c)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int col = (lane + c * TPR) * kChunk + j;
-                        if (col < p.d) {
-                            sums[col] = (s ? sums[col] : 0.f) + dw[c][j];
-                            sums[p.d + col] = (s ? sums[p.d + col] : 0.f) + db[c][j];
-                        }
+                    for (int j = 0; j < 4; ++j) {
+                        f32x2_t* at = reinterpret_cast<f32x2_t*>(sums) + chunk_of<TPR, NC>(c) * 4 + j;
+                        if (g) dw[c][j] = add2(at[0], dw[c][j]), db[c][j] = add2(at[D / 2], db[c][j]);
+                        at[0] = dw[c][j];
+                        at[D / 2] = db[c][j];
                     }
         }
-        __syncthreads();
+        if (sub != G - 1) return;   // the last group has added itself last and holds the sums
     }
     float *ow, *ob;
     bool add = false;
@@ -302,65 +575,76 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_backward_kernel(co
         ob = p.dbias ? p.dbias + node * p.lddw : nullptr;
         add = p.accumulate;
     }
-    if constexpr (RPB > 1) {
-        for (int col = threadIdx.x; col < p.d; col += BLOCK) {
-            if (ow) ow[col] = (add ? ow[col] : 0.f) + sums[col];
-            if (ob) ob[col] = (add ? ob[col] : 0.f) + sums[p.d + col];
-        }
-    } else {
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
+    for (int c = 0; c < NC; ++c)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int col = (lane + c * TPR) * kChunk + j;
-                if (col < p.d) {
-                    if (ow) ow[col] = (add ? ow[col] : 0.f) + dw[c][j];
-                    if (ob) ob[col] = (add ? ob[col] : 0.f) + db[c][j];
-                }
+        for (int j = 0; j < 8; ++j) {
+            const int col = chunk_of<TPR, NC>(c) * kChunk + j;
+            if (col < p.d) {
+                if (ow) ow[col] = (add ? ow[col] : 0.f) + element(dw[c], j);
+                if (ob) ob[col] = (add ? ob[col] : 0.f) + element(db[c], j);
             }
-    }
+        }
 }
 
 // Rows of any width: the gradient of z, one block per row, two passes over it.
 template <class T, bool VEC>
 __global__ void __launch_bounds__(1024) norm_backward_wide_kernel(const NormBackwardParams p)
 {
-    __shared__ float part[2][32];
+    __shared__ float part[32 * 2];
     const uint32_t row = blockIdx.x;
     const uint32_t node = row / p.rows, t = row - node * p.rows;
     const uint32_t chunks = (uint32_t)(p.d + kChunk - 1) / kChunk;
     const float mean = p.mean[row], rstd = p.rstd[row];
-    auto chunk_of = [&](uint32_t chunk, float* h, float* xh) {
+    const int64_t all = (int64_t)p.nodes * p.rows;
+    const Span sz = span_of<T>(p.z, p.ldz, all, p.d), sy = span_of<T>(p.dy, p.lddy, all, p.d), se = span_of<T>(p.dz, p.lddz, all, p.d);
+    auto chunk_at = [&](uint32_t chunk, f32x2_t* z, f32x2_t* dy, f32x2_t* w) {
         Raw8<T, VEC> rz, rdy;
-        float w[8];
-        rz.load(static_cast<const T*>(p.z) + (int64_t)row * p.ldz, chunk * kChunk, p.d);
-        rdy.load(static_cast<const T*>(p.dy) + (int64_t)row * p.lddy, chunk * kChunk, p.d);
+        rz.load(static_cast<const T*>(p.z) + (int64_t)row * p.ldz, chunk * kChunk, p.d, sz);
+        rdy.load(static_cast<const T*>(p.dy) + (int64_t)row * p.lddy, chunk * kChunk, p.d, sy);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = 1.f;
+        for (int j = 0; j < 4; ++j) w[j] = both(1.f);
         if (p.weight) param8(p.weight + node * p.ldw, chunk * kChunk, p.d, p.wvec, w);
-        rz.get(xh);
-        rdy.get(h);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            xh[j] = (xh[j] - mean) * rstd;
-            h[j] *= w[j];
-        }
+        rz.get(z);
+        rdy.get(dy);
     };
-    float h[8], xh[8];
-    float s1 = 0.f, s2 = 0.f;
+    f32x2_t z[4], dy[4], w[4];
+    f32x2_t s1 = both(0.f), s2 = both(0.f);
     for (uint32_t chunk = threadIdx.x; chunk < chunks; chunk += 1024) {
-        chunk_of(chunk, h, xh);
+        chunk_at(chunk, z, dy, w);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            s1 += h[j];
-            s2 = fmaf(h[j], xh[j], s2);
+        for (int j = 0; j < 4; ++j) {
+            const f32x2_t h = mul2(dy[j], w[j]);
+            s1 = add2(s1, h);
+            s2 = fma2(h, mul2(sub2(z[j], both(mean)), both(rstd)), s2);
         }
     }
-    const float mh = row_sum<1024>(s1, part[0]) / (float)p.d;
-    const float mhx = row_sum<1024>(s2, part[1]) / (float)p.d;
-    for (uint32_t chunk = threadIdx.x; chunk < chunks; chunk += 1024) {
-        chunk_of(chunk, h, xh);
-        grad_store8<T, VEC>(p, row, t, node, chunks, chunk, h, xh, rstd, mh, mhx);
+    float s[2] = {sum2(s1), sum2(s2)};
+    group_sums<1024, 2>(s, part);
+    T* dres = static_cast<T*>(p.dres) + (int64_t)row * p.lddres;
+    T* dx = static_cast<T*>(p.dx) + (p.dx ? (int64_t)row * p.lddx : 0);
+    const int lane = threadIdx.x & 31;
+    for (uint32_t first = threadIdx.x - lane; first < chunks; first += 1024) {
+        const uint32_t chunk = first + lane;
+        f32x2_t g[4];
+        if (chunk < chunks) {
+            chunk_at(chunk, z, dy, w);
+            grad8(z, dy, w, mean, rstd, s[0] / (float)p.d, s[1] / (float)p.d, g);
+            if (p.dz) {
+                Raw8<T, VEC> re;
+                f32x2_t e[4];
+                re.load(static_cast<const T*>(p.dz) + (int64_t)row * p.lddz, chunk * kChunk, p.d, se);
+                re.get(e);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) g[j] = add2(g[j], e[j]);
+            }
+        }
+        RowStore<T, VEC, 32> to_res, to_x;
+        to_res.store(dres, chunk * kChunk, p.d, g, lane, 0xFFFFFFFFu, true);
+        if (p.dx) {
+            if (chunk < chunks) drop8(p.mask, t * chunks + chunk, node, g);
+            to_x.store(dx, chunk * kChunk, p.d, g, lane, 0xFFFFFFFFu, true);
+        }
     }
 }
 
@@ -372,20 +656,24 @@ __global__ void __launch_bounds__(128) norm_columns_kernel(const NormBackwardPar
     const uint32_t node = blockIdx.z;
     const int col = (blockIdx.x * 128 + threadIdx.x) * kChunk;
     if (col >= p.d) return;
-    float dw[8] = {}, db[8] = {};
+    const int64_t all = (int64_t)p.nodes * p.rows;
+    const Span sz = span_of<T>(p.z, p.ldz, all, p.d), sy = span_of<T>(p.dy, p.lddy, all, p.d);
+    f32x2_t dw[4], db[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) dw[j] = db[j] = both(0.f);
     for (uint32_t t = blockIdx.y; t < p.rows; t += gridDim.y) {
         const int64_t row = (int64_t)node * p.rows + t;
         Raw8<T, VEC> rz, rdy;
-        float z[8], dy[8];
-        rz.load(static_cast<const T*>(p.z) + row * p.ldz, col, p.d);
-        rdy.load(static_cast<const T*>(p.dy) + row * p.lddy, col, p.d);
-        const float mean = p.mean[row], rstd = p.rstd[row];
+        f32x2_t z[4], dy[4];
+        rz.load(static_cast<const T*>(p.z) + row * p.ldz, col, p.d, sz);
+        rdy.load(static_cast<const T*>(p.dy) + row * p.lddy, col, p.d, sy);
+        const f32x2_t m = both(p.mean[row]), q = both(p.rstd[row]);
         rz.get(z);
         rdy.get(dy);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            dw[j] = fmaf(dy[j], (z[j] - mean) * rstd, dw[j]);
-            db[j] += dy[j];
+        for (int j = 0; j < 4; ++j) {
+            dw[j] = fma2(dy[j], mul2(sub2(z[j], m), q), dw[j]);
+            db[j] = add2(db[j], dy[j]);
         }
     }
     const bool add = p.splits == 1 && p.accumulate;
@@ -395,8 +683,8 @@ __global__ void __launch_bounds__(128) norm_columns_kernel(const NormBackwardPar
 #pragma unroll
     for (int j = 0; j < 8; ++j)
         if (col + j < p.d) {
-            if (ow) ow[col + j] = (add ? ow[col + j] : 0.f) + dw[j];
-            if (ob) ob[col + j] = (add ? ob[col + j] : 0.f) + db[j];
+            if (ow) ow[col + j] = (add ? ow[col + j] : 0.f) + element(dw, j);
+            if (ob) ob[col + j] = (add ? ob[col + j] : 0.f) + element(db, j);
         }
 }
 
@@ -436,50 +724,122 @@ __global__ void zero_params_kernel(const NormBackwardParams p)
 }
 
 // ---- launches ---------------------------------------------------------------------------------------
-constexpr int kForwardWide = 16384, kBackwardWide = 8192;   // widest rows that stay in registers
+constexpr int kForwardWide = 16384, kForwardOddWide = 8192, kBackwardWide = 8192;   // widest rows that stay in registers
+
+// Blocks of a kernel that an SM holds, from its registers (looked up once) and shared memory.
+template <class Kernel>
+int blocks_per_sm(Kernel kernel, int block, size_t smem, int& regs)
+{
+    if (!regs) {
+        cudaFuncAttributes at;
+        regs = cudaFuncGetAttributes(&at, kernel) == cudaSuccess && at.numRegs > 0 ? at.numRegs : 128;
+    }
+    int n = 65536 / ((regs + 7) / 8 * 8 * block);
+    if (n > 2048 / block) n = 2048 / block;
+    const int by_smem = (int)(227 * 1024 / (smem + 2048));
+    if (n > by_smem) n = by_smem;
+    return n < 1 ? 1 : n;
+}
 
 template <class T, bool VEC, int TPR, int NC>
+cudaError_t dropout_rows(DropoutParams& p, cudaStream_t s)
+{
+    p.stretches = make_divisor((p.chunks.d + NC * TPR - 1) / (NC * TPR));
+    const uint64_t groups = (uint64_t)p.rows * p.stretches.d;
+    dropout_rows_kernel<T, VEC, TPR, NC><<<dim3((unsigned)((groups + 256 / TPR - 1) / (256 / TPR)), p.nodes), 256, 0, s>>>(p);
+    return cudaGetLastError();
+}
+
+template <class T, bool VEC>
+cudaError_t dropout_of(DropoutParams p, cudaStream_t s)
+{
+    const uint32_t chunks = (uint32_t)(p.d + kChunk - 1) / kChunk;
+    const uint64_t total = (uint64_t)p.rows * chunks;   // per node, below 2^32
+    p.chunks = make_divisor(chunks);
+    if constexpr (VEC) {
+        if (p.ldx == p.d && p.ldy == p.d && total < (uint64_t(1) << 32) - 1024) {
+            // four chunks per thread where that still fills the SMs with blocks
+            if (p.nodes * total < 148 * 8 * 1024) dropout_dense_kernel<T, 1><<<dim3((unsigned)((total + 255) / 256), p.nodes), 256, 0, s>>>(p);
+            else dropout_dense_kernel<T, 4><<<dim3((unsigned)((total + 1023) / 1024), p.nodes), 256, 0, s>>>(p);
+            return cudaGetLastError();
+        }
+    }
+    return chunks <= 8    ? dropout_rows<T, VEC, 8, 1>(p, s)
+           : chunks <= 32 ? dropout_rows<T, VEC, 32, 1>(p, s)
+           : chunks <= 64 ? dropout_rows<T, VEC, 32, 2>(p, s)
+                          : dropout_rows<T, VEC, 32, 4>(p, s);
+}
+
+template <class T, bool VEC, int TPR, int NC, int R>
+cudaError_t forward_odd(const NormForwardParams& p, cudaStream_t s)
+{
+    constexpr int BLOCK = TPR < 128 ? 128 : TPR, SET = BLOCK / TPR * R;
+    const size_t smem = (size_t)((p.d + kChunk - 1) / kChunk) * 64;
+    const auto kernel = norm_forward_odd_kernel<T, VEC, TPR, NC, R>;
+    if (smem > 47 * 1024) {
+        static unsigned long long limit_set = 0;
+        const cudaError_t e = ensure_smem_limit(kernel, kForwardOddWide * 8, limit_set);
+        if (e != cudaSuccess) return e;
+    }
+    static int regs = 0;
+    const uint32_t sets = (p.rows + SET - 1) / SET;
+    const uint32_t room = (uint32_t)(kSMs * blocks_per_sm(kernel, BLOCK, smem, regs)) / p.nodes;
+    kernel<<<dim3(sets < room ? sets : room ? room : 1, p.nodes), BLOCK, smem, s>>>(p);
+    return cudaGetLastError();
+}
+
+template <class T, int TPR, int NC, int R>
 cudaError_t forward_as(const NormForwardParams& p, cudaStream_t s)
 {
-    constexpr int BLOCK = TPR < 128 ? 128 : TPR, RPB = BLOCK / TPR;
-    const uint32_t rows = p.nodes * p.rows;
-    norm_forward_kernel<T, VEC, TPR, NC><<<(rows + RPB - 1) / RPB, BLOCK, 0, s>>>(p);
+    constexpr int BLOCK = TPR < 128 ? 128 : TPR, SET = BLOCK / TPR * R;
+    norm_forward_kernel<T, TPR, NC, R><<<dim3((p.rows + SET - 1) / SET, p.nodes), BLOCK, 0, s>>>(p);
     return cudaGetLastError();
 }
 
 template <class T, bool VEC>
 cudaError_t forward_of(const NormForwardParams& p, cudaStream_t s)
 {
-    if (p.d <= 64) return forward_as<T, VEC, 8, 1>(p, s);
-    if (p.d <= 256) return forward_as<T, VEC, 32, 1>(p, s);
-    if (p.d <= 512) return forward_as<T, VEC, 32, 2>(p, s);
-    if (p.d <= 1024) return forward_as<T, VEC, 32, 4>(p, s);
-    if (p.d <= 2048) return forward_as<T, VEC, 128, 2>(p, s);
-    if (p.d <= 4096) return forward_as<T, VEC, 128, 4>(p, s);
-    if (p.d <= 8192) return forward_as<T, VEC, 512, 2>(p, s);
-    if (p.d <= kForwardWide) return forward_as<T, VEC, 512, 4>(p, s);
+    if constexpr (VEC)
+        if (p.weight && p.bias && p.wvec) {
+            if (p.d <= 64) return forward_as<T, 8, 1, 4>(p, s);
+            if (p.d <= 256) return forward_as<T, 32, 1, 4>(p, s);
+            if (p.d <= 512) return forward_as<T, 32, 2, 2>(p, s);
+            if (p.d <= 1024) return forward_as<T, 32, 4, 1>(p, s);
+            if (p.d <= 2048) return forward_as<T, 128, 2, 2>(p, s);
+            if (p.d <= 4096) return forward_as<T, 128, 4, 1>(p, s);
+            if (p.d <= 8192) return forward_as<T, 512, 2, 1>(p, s);
+            if (p.d <= kForwardWide) return forward_as<T, 512, 4, 1>(p, s);
+        }
+    if (p.d <= 64) return forward_odd<T, VEC, 8, 1, 2>(p, s);
+    if (p.d <= 256) return forward_odd<T, VEC, 32, 1, 2>(p, s);
+    if (p.d <= 512) return forward_odd<T, VEC, 32, 2, 1>(p, s);
+    if (p.d <= 1024) return forward_odd<T, VEC, 64, 2, 1>(p, s);
+    if (p.d <= 2048) return forward_odd<T, VEC, 128, 2, 1>(p, s);
+    if (p.d <= 4096) return forward_odd<T, VEC, 256, 2, 1>(p, s);
+    if (p.d <= kForwardOddWide) return forward_odd<T, VEC, 512, 2, 1>(p, s);
     norm_forward_wide_kernel<T, VEC><<<p.nodes * p.rows, 1024, 0, s>>>(p);
     return cudaGetLastError();
 }
 
-template <class T, bool VEC, int TPR, int NC>
+template <class T, bool VEC, int TPR, int NC, int R>
 cudaError_t backward_as(const NormBackwardParams& p, cudaStream_t s)
 {
-    constexpr int BLOCK = TPR < 256 ? 256 : TPR, RPB = BLOCK / TPR;
-    norm_backward_kernel<T, VEC, TPR, NC><<<dim3(p.splits, p.nodes), BLOCK, RPB > 1 ? 2 * p.d * sizeof(float) : 0, s>>>(p);
+    norm_backward_kernel<T, VEC, TPR, NC, R><<<dim3(p.splits, p.nodes), TPR < 128 ? 128 : TPR, 0, s>>>(p);
     return cudaGetLastError();
 }
 
 template <class T, bool VEC>
 cudaError_t backward_of(const NormBackwardParams& p, cudaStream_t s)
 {
-    if (p.d <= 64) return backward_as<T, VEC, 8, 1>(p, s);
-    if (p.d <= 256) return backward_as<T, VEC, 32, 1>(p, s);
-    if (p.d <= 512) return backward_as<T, VEC, 32, 2>(p, s);
-    if (p.d <= 1024) return backward_as<T, VEC, 32, 4>(p, s);
-    if (p.d <= 2048) return backward_as<T, VEC, 256, 1>(p, s);
-    if (p.d <= 4096) return backward_as<T, VEC, 512, 1>(p, s);
-    if (p.d <= kBackwardWide) return backward_as<T, VEC, 512, 2>(p, s);
+    // rows at a time: what 128 registers hold
+    constexpr int R = sizeof(T) == 4 ? (VEC ? 2 : 1) : (VEC ? 4 : 2);
+    if (p.d <= 64) return backward_as<T, VEC, 8, 1, R>(p, s);
+    if (p.d <= 256) return backward_as<T, VEC, 32, 1, R>(p, s);
+    if (p.d <= 512) return backward_as<T, VEC, 64, 1, R>(p, s);
+    if (p.d <= 1024) return backward_as<T, VEC, 128, 1, R>(p, s);
+    if (p.d <= 2048) return backward_as<T, VEC, 256, 1, R>(p, s);
+    if (p.d <= 4096) return backward_as<T, VEC, 512, 1, R>(p, s);
+    if (p.d <= kBackwardWide) return backward_as<T, VEC, 512, 2, 1>(p, s);
     if (p.dweight || p.dbias) {
         norm_columns_kernel<T, VEC><<<dim3((p.d + 1023) / 1024, p.splits, p.nodes), 128, 0, s>>>(p);
         const cudaError_t e = cudaGetLastError();
@@ -498,10 +858,8 @@ cudaError_t backward_of(const NormBackwardParams& p, cudaStream_t s)
 
 cudaError_t launch_dropout(const DropoutParams& p, int dtype, bool vec, cudaStream_t s)
 {
-    const uint64_t total = (uint64_t)p.nodes * p.rows * ((p.d + kChunk - 1) / kChunk);
-    if (!total) return cudaSuccess;
-    const unsigned grid = (unsigned)((total + 255) / 256);
-#define GPGA_CALL(T, V) (dropout_kernel<T, V><<<grid, 256, 0, s>>>(p), cudaGetLastError())
+    if (!p.rows) return cudaSuccess;
+#define GPGA_CALL(T, V) dropout_of<T, V>(p, s)
     return GPGA_BY_TYPE(GPGA_CALL);
 #undef GPGA_CALL
 }
@@ -517,11 +875,11 @@ cudaError_t launch_norm_forward(const NormForwardParams& p, int dtype, bool vec,
 int norm_backward_splits(int64_t nodes, int64_t rows, int64_t d)
 {
     if (rows < 1) return 1;
-    // rows a block works on at a time, and blocks that fit an SM
-    const int64_t rpb = d <= 64 ? 32 : d <= 1024 ? 8 : 1;
-    const int64_t per_sm = d <= 512 ? 3 : d <= 4096 ? 2 : 1;
-    int64_t splits = (kSMs * per_sm + nodes - 1) / nodes;
-    const int64_t groups = (rows + rpb - 1) / rpb;
+    // rows a block works on at a time, and blocks that an SM holds
+    const int64_t set = 4 * (d <= 64 ? 16 : d <= 256 ? 4 : d <= 512 ? 2 : 1);
+    const int64_t per_sm = d <= 1024 ? 4 : d <= 2048 ? 2 : 1;
+    int64_t splits = (kSMs * per_sm) / nodes;
+    const int64_t groups = (rows + set - 1) / set;
     if (splits > groups) splits = groups;
     return (int)(splits < 1 ? 1 : splits);
 }
@@ -538,8 +896,7 @@ cudaError_t launch_norm_backward(const NormBackwardParams& p, int dtype, bool ve
     const cudaError_t e = GPGA_BY_TYPE(GPGA_CALL);
 #undef GPGA_CALL
     if (e != cudaSuccess || p.splits == 1 || !params) return e;
-    norm_params_kernel<<<dim3((unsigned)((2 * (int64_t)p.d + 31) / 32), p.nodes), 256, 0, s>>>(p);
-    return cudaGetLastError();
+    return launch_after_trigger(norm_params_kernel, dim3((unsigned)((2 * (int64_t)p.d + 31) / 32), p.nodes), dim3(256), 0, s, true, p);
 }
 
 }  // namespace gpga

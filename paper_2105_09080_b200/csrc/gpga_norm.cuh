@@ -10,6 +10,7 @@ struct DropoutParams {
     int64_t ldx, ldy;        // row strides in elements
     uint32_t nodes, rows;    // rows per node
     int32_t d;
+    Divisor chunks, stretches;   // set by the launch
     DropMask mask;
 };
 

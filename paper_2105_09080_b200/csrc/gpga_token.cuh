@@ -45,98 +45,285 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi, __half)
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// The eight columns col .. col + 7 of a row as read from memory.  VEC: 128-bit accesses (the host has
-// checked alignment and that d is a multiple of eight).  Otherwise element by element, columns from d on
-// read as zero.
-template <class T, bool VEC> struct Raw8;
-template <class T> struct Raw8<T, true> {
-    uint4 w;
-    __device__ __forceinline__ void load(const T* row, int col, int) { w = __ldcs(reinterpret_cast<const uint4*>(row + col)); }
-    __device__ __forceinline__ void get(float* v) const
-    {
-        unpack16(w.x, v[0], v[1], T());
-        unpack16(w.y, v[2], v[3], T());
-        unpack16(w.z, v[4], v[5], T());
-        unpack16(w.w, v[6], v[7], T());
-    }
+// Accesses to rows in chunks of eight columns, column 8 chunk .. 8 chunk + 7.
+//
+// VEC: every row starts on 16 bytes and d is a multiple of eight (the host has checked): 128-bit accesses.
+//
+// Otherwise a row starts at any element and its last chunk may be partial, but the accesses stay 128 bits wide: a chunk
+// is cut out of the two or three aligned 16-byte pieces ("granules") it lies in, and a granule is written by the lane
+// that holds its last columns, which takes the others from its neighbour (a shuffle).  Element by element, 16-bit
+// rows of 1001 columns moved at 1.8 TB/s (layer norm of 32,000 of them, with residual and dropout); this way see
+// gpga_norm.cu.
+// A granule that reaches past the array's first or last byte is read element by element; bytes of neighbouring rows
+// that come along are dropped, never written.
+struct Span {   // bytes of a whole array: first byte of its first row, one past the last of its last row
+    const char *lo, *hi;
 };
-template <> struct Raw8<float, true> {
-    float4 a, b;
-    __device__ __forceinline__ void load(const float* row, int col, int)
-    {
-        a = __ldcs(reinterpret_cast<const float4*>(row + col));
-        b = __ldcs(reinterpret_cast<const float4*>(row + col) + 1);
-    }
-    __device__ __forceinline__ void get(float* v) const
-    {
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-        v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    }
-};
-template <class T> struct Raw8<T, false> {
-    T e[8];
-    __device__ __forceinline__ void load(const T* row, int col, int d)
-    {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) e[j] = col + j < d ? row[col + j] : from_f32<T>(0.f);
-    }
-    __device__ __forceinline__ void get(float* v) const
-    {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = to_f32(e[j]);
-    }
-};
-
-template <class T, bool VEC>
-__device__ __forceinline__ void store8(T* row, int col, int d, const float* v)
+template <class T>
+__device__ __forceinline__ Span span_of(const void* p, int64_t ld, int64_t rows, int d)
 {
-    if constexpr (!VEC) {
+    const char* lo = static_cast<const char*>(p);
+    return {lo, lo + ((rows - 1) * ld + d) * (int64_t)sizeof(T)};
+}
+
+// Words o[0 .. N) = bytes a .. a + 4 N - 1 of the words w[0 .. N + 4), 0 <= a < 16.
+template <int N>
+__device__ __forceinline__ void cut(const uint32_t* w, uint32_t a, uint32_t* o)
+{
+    uint32_t u[N + 2], t[N + 1];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (col + j < d) row[col + j] = from_f32<T>(v[j]);
-    } else if constexpr (sizeof(T) == 4) {
-        __stcs(reinterpret_cast<float4*>(row + col), make_float4(v[0], v[1], v[2], v[3]));
-        __stcs(reinterpret_cast<float4*>(row + col) + 1, make_float4(v[4], v[5], v[6], v[7]));
-    } else {
-        __stcs(reinterpret_cast<uint4*>(row + col), make_uint4(pack16(v[0], v[1], T()), pack16(v[2], v[3], T()),
-                                                              pack16(v[4], v[5], T()), pack16(v[6], v[7], T())));
+    for (int i = 0; i < N + 2; ++i) u[i] = a & 8 ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < N + 1; ++i) t[i] = a & 4 ? u[i + 1] : u[i];
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] = __funnelshift_r(t[i], t[i + 1], (a & 3) * 8);
+}
+
+// A chunk in registers is four pairs of fp32, so that its arithmetic takes packed instructions.
+template <class T>
+__device__ __forceinline__ void unpack8(const uint32_t* w, f32x2_t* v)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (sizeof(T) == 4) {
+            v[j] = pack2(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1]));
+        } else {
+            float lo, hi;
+            unpack16(w[j], lo, hi, T());
+            v[j] = pack2(lo, hi);
+        }
+    }
+}
+template <class T>
+__device__ __forceinline__ void pack8(const f32x2_t* v, uint32_t* w)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float2 f = unpack2(v[j]);
+        if constexpr (sizeof(T) == 4) {
+            w[2 * j] = __float_as_uint(f.x);
+            w[2 * j + 1] = __float_as_uint(f.y);
+        } else {
+            w[j] = pack16(f.x, f.y, T());
+        }
+    }
+}
+__device__ __forceinline__ float element(const f32x2_t* v, int j) { return j & 1 ? unpack2(v[j >> 1]).y : unpack2(v[j >> 1]).x; }
+// Zeroes the columns from the n-th on (the end of a row that is not a multiple of eight).
+__device__ __forceinline__ void keep_first(f32x2_t* v, int n)
+{
+    if (n >= 8) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float2 f = unpack2(v[j]);
+        v[j] = pack2(2 * j < n ? f.x : 0.f, 2 * j + 1 < n ? f.y : 0.f);
     }
 }
 
-// Eight fp32 parameters (a weight row's columns), kept in the caches: every row of a node reads them.
-__device__ __forceinline__ void param8(const float* w, int col, int d, bool vec, float* v)
+// A chunk as read from memory.
+template <class T, bool VEC> struct Raw8 {
+    static constexpr int W = 2 * sizeof(T);   // words of a chunk
+    uint32_t w[VEC ? W : W + 4];
+    uint32_t a;   // !VEC: byte offset of the chunk in w
+    int n;        // !VEC: columns that the row has here
+    // read once (VEC: with the streaming hint)
+    __device__ __forceinline__ void load(const T* row, int col, int d, const Span& s) { load_as<true>(row, col, d, s); }
+    // kept in the caches: other rows of the launch may be read again
+    __device__ __forceinline__ void load_cached(const T* row, int col, int d, const Span& s) { load_as<false>(row, col, d, s); }
+    template <bool ONCE>
+    __device__ __forceinline__ void load_as(const T* row, int col, int d, const Span& s)
+    {
+        if constexpr (VEC) {
+#pragma unroll
+            for (int i = 0; i < W / 4; ++i) {
+                const uint4* at = reinterpret_cast<const uint4*>(row + col) + i;
+                const uint4 q = ONCE ? __ldcs(at) : *at;
+                w[4 * i] = q.x; w[4 * i + 1] = q.y; w[4 * i + 2] = q.z; w[4 * i + 3] = q.w;
+            }
+        } else {
+            n = max(0, min(8, d - col));
+            a = 0;
+            if (n == 0) return;
+            const char* at = reinterpret_cast<const char*>(row + col);
+            a = (uint32_t)(uintptr_t)at & 15u;
+            const char* g = at - a;
+            const int bytes = (int)a + n * (int)sizeof(T);
+            if (g >= s.lo && g + (bytes + 15) / 16 * 16 <= s.hi) {
+#pragma unroll
+                for (int i = 0; i < W / 4 + 1; ++i) {
+                    uint4 q = make_uint4(0, 0, 0, 0);
+                    if (16 * i < bytes) q = reinterpret_cast<const uint4*>(g)[i];
+                    w[4 * i] = q.x; w[4 * i + 1] = q.y; w[4 * i + 2] = q.z; w[4 * i + 3] = q.w;
+                }
+            } else {
+                float v[8];
+                f32x2_t v2[4];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = j < n ? to_f32(row[col + j]) : 0.f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v2[j] = pack2(v[2 * j], v[2 * j + 1]);
+                pack8<T>(v2, w);
+                a = 0;
+            }
+        }
+    }
+    __device__ __forceinline__ void get(f32x2_t* v) const
+    {
+        if constexpr (VEC) {
+            unpack8<T>(w, v);
+        } else {
+            uint32_t o[W];
+            cut<W>(w, a, o);
+            unpack8<T>(o, v);
+            keep_first(v, n);
+        }
+    }
+};
+
+// Stores a chunk to 16-byte aligned memory.
+template <class T>
+__device__ __forceinline__ void store8(T* at, const f32x2_t* v)
+{
+    uint32_t o[2 * sizeof(T)];
+    pack8<T>(v, o);
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+        __stcs(reinterpret_cast<uint4*>(at) + i, make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]));
+}
+
+// Stores the chunks of a row that neighbouring lanes hold.  Lane `lane` of the TPR lanes of `mask` that share the
+// call holds chunk `first + lane`, `first` growing by TPR from call to call of one row; every lane of them makes the
+// call, with n = 0 where the row has no such chunk.  prev keeps the words of the call before, so that a row leaves only
+// its two ends to single elements.
+template <class T, bool VEC, int TPR> struct RowStore {
+    static constexpr int W = 2 * sizeof(T);
+    uint32_t prev[VEC ? 1 : W];
+    bool any;   // !VEC: there was a call before
+    __device__ __forceinline__ RowStore() : any(false) {}
+    // last: no further call follows for this row in these lanes.  VEC: lanes without the chunk need not call.
+    __device__ __forceinline__ void store(T* row, int col, int d, const f32x2_t* v, int lane, unsigned mask, bool last)
+    {
+        if constexpr (VEC) {
+            if (col < d) store8<T>(row + col, v);
+        } else {
+            const int n = max(0, min(8, d - col)), next_n = max(0, min(8, d - col - 8));
+            const char* at = reinterpret_cast<const char*>(row + col);
+            const uint32_t a = (uint32_t)(uintptr_t)at & 15u;
+            const int head = (16 - (int)a) / (int)sizeof(T);   // columns up to the next granule
+            constexpr int P = 16 / sizeof(T);                  // columns of a granule
+            uint32_t c[W + 4];   // the last 16 bytes of the chunk before, then this chunk
+            pack8<T>(v, c + 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t mine = c[4 + W - 4 + i];
+                c[i] = __shfl_sync(mask, lane == TPR - 1 ? prev[W - 4 + i] : mine, (lane + TPR - 1) % TPR, TPR);
+            }
+            const bool has_prev = a == 0 || lane > 0 || any;
+            const bool has_next = lane < TPR - 1 || !last;
+#pragma unroll
+            for (int i = 0; i < W; ++i) prev[i] = c[4 + i];
+            any = true;
+            uint32_t o[W];
+            cut<W>(c, a ? 16 - a : 0, o);   // the granules that end inside this chunk
+            if (a == 0) {
+#pragma unroll
+                for (int i = 0; i < W; ++i) o[i] = c[4 + i];
+            }
+            T* g = row + col - (a ? P - head : 0);   // first granule
+            const int first_end = a ? head : P;      // columns of this chunk in it
+#pragma unroll
+            for (int i = 0; i < W / 4; ++i) {
+                const int end = first_end + i * P, begin = i ? end - P : 0;   // columns of this chunk in granule i
+                if (n >= end && (i || has_prev))
+                    __stcs(reinterpret_cast<uint4*>(g) + i, make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]));
+                else if (n > begin) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (j >= begin && j < min(n, end)) row[col + j] = from_f32<T>(element(v, j));
+                }
+            }
+            // the columns behind the last granule: the next lane writes them where it can
+            const int tail = first_end + (W / 4 - 1) * P;
+            if (n > tail && !(has_next && next_n >= head)) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (j >= tail && j < n) row[col + j] = from_f32<T>(element(v, j));
+            }
+        }
+    }
+};
+
+// Eight fp32 parameters of a row, kept in the caches; vec: 128-bit accesses (the row starts on 16 bytes and has eight
+// columns here).
+__device__ __forceinline__ void param8(const float* w, int col, int d, bool vec, f32x2_t* v)
 {
     if (vec) {
         const float4 a = __ldg(reinterpret_cast<const float4*>(w + col)), b = __ldg(reinterpret_cast<const float4*>(w + col) + 1);
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-        v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        v[0] = pack2(a.x, a.y); v[1] = pack2(a.z, a.w);
+        v[2] = pack2(b.x, b.y); v[3] = pack2(b.z, b.w);
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = col + j < d ? __ldg(w + col + j) : 0.f;
+        for (int j = 0; j < 4; ++j)
+            v[j] = pack2(col + 2 * j < d ? __ldg(w + col + 2 * j) : 0.f, col + 2 * j + 1 < d ? __ldg(w + col + 2 * j + 1) : 0.f);
     }
+}
+
+// Threads that share a row: TPR, in one warp up to 32 of them.
+template <int TPR>
+__device__ __forceinline__ unsigned group_mask()
+{
+    return TPR >= 32 ? 0xFFFFFFFFu : ((1u << (TPR & 31)) - 1u) << ((threadIdx.x & 31) / TPR * TPR);
+}
+
+__device__ __forceinline__ f32x2_t both(float v) { return pack2(v, v); }
+__device__ __forceinline__ float sum2(f32x2_t v)
+{
+    const float2 f = unpack2(v);
+    return f.x + f.y;
 }
 
 // Dropout of one activation tensor: what a launch needs to form any element's mask.
 struct DropMask {
     PhiloxKeys keys;
-    uint32_t threshold;   // dropped iff the element's 16 bits are below this; 0: no dropout
-    float scale;          // 65536 / (65536 - threshold), 0 when everything is dropped
-    uint32_t node0;       // global index of local node 0
+    bool on;          // false: nothing is dropped
+    uint32_t above;   // 65536 q - 1: an element is kept iff its 16 bits, as the upper half of a word, are above
+    float scale;      // 65536 / (65536 - q), 0 when everything is dropped
+    uint32_t node0;   // global index of local node 0
     uint32_t k, stream;
 };
 
-// Dropout of the eight columns of chunk `chunk` (columns 8 chunk .. 8 chunk + 7) of row t of local node i:
-// counter (t * chunks + chunk, node, k, stream); column 8 chunk + j owns half j & 1 (low half first) of word j >> 1.
-// A dropped element is a selected zero, so that NaN and infinities vanish with it.
-__device__ __forceinline__ void drop8(const DropMask& m, uint32_t t, uint32_t i, uint32_t chunks, uint32_t chunk, float* v)
+// Dropout of chunk `chunk` (columns 8 chunk .. 8 chunk + 7) of row t of local node i: counter (t * chunks + chunk,
+// node, k, stream); column 8 chunk + j owns half j & 1 (low half first) of word j >> 1.  A dropped element is a
+// selected zero, so that NaN and infinities vanish with it.  The lower half of a word cannot change whether the upper
+// one is above (65536 q - 1), so that the upper half is compared in place.
+__device__ __forceinline__ void drop8(const DropMask& m, uint32_t group, uint32_t i, f32x2_t* v)
 {
-    const uint4 w = philox4x32_10(t * chunks + chunk, m.node0 + i, m.k, m.stream, m.keys);
+    if (!m.on) return;
+    const uint4 w = philox4x32_10(group, m.node0 + i, m.k, m.stream, m.keys);
     const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+    const f32x2_t scale = both(m.scale);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const uint32_t bits = (j & 1) ? word[j >> 1] >> 16 : word[j >> 1] & 0xFFFFu;
-        v[j] = bits >= m.threshold ? v[j] * m.scale : 0.f;
+    for (int j = 0; j < 4; ++j) {
+        const float2 f = unpack2(mul2(v[j], scale));
+        v[j] = pack2(word[j] << 16 > m.above ? f.x : 0.f, word[j] > m.above ? f.y : 0.f);
     }
+}
+
+// n / d for n < 2^32 by a multiplication (Granlund and Montgomery's division by an invariant, with a 33-bit multiplier
+// whose top bit is the added n).
+struct Divisor {
+    uint32_t d, mul, shift;
+};
+inline Divisor make_divisor(uint32_t d)
+{
+    Divisor v{d, 0, 0};
+    while (v.shift < 32 && (uint64_t(1) << v.shift) < d) ++v.shift;
+    v.mul = (uint32_t)(((uint64_t(1) << 32) * ((uint64_t(1) << v.shift) - d)) / d + 1);
+    return v;
+}
+__device__ __forceinline__ uint32_t divide(uint32_t n, const Divisor& v)
+{
+    return (uint32_t)(((uint64_t)__umulhi(n, v.mul) + n) >> v.shift);
 }
 
 }  // namespace gpga

@@ -41,8 +41,10 @@ const char* drop_mask(DropMask& m, double p, uint64_t seed, int64_t k, int64_t s
 {
     m = DropMask{};
     if (!(p >= 0.0 && p <= 1.0)) return "p must lie in [0, 1]";
-    m.threshold = (uint32_t)std::floor(65536.0 * p + 0.5);
-    m.scale = m.threshold < 65536u ? (float)(65536.0 / (65536.0 - m.threshold)) : 0.f;
+    const uint32_t q = (uint32_t)std::floor(65536.0 * p + 0.5);
+    m.on = q > 0;
+    m.above = (uint32_t)((uint64_t)q * 65536u - 1u);
+    m.scale = q < 65536u ? (float)(65536.0 / (65536.0 - q)) : 0.f;
     if (p == 0.0) return nullptr;
     if (k < 0 || k >= (int64_t(1) << 32)) return "k must lie in [0, 2^32)";
     if (site < 0 || site >= (int64_t(1) << 30)) return "site must lie in [0, 2^30)";
