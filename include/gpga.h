@@ -510,9 +510,10 @@ int32_t gpga_logistic_gradient_noalloc(const float* A_dev, const float* y_dev, c
  *  - Results do not depend on the order in which blocks run (no floating-point atomics).
  *  - An output may be the very same array (same pointer and stride) as an activation input of the same call; any
  *    other overlap of outputs with inputs or with one another gives undefined values.
+ *  - A call's arguments come in one struct of 8-byte members (device pointers, sizes and strides in elements).
  *  - No handle: the text of an error is gpga_last_error(NULL) of the calling thread.  Scratch is caller-owned,
  *    16-byte aligned, and may be used again as soon as the call's work is done (stream order).
- *  Errors of all of them: INVALID_ARG for sizes outside the above, a stride below d, NULL pointers, an unknown dtype;
+ *  Errors of all of them: INVALID_ARG for sizes outside the above, a stride below d, NULL pointers (of args too), an unknown dtype;
  *  CUDA when a launch failed.
  */
 enum { GPGA_DTYPE_F32 = 0, GPGA_DTYPE_BF16 = 1, GPGA_DTYPE_F16 = 2 };
@@ -522,22 +523,32 @@ enum { GPGA_DTYPE_F32 = 0, GPGA_DTYPE_BF16 = 1, GPGA_DTYPE_F16 = 2 };
  * starts at table + i * node_ldt + v * ldt.  tokens: nodes * rows integers of 4 or 8 bytes (token_bytes), dense.  A
  * token outside 0 .. vocab - 1 names no row: its output row is zero (padding).  1 <= vocab < 2^31.
  */
-int32_t gpga_embedding_forward(const float* table_dev, int64_t ldt, int64_t node_ldt, const void* tokens_dev,
-                               int32_t token_bytes, void* out_dev, int64_t ldo, int32_t dtype, int64_t nodes,
-                               int64_t rows, int64_t d, int64_t vocab, float scale, void* stream);
+typedef struct gpga_embedding_forward_args {
+    const float* table;
+    const void* tokens;
+    void* out;
+    int64_t ldt, node_ldt, ldo, token_bytes, dtype, nodes, rows, d, vocab;
+    double scale;   /* used as fp32 */
+} gpga_embedding_forward_args_t;
+int32_t gpga_embedding_forward(const gpga_embedding_forward_args_t* args, void* stream);
 
 /*
- * Its gradient: grad_i[v][:] = scale * sum over the t with token[i][t] = v, in ascending order up to the grouping
- * below, of dout[i][t][:]; added to what grad holds when accumulate is not 0, otherwise every row of grad is written
- * (zero where no token names it).  Tokens outside the vocabulary are left out.  The tokens of a node are sorted on
- * chip (stable, 65536 at a time); the sum of a token is formed in fp32 over fixed groups of its sorted places, so the
- * result is the same in every run.  grad rows: grad + i * node_ldg + v * ldg.
+ * Its gradient: grad_i[v][:] = scale * sum over the t with token[i][t] = v of dout[i][t][:]; added to what grad holds
+ * when accumulate is not 0, otherwise every row of grad is written (zero where no token names it).  Tokens outside the
+ * vocabulary are left out.  The tokens of a node are sorted on chip (stable, 65536 at a time); the sum of a token is
+ * formed in fp32 over fixed groups of its sorted places, so the result is the same in every run.  grad rows: grad + i *
+ * node_ldg + v * ldg, without overlap.
  * scratch: gpga_embedding_scratch_bytes(nodes, rows, d, vocab) bytes.
  */
-int32_t gpga_embedding_backward(const void* dout_dev, int64_t ldo, int32_t dtype, const void* tokens_dev,
-                                int32_t token_bytes, float* grad_dev, int64_t ldg, int64_t node_ldg, int64_t nodes,
-                                int64_t rows, int64_t d, int64_t vocab, float scale, int32_t accumulate,
-                                void* scratch_dev, int64_t scratch_bytes, void* stream);
+typedef struct gpga_embedding_backward_args {
+    const void* dout;
+    const void* tokens;
+    float* grad;
+    void* scratch;
+    int64_t scratch_bytes, ldo, ldg, node_ldg, token_bytes, dtype, nodes, rows, d, vocab, accumulate;
+    double scale;   /* used as fp32 */
+} gpga_embedding_backward_args_t;
+int32_t gpga_embedding_backward(const gpga_embedding_backward_args_t* args, void* stream);
 int64_t gpga_embedding_scratch_bytes(int64_t nodes, int64_t rows, int64_t d, int64_t vocab);
 
 /*
@@ -547,40 +558,59 @@ int64_t gpga_embedding_scratch_bytes(int64_t nodes, int64_t rows, int64_t d, int
  * (t * ceil(d/8) + (j >> 3), node0 + i, k, GPGA_STREAM_DROPOUT + site); it is kept iff they are at least q.  So the
  * probability is p to 2^-17, and the factor is the exact inverse of the probability of being kept.  The gradient is the
  * same call on dy.  k: the iteration (0 <= k < 2^32); site: which dropout of the model this is (0 <= site < 2^30);
- * node0: global index of local node 0 (node shards), node0 + nodes <= 2^32.
+ * node0: global index of local node 0 (node shards), node0 + nodes <= 2^32.  p = 0 leaves x as it is; seed, k, site and
+ * node0 are then not looked at.
  */
-int32_t gpga_dropout(const void* x_dev, int64_t ldx, void* y_dev, int64_t ldy, int32_t dtype, int64_t nodes,
-                     int64_t rows, int64_t d, double p, uint64_t seed, int64_t k, int64_t site, int64_t node0,
-                     void* stream);
+typedef struct gpga_dropout_args {
+    const void* x;
+    void* y;
+    int64_t ldx, ldy, dtype, nodes, rows, d;
+    double p;
+    uint64_t seed;
+    int64_t k, site, node0;
+} gpga_dropout_args_t;
+int32_t gpga_dropout(const gpga_dropout_args_t* args, void* stream);
 
 /*
  * Layer norm of z = residual + dropout(x) over the d columns of every row:
  *     mean = sum z / d, rstd = 1 / sqrt(sum (z - mean)^2 / d + eps), y = (z - mean) * rstd * w_i + b_i.
- * residual_dev may be NULL (z = dropout(x)); p = 0 leaves x as it is (seed, k, site, node0 are then not looked at);
- * weight_dev NULL: w = 1; bias_dev NULL: b = 0; parameters of node i at + i * ldw (16-byte accesses where aligned).
- * z_dev (may be NULL) receives z; mean_dev and rstd_dev, nodes * rows fp32 each, what the backward call wants.
- * eps >= 0 and finite.
+ * residual NULL: z = dropout(x); p, seed, k, site, node0 as for gpga_dropout; weight NULL: w = 1; bias NULL: b = 0;
+ * parameters of node i at + i * ldw.  z (may be NULL) receives z; mean and rstd, nodes * rows fp32 each, what the
+ * backward call wants.  eps >= 0 and finite.
  */
-int32_t gpga_layer_norm_forward(const void* x_dev, int64_t ldx, const void* residual_dev, int64_t ldr,
-                                const float* weight_dev, const float* bias_dev, int64_t ldw, void* y_dev, int64_t ldy,
-                                void* z_dev, int64_t ldz, float* mean_dev, float* rstd_dev, int32_t dtype,
-                                int64_t nodes, int64_t rows, int64_t d, float eps, double p, uint64_t seed, int64_t k,
-                                int64_t site, int64_t node0, void* stream);
+typedef struct gpga_layer_norm_forward_args {
+    const void *x, *residual;
+    const float *weight, *bias;
+    void *y, *z;
+    float *mean, *rstd;
+    int64_t ldx, ldr, ldw, ldy, ldz, dtype, nodes, rows, d;
+    double eps;   /* used as fp32 */
+    double p;
+    uint64_t seed;
+    int64_t k, site, node0;
+} gpga_layer_norm_forward_args_t;
+int32_t gpga_layer_norm_forward(const gpga_layer_norm_forward_args_t* args, void* stream);
 
 /*
  * Its gradient.  With xh = (z - mean) rstd, h = w_i dy and means over a row:
  *     dresidual = g = rstd (h - mean(h) - xh mean(h xh)) + dz,   dx = dropout(g) with the forward call's mask,
  *     dw_i = sum over the node's rows of dy xh,                   db_i = sum over the node's rows of dy.
- * dz_dev (may be NULL): gradient that reaches z past the norm (the residual stream).  dx_dev: wanted when p > 0, NULL
- * when p = 0 (dx is g).  dweight_dev, dbias_dev: either may be NULL; node i at + i * lddw; added to what they hold when
- * accumulate is not 0.  scratch: gpga_layer_norm_scratch_bytes(nodes, rows, d) bytes.
+ * dz (may be NULL): gradient that reaches z past the norm (the residual stream).  dx: wanted when p > 0, NULL when
+ * p = 0 (dx is g).  dweight, dbias: either may be NULL; node i at + i * lddw; added to what they hold when accumulate
+ * is not 0.  scratch: gpga_layer_norm_scratch_bytes(nodes, rows, d) bytes.
  */
-int32_t gpga_layer_norm_backward(const void* dy_dev, int64_t lddy, const void* z_dev, int64_t ldz, const void* dz_dev,
-                                 int64_t lddz, const float* mean_dev, const float* rstd_dev, const float* weight_dev,
-                                 int64_t ldw, void* dresidual_dev, int64_t lddr, void* dx_dev, int64_t lddx,
-                                 float* dweight_dev, float* dbias_dev, int64_t lddw, int32_t accumulate, int32_t dtype,
-                                 int64_t nodes, int64_t rows, int64_t d, double p, uint64_t seed, int64_t k,
-                                 int64_t site, int64_t node0, void* scratch_dev, int64_t scratch_bytes, void* stream);
+typedef struct gpga_layer_norm_backward_args {
+    const void *dy, *z, *dz;
+    const float *mean, *rstd, *weight;
+    void *dresidual, *dx;
+    float *dweight, *dbias;
+    void* scratch;
+    int64_t scratch_bytes, lddy, ldz, lddz, ldw, lddr, lddx, lddw, accumulate, dtype, nodes, rows, d;
+    double p;
+    uint64_t seed;
+    int64_t k, site, node0;
+} gpga_layer_norm_backward_args_t;
+int32_t gpga_layer_norm_backward(const gpga_layer_norm_backward_args_t* args, void* stream);
 int64_t gpga_layer_norm_scratch_bytes(int64_t nodes, int64_t rows, int64_t d);
 
 #ifdef __cplusplus

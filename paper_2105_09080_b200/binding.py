@@ -81,16 +81,12 @@ SIGNATURES = {
     "gpga_normal_fill": (_i32, [_u64, _u32, _u32, _u32, _u32, _i64, _P, _P]),
     "gpga_logistic_gradient_noalloc": (_i32, [_P, _P, _P, _i64, _i64, _i64, _i64, _i64, _f32, _u64, _i64,
                                               _P, _P, C.POINTER(_i64)]),
-    "gpga_embedding_forward": (_i32, [_P, _i64, _i64, _P, _i32, _P, _i64, _i32, _i64, _i64, _i64, _i64, _f32, _P]),
-    "gpga_embedding_backward": (_i32, [_P, _i64, _i32, _P, _i32, _P, _i64, _i64, _i64, _i64, _i64, _i64, _f32, _i32,
-                                       _P, _i64, _P]),
+    "gpga_embedding_forward": (_i32, [_P, _P]),
+    "gpga_embedding_backward": (_i32, [_P, _P]),
     "gpga_embedding_scratch_bytes": (_i64, [_i64, _i64, _i64, _i64]),
-    "gpga_dropout": (_i32, [_P, _i64, _P, _i64, _i32, _i64, _i64, _i64, C.c_double, _u64, _i64, _i64, _i64, _P]),
-    "gpga_layer_norm_forward": (_i32, [_P, _i64, _P, _i64, _P, _P, _i64, _P, _i64, _P, _i64, _P, _P, _i32, _i64, _i64,
-                                       _i64, _f32, C.c_double, _u64, _i64, _i64, _i64, _P]),
-    "gpga_layer_norm_backward": (_i32, [_P, _i64, _P, _i64, _P, _i64, _P, _P, _P, _i64, _P, _i64, _P, _i64, _P, _P,
-                                        _i64, _i32, _i32, _i64, _i64, _i64, C.c_double, _u64, _i64, _i64, _i64, _P, _i64,
-                                        _P]),
+    "gpga_dropout": (_i32, [_P, _P]),
+    "gpga_layer_norm_forward": (_i32, [_P, _P]),
+    "gpga_layer_norm_backward": (_i32, [_P, _P]),
     "gpga_layer_norm_scratch_bytes": (_i64, [_i64, _i64, _i64]),
 }
 

@@ -27,13 +27,17 @@ bool sizes_ok(int64_t nodes, int64_t rows, int64_t d)
     return nodes * rows < (int64_t(1) << 31) && rows * chunks < (int64_t(1) << 32) && nodes * rows * chunks <= (int64_t(1) << 38);
 }
 
-int size_of(int32_t dtype) { return dtype == GPGA_DTYPE_F32 ? 4 : dtype == GPGA_DTYPE_BF16 || dtype == GPGA_DTYPE_F16 ? 2 : 0; }
+int size_of(int64_t dtype) { return dtype == GPGA_DTYPE_F32 ? 4 : dtype == GPGA_DTYPE_BF16 || dtype == GPGA_DTYPE_F16 ? 2 : 0; }
 
 bool element_aligned(const void* p, int size) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(size - 1)) == 0; }
 
 // Whether every row of an array that is there starts on 16 bytes.
 bool vectors(const void* p, int64_t ld, int size) { return !p || ((reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (ld * size) % 16 == 0); }
 
+bool vocab_ok(int64_t vocab) { return vocab >= 1 && vocab < (int64_t(1) << 31); }
+
+const char* kAlign = "pointers must be aligned to their element";
+const char* kStrides = "strides must be at least d";
 const char* kSizes = "sizes: need 1 <= nodes <= 65535, rows >= 0, 1 <= d <= 2^20 and the products stated in gpga.h";
 
 // The dropout of a call; nullptr, or what is wrong with its arguments.
@@ -60,145 +64,139 @@ const char* drop_mask(DropMask& m, double p, uint64_t seed, int64_t k, int64_t s
 
 extern "C" {
 
-int32_t gpga_embedding_forward(const float* table_dev, int64_t ldt, int64_t node_ldt, const void* tokens_dev,
-                               int32_t token_bytes, void* out_dev, int64_t ldo, int32_t dtype, int64_t nodes,
-                               int64_t rows, int64_t d, int64_t vocab, float scale, void* stream)
+int32_t gpga_embedding_forward(const gpga_embedding_forward_args_t* a, void* stream)
 {
-    const int size = size_of(dtype);
+    if (!a) return bad("NULL args");
+    const int size = size_of(a->dtype);
     if (!size) return bad("unknown dtype");
-    if (!sizes_ok(nodes, rows, d)) return bad(kSizes);
-    if (vocab < 1 || vocab >= (int64_t(1) << 31)) return bad("vocab must lie in [1, 2^31)");
-    if (token_bytes != 4 && token_bytes != 8) return bad("tokens must have 4 or 8 bytes");
-    if (ldt < d || ldo < d || (nodes > 1 && node_ldt < 0)) return bad("strides: ldt and ldo must be at least d");
-    if (rows == 0) return GPGA_OK;
-    if (!table_dev || !tokens_dev || !out_dev) return bad("NULL pointer");
-    if (!element_aligned(table_dev, 4) || !element_aligned(tokens_dev, token_bytes) || !element_aligned(out_dev, size))
-        return bad("pointers must be aligned to their element");
+    if (!sizes_ok(a->nodes, a->rows, a->d)) return bad(kSizes);
+    if (!vocab_ok(a->vocab)) return bad("vocab must lie in [1, 2^31)");
+    if (a->token_bytes != 4 && a->token_bytes != 8) return bad("tokens must have 4 or 8 bytes");
+    if (a->ldt < a->d || a->ldo < a->d || (a->nodes > 1 && a->node_ldt < 0)) return bad("strides: ldt and ldo must be at least d");
+    if (a->rows == 0) return GPGA_OK;
+    if (!a->table || !a->tokens || !a->out) return bad("NULL pointer");
+    if (!element_aligned(a->table, 4) || !element_aligned(a->tokens, (int)a->token_bytes) || !element_aligned(a->out, size))
+        return bad(kAlign);
     LookupParams p;
-    p.table = table_dev;
-    p.tokens = tokens_dev;
-    p.out = out_dev;
-    p.ldt = ldt;
-    p.node_ldt = node_ldt;
-    p.ldo = ldo;
-    p.nodes = (uint32_t)nodes;
-    p.rows = (uint32_t)rows;
-    p.vocab = (uint32_t)vocab;
-    p.d = (int32_t)d;
-    p.tokens64 = token_bytes == 8;
-    p.scale = scale;
-    return launched(launch_lookup(p, dtype, static_cast<cudaStream_t>(stream)), "gpga_embedding_forward");
+    p.table = a->table;
+    p.tokens = a->tokens;
+    p.out = a->out;
+    p.ldt = a->ldt;
+    p.node_ldt = a->node_ldt;
+    p.ldo = a->ldo;
+    p.nodes = (uint32_t)a->nodes;
+    p.rows = (uint32_t)a->rows;
+    p.vocab = (uint32_t)a->vocab;
+    p.d = (int32_t)a->d;
+    p.tokens64 = a->token_bytes == 8;
+    p.scale = (float)a->scale;
+    return launched(launch_lookup(p, (int)a->dtype, static_cast<cudaStream_t>(stream)), "gpga_embedding_forward");
 }
 
 int64_t gpga_embedding_scratch_bytes(int64_t nodes, int64_t rows, int64_t d, int64_t vocab)
 {
-    if (!sizes_ok(nodes, rows, d) || vocab < 1 || vocab >= (int64_t(1) << 31)) return 0;
-    return lookup_grad_scratch_bytes(nodes, rows, d, vocab);
+    return sizes_ok(nodes, rows, d) && vocab_ok(vocab) ? lookup_grad_scratch_bytes(nodes, rows, d, vocab) : 0;
 }
 
-int32_t gpga_embedding_backward(const void* dout_dev, int64_t ldo, int32_t dtype, const void* tokens_dev,
-                                int32_t token_bytes, float* grad_dev, int64_t ldg, int64_t node_ldg, int64_t nodes,
-                                int64_t rows, int64_t d, int64_t vocab, float scale, int32_t accumulate,
-                                void* scratch_dev, int64_t scratch_bytes, void* stream)
+int32_t gpga_embedding_backward(const gpga_embedding_backward_args_t* a, void* stream)
 {
-    const int size = size_of(dtype);
+    if (!a) return bad("NULL args");
+    const int size = size_of(a->dtype);
     if (!size) return bad("unknown dtype");
-    if (!sizes_ok(nodes, rows, d)) return bad(kSizes);
-    if (vocab < 1 || vocab >= (int64_t(1) << 31)) return bad("vocab must lie in [1, 2^31)");
-    if (token_bytes != 4 && token_bytes != 8) return bad("tokens must have 4 or 8 bytes");
+    if (!sizes_ok(a->nodes, a->rows, a->d)) return bad(kSizes);
+    if (!vocab_ok(a->vocab)) return bad("vocab must lie in [1, 2^31)");
+    if (a->token_bytes != 4 && a->token_bytes != 8) return bad("tokens must have 4 or 8 bytes");
     // rows of grad must not overlap: each has one writer
-    if (ldo < d || ldg < d || (nodes > 1 && node_ldg < (vocab - 1) * ldg + d))
+    if (a->ldo < a->d || a->ldg < a->d || (a->nodes > 1 && a->node_ldg < (a->vocab - 1) * a->ldg + a->d))
         return bad("strides: ldo and ldg must be at least d, node_ldg at least a node's table");
-    if (!grad_dev || (rows && (!dout_dev || !tokens_dev))) return bad("NULL pointer");
-    if (!element_aligned(grad_dev, 4) || !element_aligned(dout_dev, size) || !element_aligned(tokens_dev, token_bytes))
-        return bad("pointers must be aligned to their element");
-    if (!scratch_dev || (reinterpret_cast<uintptr_t>(scratch_dev) & 15u)) return bad("scratch must be 16-byte aligned");
-    if (scratch_bytes < lookup_grad_scratch_bytes(nodes, rows, d, vocab)) return bad("scratch is too small: see gpga_embedding_scratch_bytes");
-    if (rows == 0 && accumulate) return GPGA_OK;
+    if (!a->grad || (a->rows && (!a->dout || !a->tokens))) return bad("NULL pointer");
+    if (!element_aligned(a->grad, 4) || !element_aligned(a->dout, size) || !element_aligned(a->tokens, (int)a->token_bytes))
+        return bad(kAlign);
+    if (!a->scratch || (reinterpret_cast<uintptr_t>(a->scratch) & 15u)) return bad("scratch must be 16-byte aligned");
+    if (a->scratch_bytes < lookup_grad_scratch_bytes(a->nodes, a->rows, a->d, a->vocab))
+        return bad("scratch is too small: see gpga_embedding_scratch_bytes");
+    if (a->rows == 0 && a->accumulate) return GPGA_OK;
     LookupGradParams p;
-    p.dout = dout_dev;
-    p.tokens = tokens_dev;
-    p.grad = grad_dev;
-    p.ldo = ldo;
-    p.ldg = ldg;
-    p.node_ldg = node_ldg;
-    p.nodes = (uint32_t)nodes;
-    p.rows = (uint32_t)rows;
-    p.vocab = (uint32_t)vocab;
-    p.d = (int32_t)d;
-    p.tokens64 = token_bytes == 8;
-    p.accumulate = accumulate != 0;
-    p.scale = scale;
-    p.scratch = static_cast<char*>(scratch_dev);
-    return launched(launch_lookup_grad(p, dtype, static_cast<cudaStream_t>(stream)), "gpga_embedding_backward");
+    p.dout = a->dout;
+    p.tokens = a->tokens;
+    p.grad = a->grad;
+    p.ldo = a->ldo;
+    p.ldg = a->ldg;
+    p.node_ldg = a->node_ldg;
+    p.nodes = (uint32_t)a->nodes;
+    p.rows = (uint32_t)a->rows;
+    p.vocab = (uint32_t)a->vocab;
+    p.d = (int32_t)a->d;
+    p.tokens64 = a->token_bytes == 8;
+    p.accumulate = a->accumulate != 0;
+    p.scale = (float)a->scale;
+    p.scratch = static_cast<char*>(a->scratch);
+    return launched(launch_lookup_grad(p, (int)a->dtype, static_cast<cudaStream_t>(stream)), "gpga_embedding_backward");
 }
 
-int32_t gpga_dropout(const void* x_dev, int64_t ldx, void* y_dev, int64_t ldy, int32_t dtype, int64_t nodes,
-                     int64_t rows, int64_t d, double p, uint64_t seed, int64_t k, int64_t site, int64_t node0,
-                     void* stream)
+int32_t gpga_dropout(const gpga_dropout_args_t* a, void* stream)
 {
-    const int size = size_of(dtype);
+    if (!a) return bad("NULL args");
+    const int size = size_of(a->dtype);
     if (!size) return bad("unknown dtype");
-    if (!sizes_ok(nodes, rows, d)) return bad(kSizes);
-    if (ldx < d || ldy < d) return bad("strides must be at least d");
+    if (!sizes_ok(a->nodes, a->rows, a->d)) return bad(kSizes);
+    if (a->ldx < a->d || a->ldy < a->d) return bad(kStrides);
     DropoutParams q;
-    if (const char* text = drop_mask(q.mask, p, seed, k, site, node0, nodes)) return bad(text);
-    if (rows == 0) return GPGA_OK;
-    if (!x_dev || !y_dev) return bad("NULL pointer");
-    if (!element_aligned(x_dev, size) || !element_aligned(y_dev, size)) return bad("pointers must be aligned to their element");
-    q.x = x_dev;
-    q.y = y_dev;
-    q.ldx = ldx;
-    q.ldy = ldy;
-    q.nodes = (uint32_t)nodes;
-    q.rows = (uint32_t)rows;
-    q.d = (int32_t)d;
-    const bool vec = d % kChunk == 0 && vectors(x_dev, ldx, size) && vectors(y_dev, ldy, size);
-    return launched(launch_dropout(q, dtype, vec, static_cast<cudaStream_t>(stream)), "gpga_dropout");
+    if (const char* text = drop_mask(q.mask, a->p, a->seed, a->k, a->site, a->node0, a->nodes)) return bad(text);
+    if (a->rows == 0) return GPGA_OK;
+    if (!a->x || !a->y) return bad("NULL pointer");
+    if (!element_aligned(a->x, size) || !element_aligned(a->y, size)) return bad(kAlign);
+    q.x = a->x;
+    q.y = a->y;
+    q.ldx = a->ldx;
+    q.ldy = a->ldy;
+    q.nodes = (uint32_t)a->nodes;
+    q.rows = (uint32_t)a->rows;
+    q.d = (int32_t)a->d;
+    const bool vec = a->d % kChunk == 0 && vectors(a->x, a->ldx, size) && vectors(a->y, a->ldy, size);
+    return launched(launch_dropout(q, (int)a->dtype, vec, static_cast<cudaStream_t>(stream)), "gpga_dropout");
 }
 
-int32_t gpga_layer_norm_forward(const void* x_dev, int64_t ldx, const void* residual_dev, int64_t ldr,
-                                const float* weight_dev, const float* bias_dev, int64_t ldw, void* y_dev, int64_t ldy,
-                                void* z_dev, int64_t ldz, float* mean_dev, float* rstd_dev, int32_t dtype,
-                                int64_t nodes, int64_t rows, int64_t d, float eps, double p, uint64_t seed, int64_t k,
-                                int64_t site, int64_t node0, void* stream)
+int32_t gpga_layer_norm_forward(const gpga_layer_norm_forward_args_t* a, void* stream)
 {
-    const int size = size_of(dtype);
+    if (!a) return bad("NULL args");
+    const int size = size_of(a->dtype);
     if (!size) return bad("unknown dtype");
-    if (!sizes_ok(nodes, rows, d)) return bad(kSizes);
-    if (ldx < d || ldy < d || (residual_dev && ldr < d) || (z_dev && ldz < d)) return bad("strides must be at least d");
-    if (nodes > 1 && (weight_dev || bias_dev) && ldw < 0) return bad("ldw must not be negative");
+    if (!sizes_ok(a->nodes, a->rows, a->d)) return bad(kSizes);
+    if (a->ldx < a->d || a->ldy < a->d || (a->residual && a->ldr < a->d) || (a->z && a->ldz < a->d)) return bad(kStrides);
+    if (a->nodes > 1 && (a->weight || a->bias) && a->ldw < 0) return bad("ldw must not be negative");
+    const float eps = (float)a->eps;
     if (!(eps >= 0.f) || std::isinf(eps)) return bad("eps must be finite and not negative");
     NormForwardParams q;
-    if (const char* text = drop_mask(q.mask, p, seed, k, site, node0, nodes)) return bad(text);
-    if (rows == 0) return GPGA_OK;
-    if (!x_dev || !y_dev || !mean_dev || !rstd_dev) return bad("NULL pointer");
-    if (!element_aligned(x_dev, size) || !element_aligned(residual_dev, size) || !element_aligned(y_dev, size) ||
-        !element_aligned(z_dev, size) || !element_aligned(weight_dev, 4) || !element_aligned(bias_dev, 4) ||
-        !element_aligned(mean_dev, 4) || !element_aligned(rstd_dev, 4))
-        return bad("pointers must be aligned to their element");
-    q.x = x_dev;
-    q.residual = residual_dev;
-    q.weight = weight_dev;
-    q.bias = bias_dev;
-    q.y = y_dev;
-    q.z = z_dev;
-    q.mean = mean_dev;
-    q.rstd = rstd_dev;
-    q.ldx = ldx;
-    q.ldr = ldr;
-    q.ldy = ldy;
-    q.ldz = ldz;
-    q.ldw = ldw;
-    q.nodes = (uint32_t)nodes;
-    q.rows = (uint32_t)rows;
-    q.d = (int32_t)d;
+    if (const char* text = drop_mask(q.mask, a->p, a->seed, a->k, a->site, a->node0, a->nodes)) return bad(text);
+    if (a->rows == 0) return GPGA_OK;
+    if (!a->x || !a->y || !a->mean || !a->rstd) return bad("NULL pointer");
+    if (!element_aligned(a->x, size) || !element_aligned(a->residual, size) || !element_aligned(a->y, size) ||
+        !element_aligned(a->z, size) || !element_aligned(a->weight, 4) || !element_aligned(a->bias, 4) ||
+        !element_aligned(a->mean, 4) || !element_aligned(a->rstd, 4))
+        return bad(kAlign);
+    q.x = a->x;
+    q.residual = a->residual;
+    q.weight = a->weight;
+    q.bias = a->bias;
+    q.y = a->y;
+    q.z = a->z;
+    q.mean = a->mean;
+    q.rstd = a->rstd;
+    q.ldx = a->ldx;
+    q.ldr = a->ldr;
+    q.ldy = a->ldy;
+    q.ldz = a->ldz;
+    q.ldw = a->ldw;
+    q.nodes = (uint32_t)a->nodes;
+    q.rows = (uint32_t)a->rows;
+    q.d = (int32_t)a->d;
     q.eps = eps;
-    const bool full = d % kChunk == 0;
-    q.wvec = full && vectors(weight_dev, ldw, 4) && vectors(bias_dev, ldw, 4);
-    const bool vec = full && vectors(x_dev, ldx, size) && vectors(residual_dev, ldr, size) && vectors(y_dev, ldy, size) &&
-                     vectors(z_dev, ldz, size);
-    return launched(launch_norm_forward(q, dtype, vec, static_cast<cudaStream_t>(stream)), "gpga_layer_norm_forward");
+    const bool full = a->d % kChunk == 0;
+    q.wvec = full && vectors(a->weight, a->ldw, 4) && vectors(a->bias, a->ldw, 4);
+    const bool vec = full && vectors(a->x, a->ldx, size) && vectors(a->residual, a->ldr, size) && vectors(a->y, a->ldy, size) &&
+                     vectors(a->z, a->ldz, size);
+    return launched(launch_norm_forward(q, (int)a->dtype, vec, static_cast<cudaStream_t>(stream)), "gpga_layer_norm_forward");
 }
 
 int64_t gpga_layer_norm_scratch_bytes(int64_t nodes, int64_t rows, int64_t d)
@@ -208,59 +206,56 @@ int64_t gpga_layer_norm_scratch_bytes(int64_t nodes, int64_t rows, int64_t d)
     return splits > 1 ? nodes * splits * 2 * d * 4 : 0;
 }
 
-int32_t gpga_layer_norm_backward(const void* dy_dev, int64_t lddy, const void* z_dev, int64_t ldz, const void* dz_dev,
-                                 int64_t lddz, const float* mean_dev, const float* rstd_dev, const float* weight_dev,
-                                 int64_t ldw, void* dresidual_dev, int64_t lddr, void* dx_dev, int64_t lddx,
-                                 float* dweight_dev, float* dbias_dev, int64_t lddw, int32_t accumulate, int32_t dtype,
-                                 int64_t nodes, int64_t rows, int64_t d, double p, uint64_t seed, int64_t k,
-                                 int64_t site, int64_t node0, void* scratch_dev, int64_t scratch_bytes, void* stream)
+int32_t gpga_layer_norm_backward(const gpga_layer_norm_backward_args_t* a, void* stream)
 {
-    const int size = size_of(dtype);
+    if (!a) return bad("NULL args");
+    const int size = size_of(a->dtype);
     if (!size) return bad("unknown dtype");
-    if (!sizes_ok(nodes, rows, d)) return bad(kSizes);
-    if (lddy < d || ldz < d || (dz_dev && lddz < d) || lddr < d || (dx_dev && lddx < d)) return bad("strides must be at least d");
-    if (nodes > 1 && weight_dev && ldw < 0) return bad("ldw must not be negative");
-    if (nodes > 1 && (dweight_dev || dbias_dev) && lddw < d) return bad("lddw must be at least d");
+    if (!sizes_ok(a->nodes, a->rows, a->d)) return bad(kSizes);
+    if (a->lddy < a->d || a->ldz < a->d || (a->dz && a->lddz < a->d) || a->lddr < a->d || (a->dx && a->lddx < a->d))
+        return bad(kStrides);
+    if (a->nodes > 1 && a->weight && a->ldw < 0) return bad("ldw must not be negative");
+    if (a->nodes > 1 && (a->dweight || a->dbias) && a->lddw < a->d) return bad("lddw must be at least d");
     NormBackwardParams q;
-    if (const char* text = drop_mask(q.mask, p, seed, k, site, node0, nodes)) return bad(text);
-    if ((p > 0.0) != (dx_dev != nullptr) && (rows || p == 0.0)) return bad("dx is wanted exactly when p > 0");
-    if (rows && (!dy_dev || !z_dev || !mean_dev || !rstd_dev || !dresidual_dev)) return bad("NULL pointer");
-    if (!element_aligned(dy_dev, size) || !element_aligned(z_dev, size) || !element_aligned(dz_dev, size) ||
-        !element_aligned(dresidual_dev, size) || !element_aligned(dx_dev, size) || !element_aligned(mean_dev, 4) ||
-        !element_aligned(rstd_dev, 4) || !element_aligned(weight_dev, 4) || !element_aligned(dweight_dev, 4) ||
-        !element_aligned(dbias_dev, 4))
-        return bad("pointers must be aligned to their element");
-    const int64_t need = gpga_layer_norm_scratch_bytes(nodes, rows, d);
-    if (need && (!scratch_dev || (reinterpret_cast<uintptr_t>(scratch_dev) & 15u))) return bad("scratch must be 16-byte aligned");
-    if (scratch_bytes < need) return bad("scratch is too small: see gpga_layer_norm_scratch_bytes");
-    q.dy = dy_dev;
-    q.z = z_dev;
-    q.dz = dz_dev;
-    q.mean = mean_dev;
-    q.rstd = rstd_dev;
-    q.weight = weight_dev;
-    q.dres = dresidual_dev;
-    q.dx = dx_dev;
-    q.dweight = dweight_dev;
-    q.dbias = dbias_dev;
-    q.partial = static_cast<float*>(scratch_dev);
-    q.lddy = lddy;
-    q.ldz = ldz;
-    q.lddz = lddz;
-    q.lddres = lddr;
-    q.lddx = lddx;
-    q.ldw = ldw;
-    q.lddw = lddw;
-    q.nodes = (uint32_t)nodes;
-    q.rows = (uint32_t)rows;
-    q.d = (int32_t)d;
-    q.splits = norm_backward_splits(nodes, rows, d);
-    q.accumulate = accumulate != 0;
-    const bool full = d % kChunk == 0;
-    q.wvec = full && vectors(weight_dev, ldw, 4);
-    const bool vec = full && vectors(dy_dev, lddy, size) && vectors(z_dev, ldz, size) && vectors(dz_dev, lddz, size) &&
-                     vectors(dresidual_dev, lddr, size) && vectors(dx_dev, lddx, size);
-    return launched(launch_norm_backward(q, dtype, vec, static_cast<cudaStream_t>(stream)), "gpga_layer_norm_backward");
+    if (const char* text = drop_mask(q.mask, a->p, a->seed, a->k, a->site, a->node0, a->nodes)) return bad(text);
+    if ((a->p > 0.0) != (a->dx != nullptr) && (a->rows || a->p == 0.0)) return bad("dx is wanted exactly when p > 0");
+    if (a->rows && (!a->dy || !a->z || !a->mean || !a->rstd || !a->dresidual)) return bad("NULL pointer");
+    if (!element_aligned(a->dy, size) || !element_aligned(a->z, size) || !element_aligned(a->dz, size) ||
+        !element_aligned(a->dresidual, size) || !element_aligned(a->dx, size) || !element_aligned(a->mean, 4) ||
+        !element_aligned(a->rstd, 4) || !element_aligned(a->weight, 4) || !element_aligned(a->dweight, 4) ||
+        !element_aligned(a->dbias, 4))
+        return bad(kAlign);
+    const int64_t need = gpga_layer_norm_scratch_bytes(a->nodes, a->rows, a->d);
+    if (need && (!a->scratch || (reinterpret_cast<uintptr_t>(a->scratch) & 15u))) return bad("scratch must be 16-byte aligned");
+    if (a->scratch_bytes < need) return bad("scratch is too small: see gpga_layer_norm_scratch_bytes");
+    q.dy = a->dy;
+    q.z = a->z;
+    q.dz = a->dz;
+    q.mean = a->mean;
+    q.rstd = a->rstd;
+    q.weight = a->weight;
+    q.dres = a->dresidual;
+    q.dx = a->dx;
+    q.dweight = a->dweight;
+    q.dbias = a->dbias;
+    q.partial = static_cast<float*>(a->scratch);
+    q.lddy = a->lddy;
+    q.ldz = a->ldz;
+    q.lddz = a->lddz;
+    q.lddres = a->lddr;
+    q.lddx = a->lddx;
+    q.ldw = a->ldw;
+    q.lddw = a->lddw;
+    q.nodes = (uint32_t)a->nodes;
+    q.rows = (uint32_t)a->rows;
+    q.d = (int32_t)a->d;
+    q.splits = norm_backward_splits(a->nodes, a->rows, a->d);
+    q.accumulate = a->accumulate != 0;
+    const bool full = a->d % kChunk == 0;
+    q.wvec = full && vectors(a->weight, a->ldw, 4);
+    const bool vec = full && vectors(a->dy, a->lddy, size) && vectors(a->z, a->ldz, size) && vectors(a->dz, a->lddz, size) &&
+                     vectors(a->dresidual, a->lddr, size) && vectors(a->dx, a->lddx, size);
+    return launched(launch_norm_backward(q, (int)a->dtype, vec, static_cast<cudaStream_t>(stream)), "gpga_layer_norm_backward");
 }
 
 }  // extern "C"

@@ -15,7 +15,8 @@ streams is the caller's part.
 """
 from __future__ import annotations
 
-import contextlib
+import functools
+import struct
 
 import torch
 
@@ -24,16 +25,63 @@ from .binding import GPGA_ERR_INVALID_ARG, GPGA_OK, GpgaError, lib
 GPGA_DTYPE_F32, GPGA_DTYPE_BF16, GPGA_DTYPE_F16 = 0, 1, 2
 _DTYPE = {torch.float32: GPGA_DTYPE_F32, torch.bfloat16: GPGA_DTYPE_BF16, torch.float16: GPGA_DTYPE_F16}
 _TOKEN_BYTES = {torch.int32: 4, torch.int64: 8}
-_nothing = contextlib.nullcontext()
+
+# The argument structs of include/gpga.h, packed in one go (a small call's time is its marshalling): Q device pointer or
+# seed, q size or stride, d double.
+ARGS = {
+    "gpga_embedding_forward": struct.Struct("=3Q9qd"),
+    "gpga_embedding_backward": struct.Struct("=4Q11qd"),
+    "gpga_dropout": struct.Struct("=2Q6qdQ3q"),
+    "gpga_layer_norm_forward": struct.Struct("=8Q9q2dQ3q"),
+    "gpga_layer_norm_backward": struct.Struct("=11Q13qdQ3q"),
+}
+
+_current_device = torch.cuda.current_device
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _bad(text):
     raise GpgaError(GPGA_ERR_INVALID_ARG, text)
 
 
-def _check(st):
-    if st != GPGA_OK:
-        raise GpgaError(st, lib().gpga_last_error(None).decode())
+@functools.lru_cache(maxsize=None)
+def _entry(name):
+    """What calls a C entry on the current stream of a device with the members of its argument struct."""
+    fn, pack, L = getattr(lib(), name), ARGS[name].pack, lib()
+
+    def call(device, *members):
+        if device != _current_device():
+            _bad(f"tensors live on cuda:{device} but cuda:{_current_device()} is current")
+        try:
+            args = pack(*members)
+        except struct.error as e:
+            _bad(f"argument out of range: {e}")
+        st = fn(args, _raw_stream(device))
+        if st != GPGA_OK:
+            raise GpgaError(st, L.gpga_last_error(None).decode())
+    return call
+
+
+@functools.lru_cache(maxsize=4096)
+def _embedding_scratch(nodes, rows, d, vocab):
+    return lib().gpga_embedding_scratch_bytes(nodes, rows, d, vocab)
+
+
+@functools.lru_cache(maxsize=4096)
+def _norm_scratch(nodes, rows, d):
+    return lib().gpga_layer_norm_scratch_bytes(nodes, rows, d)
+
+
+def _on_stream(fn, args):
+    """The same call with ``stream`` as the current stream; tensors of another stream are marked for the allocator."""
+    stream = args.pop("stream")
+    s = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
+    if s.cuda_stream != torch.cuda.current_stream(s.device).cuda_stream:
+        for t in args.values():
+            if isinstance(t, torch.Tensor) and t.is_cuda:
+                t.record_stream(s)
+    with torch.cuda.stream(s):
+        return fn(**args)
 
 
 def _spacing(t):
@@ -55,88 +103,66 @@ def _spacing(t):
     return t.shape[-1] if ld is None else ld
 
 
-def _act(t, what, like, dtype=None):
-    """Pointer and spacing of an activation that must have the shape (and type) of ``like``; None gives NULL."""
-    if t is None:
-        return None, 0
-    if t.dtype != (dtype or like.dtype) or t.shape != like.shape or t.device != like.device:
-        _bad(f"{what}: got {tuple(t.shape)} {t.dtype} on {t.device}, want {tuple(like.shape)} {dtype or like.dtype} on {like.device}")
-    return t.data_ptr(), _spacing(t)
+def _same(t, what, shape, dtype, device, d):
+    """Spacing of an activation that must have this shape and type."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
+        _bad(f"{what}: got {tuple(t.shape)} {t.dtype} on {t.device}, want {tuple(shape)} {dtype} on cuda:{device}")
+    return d if t.is_contiguous() else _spacing(t)
 
 
-def _stats(t, what, like):
-    """Pointer of a dense float32 vector of one value per row of ``like``."""
-    if t.dtype != torch.float32 or t.numel() * like.shape[-1] != like.numel() or not t.is_contiguous() or t.device != like.device:
-        _bad(f"{what} must be contiguous float32, one value per row, on {like.device}")
+def _stats(t, what, vectors, device):
+    """Pointer of a dense float32 vector of one value per row."""
+    if t.dtype is not torch.float32 or t.numel() != vectors or t.get_device() != device or not t.is_contiguous():
+        _bad(f"{what} must be contiguous float32 on cuda:{device}, {vectors} values (one per row)")
     return t.data_ptr()
 
 
 def _params(t, what, nodes, d, device):
-    """Pointer and node stride of a float32 parameter (d,) or (nodes, d); None gives NULL."""
-    if t is None:
-        return None, 0
-    if t.dtype != torch.float32 or t.device != device or t.shape[-1] != d or t.numel() != nodes * d or t.dim() > 2 \
-            or (t.stride(-1) != 1 and d > 1):
-        _bad(f"{what}: got {tuple(t.shape)} {t.dtype} on {t.device}, want dense float32 rows of ({nodes}, {d}) on {device}")
-    return t.data_ptr(), (t.stride(0) if t.dim() == 2 and nodes > 1 else d)
+    """Node stride of a float32 parameter (d,) or (nodes, d)."""
+    if t.dtype is not torch.float32 or t.get_device() != device or t.numel() != nodes * d or t.shape[-1] != d or t.dim() > 2:
+        _bad(f"{what}: got {tuple(t.shape)} {t.dtype} on {t.device}, want float32 ({nodes}, {d}) on cuda:{device}")
+    if t.is_contiguous():
+        return d
+    if t.stride(-1) != 1 and d > 1:
+        _bad(f"{what}: rows must be dense, got strides {t.stride()}")
+    return t.stride(0) if nodes > 1 else d
 
 
 def _table(t, what, tokens):
-    """(nodes, vocab, d, row stride, node stride) of a table (vocab, d) or (nodes, vocab, d)."""
-    if t.dtype != torch.float32 or t.dim() not in (2, 3) or not t.is_cuda or (t.stride(-1) != 1 and t.shape[-1] > 1):
-        _bad(f"{what} must be a float32 CUDA tensor (vocab, d) or (nodes, vocab, d) with dense rows, got {tuple(t.shape)} {t.dtype}")
-    if tokens.dtype not in _TOKEN_BYTES or not tokens.is_contiguous() or tokens.device != t.device:
+    """(device, nodes, vocab, d, row stride, node stride) of a table (vocab, d) or (nodes, vocab, d)."""
+    shape, device = t.shape, t.get_device()
+    if t.dtype is not torch.float32 or len(shape) not in (2, 3) or device < 0 or 0 in shape:
+        _bad(f"{what} must be a float32 CUDA tensor (vocab, d) or (nodes, vocab, d), got {tuple(shape)} {t.dtype} on {t.device}")
+    if tokens.dtype not in _TOKEN_BYTES or tokens.get_device() != device or not tokens.is_contiguous():
         _bad(f"tokens must be contiguous int32 or int64 on {t.device}, got {tokens.dtype} on {tokens.device}")
-    if t.dim() == 2:
-        return 1, t.shape[0], t.shape[1], max(t.stride(0), t.shape[1]) if t.shape[0] == 1 else t.stride(0), 0
-    if tokens.dim() < 1 or tokens.shape[0] != t.shape[0]:
-        _bad(f"tokens must be (nodes, ...) with nodes = {t.shape[0]}, got {tuple(tokens.shape)}")
-    n, vocab, d = t.shape
-    ld = max(t.stride(1), d) if vocab == 1 else t.stride(1)
-    return n, vocab, d, ld, (max(t.stride(0), (vocab - 1) * ld + d) if n == 1 else t.stride(0))
+    vocab, d = shape[-2:]
+    nodes = shape[0] if len(shape) == 3 else 1
+    if len(shape) == 3 and (tokens.dim() < 1 or tokens.shape[0] != nodes):
+        _bad(f"tokens must be (nodes, ...) with nodes = {nodes}, got {tuple(tokens.shape)}")
+    if t.is_contiguous():
+        return device, nodes, vocab, d, d, vocab * d
+    stride = t.stride()
+    if stride[-1] != 1 and d > 1:
+        _bad(f"{what}: rows must be dense, got strides {stride}")
+    ld = stride[-2] if vocab > 1 else d
+    return device, nodes, vocab, d, ld, stride[0] if nodes > 1 else vocab * ld
 
 
-def _on(stream, *tensors):
-    """Stream pointer of a launch; the tensors' device must be current.  Tensors used on a stream that is not the
-    current one are marked for the allocator."""
-    index = tensors[0].device.index
-    if torch.cuda.current_device() != index:
-        _bad(f"tensors live on {tensors[0].device} but cuda:{torch.cuda.current_device()} is current")
-    if stream is None:
-        return torch.cuda.current_stream(index).cuda_stream
-    s = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
-    if s.cuda_stream != torch.cuda.current_stream(index).cuda_stream:
-        for t in tensors:
-            if t is not None:
-                t.record_stream(s)
-    return s.cuda_stream
-
-
-def _owner(stream):
-    """Where new tensors of a call are allocated: the launch's stream."""
-    if stream is None:
-        return _nothing
-    return torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
-
-
-def _scratch(need, scratch, device):
-    if scratch is None:
-        return torch.empty(need, dtype=torch.uint8, device=device)
-    if scratch.device != device or not scratch.is_contiguous():
-        _bad(f"scratch must be contiguous on {device}")
-    return scratch
-
-
-def _rows(x, nodes):
-    """Activation checks: (rows per node, d, dtype code)."""
-    dtype = _DTYPE.get(x.dtype)
-    if dtype is None or not x.is_cuda or x.dim() < 1 or x.shape[-1] < 1:
-        _bad(f"activations must be float32, bfloat16 or float16 CUDA tensors (..., d), got {tuple(x.shape)} {x.dtype} on {x.device}")
-    d = x.shape[-1]
+def _vectors(x, nodes):
+    """Checks of the activation that a call goes by: (shape, type, its code, device, d, rows per node)."""
+    dtype, shape, device = x.dtype, x.shape, x.get_device()
+    code = _DTYPE.get(dtype)
+    if code is None or device < 0 or not shape or not shape[-1]:
+        _bad(f"activations must be float32, bfloat16 or float16 CUDA tensors (..., d), got {tuple(shape)} {dtype} on {x.device}")
+    d = shape[-1]
     vectors = x.numel() // d
     if nodes < 1 or vectors % nodes:
         _bad(f"{vectors} vectors do not split over {nodes} nodes")
-    return vectors // nodes, d, dtype
+    return shape, dtype, code, device, d, vectors // nodes
+
+
+def _like(x):
+    return torch.empty_like(x, memory_format=torch.contiguous_format)
 
 
 def embedding_forward(table, tokens, scale=1.0, dtype=None, out=None, stream=None):
@@ -145,18 +171,18 @@ def embedding_forward(table, tokens, scale=1.0, dtype=None, out=None, stream=Non
     ``table`` (V, d) with ``tokens`` of any shape, or (n, V, d) with tokens (n, ...): node i looks up in table[i].
     Tokens outside [0, V) give zero rows.  ``dtype``: of the new output (default float32); ``out``: write here.
     """
-    nodes, vocab, d, ldt, node_ldt = _table(table, "table", tokens)
+    if stream is not None:
+        return _on_stream(embedding_forward, locals())
+    device, nodes, vocab, d, ldt, node_ldt = _table(table, "table", tokens)
+    shape = tokens.shape + (d,)
     if out is None:
-        with _owner(stream):
-            out = torch.empty(tokens.shape + (d,), dtype=dtype or torch.float32, device=table.device)
-    elif out.shape != tokens.shape + (d,) or out.device != table.device or (dtype is not None and out.dtype != dtype):
-        _bad(f"out: got {tuple(out.shape)} {out.dtype}, want {tuple(tokens.shape) + (d,)} on {table.device}")
+        out = table.new_empty(shape, dtype=dtype or torch.float32)
     code = _DTYPE.get(out.dtype)
     if code is None:
         _bad(f"out must be float32, bfloat16 or float16, got {out.dtype}")
-    _check(lib().gpga_embedding_forward(table.data_ptr(), ldt, node_ldt, tokens.data_ptr(), _TOKEN_BYTES[tokens.dtype],
-                                        out.data_ptr(), _spacing(out), code, nodes, tokens.numel() // nodes, d, vocab,
-                                        scale, _on(stream, table, tokens, out)))
+    ldo = _same(out, "out", shape, dtype or out.dtype, device, d)
+    _entry("gpga_embedding_forward")(device, table.data_ptr(), tokens.data_ptr(), out.data_ptr(), ldt, node_ldt, ldo,
+                                     _TOKEN_BYTES[tokens.dtype], code, nodes, tokens.numel() // nodes, d, vocab, scale)
     return out
 
 
@@ -165,17 +191,21 @@ def embedding_backward(dout, tokens, grad_table, scale=1.0, accumulate=False, sc
 
     ``grad_table`` has the table's shape, float32, and is returned; without ``accumulate`` all of its rows are written.
     """
-    nodes, vocab, d, ldg, node_ldg = _table(grad_table, "grad_table", tokens)
+    if stream is not None:
+        return _on_stream(embedding_backward, locals())
+    device, nodes, vocab, d, ldg, node_ldg = _table(grad_table, "grad_table", tokens)
     code = _DTYPE.get(dout.dtype)
-    if code is None or dout.shape != tokens.shape + (d,) or dout.device != grad_table.device:
-        _bad(f"dout: got {tuple(dout.shape)} {dout.dtype} on {dout.device}, want {tuple(tokens.shape) + (d,)} on {grad_table.device}")
+    if code is None:
+        _bad(f"dout must be float32, bfloat16 or float16, got {dout.dtype}")
+    ldo = _same(dout, "dout", tokens.shape + (d,), dout.dtype, device, d)
     rows = tokens.numel() // nodes
-    with _owner(stream):
-        scratch = _scratch(lib().gpga_embedding_scratch_bytes(nodes, rows, d, vocab), scratch, dout.device)
-    _check(lib().gpga_embedding_backward(dout.data_ptr(), _spacing(dout), code, tokens.data_ptr(), _TOKEN_BYTES[tokens.dtype],
-                                         grad_table.data_ptr(), ldg, node_ldg, nodes, rows, d, vocab, scale, accumulate,
-                                         scratch.data_ptr(), scratch.numel() * scratch.element_size(),
-                                         _on(stream, dout, tokens, grad_table, scratch)))
+    if scratch is None:
+        scratch = dout.new_empty(_embedding_scratch(nodes, rows, d, vocab), dtype=torch.uint8)
+    elif scratch.get_device() != device or not scratch.is_contiguous():
+        _bad(f"scratch must be contiguous on cuda:{device}")
+    _entry("gpga_embedding_backward")(device, dout.data_ptr(), tokens.data_ptr(), grad_table.data_ptr(), scratch.data_ptr(),
+                                      scratch.nbytes, ldo, ldg, node_ldg, _TOKEN_BYTES[tokens.dtype], code, nodes, rows, d,
+                                      vocab, accumulate, scale)
     return grad_table
 
 
@@ -185,13 +215,14 @@ def dropout(x, p, seed, k=0, site=0, node0=0, nodes=1, out=None, stream=None):
     The mask is a function of (seed, k, site, node, row of the node, column); the gradient is the same call on the
     output's gradient.  ``out`` may be ``x``.
     """
-    rows, d, dtype = _rows(x, nodes)
+    if stream is not None:
+        return _on_stream(dropout, locals())
+    shape, dtype, code, device, d, rows = _vectors(x, nodes)
     if out is None:
-        with _owner(stream):
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    yp, ldy = _act(out, "out", x)
-    _check(lib().gpga_dropout(x.data_ptr(), _spacing(x), yp, ldy, dtype, nodes, rows, d, p, seed, k, site, node0,
-                              _on(stream, x, out)))
+        out = _like(x)
+    ldy = _same(out, "out", shape, dtype, device, d)
+    _entry("gpga_dropout")(device, x.data_ptr(), out.data_ptr(), d if x.is_contiguous() else _spacing(x), ldy, code, nodes, rows,
+                           d, p, seed, k, site, node0)
     return out
 
 
@@ -208,30 +239,37 @@ def layer_norm_forward(x, weight, bias, eps=1e-5, residual=None, p=0.0, seed=0, 
     ``weight`` and ``bias``: (d,), (nodes, d) or None.  z is ``x`` itself where there is neither a residual nor
     dropout.  mean and rstd: one float32 per row.  What the backward call wants is z, mean and rstd.
     """
+    if stream is not None:
+        return _on_stream(layer_norm_forward, locals())
     nodes = _nodes_of(weight, nodes)
-    rows, d, dtype = _rows(x, nodes)
-    mixed = residual is not None or p > 0
-    with _owner(stream):
-        if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        if z is None and mixed:
-            z = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        if mean is None:
-            mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-        if rstd is None:
-            rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-    wp, ldw = _params(weight, "weight", nodes, d, x.device)
-    bp, ldb = _params(bias, "bias", nodes, d, x.device)
-    if bp is not None and wp is not None and ldb != ldw:
-        _bad("weight and bias must have one node stride")
-    rp, ldr = _act(residual, "residual", x)
-    yp, ldy = _act(out, "out", x)
-    zp, ldz = _act(z, "z", x)
-    _check(lib().gpga_layer_norm_forward(x.data_ptr(), _spacing(x), rp, ldr, wp, bp, ldw if wp is not None else ldb, yp, ldy,
-                                         zp, ldz, _stats(mean, "mean", x), _stats(rstd, "rstd", x), dtype, nodes, rows, d, eps,
-                                         p, seed, k, site, node0,
-                                         _on(stream, x, residual, weight, bias, out, z, mean, rstd)))
-    return out, (z if z is not None else x), mean, rstd
+    shape, dtype, code, device, d, rows = _vectors(x, nodes)
+    if out is None:
+        out = _like(x)
+    if z is None and (residual is not None or p > 0):
+        z = _like(x)
+    if mean is None:
+        mean = x.new_empty(shape[:-1], dtype=torch.float32)
+    if rstd is None:
+        rstd = x.new_empty(shape[:-1], dtype=torch.float32)
+    wp = bp = rp = zp = ldw = ldr = ldz = 0
+    if weight is not None:
+        wp, ldw = weight.data_ptr(), _params(weight, "weight", nodes, d, device)
+    if bias is not None:
+        bp, ldb = bias.data_ptr(), _params(bias, "bias", nodes, d, device)
+        if weight is None:
+            ldw = ldb
+        elif ldb != ldw:
+            _bad("weight and bias must have one node stride")
+    if residual is not None:
+        rp, ldr = residual.data_ptr(), _same(residual, "residual", shape, dtype, device, d)
+    if z is not None:
+        zp, ldz = z.data_ptr(), _same(z, "z", shape, dtype, device, d)
+    _entry("gpga_layer_norm_forward")(device, x.data_ptr(), rp, wp, bp, out.data_ptr(), zp,
+                                      _stats(mean, "mean", nodes * rows, device), _stats(rstd, "rstd", nodes * rows, device),
+                                      d if x.is_contiguous() else _spacing(x), ldr, ldw,
+                                      _same(out, "out", shape, dtype, device, d), ldz, code, nodes, rows, d, eps, p, seed, k,
+                                      site, node0)
+    return out, (x if z is None else z), mean, rstd
 
 
 def layer_norm_backward(dy, z, mean, rstd, weight, dz=None, p=0.0, seed=0, k=0, site=0, node0=0, nodes=None,
@@ -242,33 +280,49 @@ def layer_norm_backward(dy, z, mean, rstd, weight, dz=None, p=0.0, seed=0, k=0, 
     each node's rows, added to what the given tensors hold with ``accumulate``; without a weight they are None unless
     given.
     """
+    if stream is not None:
+        return _on_stream(layer_norm_backward, locals())
     nodes = _nodes_of(weight, nodes)
-    rows, d, dtype = _rows(z, nodes)
+    shape, dtype, code, device, d, rows = _vectors(z, nodes)
     if accumulate and (dweight is None or dbias is None):
         _bad("accumulate wants dweight and dbias")
-    with _owner(stream):
-        if dresidual is None:
-            dresidual = torch.empty(z.shape, dtype=z.dtype, device=z.device)
-        if dx is None and p > 0:
-            dx = torch.empty(z.shape, dtype=z.dtype, device=z.device)
-        if weight is not None:
-            if dweight is None:
-                dweight = torch.empty(weight.shape, dtype=torch.float32, device=z.device)
-            if dbias is None:
-                dbias = torch.empty(weight.shape, dtype=torch.float32, device=z.device)
-        scratch = _scratch(lib().gpga_layer_norm_scratch_bytes(nodes, rows, d), scratch, z.device)
-    wp, ldw = _params(weight, "weight", nodes, d, z.device)
-    dwp, lddw = _params(dweight, "dweight", nodes, d, z.device)
-    dbp, lddb = _params(dbias, "dbias", nodes, d, z.device)
-    if dwp is not None and dbp is not None and lddw != lddb:
-        _bad("dweight and dbias must have one node stride")
-    dyp, lddy = _act(dy, "dy", z)
-    ep, lde = _act(dz, "dz", z)
-    gp, ldg = _act(dresidual, "dresidual", z)
-    xp, ldx = _act(dx, "dx", z)
-    _check(lib().gpga_layer_norm_backward(dyp, lddy, z.data_ptr(), _spacing(z), ep, lde, _stats(mean, "mean", z),
-                                          _stats(rstd, "rstd", z), wp, ldw, gp, ldg, xp, ldx, dwp, dbp,
-                                          lddw if dwp is not None else lddb, accumulate, dtype, nodes, rows, d, p, seed, k,
-                                          site, node0, scratch.data_ptr(), scratch.numel() * scratch.element_size(),
-                                          _on(stream, z, dy, dz, mean, rstd, weight, dresidual, dx, dweight, dbias, scratch)))
-    return dresidual, (dx if dx is not None else dresidual), dweight, dbias
+    if dresidual is None:
+        dresidual = _like(z)
+    if dx is None and p > 0:
+        dx = _like(z)
+    wp = dwp = dbp = ep = xp = ldw = lddw = lde = ldx = 0
+    if weight is not None:
+        wp, ldw = weight.data_ptr(), _params(weight, "weight", nodes, d, device)
+        if dweight is None:
+            dweight = weight.new_empty(weight.shape)
+        if dbias is None:
+            dbias = weight.new_empty(weight.shape)
+    if dweight is not None:
+        dwp, lddw = dweight.data_ptr(), _params(dweight, "dweight", nodes, d, device)
+    if dbias is not None:
+        dbp, lddb = dbias.data_ptr(), _params(dbias, "dbias", nodes, d, device)
+        if dweight is None:
+            lddw = lddb
+        elif lddb != lddw:
+            _bad("dweight and dbias must have one node stride")
+    if dz is not None:
+        ep, lde = dz.data_ptr(), _same(dz, "dz", shape, dtype, device, d)
+    if dx is not None:
+        xp, ldx = dx.data_ptr(), _same(dx, "dx", shape, dtype, device, d)
+    scratch_p = scratch_bytes = 0
+    if scratch is None:
+        scratch_bytes = _norm_scratch(nodes, rows, d)
+        if scratch_bytes:
+            scratch = z.new_empty(scratch_bytes, dtype=torch.uint8)
+            scratch_p = scratch.data_ptr()
+    elif scratch.get_device() != device or not scratch.is_contiguous():
+        _bad(f"scratch must be contiguous on cuda:{device}")
+    else:
+        scratch_p, scratch_bytes = scratch.data_ptr(), scratch.nbytes
+    _entry("gpga_layer_norm_backward")(device, dy.data_ptr(), z.data_ptr(), ep, _stats(mean, "mean", nodes * rows, device),
+                                       _stats(rstd, "rstd", nodes * rows, device), wp, dresidual.data_ptr(), xp, dwp, dbp,
+                                       scratch_p, scratch_bytes, _same(dy, "dy", shape, dtype, device, d),
+                                       d if z.is_contiguous() else _spacing(z), lde, ldw,
+                                       _same(dresidual, "dresidual", shape, dtype, device, d), ldx, lddw, accumulate, code,
+                                       nodes, rows, d, p, seed, k, site, node0)
+    return dresidual, (dresidual if dx is None else dx), dweight, dbias
