@@ -50,13 +50,14 @@ __global__ void __launch_bounds__(256) lookup_kernel(const LookupParams p)
 }
 
 // ---- gradient: sort -----------------------------------------------------------------------------------
-// Layout of the scratch area for one call: sorted tokens and their positions, one bit per vocabulary row that
-// some token names, and the partial sums of runs that cross tiles.
-constexpr uint32_t kSortPerBlock = 8192, kSortThreads = 1024, kSortWarps = kSortThreads / 32;
-constexpr uint32_t kSortMax = 8 * kSortPerBlock;   // tokens of a node sorted by one cluster of eight blocks
+// A sorted entry is token << 32 | position.  Scratch area of one call: the sorted entries, one bit per vocabulary row
+// that some token names, and the partial sums of runs that cross tiles.
+constexpr uint32_t kSortPerBlock = 8192, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortBlocks = 8;
+constexpr uint32_t kSortMax = kSortBlocks * kSortPerBlock;   // tokens of a node sorted by one cluster of blocks
+constexpr uint32_t kDirectTokens = 256;   // up to here no sort: see lookup_grad_direct_kernel
 
 struct GradLayout {
-    int64_t key_off, pos_off, bit_off, part_off, total;
+    int64_t entry_off, bit_off, part_off, total;
     uint32_t words;         // words of the bit map per node
     uint32_t tile, tiles;   // sorted entries per tile, tiles per node
     int32_t dpad;
@@ -68,15 +69,15 @@ uint32_t tile_entries(int64_t nodes, int64_t rows) { return nodes * rows >= 64 *
 GradLayout grad_layout(int64_t nodes, int64_t rows, int64_t d, int64_t vocab)
 {
     auto up = [](int64_t v) { return (v + 255) / 256 * 256; };
+    GradLayout L = {};
+    L.dpad = (int32_t)((d + 7) / 8 * 8);
+    L.words = (uint32_t)((vocab + 31) / 32);
+    if (rows <= kDirectTokens) return L;
     if (rows > (int64_t)kSortMax) rows = kSortMax;
-    GradLayout L;
     L.tile = tile_entries(nodes, rows);
     L.tiles = (uint32_t)((rows + L.tile - 1) / L.tile);
-    L.words = (uint32_t)((vocab + 31) / 32);
-    L.dpad = (int32_t)((d + 7) / 8 * 8);
-    L.key_off = 0;
-    L.pos_off = L.key_off + up(nodes * rows * 4);
-    L.bit_off = L.pos_off + up(nodes * rows * 4);
+    L.entry_off = 0;
+    L.bit_off = L.entry_off + up(nodes * rows * 8);
     L.part_off = L.bit_off + up(nodes * (int64_t)L.words * 4);
     L.total = L.part_off + up(L.tiles > 1 ? nodes * (int64_t)L.tiles * 2 * L.dpad * 4 : 0);
     return L;
@@ -84,7 +85,8 @@ GradLayout grad_layout(int64_t nodes, int64_t rows, int64_t d, int64_t vocab)
 
 struct SortParams {
     const void* tokens;
-    uint32_t *keys, *pos, *bits;
+    uint64_t* entries;
+    uint32_t* bits;
     int64_t node_tokens;   // tokens of one node in `tokens` (this call may sort a part of them)
     uint32_t first, count; // the part: tokens first .. first + count - 1 of every node
     uint32_t vocab, words;
@@ -97,7 +99,7 @@ __device__ __forceinline__ void cluster_barrier()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// Address of this block's shared-memory word in block `rank` of the cluster, and a store to it.
+// Address of this block's shared-memory word in block `rank` of the cluster, and stores to it.
 __device__ __forceinline__ uint32_t cluster_address(const void* p, uint32_t rank)
 {
     uint32_t a;
@@ -108,43 +110,70 @@ __device__ __forceinline__ void cluster_store(uint32_t address, uint32_t v)
 {
     asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(address), "r"(v) : "memory");
 }
+__device__ __forceinline__ void cluster_store(uint32_t address, uint64_t v)
+{
+    asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(address), "l"(v) : "memory");
+}
 
-// Stable radix sort of one node's (token, position) pairs, least significant digit first, by a cluster of blocks
-// that hold them in shared memory: entry e lives in block e / per_block.  A pass ranks every entry among the
-// equal digits before it (lanes by a match, warps by a scan of their counts, blocks by the counts that every
-// block sends to all others) and stores it straight into the block where it belongs.
+// Shared memory of the sort, in 32-bit words before the entries.
+constexpr uint32_t kSortWords = kSortWarps * 256 + kSortBlocks * 256 + 4 * 256 + 3 * 256 + 32;
+
+// Stable radix sort of one node's entries, least significant digit first, by a cluster of blocks that hold them in
+// shared memory: entry e lives in block e / per_block.  A pass ranks every entry among the equal digits before it
+// (lanes by ballots, warps by a scan of their counts), brings the block's entries into the order of their digits, and
+// sends the runs of one digit to their places in the cluster's blocks (the counts of the other blocks come from a
+// table that every block sends to all); the last pass writes them to memory.
 // A token outside the vocabulary sorts behind all others, as the key `vocab`.
 __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const SortParams p)
 {
     extern __shared__ uint32_t smem[];
-    uint32_t* hist = smem;                          // kSortWarps x 256
-    uint32_t* totals = hist + kSortWarps * 256;     // 8 x 256: every block's digit counts
-    uint32_t* base = totals + 8 * 256;              // 256
-    uint32_t* scan = base + 256;                    // 32
-    uint32_t* key[2] = {scan + 32, scan + 32 + 2 * p.per_block};
-    uint32_t* pos[2] = {key[0] + p.per_block, key[1] + p.per_block};
+    uint32_t* hist = smem;                            // kSortWarps x 256: equal digits in the block before the warp's
+    uint32_t* totals = hist + kSortWarps * 256;       // kSortBlocks x 256: every block's digit counts
+    uint32_t* quarter = totals + kSortBlocks * 256;   // 4 x 256: counts of eight warps each
+    uint32_t* local = quarter + 4 * 256;              // 256: first place of a digit in the block's order
+    uint32_t* global = local + 256;                   // 256: the same in the node's order, for this block's entries
+    uint32_t* scan = global + 256;                    // 2 x 8, padded
+    uint64_t* buffer[2] = {reinterpret_cast<uint64_t*>(smem + kSortWords), reinterpret_cast<uint64_t*>(smem + kSortWords) + p.per_block};
     uint32_t rank, blocks;
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(blocks));
     const uint32_t node = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t e0 = rank * p.per_block;
     const uint32_t mine = e0 >= p.count ? 0 : min(p.per_block, p.count - e0);
-    for (uint32_t e = tid; e < mine; e += kSortThreads) {
-        const int64_t token = token_at(p.tokens, p.tokens64, (int64_t)node * p.node_tokens + p.first + e0 + e);
-        key[0][e] = token >= 0 && token < (int64_t)p.vocab ? (uint32_t)token : p.vocab;
-        pos[0][e] = p.first + e0 + e;
-    }
-    cluster_barrier();   // every block of the cluster runs before any of them is written to
-    uint32_t* bits = p.bits + (int64_t)node * p.words;
-    for (uint32_t w = rank * kSortThreads + tid; w < p.words; w += blocks * kSortThreads) bits[w] = 0;
-
+    const uint32_t digits = 1u << p.digit_bits;
+    constexpr int kMost = kSortPerBlock / kSortThreads;   // entries of a thread
     // a warp's stretch of the block's entries
     const uint32_t stretch = ((mine + kSortWarps - 1) / kSortWarps + 31) / 32 * 32;
-    constexpr int kMost = kSortPerBlock / kSortThreads;   // entries of a thread
-    const uint32_t digits = 1u << p.digit_bits;
-    int cur = 0;
-    for (int pass = 0; pass < p.passes; ++pass, cur ^= 1) {
-        const int shift = pass * p.digit_bits;
+
+    uint64_t entry[kMost];
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+        const uint32_t off = i * 32 + lane, e = warp * stretch + off;
+        if (off < stretch && e < mine) {
+            const int64_t token = token_at(p.tokens, p.tokens64, (int64_t)node * p.node_tokens + p.first + e0 + e);
+            const uint32_t key = token >= 0 && token < (int64_t)p.vocab ? (uint32_t)token : p.vocab;
+            entry[i] = (uint64_t)key << 32 | (p.first + e0 + e);
+        }
+    }
+    uint32_t* bits = p.bits + (int64_t)node * p.words;
+    for (uint32_t w = rank * kSortThreads + tid; w < p.words; w += blocks * kSortThreads) bits[w] = 0;
+    cluster_barrier();   // the map is clear, and every block of the cluster runs before any of them is written to
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+        const uint32_t off = i * 32 + lane, e = warp * stretch + off, key = (uint32_t)(entry[i] >> 32);
+        // the load spares the frequent words' many atomics
+        if (off < stretch && e < mine && key < p.vocab && !(__ldcg(bits + (key >> 5)) >> (key & 31) & 1))
+            atomicOr(bits + (key >> 5), 1u << (key & 31));
+    }
+
+    for (int pass = 0; pass < p.passes; ++pass) {
+        const int shift = 32 + pass * p.digit_bits;
+        if (pass)
+#pragma unroll
+            for (int i = 0; i < kMost; ++i) {
+                const uint32_t off = i * 32 + lane, e = warp * stretch + off;
+                if (off < stretch && e < mine) entry[i] = buffer[pass & 1][e];
+            }
         for (uint32_t h = tid; h < kSortWarps * 256; h += kSortThreads) hist[h] = 0;
         __syncthreads();
         uint32_t before[kMost];   // equal digits before the entry in the warp's stretch
@@ -152,108 +181,171 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const SortPar
         for (int i = 0; i < kMost; ++i) {
             const uint32_t off = i * 32 + lane, e = warp * stretch + off;
             const bool live = off < stretch && e < mine;
-            const unsigned active = __ballot_sync(0xFFFFFFFFu, live);
-            if (!active) break;
-            if (live) {
-                const uint32_t digit = (key[cur][e] >> shift) & (digits - 1);
-                const unsigned same = __match_any_sync(active, digit);
-                const uint32_t had = hist[warp * 256 + digit];
-                __syncwarp(active);
-                before[i] = had + __popc(same & ((1u << lane) - 1u));
-                if ((int)lane == __ffs(same) - 1) hist[warp * 256 + digit] = had + __popc(same);
+            unsigned same = __ballot_sync(0xFFFFFFFFu, live);
+            if (!same) break;
+            const uint32_t digit = (uint32_t)(entry[i] >> shift) & (digits - 1);
+            for (int b = 0; b < p.digit_bits; ++b) {
+                const bool one = digit >> b & 1;
+                const unsigned ones = __ballot_sync(0xFFFFFFFFu, live && one);
+                same &= one ? ones : ~ones;
             }
+            uint32_t had = 0;
+            if (live) had = hist[warp * 256 + digit];
+            __syncwarp();
+            before[i] = had + __popc(same & ((1u << lane) - 1u));
+            if (live && (int)lane == __ffs(same) - 1) hist[warp * 256 + digit] = had + __popc(same);
             __syncwarp();
         }
         __syncthreads();
-        if (tid < digits) {
-            uint32_t run = 0;
-            for (uint32_t w = 0; w < kSortWarps; ++w) {
-                const uint32_t n = hist[w * 256 + tid];
-                hist[w * 256 + tid] = run;
-                run += n;
-            }
-            for (uint32_t b = 0; b < blocks; ++b) cluster_store(cluster_address(totals + rank * 256 + tid, b), run);
+        // counts of a digit over the warps, eight warps per quarter of the threads
+        const uint32_t digit_t = tid & 255, q = tid >> 8;
+        uint32_t sum = 0, count[8];
+#pragma unroll
+        for (int w = 0; w < 8; ++w) count[w] = hist[(q * 8 + w) * 256 + digit_t];
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+            const uint32_t n = count[w];
+            count[w] = sum;
+            sum += n;
         }
+        quarter[q * 256 + digit_t] = sum;
+        __syncthreads();
+        uint32_t total = 0, ahead_q = 0;
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k) {
+            const uint32_t n = quarter[k * 256 + digit_t];
+            if (k < q) ahead_q += n;
+            total += n;
+        }
+#pragma unroll
+        for (int w = 0; w < 8; ++w) hist[(q * 8 + w) * 256 + digit_t] = count[w] + ahead_q;
+        if (q == 0)
+            for (uint32_t b = 0; b < blocks; ++b) cluster_store(cluster_address(totals + rank * 256 + digit_t, b), total);
         cluster_barrier();
         uint32_t all = 0, ahead = 0;   // of this digit: in all blocks, in the blocks before this one
-        if (tid < digits)
+        if (q == 0)
             for (uint32_t b = 0; b < blocks; ++b) {
-                const uint32_t n = totals[b * 256 + tid];
+                const uint32_t n = totals[b * 256 + digit_t];
                 if (b < rank) ahead += n;
                 all += n;
             }
-        uint32_t upto = all;   // inclusive scan over the digits
+        if (q == 0) {   // inclusive scans over the digits, of the block's counts and of all blocks'
+            uint32_t in_block = total, in_all = all;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t n = __shfl_up_sync(0xFFFFFFFFu, upto, o);
-            if (lane >= (uint32_t)o) upto += n;
-        }
-        if (lane == 31 && warp < 8) scan[warp] = upto;
-        __syncthreads();
-        if (tid < digits) {
-            for (uint32_t w = 0; w < warp; ++w) upto += scan[w];
-            base[tid] = upto - all + ahead;
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t n = __shfl_up_sync(0xFFFFFFFFu, in_block, o), m = __shfl_up_sync(0xFFFFFFFFu, in_all, o);
+                if (lane >= (uint32_t)o) in_block += n, in_all += m;
+            }
+            if (lane == 31) scan[warp] = in_block, scan[8 + warp] = in_all;
+            local[digit_t] = in_block - total;
+            global[digit_t] = in_all - all + ahead;
         }
         __syncthreads();
+        if (q == 0) {
+            uint32_t n = 0, m = 0;
+            for (uint32_t w = 0; w < warp; ++w) n += scan[w], m += scan[8 + w];
+            local[digit_t] += n;
+            global[digit_t] += m;
+        }
+        __syncthreads();
+        uint64_t* order = buffer[pass & 1];   // its entries are in registers
 #pragma unroll
         for (int i = 0; i < kMost; ++i) {
             const uint32_t off = i * 32 + lane, e = warp * stretch + off;
             if (off < stretch && e < mine) {
-                const uint32_t k = key[cur][e], digit = (k >> shift) & (digits - 1);
-                const uint32_t to = base[digit] + hist[warp * 256 + digit] + before[i];
-                const uint32_t block = to / p.per_block, at = to - block * p.per_block;
-                cluster_store(cluster_address(key[cur ^ 1] + at, block), k);
-                cluster_store(cluster_address(pos[cur ^ 1] + at, block), pos[cur][e]);
+                const uint32_t digit = (uint32_t)(entry[i] >> shift) & (digits - 1);
+                order[local[digit] + hist[warp * 256 + digit] + before[i]] = entry[i];
             }
         }
-        cluster_barrier();
-    }
-    const int64_t out = (int64_t)node * p.count + e0;
-    for (uint32_t e = tid; e < mine; e += kSortThreads) {
-        const uint32_t k = key[cur][e];
-        p.keys[out + e] = k;
-        p.pos[out + e] = pos[cur][e];
-        if (k < p.vocab && (e == 0 || key[cur][e - 1] != k)) atomicOr(bits + (k >> 5), 1u << (k & 31));
+        __syncthreads();
+        const bool last = pass + 1 == p.passes;
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) {
+            const uint32_t e = i * kSortThreads + tid;
+            if (e < mine) {
+                const uint64_t v = order[e];
+                const uint32_t digit = (uint32_t)(v >> shift) & (digits - 1);
+                const uint32_t to = global[digit] + (e - local[digit]);
+                if (last) p.entries[(int64_t)node * p.count + to] = v;
+                else {
+                    const uint32_t block = to / p.per_block;
+                    cluster_store(cluster_address(buffer[pass & 1 ^ 1] + (to - block * p.per_block), block), v);
+                }
+            }
+        }
+        if (!last) cluster_barrier();
     }
 }
 
 // ---- gradient: sums -----------------------------------------------------------------------------------
 struct SumParams {
     const void* dout;
+    const void* tokens;      // direct kernel only
     float* grad;
-    const uint32_t *keys, *pos, *bits;
+    const uint64_t* entries;
+    const uint32_t* bits;
     float* part;
     int64_t ldo, ldg, node_ldg;
     int64_t node_rows;       // rows of dout per node
     uint32_t count, vocab, words, tile, tiles;
     int32_t d, dpad;
-    uint32_t tile_blocks;    // blocks 0 .. tile_blocks - 1 (x) sum, the others write zeros
+    uint32_t sum_blocks;     // blocks 0 .. sum_blocks - 1 (x) sum, the others write zeros
     uint32_t zero_blocks;
     float scale;
-    bool accumulate, gvec;   // gvec: 128-bit accesses to grad
+    bool tokens64, accumulate, gvec;   // gvec: 128-bit accesses to grad
 };
+
+// Writes (or adds) a token's sum to its row of grad; the lanes of `group` that share it make the call together.  GVEC:
+// every row of grad is aligned and d is a multiple of four.
+template <bool GVEC, int LANES>
+__device__ __forceinline__ void write_sum(const SumParams& p, uint32_t node, uint32_t token, int c, int lane, unsigned group, f32x2_t* acc)
+{
+    float* to = p.grad + node * p.node_ldg + (int64_t)token * p.ldg;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] = mul2(acc[j], both(p.scale));
+    if constexpr (GVEC) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (c + 4 * h < p.d) {
+                float4 a = join4(acc[2 * h], acc[2 * h + 1]);
+                float4* at = reinterpret_cast<float4*>(to + c) + h;
+                if (p.accumulate) a = add4(*at, a);
+                __stcs(at, a);
+            }
+    } else {
+        if (p.accumulate) {
+            Raw8<float, false> old;
+            f32x2_t v[4];
+            old.load(to, c, p.d, span_of<float>(to, 0, 1, p.d));
+            old.get(v);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[j] = add2(v[j], acc[j]);
+        }
+        RowStore<float, false, LANES> store;
+        store.store(to, c, p.d, acc, lane, group, true);
+    }
+}
 
 // The sorted entries are cut into tiles of p.tile; TX threads walk a tile's entries over 8 TX columns and keep the
 // running sum of one token.  A token whose entries all lie in the tile is written to its row of grad; one that
 // comes from the tile before or goes on into the next leaves a partial sum (slot 0: came from before, slot 1:
 // starts here and goes on).
-template <class T, bool VEC, int TX>
+template <class T, bool VEC, bool GVEC, int TX>
 __device__ __forceinline__ void sum_tile(const SumParams& p, uint32_t node, uint32_t tile, int c0, int tx)
 {
     constexpr int U = VEC && sizeof(T) == 2 ? 8 : 4;   // entries whose loads are in flight together
     constexpr int LANES = TX < 32 ? TX : 32;
-    const uint32_t* keys = p.keys + (int64_t)node * p.count;
-    const uint32_t* pos = p.pos + (int64_t)node * p.count;
+    const uint64_t* entries = p.entries + (int64_t)node * p.count;
     const T* dout = static_cast<const T*>(p.dout) + (int64_t)node * p.node_rows * p.ldo;
     const Span span = span_of<T>(dout, p.ldo, p.node_rows, p.d);
     const uint32_t begin = tile * p.tile, end = min(begin + p.tile, p.count);
     float* part = p.part + ((int64_t)node * p.tiles + tile) * 2 * p.dpad;
     const uint32_t none = 0xFFFFFFFFu;
-    const uint32_t prev = begin ? keys[begin - 1] : none, next = end < p.count ? keys[end] : none;
+    const uint32_t prev = begin ? (uint32_t)(entries[begin - 1] >> 32) : none, next = end < p.count ? (uint32_t)(entries[end] >> 32) : none;
     const unsigned group = group_mask<TX>();
     const int c = c0 + tx * 8;
     f32x2_t acc[4] = {both(0.f), both(0.f), both(0.f), both(0.f)};
-    uint32_t cur = keys[begin];
+    uint32_t cur = (uint32_t)(entries[begin] >> 32);
     bool from_before = cur == prev;
     auto flush = [&](bool goes_on) {
         if (cur >= p.vocab) return;
@@ -263,42 +355,18 @@ __device__ __forceinline__ void sum_tile(const SumParams& p, uint32_t node, uint
                 *reinterpret_cast<float4*>(to + c) = join4(acc[0], acc[1]);
                 *reinterpret_cast<float4*>(to + c + 4) = join4(acc[2], acc[3]);
             }
-            return;
-        }
-        float* to = p.grad + node * p.node_ldg + (int64_t)cur * p.ldg;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[j] = mul2(acc[j], both(p.scale));
-        if (p.gvec) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                if (c + 4 * h < p.d) {
-                    float4 a = join4(acc[2 * h], acc[2 * h + 1]);
-                    float4* at = reinterpret_cast<float4*>(to + c) + h;
-                    if (p.accumulate) a = add4(*at, a);
-                    __stcs(at, a);
-                }
         } else {
-            if (p.accumulate) {
-                Raw8<float, false> old;
-                f32x2_t v[4];
-                old.load(to, c, p.d, span_of<float>(to, 0, 1, p.d));
-                old.get(v);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[j] = add2(v[j], acc[j]);
-            }
-            RowStore<float, false, LANES> store;
-            store.store(to, c, p.d, acc, tx % LANES, group, true);
+            write_sum<GVEC, LANES>(p, node, cur, c, tx % LANES, group, acc);
         }
     };
     for (uint32_t e0 = begin; e0 < end; e0 += U) {
-        const uint32_t own_e = min(e0 + (tx & (U - 1)), end - 1);
-        const uint32_t own_key = keys[own_e], own_pos = pos[own_e];
+        const uint64_t own = entries[min(e0 + (tx & (U - 1)), end - 1)];
         uint32_t k[U];
         Raw8<T, VEC> raw[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            k[u] = __shfl_sync(group, own_key, u, U);
-            const uint32_t at = __shfl_sync(group, own_pos, u, U);
+            k[u] = __shfl_sync(group, (uint32_t)(own >> 32), u, U);
+            const uint32_t at = __shfl_sync(group, (uint32_t)own, u, U);
             if (e0 + u < end && k[u] < p.vocab && (!VEC || c < p.d)) raw[u].load(dout + (int64_t)at * p.ldo, c, p.d, span);
         }
 #pragma unroll
@@ -323,91 +391,89 @@ __device__ __forceinline__ void sum_tile(const SumParams& p, uint32_t node, uint
     flush(cur == next);
 }
 
-// Rows of grad that no token names: eight rows (a byte of the bit map) at a time.
-__device__ __forceinline__ void zero_rows(const SumParams& p, uint32_t node, uint32_t first)
+__device__ __forceinline__ void zero_row(const SumParams& p, uint32_t node, uint32_t v)
 {
-    const uint32_t eighths = (p.vocab + 7) / 8;
-    const uint32_t* bits = p.bits + (int64_t)node * p.words;
-    for (uint32_t q = first; q < eighths; q += p.zero_blocks) {
-        const uint32_t named = (bits[q >> 2] >> ((q & 3) * 8)) & 0xFFu;
-        for (uint32_t r = 0; r < 8; ++r) {
-            const uint32_t v = q * 8 + r;
-            if (v >= p.vocab || (named >> r & 1)) continue;
-            float* to = p.grad + node * p.node_ldg + (int64_t)v * p.ldg;
-            if (p.gvec) {
-                for (int c = threadIdx.x * 4; c < p.d; c += blockDim.x * 4)
-                    __stcs(reinterpret_cast<float4*>(to + c), make_float4(0.f, 0.f, 0.f, 0.f));
-            } else {
-                for (int c = threadIdx.x; c < p.d; c += blockDim.x) to[c] = 0.f;
-            }
-        }
+    float* to = p.grad + node * p.node_ldg + (int64_t)v * p.ldg;
+    if (p.gvec) {
+        for (int c = threadIdx.x * 4; c < p.d; c += 128 * 4) __stcs(reinterpret_cast<float4*>(to + c), make_float4(0.f, 0.f, 0.f, 0.f));
+    } else {
+        for (int c = threadIdx.x; c < p.d; c += 128) to[c] = 0.f;
     }
 }
 
-template <class T, bool VEC, int TX>
+template <class T, bool VEC, bool GVEC, int TX>
 __global__ void __launch_bounds__(128) lookup_grad_kernel(const SumParams p)
 {
     const uint32_t node = blockIdx.z;
     grid_dependency_wait();
-    if (blockIdx.x >= p.tile_blocks) {
-        if (blockIdx.y == 0) zero_rows(p, node, blockIdx.x - p.tile_blocks);
+    if (blockIdx.x >= p.sum_blocks) {
+        // rows of grad that no token names, eight rows (a byte of the bit map) at a time
+        if (blockIdx.y) return;
+        const uint32_t* bits = p.bits + (int64_t)node * p.words;
+        for (uint32_t q = blockIdx.x - p.sum_blocks; q < (p.vocab + 7) / 8; q += p.zero_blocks) {
+            const uint32_t named = bits[q >> 2] >> ((q & 3) * 8) & 0xFFu;
+            for (uint32_t r = 0; r < 8 && q * 8 + r < p.vocab; ++r)
+                if (!(named >> r & 1)) zero_row(p, node, q * 8 + r);
+        }
         return;
     }
     const uint32_t tile = blockIdx.x * (128 / TX) + threadIdx.x / TX;
-    if (tile < p.tiles) sum_tile<T, VEC, TX>(p, node, tile, blockIdx.y * TX * 8, threadIdx.x % TX);
+    if (tile < p.tiles) sum_tile<T, VEC, GVEC, TX>(p, node, tile, blockIdx.y * TX * 8, threadIdx.x % TX);
 }
 
-// Tokens whose entries span tiles: the sum of the tiles' partial sums, in their order.
-// Blocks 0 .. tiles - 1 (x): the token that goes on from tile x and starts there, if it spans at most kShortRun
-// more tiles; a thread adds four columns.  The other blocks: a longer run, taken by the first tile inside it
-// whose number is a multiple of kShortRun; eight warps add every eighth partial sum of 128 columns.
+// Tokens whose entries span tiles: the sum of the tiles' partial sums, in their order.  A boundary between tiles lies
+// inside a run when the entries on both sides have one token; lanes look at 32 boundaries at a time.
+// Blocks 0 .. tiles slabs - 1 (x): the token that starts in a tile and goes on, if it spans at most kShortRun more
+// tiles; a thread adds four columns.  The other blocks: a longer run, taken by the first tile inside it whose number is
+// a multiple of kShortRun; eight warps add every eighth partial sum of 128 columns, then the warps' sums in their order.
 constexpr uint32_t kShortRun = 16;
 __global__ void __launch_bounds__(256) lookup_grad_join_kernel(const SumParams p)
 {
     __shared__ float4 sums[8][32];
     grid_dependency_wait();
-    const uint32_t node = blockIdx.z;
-    const uint32_t* keys = p.keys + (int64_t)node * p.count;
-    const bool is_long = blockIdx.x >= p.tiles;
-    uint32_t tile = is_long ? (blockIdx.x - p.tiles + 1) * kShortRun : blockIdx.x;
-    if (tile >= p.tiles) return;
-    uint32_t token;
+    const uint32_t node = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint64_t* entries = p.entries + (int64_t)node * p.count;
+    auto key = [&](uint32_t e) { return (uint32_t)(entries[e] >> 32); };
+    const uint32_t slabs = (uint32_t)(p.d + 1023) / 1024, long_slabs = (uint32_t)(p.d + 127) / 128;
+    const bool is_long = blockIdx.x >= p.tiles * slabs;
+    const uint32_t item = is_long ? blockIdx.x - p.tiles * slabs : blockIdx.x;
+    uint32_t tile, token;
+    int c;
     if (is_long) {
         // the run that comes into this tile, and the tile where it starts
-        const uint32_t begin = tile * p.tile;
-        token = keys[begin];
-        if (token >= p.vocab || keys[begin - 1] != token) return;
-        uint32_t lo = 0, hi = begin;   // first entry of the token
-        while (lo < hi) {
-            const uint32_t mid = (lo + hi) / 2;
-            if (keys[mid] < token) lo = mid + 1; else hi = mid;
-        }
-        const uint32_t start = lo / p.tile;
-        if (start + kShortRun < tile) return;   // an earlier multiple of kShortRun is inside the run
-        tile = start;
+        tile = (item / long_slabs + 1) * kShortRun;
+        c = (int)(item % long_slabs * 128 + lane * 4);
+        token = key(tile * p.tile);
+        if (token >= p.vocab) return;
+        const unsigned in = __ballot_sync(0xFFFFFFFFu, lane < tile && key((tile - min(lane, tile - 1)) * p.tile - 1) == token);
+        const uint32_t back = __ffs(~in) ? __ffs(~in) - 1 : 32;   // boundaries inside the run from this one back
+        if (back == 0 || back > kShortRun) return;   // none, or an earlier multiple of kShortRun is inside it too
+        tile -= back;
     } else {
+        tile = item / slabs;
+        c = (int)((item % slabs * 256 + threadIdx.x) * 4);
         const uint32_t begin = tile * p.tile, end = begin + p.tile;
         if (end >= p.count) return;
-        token = keys[end];
-        if (token >= p.vocab || keys[end - 1] != token) return;
-        if (begin && keys[begin - 1] == token) return;   // starts in an earlier tile
+        token = key(end);
+        if (token >= p.vocab || key(end - 1) != token) return;
+        if (begin && key(begin - 1) == token) return;   // starts in an earlier tile
     }
-    uint32_t lo = (tile + 1) * p.tile, hi = p.count;   // one past the token's last entry
-    while (lo < hi) {
-        const uint32_t mid = (lo + hi) / 2;
-        if (keys[mid] <= token) lo = mid + 1; else hi = mid;
+    uint32_t more = 0;   // tiles after the first
+    for (;;) {
+        const uint32_t b = tile + 1 + more + lane;
+        const unsigned in = __ballot_sync(0xFFFFFFFFu, b < p.tiles && key(b * p.tile) == token);
+        more += ~in ? __ffs(~in) - 1 : 32;
+        if (~in) break;
     }
-    const uint32_t more = (lo - 1) / p.tile - tile;   // tiles after the first
     if ((more > kShortRun) != is_long) return;
     const float* part = p.part + ((int64_t)node * p.tiles + tile) * 2 * p.dpad;
     const int64_t step = 2 * (int64_t)p.dpad;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int c = is_long ? blockIdx.y * 128 + lane * 4 : (blockIdx.y * 256 + threadIdx.x) * 4;
     if (!is_long && c >= p.d) return;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
     if (c < p.d) {
         if (!is_long) {
             sum = *reinterpret_cast<const float4*>(part + p.dpad + c);
+#pragma unroll 4
             for (uint32_t m = 1; m <= more; ++m) sum = add4(sum, *reinterpret_cast<const float4*>(part + m * step + c));
         } else {
             if (warp == 0) sum = *reinterpret_cast<const float4*>(part + p.dpad + c);
@@ -424,7 +490,7 @@ __global__ void __launch_bounds__(256) lookup_grad_join_kernel(const SumParams p
     }
     float* to = p.grad + node * p.node_ldg + (int64_t)token * p.ldg + c;
     sum = scale4(sum, p.scale);
-    if (p.gvec && c + 4 <= p.d) {
+    if (p.gvec) {
         if (p.accumulate) sum = add4(*reinterpret_cast<const float4*>(to), sum);
         __stcs(reinterpret_cast<float4*>(to), sum);
     } else {
@@ -435,28 +501,115 @@ __global__ void __launch_bounds__(256) lookup_grad_join_kernel(const SumParams p
     }
 }
 
-template <class T, bool VEC, int TX>
+// Few tokens (at most kDirectTokens per node): one launch, no sort, no scratch.  Blocks 0 .. count - 1 (x): the block
+// of a token's first place adds the rows of all its places, in their order, over 1024 columns.  The other blocks clear
+// the rows of their share of the vocabulary that no token names.
+template <class T, bool VEC, bool GVEC>
+__global__ void __launch_bounds__(128) lookup_grad_direct_kernel(const SumParams p)
+{
+    __shared__ uint32_t keys[kDirectTokens], list[kDirectTokens], found[kDirectTokens / 32];
+    constexpr uint32_t kSpan = 1024;   // vocabulary rows of a clearing step
+    __shared__ uint32_t named[kSpan / 32];
+    const uint32_t node = blockIdx.z, tid = threadIdx.x, lane = tid & 31;
+    for (uint32_t i = tid; i < p.count; i += 128) {
+        const int64_t token = token_at(p.tokens, p.tokens64, (int64_t)node * p.count + i);
+        keys[i] = token >= 0 && token < (int64_t)p.vocab ? (uint32_t)token : p.vocab;
+    }
+    __syncthreads();
+    if (blockIdx.x >= p.sum_blocks) {
+        if (blockIdx.y) return;
+        const uint32_t share = (p.vocab + p.zero_blocks - 1) / p.zero_blocks;
+        const uint32_t first = (blockIdx.x - p.sum_blocks) * share, end = min(first + share, p.vocab);
+        for (uint32_t v0 = first; v0 < end; v0 += kSpan) {
+            if (v0 != first) __syncthreads();
+            if (tid < kSpan / 32) named[tid] = 0;
+            __syncthreads();
+            for (uint32_t i = tid; i < p.count; i += 128)
+                if (keys[i] >= v0 && keys[i] - v0 < kSpan) atomicOr(&named[(keys[i] - v0) >> 5], 1u << ((keys[i] - v0) & 31));
+            __syncthreads();
+            for (uint32_t v = v0; v < end && v < v0 + kSpan; ++v)
+                if (!(named[(v - v0) >> 5] >> ((v - v0) & 31) & 1)) zero_row(p, node, v);
+        }
+        return;
+    }
+    const uint32_t at = blockIdx.x, token = keys[at];
+    if (token >= p.vocab) return;
+    bool earlier = false;
+    for (uint32_t i = tid; i < kDirectTokens; i += 128) {
+        const bool hit = i < p.count && keys[i] == token;
+        earlier |= hit && i < at;
+        const unsigned hits = __ballot_sync(0xFFFFFFFFu, hit);
+        if (lane == 0) found[i >> 5] = hits;
+    }
+    if (__syncthreads_or(earlier)) return;
+    uint32_t places = 0;
+#pragma unroll
+    for (uint32_t w = 0; w < kDirectTokens / 32; ++w) {
+        if (tid >> 5 == (w & 3) && found[w] >> lane & 1) list[places + __popc(found[w] & ((1u << lane) - 1u))] = w * 32 + lane;
+        places += __popc(found[w]);
+    }
+    __syncthreads();
+    constexpr int U = VEC && sizeof(T) == 2 ? 8 : 4;
+    const T* dout = static_cast<const T*>(p.dout) + (int64_t)node * p.node_rows * p.ldo;
+    const Span span = span_of<T>(dout, p.ldo, p.node_rows, p.d);
+    const int c = (int)(blockIdx.y * 128 + tid) * 8;
+    f32x2_t acc[4] = {both(0.f), both(0.f), both(0.f), both(0.f)};
+    for (uint32_t e0 = 0; e0 < places; e0 += U) {
+        Raw8<T, VEC> raw[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (e0 + u < places && c < p.d) raw[u].load(dout + (int64_t)list[e0 + u] * p.ldo, c, p.d, span);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (e0 + u < places && c < p.d) {
+                f32x2_t v[4];
+                raw[u].get(v);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[j] = add2(acc[j], v[j]);
+            }
+    }
+    write_sum<GVEC, 32>(p, node, token, c, lane, 0xFFFFFFFFu, acc);
+}
+
+// Blocks that clear rows: the units of work there are, at most sixteen blocks per SM in all.
+uint32_t zero_blocks_for(const SumParams& p, uint32_t nodes, uint32_t rows_per_unit)
+{
+    if (p.accumulate) return 0;
+    const uint32_t units = (p.vocab + rows_per_unit - 1) / rows_per_unit, most = (148 * 16 + nodes - 1) / nodes;
+    return units < most ? units : most;
+}
+
+template <class T, bool VEC, bool GVEC, int TX>
 cudaError_t sums_as(SumParams p, uint32_t nodes, cudaStream_t s)
 {
     const uint32_t per = 128 / TX;
-    p.tile_blocks = (p.tiles + per - 1) / per;
+    p.sum_blocks = (p.tiles + per - 1) / per;
+    p.zero_blocks = zero_blocks_for(p, nodes, 8);
     const uint32_t slabs = (uint32_t)(p.d + 8 * TX - 1) / (8 * TX);
-    if (p.accumulate) p.zero_blocks = 0;
-    else {
-        const uint32_t eighths = (p.vocab + 7) / 8, most = (148 * 16 + nodes - 1) / nodes;
-        p.zero_blocks = eighths < most ? eighths : most;
-    }
-    if (!(p.tile_blocks + p.zero_blocks)) return cudaSuccess;
-    return launch_after_trigger(lookup_grad_kernel<T, VEC, TX>, dim3(p.tile_blocks + p.zero_blocks, slabs, nodes), dim3(128), 0, s,
+    return launch_after_trigger(lookup_grad_kernel<T, VEC, GVEC, TX>, dim3(p.sum_blocks + p.zero_blocks, slabs, nodes), dim3(128), 0, s,
                                 true, p);
 }
 
-template <class T, bool VEC>
-cudaError_t sums_of(const SumParams& p, uint32_t nodes, cudaStream_t s)
+template <class T, bool VEC, bool GVEC>
+cudaError_t sums_of(SumParams p, bool direct, uint32_t nodes, cudaStream_t s)
 {
-    if (p.d <= 64) return sums_as<T, VEC, 8>(p, nodes, s);
-    if (p.d <= 256) return sums_as<T, VEC, 32>(p, nodes, s);
-    return sums_as<T, VEC, 128>(p, nodes, s);
+    if (direct) {
+        p.sum_blocks = p.count;
+        p.zero_blocks = zero_blocks_for(p, nodes, 8);
+        if (!(p.sum_blocks + p.zero_blocks)) return cudaSuccess;
+        lookup_grad_direct_kernel<T, VEC, GVEC><<<dim3(p.sum_blocks + p.zero_blocks, (unsigned)(p.d + 1023) / 1024, nodes), 128, 0, s>>>(p);
+        return cudaGetLastError();
+    }
+    if (p.d <= 64) return sums_as<T, VEC, GVEC, 8>(p, nodes, s);
+    if (p.d <= 256) return sums_as<T, VEC, GVEC, 32>(p, nodes, s);
+    return sums_as<T, VEC, GVEC, 128>(p, nodes, s);
+}
+
+template <class T>
+cudaError_t sums_by_alignment(const SumParams& p, bool direct, uint32_t nodes, bool vec, cudaStream_t s)
+{
+    if (!vec) return sums_of<T, false, false>(p, direct, nodes, s);
+    return p.gvec ? sums_of<T, true, true>(p, direct, nodes, s) : sums_of<T, true, false>(p, direct, nodes, s);
 }
 
 bool aligned(const void* p, int64_t ld, int size) { return (((uintptr_t)p) & 15u) == 0 && (ld * size) % 16 == 0; }
@@ -504,10 +657,36 @@ int64_t lookup_grad_scratch_bytes(int64_t nodes, int64_t rows, int64_t d, int64_
 cudaError_t launch_lookup_grad(const LookupGradParams& g, int dtype, cudaStream_t s)
 {
     const GradLayout L = grad_layout(g.nodes, g.rows, g.d, g.vocab);
-    SortParams q;
+    const bool direct = g.rows <= kDirectTokens;
+    SumParams p = {};
+    p.dout = g.dout;
+    p.tokens = g.tokens;
+    p.tokens64 = g.tokens64;
+    p.grad = g.grad;
+    p.ldo = g.ldo;
+    p.ldg = g.ldg;
+    p.node_ldg = g.node_ldg;
+    p.node_rows = g.rows;
+    p.count = g.rows;
+    p.vocab = g.vocab;
+    p.words = L.words;
+    p.tile = L.tile;
+    p.d = g.d;
+    p.dpad = L.dpad;
+    p.scale = g.scale;
+    p.accumulate = g.accumulate;
+    p.gvec = g.d % 4 == 0 && aligned(g.grad, g.ldg, 4) && g.node_ldg % 4 == 0;
+    const bool vec = g.d % 8 == 0 && aligned(g.dout, g.ldo, dtype == GPGA_DTYPE_F32 ? 4 : 2);
+    auto sums = [&]() {
+        return dtype == GPGA_DTYPE_F32    ? sums_by_alignment<float>(p, direct, g.nodes, vec, s)
+               : dtype == GPGA_DTYPE_BF16 ? sums_by_alignment<__nv_bfloat16>(p, direct, g.nodes, vec, s)
+                                          : sums_by_alignment<__half>(p, direct, g.nodes, vec, s);
+    };
+    if (direct) return sums();
+
+    SortParams q = {};
     q.tokens = g.tokens;
-    q.keys = reinterpret_cast<uint32_t*>(g.scratch + L.key_off);
-    q.pos = reinterpret_cast<uint32_t*>(g.scratch + L.pos_off);
+    q.entries = reinterpret_cast<uint64_t*>(g.scratch + L.entry_off);
     q.bits = reinterpret_cast<uint32_t*>(g.scratch + L.bit_off);
     q.node_tokens = g.rows;
     q.vocab = g.vocab;
@@ -517,47 +696,26 @@ cudaError_t launch_lookup_grad(const LookupGradParams& g, int dtype, cudaStream_
     while (g.vocab >> key_bits) ++key_bits;   // keys are 0 .. vocab
     q.passes = (key_bits + 7) / 8;
     q.digit_bits = (key_bits + q.passes - 1) / q.passes;
-
-    SumParams p;
-    p.dout = g.dout;
-    p.grad = g.grad;
-    p.keys = q.keys;
-    p.pos = q.pos;
+    p.entries = q.entries;
     p.bits = q.bits;
     p.part = reinterpret_cast<float*>(g.scratch + L.part_off);
-    p.ldo = g.ldo;
-    p.ldg = g.ldg;
-    p.node_ldg = g.node_ldg;
-    p.node_rows = g.rows;
-    p.vocab = g.vocab;
-    p.words = L.words;
-    p.tile = L.tile;
-    p.d = g.d;
-    p.dpad = L.dpad;
-    p.scale = g.scale;
-    p.gvec = g.d % 4 == 0 && aligned(g.grad, g.ldg, 4) && g.node_ldg % 4 == 0;
-    const int size = dtype == GPGA_DTYPE_F32 ? 4 : 2;
-    const bool vec = g.d % 8 == 0 && aligned(g.dout, g.ldo, size);
 
     // one cluster sorts up to kSortMax tokens of a node; the parts of a longer row list are added up one after
     // the other
-    uint32_t first = 0;
-    do {
+    for (uint32_t first = 0; first < g.rows;) {
         const uint32_t count = g.rows - first < kSortMax ? g.rows - first : kSortMax;
         q.first = first;
         q.count = count;
         uint32_t blocks = 1;
-        while (blocks < 8 && blocks * 1024 < count) blocks *= 2;
+        while (blocks < kSortBlocks && blocks * 1024 < count) blocks *= 2;
         q.per_block = (count + blocks - 1) / blocks;
-        if (q.per_block == 0) q.per_block = 1;
-        const size_t smem = (kSortWarps * 256 + 8 * 256 + 256 + 32 + 4 * (size_t)q.per_block) * 4;
         static unsigned long long limit_set = 0;
-        cudaError_t e = ensure_smem_limit(sort_tokens_kernel, (kSortWarps * 256 + 8 * 256 + 256 + 32 + 4 * (int)kSortPerBlock) * 4, limit_set);
+        cudaError_t e = ensure_smem_limit(sort_tokens_kernel, (kSortWords + 4 * kSortPerBlock) * 4, limit_set);
         if (e != cudaSuccess) return e;
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(blocks, g.nodes);
         cfg.blockDim = dim3(kSortThreads);
-        cfg.dynamicSmemBytes = smem;
+        cfg.dynamicSmemBytes = (kSortWords + 4 * (size_t)q.per_block) * 4;
         cfg.stream = s;
         cudaLaunchAttribute attr[1];
         attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -572,18 +730,15 @@ cudaError_t launch_lookup_grad(const LookupGradParams& g, int dtype, cudaStream_
         p.count = count;
         p.tiles = (count + L.tile - 1) / L.tile;
         p.accumulate = g.accumulate || first > 0;
-        e = dtype == GPGA_DTYPE_F32    ? (vec ? sums_of<float, true>(p, g.nodes, s) : sums_of<float, false>(p, g.nodes, s))
-            : dtype == GPGA_DTYPE_BF16 ? (vec ? sums_of<__nv_bfloat16, true>(p, g.nodes, s) : sums_of<__nv_bfloat16, false>(p, g.nodes, s))
-                                       : (vec ? sums_of<__half, true>(p, g.nodes, s) : sums_of<__half, false>(p, g.nodes, s));
+        e = sums();
         if (e != cudaSuccess) return e;
         if (p.tiles > 1) {
-            // y covers the columns at 1024 per block for the short runs and at 128 for the long ones
-            const uint32_t longs = (p.tiles - 1) / kShortRun;
-            e = launch_after_trigger(lookup_grad_join_kernel, dim3(p.tiles + longs, (g.d + 127) / 128, g.nodes), dim3(256), 0, s, true, p);
+            const uint32_t blocks_x = p.tiles * ((g.d + 1023) / 1024) + (p.tiles - 1) / kShortRun * ((g.d + 127) / 128);
+            e = launch_after_trigger(lookup_grad_join_kernel, dim3(blocks_x, g.nodes), dim3(256), 0, s, true, p);
             if (e != cudaSuccess) return e;
         }
         first += count;
-    } while (first < g.rows);
+    }
     return cudaSuccess;
 }
 

@@ -112,8 +112,9 @@ int32_t gpga_embedding_backward(const gpga_embedding_backward_args_t* a, void* s
     if (!a->grad || (a->rows && (!a->dout || !a->tokens))) return bad("NULL pointer");
     if (!element_aligned(a->grad, 4) || !element_aligned(a->dout, size) || !element_aligned(a->tokens, (int)a->token_bytes))
         return bad(kAlign);
-    if (!a->scratch || (reinterpret_cast<uintptr_t>(a->scratch) & 15u)) return bad("scratch must be 16-byte aligned");
-    if (a->scratch_bytes < lookup_grad_scratch_bytes(a->nodes, a->rows, a->d, a->vocab))
+    const int64_t need = lookup_grad_scratch_bytes(a->nodes, a->rows, a->d, a->vocab);
+    if (need && (!a->scratch || (reinterpret_cast<uintptr_t>(a->scratch) & 15u))) return bad("scratch must be 16-byte aligned");
+    if (a->scratch_bytes < need)
         return bad("scratch is too small: see gpga_embedding_scratch_bytes");
     if (a->rows == 0 && a->accumulate) return GPGA_OK;
     LookupGradParams p;

@@ -165,6 +165,17 @@ def _like(x):
     return torch.empty_like(x, memory_format=torch.contiguous_format)
 
 
+def _scratch(scratch, need, like, device):
+    """(tensor, pointer, bytes) of a call's scratch: the given tensor, or a new one where the call needs any."""
+    if scratch is None:
+        if not need:
+            return None, 0, 0
+        scratch = like.new_empty(need, dtype=torch.uint8)
+    elif scratch.get_device() != device or not scratch.is_contiguous():
+        _bad(f"scratch must be contiguous on cuda:{device}")
+    return scratch, scratch.data_ptr(), scratch.nbytes
+
+
 def embedding_forward(table, tokens, scale=1.0, dtype=None, out=None, stream=None):
     """out[..., :] = scale * table[tokens[...], :] (gpga_embedding_forward).
 
@@ -199,12 +210,9 @@ def embedding_backward(dout, tokens, grad_table, scale=1.0, accumulate=False, sc
         _bad(f"dout must be float32, bfloat16 or float16, got {dout.dtype}")
     ldo = _same(dout, "dout", tokens.shape + (d,), dout.dtype, device, d)
     rows = tokens.numel() // nodes
-    if scratch is None:
-        scratch = dout.new_empty(_embedding_scratch(nodes, rows, d, vocab), dtype=torch.uint8)
-    elif scratch.get_device() != device or not scratch.is_contiguous():
-        _bad(f"scratch must be contiguous on cuda:{device}")
-    _entry("gpga_embedding_backward")(device, dout.data_ptr(), tokens.data_ptr(), grad_table.data_ptr(), scratch.data_ptr(),
-                                      scratch.nbytes, ldo, ldg, node_ldg, _TOKEN_BYTES[tokens.dtype], code, nodes, rows, d,
+    scratch, scratch_p, scratch_bytes = _scratch(scratch, _embedding_scratch(nodes, rows, d, vocab), dout, device)
+    _entry("gpga_embedding_backward")(device, dout.data_ptr(), tokens.data_ptr(), grad_table.data_ptr(), scratch_p,
+                                      scratch_bytes, ldo, ldg, node_ldg, _TOKEN_BYTES[tokens.dtype], code, nodes, rows, d,
                                       vocab, accumulate, scale)
     return grad_table
 
@@ -309,16 +317,7 @@ def layer_norm_backward(dy, z, mean, rstd, weight, dz=None, p=0.0, seed=0, k=0, 
         ep, lde = dz.data_ptr(), _same(dz, "dz", shape, dtype, device, d)
     if dx is not None:
         xp, ldx = dx.data_ptr(), _same(dx, "dx", shape, dtype, device, d)
-    scratch_p = scratch_bytes = 0
-    if scratch is None:
-        scratch_bytes = _norm_scratch(nodes, rows, d)
-        if scratch_bytes:
-            scratch = z.new_empty(scratch_bytes, dtype=torch.uint8)
-            scratch_p = scratch.data_ptr()
-    elif scratch.get_device() != device or not scratch.is_contiguous():
-        _bad(f"scratch must be contiguous on cuda:{device}")
-    else:
-        scratch_p, scratch_bytes = scratch.data_ptr(), scratch.nbytes
+    scratch, scratch_p, scratch_bytes = _scratch(scratch, _norm_scratch(nodes, rows, d), z, device)
     _entry("gpga_layer_norm_backward")(device, dy.data_ptr(), z.data_ptr(), ep, _stats(mean, "mean", nodes * rows, device),
                                        _stats(rstd, "rstd", nodes * rows, device), wp, dresidual.data_ptr(), xp, dwp, dbp,
                                        scratch_p, scratch_bytes, _same(dy, "dy", shape, dtype, device, d),
