@@ -138,7 +138,8 @@ def grad_reference(dout, tokens, vocab, scale):
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("nodes,rows,d,vocab", [(1, 1, 1, 1), (1, 1, 64, 300), (2, 16, 8, 5), (3, 17, 65, 1000), (1, 700, 257, 30),
                                                 (2, 1025, 1024, 77), (1, 5000, 40, 300000), (4, 9, 1100, 65536), (1, 20011, 136, 3),
-                                                (2, 256, 1030, 40), (3, 257, 20, 40), (1, 40000, 264, 5000), (2, 300, 2052, 900), (1, 9000, 8, 70000)])
+                                                (2, 512, 1030, 40), (3, 513, 20, 40), (1, 40000, 264, 5000), (2, 600, 2052, 900), (1, 9000, 8, 70000),
+                                                (1, 700, 9, 1000003), (3, 17000, 40, 50)])
 def test_lookup_gradient(dtype, nodes, rows, d, vocab):
     g = gen(3)
     tokens = torch.randint(-1, vocab + 1, (nodes, rows), generator=g, device="cuda", dtype=torch.int64 if d % 2 else torch.int32)
@@ -527,7 +528,7 @@ def test_refusals():
         lambda: pkg.embedding_forward(table.transpose(1, 2), tokens),
         lambda: pkg.embedding_forward(table.cpu(), tokens.cpu()),
         lambda: pkg.embedding_backward(x[..., :15], tokens, table),
-        lambda: pkg.embedding_backward(x[:1].expand(2, 4, 16).repeat(1, 100, 1), tokens.repeat(1, 100), table,
+        lambda: pkg.embedding_backward(x[:1].expand(2, 4, 16).repeat(1, 200, 1), tokens.repeat(1, 200), table,
                                        scratch=torch.empty(16, dtype=torch.uint8, device="cuda")),
         lambda: pkg.embedding_backward(x, tokens, torch.ones((1, 5, 16), device="cuda").expand(2, 5, 16)),
         lambda: pkg.dropout(x, 1.5, 0),
