@@ -38,6 +38,7 @@ struct NormBackwardParams {
     int32_t d;
     int32_t splits;          // blocks per node
     bool wvec, accumulate;
+    bool shifted;            // rows of all activations are off the 16-byte alignment alike
     DropMask mask;
 };
 

@@ -167,6 +167,13 @@ template <class T, bool VEC> struct Raw8 {
             }
         }
     }
+    // Makes the compiler unpack the words again after this point instead of keeping the values it has (in more registers
+    // than the words take, or spilled) since an earlier get().
+    __device__ __forceinline__ void unpack_again()
+    {
+#pragma unroll
+        for (int i = 0; i < (VEC ? W : W + 4); ++i) asm volatile("" : "+r"(w[i]));
+    }
     __device__ __forceinline__ void get(f32x2_t* v) const
     {
         if constexpr (VEC) {
@@ -296,17 +303,98 @@ struct DropMask {
 // node, k, stream); column 8 chunk + j owns half j & 1 (low half first) of word j >> 1.  A dropped element is a
 // selected zero, so that NaN and infinities vanish with it.  The lower half of a word cannot change whether the upper
 // one is above (65536 q - 1), so that the upper half is compared in place.
-__device__ __forceinline__ void drop8(const DropMask& m, uint32_t group, uint32_t i, f32x2_t* v)
+__device__ __forceinline__ uint4 drop_words(const DropMask& m, uint32_t group, uint32_t i)
 {
-    if (!m.on) return;
-    const uint4 w = philox4x32_10(group, m.node0 + i, m.k, m.stream, m.keys);
-    const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+    return philox4x32_10(group, m.node0 + i, m.k, m.stream, m.keys);
+}
+__device__ __forceinline__ void drop8_by(const DropMask& m, const uint32_t* word, f32x2_t* v)
+{
     const f32x2_t scale = both(m.scale);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const float2 f = unpack2(mul2(v[j], scale));
         v[j] = pack2(word[j] << 16 > m.above ? f.x : 0.f, word[j] > m.above ? f.y : 0.f);
     }
+}
+__device__ __forceinline__ void drop8(const DropMask& m, uint32_t group, uint32_t i, f32x2_t* v)
+{
+    if (!m.on) return;
+    const uint4 w = drop_words(m, group, i);
+    const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+    drop8_by(m, word, v);
+}
+
+// ---- shifted chunks ---------------------------------------------------------------------------------
+// Rows that start off a 16-byte boundary but all alike: where every activation of a call has the same distance s (in
+// columns) of its rows from the boundary before them, chunk m is taken as columns 8 m - s .. 8 m - s + 7, which is aligned
+// memory in each of them; only the first and the last chunk of a row are partial.  s repeats after 16 / sizeof(T) rows,
+// and a block takes rows of one s.
+// kShiftRows: rows after which s repeats.
+template <class T> constexpr uint32_t kShiftRows = 16 / sizeof(T);
+
+template <class T>
+__device__ __forceinline__ int shift_of(const T* row) { return (int)((uint32_t)(uintptr_t)row & 15u) / (int)sizeof(T); }
+
+// Zeroes the columns outside first .. end - 1 of a chunk that starts at column `col`.
+__device__ __forceinline__ void keep_columns(f32x2_t* v, int col, int d)
+{
+    if (col >= 0 && col + 8 <= d) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float2 f = unpack2(v[j]);
+        const int c = col + 2 * j;
+        v[j] = pack2(c >= 0 && c < d ? f.x : 0.f, c + 1 >= 0 && c + 1 < d ? f.y : 0.f);
+    }
+}
+
+// Reads the aligned chunk at column `col` (possibly before the row's start or past its end) into the words of a chunk;
+// bytes outside the array's span are not touched and come out zero.
+template <class T>
+__device__ __forceinline__ void load_shifted(const T* row, int col, int d, const Span& s, Raw8<T, true>& raw)
+{
+    constexpr int W = 2 * sizeof(T);
+    const char* at = reinterpret_cast<const char*>(row + col);
+    if (at >= s.lo && at + 4 * W <= s.hi) {
+        raw.load(row, col, d, s);
+    } else {
+        f32x2_t v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int c = col + 2 * j;
+            v[j] = pack2(c >= 0 && c < d ? to_f32(row[c]) : 0.f, c + 1 >= 0 && c + 1 < d ? to_f32(row[c + 1]) : 0.f);
+        }
+        pack8<T>(v, raw.w);
+    }
+}
+
+template <class T>
+__device__ __forceinline__ void store_shifted(T* row, int col, int d, const f32x2_t* v)
+{
+    if (col >= 0 && col + 8 <= d) {
+        store8<T>(row + col, v);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (col + j >= 0 && col + j < d) row[col + j] = from_f32<T>(element(v, j));
+    }
+}
+
+// The random words of a shifted chunk: those of generator calls m - 1 (the chunk's first s columns) and m.
+__device__ __forceinline__ void shifted_words(const uint4& before, const uint4& own, int s, uint32_t* word)
+{
+    const uint32_t w[8] = {before.x, before.y, before.z, before.w, own.x, own.y, own.z, own.w};
+    if (s) {
+        cut<4>(w, (uint32_t)(16 - 2 * s), word);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) word[j] = w[4 + j];
+    }
+}
+
+__device__ __forceinline__ uint4 shfl4(unsigned mask, const uint4& v, int src, int width)
+{
+    return make_uint4(__shfl_sync(mask, v.x, src, width), __shfl_sync(mask, v.y, src, width), __shfl_sync(mask, v.z, src, width),
+                      __shfl_sync(mask, v.w, src, width));
 }
 
 // n / d for n < 2^32 by a multiplication (Granlund and Montgomery's division by an invariant, with a 33-bit multiplier

@@ -15,6 +15,7 @@ int32_t bad(const char* text) { return token_error(GPGA_ERR_INVALID_ARG, text); 
 int32_t launched(cudaError_t e, const char* where)
 {
     if (e == cudaSuccess) return GPGA_OK;
+    (void)cudaGetLastError();   // reported here, not by the next call
     char text[256];
     std::snprintf(text, sizeof text, "%s: %s", where, cudaGetErrorString(e));
     return token_error(GPGA_ERR_CUDA, text);
@@ -38,6 +39,19 @@ bool vocab_ok(int64_t vocab) { return vocab >= 1 && vocab < (int64_t(1) << 31); 
 
 const char* kAlign = "pointers must be aligned to their element";
 const char* kStrides = "strides must be at least d";
+// Rows of several arrays that are all off the 16-byte alignment alike.
+struct Alike {
+    bool yes = true, any = false;
+    uintptr_t base = 0, step = 0;
+    void add(const void* p, int64_t ld, int size)
+    {
+        if (!p) return;
+        const uintptr_t b = reinterpret_cast<uintptr_t>(p) & 15u, s = (uintptr_t)(ld * size) & 15u;
+        if (any && (b != base || s != step)) yes = false;
+        base = b, step = s, any = true;
+    }
+};
+
 const char* kSizes = "sizes: need 1 <= nodes <= 65535, rows >= 0, 1 <= d <= 2^20 and the products stated in gpga.h";
 
 // The dropout of a call; nullptr, or what is wrong with its arguments.
@@ -256,6 +270,13 @@ int32_t gpga_layer_norm_backward(const gpga_layer_norm_backward_args_t* a, void*
     q.wvec = full && vectors(a->weight, a->ldw, 4);
     const bool vec = full && vectors(a->dy, a->lddy, size) && vectors(a->z, a->ldz, size) && vectors(a->dz, a->lddz, size) &&
                      vectors(a->dresidual, a->lddr, size) && vectors(a->dx, a->lddx, size);
+    Alike alike;
+    alike.add(a->dy, a->lddy, size);
+    alike.add(a->z, a->ldz, size);
+    alike.add(a->dz, a->lddz, size);
+    alike.add(a->dresidual, a->lddr, size);
+    alike.add(a->dx, a->lddx, size);
+    q.shifted = alike.yes;
     return launched(launch_norm_backward(q, (int)a->dtype, vec, static_cast<cudaStream_t>(stream)), "gpga_layer_norm_backward");
 }
 
