@@ -137,6 +137,46 @@ __global__ void __launch_bounds__(256) dropout_rows_kernel(const DropoutParams p
     }
 }
 
+// Rows of x and y off the alignment alike: shifted chunks.  p.stretches counts those of the widest shift.
+template <class T, int TPR, int NC>
+__global__ void __launch_bounds__(256) dropout_shifted_kernel(const DropoutParams p)
+{
+    const uint32_t node = blockIdx.y, chunks = p.chunks.d;
+    const uint32_t g = blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+    const uint32_t t = divide(g, p.stretches);
+    if (t >= p.rows) return;
+    const int64_t row = (int64_t)node * p.rows + t;
+    const T* x = static_cast<const T*>(p.x) + row * p.ldx;
+    T* y = static_cast<T*>(p.y) + row * p.ldy;
+    const int lane = threadIdx.x % TPR, shift = shift_of(x);
+    const uint32_t first = (g - t * p.stretches.d) * (NC * TPR);
+    if ((int)first * kChunk - shift >= p.d) return;
+    __shared__ __align__(16) T slots[256 / TPR][16];
+    const Span span = span_of<T>(p.x, p.ldx, (int64_t)p.nodes * p.rows, p.d);
+    auto col = [&](int c) { return (int)(first + c * TPR + lane) * kChunk - shift; };
+    Raw8<T, true> raw[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+        if (col(c) < p.d) load_shifted(x, col(c), p.d, span, raw[c], slots[threadIdx.x / TPR]);
+    const uint32_t groups = t * chunks + first;
+    uint4 before = make_uint4(0, 0, 0, 0);
+    if (p.mask.on && shift) before = drop_words(p.mask, groups - 1, node);
+    f32x2_t v[NC][4];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        raw[c].get(v[c]);
+        if (p.mask.on) {
+            const uint4 own = drop_words(p.mask, groups + c * TPR + lane, node);
+            const uint4 left = shfl4(group_mask<TPR>(), own, (lane + TPR - 1) % TPR, TPR);
+            uint32_t word[4];
+            shifted_words(lane ? left : before, own, shift, word);
+            before = left;   // lane 0 has the last lane's
+            drop8_by(p.mask, word, v[c]);
+        }
+    }
+    store_shifted<T, TPR, NC>(y, col(0), p.d, shift, v, slots[threadIdx.x / TPR], lane, group_mask<TPR>());
+}
+
 // ---- layer norm, forward ----------------------------------------------------------------------------
 // (z - mean) rstd w + b
 __device__ __forceinline__ void scale8(const f32x2_t* v, float mean, float rstd, const f32x2_t* w, const f32x2_t* b, f32x2_t* y)
@@ -148,14 +188,15 @@ __device__ __forceinline__ void scale8(const f32x2_t* v, float mean, float rstd,
 
 __device__ __forceinline__ f32x2_t sum4(const f32x2_t* v) { return add2(add2(v[0], v[1]), add2(v[2], v[3])); }
 
-// Sum of (v - mean)^2 over the first n of eight columns.
-__device__ __forceinline__ f32x2_t squares8(const f32x2_t* v, float mean, int n)
+// Sum of (v - mean)^2 over the columns of a chunk at column `col` that lie in the row; EDGE: some may not.
+template <bool EDGE>
+__device__ __forceinline__ f32x2_t squares8(const f32x2_t* v, float mean, int col, int d)
 {
     const f32x2_t m = both(mean);
     f32x2_t e[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) e[j] = sub2(v[j], m);
-    keep_first(e, n);
+    if (EDGE) keep_columns(e, columns_there(col, d));
     f32x2_t s = mul2(e[0], e[0]);
 #pragma unroll
     for (int j = 1; j < 4; ++j) s = fma2(e[j], e[j], s);
@@ -172,9 +213,10 @@ __device__ __forceinline__ float mean_of(float s, float n, float inv_n)
 }
 
 // Statistics of R rows that a group of TPR threads holds in registers (columns and rows that are not there: zero).  The
-// variance is a second pass over the registers, so that nothing cancels.  FULL: every chunk is there.
-template <bool FULL, bool VEC, int TPR, int NC, int R>
-__device__ __forceinline__ void row_statistics(const f32x2_t (*v)[NC][4], int d, float eps, float* part, float* mean, float* rstd)
+// variance is a second pass over the registers, so that nothing cancels.  FULL: every chunk is there; EDGE: chunks may be
+// partial.  Chunk m starts at column 8 m - shift.
+template <bool FULL, bool EDGE, int TPR, int NC, int R>
+__device__ __forceinline__ void row_statistics(const f32x2_t (*v)[NC][4], int d, int shift, float eps, float* part, float* mean, float* rstd)
 {
     const float n = (float)d, inv_n = 1.f / n;
     float s[R];
@@ -192,8 +234,8 @@ __device__ __forceinline__ void row_statistics(const f32x2_t (*v)[NC][4], int d,
         f32x2_t sum = both(0.f);
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            const int col = chunk_of<TPR, NC>(c) * kChunk;
-            if (FULL || col < d) sum = add2(sum, squares8(v[r][c], mean[r], VEC ? 8 : d - col));
+            const int col = (int)chunk_of<TPR, NC>(c) * kChunk - shift;
+            if (FULL || col < d) sum = add2(sum, squares8<EDGE>(v[r][c], mean[r], col, d));
         }
         s[r] = sum2(sum);
     }
@@ -264,7 +306,7 @@ __device__ __forceinline__ void norm_forward(const NormForwardParams& p, float* 
     f32x2_t v[R][NC][4];
     load_mixed<T, FULL, true, TPR, NC, R>(p, node, t, v);
     float mean[R], rstd[R];
-    row_statistics<FULL, true, TPR, NC, R>(v, p.d, p.eps, part, mean, rstd);
+    row_statistics<FULL, false, TPR, NC, R>(v, p.d, 0, p.eps, part, mean, rstd);
     if (threadIdx.x % TPR == 0)
 #pragma unroll
         for (int r = 0; r < R; ++r)
@@ -307,9 +349,134 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) norm_forward_kernel(con
     else norm_forward<T, false, TPR, NC, R>(p, part);
 }
 
-// Otherwise: the same per row, by blocks that take every gridDim.x-th set of rows of one node.  The node's weight and
-// bias (one and zero where there is none), which might have to be cut as well, are laid out in shared memory once per
-// block, each chunk's two halves in planes of their own (no bank conflicts).
+// A node's weight and bias (one and zero where there is none) laid out in shared memory, chunk m from column 8 m - shift
+// on, zero beside the row; each chunk's two halves in planes of their own (no bank conflicts).
+template <int BLOCK>
+__device__ __forceinline__ void stage_params(const NormForwardParams& p, uint32_t node, int shift, uint32_t chunks, float4* params)
+{
+    for (uint32_t at = threadIdx.x; at < chunks * kChunk; at += BLOCK) {
+        const int col = (int)at - shift;
+        const bool in = col >= 0 && col < p.d;
+        float* to = reinterpret_cast<float*>(params + (at >> 2 & 1) * chunks + (at >> 3)) + (at & 3);
+        to[0] = !in ? 0.f : p.weight ? p.weight[node * p.ldw + col] : 1.f;
+        to[8 * chunks] = in && p.bias ? p.bias[node * p.ldw + col] : 0.f;
+    }
+    __syncthreads();
+}
+__device__ __forceinline__ void staged_params(const float4* params, uint32_t chunks, uint32_t chunk, f32x2_t* w, f32x2_t* b)
+{
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const float4 qw = params[h * chunks + chunk], qb = params[(2 + h) * chunks + chunk];
+        w[2 * h] = pack2(qw.x, qw.y); w[2 * h + 1] = pack2(qw.z, qw.w);
+        b[2 * h] = pack2(qb.x, qb.y); b[2 * h + 1] = pack2(qb.z, qb.w);
+    }
+}
+
+// Rows off the alignment all alike: shifted chunks, which are aligned memory in every array.  A block takes sets of rows
+// that have one shift, and lays out the node's parameters for it once.
+template <class T, int TPR, int NC, int R>
+__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, (NC < 3 ? 640 : 512) / (TPR < 128 ? 128 : TPR)) norm_forward_shifted_kernel(const NormForwardParams p)
+{
+    constexpr int BLOCK = TPR < 128 ? 128 : TPR, G = BLOCK / TPR, LANES = lanes_of(TPR);
+    constexpr uint32_t P = kShiftRows<T>;
+    extern __shared__ float4 params[];
+    __shared__ __align__(16) float part[2 * 32 * R];
+    __shared__ __align__(16) T slots[BLOCK / LANES][16];
+    const uint32_t node = blockIdx.y, chunks = (uint32_t)(p.d + kChunk - 1) / kChunk, first_row = blockIdx.x % P;
+    const uint32_t rows = p.rows > first_row ? (p.rows - first_row + P - 1) / P : 0;   // first_row + P i
+    const int64_t all = (int64_t)p.nodes * p.rows, row0 = (int64_t)node * p.rows + first_row;
+    const int shift = shift_of(static_cast<const T*>(p.x) + row0 * p.ldx), lane = threadIdx.x % LANES;
+    const uint32_t shifted = (uint32_t)(p.d + shift + kChunk - 1) / kChunk;   // chunks of a row
+    const Span sx = span_of<T>(p.x, p.ldx, all, p.d), sr = span_of<T>(p.residual, p.ldr, all, p.d);
+    const int col0 = (int)chunk_of<TPR, NC>(0) * kChunk - shift;
+    auto col = [&](int c) { return col0 + c * LANES * kChunk; };
+    T* own_slots = slots[threadIdx.x / LANES];
+    uint32_t there[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) there[c] = columns_there(col(c), p.d);
+    stage_params<BLOCK>(p, node, shift, shifted, params);
+    const uint32_t step = gridDim.x / P * (G * R);
+    uint32_t i0 = blockIdx.x / P * (G * R), i = i0 + (G == 1 ? 0 : threadIdx.x / TPR * R);
+    for (; i0 < rows; i0 += step, i += step) {
+        const int64_t at = row0 + (int64_t)i * P;   // from here: fewer registers than pointers that are carried along
+        const T *x = static_cast<const T*>(p.x) + at * p.ldx, *res = static_cast<const T*>(p.residual) + at * p.ldr;
+        Raw8<T, true> rx[R][NC], rr[R][NC];
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (i + r < rows)
+#pragma unroll
+                for (int c = 0; c < NC; ++c)
+                    if (there[c]) load_shifted(x + r * P * p.ldx, col(c), p.d, sx, rx[r][c], own_slots);
+        if (p.residual)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (i + r < rows)
+#pragma unroll
+                    for (int c = 0; c < NC; ++c)
+                        if (there[c]) load_shifted(res + r * P * p.ldr, col(c), p.d, sr, rr[r][c], own_slots);
+        f32x2_t v[R][NC][4];
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) rx[r][c].get(v[r][c]);
+        if (p.mask.on) {
+            // lane r works out the words before the warp's first chunk in row r
+            const uint32_t t_edge = first_row + (i + (lane < R ? lane : 0)) * P;
+            const uint4 edge = drop_words(p.mask, t_edge * chunks + first_chunk_of<TPR, NC>(0) - 1, node);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                uint4 before = shfl4(group_mask<TPR>(), edge, r, LANES);
+                const uint32_t groups = (first_row + (i + r) * P) * chunks;
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    const uint4 own = drop_words(p.mask, groups + chunk_of<TPR, NC>(c), node);
+                    const uint4 left = shfl4(group_mask<TPR>(), own, (lane + LANES - 1) % LANES, LANES);
+                    uint32_t word[4];
+                    shifted_words(lane ? left : before, own, shift, word);
+                    before = left;   // lane 0 has the last lane's
+                    drop8_by(p.mask, word, v[r][c]);
+                }
+            }
+        }
+        if (p.residual)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    f32x2_t e[4];
+                    rr[r][c].get(e);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[r][c][j] = add2(v[r][c][j], e[j]);
+                }
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) keep_columns(v[r][c], i + r < rows ? there[c] : 0u);   // the rest was never loaded, or lies beside the row
+        float mean[R], rstd[R];
+        row_statistics<false, true, TPR, NC, R>(v, p.d, shift, p.eps, part, mean, rstd);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (i + r >= rows) continue;
+            if (threadIdx.x % TPR == 0) {
+                p.mean[at + r * P] = mean[r];
+                p.rstd[at + r * P] = rstd[r];
+            }
+            if (p.z) store_shifted<T, LANES, NC>(static_cast<T*>(p.z) + (at + r * P) * p.ldz, col0, p.d, shift, v[r], own_slots, lane, group_mask<TPR>());
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                if (there[c]) {
+                    f32x2_t w[4], b[4];
+                    staged_params(params, shifted, chunk_of<TPR, NC>(c), w, b);
+                    scale8(v[r][c], mean[r], rstd[r], w, b, v[r][c]);
+                }
+            store_shifted<T, LANES, NC>(static_cast<T*>(p.y) + (at + r * P) * p.ldy, col0, p.d, shift, v[r], own_slots, lane, group_mask<TPR>());
+        }
+    }
+}
+
+// Otherwise (rows off the alignment in different ways, or aligned ones whose parameters are not): by blocks that take
+// every gridDim.x-th set of rows of one node, each chunk cut out of the pieces of memory it lies in.
 template <class T, bool VEC, int TPR, int NC, int R>
 __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, 512 / (TPR < 128 ? 128 : TPR)) norm_forward_odd_kernel(const NormForwardParams p)
 {
@@ -319,13 +486,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, 512 / (TPR < 128 ? 128 
     const int lane = threadIdx.x % LANES;
     const uint32_t node = blockIdx.y;
     const uint32_t chunks = (uint32_t)(p.d + kChunk - 1) / kChunk;
-    for (uint32_t col = threadIdx.x; col < chunks * kChunk; col += BLOCK) {
-        const bool in = col < (uint32_t)p.d;
-        float* at = reinterpret_cast<float*>(params + (col >> 2 & 1) * chunks + (col >> 3)) + (col & 3);
-        at[0] = !in ? 0.f : p.weight ? p.weight[node * p.ldw + col] : 1.f;
-        at[8 * chunks] = in && p.bias ? p.bias[node * p.ldw + col] : 0.f;
-    }
-    __syncthreads();
+    stage_params<BLOCK>(p, node, 0, chunks, params);
     // all groups of a block go round equally often (barriers inside)
     for (uint32_t t0 = blockIdx.x * (G * R); t0 < p.rows; t0 += gridDim.x * (G * R)) {
         const uint32_t t = t0 + threadIdx.x / TPR * R;
@@ -333,7 +494,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, 512 / (TPR < 128 ? 128 
         f32x2_t v[R][NC][4];
         load_mixed<T, false, VEC, TPR, NC, R>(p, node, t, v);
         float mean[R], rstd[R];
-        row_statistics<false, VEC, TPR, NC, R>(v, p.d, p.eps, part, mean, rstd);
+        row_statistics<false, !VEC, TPR, NC, R>(v, p.d, 0, p.eps, part, mean, rstd);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             if (t + r >= p.rows) continue;
@@ -353,12 +514,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, 512 / (TPR < 128 ? 128 
                 f32x2_t out[4];
                 if (chunk < chunks) {
                     f32x2_t w[4], b[4];
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const float4 qw = params[h * chunks + chunk], qb = params[(2 + h) * chunks + chunk];
-                        w[2 * h] = pack2(qw.x, qw.y); w[2 * h + 1] = pack2(qw.z, qw.w);
-                        b[2 * h] = pack2(qb.x, qb.y); b[2 * h + 1] = pack2(qb.z, qb.w);
-                    }
+                    staged_params(params, chunks, chunk, w, b);
                     scale8(v[r][c], mean[r], rstd[r], w, b, out);
                 }
                 to_y.store(y, chunk * kChunk, p.d, out, lane, group_mask<TPR>(), last);
@@ -403,7 +559,7 @@ __global__ void __launch_bounds__(1024) norm_forward_wide_kernel(const NormForwa
     float sq[1] = {0.f};
     for (uint32_t chunk = threadIdx.x; chunk < chunks; chunk += 1024) {
         chunk_at(chunk, v);
-        sq[0] += sum2(squares8(v, mean, VEC ? 8 : p.d - (int)chunk * kChunk));
+        sq[0] += sum2(squares8<!VEC>(v, mean, (int)chunk * kChunk, p.d));
     }
     group_sums<1024, 1>(sq, part[1]);
     const float rstd = rsqrtf(sq[0] / (float)p.d + p.eps);   // within 2 ulp
@@ -519,6 +675,8 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR <= 32 ? 5 : TPR <= 
     constexpr int E = 16 / sizeof(T);   // columns of a piece
     extern __shared__ uint4 stage[];   // two sets of [tensor][r][c][warp][piece]
     __shared__ __align__(16) float part[2][BLOCK / 32 * 2 * R];
+    __shared__ __align__(16) T slots[SHIFT ? BLOCK / LANES : 1][16];
+    T* own_slots = slots[SHIFT ? threadIdx.x / LANES : 0];
     const int sub = G == 1 ? 0 : threadIdx.x / TPR, tensors = p.dz ? 3 : 2;
     const uint32_t node = blockIdx.y, chunks = (uint32_t)(p.d + kChunk - 1) / kChunk;
     const uint32_t first_row = SHIFT ? blockIdx.x % P : 0;   // the block's rows: first_row + P i
@@ -534,9 +692,11 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR <= 32 ? 5 : TPR <= 
         return stage + ((((buf * 3 + tensor) * R + r) * NC + c) * BLOCK + (threadIdx.x - lane)) * Q + at;
     };
 
+    uint32_t there[NC];
     f32x2_t w[NC][4], dw[NC][4], db[NC][4];
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
+        there[c] = SHIFT ? columns_there(col(c), p.d) : 0xFFu;
 #pragma unroll
         for (int j = 0; j < 4; ++j) dw[c][j] = db[c][j] = both(0.f), w[c][j] = both(1.f);
         if (p.weight && mine(c)) {
@@ -572,13 +732,11 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR <= 32 ? 5 : TPR <= 
                 if (!full && at >= p.d) continue;
                 const T* from = row + at;
                 uint4* to = place(buf, tensor, r, c, piece);
-                if (!SHIFT || (reinterpret_cast<const char*>(from) >= s.lo && reinterpret_cast<const char*>(from + E) <= s.hi)) {
+                if (!SHIFT || (at >= 0 && at + E <= p.d) || (reinterpret_cast<const char*>(from) >= s.lo && reinterpret_cast<const char*>(from + E) <= s.hi)) {
                     copy16_async(smem_u32(to), from);
                 } else {   // the array's first or last row
-                    T v[E];
-#pragma unroll
-                    for (int e = 0; e < E; ++e) v[e] = at + e >= 0 && at + e < p.d ? from[e] : from_f32<T>(0.f);
-                    *to = *reinterpret_cast<const uint4*>(v);
+#pragma unroll 1
+                    for (int e = 0; e < E; ++e) reinterpret_cast<T*>(to)[e] = at + e >= 0 && at + e < p.d ? from[e] : from_f32<T>(0.f);
                 }
             }
     };
@@ -638,8 +796,8 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR <= 32 ? 5 : TPR <= 
                     chunk_in(buf, 0, r, c, vz);
                     chunk_in(buf, 1, r, c, vy);
                     if (SHIFT) {   // what lies beside the row; the second pass does not store it
-                        keep_columns(vz, col(c), p.d);
-                        keep_columns(vy, col(c), p.d);
+                        keep_columns(vz, there[c]);
+                        keep_columns(vy, there[c]);
                     }
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
@@ -684,11 +842,9 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR <= 32 ? 5 : TPR <= 
                     for (int j = 0; j < 4; ++j) g[c][j] = add2(g[c][j], e[j]);
                 }
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                if (!FULL && !mine(c)) continue;
-                if (SHIFT) store_shifted(dres + r * row_g, col(c), p.d, g[c]);
-                else store8<T>(dres + r * row_g + col(c), g[c]);
-            }
+            for (int c = 0; c < NC; ++c)
+                if (!SHIFT && (FULL || mine(c))) store8<T>(dres + r * row_g + col(c), g[c]);
+            if (SHIFT) store_shifted<T, LANES, NC>(dres + r * row_g, col(0), p.d, shift, g, own_slots, lane, group_mask<TPR>());
             if (!p.dx) continue;
             const uint32_t groups = (first_row + (i + r) * P) * chunks;
             uint4 before = SHIFT ? shfl4(group_mask<TPR>(), edge, r, LANES) : edge;
@@ -701,15 +857,14 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR <= 32 ? 5 : TPR <= 
                     uint32_t word[4];
                     shifted_words(lane ? left : before, own, shift, word);
                     before = left;   // lane 0 has the last lane's
-                    if (!mine(c)) continue;
                     drop8_by(p.mask, word, g[c]);
-                    store_shifted(dx + r * row_x, col(c), p.d, g[c]);
                 } else {
                     if (!FULL && !mine(c)) continue;
                     drop8(p.mask, group, node, g[c]);
                     store8<T>(dx + r * row_x + col(c), g[c]);
                 }
             }
+            if (SHIFT) store_shifted<T, LANES, NC>(dx + r * row_x, col(0), p.d, shift, g, own_slots, lane, group_mask<TPR>());
         }
     };
 #pragma unroll
@@ -983,6 +1138,15 @@ cudaError_t dropout_rows(DropoutParams& p, cudaStream_t s)
     return cudaGetLastError();
 }
 
+template <class T, int TPR, int NC>
+cudaError_t dropout_shifted(DropoutParams& p, cudaStream_t s)
+{
+    p.stretches = make_divisor((p.d + kShiftRows<T> - 1 + NC * TPR * kChunk - 1) / (NC * TPR * kChunk));
+    const uint64_t groups = (uint64_t)p.rows * p.stretches.d;
+    dropout_shifted_kernel<T, TPR, NC><<<dim3((unsigned)((groups + 256 / TPR - 1) / (256 / TPR)), p.nodes), 256, 0, s>>>(p);
+    return cudaGetLastError();
+}
+
 template <class T, bool VEC>
 cudaError_t dropout_of(DropoutParams p, cudaStream_t s)
 {
@@ -996,6 +1160,13 @@ cudaError_t dropout_of(DropoutParams p, cudaStream_t s)
             else dropout_dense_kernel<T, 4><<<dim3((unsigned)((total + 1023) / 1024), p.nodes), 256, 0, s>>>(p);
             return cudaGetLastError();
         }
+    }
+    if (!VEC && p.shifted) {
+        const int d = p.d + (int)kShiftRows<T> - 1;
+        return d <= 64    ? dropout_shifted<T, 8, 1>(p, s)
+               : d <= 256 ? dropout_shifted<T, 32, 1>(p, s)
+               : d <= 512 ? dropout_shifted<T, 32, 2>(p, s)
+                          : dropout_shifted<T, 32, 4>(p, s);
     }
     return chunks <= 8    ? dropout_rows<T, VEC, 8, 1>(p, s)
            : chunks <= 32 ? dropout_rows<T, VEC, 32, 1>(p, s)
@@ -1022,6 +1193,26 @@ cudaError_t forward_odd(const NormForwardParams& p, cudaStream_t s)
 }
 
 template <class T, int TPR, int NC, int R>
+cudaError_t forward_shifted(const NormForwardParams& p, cudaStream_t s)
+{
+    constexpr int BLOCK = TPR < 128 ? 128 : TPR, SET = BLOCK / TPR * R;
+    constexpr uint32_t P = kShiftRows<T>;
+    const size_t smem = (size_t)((p.d + P + kChunk - 1) / kChunk) * 64;
+    const auto kernel = norm_forward_shifted_kernel<T, TPR, NC, R>;
+    if (smem > 47 * 1024) {
+        static unsigned long long limit_set = 0;
+        const cudaError_t e = ensure_smem_limit(kernel, (kForwardOddWide + 16) * 8, limit_set);
+        if (e != cudaSuccess) return e;
+    }
+    static int regs = 0;
+    // as many blocks as fit, in whole classes of rows
+    const uint32_t sets = ((p.rows + P - 1) / P + SET - 1) / SET;
+    const uint32_t room = (uint32_t)(kSMs * blocks_per_sm(kernel, BLOCK, smem, regs)) / (p.nodes * P);
+    kernel<<<dim3(P * (sets < room ? sets : room ? room : 1), p.nodes), BLOCK, smem, s>>>(p);
+    return cudaGetLastError();
+}
+
+template <class T, int TPR, int NC, int R>
 cudaError_t forward_as(const NormForwardParams& p, cudaStream_t s)
 {
     constexpr int BLOCK = TPR < 128 ? 128 : TPR, SET = BLOCK / TPR * R;
@@ -1042,6 +1233,18 @@ cudaError_t forward_of(const NormForwardParams& p, cudaStream_t s)
             if (p.d <= 4096) return forward_as<T, 128, 4, 1>(p, s);
             if (p.d <= 8192) return forward_as<T, 512, 2, 1>(p, s);
             if (p.d <= kForwardWide) return forward_as<T, 512, 4, 1>(p, s);
+        }
+    if constexpr (!VEC)
+        if (p.shifted) {
+            const int d = p.d + (int)kShiftRows<T> - 1;
+            if (d <= 64) return forward_shifted<T, 8, 1, 2>(p, s);
+            if (d <= 256) return forward_shifted<T, 32, 1, 2>(p, s);
+            if (d <= 512) return forward_shifted<T, 32, 2, 1>(p, s);
+            if (d <= 1024) return forward_shifted<T, 64, 2, 1>(p, s);
+            if (d <= 1536) return forward_shifted<T, 64, 3, 1>(p, s);
+            if (d <= 2048) return forward_shifted<T, 128, 2, 1>(p, s);
+            if (d <= 4096) return forward_shifted<T, 256, 2, 1>(p, s);
+            if (d <= kForwardOddWide) return forward_shifted<T, 512, 2, 1>(p, s);
         }
     if (p.d <= 64) return forward_odd<T, VEC, 8, 1, 2>(p, s);
     if (p.d <= 256) return forward_odd<T, VEC, 32, 1, 2>(p, s);
@@ -1090,7 +1293,9 @@ cudaError_t backward_by_width(const NormBackwardParams& p, cudaStream_t s)
     if (d <= 1024) return backward_as<T, SHIFT, 128, 1, R, 2>(p, s);
     if (d <= 2048) return backward_as<T, SHIFT, 256, 1, R, 2>(p, s);
     if (d <= 4096) return backward_as<T, SHIFT, 512, 1, R, 2>(p, s);
-    return backward_as<T, SHIFT, 1024, 1, R / 2, 2>(p, s);
+    // (a shifted row's kernel does not fit the 64 registers of 1024 threads)
+    if constexpr (SHIFT) return backward_as<T, SHIFT, 512, 2, R / 2, 2>(p, s);
+    else return backward_as<T, SHIFT, 1024, 1, R / 2, 2>(p, s);
 }
 
 template <class T, bool VEC>

@@ -11,6 +11,7 @@ struct DropoutParams {
     uint32_t nodes, rows;    // rows per node
     int32_t d;
     Divisor chunks, stretches;   // set by the launch
+    bool shifted;                // rows of x and y are off the 16-byte alignment alike
     DropMask mask;
 };
 
@@ -24,6 +25,7 @@ struct NormForwardParams {
     int32_t d;
     float eps;
     bool wvec;               // weight and bias rows allow 128-bit accesses
+    bool shifted;            // rows of all activations are off the 16-byte alignment alike
     DropMask mask;
 };
 

@@ -335,48 +335,74 @@ template <class T> constexpr uint32_t kShiftRows = 16 / sizeof(T);
 template <class T>
 __device__ __forceinline__ int shift_of(const T* row) { return (int)((uint32_t)(uintptr_t)row & 15u) / (int)sizeof(T); }
 
-// Zeroes the columns outside first .. end - 1 of a chunk that starts at column `col`.
-__device__ __forceinline__ void keep_columns(f32x2_t* v, int col, int d)
+// The columns of a chunk from column `col` on that lie in the row, a bit each; and zero in place of the others.
+__device__ __forceinline__ uint32_t columns_there(int col, int d)
 {
-    if (col >= 0 && col + 8 <= d) return;
+    const int first = max(0, -col), end = max(first, min(8, d - col));
+    return (1u << end) - (1u << first);
+}
+__device__ __forceinline__ void keep_columns(f32x2_t* v, uint32_t there)
+{
+    if (there == 0xFFu) return;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const float2 f = unpack2(v[j]);
-        const int c = col + 2 * j;
-        v[j] = pack2(c >= 0 && c < d ? f.x : 0.f, c + 1 >= 0 && c + 1 < d ? f.y : 0.f);
+        v[j] = pack2(there & 1u << 2 * j ? f.x : 0.f, there & 2u << 2 * j ? f.y : 0.f);
     }
 }
 
 // Reads the aligned chunk at column `col` (possibly before the row's start or past its end) into the words of a chunk;
-// bytes outside the array's span are not touched and come out zero.
+// bytes outside the array's span are not touched and come out zero.  slots: as for store_shifted.
 template <class T>
-__device__ __forceinline__ void load_shifted(const T* row, int col, int d, const Span& s, Raw8<T, true>& raw)
+__device__ __forceinline__ void load_shifted(const T* row, int col, int d, const Span& s, Raw8<T, true>& raw, T* slots)
 {
     constexpr int W = 2 * sizeof(T);
     const char* at = reinterpret_cast<const char*>(row + col);
-    if (at >= s.lo && at + 4 * W <= s.hi) {
+    if ((col >= 0 && col + 8 <= d) || (at >= s.lo && at + 4 * W <= s.hi)) {
         raw.load(row, col, d, s);
-    } else {
-        f32x2_t v[4];
+    } else {   // an end of the array's first or last row
+        T* to = slots + (col < 0 ? 0 : 8);
+#pragma unroll 1
+        for (int j = 0; j < 8; ++j) to[j] = col + j >= 0 && col + j < d ? row[col + j] : from_f32<T>(0.f);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int c = col + 2 * j;
-            v[j] = pack2(c >= 0 && c < d ? to_f32(row[c]) : 0.f, c + 1 >= 0 && c + 1 < d ? to_f32(row[c + 1]) : 0.f);
+        for (int i = 0; i < W / 4; ++i) {
+            const uint4 q = reinterpret_cast<const uint4*>(to)[i];
+            raw.w[4 * i] = q.x; raw.w[4 * i + 1] = q.y; raw.w[4 * i + 2] = q.z; raw.w[4 * i + 3] = q.w;
         }
-        pack8<T>(v, raw.w);
     }
 }
 
-template <class T>
-__device__ __forceinline__ void store_shifted(T* row, int col, int d, const f32x2_t* v)
+// Stores the NC chunks (the c-th at column col0 + 8 c LANES, col0 = 8 m - shift for the lane's m) that each of LANES lanes
+// holds of a row.  The partial chunks at the row's ends go through `slots` (two chunks for these lanes), from where a lane
+// stores one element each: element by element from the two lanes that hold them, the ends cost more than all the rest.
+template <class T, int LANES, int NC>
+__device__ __forceinline__ void store_shifted(T* row, int col0, int d, int shift, const f32x2_t (*v)[4], T* slots, int lane, unsigned mask)
 {
-    if (col >= 0 && col + 8 <= d) {
-        store8<T>(row + col, v);
-    } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (col + j >= 0 && col + j < d) row[col + j] = from_f32<T>(element(v, j));
+    for (int c = 0; c < NC; ++c) {
+        const int col = col0 + 8 * c * LANES;
+        if (col >= 0 && col + 8 <= d) {
+            store8<T>(row + col, v[c]);
+        } else if (col < d) {
+            T* to = slots + (col < 0 ? 0 : 8);
+            uint32_t o[2 * sizeof(T)];
+            pack8<T>(v[c], o);
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+                reinterpret_cast<uint4*>(to)[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+        }
     }
+    // the same for all these lanes: whether the row's ends are theirs
+    const int first = col0 - 8 * lane, last = (d + shift - 1) / 8 * 8 - shift;   // column of their first chunk, of the row's last
+    const bool head = first < 0, tail = last >= 0 && last + 8 > d && last >= first && last < first + 8 * NC * LANES;
+    if (!head && !tail) return;
+    __syncwarp(mask);
+#pragma unroll
+    for (int k = 0; k < (LANES < 16 ? 2 : 1); ++k) {
+        const int e = lane + k * LANES, at = e < 8 ? first + e : last + e - 8;
+        if (e < 16 && (e < 8 ? head : tail) && at >= 0 && at < d) row[at] = slots[e];
+    }
+    __syncwarp(mask);   // the slots may be written again
 }
 
 // The random words of a shifted chunk: those of generator calls m - 1 (the chunk's first s columns) and m.

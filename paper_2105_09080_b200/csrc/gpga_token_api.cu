@@ -169,6 +169,10 @@ int32_t gpga_dropout(const gpga_dropout_args_t* a, void* stream)
     q.rows = (uint32_t)a->rows;
     q.d = (int32_t)a->d;
     const bool vec = a->d % kChunk == 0 && vectors(a->x, a->ldx, size) && vectors(a->y, a->ldy, size);
+    Alike alike;
+    alike.add(a->x, a->ldx, size);
+    alike.add(a->y, a->ldy, size);
+    q.shifted = alike.yes;
     return launched(launch_dropout(q, (int)a->dtype, vec, static_cast<cudaStream_t>(stream)), "gpga_dropout");
 }
 
@@ -211,6 +215,12 @@ int32_t gpga_layer_norm_forward(const gpga_layer_norm_forward_args_t* a, void* s
     q.wvec = full && vectors(a->weight, a->ldw, 4) && vectors(a->bias, a->ldw, 4);
     const bool vec = full && vectors(a->x, a->ldx, size) && vectors(a->residual, a->ldr, size) && vectors(a->y, a->ldy, size) &&
                      vectors(a->z, a->ldz, size);
+    Alike alike;
+    alike.add(a->x, a->ldx, size);
+    alike.add(a->residual, a->ldr, size);
+    alike.add(a->y, a->ldy, size);
+    alike.add(a->z, a->ldz, size);
+    q.shifted = alike.yes;
     return launched(launch_norm_forward(q, (int)a->dtype, vec, static_cast<cudaStream_t>(stream)), "gpga_layer_norm_forward");
 }
 
