@@ -24,6 +24,8 @@ __device__ __forceinline__ uint32_t first_chunk_of(int c)
 {
     return TPR <= 32 ? c * TPR : (threadIdx.x % TPR / 32 * NC + c) * 32;
 }
+// Threads of a block for groups of TPR: several groups of up to 64, one wider one.
+__host__ __device__ constexpr int block_of(int tpr) { return tpr <= 64 ? 128 : tpr; }
 __host__ __device__ constexpr int lanes_of(int tpr) { return tpr < 32 ? tpr : 32; }
 
 
@@ -617,7 +619,7 @@ template <int TPR, int NC, class Col0>
 __device__ __forceinline__ void write_column_sums(const NormBackwardParams& p, uint32_t node, f32x2_t (*dw)[4], f32x2_t (*db)[4], float* sums,
                                                   Col0 col0)
 {
-    constexpr int BLOCK = TPR < 128 ? 128 : TPR, G = BLOCK / TPR;
+    constexpr int G = block_of(TPR) / TPR;
     if (!p.dweight && !p.dbias) return;
     const int sub = threadIdx.x / TPR;
     if constexpr (G > 1) {
@@ -667,10 +669,10 @@ __device__ __forceinline__ void write_column_sums(const NormBackwardParams& p, u
 // there again.  In fp32 a chunk is two 16-byte pieces; lanes copy neighbouring pieces, so that whole sectors come at once,
 // and the pieces lie exchanged in every other group of eight, so that a warp reads its chunks without bank conflicts.
 // kSets: sets of rows in shared memory, one worked on, the others on their way.
-template <class T, bool SHIFT, int TPR, int NC, int R, int kSets>
-__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR <= 32 ? 5 : TPR <= 128 ? 4 : TPR == 256 ? 2 : 1) norm_backward_kernel(const NormBackwardParams p)
+template <class T, bool SHIFT, int TPR, int NC, int R, int kSets, int kPerSM>
+__global__ void __launch_bounds__(block_of(TPR), kPerSM) norm_backward_kernel(const NormBackwardParams p)
 {
-    constexpr int BLOCK = TPR < 128 ? 128 : TPR, G = BLOCK / TPR, LANES = lanes_of(TPR), Q = sizeof(T) / 2;   // Q: 16-byte pieces of a chunk
+    constexpr int BLOCK = block_of(TPR), G = BLOCK / TPR, LANES = lanes_of(TPR), Q = sizeof(T) / 2;   // Q: 16-byte pieces of a chunk
     constexpr uint32_t P = SHIFT ? kShiftRows<T> : 1;
     constexpr int E = 16 / sizeof(T);   // columns of a piece
     extern __shared__ uint4 stage[];   // two sets of [tensor][r][c][warp][piece]
@@ -1257,13 +1259,13 @@ cudaError_t forward_of(const NormForwardParams& p, cudaStream_t s)
     return cudaGetLastError();
 }
 
-template <class T, bool SHIFT, int TPR, int NC, int R, int kSets>
+template <class T, bool SHIFT, int TPR, int NC, int R, int kSets, int kPerSM>
 cudaError_t backward_as(const NormBackwardParams& p, cudaStream_t s)
 {
-    constexpr int BLOCK = TPR < 128 ? 128 : TPR, G = BLOCK / TPR;
+    constexpr int BLOCK = block_of(TPR), G = BLOCK / TPR;
     constexpr size_t kStage = (size_t)kSets * 3 * R * NC * 8 * sizeof(T) * BLOCK, kSums = G > 1 ? (size_t)2 * TPR * NC * 8 * 4 : 0;
     constexpr size_t smem = kStage > kSums ? kStage : kSums;
-    const auto kernel = norm_backward_kernel<T, SHIFT, TPR, NC, R, kSets>;
+    const auto kernel = norm_backward_kernel<T, SHIFT, TPR, NC, R, kSets, kPerSM>;
     static unsigned long long limit_set = 0;
     const cudaError_t e = ensure_smem_limit(kernel, (int)smem, limit_set);
     if (e != cudaSuccess) return e;
@@ -1287,15 +1289,19 @@ cudaError_t backward_by_width(const NormBackwardParams& p, cudaStream_t s)
     // 44 and 37 us for 4 x 60000 rows of 64.
     constexpr int R = sizeof(T) == 4 ? 2 : 4;
     const int d = p.d + (SHIFT ? (int)kShiftRows<T> - 1 : 0);
-    if (d <= 64) return backward_as<T, SHIFT, 8, 1, R / 2, 3>(p, s);
-    if (d <= 256) return backward_as<T, SHIFT, 32, 1, R / 2, 3>(p, s);
-    if (d <= 512) return backward_as<T, SHIFT, 64, 1, R, 2>(p, s);
-    if (d <= 1024) return backward_as<T, SHIFT, 128, 1, R, 2>(p, s);
-    if (d <= 2048) return backward_as<T, SHIFT, 256, 1, R, 2>(p, s);
-    if (d <= 4096) return backward_as<T, SHIFT, 512, 1, R, 2>(p, s);
+    if (d <= 64) return backward_as<T, SHIFT, 8, 1, R / 2, 3, 5>(p, s);
+    if (d <= 256) return backward_as<T, SHIFT, 32, 1, R / 2, 3, 5>(p, s);
+    if (d <= 512) return backward_as<T, SHIFT, 64, 1, R, 2, 4>(p, s);
+    if (d <= 768) return backward_as<T, SHIFT, 96, 1, R, 2, 5>(p, s);
+    if (d <= 1024) return backward_as<T, SHIFT, 128, 1, R, 2, 4>(p, s);
+    if (d <= 1280) return backward_as<T, SHIFT, 160, 1, R, 2, 3>(p, s);
+    if (d <= 1536) return backward_as<T, SHIFT, 192, 1, R, 2, SHIFT ? 2 : 3>(p, s);
+    if (d <= 2048) return backward_as<T, SHIFT, 256, 1, R, 2, 2>(p, s);
+    if (d <= 2560) return backward_as<T, SHIFT, 320, 1, R / 2, 3, SHIFT ? 1 : 2>(p, s);
+    if (d <= 4096) return backward_as<T, SHIFT, 512, 1, R, 2, 1>(p, s);
     // (a shifted row's kernel does not fit the 64 registers of 1024 threads)
-    if constexpr (SHIFT) return backward_as<T, SHIFT, 512, 2, R / 2, 2>(p, s);
-    else return backward_as<T, SHIFT, 1024, 1, R / 2, 2>(p, s);
+    if constexpr (SHIFT) return backward_as<T, SHIFT, 512, 2, 1, 2, 1>(p, s);
+    else return backward_as<T, SHIFT, 1024, 1, R / 2, 2, 1>(p, s);
 }
 
 template <class T, bool VEC>
@@ -1353,7 +1359,7 @@ int norm_backward_splits(int64_t nodes, int64_t rows, int64_t d)
     // Blocks that an SM holds (four or five of 128 threads by their shared memory), and no more than sets of four rows per
     // group; a multiple of eight where there are as many, since blocks of shifted rows take every eighth row (a fourth in fp32).
     const int64_t set = 4 * (d <= 64 ? 16 : d <= 256 ? 4 : d <= 512 ? 2 : 1);
-    const int64_t per_sm = d <= 256 ? 5 : d <= 1024 ? 4 : d <= 2048 ? 2 : 1;
+    const int64_t per_sm = d <= 256 ? 5 : d <= 512 ? 4 : d <= 768 ? 5 : d <= 1024 ? 4 : d <= 1536 ? 3 : d <= 2560 ? 2 : 1;
     int64_t splits = (kSMs * per_sm) / nodes;
     const int64_t groups = (rows + set - 1) / set;
     if (splits > groups) splits = groups;
