@@ -400,23 +400,29 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, (NC < 3 ? 640 : 512) / 
     stage_params<BLOCK>(p, node, shift, shifted, params);
     const uint32_t step = gridDim.x / P * (G * R);
     uint32_t i0 = blockIdx.x / P * (G * R), i = i0 + (G == 1 ? 0 : threadIdx.x / TPR * R);
-    for (; i0 < rows; i0 += step, i += step) {
-        const int64_t at = row0 + (int64_t)i * P;   // from here: fewer registers than pointers that are carried along
-        const T *x = static_cast<const T*>(p.x) + at * p.ldx, *res = static_cast<const T*>(p.residual) + at * p.ldr;
-        Raw8<T, true> rx[R][NC], rr[R][NC];
+    Raw8<T, true> rx[R][NC], rr[R][NC];
+    auto load = [&](uint32_t from) {   // rows first_row + P from, ...
+        const int64_t at = row0 + (int64_t)from * P;
+        const T* x = static_cast<const T*>(p.x) + at * p.ldx;
 #pragma unroll
         for (int r = 0; r < R; ++r)
-            if (i + r < rows)
+            if (from + r < rows)
 #pragma unroll
                 for (int c = 0; c < NC; ++c)
                     if (there[c]) load_shifted(x + r * P * p.ldx, col(c), p.d, sx, rx[r][c], own_slots);
-        if (p.residual)
+        if (p.residual) {
+            const T* res = static_cast<const T*>(p.residual) + at * p.ldr;
 #pragma unroll
             for (int r = 0; r < R; ++r)
-                if (i + r < rows)
+                if (from + r < rows)
 #pragma unroll
                     for (int c = 0; c < NC; ++c)
                         if (there[c]) load_shifted(res + r * P * p.ldr, col(c), p.d, sr, rr[r][c], own_slots);
+        }
+    };
+    load(i);
+    for (; i0 < rows; i0 += step, i += step) {
+        const int64_t at = row0 + (int64_t)i * P;   // pointers from here: fewer registers than ones that are carried along
         f32x2_t v[R][NC][4];
 #pragma unroll
         for (int r = 0; r < R; ++r)
@@ -455,6 +461,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, (NC < 3 ? 640 : 512) / 
         for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int c = 0; c < NC; ++c) keep_columns(v[r][c], i + r < rows ? there[c] : 0u);   // the rest was never loaded, or lies beside the row
+        load(i + step);   // on their way during the sums
         float mean[R], rstd[R];
         row_statistics<false, true, TPR, NC, R>(v, p.d, shift, p.eps, part, mean, rstd);
 #pragma unroll
@@ -818,7 +825,7 @@ __global__ void __launch_bounds__(block_of(TPR), kPerSM) norm_backward_kernel(co
         group_sums<TPR, 2 * R>(s, part[odd]);
         asm volatile("" ::: "memory");   // the chunks are read again, not kept
         uint4 edge = make_uint4(0, 0, 0, 0);   // SHIFT: lane r has the words before the warp's first chunk in row r
-        if (SHIFT && p.dx) {
+        if (SHIFT && p.dx && p.mask.on) {
             const uint32_t t = first_row + (i + (lane < R ? lane : 0)) * P;
             edge = drop_words(p.mask, t * chunks + first_chunk_of<TPR, NC>(0) - 1, node);
         }
@@ -854,6 +861,7 @@ __global__ void __launch_bounds__(block_of(TPR), kPerSM) norm_backward_kernel(co
             for (int c = 0; c < NC; ++c) {
                 const uint32_t group = groups + chunk_of<TPR, NC>(c);
                 if constexpr (SHIFT) {
+                    if (!p.mask.on) continue;   // a probability that rounds to zero
                     const uint4 own = drop_words(p.mask, group, node);
                     const uint4 left = shfl4(group_mask<TPR>(), own, (lane + LANES - 1) % LANES, LANES);
                     uint32_t word[4];
@@ -1228,6 +1236,7 @@ cudaError_t forward_of(const NormForwardParams& p, cudaStream_t s)
     if constexpr (VEC)
         if (p.weight && p.bias && p.wvec) {
             if (p.d <= 64) return forward_as<T, 8, 1, 4>(p, s);
+            if (p.d <= 128) return forward_as<T, 16, 1, 4>(p, s);
             if (p.d <= 256) return forward_as<T, 32, 1, 4>(p, s);
             if (p.d <= 512) return forward_as<T, 32, 2, 2>(p, s);
             if (p.d <= 1024) return forward_as<T, 32, 4, 1>(p, s);
@@ -1240,6 +1249,7 @@ cudaError_t forward_of(const NormForwardParams& p, cudaStream_t s)
         if (p.shifted) {
             const int d = p.d + (int)kShiftRows<T> - 1;
             if (d <= 64) return forward_shifted<T, 8, 1, 2>(p, s);
+            if (d <= 128) return forward_shifted<T, 16, 1, 2>(p, s);
             if (d <= 256) return forward_shifted<T, 32, 1, 2>(p, s);
             if (d <= 512) return forward_shifted<T, 32, 2, 1>(p, s);
             if (d <= 1024) return forward_shifted<T, 64, 2, 1>(p, s);
@@ -1290,6 +1300,7 @@ cudaError_t backward_by_width(const NormBackwardParams& p, cudaStream_t s)
     constexpr int R = sizeof(T) == 4 ? 2 : 4;
     const int d = p.d + (SHIFT ? (int)kShiftRows<T> - 1 : 0);
     if (d <= 64) return backward_as<T, SHIFT, 8, 1, R / 2, 3, 5>(p, s);
+    if (d <= 128) return backward_as<T, SHIFT, 16, 1, R / 2, 3, 5>(p, s);
     if (d <= 256) return backward_as<T, SHIFT, 32, 1, R / 2, 3, 5>(p, s);
     if (d <= 512) return backward_as<T, SHIFT, 64, 1, R, 2, 4>(p, s);
     if (d <= 768) return backward_as<T, SHIFT, 96, 1, R, 2, 5>(p, s);
@@ -1358,11 +1369,12 @@ int norm_backward_splits(int64_t nodes, int64_t rows, int64_t d)
     if (rows < 1) return 1;
     // Blocks that an SM holds (four or five of 128 threads by their shared memory), and no more than sets of four rows per
     // group; a multiple of eight where there are as many, since blocks of shifted rows take every eighth row (a fourth in fp32).
-    const int64_t set = 4 * (d <= 64 ? 16 : d <= 256 ? 4 : d <= 512 ? 2 : 1);
+    const int64_t set = 4 * (d <= 64 ? 16 : d <= 128 ? 8 : d <= 256 ? 4 : d <= 512 ? 2 : 1);
     const int64_t per_sm = d <= 256 ? 5 : d <= 512 ? 4 : d <= 768 ? 5 : d <= 1024 ? 4 : d <= 1536 ? 3 : d <= 2560 ? 2 : 1;
     int64_t splits = (kSMs * per_sm) / nodes;
     const int64_t groups = (rows + set - 1) / set;
     if (splits > groups) splits = groups;
+    if (groups <= 2) splits = 1;   // one launch: 8 rows of 1024 one set after the other 4.8 us, 32 rows in two launches 5.3 us
     if (splits >= 8) splits = splits / 8 * 8;
     return (int)(splits < 1 ? 1 : splits);
 }

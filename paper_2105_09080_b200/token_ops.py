@@ -36,7 +36,7 @@ ARGS = {
     "gpga_layer_norm_backward": struct.Struct("=11Q13qdQ3q"),
 }
 
-_current_device = torch.cuda.current_device
+_current_device = torch._C._cuda_getDevice
 _raw_stream = torch._C._cuda_getCurrentRawStream
 
 

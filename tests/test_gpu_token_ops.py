@@ -269,7 +269,7 @@ def test_dropout_of_views_and_special_values():
 
 
 # ---- layer norm ------------------------------------------------------------------------------------
-SHAPES = [(1, 1, 1), (1, 3, 7), (2, 5, 8), (1, 40, 64), (3, 11, 65), (2, 9, 200), (1, 300, 256), (2, 13, 512), (1, 17, 1000),
+SHAPES = [(1, 1, 1), (1, 3, 7), (2, 70, 121), (1, 33, 128), (3, 9, 700), (1, 19, 1208), (2, 7, 1501), (1, 6, 2560), (2, 5, 8), (1, 40, 64), (3, 11, 65), (2, 9, 200), (1, 300, 256), (2, 13, 512), (1, 17, 1000),
           (3, 50, 1023), (2, 33, 1024), (1, 6, 2048), (2, 3, 2056), (1, 4, 4100), (1, 5, 8192), (1, 3, 9001), (2, 2, 16392)]
 
 
@@ -462,6 +462,79 @@ def test_layer_norm_of_views_in_place_and_without_rows():
     dres, _, dw, db = pkg.layer_norm_backward(none, none, mean, rstd, w)
     assert y.shape == none.shape and (dw == 0).all() and (db == 0).all()
     assert pkg.dropout(none, 0.5, 1).shape == none.shape
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [1, 5, 64, 120, 513, 1024, 1030, 2050, 4099, 8185])
+def test_vectors_off_the_alignment_alike(dtype, d):
+    """Every activation a slice at one place of a buffer of one width: the results are a dense copy's, and nothing beside
+    the slices is written."""
+    g = gen(17)
+    n, T, at = 2, 301, 3
+    w, b = 1 + 0.2 * normal(g, n, d), normal(g, n, d)
+
+    def wide(fill=None):
+        t = normal(g, n, T, d + 13, dtype=dtype) if fill is None else torch.full((n, T, d + 13), fill, device="cuda", dtype=dtype)
+        return t, t[..., at:at + d]
+
+    (_, x), (_, r), (_, dy), (_, e) = wide(), wide(), wide(), wide()
+    outs = [wide(9.0) for _ in range(5)]
+    mask = {"p": 0.3, "seed": 4, "k": 2, "site": 1}
+    y, z, mean, rstd = pkg.layer_norm_forward(x, w, b, residual=r, out=outs[0][1], z=outs[1][1], **mask)
+    check_forward(x.contiguous(), r.contiguous(), w, b, 1e-5, 0.3, {**mask, "node0": 0}, n, (y, z, mean, rstd), dtype)
+    got = pkg.layer_norm_backward(dy, z, mean, rstd, w, dz=e, dresidual=outs[2][1], dx=outs[3][1], **mask)
+    ref = pkg.layer_norm_backward(dy.contiguous(), z.contiguous(), mean, rstd, w, dz=e.contiguous(), **mask)
+    size = ref[0].double().abs().max()
+    for a, c in zip(got[:2], ref[:2]):   # the same sums, perhaps in another grouping
+        assert (a.double() - c.double()).abs().max() <= (EPS[dtype] + 2 * depth(d) * U) * 4 * size
+    xh = (z.double() - mean.double()[..., None]) * rstd.double()[..., None]
+    near(got[2], (dy.double() * xh).sum(1), (T + 3) * U * (dy.double() * xh).abs().sum(1), torch.float32)
+    near(got[3], dy.double().sum(1), T * U * dy.double().abs().sum(1), torch.float32)
+    drop = pkg.dropout(x, 0.3, 11, nodes=n, out=outs[4][1])
+    assert torch.equal(drop, pkg.dropout(x.contiguous(), 0.3, 11, nodes=n))
+    for buf, _ in outs:
+        assert (buf[..., :at] == 9).all() and (buf[..., at + d:] == 9).all()
+
+
+@pytest.mark.parametrize("d", [40, 41, 1030, 4500])
+def test_probabilities_that_round_to_zero_and_one(d):
+    """p below 2^-17 drops nothing and leaves the factor 1, p above 1 - 2^-17 drops everything, in every operator."""
+    g = gen(18)
+    x, w = normal(g, 1, 600, d, dtype=torch.bfloat16), torch.ones(d, device="cuda")
+    for p in (1e-6, 1 - 1e-6):
+        keep = torch.ones_like(x) if p < 0.5 else torch.zeros_like(x)
+        assert torch.equal(pkg.dropout(x, p, 5), x * keep)
+        y, z, mean, rstd = pkg.layer_norm_forward(x, w, None, p=p, seed=5)
+        assert torch.equal(z, x * keep)
+        dres, dx, _, _ = pkg.layer_norm_backward(x, z, mean, rstd, w, p=p, seed=5)
+        assert torch.equal(dx, dres * keep) and (p > 0.5 or dres.abs().max() > 0)
+
+
+@pytest.mark.parametrize("d", [96, 97, 1000, 9000])
+def test_parameters_shared_and_left_out(d):
+    """One weight and one table for all nodes (node stride 0), a weight without a bias, no weight at all."""
+    g = gen(19)
+    n, T, V = 3, 7, 11
+    x, w, b = normal(g, n, T, d), 1 + 0.2 * normal(g, d), normal(g, d)
+    shared = pkg.layer_norm_forward(x, w.expand(n, d), b.expand(n, d))
+    alone = pkg.layer_norm_forward(x, w, b)
+    assert all(torch.equal(a, c) for a, c in zip(shared[::2], alone[::2]))
+    y, _, mean, rstd = pkg.layer_norm_forward(x, w, None)
+    check_forward(x, None, w[None], None, 1e-5, 0.0, None, 1, (y.view(1, n * T, d), x.view(1, n * T, d), mean, rstd), torch.float32)
+    bare = pkg.layer_norm_forward(x, None, None)
+    check_forward(x, None, None, None, 1e-5, 0.0, None, 1, (bare[0].view(1, n * T, d), x.view(1, n * T, d), mean, rstd), torch.float32)
+    dy = normal(g, n, T, d)
+    per_node = pkg.layer_norm_backward(dy, x, mean, rstd, w.expand(n, d))
+    total = pkg.layer_norm_backward(dy, x, mean, rstd, w)
+    assert per_node[2].shape == (n, d)
+    for a, c, terms in ((per_node[2], total[2], dy * (x - mean[..., None]) * rstd[..., None]), (per_node[3], total[3], dy)):
+        assert ((a.double().sum(0) - c.double()).abs() <= 2 * (n * T + 3) * U * terms.double().abs().sum((0, 1))).all()
+    none = pkg.layer_norm_backward(dy, x, mean, rstd, None)
+    ones = pkg.layer_norm_backward(dy, x, mean, rstd, torch.ones(d, device="cuda"))
+    assert torch.equal(none[0], ones[0]) and none[2] is None and none[3] is None
+    table = normal(g, V, d)
+    tokens = torch.randint(0, V, (n, T), generator=g, device="cuda")
+    assert torch.equal(pkg.embedding_forward(table.expand(n, V, d), tokens), table[tokens])
 
 
 def test_activations_beyond_32_bit_offsets():
