@@ -71,8 +71,9 @@ GradLayout grad_layout(int64_t nodes, int64_t rows, int64_t d, int64_t vocab)
     L.words = (uint32_t)((vocab + 31) / 32);
     if (rows <= kDirectTokens) return L;
     if (rows > (int64_t)kSortMax) rows = kSortMax;
-    // entries per tile: 32 leave fewer partial sums, 16 spread few tokens over the SMs (512 threads each)
-    L.tile = (rows + 31) / 32 * nodes * (L.dpad / 8) < 148 * 512 ? 16 : 32;
+    // entries per tile: 32 leave fewer partial sums, 16 or 8 spread few tokens over the SMs (512 threads each)
+    L.tile = 32;
+    while (L.tile > 8 && (rows + L.tile - 1) / L.tile * nodes * (L.dpad / 8) < 148 * 512) L.tile /= 2;
     L.tiles = (uint32_t)((rows + L.tile - 1) / L.tile);
     L.entry_off = 0;
     L.bit_off = L.entry_off + up(nodes * rows * 8);
@@ -475,19 +476,34 @@ __device__ __forceinline__ void sum_tile(const SumParams& p, uint32_t node, uint
     flush(ends.split_out);
 }
 
-// Clears a row of grad, by a warp.
-__device__ __forceinline__ void clear_row(const SumParams& p, uint32_t node, uint32_t v, uint32_t lane)
+// Zeroes `count` floats from `to` on, by THREADS threads: single ones up to the first 16 bytes and behind the last.
+template <int THREADS>
+__device__ __forceinline__ void clear_range(float* to, int64_t count, uint32_t thread)
 {
-    float* to = p.grad + node * p.node_ldg + (int64_t)v * p.ldg;
-    const int head = p.gvec ? 0 : min(p.d, (int)(-((uint32_t)(uintptr_t)to >> 2) & 3u));   // columns before the first 16 bytes
-    const int body = (p.d - head) & ~3;
-    if ((int)lane < head) to[lane] = 0.f;
+    const int64_t head = min(count, (int64_t)(-((uint32_t)(uintptr_t)to >> 2) & 3u)), body = (count - head) / 4;
+    float4* at = reinterpret_cast<float4*>(to + head);
+    if (thread < head) to[thread] = 0.f;
 #pragma unroll 4
-    for (int c = lane * 4; c < body; c += 128) __stcs(reinterpret_cast<float4*>(to + head + c), make_float4(0.f, 0.f, 0.f, 0.f));
-    if (head + body + (int)lane < p.d) to[head + body + lane] = 0.f;
+    for (int64_t i = thread; i < body; i += THREADS) __stcs(at + i, make_float4(0.f, 0.f, 0.f, 0.f));
+    const int64_t tail = head + body * 4 + thread;
+    if (tail < count) to[tail] = 0.f;
 }
 
-// Blocks 0 .. sum_blocks - 1 (x) sum tiles; the others clear the rows of grad that no token names, a warp at a time.
+// Clears the rows first .. first + n - 1 (n <= 32) of a node's grad whose bit in `named` is not set.  Neighbouring rows are
+// one range where nothing lies between them: rows of an odd width would otherwise leave partial sectors at their ends.
+template <int THREADS>
+__device__ __forceinline__ void clear_rows(const SumParams& p, uint32_t node, uint32_t first, uint32_t n, uint32_t named, uint32_t thread)
+{
+    uint32_t open = ~named & (n == 32 ? ~0u : (1u << n) - 1u);
+    while (open) {
+        const uint32_t a = __ffs(open) - 1, run = p.ldg == p.d ? __ffs(~(open >> a)) : 0;   // run: rows plus one; 0: all 32
+        const uint32_t rows = p.ldg == p.d ? (run ? run - 1 : 32 - a) : 1;
+        clear_range<THREADS>(p.grad + node * p.node_ldg + (int64_t)(first + a) * p.ldg, (int64_t)rows * p.d, thread);
+        open &= rows + a >= 32 ? 0u : ~0u << (a + rows);
+    }
+}
+
+// Blocks 0 .. sum_blocks - 1 (x) sum tiles; the others clear the rows of grad that no token names, four rows to a warp at a time.
 // Both in one launch: reads of dout and writes of grad then share the memory's time.  (The clearing blocks first, at
 // eight per SM beside the sums: 64 us instead of 58 for 65536 tokens, 1024 columns, 50021 rows.)
 template <class T, bool VEC, bool GVEC, int TX>
@@ -498,8 +514,14 @@ __global__ void __launch_bounds__(128) lookup_grad_kernel(const SumParams p)
     if (blockIdx.x >= p.sum_blocks) {
         if (blockIdx.y) return;
         const uint32_t* bits = p.bits + (int64_t)node * p.words;
-        for (uint32_t v = (blockIdx.x - p.sum_blocks) * 4 + threadIdx.x / 32; v < p.vocab; v += p.clear_blocks * 4)
-            if (!(bits[v >> 5] >> (v & 31) & 1)) clear_row(p, node, v, threadIdx.x & 31);
+        const uint32_t warp = (blockIdx.x - p.sum_blocks) * 4 + threadIdx.x / 32;
+        if (GVEC) {
+            for (uint32_t v = warp; v < p.vocab; v += p.clear_blocks * 4)
+                clear_rows<32>(p, node, v, 1, bits[v >> 5] >> (v & 31) & 1u, threadIdx.x & 31);
+        } else {
+            for (uint32_t q = warp; q * 4 < p.vocab; q += p.clear_blocks * 4)   // four rows
+                clear_rows<32>(p, node, q * 4, min(4u, p.vocab - q * 4), bits[q >> 3] >> (q & 7) * 4 & 15u, threadIdx.x & 31);
+        }
         return;
     }
     const uint32_t tile = blockIdx.x * (128 / TX) + threadIdx.x / TX;
@@ -631,17 +653,27 @@ __global__ void __launch_bounds__(128) lookup_grad_direct_kernel(const SumParams
     __syncthreads();
     if (blockIdx.x >= p.sum_blocks) {
         if (blockIdx.y) return;
-        const uint32_t share = (p.vocab + p.clear_blocks - 1) / p.clear_blocks;
-        const uint32_t begin = min((blockIdx.x - p.sum_blocks) * share, p.vocab), end = min(begin + share, p.vocab);
-        for (uint32_t v0 = begin; v0 < end; v0 += kSpan) {
-            if (v0 != begin) __syncthreads();
+        // every clear_blocks-th group of eight rows, so that the blocks that run together write one stretch of memory; a row
+        // to a warp where rows are aligned (8 tables of 32000 x 1024: 176 us, as ranges by the block 182), neighbouring rows as
+        // one range by the block where not (4 tables of 28353 x 1663: 117 us, a row to a warp 125)
+        const uint32_t block = blockIdx.x - p.sum_blocks, groups = (p.vocab + 7) / 8;
+        for (uint32_t s0 = 0; block + s0 * p.clear_blocks < groups; s0 += kSpan / 8) {
+            if (s0) __syncthreads();
             if (tid < kSpan / 32) named[tid] = 0;
             __syncthreads();
-            for (uint32_t i = tid; i < p.count; i += 128)
-                if (keys[i] >= v0 && keys[i] - v0 < kSpan) atomicOr(&named[(keys[i] - v0) >> 5], 1u << ((keys[i] - v0) & 31));
+            for (uint32_t i = tid; i < p.count; i += 128) {
+                const uint32_t group = keys[i] / 8, slot = group / p.clear_blocks;
+                if (keys[i] < p.vocab && group - slot * p.clear_blocks == block && slot >= s0 && slot - s0 < kSpan / 8)
+                    atomicOr(&named[(slot - s0) >> 2], 1u << (((slot - s0) & 3) * 8 + (keys[i] & 7)));
+            }
             __syncthreads();
-            for (uint32_t v = v0 + tid / 32; v < min(end, v0 + kSpan); v += 4)
-                if (!(named[(v - v0) >> 5] >> ((v - v0) & 31) & 1)) clear_row(p, node, v, lane);
+            for (uint32_t slot = s0; slot < s0 + kSpan / 8; ++slot) {
+                const uint32_t first = (block + slot * p.clear_blocks) * 8, of_slot = named[(slot - s0) >> 2] >> ((slot - s0) & 3) * 8 & 0xFFu;
+                if (first >= p.vocab) break;
+                if (!GVEC) clear_rows<128>(p, node, first, min(8u, p.vocab - first), of_slot, tid);
+                else
+                    for (uint32_t r = tid / 32; r < min(8u, p.vocab - first); r += 4) clear_rows<32>(p, node, first + r, 1, of_slot >> r & 1u, lane);
+            }
         }
         return;
     }
@@ -684,7 +716,7 @@ __global__ void __launch_bounds__(128) lookup_grad_direct_kernel(const SumParams
     write_sum<GVEC, 32>(p, node, token, c, lane, 0xFFFFFFFFu, acc);
 }
 
-// Blocks that clear rows, per node: four rows at least, one per warp, to a block; at most sixteen such blocks per SM.
+// Blocks that clear rows, per node: four rows at least to a block; at most sixteen such blocks per SM.
 uint32_t clear_blocks_for(const SumParams& p, uint32_t nodes)
 {
     const uint32_t units = (p.vocab + 3) / 4, most = (148 * 16 + nodes - 1) / nodes;
