@@ -14,18 +14,23 @@ __device__ __forceinline__ int64_t token_at(const void* tokens, bool is64, int64
 
 // ---- lookup -----------------------------------------------------------------------------------------
 // TPR lanes take a stretch of NC * TPR chunks of one row: one token and one division per 32 NC chunks of loads.  VEC: the
-// rows of the table and of out are aligned.  Bound: HBM, where words repeat L2.  8 x 4096 tokens of 1024 into bf16 22 us
-// (5.8 TB/s of distinct rows and outputs), a chunk per thread 27 us; 8 x 4096 of 1001 cut from the rows 41 us.
+// rows of the table and of out are aligned; otherwise chunks are shifted to out's alignment and cut out of the table's rows.
+// Bound: HBM, where words repeat L2.  8 x 4096 tokens of 1024 into bf16 22 us (5.8 TB/s of distinct rows and outputs), a
+// chunk per thread 27 us.
 template <class T, bool VEC, int TPR, int NC>
 __global__ void __launch_bounds__(256) lookup_kernel(const LookupParams p)
 {
-    const uint32_t node = blockIdx.y, chunks = p.chunks.d;
+    __shared__ __align__(16) T slots[VEC ? 1 : 256 / TPR][16];
+    const uint32_t node = blockIdx.y;
     const uint32_t g = blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
     const uint32_t t = divide(g, p.stretches);
     if (t >= p.rows) return;
-    const uint32_t first = (g - t * p.stretches.d) * (NC * TPR);
     const int lane = threadIdx.x % TPR;
     const int64_t row = (int64_t)node * p.rows + t;
+    T* out = static_cast<T*>(p.out) + row * p.ldo;
+    const int shift = VEC ? 0 : shift_of(out);
+    const int first = (int)(g - t * p.stretches.d) * (NC * TPR * kChunk) - shift, col0 = first + lane * kChunk;
+    if (first >= p.d) return;
     const int64_t token = token_at(p.tokens, p.tokens64, row);
     const bool named = token >= 0 && token < (int64_t)p.vocab;
     const float* table = p.table + node * p.node_ldt;
@@ -34,20 +39,20 @@ __global__ void __launch_bounds__(256) lookup_kernel(const LookupParams p)
     Raw8<float, VEC> raw[NC];
 #pragma unroll
     for (int c = 0; c < NC; ++c)
-        if (!VEC || first + c * TPR + lane < chunks) raw[c].load_cached(from, (int)(first + c * TPR + lane) * kChunk, p.d, span);
-    RowStore<T, VEC, TPR> store;
-    T* out = static_cast<T*>(p.out) + row * p.ldo;
+        if (!VEC || col0 + c * TPR * kChunk < p.d) raw[c].load_cached(from, col0 + c * TPR * kChunk, p.d, span);
+    f32x2_t v[NC][4];
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        const uint32_t base = first + c * TPR;
-        if (base >= chunks) break;
-        f32x2_t v[4];
-        if (!VEC || base + lane < chunks) {
-            raw[c].get(v);
+        raw[c].get(v[c]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = named ? mul2(v[j], both(p.scale)) : both(0.f);
-        }
-        store.store(out, (int)(base + lane) * kChunk, p.d, v, lane, group_mask<TPR>(), c + 1 == NC || base + TPR >= chunks);
+        for (int j = 0; j < 4; ++j) v[c][j] = named ? mul2(v[c][j], both(p.scale)) : both(0.f);
+    }
+    if constexpr (VEC) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+            if (col0 + c * TPR * kChunk < p.d) store8<T>(out + col0 + c * TPR * kChunk, v[c]);
+    } else {
+        store_shifted<T, TPR, NC>(out, col0, p.d, shift, v, slots[threadIdx.x / TPR], lane, group_mask<TPR>());
     }
 }
 
@@ -778,7 +783,7 @@ bool aligned(const void* p, int64_t ld, int size) { return (((uintptr_t)p) & 15u
 template <class T, bool VEC, int TPR, int NC>
 cudaError_t lookup_as(LookupParams& p, cudaStream_t s)
 {
-    p.stretches = make_divisor((p.chunks.d + NC * TPR - 1) / (NC * TPR));
+    p.stretches = make_divisor((uint32_t)(p.d + (VEC ? 0 : (int)kShiftRows<T> - 1) + NC * TPR * kChunk - 1) / (NC * TPR * kChunk));
     const uint64_t groups = (uint64_t)p.rows * p.stretches.d;
     lookup_kernel<T, VEC, TPR, NC><<<dim3((unsigned)((groups + 256 / TPR - 1) / (256 / TPR)), p.nodes), 256, 0, s>>>(p);
     return cudaGetLastError();
@@ -787,18 +792,17 @@ cudaError_t lookup_as(LookupParams& p, cudaStream_t s)
 template <class T, bool VEC>
 cudaError_t lookup_by_width(LookupParams& p, cudaStream_t s)
 {
-    const uint32_t chunks = p.chunks.d;
-    return chunks <= 8    ? lookup_as<T, VEC, 8, 1>(p, s)
-           : chunks <= 32 ? lookup_as<T, VEC, 32, 1>(p, s)
-           : chunks <= 64 ? lookup_as<T, VEC, 32, 2>(p, s)
-                          : lookup_as<T, VEC, 32, 4>(p, s);
+    const int d = p.d + (VEC ? 0 : (int)kShiftRows<T> - 1);
+    return d <= 64    ? lookup_as<T, VEC, 8, 1>(p, s)
+           : d <= 256 ? lookup_as<T, VEC, 32, 1>(p, s)
+           : d <= 512 ? lookup_as<T, VEC, 32, 2>(p, s)
+                      : lookup_as<T, VEC, 32, 4>(p, s);
 }
 
 template <class T>
 cudaError_t lookup_of(LookupParams p, cudaStream_t s)
 {
     if (!p.rows) return cudaSuccess;
-    p.chunks = make_divisor((uint32_t)(p.d + kChunk - 1) / kChunk);
     const bool vec = p.d % kChunk == 0 && aligned(p.table, p.ldt, 4) && p.node_ldt % 4 == 0 && aligned(p.out, p.ldo, sizeof(T));
     return vec ? lookup_by_width<T, true>(p, s) : lookup_by_width<T, false>(p, s);
 }

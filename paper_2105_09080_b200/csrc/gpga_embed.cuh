@@ -14,7 +14,7 @@ struct LookupParams {
     int32_t d;
     bool tokens64;
     float scale;
-    Divisor chunks, stretches;   // set by the launch
+    Divisor stretches;       // of a row, set by the launch
 };
 
 struct LookupGradParams {

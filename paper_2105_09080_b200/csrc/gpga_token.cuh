@@ -159,7 +159,7 @@ template <class T, bool VEC> struct Raw8 {
                 float v[8];
                 f32x2_t v2[4];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = j < n ? to_f32(row[col + j]) : 0.f;
+                for (int j = 0; j < 8; ++j) v[j] = j < n && col + j >= 0 ? to_f32(row[col + j]) : 0.f;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v2[j] = pack2(v[2 * j], v[2 * j + 1]);
                 pack8<T>(v2, w);
