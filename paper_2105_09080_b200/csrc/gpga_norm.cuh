@@ -1,4 +1,4 @@
-// Dropout and layer norm: launch parameters (kernels in gpga_norm.cu).
+// Dropout and layer norm: launch parameters (kernels in gpga_dropout.cu, gpga_norm.cu and gpga_norm_grad.cu).
 #pragma once
 #include "gpga_token.cuh"
 

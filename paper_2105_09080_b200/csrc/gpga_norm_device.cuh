@@ -1,0 +1,91 @@
+// What the dropout and layer norm kernels share: how a row is spread over threads, sums over them, dispatch by type.
+#pragma once
+#include "../../include/gpga.h"
+#include "gpga_launch.cuh"
+#include "gpga_norm.cuh"
+
+namespace gpga {
+
+constexpr int kSMs = 148;
+
+// Chunk c of a thread.  A group of at most 32 threads takes neighbouring chunks call by call; in wider groups every
+// warp has NC * 32 neighbouring chunks, so that only its two ends meet other warps' columns.
+template <int TPR, int NC>
+__device__ __forceinline__ uint32_t chunk_of(int c)
+{
+    if (TPR <= 32) return threadIdx.x % TPR + c * TPR;
+    return (threadIdx.x % TPR / 32 * NC + c) * 32 + threadIdx.x % 32;
+}
+// First chunk of the lanes that share a store with this thread, for its chunk c.
+template <int TPR, int NC>
+__device__ __forceinline__ uint32_t first_chunk_of(int c)
+{
+    return TPR <= 32 ? c * TPR : (threadIdx.x % TPR / 32 * NC + c) * 32;
+}
+// Threads of a block for groups of TPR: several groups of up to 64, one wider one.
+__host__ __device__ constexpr int block_of(int tpr) { return tpr <= 64 ? 128 : tpr; }
+__host__ __device__ constexpr int lanes_of(int tpr) { return tpr < 32 ? tpr : 32; }
+
+
+// Sums of M values over the TPR threads of a group; every thread gets them all.  In a warp, M values take M - 1
+// shuffles to halve down to one per lane (a lane gives away the half it does not keep), the remaining steps on that
+// one, and M to hand the sums round: 17 for M = 8 instead of 40.  Wider groups go on through shared memory: one
+// barrier; `part` ([warps][M], on 16 bytes) may be used again by the next call but one.
+template <int TPR, int M>
+__device__ __forceinline__ void group_sums(float* v, float* part)
+{
+    constexpr int L = lanes_of(TPR);
+    const unsigned mask = group_mask<TPR>();
+    const int lane = threadIdx.x % L;
+    int o = L / 2;
+#pragma unroll
+    for (int m = M / 2; m >= 1; m /= 2, o /= 2) {
+        const bool upper = lane & o;
+#pragma unroll
+        for (int i = 0; i < m; ++i) {
+            const float give = upper ? v[i] : v[i + m], keep = upper ? v[i + m] : v[i];
+            v[i] = keep + __shfl_xor_sync(mask, give, o);
+        }
+    }
+#pragma unroll
+    for (; o >= 1; o /= 2) v[0] += __shfl_xor_sync(mask, v[0], o);
+    // lane l now has value l / (L / M)
+    if constexpr (TPR > 32) {
+        const int warp = threadIdx.x / 32;
+        if (lane % (L / M) == 0) part[warp * M + lane / (L / M)] = v[0];
+        __syncthreads();
+        const int w0 = threadIdx.x / TPR * (TPR / 32);
+        if constexpr (M >= 4) {
+            f32x2_t sum[M / 2];
+#pragma unroll
+            for (int w = 0; w < TPR / 32; ++w)
+#pragma unroll
+                for (int i = 0; i < M / 4; ++i) {
+                    const float4 q = reinterpret_cast<const float4*>(part)[(w0 + w) * (M / 4) + i];
+                    sum[2 * i] = w ? add2(sum[2 * i], pack2(q.x, q.y)) : pack2(q.x, q.y);
+                    sum[2 * i + 1] = w ? add2(sum[2 * i + 1], pack2(q.z, q.w)) : pack2(q.z, q.w);
+                }
+#pragma unroll
+            for (int i = 0; i < M; ++i) v[i] = element(sum, i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < M; ++i) v[i] = 0.f;
+#pragma unroll
+            for (int w = 0; w < TPR / 32; ++w)
+#pragma unroll
+                for (int i = 0; i < M; ++i) v[i] += part[(w0 + w) * M + i];
+        }
+    } else if constexpr (M > 1) {
+        const float mine = v[0];
+#pragma unroll
+        for (int i = 0; i < M; ++i) v[i] = __shfl_sync(mask, mine, i * (L / M), L);
+    }
+}
+
+}  // namespace gpga
+
+// call(type, vec) for the activation type `dtype` and the runtime `vec`.
+#define GPGA_BY_TYPE(call)                                                              \
+    (dtype == GPGA_DTYPE_F32    ? (vec ? call(float, true) : call(float, false))        \
+     : dtype == GPGA_DTYPE_BF16 ? (vec ? call(__nv_bfloat16, true) : call(__nv_bfloat16, false)) \
+                                : (vec ? call(__half, true) : call(__half, false)))
