@@ -27,15 +27,11 @@ __host__ __device__ constexpr int block_of(int tpr) { return tpr <= 64 ? 128 : t
 __host__ __device__ constexpr int lanes_of(int tpr) { return tpr < 32 ? tpr : 32; }
 
 
-// Sums of M values over the TPR threads of a group; every thread gets them all.  In a warp, M values take M - 1
-// shuffles to halve down to one per lane (a lane gives away the half it does not keep), the remaining steps on that
-// one, and M to hand the sums round: 17 for M = 8 instead of 40.  Wider groups go on through shared memory: one
-// barrier; `part` ([warps][M], on 16 bytes) may be used again by the next call but one.
-template <int TPR, int M>
-__device__ __forceinline__ void group_sums(float* v, float* part)
+// Sums of M values over L lanes; lane l is left with value l / (L / M).  M values take M - 1 shuffles to halve down to one
+// per lane (a lane gives away the half it does not keep), the remaining steps on that one.
+template <int L, int M>
+__device__ __forceinline__ float lane_sums(float* v, unsigned mask)
 {
-    constexpr int L = lanes_of(TPR);
-    const unsigned mask = group_mask<TPR>();
     const int lane = threadIdx.x % L;
     int o = L / 2;
 #pragma unroll
@@ -49,16 +45,40 @@ __device__ __forceinline__ void group_sums(float* v, float* part)
     }
 #pragma unroll
     for (; o >= 1; o /= 2) v[0] += __shfl_xor_sync(mask, v[0], o);
-    // lane l now has value l / (L / M)
-    if constexpr (TPR > 32) {
-        const int warp = threadIdx.x / 32;
-        if (lane % (L / M) == 0) part[warp * M + lane / (L / M)] = v[0];
+    return v[0];
+}
+// Hands the M sums round: every lane gets them all.
+template <int L, int M>
+__device__ __forceinline__ void share_sums(float mine, float* v, unsigned mask)
+{
+#pragma unroll
+    for (int i = 0; i < M; ++i) v[i] = M > 1 ? __shfl_sync(mask, mine, i * (L / M), L) : mine;
+}
+
+// Sums of M values over the TPR threads of a group; every thread gets them all: 17 shuffles for M = 8 in a warp instead of
+// 40.  Wider groups go on through shared memory: one barrier; `part` ([warps][M], on 16 bytes) may be used again by the
+// next call but one.  Up to seven warps' sums are read by every thread, more are added by the lanes once more (32 warps'
+// pairs: 20 instructions instead of 130).
+template <int TPR, int M>
+__device__ __forceinline__ void group_sums(float* v, float* part)
+{
+    constexpr int L = lanes_of(TPR), W = TPR / 32;
+    const unsigned mask = group_mask<TPR>();
+    const float mine = lane_sums<L, M>(v, mask);
+    if constexpr (TPR <= 32) {
+        share_sums<L, M>(mine, v, mask);
+    } else {
+        const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, w0 = threadIdx.x / TPR * W;
+        if (lane % (L / M) == 0) part[warp * M + lane / (L / M)] = mine;
         __syncthreads();
-        const int w0 = threadIdx.x / TPR * (TPR / 32);
-        if constexpr (M >= 4) {
+        if constexpr (W >= 8) {
+#pragma unroll
+            for (int i = 0; i < M; ++i) v[i] = lane < W ? part[(w0 + lane) * M + i] : 0.f;
+            share_sums<32, M>(lane_sums<32, M>(v, mask), v, mask);
+        } else if constexpr (M >= 4) {
             f32x2_t sum[M / 2];
 #pragma unroll
-            for (int w = 0; w < TPR / 32; ++w)
+            for (int w = 0; w < W; ++w)
 #pragma unroll
                 for (int i = 0; i < M / 4; ++i) {
                     const float4 q = reinterpret_cast<const float4*>(part)[(w0 + w) * (M / 4) + i];
@@ -71,14 +91,10 @@ __device__ __forceinline__ void group_sums(float* v, float* part)
 #pragma unroll
             for (int i = 0; i < M; ++i) v[i] = 0.f;
 #pragma unroll
-            for (int w = 0; w < TPR / 32; ++w)
+            for (int w = 0; w < W; ++w)
 #pragma unroll
                 for (int i = 0; i < M; ++i) v[i] += part[(w0 + w) * M + i];
         }
-    } else if constexpr (M > 1) {
-        const float mine = v[0];
-#pragma unroll
-        for (int i = 0; i < M; ++i) v[i] = __shfl_sync(mask, mine, i * (L / M), L);
     }
 }
 
