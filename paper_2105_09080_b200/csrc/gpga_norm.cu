@@ -15,15 +15,15 @@ __device__ __forceinline__ void scale8(const f32x2_t* v, float mean, float rstd,
 
 __device__ __forceinline__ f32x2_t sum4(const f32x2_t* v) { return add2(add2(v[0], v[1]), add2(v[2], v[3])); }
 
-// Sum of (v - mean)^2 over the columns of a chunk at column `col` that lie in the row; EDGE: some may not.
+// Sum of (v - mean)^2 over the columns of a chunk that lie in the row (a bit each); EDGE: some may not.
 template <bool EDGE>
-__device__ __forceinline__ f32x2_t squares8(const f32x2_t* v, float mean, int col, int d)
+__device__ __forceinline__ f32x2_t squares8(const f32x2_t* v, float mean, uint32_t there)
 {
     const f32x2_t m = both(mean);
     f32x2_t e[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) e[j] = sub2(v[j], m);
-    if (EDGE) keep_columns(e, columns_there(col, d));
+    if (EDGE) keep_columns(e, there);
     f32x2_t s = mul2(e[0], e[0]);
 #pragma unroll
     for (int j = 1; j < 4; ++j) s = fma2(e[j], e[j], s);
@@ -41,9 +41,9 @@ __device__ __forceinline__ float mean_of(float s, float n, float inv_n)
 
 // Statistics of R rows that a group of TPR threads holds in registers (columns and rows that are not there: zero).  The
 // variance is a second pass over the registers, so that nothing cancels.  FULL: every chunk is there; EDGE: chunks may be
-// partial.  Chunk m starts at column 8 m - shift.
-template <bool FULL, bool EDGE, int TPR, int NC, int R>
-__device__ __forceinline__ void row_statistics(const f32x2_t (*v)[NC][4], int d, int shift, float eps, float* part, float* mean, float* rstd)
+// partial.  there(c): the columns of chunk c that lie in the row, a bit each.
+template <bool FULL, bool EDGE, int TPR, int NC, int R, class There>
+__device__ __forceinline__ void row_statistics(const f32x2_t (*v)[NC][4], const There& there, int d, float eps, float* part, float* mean, float* rstd)
 {
     const float n = (float)d, inv_n = 1.f / n;
     float s[R];
@@ -60,10 +60,8 @@ __device__ __forceinline__ void row_statistics(const f32x2_t (*v)[NC][4], int d,
         mean[r] = mean_of(s[r], n, inv_n);
         f32x2_t sum = both(0.f);
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const int col = (int)chunk_of<TPR, NC>(c) * kChunk - shift;
-            if (FULL || col < d) sum = add2(sum, squares8<EDGE>(v[r][c], mean[r], col, d));
-        }
+        for (int c = 0; c < NC; ++c)
+            if (FULL || there(c)) sum = add2(sum, squares8<EDGE>(v[r][c], mean[r], there(c)));
         s[r] = sum2(sum);
     }
     group_sums<TPR, R>(s, part + 32 * R);
@@ -136,7 +134,7 @@ __device__ __forceinline__ void norm_forward(const NormForwardParams& p, float* 
     f32x2_t v[R][NC][4];
     load_mixed<T, FULL, true, TPR, NC, R>(p, node, t, v);
     float mean[R], rstd[R];
-    row_statistics<FULL, false, TPR, NC, R>(v, p.d, 0, p.eps, part, mean, rstd);
+    row_statistics<FULL, false, TPR, NC, R>(v, [&](int c) { return chunk_of<TPR, NC>(c) < chunks; }, p.d, p.eps, part, mean, rstd);
     if (threadIdx.x % TPR == 0)
 #pragma unroll
         for (int r = 0; r < R; ++r)
@@ -204,17 +202,19 @@ __device__ __forceinline__ void staged_params(const float4* params, uint32_t chu
 }
 
 // Rows off the alignment all alike: shifted chunks, which are aligned memory in every array.  A block takes sets of rows
-// that have one shift, and lays out the node's parameters for it once.  Bound: latency of a row's two sums at 16 to 20 warps
-// per SM, then issue slots.  2 x 5001 rows of 1023 f16 19 us (cut chunks 27 us, single elements 39 us), 4 x 8000 rows of 1001
-// bf16 with residual and dropout 85 us (121, 175), fp32 without dropout 94 us (130, 227).
-template <class T, int TPR, int NC, int R>
-__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, (NC < 3 ? 640 : 512) / (TPR < 128 ? 128 : TPR)) norm_forward_shifted_kernel(const NormForwardParams p)
+// that have one shift, and lays out the node's parameters for it once.  The next set is on its way, to shared memory (STAGED)
+// or to registers.  Bound: issue slots (55 %) and latency at 16 to 20 warps per SM.  2 x 5001 rows of 1023 f16 19 us (cut
+// chunks 27 us, single elements 39 us), 4 x 8000 rows of 1001 bf16 with residual and dropout 69 us (121, 175), fp32 without
+// dropout 94 us (130, 227).  The generator call before a warp's first chunk is made for a row per lane at a time (a call
+// for each row, of which one lane's words are used: 85 us instead of 75, at two chunks per lane).
+template <class T, int TPR, int NC, int R, bool STAGED>
+__global__ void __launch_bounds__(block_of(TPR), (STAGED && NC < 4 ? 640 : 512) / block_of(TPR)) norm_forward_shifted_kernel(const NormForwardParams p)
 {
-    constexpr int BLOCK = TPR < 128 ? 128 : TPR, G = BLOCK / TPR, LANES = lanes_of(TPR);
+    constexpr int BLOCK = block_of(TPR), G = BLOCK / TPR, LANES = lanes_of(TPR);
     constexpr uint32_t P = kShiftRows<T>;
     extern __shared__ float4 params[];
     __shared__ __align__(16) float part[2 * 32 * R];
-    __shared__ __align__(16) T slots[BLOCK / LANES][16];
+    __shared__ __align__(128) T slots[BLOCK / LANES][2][16];
     const uint32_t node = blockIdx.y, chunks = (uint32_t)(p.d + kChunk - 1) / kChunk, first_row = blockIdx.x % P;
     const uint32_t rows = p.rows > first_row ? (p.rows - first_row + P - 1) / P : 0;   // first_row + P i
     const int64_t all = (int64_t)p.nodes * p.rows, row0 = (int64_t)node * p.rows + first_row;
@@ -223,48 +223,65 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, (NC < 3 ? 640 : 512) / 
     const Span sx = span_of<T>(p.x, p.ldx, all, p.d), sr = span_of<T>(p.residual, p.ldr, all, p.d);
     const int col0 = (int)chunk_of<TPR, NC>(0) * kChunk - shift;
     auto col = [&](int c) { return col0 + c * LANES * kChunk; };
-    T* own_slots = slots[threadIdx.x / LANES];
+    __shared__ uint4 edges[BLOCK];
+    const Staged<T, true, TPR, NC, R> staged{reinterpret_cast<uint4*>(params + 4 * shifted), p.d, shift, lane};
+    uint4* own_edges = edges + threadIdx.x / LANES * LANES;
+    ShiftedStore<T, LANES, NC> to(col0, p.d, shift, slots[threadIdx.x / LANES][0], lane);
     uint32_t there[NC];
 #pragma unroll
     for (int c = 0; c < NC; ++c) there[c] = columns_there(col(c), p.d);
     stage_params<BLOCK>(p, node, shift, shifted, params);
     const uint32_t step = gridDim.x / P * (G * R);
     uint32_t i0 = blockIdx.x / P * (G * R), i = i0 + (G == 1 ? 0 : threadIdx.x / TPR * R);
-    Raw8<T, true> rx[R][NC], rr[R][NC];
-    auto load = [&](uint32_t from) {   // rows first_row + P from, ...
-        const int64_t at = row0 + (int64_t)from * P;
-        const T* x = static_cast<const T*>(p.x) + at * p.ldx;
+    __shared__ __align__(16) T load_slots[STAGED ? 1 : BLOCK / LANES][16];
+    Raw8<T, true> rx[STAGED ? 1 : R][NC], rr[STAGED ? 1 : R][NC];
+    auto fetch_row = [&](const T* row, const Span& s, int place, int r, Raw8<T, true>* raw) {
+        if constexpr (STAGED) {
+            staged.fetch(row, s, place, r, false);
+        } else {
+            const bool in = inside(row, p.d, s);
 #pragma unroll
-        for (int r = 0; r < R; ++r)
-            if (from + r < rows)
-#pragma unroll
-                for (int c = 0; c < NC; ++c)
-                    if (there[c]) load_shifted(x + r * P * p.ldx, col(c), p.d, sx, rx[r][c], own_slots);
-        if (p.residual) {
-            const T* res = static_cast<const T*>(p.residual) + at * p.ldr;
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-                if (from + r < rows)
-#pragma unroll
-                    for (int c = 0; c < NC; ++c)
-                        if (there[c]) load_shifted(res + r * P * p.ldr, col(c), p.d, sr, rr[r][c], own_slots);
+            for (int c = 0; c < NC; ++c)
+                if (there[c]) load_shifted(row, col(c), in || there[c] == 0xFFu, p.d, raw[c], load_slots[threadIdx.x / LANES]);
         }
     };
-    load(i);
-    for (; i0 < rows; i0 += step, i += step) {
+    auto fetch = [&](uint32_t from, int buf) {   // rows first_row + P from, ...
+        const int64_t at = row0 + (int64_t)from * P;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (from + r < rows) {
+                const int q = STAGED ? 0 : r;
+                fetch_row(static_cast<const T*>(p.x) + (at + r * P) * p.ldx, sx, 2 * buf, r, rx[q]);
+                if (p.residual) fetch_row(static_cast<const T*>(p.residual) + (at + r * P) * p.ldr, sr, 2 * buf + 1, r, rr[q]);
+            }
+        if (STAGED) copies_commit();
+    };
+    fetch(i, 0);
+    for (uint32_t set = 0; i0 < rows; ++set, i0 += step, i += step) {
         const int64_t at = row0 + (int64_t)i * P;   // pointers from here: fewer registers than ones that are carried along
+        const int buf = set & 1;
+        if constexpr (STAGED) {
+            __syncwarp(group_mask<TPR>());   // the other lanes have read what these copies replace
+            fetch(i + step, buf ^ 1);
+            copies_wait<1>();
+            __syncwarp(group_mask<TPR>());   // the other lanes' copies of this set are there
+        }
         f32x2_t v[R][NC][4];
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int c = 0; c < NC; ++c) rx[r][c].get(v[r][c]);
+            for (int c = 0; c < NC; ++c)
+                if constexpr (STAGED) staged.chunk(2 * buf, r, c, v[r][c]);
+                else rx[r][c].get(v[r][c]);
         if (p.mask.on) {
-            // lane r works out the words before the warp's first chunk in row r
-            const uint32_t t_edge = first_row + (i + (lane < R ? lane : 0)) * P;
-            const uint4 edge = drop_words(p.mask, t_edge * chunks + first_chunk_of<TPR, NC>(0) - 1, node);
+            if (set % (LANES / R) == 0) {   // lane l works out the words before the warp's first chunk, in row l % R of set l / R from here
+                __syncwarp(group_mask<TPR>());
+                own_edges[lane] = drop_words(p.mask, (first_row + (i + lane / R * step + lane % R) * P) * chunks + first_chunk_of<TPR, NC>(0) - 1, node);
+                __syncwarp(group_mask<TPR>());
+            }
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                uint4 before = shfl4(group_mask<TPR>(), edge, r, LANES);
+                uint4 before = own_edges[set % (LANES / R) * R + r];
                 const uint32_t groups = (first_row + (i + r) * P) * chunks;
 #pragma unroll
                 for (int c = 0; c < NC; ++c) {
@@ -283,7 +300,8 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, (NC < 3 ? 640 : 512) / 
 #pragma unroll
                 for (int c = 0; c < NC; ++c) {
                     f32x2_t e[4];
-                    rr[r][c].get(e);
+                    if constexpr (STAGED) staged.chunk(2 * buf + 1, r, c, e);
+                    else rr[r][c].get(e);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) v[r][c][j] = add2(v[r][c][j], e[j]);
                 }
@@ -291,9 +309,9 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, (NC < 3 ? 640 : 512) / 
         for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int c = 0; c < NC; ++c) keep_columns(v[r][c], i + r < rows ? there[c] : 0u);   // the rest was never loaded, or lies beside the row
-        load(i + step);   // on their way during the sums
         float mean[R], rstd[R];
-        row_statistics<false, true, TPR, NC, R>(v, p.d, shift, p.eps, part, mean, rstd);
+        if constexpr (!STAGED) fetch(i + step, 0);   // on their way during the sums
+        row_statistics<false, true, TPR, NC, R>(v, [&](int c) { return there[c]; }, p.d, p.eps, part, mean, rstd);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             if (i + r >= rows) continue;
@@ -301,7 +319,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, (NC < 3 ? 640 : 512) / 
                 p.mean[at + r * P] = mean[r];
                 p.rstd[at + r * P] = rstd[r];
             }
-            if (p.z) store_shifted<T, LANES, NC>(static_cast<T*>(p.z) + (at + r * P) * p.ldz, col0, p.d, shift, v[r], own_slots, lane, group_mask<TPR>());
+            if (p.z) to.store(static_cast<T*>(p.z) + (at + r * P) * p.ldz, col0, v[r], lane, group_mask<TPR>());
 #pragma unroll
             for (int c = 0; c < NC; ++c)
                 if (there[c]) {
@@ -309,7 +327,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, (NC < 3 ? 640 : 512) / 
                     staged_params(params, shifted, chunk_of<TPR, NC>(c), w, b);
                     scale8(v[r][c], mean[r], rstd[r], w, b, v[r][c]);
                 }
-            store_shifted<T, LANES, NC>(static_cast<T*>(p.y) + (at + r * P) * p.ldy, col0, p.d, shift, v[r], own_slots, lane, group_mask<TPR>());
+            to.store(static_cast<T*>(p.y) + (at + r * P) * p.ldy, col0, v[r], lane, group_mask<TPR>());
         }
     }
 }
@@ -333,7 +351,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, 512 / (TPR < 128 ? 128 
         f32x2_t v[R][NC][4];
         load_mixed<T, false, VEC, TPR, NC, R>(p, node, t, v);
         float mean[R], rstd[R];
-        row_statistics<false, !VEC, TPR, NC, R>(v, p.d, 0, p.eps, part, mean, rstd);
+        row_statistics<false, !VEC, TPR, NC, R>(v, [&](int c) { return columns_there((int)chunk_of<TPR, NC>(c) * kChunk, p.d); }, p.d, p.eps, part, mean, rstd);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             if (t + r >= p.rows) continue;
@@ -398,7 +416,7 @@ __global__ void __launch_bounds__(1024) norm_forward_wide_kernel(const NormForwa
     float sq[1] = {0.f};
     for (uint32_t chunk = threadIdx.x; chunk < chunks; chunk += 1024) {
         chunk_at(chunk, v);
-        sq[0] += sum2(squares8<!VEC>(v, mean, (int)chunk * kChunk, p.d));
+        sq[0] += sum2(squares8<!VEC>(v, mean, columns_there((int)chunk * kChunk, p.d)));
     }
     group_sums<1024, 1>(sq, part[1]);
     const float rstd = rsqrtf(sq[0] / (float)p.d + p.eps);   // within 2 ulp
@@ -432,15 +450,12 @@ constexpr int kForwardWide = 16384, kForwardOddWide = 8192;   // widest rows tha
 
 // Blocks of a kernel that an SM holds, from its registers (looked up once) and shared memory.
 template <class Kernel>
-int blocks_per_sm(Kernel kernel, int block, size_t smem, int& regs)
+int blocks_per_sm(Kernel kernel, int block, size_t smem, cudaFuncAttributes& at)
 {
-    if (!regs) {
-        cudaFuncAttributes at;
-        regs = cudaFuncGetAttributes(&at, kernel) == cudaSuccess && at.numRegs > 0 ? at.numRegs : 128;
-    }
-    int n = 65536 / ((regs + 7) / 8 * 8 * block);
+    if (!at.numRegs && (cudaFuncGetAttributes(&at, kernel) != cudaSuccess || !at.numRegs)) at.numRegs = 128;
+    int n = 65536 / ((at.numRegs + 7) / 8 * 8 * block);
     if (n > 2048 / block) n = 2048 / block;
-    const int by_smem = (int)(227 * 1024 / (smem + 2048));
+    const int by_smem = (int)(227 * 1024 / (smem + at.sharedSizeBytes + 1024));
     if (n > by_smem) n = by_smem;
     return n < 1 ? 1 : n;
 }
@@ -456,29 +471,28 @@ cudaError_t forward_odd(const NormForwardParams& p, cudaStream_t s)
         const cudaError_t e = ensure_smem_limit(kernel, kForwardOddWide * 8, limit_set);
         if (e != cudaSuccess) return e;
     }
-    static int regs = 0;
+    static cudaFuncAttributes use = {};
     const uint32_t sets = (p.rows + SET - 1) / SET;
-    const uint32_t room = (uint32_t)(kSMs * blocks_per_sm(kernel, BLOCK, smem, regs)) / p.nodes;
+    const uint32_t room = (uint32_t)(kSMs * blocks_per_sm(kernel, BLOCK, smem, use)) / p.nodes;
     kernel<<<dim3(sets < room ? sets : room ? room : 1, p.nodes), BLOCK, smem, s>>>(p);
     return cudaGetLastError();
 }
 
-template <class T, int TPR, int NC, int R>
+template <class T, int TPR, int NC, int R, bool STAGED>
 cudaError_t forward_shifted(const NormForwardParams& p, cudaStream_t s)
 {
-    constexpr int BLOCK = TPR < 128 ? 128 : TPR, SET = BLOCK / TPR * R;
+    constexpr int BLOCK = block_of(TPR), SET = BLOCK / TPR * R;
     constexpr uint32_t P = kShiftRows<T>;
-    const size_t smem = (size_t)((p.d + P + kChunk - 1) / kChunk) * 64;
-    const auto kernel = norm_forward_shifted_kernel<T, TPR, NC, R>;
-    if (smem > 47 * 1024) {
-        static unsigned long long limit_set = 0;
-        const cudaError_t e = ensure_smem_limit(kernel, (kForwardOddWide + 16) * 8, limit_set);
-        if (e != cudaSuccess) return e;
-    }
-    static int regs = 0;
+    constexpr int kStage = !STAGED ? 0 : 4 * R * NC * BLOCK * kChunk * (int)sizeof(T);
+    const size_t smem = (size_t)((p.d + P + kChunk - 1) / kChunk) * 64 + kStage;
+    const auto kernel = norm_forward_shifted_kernel<T, TPR, NC, R, STAGED>;
+    static unsigned long long limit_set = 0;
+    const cudaError_t e = ensure_smem_limit(kernel, (TPR * NC + 2) * kChunk * 8 + kStage, limit_set);
+    if (e != cudaSuccess) return e;
+    static cudaFuncAttributes use = {};
     // as many blocks as fit, in whole classes of rows
     const uint32_t sets = ((p.rows + P - 1) / P + SET - 1) / SET;
-    const uint32_t room = (uint32_t)(kSMs * blocks_per_sm(kernel, BLOCK, smem, regs)) / (p.nodes * P);
+    const uint32_t room = (uint32_t)(kSMs * blocks_per_sm(kernel, BLOCK, smem, use)) / (p.nodes * P);
     kernel<<<dim3(P * (sets < room ? sets : room ? room : 1), p.nodes), BLOCK, smem, s>>>(p);
     return cudaGetLastError();
 }
@@ -508,16 +522,24 @@ cudaError_t forward_of(const NormForwardParams& p, cudaStream_t s)
         }
     if constexpr (!VEC)
         if (p.shifted) {
+            // Chunks per thread, threads per row, and whether rows are staged: narrow rows gain from few lanes (4 x 30000 rows of 203
+            // bf16 64 us, a chunk for each of 32 lanes 82 us), wide ones lose warps to the shared memory of two sets (4 x 1500
+            // rows of 5001 fp32 staged 155 us, in registers 122 us; 4 x 8000 of 1001 bf16 staged 69 us, in registers 77 us).
+            constexpr bool W = sizeof(T) == 4;
             const int d = p.d + (int)kShiftRows<T> - 1;
-            if (d <= 64) return forward_shifted<T, 8, 1, 2>(p, s);
-            if (d <= 128) return forward_shifted<T, 16, 1, 2>(p, s);
-            if (d <= 256) return forward_shifted<T, 32, 1, 2>(p, s);
-            if (d <= 512) return forward_shifted<T, 32, 2, 1>(p, s);
-            if (d <= 1024) return forward_shifted<T, 64, 2, 1>(p, s);
-            if (d <= 1536) return forward_shifted<T, 64, 3, 1>(p, s);
-            if (d <= 2048) return forward_shifted<T, 128, 2, 1>(p, s);
-            if (d <= 4096) return forward_shifted<T, 256, 2, 1>(p, s);
-            if (d <= kForwardOddWide) return forward_shifted<T, 512, 2, 1>(p, s);
+            if (d <= 64) return forward_shifted<T, 8, 1, 2, true>(p, s);
+            if (d <= 128) return forward_shifted<T, 8, 2, 1, true>(p, s);
+            if (d <= 256) return forward_shifted<T, W ? 16 : 8, W ? 2 : 4, 1, true>(p, s);
+            if (d <= 512) return forward_shifted<T, W ? 32 : 16, W ? 2 : 4, 1, true>(p, s);
+            if (d <= 768) return forward_shifted<T, 32, 3, 1, false>(p, s);
+            if (d <= 1024) return forward_shifted<T, W ? 64 : 32, W ? 2 : 4, 1, !W>(p, s);
+            if (!W && d <= 1280) return forward_shifted<T, W ? 96 : 32, W ? 2 : 5, 1, !W>(p, s);
+            if (d <= 1536) return forward_shifted<T, W ? 96 : 64, W ? 2 : 3, 1, false>(p, s);
+            if (d <= 2048) return forward_shifted<T, W ? 128 : 64, W ? 2 : 4, 1, !W>(p, s);
+            if (d <= 2560) return forward_shifted<T, W ? 160 : 128, W ? 2 : 3, 1, false>(p, s);
+            if (d <= 4096) return forward_shifted<T, 256, 2, 1, false>(p, s);
+            if (d <= 6144) return forward_shifted<T, 256, 3, 1, false>(p, s);
+            if (d <= kForwardOddWide) return forward_shifted<T, W ? 512 : 256, W ? 2 : 4, 1, false>(p, s);
         }
     if (p.d <= 64) return forward_odd<T, VEC, 8, 1, 2>(p, s);
     if (p.d <= 256) return forward_odd<T, VEC, 32, 1, 2>(p, s);

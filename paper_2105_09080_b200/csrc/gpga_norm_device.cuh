@@ -3,6 +3,7 @@
 #include "../../include/gpga.h"
 #include "gpga_launch.cuh"
 #include "gpga_norm.cuh"
+#include "gpga_tma.cuh"
 
 namespace gpga {
 
@@ -26,6 +27,59 @@ __device__ __forceinline__ uint32_t first_chunk_of(int c)
 __host__ __device__ constexpr int block_of(int tpr) { return tpr <= 64 ? 128 : tpr; }
 __host__ __device__ constexpr int lanes_of(int tpr) { return tpr < 32 ? tpr : 32; }
 
+// 16 bytes from memory to shared memory without a register; a thread waits for its own copies.
+__device__ __forceinline__ void copy16_async(uint32_t to, const void* from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Chunks of R rows on their way to a warp through its own places in shared memory, so that loads in flight take no registers;
+// place: [tensor][r][c][warp][piece].  In fp32 a chunk is two 16-byte pieces (Q); lanes copy neighbouring pieces, so that
+// whole sectors come at once, and the pieces lie exchanged in every other group of eight, so that a warp reads its chunks
+// without bank conflicts.  A group's lanes synchronise between copies that have landed and reads, where Q > 1 or rows are shifted.
+template <class T, bool SHIFT, int TPR, int NC, int R> struct Staged {
+    static constexpr int BLOCK = block_of(TPR), LANES = lanes_of(TPR), Q = sizeof(T) / 2, E = 16 / sizeof(T);   // E: columns of a piece
+    uint4* stage;
+    int d, shift, lane;
+    __device__ __forceinline__ uint4* place(int tensor, int r, int c, int piece) const
+    {
+        const int at = Q == 1 ? piece : piece ^ (piece >> 3 & 1);
+        return stage + ((tensor * R + r) * NC + c) * BLOCK * Q + (threadIdx.x - lane) * Q + at;
+    }
+    // full: every chunk is there
+    __device__ __forceinline__ void fetch(const T* row, const Span& s, int tensor, int r, bool full) const
+    {
+        const bool in = !SHIFT || inside(row, d, s);
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                const int piece = q * LANES + lane, at = (int)first_chunk_of<TPR, NC>(c) * kChunk - shift + piece * E;
+                if (!full && at >= d) continue;
+                const T* from = row + at;
+                uint4* to = place(tensor, r, c, piece);
+                if (in || (at >= 0 && at + E <= d)) {
+                    copy16_async(smem_u32(to), from);
+                } else {   // the array's first and last rows
+#pragma unroll 1
+                    for (int e = 0; e < E; ++e) reinterpret_cast<T*>(to)[e] = at + e >= 0 && at + e < d ? from[e] : from_f32<T>(0.f);
+                }
+            }
+    }
+    __device__ __forceinline__ void chunk(int tensor, int r, int c, f32x2_t* v) const
+    {
+        Raw8<T, true> raw;
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            const uint4 x = *place(tensor, r, c, Q * lane + q);
+            raw.w[4 * q] = x.x; raw.w[4 * q + 1] = x.y; raw.w[4 * q + 2] = x.z; raw.w[4 * q + 3] = x.w;
+        }
+        raw.get(v);
+    }
+};
 
 // Sums of M values over L lanes; lane l is left with value l / (L / M).  M values take M - 1 shuffles to halve down to one
 // per lane (a lane gives away the half it does not keep), the remaining steps on that one.

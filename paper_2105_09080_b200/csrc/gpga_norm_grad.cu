@@ -1,6 +1,5 @@
 // Gradient of the layer norm of residual + dropout(x): of z and x row by row, of the weight and the bias over the rows.
 #include "gpga_norm_device.cuh"
-#include "gpga_tma.cuh"
 
 namespace gpga {
 
@@ -17,15 +16,6 @@ __device__ __forceinline__ void grad8(const f32x2_t* z, const f32x2_t* dy, const
 
 struct Yes { static constexpr bool value = true; };
 struct No { static constexpr bool value = false; };
-
-// 16 bytes from memory to shared memory without a register; a thread waits for its own copies.
-__device__ __forceinline__ void copy16_async(uint32_t to, const void* from)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
-}
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // The block's column sums: its groups of threads one after the other, then out, to the node's gradients or to the block's
 // row of partial sums.  `sums` (2 * TPR * NC * 8 floats) is used where the block has several groups.  col0(c): first
@@ -90,13 +80,11 @@ __device__ __forceinline__ void write_column_sums(const NormBackwardParams& p, u
 template <class T, bool SHIFT, int TPR, int NC, int R, int kSets, int kPerSM>
 __global__ void __launch_bounds__(block_of(TPR), kPerSM) norm_backward_kernel(const NormBackwardParams p)
 {
-    constexpr int BLOCK = block_of(TPR), G = BLOCK / TPR, LANES = lanes_of(TPR), Q = sizeof(T) / 2;   // Q: 16-byte pieces of a chunk
+    constexpr int BLOCK = block_of(TPR), G = BLOCK / TPR, LANES = lanes_of(TPR), Q = sizeof(T) / 2;
     constexpr uint32_t P = SHIFT ? kShiftRows<T> : 1;
-    constexpr int E = 16 / sizeof(T);   // columns of a piece
     extern __shared__ uint4 stage[];   // two sets of [tensor][r][c][warp][piece]
     __shared__ __align__(16) float part[2][BLOCK / 32 * 2 * R];
-    __shared__ __align__(16) T slots[SHIFT ? BLOCK / LANES : 1][16];
-    T* own_slots = slots[SHIFT ? threadIdx.x / LANES : 0];
+    __shared__ __align__(128) T slots[SHIFT ? BLOCK / LANES : 1][2][16];
     const int sub = G == 1 ? 0 : threadIdx.x / TPR, tensors = p.dz ? 3 : 2;
     const uint32_t node = blockIdx.y, chunks = (uint32_t)(p.d + kChunk - 1) / kChunk;
     const uint32_t first_row = SHIFT ? blockIdx.x % P : 0;   // the block's rows: first_row + P i
@@ -107,11 +95,7 @@ __global__ void __launch_bounds__(block_of(TPR), kPerSM) norm_backward_kernel(co
     auto col = [&](int c) { return (int)chunk_of<TPR, NC>(c) * kChunk - shift; };
     auto mine = [&](int c) { return col(c) < p.d; };
     const int lane = threadIdx.x % LANES;
-    auto place = [&](int buf, int tensor, int r, int c, int piece) {
-        const int at = Q == 1 ? piece : piece ^ (piece >> 3 & 1);
-        return stage + ((((buf * 3 + tensor) * R + r) * NC + c) * BLOCK + (threadIdx.x - lane)) * Q + at;
-    };
-
+    const Staged<T, SHIFT, TPR, NC, R> staged{stage, p.d, shift, lane};
     uint32_t there[NC];
     f32x2_t w[NC][4], dw[NC][4], db[NC][4];
 #pragma unroll
@@ -143,50 +127,24 @@ __global__ void __launch_bounds__(block_of(TPR), kPerSM) norm_backward_kernel(co
     const int64_t row_z = p.ldz * P, row_y = p.lddy * P, row_e = p.lddz * P, row_g = p.lddres * P, row_x = p.lddx * P;
     const bool all_columns = p.d == TPR * NC * kChunk;   // with no shift: every thread has all its chunks
 
-    auto fetch_one = [&](const T* row, const Span& s, int tensor, int buf, int r, bool full) {
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int q = 0; q < Q; ++q) {
-                const int piece = q * LANES + lane, at = (int)first_chunk_of<TPR, NC>(c) * kChunk - shift + piece * E;
-                if (!full && at >= p.d) continue;
-                const T* from = row + at;
-                uint4* to = place(buf, tensor, r, c, piece);
-                if (!SHIFT || (at >= 0 && at + E <= p.d) || (reinterpret_cast<const char*>(from) >= s.lo && reinterpret_cast<const char*>(from + E) <= s.hi)) {
-                    copy16_async(smem_u32(to), from);
-                } else {   // the array's first or last row
-#pragma unroll 1
-                    for (int e = 0; e < E; ++e) reinterpret_cast<T*>(to)[e] = at + e >= 0 && at + e < p.d ? from[e] : from_f32<T>(0.f);
-                }
-            }
-    };
     // the set whose first row is `set` rows behind the current pointers; n: rows that it has
     auto fetch_rows = [&](uint32_t set, int buf, uint32_t n, bool full) {
 #pragma unroll
         for (int r = 0; r < R; ++r)
             if (full || (uint32_t)r < n) {
-                fetch_one(z + (int64_t)(set + r) * row_z, sz, 0, buf, r, full);
-                fetch_one(dy + (int64_t)(set + r) * row_y, sy, 1, buf, r, full);
+                staged.fetch(z + (int64_t)(set + r) * row_z, sz, buf * 3 + 0, r, full);
+                staged.fetch(dy + (int64_t)(set + r) * row_y, sy, buf * 3 + 1, r, full);
             }
         if (tensors == 3)
 #pragma unroll
             for (int r = 0; r < R; ++r)
-                if (full || (uint32_t)r < n) fetch_one(dz + (int64_t)(set + r) * row_e, se, 2, buf, r, full);
+                if (full || (uint32_t)r < n) staged.fetch(dz + (int64_t)(set + r) * row_e, se, buf * 3 + 2, r, full);
     };
     auto fetch = [&](uint32_t set, int buf) {
         const uint32_t from = i + set, n = from < rows ? min((uint32_t)R, rows - from) : 0;
         if (!SHIFT && all_columns && i0 + set + G * R <= rows) fetch_rows(set, buf, R, true);
         else fetch_rows(set, buf, n, false);
         copies_commit();
-    };
-    auto chunk_in = [&](int buf, int tensor, int r, int c, f32x2_t* v) {
-        Raw8<T, true> raw;
-#pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            const uint4 x = *place(buf, tensor, r, c, Q * lane + q);
-            raw.w[4 * q] = x.x; raw.w[4 * q + 1] = x.y; raw.w[4 * q + 2] = x.z; raw.w[4 * q + 3] = x.w;
-        }
-        raw.get(v);
     };
     const float inv_d = 1.f / (float)p.d;
     float mean_next[R], rstd_next[R];   // of the next set
@@ -200,6 +158,10 @@ __global__ void __launch_bounds__(block_of(TPR), kPerSM) norm_backward_kernel(co
             }
         }
     };
+    ShiftedStore<T, LANES, NC> to(col(0), p.d, shift, slots[SHIFT ? threadIdx.x / LANES : 0][0], lane);
+    uint32_t set = 0;
+    __shared__ uint4 edges[SHIFT ? BLOCK : 1];
+    uint4* own_edges = edges + (SHIFT ? threadIdx.x - lane : 0);
     // one set; full: all its rows and chunks are there
     auto work = [&](int buf, int odd, const float* mean, const float* rstd, auto full_) {
         constexpr bool FULL = decltype(full_)::value;
@@ -213,8 +175,8 @@ __global__ void __launch_bounds__(block_of(TPR), kPerSM) norm_backward_kernel(co
                 for (int c = 0; c < NC; ++c) {
                     if (!FULL && !mine(c)) continue;
                     f32x2_t vz[4], vy[4];
-                    chunk_in(buf, 0, r, c, vz);
-                    chunk_in(buf, 1, r, c, vy);
+                    staged.chunk(buf * 3 + 0, r, c, vz);
+                    staged.chunk(buf * 3 + 1, r, c, vy);
                     if (SHIFT) {   // what lies beside the row; the second pass does not store it
                         keep_columns(vz, there[c]);
                         keep_columns(vy, there[c]);
@@ -235,10 +197,10 @@ __global__ void __launch_bounds__(block_of(TPR), kPerSM) norm_backward_kernel(co
         }
         group_sums<TPR, 2 * R>(s, part[odd]);
         asm volatile("" ::: "memory");   // the chunks are read again, not kept
-        uint4 edge = make_uint4(0, 0, 0, 0);   // SHIFT: lane r has the words before the warp's first chunk in row r
-        if (SHIFT && p.dx && p.mask.on) {
-            const uint32_t t = first_row + (i + (lane < R ? lane : 0)) * P;
-            edge = drop_words(p.mask, t * chunks + first_chunk_of<TPR, NC>(0) - 1, node);
+        if (SHIFT && p.dx && p.mask.on && set % (LANES / R) == 0) {   // lane l works out the words before the warp's first chunk, in row l % R of set l / R from here
+            __syncwarp(group_mask<TPR>());
+            own_edges[lane] = drop_words(p.mask, (first_row + (i + lane / R * step + lane % R) * P) * chunks + first_chunk_of<TPR, NC>(0) - 1, node);
+            __syncwarp(group_mask<TPR>());
         }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -248,8 +210,8 @@ __global__ void __launch_bounds__(block_of(TPR), kPerSM) norm_backward_kernel(co
             for (int c = 0; c < NC; ++c) {
                 if (!FULL && !mine(c)) continue;
                 f32x2_t vz[4], vy[4];
-                chunk_in(buf, 0, r, c, vz);
-                chunk_in(buf, 1, r, c, vy);
+                staged.chunk(buf * 3 + 0, r, c, vz);
+                staged.chunk(buf * 3 + 1, r, c, vy);
                 grad8(vz, vy, w[c], mean[r], rstd[r], s[2 * r] * inv_d, s[2 * r + 1] * inv_d, g[c]);
             }
             if (tensors == 3)
@@ -257,17 +219,18 @@ __global__ void __launch_bounds__(block_of(TPR), kPerSM) norm_backward_kernel(co
                 for (int c = 0; c < NC; ++c) {
                     if (!FULL && !mine(c)) continue;
                     f32x2_t e[4];
-                    chunk_in(buf, 2, r, c, e);
+                    staged.chunk(buf * 3 + 2, r, c, e);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) g[c][j] = add2(g[c][j], e[j]);
                 }
 #pragma unroll
             for (int c = 0; c < NC; ++c)
                 if (!SHIFT && (FULL || mine(c))) store8<T>(dres + r * row_g + col(c), g[c]);
-            if (SHIFT) store_shifted<T, LANES, NC>(dres + r * row_g, col(0), p.d, shift, g, own_slots, lane, group_mask<TPR>());
+            if (SHIFT) to.store(dres + r * row_g, col(0), g, lane, group_mask<TPR>());
             if (!p.dx) continue;
             const uint32_t groups = (first_row + (i + r) * P) * chunks;
-            uint4 before = SHIFT ? shfl4(group_mask<TPR>(), edge, r, LANES) : edge;
+            uint4 before = make_uint4(0, 0, 0, 0);
+            if (SHIFT) before = own_edges[set % (LANES / R) * R + r];
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
                 const uint32_t group = groups + chunk_of<TPR, NC>(c);
@@ -285,7 +248,7 @@ __global__ void __launch_bounds__(block_of(TPR), kPerSM) norm_backward_kernel(co
                     store8<T>(dx + r * row_x + col(c), g[c]);
                 }
             }
-            if (SHIFT) store_shifted<T, LANES, NC>(dx + r * row_x, col(0), p.d, shift, g, own_slots, lane, group_mask<TPR>());
+            if (SHIFT) to.store(dx + r * row_x, col(0), g, lane, group_mask<TPR>());
         }
     };
 #pragma unroll
@@ -302,7 +265,7 @@ __global__ void __launch_bounds__(block_of(TPR), kPerSM) norm_backward_kernel(co
         if (Q > 1 || SHIFT) __syncwarp(group_mask<TPR>());   // and their copies of this set are there
         if (!SHIFT && all_columns && i0 + G * R <= rows) work(buf, odd, mean, rstd, Yes());
         else work(buf, odd, mean, rstd, No());
-        i0 += step, i += step;
+        ++set, i0 += step, i += step;
         z += step * row_z, dy += step * row_y, dz += step * row_e, dres += step * row_g, dx += step * row_x;
         means += (int64_t)step * P, rstds += (int64_t)step * P;
     }

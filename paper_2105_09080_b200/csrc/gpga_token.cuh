@@ -57,6 +57,10 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi, __half)
 // that come along are dropped, never written.
 struct Span {   // bytes of a whole array: first byte of its first row, one past the last of its last row
     const char *lo, *hi;
+    __device__ __forceinline__ bool has(const void* p, int bytes) const
+    {
+        return static_cast<const char*>(p) >= lo && static_cast<const char*>(p) + bytes <= hi;
+    }
 };
 template <class T>
 __device__ __forceinline__ Span span_of(const void* p, int64_t ld, int64_t rows, int d)
@@ -350,16 +354,19 @@ __device__ __forceinline__ void keep_columns(f32x2_t* v, uint32_t there)
     }
 }
 
-// Reads the aligned chunk at column `col` (possibly before the row's start or past its end) into the words of a chunk;
-// bytes outside the array's span are not touched and come out zero.  slots: as for store_shifted.
+// Whether the memory that a row's partial chunks reach into on both sides belongs to the array.
 template <class T>
-__device__ __forceinline__ void load_shifted(const T* row, int col, int d, const Span& s, Raw8<T, true>& raw, T* slots)
+__device__ __forceinline__ bool inside(const T* row, int d, const Span& s) { return s.has(row - 7, (d + 14) * (int)sizeof(T)); }
+
+// Reads the aligned chunk at column `col` (possibly before the row's start or past its end) into the words of a chunk.
+// safe: the whole chunk is in the row or in the array; otherwise bytes beside the row are not touched and come out zero.  slots: two chunks of shared memory for the lanes of a row.
+template <class T>
+__device__ __forceinline__ void load_shifted(const T* row, int col, bool safe, int d, Raw8<T, true>& raw, T* slots)
 {
     constexpr int W = 2 * sizeof(T);
-    const char* at = reinterpret_cast<const char*>(row + col);
-    if ((col >= 0 && col + 8 <= d) || (at >= s.lo && at + 4 * W <= s.hi)) {
-        raw.load(row, col, d, s);
-    } else {   // an end of the array's first or last row
+    if (safe) {
+        raw.load(row, col, d, Span());
+    } else {
         T* to = slots + (col < 0 ? 0 : 8);
 #pragma unroll 1
         for (int j = 0; j < 8; ++j) to[j] = col + j >= 0 && col + j < d ? row[col + j] : from_f32<T>(0.f);
@@ -372,37 +379,54 @@ __device__ __forceinline__ void load_shifted(const T* row, int col, int d, const
 }
 
 // Stores the NC chunks (the c-th at column col0 + 8 c LANES, col0 = 8 m - shift for the lane's m) that each of LANES lanes
-// holds of a row.  The partial chunks at the row's ends go through `slots` (two chunks for these lanes), from where a lane
-// stores one element each: element by element from the two lanes that hold them, the ends cost more than all the rest.
-template <class T, int LANES, int NC>
-__device__ __forceinline__ void store_shifted(T* row, int col0, int d, int shift, const f32x2_t (*v)[4], T* slots, int lane, unsigned mask)
-{
+// holds of a row.  The partial chunks at the row's ends go through shared memory, from where a lane stores one element each:
+// element by element from the two lanes that hold them, the ends cost more than all the rest.  What depends on the columns
+// alone is worked out once for all rows.
+template <class T, int LANES, int NC> struct ShiftedStore {
+    T* slots;        // two pairs of chunks for these lanes, used in turn: a row's are read while the next one's are written
+    int at0, at1;    // columns of the ends that this lane stores, -1: none
+    uint32_t whole;  // a bit for every chunk that lies in the row; from bit 8 on, for every one that does in part
+    bool ends;       // the same for all these lanes: whether any chunk is partial
+    __device__ __forceinline__ ShiftedStore(int col0, int d, int shift, T* slots_, int lane) : slots(slots_), at0(-1), at1(-1), whole(0)
+    {
+        const int first = col0 - 8 * lane, last = (d + shift - 1) / 8 * 8 - shift;   // column of their first chunk, of the row's last
+        const bool head = first < 0, tail = last >= 0 && last + 8 > d && last >= first && last < first + 8 * NC * LANES;
+        ends = head || tail;
+        auto end_at = [&](int e) {   // element e of the two chunks
+            const int at = e < 8 ? first + e : last + e - 8;
+            return e < 16 && (e < 8 ? head : tail) && at >= 0 && at < d ? at : -1;
+        };
+        at0 = end_at(lane);
+        if (LANES < 16) at1 = end_at(lane + LANES);
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-        const int col = col0 + 8 * c * LANES;
-        if (col >= 0 && col + 8 <= d) {
-            store8<T>(row + col, v[c]);
-        } else if (col < d) {
-            T* to = slots + (col < 0 ? 0 : 8);
-            uint32_t o[2 * sizeof(T)];
-            pack8<T>(v[c], o);
-#pragma unroll
-            for (int i = 0; i < (int)sizeof(T) / 2; ++i)
-                reinterpret_cast<uint4*>(to)[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+        for (int c = 0; c < NC; ++c) {
+            const int col = col0 + 8 * c * LANES;
+            if (col >= 0 && col + 8 <= d) whole |= 1u << c;
+            else if (col < d) whole |= 256u << c;
         }
     }
-    // the same for all these lanes: whether the row's ends are theirs
-    const int first = col0 - 8 * lane, last = (d + shift - 1) / 8 * 8 - shift;   // column of their first chunk, of the row's last
-    const bool head = first < 0, tail = last >= 0 && last + 8 > d && last >= first && last < first + 8 * NC * LANES;
-    if (!head && !tail) return;
-    __syncwarp(mask);
+    __device__ __forceinline__ void store(T* row, int col0, const f32x2_t (*v)[4], int lane, unsigned mask)
+    {
 #pragma unroll
-    for (int k = 0; k < (LANES < 16 ? 2 : 1); ++k) {
-        const int e = lane + k * LANES, at = e < 8 ? first + e : last + e - 8;
-        if (e < 16 && (e < 8 ? head : tail) && at >= 0 && at < d) row[at] = slots[e];
+        for (int c = 0; c < NC; ++c) {
+            if (whole >> c & 1) {
+                store8<T>(row + col0 + 8 * c * LANES, v[c]);
+            } else if (whole >> c & 256) {
+                T* to = slots + (col0 + 8 * c * LANES < 0 ? 0 : 8);
+                uint32_t o[2 * sizeof(T)];
+                pack8<T>(v[c], o);
+#pragma unroll
+                for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+                    reinterpret_cast<uint4*>(to)[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+            }
+        }
+        if (!ends) return;
+        __syncwarp(mask);
+        if (at0 >= 0) row[at0] = slots[lane];
+        if (LANES < 16 && at1 >= 0) row[at1] = slots[lane + LANES];
+        slots = reinterpret_cast<T*>(reinterpret_cast<uintptr_t>(slots) ^ 16 * sizeof(T));   // [2][16] on a boundary of its size
     }
-    __syncwarp(mask);   // the slots may be written again
-}
+};
 
 // The random words of a shifted chunk: those of generator calls m - 1 (the chunk's first s columns) and m.
 __device__ __forceinline__ void shifted_words(const uint4& before, const uint4& own, int s, uint32_t* word)

@@ -465,6 +465,15 @@ def test_layer_norm_of_views_in_place_and_without_rows():
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,d", [(100000, 51), (100000, 77), (3001, 203), (30000, 333), (9001, 701), (80000, 1003), (5001, 1023), (2000, 1501),
+                                    (9000, 1999), (2003, 2501), (12000, 3999), (700, 5001), (601, 7001)])
+def test_many_dense_rows_of_odd_widths(dtype, rows, d):
+    """Rows that are off the alignment each in its own way, more of them than the blocks take at once."""
+    test_layer_norm_forward(dtype, 1, rows, d, True, 0.25)
+    test_layer_norm_backward(dtype, 1, rows, d, True, 0.25)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("d", [1, 5, 64, 120, 513, 1024, 1030, 2050, 4099, 8185])
 def test_vectors_off_the_alignment_alike(dtype, d):
     """Every activation a slice at one place of a buffer of one width: the results are a dense copy's, and nothing beside
