@@ -77,13 +77,13 @@ __global__ void __launch_bounds__(256) dropout_shifted_kernel(const DropoutParam
     const int lane = threadIdx.x % TPR, shift = shift_of(x);
     const uint32_t first = (g - t * p.stretches.d) * (NC * TPR);
     if ((int)first * kChunk - shift >= p.d) return;
-    __shared__ __align__(128) T slots[256 / TPR][2][16];
+    __shared__ __align__(16) T slots[256 / TPR][16];
     const Span span = span_of<T>(p.x, p.ldx, (int64_t)p.nodes * p.rows, p.d);
     auto col = [&](int c) { return (int)(first + c * TPR + lane) * kChunk - shift; };
     Raw8<T, true> raw[NC];
 #pragma unroll
     for (int c = 0; c < NC; ++c)
-        if (col(c) < p.d) load_shifted(x, col(c), (col(c) >= 0 && col(c) + 8 <= p.d) || span.has(x + col(c), 8 * (int)sizeof(T)), p.d, raw[c], slots[threadIdx.x / TPR][0]);
+        if (col(c) < p.d) load_shifted(x, col(c), (col(c) >= 0 && col(c) + 8 <= p.d) || span.has(x + col(c), 8 * (int)sizeof(T)), p.d, raw[c], slots[threadIdx.x / TPR]);
     const uint32_t groups = t * chunks + first;
     uint4 before = make_uint4(0, 0, 0, 0);
     if (p.mask.on && shift) before = drop_words(p.mask, groups - 1, node);
@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(256) dropout_shifted_kernel(const DropoutParam
             drop8_by(p.mask, word, v[c]);
         }
     }
-    ShiftedStore<T, TPR, NC>(col(0), p.d, shift, slots[threadIdx.x / TPR][0], lane).store(y, col(0), v, lane, group_mask<TPR>());
+    store_shifted<T, TPR, NC>(y, col(0), p.d, shift, v, slots[threadIdx.x / TPR], lane, group_mask<TPR>());
 }
 
 // ---- launches ---------------------------------------------------------------------------------------

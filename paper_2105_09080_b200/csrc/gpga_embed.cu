@@ -20,7 +20,7 @@ __device__ __forceinline__ int64_t token_at(const void* tokens, bool is64, int64
 template <class T, bool VEC, int TPR, int NC>
 __global__ void __launch_bounds__(256) lookup_kernel(const LookupParams p)
 {
-    __shared__ __align__(128) T slots[VEC ? 1 : 256 / TPR][2][16];
+    __shared__ __align__(16) T slots[VEC ? 1 : 256 / TPR][16];
     const uint32_t node = blockIdx.y;
     const uint32_t g = blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
     const uint32_t t = divide(g, p.stretches);
@@ -52,7 +52,7 @@ __global__ void __launch_bounds__(256) lookup_kernel(const LookupParams p)
         for (int c = 0; c < NC; ++c)
             if (col0 + c * TPR * kChunk < p.d) store8<T>(out + col0 + c * TPR * kChunk, v[c]);
     } else {
-        ShiftedStore<T, TPR, NC>(col0, p.d, shift, slots[threadIdx.x / TPR][0], lane).store(out, col0, v, lane, group_mask<TPR>());
+        store_shifted<T, TPR, NC>(out, col0, p.d, shift, v, slots[threadIdx.x / TPR], lane, group_mask<TPR>());
     }
 }
 

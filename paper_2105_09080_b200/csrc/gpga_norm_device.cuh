@@ -47,7 +47,7 @@ template <class T, bool SHIFT, int TPR, int NC, int R> struct Staged {
     __device__ __forceinline__ uint4* place(int tensor, int r, int c, int piece) const
     {
         const int at = Q == 1 ? piece : piece ^ (piece >> 3 & 1);
-        return stage + ((tensor * R + r) * NC + c) * BLOCK * Q + (threadIdx.x - lane) * Q + at;
+        return stage + (((tensor * R + r) * NC + c) * BLOCK + (threadIdx.x - lane)) * Q + at;
     }
     // full: every chunk is there
     __device__ __forceinline__ void fetch(const T* row, const Span& s, int tensor, int r, bool full) const

@@ -1,4 +1,5 @@
 // Gradient of the layer norm of residual + dropout(x): of z and x row by row, of the weight and the bias over the rows.
+#include <type_traits>
 #include "gpga_norm_device.cuh"
 
 namespace gpga {
@@ -14,6 +15,9 @@ __device__ __forceinline__ void grad8(const f32x2_t* z, const f32x2_t* dy, const
     for (int j = 0; j < 4; ++j) g[j] = mul2(s, fma2(mul2(sub2(z[j], m), s), c, fma2(dy[j], w[j], a)));
 }
 
+struct NoStore {   // in a kernel's aligned form, in place of a ShiftedStore
+    __device__ __forceinline__ NoStore(int, int, int, const void*, int) {}
+};
 struct Yes { static constexpr bool value = true; };
 struct No { static constexpr bool value = false; };
 
@@ -158,7 +162,7 @@ __global__ void __launch_bounds__(block_of(TPR), kPerSM) norm_backward_kernel(co
             }
         }
     };
-    ShiftedStore<T, LANES, NC> to(col(0), p.d, shift, slots[SHIFT ? threadIdx.x / LANES : 0][0], lane);
+    std::conditional_t<SHIFT, ShiftedStore<T, LANES, NC>, NoStore> to(col(0), p.d, shift, slots[SHIFT ? threadIdx.x / LANES : 0][0], lane);
     uint32_t set = 0;
     __shared__ uint4 edges[SHIFT ? BLOCK : 1];
     uint4* own_edges = edges + (SHIFT ? threadIdx.x - lane : 0);
@@ -226,7 +230,7 @@ __global__ void __launch_bounds__(block_of(TPR), kPerSM) norm_backward_kernel(co
 #pragma unroll
             for (int c = 0; c < NC; ++c)
                 if (!SHIFT && (FULL || mine(c))) store8<T>(dres + r * row_g + col(c), g[c]);
-            if (SHIFT) to.store(dres + r * row_g, col(0), g, lane, group_mask<TPR>());
+            if constexpr (SHIFT) to.store(dres + r * row_g, col(0), g, lane, group_mask<TPR>());
             if (!p.dx) continue;
             const uint32_t groups = (first_row + (i + r) * P) * chunks;
             uint4 before = make_uint4(0, 0, 0, 0);
@@ -248,7 +252,7 @@ __global__ void __launch_bounds__(block_of(TPR), kPerSM) norm_backward_kernel(co
                     store8<T>(dx + r * row_x + col(c), g[c]);
                 }
             }
-            if (SHIFT) to.store(dx + r * row_x, col(0), g, lane, group_mask<TPR>());
+            if constexpr (SHIFT) to.store(dx + r * row_x, col(0), g, lane, group_mask<TPR>());
         }
     };
 #pragma unroll
