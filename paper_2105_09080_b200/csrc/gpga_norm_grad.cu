@@ -79,7 +79,8 @@ __device__ __forceinline__ void write_column_sums(const NormBackwardParams& p, u
 // and the pieces lie exchanged in every other group of eight, so that a warp reads its chunks without bank conflicts.
 // Bound: issue slots (56 % busy at 16 warps per SM) beside HBM.  8 x 4096 rows of 1024 bf16, residual and dropout 63 us =
 // 5.3 TB/s, without either 41 us; fp32 130 us = 5.2 TB/s; 2000 rows of 8192 fp32 58 us = 3.4 TB/s, bound by the chain of one
-// row per SM; shifted rows of 1001 bf16 (4 x 8000) 132 us against 184 us when cut.
+// row per SM; shifted rows of 1001 bf16 (4 x 8000) 115 us against 184 us
+// when cut (123 us with a test for every row and chunk).
 // kSets: sets of rows in shared memory, one worked on, the others on their way.
 template <class T, bool SHIFT, int TPR, int NC, int R, int kSets, int kPerSM>
 __global__ void __launch_bounds__(block_of(TPR), kPerSM) norm_backward_kernel(const NormBackwardParams p)
@@ -166,7 +167,7 @@ __global__ void __launch_bounds__(block_of(TPR), kPerSM) norm_backward_kernel(co
     uint32_t set = 0;
     __shared__ uint4 edges[SHIFT ? BLOCK : 1];
     uint4* own_edges = edges + (SHIFT ? threadIdx.x - lane : 0);
-    // one set; full: all its rows and chunks are there
+    // one set; full: all its rows are there, and all chunks or (SHIFT) zeroes in place of what is not
     auto work = [&](int buf, int odd, const float* mean, const float* rstd, auto full_) {
         constexpr bool FULL = decltype(full_)::value;
         float s[2 * R];
@@ -267,7 +268,7 @@ __global__ void __launch_bounds__(block_of(TPR), kPerSM) norm_backward_kernel(co
         fetch_statistics(step);
         copies_wait<kSets - 1>();
         if (Q > 1 || SHIFT) __syncwarp(group_mask<TPR>());   // and their copies of this set are there
-        if (!SHIFT && all_columns && i0 + G * R <= rows) work(buf, odd, mean, rstd, Yes());
+        if ((SHIFT || all_columns) && i0 + G * R <= rows) work(buf, odd, mean, rstd, Yes());
         else work(buf, odd, mean, rstd, No());
         ++set, i0 += step, i += step;
         z += step * row_z, dy += step * row_y, dz += step * row_e, dres += step * row_g, dx += step * row_x;
