@@ -75,12 +75,11 @@ __device__ __forceinline__ void write_column_sums(const NormBackwardParams& p, u
 // columns in every row and so keeps the column sums (dw += dy xh, db += dy) in registers.  The rows' chunks come to a warp
 // through its own places in shared memory, one set ahead, so that the loads in flight take no registers (four rows of
 // three tensors in registers: 75 us for 8 x 4096 rows of 1024 bf16 columns instead of 63); the second pass reads them
-// there again.  In fp32 a chunk is two 16-byte pieces; lanes copy neighbouring pieces, so that whole sectors come at once,
-// and the pieces lie exchanged in every other group of eight, so that a warp reads its chunks without bank conflicts.
+// there again.
 // Bound: issue slots (56 % busy at 16 warps per SM) beside HBM.  8 x 4096 rows of 1024 bf16, residual and dropout 63 us =
 // 5.3 TB/s, without either 41 us; fp32 130 us = 5.2 TB/s; 2000 rows of 8192 fp32 58 us = 3.4 TB/s, bound by the chain of one
-// row per SM; shifted rows of 1001 bf16 (4 x 8000) 115 us against 184 us
-// when cut (123 us with a test for every row and chunk).
+// row per SM; shifted rows of 1001 bf16 (4 x 8000) 115 us against 184 us when cut, and
+// 123 us with a test for every row and chunk of every set.
 // kSets: sets of rows in shared memory, one worked on, the others on their way.
 template <class T, bool SHIFT, int TPR, int NC, int R, int kSets, int kPerSM>
 __global__ void __launch_bounds__(block_of(TPR), kPerSM) norm_backward_kernel(const NormBackwardParams p)
