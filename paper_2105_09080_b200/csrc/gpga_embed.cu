@@ -141,7 +141,7 @@ constexpr uint32_t kSortWords = kSortWarps * 256 + kSortBlocks * 256 + 4 * 256 +
 // maps (for a vocabulary beyond 800,000 rows or so: atomics on the map in memory, which cost 6 us for 65536 tokens).
 __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const SortParams p)
 {
-    extern __shared__ uint32_t smem[];
+    extern __shared__ __align__(16) uint32_t smem[];
     uint32_t rank, blocks;
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(blocks));

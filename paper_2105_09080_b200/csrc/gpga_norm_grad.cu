@@ -22,10 +22,10 @@ struct Yes { static constexpr bool value = true; };
 struct No { static constexpr bool value = false; };
 
 // The block's column sums: its groups of threads one after the other, then out, to the node's gradients or to the block's
-// row of partial sums.  `sums` (2 * TPR * NC * 8 floats) is used where the block has several groups.  col0(c): first
+// row of partial sums.  `sums` (2 * TPR * NC * 4 pairs) is used where the block has several groups.  col0(c): first
 // column of the thread's chunk c.
 template <int TPR, int NC, class Col0>
-__device__ __forceinline__ void write_column_sums(const NormBackwardParams& p, uint32_t node, f32x2_t (*dw)[4], f32x2_t (*db)[4], float* sums,
+__device__ __forceinline__ void write_column_sums(const NormBackwardParams& p, uint32_t node, f32x2_t (*dw)[4], f32x2_t (*db)[4], f32x2_t* sums,
                                                   Col0 col0)
 {
     constexpr int G = block_of(TPR) / TPR;
@@ -40,7 +40,7 @@ __device__ __forceinline__ void write_column_sums(const NormBackwardParams& p, u
                 for (int c = 0; c < NC; ++c)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        f32x2_t* at = reinterpret_cast<f32x2_t*>(sums) + chunk_of<TPR, NC>(c) * 4 + j;
+                        f32x2_t* at = sums + chunk_of<TPR, NC>(c) * 4 + j;
                         if (g) dw[c][j] = add2(at[0], dw[c][j]), db[c][j] = add2(at[D / 2], db[c][j]);
                         at[0] = dw[c][j];
                         at[D / 2] = db[c][j];
@@ -275,7 +275,7 @@ __global__ void __launch_bounds__(block_of(TPR), kPerSM) norm_backward_kernel(co
     }
     copies_wait<0>();
     __syncthreads();
-    write_column_sums<TPR, NC>(p, node, dw, db, reinterpret_cast<float*>(stage), col);
+    write_column_sums<TPR, NC>(p, node, dw, db, reinterpret_cast<f32x2_t*>(stage), col);
 }
 
 // Rows that are off the alignment in different ways: each chunk is cut out of the pieces of memory it lies in.
@@ -284,7 +284,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) norm_backward_odd_kerne
 {
     constexpr int BLOCK = TPR < 128 ? 128 : TPR, G = BLOCK / TPR, LANES = lanes_of(TPR);
     __shared__ __align__(16) float part[2][BLOCK / 32 * 2];
-    __shared__ float sums[G > 1 ? 2 * TPR * NC * 8 : 1];
+    __shared__ f32x2_t sums[G > 1 ? 2 * TPR * NC * 4 : 1];
     const uint32_t node = blockIdx.y, chunks = (uint32_t)(p.d + kChunk - 1) / kChunk;
     const int64_t all = (int64_t)p.nodes * p.rows;
     const Span sz = span_of<T>(p.z, p.ldz, all, p.d), sy = span_of<T>(p.dy, p.lddy, all, p.d), se = span_of<T>(p.dz, p.lddz, all, p.d);
@@ -367,7 +367,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) norm_backward_odd_kerne
 template <class T, bool VEC>
 __global__ void __launch_bounds__(1024) norm_backward_wide_kernel(const NormBackwardParams p)
 {
-    __shared__ float part[32 * 2];
+    __shared__ __align__(16) float part[32 * 2];
     const uint32_t row = blockIdx.x;
     const uint32_t node = row / p.rows, t = row - node * p.rows;
     const uint32_t chunks = (uint32_t)(p.d + kChunk - 1) / kChunk;

@@ -1,0 +1,32 @@
+"""What can be seen of the token-block kernels without a GPU: declarations that the compiler accepts and that only its
+placement or luck in timing would make right."""
+import re
+from pathlib import Path
+
+import pytest
+
+CSRC = Path(__file__).resolve().parent.parent / "paper_2105_09080_b200" / "csrc"
+FILES = ["gpga_dropout.cu", "gpga_norm.cu", "gpga_norm_grad.cu", "gpga_embed.cu"]
+
+
+def code(name):
+    """A source file without its comments."""
+    text = (CSRC / name).read_text()
+    return re.sub(r"//[^\n]*", "", re.sub(r"/\*.*?\*/", "", text, flags=re.S))
+
+
+@pytest.mark.parametrize("name", FILES)
+def test_shared_arrays_that_are_read_wider_than_their_type_are_aligned(name):
+    """An array of a type below eight bytes has that type's alignment unless it says more.  One that is only indexed needs
+    no more; one that is handed on (a pointer to it, an argument) meets 64- and 128-bit accesses there."""
+    found = 0
+    for kernel in re.split(r"\b__global__\b", code(name))[1:]:
+        for m in re.finditer(r"__shared__ (__align__\(\d+\) )?(float|uint32_t|int|T) ([^;]+);", kernel):
+            found += 1
+            for array in re.findall(r"(\w+)(?:\[[^,]*\])+", m[3]):
+                rest = kernel[:m.start()] + kernel[m.end():]
+                handed_on = re.search(rf"\b{array}\b(?!\s*\[)", rest)
+                assert m[1] or not handed_on, f"{name}: {array} in '{m[0]}'"
+    assert found
+
+
