@@ -768,7 +768,7 @@ cudaError_t sums_by_alignment(const SumParams& p, bool direct, uint32_t nodes, b
 }
 
 // Clusters of sixteen blocks have to be asked for, once per device.
-cudaError_t allow_wide_clusters(unsigned long long& done_mask)
+cudaError_t allow_wide_clusters(std::atomic<unsigned long long>& done_mask)
 {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -877,7 +877,7 @@ cudaError_t launch_lookup_grad(const LookupGradParams& g, int dtype, cudaStream_
         size_t smem = (kSortWords + 4 * (size_t)q.per_block) * 4;
         q.map_on_chip = smem + 4 * (size_t)L.words <= kMost;
         if (q.map_on_chip) smem += 4 * (size_t)L.words;
-        static unsigned long long limit_set = 0, wide_set = 0;
+        static std::atomic<unsigned long long> limit_set{0}, wide_set{0};
         cudaError_t e = ensure_smem_limit(sort_tokens_kernel, kMost, limit_set);
         if (e == cudaSuccess && blocks > 8) e = allow_wide_clusters(wide_set);
         if (e != cudaSuccess) return e;

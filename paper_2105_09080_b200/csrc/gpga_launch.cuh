@@ -2,14 +2,16 @@
 #pragma once
 #include <cuda_runtime.h>
 
+#include <atomic>
+
 namespace gpga {
 
 // Raises a kernel's dynamic shared-memory limit once per device instead of on every
 // launch (the attribute call costs about as much as a launch).  `done_mask` is a static
-// of the call site, one bit per device; setting the attribute twice is harmless, so a
-// race between host threads only repeats the call.
+// of the call site, one bit per device; setting the attribute twice is harmless, so
+// host threads that come first together only repeat the call.
 template <class Kernel>
-inline cudaError_t ensure_smem_limit(Kernel kernel, int bytes, unsigned long long& done_mask)
+inline cudaError_t ensure_smem_limit(Kernel kernel, int bytes, std::atomic<unsigned long long>& done_mask)
 {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);

@@ -452,7 +452,7 @@ cudaError_t launch_logreg_partial(const LogregParams& p, cudaStream_t s)
         int slots = kRegSmemBytes / (kRegWarps * (int)p.d * 4);   // row buffers per warp
         if (slots > kRegMaxSlots) slots = kRegMaxSlots;
         const size_t smem_reg = (size_t)kRegWarps * slots * p.d * sizeof(float);
-        static unsigned long long reg_limit_set = 0;
+        static std::atomic<unsigned long long> reg_limit_set{0};
         cudaError_t e = ensure_smem_limit(logreg_partial_tma_reg_kernel, kRegSmemBytes, reg_limit_set);
         if (e != cudaSuccess) return e;
         return launch_after_trigger(logreg_partial_tma_reg_kernel, dim3((unsigned)p.n, (unsigned)chunks),
@@ -464,7 +464,7 @@ cudaError_t launch_logreg_partial(const LogregParams& p, cudaStream_t s)
         const size_t smem_cols = 2 * (size_t)kColsCells * p.d * sizeof(float);   // before / J below
 #define GPGA_COLS(J)                                                                                   \
     do {                                                                                               \
-        static unsigned long long limit_set = 0;                                                       \
+        static std::atomic<unsigned long long> limit_set{0};                                           \
         cudaError_t e = ensure_smem_limit(logreg_partial_tma_cols_kernel<J>, 64 * 1024, limit_set);    \
         if (e != cudaSuccess) return e;                                                                \
         return launch_after_trigger(logreg_partial_tma_cols_kernel<J>, grid, dim3(kLrBlock), smem_cols / J, s, \
@@ -476,7 +476,7 @@ cudaError_t launch_logreg_partial(const LogregParams& p, cudaStream_t s)
 #undef GPGA_COLS
     }
     const size_t smem = (size_t)(p.d + kChunkRows) * sizeof(float);
-    static unsigned long long plain_limit_set = 0;
+    static std::atomic<unsigned long long> plain_limit_set{0};
     cudaError_t e = ensure_smem_limit(logreg_partial_kernel, 200 * 1024, plain_limit_set);
     if (e != cudaSuccess) return e;
     logreg_partial_kernel<<<dim3((unsigned)p.n, (unsigned)chunks), kLrBlock, smem, s>>>(p);

@@ -528,7 +528,7 @@ cudaError_t run_config(cudaLaunchConfig_t* cfg, cudaLaunchAttribute* attrs, int 
     attrs[0].val.clusterDim.z = 1;
     cfg->attrs = attrs;
     cfg->numAttrs = 1;
-    static unsigned long long limit_set = 0, limit_set_full = 0;
+    static std::atomic<unsigned long long> limit_set{0}, limit_set_full{0};
     const cudaError_t e = ensure_smem_limit(logreg_run_kernel<false>, kRunSmemLimit, limit_set);
     return e != cudaSuccess ? e : ensure_smem_limit(logreg_run_kernel<true>, kRunSmemLimit, limit_set_full);
 }

@@ -142,7 +142,7 @@ cudaError_t launch_logistic_global_loss(const float* A, const float* y, const fl
     const int rows_per_block = (int)((m + chunks - 1) / chunks);
     chunks = (m + rows_per_block - 1) / rows_per_block;
     if ((size_t)d * sizeof(float) > 48 * 1024) {   // xbar in shared memory beyond the default limit
-        static unsigned long long limit_set = 0;
+        static std::atomic<unsigned long long> limit_set{0};
         cudaError_t e = ensure_smem_limit(logistic_full_loss_kernel, 200 * 1024, limit_set);
         if (e != cudaSuccess) return e;
     }
@@ -285,7 +285,7 @@ cudaError_t launch_shard_logistic_loss_part(const float* A, const float* y, long
     const int rows_per_block = (int)((m + chunks - 1) / chunks);
     chunks = (m + rows_per_block - 1) / rows_per_block;
     if ((size_t)d * sizeof(float) > 48 * 1024) {
-        static unsigned long long limit_set = 0;
+        static std::atomic<unsigned long long> limit_set{0};
         cudaError_t e = ensure_smem_limit(logistic_full_loss_kernel, 200 * 1024, limit_set);
         if (e != cudaSuccess) return e;
     }

@@ -448,14 +448,25 @@ __global__ void __launch_bounds__(1024) norm_forward_wide_kernel(const NormForwa
 // ---- launches ---------------------------------------------------------------------------------------
 constexpr int kForwardWide = 16384, kForwardOddWide = 8192;   // widest rows that stay in registers
 
-// Blocks of a kernel that an SM holds, from its registers (looked up once) and shared memory.
+// What a block of a kernel takes of an SM beside its dynamic shared memory; looked up once, by the initialiser of a static
+// (host threads that come first together wait for it).
+struct KernelUse {
+    int regs;      // per thread
+    size_t smem;   // static
+};
 template <class Kernel>
-int blocks_per_sm(Kernel kernel, int block, size_t smem, cudaFuncAttributes& at)
+KernelUse use_of(Kernel kernel)
 {
-    if (!at.numRegs && (cudaFuncGetAttributes(&at, kernel) != cudaSuccess || !at.numRegs)) at.numRegs = 128;
-    int n = 65536 / ((at.numRegs + 7) / 8 * 8 * block);
+    cudaFuncAttributes at = {};
+    if (cudaFuncGetAttributes(&at, kernel) != cudaSuccess) (void)cudaGetLastError();   // the launch will say what is wrong
+    return {at.numRegs > 0 ? at.numRegs : 128, at.sharedSizeBytes};
+}
+// Blocks that an SM holds.
+int blocks_per_sm(const KernelUse& use, int block, size_t smem)
+{
+    int n = 65536 / ((use.regs + 7) / 8 * 8 * block);
     if (n > 2048 / block) n = 2048 / block;
-    const int by_smem = (int)(227 * 1024 / (smem + at.sharedSizeBytes + 1024));
+    const int by_smem = (int)(227 * 1024 / (smem + use.smem + 1024));
     if (n > by_smem) n = by_smem;
     return n < 1 ? 1 : n;
 }
@@ -467,13 +478,13 @@ cudaError_t forward_odd(const NormForwardParams& p, cudaStream_t s)
     const size_t smem = (size_t)((p.d + kChunk - 1) / kChunk) * 64;
     const auto kernel = norm_forward_odd_kernel<T, VEC, TPR, NC, R>;
     if (smem > 47 * 1024) {
-        static unsigned long long limit_set = 0;
+        static std::atomic<unsigned long long> limit_set{0};
         const cudaError_t e = ensure_smem_limit(kernel, kForwardOddWide * 8, limit_set);
         if (e != cudaSuccess) return e;
     }
-    static cudaFuncAttributes use = {};
+    static const KernelUse use = use_of(kernel);
     const uint32_t sets = (p.rows + SET - 1) / SET;
-    const uint32_t room = (uint32_t)(kSMs * blocks_per_sm(kernel, BLOCK, smem, use)) / p.nodes;
+    const uint32_t room = (uint32_t)(kSMs * blocks_per_sm(use, BLOCK, smem)) / p.nodes;
     kernel<<<dim3(sets < room ? sets : room ? room : 1, p.nodes), BLOCK, smem, s>>>(p);
     return cudaGetLastError();
 }
@@ -486,13 +497,13 @@ cudaError_t forward_shifted(const NormForwardParams& p, cudaStream_t s)
     constexpr int kStage = !STAGED ? 0 : 4 * R * NC * BLOCK * kChunk * (int)sizeof(T);
     const size_t smem = (size_t)((p.d + P + kChunk - 1) / kChunk) * 64 + kStage;
     const auto kernel = norm_forward_shifted_kernel<T, TPR, NC, R, STAGED>;
-    static unsigned long long limit_set = 0;
+    static std::atomic<unsigned long long> limit_set{0};
     const cudaError_t e = ensure_smem_limit(kernel, (TPR * NC + 2) * kChunk * 8 + kStage, limit_set);
     if (e != cudaSuccess) return e;
-    static cudaFuncAttributes use = {};
+    static const KernelUse use = use_of(kernel);
     // as many blocks as fit, in whole classes of rows
     const uint32_t sets = ((p.rows + P - 1) / P + SET - 1) / SET;
-    const uint32_t room = (uint32_t)(kSMs * blocks_per_sm(kernel, BLOCK, smem, use)) / (p.nodes * P);
+    const uint32_t room = (uint32_t)(kSMs * blocks_per_sm(use, BLOCK, smem)) / (p.nodes * P);
     kernel<<<dim3(P * (sets < room ? sets : room ? room : 1), p.nodes), BLOCK, smem, s>>>(p);
     return cudaGetLastError();
 }

@@ -510,7 +510,7 @@ cudaError_t backward_as(const NormBackwardParams& p, cudaStream_t s)
     constexpr size_t kStage = (size_t)kSets * 3 * R * NC * 8 * sizeof(T) * BLOCK, kSums = G > 1 ? (size_t)2 * TPR * NC * 8 * 4 : 0;
     constexpr size_t smem = kStage > kSums ? kStage : kSums;
     const auto kernel = norm_backward_kernel<T, SHIFT, TPR, NC, R, kSets, kPerSM>;
-    static unsigned long long limit_set = 0;
+    static std::atomic<unsigned long long> limit_set{0};
     const cudaError_t e = ensure_smem_limit(kernel, (int)smem, limit_set);
     if (e != cudaSuccess) return e;
     kernel<<<dim3(p.splits, p.nodes), BLOCK, smem, s>>>(p);

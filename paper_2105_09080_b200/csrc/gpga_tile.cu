@@ -385,7 +385,7 @@ cudaError_t launch_step_tile_w(const StepParams& p, int mode, bool vec, int mix,
     const int blk = cells >= kTileBlock ? kTileBlock : (int)((cells + 31) / 32 * 32);
 #define GPGA_TILE(M, V)                                                                          \
     do {                                                                                         \
-        static unsigned long long limit_set = 0;                                                 \
+        static std::atomic<unsigned long long> limit_set{0};                                     \
         cudaError_t e = ensure_smem_limit(step_tile_kernel<M, V>, kTileSmemBytes, limit_set);    \
         if (e != cudaSuccess) return e;                                                          \
         step_tile_kernel<M, V><<<grd, blk, smem, s>>>(p, mix, tile_groups, log2n, sw);           \
@@ -393,7 +393,7 @@ cudaError_t launch_step_tile_w(const StepParams& p, int mode, bool vec, int mix,
     if (mode == GRAD_PARTIALS) {   // logistic objective: d % 4 == 0 is required upstream
         // always follows the gradient kernel on the stream and waits for it first thing, so it may
         // be made resident while that kernel drains
-        static unsigned long long limit_set = 0;
+        static std::atomic<unsigned long long> limit_set{0};
         cudaError_t e = ensure_smem_limit(step_tile_kernel<GRAD_PARTIALS, true>, kTileSmemBytes, limit_set);
         if (e != cudaSuccess) return e;
         return launch_after_trigger(step_tile_kernel<GRAD_PARTIALS, true>, dim3(grd), dim3(blk), smem, s, true, p,
@@ -460,7 +460,7 @@ cudaError_t launch_run_tile(const StepParams& p, int mode, bool vec, int topolog
     const int blk = cells >= kTileBlock ? kTileBlock : (int)((cells + 31) / 32 * 32);
 #define GPGA_RUN_TILE(M, V)                                                                      \
     do {                                                                                         \
-        static unsigned long long limit_set = 0;                                                 \
+        static std::atomic<unsigned long long> limit_set{0};                                     \
         cudaError_t e = ensure_smem_limit(run_tile_kernel<M, V>, kTileSmemBytes, limit_set);     \
         if (e != cudaSuccess) return e;                                                          \
         run_tile_kernel<M, V><<<grd, blk, smem, s>>>(p, topology, H, phase0, hop0, steps, tile_groups, log2n, sw); \

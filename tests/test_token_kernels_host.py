@@ -30,3 +30,11 @@ def test_shared_arrays_that_are_read_wider_than_their_type_are_aligned(name):
     assert found
 
 
+
+
+@pytest.mark.parametrize("name", FILES + ["gpga_token_api.cu", "gpga_launch.cuh"])
+def test_host_statics_can_be_shared_by_threads(name):
+    """The entries take no handle and may be called from several threads: what a host function keeps from one call to the
+    next is initialised once by the language (const) or atomic."""
+    kept = re.findall(r"^\s+static (?!__device__|inline\b|constexpr\b)[^;({]*", code(name), flags=re.M)
+    assert all(re.match(r"\s+static (const |std::atomic<)", s) for s in kept), kept
