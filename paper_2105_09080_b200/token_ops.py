@@ -245,7 +245,8 @@ def layer_norm_forward(x, weight, bias, eps=1e-5, residual=None, p=0.0, seed=0, 
     """Layer norm of z = residual + dropout(x) (gpga_layer_norm_forward): returns (y, z, mean, rstd).
 
     ``weight`` and ``bias``: (d,), (nodes, d) or None.  z is ``x`` itself where there is neither a residual nor
-    dropout.  mean and rstd: one float32 per row.  What the backward call wants is z, mean and rstd.
+    dropout, unless y replaces it (``out`` in x's place): then z is a tensor of its own.  mean and rstd: one float32 per
+    row.  What the backward call wants is z, mean and rstd.
     """
     if stream is not None:
         return _on_stream(layer_norm_forward, locals())
@@ -253,7 +254,7 @@ def layer_norm_forward(x, weight, bias, eps=1e-5, residual=None, p=0.0, seed=0, 
     shape, dtype, code, device, d, rows = _vectors(x, nodes)
     if out is None:
         out = _like(x)
-    if z is None and (residual is not None or p > 0):
+    if z is None and (residual is not None or p > 0 or out.data_ptr() == x.data_ptr()):
         z = _like(x)
     if mean is None:
         mean = x.new_empty(shape[:-1], dtype=torch.float32)
