@@ -576,7 +576,8 @@ int32_t gpga_dropout(const gpga_dropout_args_t* args, void* stream);
  *     mean = sum z / d, rstd = 1 / sqrt(sum (z - mean)^2 / d + eps), y = (z - mean) * rstd * w_i + b_i.
  * residual NULL: z = dropout(x); p, seed, k, site, node0 as for gpga_dropout; weight NULL: w = 1; bias NULL: b = 0;
  * parameters of node i at + i * ldw.  z (may be NULL) receives z; mean and rstd, nodes * rows fp32 each, what the
- * backward call wants.  eps >= 0 and finite.
+ * backward call wants.  eps >= 0 and finite.  With eps = 0 a row of equal values has no defined y: what is left of it is
+ * the rounding of its mean, divided by itself.
  */
 typedef struct gpga_layer_norm_forward_args {
     const void *x, *residual;

@@ -30,8 +30,9 @@ __device__ __forceinline__ f32x2_t squares8(const f32x2_t* v, float mean, uint32
     return s;
 }
 
-// s / n for a row's mean: one multiplication by fl(1 / n), corrected by the exact remainder.  (A constant row's mean is
-// exact this way, as by a division, which takes several times the instructions.)
+// s / n for a row's mean: one multiplication by fl(1 / n), corrected by the exact remainder: as good as a division, which
+// takes several times the instructions.  (A constant row's mean is exact where the sum s is, otherwise off by the sum's rounding:
+// of 200 random constants 69 at 1000 columns, none at 1024 or 4096.)
 __device__ __forceinline__ float mean_of(float s, float n, float inv_n)
 {
     const float m = s * inv_n;

@@ -1,0 +1,31 @@
+"""Token-block operators at the edges of what their definitions say."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2105_09080_b200 as pkg
+from test_gpu_token_ops import U, depth, gen, normal
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("d", [7, 77, 640, 1000, 1001, 1024, 5000, 9001, 20000])
+def test_layer_norm_of_constant_rows(d):
+    """A constant row's mean is as good as its sum: off by at most the additions' rounding, and by one product's and its
+    correction's.  What remains of the row is that error times 1 / sqrt(eps), the variance at most its square."""
+    g = gen(41)
+    values = torch.tensor([0.36159506, 3.0, -0.1, 1e-3, 1234.567, -7e4, 0.0], device="cuda")
+    x = values[:, None].expand(-1, d).contiguous()
+    w, b = 1 + 0.2 * normal(g, d), 0.3 * normal(g, d)
+    eps = float(np.float32(1e-5))
+    c = values.double()[:, None]
+    off = (depth(d) + 2) * U * c.abs()
+    for weight, bias in ((w, b), (w, None), (None, None)):
+        y, z, mean, rstd = pkg.layer_norm_forward(x, weight, bias, eps=1e-5)
+        W = weight.double().abs() if weight is not None else 1.0
+        B = bias.double() if bias is not None else torch.zeros(d, dtype=torch.float64, device="cuda")
+        assert z is x and ((mean.double()[:, None] - c).abs() <= off).all()
+        assert (rstd.double()[:, None] <= eps ** -0.5 * (1 + 4 * U)).all()
+        assert (rstd.double()[:, None] >= (eps + off * off) ** -0.5 * (1 - 8 * U)).all()
+        assert ((y.double() - B).abs() <= W * off * eps ** -0.5 * (1 + 8 * U) + 2 * U * B.abs()).all()
+        assert torch.equal(y[-1].double(), B.expand(d))
