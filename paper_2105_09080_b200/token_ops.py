@@ -119,7 +119,7 @@ def _stats(t, what, vectors, device):
 
 def _params(t, what, nodes, d, device):
     """Node stride of a float32 parameter (d,) or (nodes, d)."""
-    if t.dtype is not torch.float32 or t.get_device() != device or t.numel() != nodes * d or t.shape[-1] != d or t.dim() > 2:
+    if t.dtype is not torch.float32 or t.get_device() != device or t.numel() != nodes * d or t.dim() not in (1, 2) or t.shape[-1] != d:
         _bad(f"{what}: got {tuple(t.shape)} {t.dtype} on {t.device}, want float32 ({nodes}, {d}) on cuda:{device}")
     if t.is_contiguous():
         return d
