@@ -234,23 +234,27 @@ def dropout(x, p, seed, k=0, site=0, node0=0, nodes=1, out=None, stream=None):
     return out
 
 
-def _nodes_of(weight, nodes):
+def _nodes_of(nodes, *params):
+    """The given number of nodes, or that of the first parameter that is there."""
     if nodes is not None:
         return nodes
-    return weight.shape[0] if weight is not None and weight.dim() == 2 else 1
+    for t in params:
+        if t is not None:
+            return t.shape[0] if t.dim() == 2 else 1
+    return 1
 
 
 def layer_norm_forward(x, weight, bias, eps=1e-5, residual=None, p=0.0, seed=0, k=0, site=0, node0=0, nodes=None,
                        out=None, z=None, mean=None, rstd=None, stream=None):
     """Layer norm of z = residual + dropout(x) (gpga_layer_norm_forward): returns (y, z, mean, rstd).
 
-    ``weight`` and ``bias``: (d,), (nodes, d) or None.  z is ``x`` itself where there is neither a residual nor
-    dropout, unless y replaces it (``out`` in x's place): then z is a tensor of its own.  mean and rstd: one float32 per
-    row.  What the backward call wants is z, mean and rstd.
+    ``weight`` and ``bias``: (d,), (nodes, d) or None; without ``nodes`` they say how many there are.  z is ``x`` itself
+    where there is neither a residual nor dropout, unless y replaces it (``out`` in x's place): then z is a tensor of its
+    own.  mean and rstd: one float32 per row.  What the backward call wants is z, mean and rstd.
     """
     if stream is not None:
         return _on_stream(layer_norm_forward, locals())
-    nodes = _nodes_of(weight, nodes)
+    nodes = _nodes_of(nodes, weight, bias)
     shape, dtype, code, device, d, rows = _vectors(x, nodes)
     if out is None:
         out = _like(x)
@@ -286,14 +290,14 @@ def layer_norm_backward(dy, z, mean, rstd, weight, dz=None, p=0.0, seed=0, k=0, 
     """Gradient of ``layer_norm_forward`` (gpga_layer_norm_backward): returns (dresidual, dx, dweight, dbias).
 
     ``dz``: gradient that reaches z past the norm.  dx is dresidual itself where p = 0.  dweight and dbias are sums over
-    each node's rows, added to what the given tensors hold with ``accumulate``; without a weight they are None unless
-    given.
+    each node's rows, added to what the given tensors hold with ``accumulate`` (which wants both beside a weight);
+    without a weight they are None unless given.
     """
     if stream is not None:
         return _on_stream(layer_norm_backward, locals())
-    nodes = _nodes_of(weight, nodes)
+    nodes = _nodes_of(nodes, weight, dweight, dbias)
     shape, dtype, code, device, d, rows = _vectors(z, nodes)
-    if accumulate and (dweight is None or dbias is None):
+    if accumulate and weight is not None and (dweight is None or dbias is None):
         _bad("accumulate wants dweight and dbias")
     if dresidual is None:
         dresidual = _like(z)

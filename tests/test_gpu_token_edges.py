@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2105_09080_b200 as pkg
-from test_gpu_token_ops import U, depth, gen, normal
+from test_gpu_token_ops import U, check_forward, depth, gen, normal
 
 pytestmark = pytest.mark.gpu
 
@@ -29,3 +29,33 @@ def test_layer_norm_of_constant_rows(d):
         assert (rstd.double()[:, None] >= (eps + off * off) ** -0.5 * (1 - 8 * U)).all()
         assert ((y.double() - B).abs() <= W * off * eps ** -0.5 * (1 + 8 * U) + 2 * U * B.abs()).all()
         assert torch.equal(y[-1].double(), B.expand(d))
+
+
+@pytest.mark.parametrize("d", [24, 77, 1024])
+def test_norms_without_a_weight(d):
+    """A bias of every node alone, gradients of parameters that the norm does not multiply by, nothing to add up: the
+    gradients are those of a weight of ones."""
+    g = gen(42)
+    n, T = 3, 9
+    x, b, dy = normal(g, n, T, d), normal(g, n, d), normal(g, n, T, d)
+    ones = torch.ones((n, d), device="cuda")
+    y, z, mean, rstd = pkg.layer_norm_forward(x, None, b)
+    check_forward(x, None, None, b, 1e-5, 0.0, None, n, (y, z, mean, rstd), torch.float32)
+    assert torch.equal(y, pkg.layer_norm_forward(x, None, b, nodes=n)[0])
+    want = pkg.layer_norm_backward(dy, x, mean, rstd, ones)
+    start = normal(g, n, d)
+    for names in (("dweight",), ("dbias",), ("dweight", "dbias")):
+        given = {k: torch.full((n, d), float("nan"), device="cuda") for k in names}
+        got = pkg.layer_norm_backward(dy, x, mean, rstd, None, **given)
+        assert torch.equal(got[0], want[0])
+        for at, name in ((2, "dweight"), (3, "dbias")):
+            assert got[at] is given.get(name) and (got[at] is None or torch.equal(got[at], want[at]))
+        more = {k: start.clone() for k in names}
+        got = pkg.layer_norm_backward(dy, x, mean, rstd, None, accumulate=True, **more)
+        for at, name in ((2, "dweight"), (3, "dbias")):
+            assert got[at] is None or torch.equal(got[at], start + want[at])
+    got = pkg.layer_norm_backward(dy, x, mean, rstd, None, accumulate=True)
+    assert torch.equal(got[0], want[0]) and got[2] is None and got[3] is None
+    for given in ({}, {"dweight": start.clone()}, {"dbias": start.clone()}):      # with a weight both are written
+        with pytest.raises(pkg.GpgaError):
+            pkg.layer_norm_backward(dy, x, mean, rstd, ones, accumulate=True, **given)
