@@ -545,7 +545,8 @@ cudaError_t forward_of(const NormForwardParams& p, cudaStream_t s)
             if (d <= 512) return forward_shifted<T, W ? 32 : 16, W ? 2 : 4, 1, true>(p, s);
             if (d <= 768) return forward_shifted<T, 32, 3, 1, false>(p, s);
             if (d <= 1024) return forward_shifted<T, W ? 64 : 32, W ? 2 : 4, 1, !W>(p, s);
-            if (!W && d <= 1280) return forward_shifted<T, W ? 96 : 32, W ? 2 : 5, 1, !W>(p, s);
+            if constexpr (!W)
+                if (d <= 1280) return forward_shifted<T, 32, 5, 1, true>(p, s);
             if (d <= 1536) return forward_shifted<T, W ? 96 : 64, W ? 2 : 3, 1, false>(p, s);
             if (d <= 2048) return forward_shifted<T, W ? 128 : 64, W ? 2 : 4, 1, !W>(p, s);
             if (d <= 2560) return forward_shifted<T, W ? 160 : 128, W ? 2 : 3, 1, false>(p, s);
