@@ -12,6 +12,10 @@ Outputs, statistics and scratch are allocated unless they are given.  Calls are 
 current one), allocate through torch's allocator only and can be captured in a CUDA graph.  With a ``stream`` other than
 the current one the new tensors belong to that stream and the given ones are marked as used there; ordering the two
 streams is the caller's part.
+
+These are plain functions, outside automatic differentiation: tensors that require gradients are taken for their values,
+what comes back has no graph behind it, and a model calls the ``_backward`` functions itself (as ``token_experiment``
+does, or inside a ``torch.autograd.Function`` of its own).
 """
 from __future__ import annotations
 

@@ -59,3 +59,19 @@ def test_norms_without_a_weight(d):
     for given in ({}, {"dweight": start.clone()}, {"dbias": start.clone()}):      # with a weight both are written
         with pytest.raises(pkg.GpgaError):
             pkg.layer_norm_backward(dy, x, mean, rstd, ones, accumulate=True, **given)
+
+
+def test_tensors_that_require_gradients_are_taken_for_their_values():
+    """No call takes part in automatic differentiation: the same values with and without, and nothing behind them."""
+    g = gen(43)
+    table, w, x = normal(g, 11, 40), normal(g, 40), normal(g, 6, 40)
+    tokens = torch.randint(0, 11, (6,), generator=g, device="cuda")
+
+    def calls(table, w, x):
+        y, z, mean, rstd = pkg.layer_norm_forward(x, w, w, residual=x, p=0.1, seed=3)
+        return [pkg.embedding_forward(table, tokens), pkg.dropout(x, 0.3, 5), y, z, mean, rstd,
+                *pkg.layer_norm_backward(x, z, mean, rstd, w, p=0.1, seed=3)]
+
+    want = calls(table, w, x)
+    got = calls(*(torch.nn.Parameter(t) for t in (table, w, x)))
+    assert all(torch.equal(a, b) and not a.requires_grad for a, b in zip(got, want))
