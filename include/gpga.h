@@ -538,6 +538,8 @@ int32_t gpga_embedding_forward(const gpga_embedding_forward_args_t* args, void* 
  * vocabulary are left out.  The tokens of a node are sorted on chip (stable, 65536 at a time); the sum of a token is
  * formed in fp32 over fixed groups of its sorted places, so the result is the same in every run.  grad rows: grad + i *
  * node_ldg + v * ldg, without overlap.
+ * More than 8192 tokens per node are sorted by a cluster of sixteen thread blocks, a non-portable size that every undivided
+ * B200 places; where a partition of a device cannot, the call returns CUDA and writes nothing.
  * scratch: gpga_embedding_scratch_bytes(nodes, rows, d, vocab) bytes.
  */
 typedef struct gpga_embedding_backward_args {
