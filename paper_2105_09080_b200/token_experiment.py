@@ -44,7 +44,8 @@ class TokenModel:
         row[3 * table + dim:] = 0.0
         self.X[:, :self.d] = row                           # Algorithm 1: equal initial rows
         # The mixing alone: learning rate 0 leaves the half-step of the library's quadratic objective at X, whose local
-        # update is done before the call; in place (one buffer for X and X+), G stands in for the unused data.
+        # update is done before the call; in place (one buffer for X and X+), G stands in for the data, which is read and
+        # multiplied by zero: an infinite gradient leaves NaN in the rows it reaches.
         self.mixer = B.Gpga(n, self.d, topology, H, 0.0, seed)
         self.mixer.set_row_stride(ld)
         self.mixer.bind(self.X, self.X, self.G)
