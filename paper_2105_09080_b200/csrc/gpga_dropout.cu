@@ -7,7 +7,8 @@ namespace {
 
 // Both tensors dense and aligned: U chunks per thread, 256 apart, their loads in flight together; no index arithmetic per
 // chunk but an addition (with a division by the row's length and 64-bit products it took 134 instructions per chunk instead
-// of 97, and issue slots bounded it).  Bound: HBM.  8 x 4096 x 4096 bf16 80 us = 6.7 TB/s, one chunk per thread 118 us.
+// of 97, and issue slots bounded it).  Bound: HBM.  8 x 4096 x 4096 bf16: calls one after the other 88 us = 6.1 TB/s (a plain
+// copy: 6.5); replayed in a graph, where part of the last pass is still in L2, 80 us, one chunk per thread 118 us.
 template <class T, int U>
 __global__ void __launch_bounds__(256) dropout_dense_kernel(const DropoutParams p)
 {

@@ -138,7 +138,7 @@ constexpr uint32_t kSortWords = kSortWarps * 256 + kSortBlocks * 256 + 4 * 256 +
 // block sends to all); the last pass writes them to memory.  A token outside the vocabulary sorts behind all others, as
 // the key `vocab`.  65536 tokens of 50021 words 19 us, 4096 of 32000 10 us: barriers and shared-memory latency of two
 // passes, 3200 cycles of ranking in each.  On the way the blocks mark the vocabulary rows that are named, each in a map of its own, and join the
-// maps (for a vocabulary beyond 800,000 rows or so: atomics on the map in memory, which cost 6 us for 65536 tokens).
+// maps (where that does not fit, from 0.9 million rows on at 4096 entries per block, 1.3 million at 700: atomics on the map in memory, which cost 6 us for 65536 tokens).
 __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const SortParams p)
 {
     extern __shared__ __align__(16) uint32_t smem[];

@@ -76,8 +76,8 @@ __device__ __forceinline__ void write_column_sums(const NormBackwardParams& p, u
 // through its own places in shared memory, one set ahead, so that the loads in flight take no registers (four rows of
 // three tensors in registers: 75 us for 8 x 4096 rows of 1024 bf16 columns instead of 63); the second pass reads them
 // there again.
-// Bound: issue slots (56 % busy at 16 warps per SM) beside HBM.  8 x 4096 rows of 1024 bf16, residual and dropout 63 us =
-// 5.3 TB/s, without either 41 us; fp32 130 us = 5.2 TB/s; 2000 rows of 8192 fp32 58 us = 3.4 TB/s, bound by the chain of one
+// Bound: neither issue slots (56 % busy) nor HBM alone, but latency at 16 warps per SM beside both.  8 x 4096 rows of 1024
+// bf16, residual and dropout 63 us = 5.3 TB/s in a graph (whole calls 69 us), without either 41 us; fp32 130 us = 5.2 TB/s; 2000 rows of 8192 fp32 58 us = 3.4 TB/s, bound by the chain of one
 // row per SM; shifted rows of 1001 bf16 (4 x 8000) 115 us against 184 us when cut, and
 // 123 us with a test for every row and chunk of every set.
 // kSets: sets of rows in shared memory, one worked on, the others on their way.

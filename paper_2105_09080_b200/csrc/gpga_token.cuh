@@ -411,7 +411,8 @@ __device__ __forceinline__ void store_shifted(T* row, int col0, int d, int shift
 }
 
 // The same for row after row: what depends on the columns alone is worked out once (lookup of 4 x 4096 rows of 1663 fp32, one
-// row each: 39 us this way, 35 us with the function above; norm gradient of 4 x 8000 rows of 1001: 126 and 137 us).
+// row each: 39 us this way, 35 us with the function above; norm gradient of 4 x 8000 rows of 1001: 126 and 137 us
+// when this was measured, 115 us with the tests taken out of full sets since).
 template <class T, int LANES, int NC> struct ShiftedStore {
     T* slots;        // two pairs of chunks for these lanes, used in turn: a row's are read while the next one's are written
     int at0, at1;    // columns of the ends that this lane stores, -1: none
