@@ -616,6 +616,73 @@ typedef struct gpga_layer_norm_backward_args {
 int32_t gpga_layer_norm_backward(const gpga_layer_norm_backward_args_t* args, void* stream);
 int64_t gpga_layer_norm_scratch_bytes(int64_t nodes, int64_t rows, int64_t d);
 
+/*
+ * Matrix operators: the parts of a token model whose work is matrix products, on the tensor cores.  The conventions of
+ * the token-block operators hold, and these:
+ *
+ *  - A matrix of node i is row-major and starts at p + i * node_p, its rows ld_p apart (elements).  Weights are fp32 (slices of
+ *    X) or of the activations' type; fp32 weights beside 16-bit activations are rounded to that type once per call.
+ *  - fp32 operands (all of a call with fp32 activations) are taken as exact sums of three bfloat16 values, so that results
+ *    are as good as fp32 arithmetic gives; an infinity among them gives NaN in what it reaches.  16-bit operands are taken as
+ *    they are.  Sums are fp32.  What passes from one product to the next (h, dg, du) has the activations' type.
+ *  - Scratch: the _scratch_bytes function of an entry, given the entry's own argument struct (its scratch members are not
+ *    looked at), says how much it needs; 0 also where the arguments are wrong.
+ *  - Waits inside the kernels are bounded.  One that gives up (which takes seconds and does not happen in a sound run) ends
+ *    the call's kernels with undefined results; gpga_token_status, which waits for the stream, then returns TIMEOUT, from
+ *    then on and for the current device.
+ */
+enum { GPGA_ACTIVATION_SILU = 0, GPGA_ACTIVATION_GELU = 1, GPGA_ACTIVATION_RELU = 2 };
+int32_t gpga_token_status(void* stream);
+
+/*
+ * Gated feed-forward block, per node (gate, up: f x d; down: d x f):
+ *     g = x gate^T,  u = x up^T,  h = act(g) u,  y = h down^T.
+ * act: silu(v) = v / (1 + exp(-v)), gelu(v) = v (1 + erf(v / sqrt 2)) / 2, relu(v) = max(v, 0).  g and u (both or neither
+ * may be NULL) receive the projections, which the backward call wants; they are nodes * rows vectors of f.  1 <= f <= 2^20,
+ * nodes * d * f <= 2^40, nodes * rows * max(d, f) <= 2^40.  y may be x itself.
+ */
+typedef struct gpga_feed_forward_forward_args {
+    const void *x, *gate, *up, *down;
+    void *y, *g, *u, *scratch;
+    int64_t scratch_bytes, ldx, ldgate, node_gate, ldup, node_up, lddown, node_down, ldy, ldg, ldu, dtype, weight_dtype, activation, nodes, rows, d, f;
+} gpga_feed_forward_forward_args_t;
+int32_t gpga_feed_forward_forward(const gpga_feed_forward_forward_args_t* args, void* stream);
+int64_t gpga_feed_forward_forward_scratch_bytes(const gpga_feed_forward_forward_args_t* args);
+
+/*
+ * Its gradient, from the g and u that the forward call kept:
+ *     dh = dy down,  du = dh act(g),  dg = dh u act'(g),  h = act(g) u,
+ *     ddown = dy^T h,  dgate = dg^T x,  dup = du^T x  (sums over the node's rows),  dx = dg gate + du up.
+ * relu'(0) = 0.  The weights' gradients have type grad_dtype: fp32 or the activations' type; they are added to what the
+ * arrays hold where accumulate is not 0.  dx may be dy or x itself.
+ */
+typedef struct gpga_feed_forward_backward_args {
+    const void *dy, *x, *g, *u, *gate, *up, *down;
+    void *dx, *dgate, *dup, *ddown, *scratch;
+    int64_t scratch_bytes, lddy, ldx, ldg, ldu, ldgate, node_gate, ldup, node_up, lddown, node_down, lddx, lddgate, node_dgate, lddup, node_dup, ldddown,
+        node_ddown, dtype, weight_dtype, grad_dtype, accumulate, activation, nodes, rows, d, f;
+} gpga_feed_forward_backward_args_t;
+int32_t gpga_feed_forward_backward(const gpga_feed_forward_backward_args_t* args, void* stream);
+int64_t gpga_feed_forward_backward_scratch_bytes(const gpga_feed_forward_backward_args_t* args);
+
+/*
+ * Orthogonalises an update: per node, with the r x c matrix M,
+ *     X = M / (|M| + eps)  (Frobenius norm),  then `steps` times  X <- c1 X + c3 (X X^T) X + c5 (X X^T)^2 X,
+ *     out = scale X, or out + scale X where accumulate is not 0 (a local update x - gamma X is scale = -gamma).
+ * A singular value s of M / |M| becomes p(p(...p(s))) with p(s) = c1 s + c3 s^3 + c5 s^5; singular vectors stay.  Coefficients
+ * must keep p(s) within [-8, 8] on the way (fp16 range of the products).  M and out have type dtype; fp32 is computed with
+ * 22 significant bits, the 16-bit types with 11.  Zero gives zero (eps > 0); an infinity or NaN in M makes its node NaN.
+ * 1 <= r, c <= 2^20, nodes * r * c <= 2^40, 1 <= steps <= 1000.  out may be M itself.
+ */
+typedef struct gpga_orthogonalize_args {
+    const void* update;
+    void *out, *scratch;
+    int64_t scratch_bytes, ldm, node_ldm, ldo, node_ldo, dtype, nodes, r, c, steps, accumulate;
+    double c1, c3, c5, scale, eps;
+} gpga_orthogonalize_args_t;
+int32_t gpga_orthogonalize(const gpga_orthogonalize_args_t* args, void* stream);
+int64_t gpga_orthogonalize_scratch_bytes(const gpga_orthogonalize_args_t* args);
+
 #ifdef __cplusplus
 }
 #endif

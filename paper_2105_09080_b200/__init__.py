@@ -12,7 +12,8 @@ from .binding import (  # noqa: F401
 
 def __getattr__(name):
     """The token-block operators, loaded on first use (they need torch)."""
-    if name in ("embedding_forward", "embedding_backward", "dropout", "layer_norm_forward", "layer_norm_backward"):
+    if name in ("embedding_forward", "embedding_backward", "dropout", "layer_norm_forward", "layer_norm_backward",
+                "feed_forward_forward", "feed_forward_backward", "orthogonalize", "token_status"):
         from . import token_ops
         return globals().setdefault(name, getattr(token_ops, name))
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

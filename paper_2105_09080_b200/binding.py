@@ -88,6 +88,13 @@ SIGNATURES = {
     "gpga_layer_norm_forward": (_i32, [_P, _P]),
     "gpga_layer_norm_backward": (_i32, [_P, _P]),
     "gpga_layer_norm_scratch_bytes": (_i64, [_i64, _i64, _i64]),
+    "gpga_feed_forward_forward": (_i32, [_P, _P]),
+    "gpga_feed_forward_forward_scratch_bytes": (_i64, [_P]),
+    "gpga_feed_forward_backward": (_i32, [_P, _P]),
+    "gpga_feed_forward_backward_scratch_bytes": (_i64, [_P]),
+    "gpga_orthogonalize": (_i32, [_P, _P]),
+    "gpga_orthogonalize_scratch_bytes": (_i64, [_P]),
+    "gpga_token_status": (_i32, [_P]),
 }
 
 GPGA_NOALLOC_SCRATCH_BYTES = 4 * 1024 * 1024

@@ -1,0 +1,149 @@
+// Gated feed-forward block, backward.  Five products per node and three arrays between them; see include/gpga.h.
+#include "gpga_ff_device.cuh"
+
+namespace gpga {
+
+namespace {
+
+struct BackwardPlan {
+    PackPlan pack;
+    Operand x, dy, gate, up, down, h, dgu;
+};
+
+BackwardPlan plan_backward(const FeedForwardParams& p)
+{
+    BackwardPlan q;
+    const bool f32 = p.dtype == 0, wf32 = p.weight_dtype == 0;
+    q.pack.base = p.scratch;
+    q.pack.pieces = f32 ? 3 : 1;
+    q.dy = q.pack.operand(p.dy.p, p.dy.ld, p.rows * p.dy.ld, p.rows, p.d, p.nodes, f32, false);
+    q.down = q.pack.operand(p.down.p, p.down.ld, p.down.node, p.d, p.f, p.nodes, wf32, true);
+    q.x = q.pack.operand(p.x.p, p.x.ld, p.rows * p.x.ld, p.rows, p.d, p.nodes, f32, true);
+    q.gate = q.pack.operand(p.gate.p, p.gate.ld, p.gate.node, p.f, p.d, p.nodes, wf32, true);
+    q.up = q.pack.operand(p.up.p, p.up.ld, p.up.node, p.f, p.d, p.nodes, wf32, true);
+    q.h = q.pack.written(p.rows, p.f, p.nodes, true);
+    q.dgu = q.pack.written(p.rows, p.f, 2 * p.nodes, true);   // dg of all nodes, then du
+    return q;
+}
+
+template <class T>
+cudaError_t weight_gradient(const GemmPlan& g, const FeedForwardParams& p, const Matrix& out, int64_t rows, const Matrix* second, cudaStream_t stream)
+{
+    constexpr int P = PiecesOf<T>::count;
+    if (p.grad_dtype == 0) return store_product<float>(g, out, rows, second, p.accumulate, P, stream);
+    if constexpr (P == 1) return store_product<T>(g, out, rows, second, p.accumulate, P, stream);
+    return cudaErrorInvalidValue;
+}
+
+template <class T>
+cudaError_t backward(const FeedForwardParams& p, cudaStream_t stream)
+{
+    constexpr int P = PiecesOf<T>::count;
+    using T16 = typename PiecesOf<T>::type;
+    const BackwardPlan q = plan_backward(p);
+    cudaError_t e = q.pack.launch<T16, P>(stream);
+    if (e != cudaSuccess) return e;
+    Operand dg = q.dgu, du = q.dgu;    // halves of one array
+    dg.batches = du.batches = p.nodes;
+    du.base = static_cast<const T16*>(du.base) + p.nodes * du.batch;
+
+    GemmPlan g;                         // dh = dy Wd, and from it h, dg, du
+    g.half = std::is_same<T16, __half>::value;
+    g.batch = g.bmod = p.nodes;
+    g.after = q.pack.jobs.count > 0;
+    g.a[0] = q.dy;
+    g.b[0] = q.down;
+    g.m = p.rows;
+    g.n = p.f;
+    g.k[0] = p.d;
+    GateGrad<T> grad;
+    grad.g = static_cast<const T*>(p.g.p);
+    grad.u = static_cast<const T*>(p.u.p);
+    grad.ldg = p.g.ld;
+    grad.ldu = p.u.ld;
+    grad.h = pieces_of<T16>(q.h);
+    grad.dg = pieces_of<T16>(dg);
+    grad.du = pieces_of<T16>(du);
+    grad.m = (int32_t)p.rows;
+    grad.n = (int32_t)p.f;
+    grad.kind = p.activation;
+    grad.vec = rows_on_16(p.g.p, p.g.ld, p.nodes * p.rows, 0, 1, sizeof(T)) && rows_on_16(p.u.p, p.u.ld, p.nodes * p.rows, 0, 1, sizeof(T));
+    if ((e = launch_gemm<P>(g, grad, stream)) != cudaSuccess) return e;
+
+    g.after = true;                     // dWd = dy^T h
+    g.a[0] = q.dy;
+    g.a[0].mn_major = true;
+    g.b[0] = q.h;
+    g.m = p.d;
+    g.n = p.f;
+    g.k[0] = p.rows;
+    if ((e = weight_gradient<T>(g, p, p.ddown, p.d, nullptr, stream)) != cudaSuccess) return e;
+
+    g.a[0] = q.dgu;                     // dWg = dg^T x, dWu = du^T x
+    g.b[0] = q.x;
+    g.m = p.f;
+    g.n = p.d;
+    g.batch = 2 * p.nodes;
+    if ((e = weight_gradient<T>(g, p, p.dgate, p.f, &p.dup, stream)) != cudaSuccess) return e;
+
+    g.segments = 2;                     // dx = dg Wg + du Wu, last: it may take dy's or x's place
+    g.batch = p.nodes;
+    g.a[0] = dg;
+    g.a[1] = du;
+    g.a[0].mn_major = g.a[1].mn_major = false;
+    g.b[0] = q.gate;
+    g.b[1] = q.up;
+    g.m = p.rows;
+    g.n = p.d;
+    g.k[0] = g.k[1] = p.f;
+    return store_product<T>(g, p.dx, p.nodes * p.rows, nullptr, false, P, stream);
+}
+
+template <class T>
+__global__ void zero_rows(T* p, int64_t ld, int64_t node, int64_t rows, int64_t cols, int64_t count)
+{
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < count; i += (int64_t)gridDim.x * blockDim.x) {
+        const int64_t r = i / cols, b = r / rows;
+        p[b * node + (r - b * rows) * ld + (i - r * cols)] = from_f32<T>(0.f);
+    }
+}
+
+// A sum over no tokens.
+cudaError_t no_tokens(const FeedForwardParams& p, cudaStream_t stream)
+{
+    if (p.accumulate) return cudaSuccess;
+    const Matrix* out[3] = {&p.dgate, &p.dup, &p.ddown};
+    for (int i = 0; i < 3; ++i) {
+        const int64_t rows = i == 2 ? p.d : p.f, cols = i == 2 ? p.f : p.d, count = p.nodes * rows * cols;
+        const unsigned blocks = (unsigned)std::min<int64_t>((count + 255) / 256, (int64_t)sm_count() * 8);
+        if (p.grad_dtype == 0)
+            zero_rows<<<blocks, 256, 0, stream>>>(static_cast<float*>(out[i]->p), out[i]->ld, out[i]->node, rows, cols, count);
+        else if (p.grad_dtype == 1)
+            zero_rows<<<blocks, 256, 0, stream>>>(static_cast<__nv_bfloat16*>(out[i]->p), out[i]->ld, out[i]->node, rows, cols, count);
+        else
+            zero_rows<<<blocks, 256, 0, stream>>>(static_cast<__half*>(out[i]->p), out[i]->ld, out[i]->node, rows, cols, count);
+        const cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
+}  // namespace
+
+unsigned int* ff_backward_gave_up()
+{
+    void* at = nullptr;
+    return cudaGetSymbolAddress(&at, gave_up) == cudaSuccess ? static_cast<unsigned int*>(at) : nullptr;
+}
+
+int64_t ff_backward_scratch_bytes(const FeedForwardParams& p) { return p.rows ? plan_backward(p).pack.scratch.bytes : 0; }
+
+cudaError_t launch_ff_backward(const FeedForwardParams& p, cudaStream_t stream)
+{
+    if (p.rows == 0) return no_tokens(p, stream);
+    if (p.dtype == 0) return backward<float>(p, stream);
+    if (p.dtype == 1) return backward<__nv_bfloat16>(p, stream);
+    return backward<__half>(p, stream);
+}
+
+}  // namespace gpga

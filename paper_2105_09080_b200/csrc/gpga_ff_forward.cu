@@ -1,0 +1,83 @@
+// Gated feed-forward block, forward: g = x Wg^T, u = x Wu^T, h = act(g) u, y = h Wd^T per node.  See include/gpga.h.
+#include "gpga_ff_device.cuh"
+
+namespace gpga {
+
+namespace {
+
+struct ForwardPlan {
+    PackPlan pack;
+    Operand x, gate, up, down, h;
+};
+
+ForwardPlan plan_forward(const FeedForwardParams& p)
+{
+    ForwardPlan q;
+    const bool f32 = p.dtype == 0, wf32 = p.weight_dtype == 0;
+    q.pack.base = p.scratch;
+    q.pack.pieces = f32 ? 3 : 1;
+    q.x = q.pack.operand(p.x.p, p.x.ld, p.rows * p.x.ld, p.rows, p.d, p.nodes, f32, false);
+    q.gate = q.pack.operand(p.gate.p, p.gate.ld, p.gate.node, p.f, p.d, p.nodes, wf32, false);
+    q.up = q.pack.operand(p.up.p, p.up.ld, p.up.node, p.f, p.d, p.nodes, wf32, false);
+    q.down = q.pack.operand(p.down.p, p.down.ld, p.down.node, p.d, p.f, p.nodes, wf32, false);
+    q.h = q.pack.written(p.rows, p.f, p.nodes, false);
+    return q;
+}
+
+template <class T>
+cudaError_t forward(const FeedForwardParams& p, cudaStream_t stream)
+{
+    constexpr int P = PiecesOf<T>::count;
+    using T16 = typename PiecesOf<T>::type;
+    const ForwardPlan q = plan_forward(p);
+    cudaError_t e = q.pack.launch<T16, P>(stream);
+    if (e != cudaSuccess) return e;
+    GemmPlan g;
+    g.half = std::is_same<T16, __half>::value;
+    g.batch = g.bmod = p.nodes;
+    g.after = q.pack.jobs.count > 0;
+    g.a[0] = q.x;
+    g.b[0] = q.gate;
+    g.b[1] = q.up;
+    g.m = p.rows;
+    g.n = p.f;
+    g.k[0] = p.d;
+    GateUp<T> up;
+    up.g = static_cast<T*>(p.g.p);
+    up.u = static_cast<T*>(p.u.p);
+    up.ldg = p.g.ld;
+    up.ldu = p.u.ld;
+    up.h = pieces_of<T16>(q.h);
+    up.m = (int32_t)p.rows;
+    up.n = (int32_t)p.f;
+    up.kind = p.activation;
+    up.keep = p.g.p != nullptr;
+    up.vec = !up.keep || (rows_on_16(p.g.p, p.g.ld, p.nodes * p.rows, 0, 1, sizeof(T)) && rows_on_16(p.u.p, p.u.ld, p.nodes * p.rows, 0, 1, sizeof(T)));
+    e = launch_gemm<P>(g, up, stream);
+    if (e != cudaSuccess) return e;
+    g.after = true;
+    g.a[0] = q.h;
+    g.b[0] = q.down;
+    g.n = p.d;
+    g.k[0] = p.f;
+    return store_product<T>(g, p.y, p.nodes * p.rows, nullptr, false, P, stream);
+}
+
+}  // namespace
+
+unsigned int* ff_forward_gave_up()
+{
+    void* at = nullptr;
+    return cudaGetSymbolAddress(&at, gave_up) == cudaSuccess ? static_cast<unsigned int*>(at) : nullptr;
+}
+
+int64_t ff_forward_scratch_bytes(const FeedForwardParams& p) { return p.rows ? plan_forward(p).pack.scratch.bytes : 0; }
+
+cudaError_t launch_ff_forward(const FeedForwardParams& p, cudaStream_t stream)
+{
+    if (p.dtype == 0) return forward<float>(p, stream);
+    if (p.dtype == 1) return forward<__nv_bfloat16>(p, stream);
+    return forward<__half>(p, stream);
+}
+
+}  // namespace gpga

@@ -1,0 +1,548 @@
+// Matrix products of the token-block operators: one persistent kernel for all of them, with an epilogue per use.
+//
+//     acc(i, j) = sum over k of A(i, k) B(j, k), per node ("batch"), then Epi.
+//
+// Operands are 16-bit arrays that tiled asynchronous copies bring to shared memory: rows along k, or (mn_major) rows along i
+// or j, so no operand is ever transposed in memory.  An operand may be the sum of P arrays of 16 bits ("pieces": a float32
+// value is exactly three bfloat16 values); then the products of pieces p + q < P are summed, six of them for P = 3.
+// A sum may run over two pairs of operands (segments), and a tile's columns may come from two arrays (DUAL: the left half
+// from B[0], the right half from B[1]), so that both projections of a gate end in one thread's registers.
+//
+// A tile is 128 CG rows by bn columns on CG thread blocks.  Warp 0 loads, warp 1 of the leading block issues the matrix
+// instructions, warps 4 to 11 take finished tiles out of tensor memory (two accumulators: the next tile's sums run
+// meanwhile) and through shared memory, so that their accesses to global memory are along rows.
+//
+// CHUNKED (operands in pieces): the matrix unit cuts what it adds to its fp32 accumulator off, it does not round, so that a
+// sum drifts towards zero by about 2^-26 of itself per instruction (K = 256 in 96 instructions: 1.6e-6 of the result).
+// Where the result is to be as good as fp32 gives, the large products (first pieces) and the small ones have an accumulator
+// each, the sum is cut into chunks of 128, and the epilogue's threads add the chunks' sums in registers.
+//
+// Every wait has a limit (kWaitTries); when one runs out the block notes it in `gave_up`, all of its roles wind down, and
+// gpga_token_status reports it.
+#pragma once
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <atomic>
+
+#include "gpga_launch.cuh"
+#include "gpga_token.cuh"
+#include "gpga_umma.cuh"
+
+namespace gpga {
+
+constexpr int kGemmThreads = 384;
+constexpr int kTileK = 64;                                  // columns of k in a stage: 128 bytes
+constexpr int kStageLine = 36;                              // floats per staged row: 16-byte aligned, no bank conflicts
+constexpr int kStaging = 8 * 32 * kStageLine * 4;           // bytes: 32 rows x 32 columns for each epilogue warp
+constexpr int kGemmHead = 1024;                             // barriers, before the operand stages
+constexpr int kGemmSmem = 227 * 1024;
+constexpr uint32_t kWaitTries = 1u << 20;                   // polls of up to some microseconds each: seconds
+
+static __device__ unsigned int gave_up;                     // one per file that launches products
+
+struct GemmMaps {
+    CUtensorMap a[2], b[2];
+};
+
+struct GemmParams {
+    int32_t m, n;                 // of one batch
+    int32_t kblocks0, kblocks;    // steps of kTileK of the first segment; of both
+    int32_t bmod;                 // B's batch index is batch % bmod
+    int32_t tiles_m, tiles_n, tiles;
+    int32_t bn, stages, pieces, chunk;
+    uint32_t b_bytes;             // of a piece of B per stage and block
+    uint32_t idesc;
+    int32_t a_mn, b_mn;
+};
+
+struct GemmTile {
+    int32_t batch, m0, n0;
+};
+// Tiles of a batch in columns of eight row tiles, so that tiles that run together share operands in L2.
+__device__ __forceinline__ GemmTile gemm_tile(const GemmParams& p, int t, int rows)
+{
+    const int per = p.tiles_m * p.tiles_n;
+    GemmTile g;
+    g.batch = t / per;
+    int r = t - g.batch * per;
+    const int group = r / (8 * p.tiles_n);
+    const int first = group * 8, height = min(8, p.tiles_m - first);
+    r -= first * p.tiles_n;
+    g.m0 = (first + r % height) * rows;
+    g.n0 = (r / height) * p.bn;
+    return g;
+}
+
+struct WaitState {
+    volatile uint32_t* stop;
+    __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) const
+    {
+        for (uint32_t t = 0; t < kWaitTries; ++t) {
+            if (try_wait_cluster(bar, parity)) return true;
+            if (*stop) return false;
+        }
+        *stop = 1;
+        atomicOr(&gave_up, 1u);
+        return false;
+    }
+};
+
+// Columns n0 + c .. of a row, eight (or one, where rows do not all start on 16 bytes) to a call of f(row, c, v), rows side
+// by side on the lanes.  v: the warp's 32 x 32 values, thread l holding row l.
+template <bool VEC, class F>
+__device__ __forceinline__ void along_rows(const float (&v)[32], float* stage, int lane, const F& f)
+{
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        *reinterpret_cast<float4*>(stage + lane * kStageLine + 4 * j) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+    __syncwarp();
+    if constexpr (VEC) {
+        const int c = (lane & 3) * 8;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = i * 8 + (lane >> 2);
+            const float4 a = *reinterpret_cast<const float4*>(stage + row * kStageLine + c);
+            const float4 b = *reinterpret_cast<const float4*>(stage + row * kStageLine + c + 4);
+            float w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+            f(row, c, w);
+        }
+    } else {
+#pragma unroll 4
+        for (int row = 0; row < 32; ++row) {
+            float w[1] = {stage[row * kStageLine + lane]};
+            f(row, lane, w);
+        }
+    }
+}
+
+// W = 8 (aligned) or 1 values at p, of which n lie in the row.
+template <class T, int W>
+__device__ __forceinline__ void load_values(const T* p, int n, float (&v)[W])
+{
+    if constexpr (W == 1) {
+        v[0] = n > 0 ? to_f32(*p) : 0.f;
+    } else {
+        if (n >= 8) {
+            uint32_t w[2 * sizeof(T)];
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+                const uint4 q = reinterpret_cast<const uint4*>(p)[i];
+                w[4 * i] = q.x, w[4 * i + 1] = q.y, w[4 * i + 2] = q.z, w[4 * i + 3] = q.w;
+            }
+            if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) unpack16(w[i], v[2 * i], v[2 * i + 1], T());
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = i < n ? to_f32(p[i]) : 0.f;
+        }
+    }
+}
+template <class T, int W>
+__device__ __forceinline__ void store_values(T* p, int n, const float (&v)[W])
+{
+    if constexpr (W == 1) {
+        if (n > 0) *p = from_f32<T>(v[0]);
+    } else {
+        if (n >= 8) {
+            uint32_t w[2 * sizeof(T)];
+            if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(v[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = pack16(v[2 * i], v[2 * i + 1], T());
+            }
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+                reinterpret_cast<uint4*>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < n) p[i] = from_f32<T>(v[i]);
+        }
+    }
+}
+
+// The pieces of a value.  bfloat16: the upper 16 bits, the upper 16 of the rest, and what is left of it, which has eight
+// significant bits: the sum is exact (an infinity's rest is NaN).  half: rounded, then the rounded rest: 22 bits.
+template <class T16, int P>
+__device__ __forceinline__ void split(float v, T16 (&o)[P])
+{
+    if constexpr (P == 1) {
+        o[0] = from_f32<T16>(v);
+    } else if constexpr (P == 2) {
+        o[0] = from_f32<T16>(v);
+        o[1] = from_f32<T16>(v - to_f32(o[0]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            const float h = __uint_as_float(__float_as_uint(v) & 0xFFFF0000u);
+            o[i] = from_f32<T16>(h);
+            v -= h;
+        }
+    }
+}
+// Where the pieces of an array of rows are (piece, batch, row, column; rows start on 16 bytes and are padded to eight).
+template <class T16>
+struct Pieces {
+    T16* base;
+    int64_t piece, batch, ld;
+    template <int P, int W>
+    __device__ __forceinline__ void store(int b, int row, int col, int n, const float (&v)[W]) const
+    {
+        static_assert(W == 8, "pieces are stored in chunks of eight columns");
+        T16* at = base + b * batch + row * ld + col;
+        uint32_t w[P][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            T16 lo[P], hi[P];
+            split<T16, P>(2 * i < n ? v[2 * i] : 0.f, lo);
+            split<T16, P>(2 * i + 1 < n ? v[2 * i + 1] : 0.f, hi);
+#pragma unroll
+            for (int q = 0; q < P; ++q)
+                w[q][i] = (uint32_t)*reinterpret_cast<const uint16_t*>(&lo[q]) | (uint32_t)*reinterpret_cast<const uint16_t*>(&hi[q]) << 16;
+        }
+#pragma unroll
+        for (int q = 0; q < P; ++q) *reinterpret_cast<uint4*>(at + q * piece) = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
+    }
+    template <int P>
+    __device__ __forceinline__ void load(int b, int row, int col, float (&v)[8]) const
+    {
+        const T16* at = base + b * batch + row * ld + col;
+        load_values<T16, 8>(at, 8, v);
+#pragma unroll
+        for (int q = 1; q < P; ++q) {
+            float r[8];
+            load_values<T16, 8>(at + q * piece, 8, r);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += r[i];
+        }
+    }
+};
+
+// Epi: kDual; operator()(v, w, stage, lane, batch, row0, col0): the warp's 32 rows from row0, 32 columns from col0 of the
+// product (kDual: v of the first array's columns, w of the second's).
+template <int CG, bool CHUNKED, class Epi>
+__global__ void __launch_bounds__(kGemmThreads, 1)
+    gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmParams p, const __grid_constant__ Epi epi)
+{
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    unsigned char* const smem = smem_raw + ((1024 - (raw & 1023)) & 1023);
+    const uint32_t base = smem_u32(smem);
+    // head: full[8], empty[8], acc_full[2], acc_empty[2], tensor memory address, stop flag
+    const uint32_t full = base, empty = base + 64, acc_full = base + 128, acc_empty = base + 144;
+    uint32_t* const tmem_at = reinterpret_cast<uint32_t*>(smem + 160);
+    volatile uint32_t* const stop = reinterpret_cast<volatile uint32_t*>(smem + 164);
+    float* const staging = reinterpret_cast<float*>(smem + kGemmHead);
+    const uint32_t operands = base + kGemmHead + kStaging;
+    const uint32_t a_bytes = 128 * kTileK * 2, stage_bytes = p.pieces * (a_bytes + p.b_bytes);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0;
+    const int first = blockIdx.x / CG, step = gridDim.x / CG;
+    const WaitState w{stop};
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < p.stages; ++s) {
+            mbar_init(reinterpret_cast<uint64_t*>(smem + 8 * s), CG);
+            mbar_init(reinterpret_cast<uint64_t*>(smem + 64 + 8 * s), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(reinterpret_cast<uint64_t*>(smem + 128 + 8 * i), 1);
+            mbar_init(reinterpret_cast<uint64_t*>(smem + 144 + 8 * i), 8 * CG);
+        }
+        *stop = 0;
+        mbar_init_fence();
+        prefetch_map(&maps.a[0]);
+        prefetch_map(&maps.b[0]);
+    }
+    if (warp == 2) tmem_alloc<CG>(smem_u32(tmem_at), 512);
+    tmem_fence_before();
+    __syncthreads();
+    if constexpr (CG == 2) cluster_barrier();
+    tmem_fence_after();
+    const uint32_t tmem = *tmem_at;
+    grid_launch_dependents();
+    grid_dependency_wait();
+
+    uint32_t loaded = 0;   // stages filled by this block (warp 0)
+    if (warp == 0) {
+        if (lane == 0) {
+            const uint32_t nb = p.bn / CG;
+            for (int t = first; t < p.tiles; t += step) {
+                const GemmTile g = gemm_tile(p, t, 128 * CG);
+                const int m0 = g.m0 + (int)rank * 128;
+                const int bb = g.batch % p.bmod;
+                bool ok = true;
+                for (int kb = 0; kb < p.kblocks; ++kb, ++loaded) {
+                    const uint32_t s = loaded % p.stages;
+                    if (loaded >= (uint32_t)p.stages && !(ok = w.wait(empty + 8 * s, (loaded / p.stages - 1) & 1))) break;
+                    const int seg = kb >= p.kblocks0, k0 = (kb - (seg ? p.kblocks0 : 0)) * kTileK;
+                    const uint32_t bar = CG == 2 ? map_shared(full + 8 * s, 0) : full + 8 * s;
+                    if constexpr (CG == 2)
+                        arrive_expect_cluster(bar, stage_bytes);
+                    else
+                        mbar_arrive_expect_tx(reinterpret_cast<uint64_t*>(smem + 8 * s), stage_bytes);
+                    uint32_t dst = operands + s * stage_bytes;
+                    for (int q = 0; q < p.pieces; ++q, dst += a_bytes) {
+                        if (p.a_mn) {
+                            load_box<CG>(dst, &maps.a[seg], m0, k0, g.batch, q, bar);
+                            load_box<CG>(dst + 8192, &maps.a[seg], m0 + 64, k0, g.batch, q, bar);
+                        } else {
+                            load_box<CG>(dst, &maps.a[seg], k0, m0, g.batch, q, bar);
+                        }
+                    }
+                    for (int q = 0; q < p.pieces; ++q, dst += p.b_bytes) {
+                        if constexpr (Epi::kDual) {   // bn / 2 columns of each array
+                            const int n0 = g.n0 / 2;
+                            if constexpr (CG == 2) {
+                                load_box<CG>(dst, &maps.b[rank], k0, n0, bb, q, bar);
+                            } else {
+                                load_box<CG>(dst, &maps.b[0], k0, n0, bb, q, bar);
+                                load_box<CG>(dst + p.b_bytes / 2, &maps.b[1], k0, n0, bb, q, bar);
+                            }
+                        } else if (p.b_mn) {
+                            const int n0 = g.n0 + (int)(rank * nb);
+                            for (uint32_t c = 0; c < nb; c += 64) load_box<CG>(dst + c * 128, &maps.b[seg], n0 + (int)c, k0, bb, q, bar);
+                        } else {
+                            load_box<CG>(dst, &maps.b[seg], k0, g.n0 + (int)(rank * nb), bb, q, bar);
+                        }
+                    }
+                }
+                if (!ok) break;
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (rank == 0 && lane == 0) {
+            const uint64_t a_step = p.a_mn ? 2048 >> 4 : 32 >> 4, b_step = p.b_mn ? 2048 >> 4 : 32 >> 4;
+            uint32_t used = 0, sums = 0;   // stages; accumulators
+            bool ok = true;
+            for (int t = first; t < p.tiles && ok; t += step) {
+                for (int k0 = 0; k0 < p.kblocks && ok; k0 += p.chunk, ++sums) {
+                    const uint32_t buf = sums & 1;
+                    if (sums >= 2 && !(ok = w.wait(acc_empty + 8 * buf, (sums / 2 - 1) & 1))) break;
+                    tmem_fence_after();
+                    const uint32_t d = tmem + buf * 256;
+                    const int k1 = min(k0 + p.chunk, p.kblocks);
+                    uint32_t add[2] = {0, 0};
+                    for (int kb = k0; kb < k1; ++kb, ++used) {
+                        const uint32_t s = used % p.stages;
+                        if (!(ok = w.wait(full + 8 * s, (used / p.stages) & 1))) break;
+                        tmem_fence_after();
+                        const uint32_t at = operands + s * stage_bytes;
+                        const uint64_t a0 = tile_descriptor(at, p.a_mn);
+                        const uint64_t b0 = tile_descriptor(at + p.pieces * a_bytes, p.b_mn);
+                        for (int q = 0; q < p.pieces; ++q)
+                            for (int r = 0; q + r < p.pieces; ++r) {
+                                const uint64_t a = a0 + q * (a_bytes >> 4), b = b0 + r * (p.b_bytes >> 4);
+                                const int low = CHUNKED && q + r > 0;
+                                uint32_t go_on = add[low];
+#pragma unroll
+                                for (int k = 0; k < kTileK / 16; ++k) {
+                                    mma_f16<CG>(d + low * 128, a + k * a_step, b + k * b_step, p.idesc, go_on);
+                                    go_on = 1;
+                                }
+                                add[low] = 1;
+                            }
+                        mma_commit<CG>(empty + 8 * s);
+                    }
+                    if (!ok) break;
+                    mma_commit<CG>(acc_full + 8 * buf);
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp >= 4) {
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        float* const stage = staging + (warp - 4) * 32 * kStageLine;
+        const uint32_t release = CG == 2 ? map_shared(acc_empty, 0) : acc_empty;
+        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
+        uint32_t sums = 0;
+        bool ok = true;
+        for (int t = first; t < p.tiles && ok; t += step) {
+            const GemmTile g = gemm_tile(p, t, 128 * CG);
+            const int row0 = g.m0 + (int)rank * 128 + quarter * 32;
+            if constexpr (CHUNKED) {   // bn = 128: 64 columns to a warp
+                float acc[64];
+#pragma unroll
+                for (int i = 0; i < 64; ++i) acc[i] = 0.f;
+                for (int k0 = 0; k0 < p.kblocks; k0 += p.chunk, ++sums) {
+                    const uint32_t buf = sums & 1;
+                    ok = __all_sync(~0u, w.wait(acc_full + 8 * buf, (sums / 2) & 1));
+                    if (!ok) break;
+                    tmem_fence_after();
+                    const uint32_t at = lanes + buf * 256 + half * (Epi::kDual ? 32 : 64);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        float a[32], b[32];
+                        tmem_load32(at + j * (Epi::kDual ? 64 : 32), a);
+                        tmem_load32(at + j * (Epi::kDual ? 64 : 32) + 128, b);
+                        tmem_wait_load();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) acc[32 * j + i] += a[i] + b[i];
+                    }
+                    tmem_fence_before();
+                    __syncwarp();
+                    if (lane == 0) arrive_cluster(release + 8 * buf);
+                }
+                if (!ok) break;
+                if (row0 < p.m) {
+                    float a[32], b[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) a[i] = acc[i], b[i] = acc[32 + i];
+                    if constexpr (Epi::kDual) {
+                        const int col0 = g.n0 / 2 + half * 32;
+                        if (col0 < p.n) epi(a, b, stage, lane, g.batch, row0, col0);
+                    } else {
+                        const int col0 = g.n0 + half * 64;
+                        if (col0 < p.n) epi(a, a, stage, lane, g.batch, row0, col0);
+                        if (col0 + 32 < p.n) epi(b, b, stage, lane, g.batch, row0, col0 + 32);
+                    }
+                }
+            } else {
+                const uint32_t buf = sums & 1;
+                ok = __all_sync(~0u, w.wait(acc_full + 8 * buf, (sums / 2) & 1));
+                if (!ok) break;
+                ++sums;
+                tmem_fence_after();
+                const int width = p.bn / (Epi::kDual ? 4 : 2);   // columns of this warp
+                for (int c = 0; c < width; c += 32) {
+                    float a[32], b[32];
+                    const uint32_t at = lanes + buf * 256 + half * width + c;
+                    tmem_load32(at, a);
+                    if constexpr (Epi::kDual) tmem_load32(at + p.bn / 2, b);
+                    tmem_wait_load();
+                    if (c + 32 >= width) {
+                        tmem_fence_before();
+                        __syncwarp();
+                        if (lane == 0) arrive_cluster(release + 8 * buf);
+                    }
+                    const int col0 = (Epi::kDual ? g.n0 / 2 : g.n0) + half * width + c;
+                    if (row0 < p.m && col0 < p.n) {
+                        if constexpr (Epi::kDual)
+                            epi(a, b, stage, lane, g.batch, row0, col0);
+                        else
+                            epi(a, a, stage, lane, g.batch, row0, col0);
+                    }
+                }
+            }
+        }
+    }
+
+    // Everybody is done, or has given up; copies in flight must land before the block goes.
+    tmem_fence_before();
+    __syncthreads();
+    if (*stop && threadIdx.x == 0)
+        for (uint32_t i = loaded > (uint32_t)p.stages ? loaded - p.stages : 0; i < loaded; ++i)
+            for (uint32_t tries = 0; tries < 4096 && !try_wait_cluster(full + 8 * (i % p.stages), (i / p.stages) & 1); ++tries) {
+            }
+    __syncthreads();
+    if constexpr (CG == 2) cluster_barrier();
+    if (warp == 2) {
+        tmem_fence_after();
+        tmem_free<CG>(tmem, 512);
+    }
+}
+
+// ---- host side ----
+
+// A 16-bit array: `outer` rows of `inner` values, batches and pieces of them (strides in elements, multiples of eight).
+struct Operand {
+    const void* base = nullptr;
+    int64_t inner = 0, outer = 0, batches = 1, pieces = 1;
+    int64_t ld = 0, batch = 0, piece = 0;
+    bool mn_major = false;   // rows run along the product's row (column) index
+};
+
+bool operand_fits(const void* base, int64_t ld, int64_t batch);   // whether a tiled copy can read it where it lies
+
+// The driver's encoder of tensor maps, looked up once.
+cudaError_t encode_map(CUtensorMap& map, const Operand& o, bool half, int box_rows);
+
+struct GemmPlan {
+    Operand a[2], b[2];
+    int segments = 1;
+    int64_t m = 0, n = 0, k[2] = {0, 0}, batch = 1, bmod = 1;
+    bool half = false;   // fp16 operands (otherwise bfloat16)
+    bool after = false;  // the kernel before it on the stream is one of the same call
+};
+
+int sm_count();
+
+template <int CG, bool CHUNKED, class Epi>
+cudaError_t launch_gemm_as(const GemmPlan& g, int bn, const Epi& epi, cudaStream_t stream)
+{
+    GemmParams p;
+    GemmMaps maps;
+    const int pieces = (int)g.a[0].pieces;
+    p.m = (int32_t)g.m;
+    p.n = (int32_t)g.n;
+    p.kblocks0 = (int32_t)((g.k[0] + kTileK - 1) / kTileK);
+    p.kblocks = p.kblocks0 + (g.segments > 1 ? (int32_t)((g.k[1] + kTileK - 1) / kTileK) : 0);
+    p.bmod = (int32_t)g.bmod;
+    p.tiles_m = (int32_t)((g.m + 128 * CG - 1) / (128 * CG));
+    const int columns = Epi::kDual ? bn / 2 : bn;
+    p.tiles_n = (int32_t)((g.n + columns - 1) / columns);
+    const int64_t tiles = g.batch * p.tiles_m * p.tiles_n;
+    if (tiles >= (int64_t(1) << 31) - 65536) return cudaErrorInvalidValue;
+    p.tiles = (int32_t)tiles;
+    p.bn = bn;
+    p.pieces = pieces;
+    p.b_bytes = (uint32_t)(bn / CG * kTileK * 2);
+    const int stage_bytes = pieces * (128 * kTileK * 2 + (int)p.b_bytes);
+    p.stages = std::min(8, (kGemmSmem - 1024 - kGemmHead - kStaging) / stage_bytes);
+    p.chunk = CHUNKED ? 2 : p.kblocks;
+    p.a_mn = g.a[0].mn_major;
+    p.b_mn = g.b[0].mn_major;
+    p.idesc = 1u << 4 | (g.half ? 0u : 1u << 7 | 1u << 10) | (uint32_t)p.a_mn << 15 | (uint32_t)p.b_mn << 16 | (uint32_t)(bn >> 3) << 17 |
+              (uint32_t)(128 * CG >> 4) << 24;
+    const int b_rows = p.b_mn ? 64 : Epi::kDual ? bn / 2 : bn / CG;
+    for (int i = 0; i < 2; ++i) {
+        const bool b_there = i == 0 || g.segments > 1 || Epi::kDual;
+        cudaError_t e = encode_map(maps.a[i], g.a[i < g.segments ? i : 0], g.half, p.a_mn ? 64 : 128);
+        if (e == cudaSuccess) e = encode_map(maps.b[i], g.b[b_there ? i : 0], g.half, b_rows);
+        if (e != cudaSuccess) return e;
+    }
+    const auto kernel = gemm_kernel<CG, CHUNKED, Epi>;
+    static std::atomic<unsigned long long> limit_set{0};
+    const cudaError_t e = ensure_smem_limit(kernel, kGemmSmem, limit_set);
+    if (e != cudaSuccess) return e;
+    const int64_t blocks = std::min<int64_t>(tiles, sm_count() / CG) * CG;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3(kGemmThreads);
+    cfg.dynamicSmemBytes = kGemmSmem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    int n = 0;
+    if (CG == 2) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = 2;
+        attr[n].val.clusterDim.y = 1;
+        attr[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    if (g.after) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n].val.programmaticStreamSerializationAllowed = 1;
+        ++n;
+    }
+    cfg.attrs = attr;
+    cfg.numAttrs = n;
+    return cudaLaunchKernelEx(&cfg, kernel, maps, p, epi);
+}
+
+}  // namespace gpga

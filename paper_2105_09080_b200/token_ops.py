@@ -1,5 +1,6 @@
 """Token-block operators on torch CUDA tensors: embedding lookup and its gradient, dropout from the library's
-counter-based generator, layer norm (with the residual sum and the dropout in front of it) and its gradient.
+counter-based generator, layer norm (with the residual sum and the dropout in front of it) and its gradient, the gated
+feed-forward block and its gradient, and the orthogonalisation of an update by Newton-Schulz products.
 
 Argument marshalling only, as in ``binding``: every operator is one C entry of include/gpga.h, which has the formulas.
 They work node by node.  Parameters and their gradients are float32 and may be slices of the state matrix X (n, ld) and
@@ -38,7 +39,11 @@ ARGS = {
     "gpga_dropout": struct.Struct("=2Q6qdQ3q"),
     "gpga_layer_norm_forward": struct.Struct("=8Q9q2dQ3q"),
     "gpga_layer_norm_backward": struct.Struct("=11Q13qdQ3q"),
+    "gpga_feed_forward_forward": struct.Struct("=8Q18q"),
+    "gpga_feed_forward_backward": struct.Struct("=12Q27q"),
+    "gpga_orthogonalize": struct.Struct("=3Q11q5d"),
 }
+ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
 
 _current_device = torch._C._cuda_getDevice
 _raw_stream = torch._C._cuda_getCurrentRawStream
@@ -334,3 +339,171 @@ def layer_norm_backward(dy, z, mean, rstd, weight, dz=None, p=0.0, seed=0, k=0, 
                                        _same(dresidual, "dresidual", shape, dtype, device, d), ldx, lddw, accumulate, code,
                                        nodes, rows, d, p, seed, k, site, node0)
     return dresidual, (dresidual if dx is None else dx), dweight, dbias
+
+
+def _matrix(t, what, dtypes, device, nodes=None, rows=None, cols=None):
+    """(nodes, rows, cols, row stride, node stride) of a matrix (rows, cols) or (nodes, rows, cols) of one of ``dtypes``."""
+    shape = t.shape
+    if t.dtype not in dtypes or len(shape) not in (2, 3) or t.get_device() != device or device < 0:
+        _bad(f"{what} must be a matrix or one per node, of {' or '.join(map(str, dtypes))}, on cuda:{device}, got {tuple(shape)} {t.dtype} on {t.device}")
+    r, c = shape[-2:]
+    n = shape[0] if len(shape) == 3 else 1
+    if (nodes is not None and n != nodes) or (rows is not None and r != rows) or (cols is not None and c != cols) or not n * r * c:
+        _bad(f"{what}: got {tuple(shape)}, want {(nodes, rows, cols) if nodes is not None else 'no empty dimension'}")
+    if t.is_contiguous():
+        return n, r, c, c, r * c
+    stride = t.stride()
+    if stride[-1] != 1 and c > 1:
+        _bad(f"{what}: rows must be dense, got strides {stride}")
+    ld = stride[-2] if r > 1 else c
+    return n, r, c, ld, stride[0] if n > 1 else r * ld
+
+
+@functools.lru_cache(maxsize=None)
+def _scratch_entry(name):
+    fn, pack = getattr(lib(), name + "_scratch_bytes"), ARGS[name].pack
+
+    def need(pointers, *members):
+        try:
+            return fn(pack(*pointers, 0, 0, *members))
+        except struct.error as e:
+            _bad(f"argument out of range: {e}")
+    return need
+
+
+def _run_with_scratch(name, device, like, scratch, pointers, members):
+    """Calls an entry whose struct is pointers, scratch, scratch bytes, members."""
+    need = _scratch_entry(name)(pointers, *members)
+    scratch, scratch_p, scratch_bytes = _scratch(scratch, need, like, device)
+    _entry(name)(device, *pointers, scratch_p, scratch_bytes, *members)
+
+
+def _activation(name):
+    if name not in ACTIVATIONS:
+        _bad(f"activation must be one of {', '.join(ACTIVATIONS)}, got {name!r}")
+    return ACTIVATIONS[name]
+
+
+def _weights(x, gate, up, down):
+    """Checks of a block's input and weights: (shape, type, its code, device, d, nodes, rows, f, weight type, strides)."""
+    dtype = x.dtype
+    wtype = gate.dtype
+    if wtype is not torch.float32 and wtype is not dtype:
+        _bad(f"weights must be float32 or of the activations' type, got {wtype} beside {dtype}")
+    device = x.get_device()
+    nodes, f, d, ldgate, node_gate = _matrix(gate, "gate", (wtype,), device)
+    shape, dtype, code, device, dx, rows = _vectors(x, nodes)
+    if dx != d:
+        _bad(f"x has vectors of {dx} values, gate rows of {d}")
+    _, _, _, ldup, node_up = _matrix(up, "up", (wtype,), device, nodes, f, d)
+    _, _, _, lddown, node_down = _matrix(down, "down", (wtype,), device, nodes, d, f)
+    return shape, dtype, code, device, d, nodes, rows, f, _DTYPE[wtype], (ldgate, node_gate, ldup, node_up, lddown, node_down)
+
+
+def feed_forward_forward(x, gate, up, down, activation="silu", out=None, g=None, u=None, keep=True, scratch=None, stream=None):
+    """Gated feed-forward block (gpga_feed_forward_forward): g = x gate^T, u = x up^T, y = (act(g) u) down^T; returns (y, g, u).
+
+    ``x`` (..., d); ``gate`` and ``up`` (f, d), ``down`` (d, f), or (nodes, f, d) and (nodes, d, f): float32, or of x's type.
+    ``activation``: "silu", "gelu" (with erf) or "relu".  g and u (..., f) are what the backward call wants; with ``keep=False``
+    they are not stored, and None comes back in their place.  ``out`` may be ``x``.
+    """
+    if stream is not None:
+        return _on_stream(feed_forward_forward, locals())
+    shape, dtype, code, device, d, nodes, rows, f, wcode, strides = _weights(x, gate, up, down)
+    kind = _activation(activation)
+    if out is None:
+        out = _like(x)
+    gp = up_p = 0
+    ldg = ldu = f
+    if keep:
+        wide = shape[:-1] + (f,)
+        if g is None:
+            g = x.new_empty(wide)
+        if u is None:
+            u = x.new_empty(wide)
+        gp, ldg = g.data_ptr(), _same(g, "g", wide, dtype, device, f)
+        up_p, ldu = u.data_ptr(), _same(u, "u", wide, dtype, device, f)
+    elif g is not None or u is not None:
+        _bad("keep=False takes neither g nor u")
+    ldy = _same(out, "out", shape, dtype, device, d)
+    if not rows:
+        return out, g, u
+    _run_with_scratch("gpga_feed_forward_forward", device, x, scratch,
+                      (x.data_ptr(), gate.data_ptr(), up.data_ptr(), down.data_ptr(), out.data_ptr(), gp, up_p),
+                      (d if x.is_contiguous() else _spacing(x), *strides, ldy, ldg, ldu, code, wcode, kind, nodes, rows, d, f))
+    return out, g, u
+
+
+def feed_forward_backward(dy, x, g, u, gate, up, down, activation="silu", dx=None, dgate=None, dup=None, ddown=None, accumulate=False,
+                          scratch=None, stream=None):
+    """Gradient of ``feed_forward_forward`` (gpga_feed_forward_backward): returns (dx, dgate, dup, ddown).
+
+    g and u as the forward call kept them.  The weights' gradients are of the weights' type unless tensors are given (float32
+    or the activations' type, all three alike); with ``accumulate``, which wants all three, they are added to.  ``dx`` may be
+    ``dy`` or ``x``.
+    """
+    if stream is not None:
+        return _on_stream(feed_forward_backward, locals())
+    shape, dtype, code, device, d, nodes, rows, f, wcode, strides = _weights(x, gate, up, down)
+    kind = _activation(activation)
+    if accumulate and (dgate is None or dup is None or ddown is None):
+        _bad("accumulate wants dgate, dup and ddown")
+    if dx is None:
+        dx = _like(x)
+    given = next((t.dtype for t in (dgate, dup, ddown) if t is not None), gate.dtype)
+    if given is not torch.float32 and given is not dtype:
+        _bad(f"the weights' gradients must be float32 or of the activations' type, got {given} beside {dtype}")
+    if dgate is None:
+        dgate = gate.new_empty(gate.shape, dtype=given)
+    if dup is None:
+        dup = up.new_empty(up.shape, dtype=given)
+    if ddown is None:
+        ddown = down.new_empty(down.shape, dtype=given)
+    lds = (*_matrix(dgate, "dgate", (given,), device, nodes, f, d)[3:], *_matrix(dup, "dup", (given,), device, nodes, f, d)[3:],
+           *_matrix(ddown, "ddown", (given,), device, nodes, d, f)[3:])
+    wide = shape[:-1] + (f,)
+    members = (_same(dy, "dy", shape, dtype, device, d), d if x.is_contiguous() else _spacing(x), _same(g, "g", wide, dtype, device, f),
+               _same(u, "u", wide, dtype, device, f), *strides, _same(dx, "dx", shape, dtype, device, d), *lds, code, wcode, _DTYPE[given],
+               int(accumulate), kind, nodes, rows, d, f)
+    _run_with_scratch("gpga_feed_forward_backward", device, x, scratch,
+                      (dy.data_ptr(), x.data_ptr(), g.data_ptr(), u.data_ptr(), gate.data_ptr(), up.data_ptr(), down.data_ptr(),
+                       dx.data_ptr(), dgate.data_ptr(), dup.data_ptr(), ddown.data_ptr()), members)
+    return dx, dgate, dup, ddown
+
+
+def orthogonalize(update, steps=5, coefficients=(3.4445, -4.7750, 2.0315), scale=1.0, eps=1e-7, out=None, accumulate=False,
+                  scratch=None, stream=None):
+    """Orthogonalised update by Newton-Schulz products (gpga_orthogonalize): returns out = scale X, X from ``steps`` times
+    X <- a X + (b A + c A A) X with A = X X^T, started at X = update / (norm + eps).
+
+    ``update``: (r, c) or one matrix per node (nodes, r, c), float32, bfloat16 or float16.  ``out`` may be ``update``; with
+    ``accumulate`` scale X is added to what ``out`` holds (out = X's slice, scale = -gamma: the local update in one call).
+    """
+    if stream is not None:
+        return _on_stream(orthogonalize, locals())
+    device = update.get_device()
+    code = _DTYPE.get(update.dtype)
+    if code is None:
+        _bad(f"update must be float32, bfloat16 or float16, got {update.dtype}")
+    nodes, r, c, ldm, node_ldm = _matrix(update, "update", (update.dtype,), device)
+    if accumulate and out is None:
+        _bad("accumulate wants out")
+    if out is None:
+        out = _like(update)
+    if out.dim() != update.dim():
+        _bad(f"out: got {tuple(out.shape)}, want {tuple(update.shape)}")
+    ldo, node_ldo = _matrix(out, "out", (update.dtype,), device, nodes, r, c)[3:]
+    if len(coefficients) != 3:
+        _bad("three coefficients are wanted")
+    _run_with_scratch("gpga_orthogonalize", device, update, scratch, (update.data_ptr(), out.data_ptr()),
+                      (ldm, node_ldm, ldo, node_ldo, code, nodes, r, c, steps, int(accumulate), *coefficients, scale, eps))
+    return out
+
+
+def token_status(stream=None):
+    """Waits for ``stream`` (default: the current one) and raises GpgaError where a bounded wait inside a matrix operator has
+    given up on the current device (gpga_token_status)."""
+    s = torch.cuda.current_stream().cuda_stream if stream is None else stream if isinstance(stream, int) else stream.cuda_stream
+    st = lib().gpga_token_status(s)
+    if st != GPGA_OK:
+        raise GpgaError(st, lib().gpga_last_error(None).decode())
