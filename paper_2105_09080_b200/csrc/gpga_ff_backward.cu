@@ -30,8 +30,8 @@ template <class T>
 cudaError_t weight_gradient(const GemmPlan& g, const FeedForwardParams& p, const Matrix& out, int64_t rows, const Matrix* second, cudaStream_t stream)
 {
     constexpr int P = PiecesOf<T>::count;
-    if (p.grad_dtype == 0) return store_product<float>(g, out, rows, second, p.accumulate, P, stream);
-    if constexpr (P == 1) return store_product<T>(g, out, rows, second, p.accumulate, P, stream);
+    if (p.grad_dtype == 0) return store_product<float, P>(g, out, rows, second, p.accumulate, stream);
+    if constexpr (P == 1) return store_product<T, P>(g, out, rows, second, p.accumulate, stream);
     return cudaErrorInvalidValue;
 }
 
@@ -96,7 +96,7 @@ cudaError_t backward(const FeedForwardParams& p, cudaStream_t stream)
     g.m = p.rows;
     g.n = p.d;
     g.k[0] = g.k[1] = p.f;
-    return store_product<T>(g, p.dx, p.nodes * p.rows, nullptr, false, P, stream);
+    return store_product<T, P>(g, p.dx, p.nodes * p.rows, nullptr, false, stream);
 }
 
 template <class T>

@@ -44,19 +44,22 @@ struct GateUp {
     static constexpr bool kDual = true;
     using T16 = typename PiecesOf<T>::type;
     static constexpr int P = PiecesOf<T>::count;
+    using Ahead = NothingAhead;
     T *g, *u;
     int64_t ldg, ldu;
     Pieces<T16> h;
     int32_t m, n, kind, keep, vec;
 
+    __device__ __forceinline__ void load(Ahead&, int, int, int, int) const {}
+
     template <bool VEC>
     __device__ __forceinline__ void keep_values(const float (&v)[32], T* to, int64_t ld, float* stage, int lane, int batch, int row0, int col0) const
     {
-        along_rows<VEC>(v, stage, lane, [&](int row, int c, auto& x) {
+        along_rows<VEC>(v, stage, lane, [&](int, int row, int c, auto& x) {
             if (row0 + row < m && col0 + c < n) store_values(to + ((int64_t)batch * m + row0 + row) * ld + col0 + c, n - col0 - c, x);
         });
     }
-    __device__ __forceinline__ void operator()(float (&v)[32], float (&w)[32], float* stage, int lane, int batch, int row0, int col0) const
+    __device__ __forceinline__ void operator()(float (&v)[32], float (&w)[32], const Ahead&, float* stage, int lane, int batch, int row0, int col0) const
     {
         if (keep) {
             if (vec) {
@@ -69,7 +72,7 @@ struct GateUp {
         }
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] = act_value<sizeof(T) == 2>(v[i], kind) * w[i];
-        along_rows<true>(v, stage, lane, [&](int row, int c, auto& x) {
+        along_rows<true>(v, stage, lane, [&](int, int row, int c, auto& x) {
             if (row0 + row < m && col0 + c < n) h.template store<P>(batch, row0 + row, col0 + c, n - col0 - c, x);
         });
     }
@@ -81,30 +84,31 @@ struct GateGrad {
     static constexpr bool kDual = false;
     using T16 = typename PiecesOf<T>::type;
     static constexpr int P = PiecesOf<T>::count;
+    struct Ahead {
+        Raw<T> g[4], u[4];
+    };
     const T *g, *u;
     int64_t ldg, ldu;
     Pieces<T16> h, dg, du;
     int32_t m, n, kind, vec;
 
-    __device__ __forceinline__ void operator()(float (&v)[32], float (&)[32], float* stage, int lane, int batch, int row0, int col0) const
+    __device__ __forceinline__ void load(Ahead& ahead, int lane, int batch, int row0, int col0) const
     {
-        along_rows<true>(v, stage, lane, [&](int row, int c, auto& dh) {
+        ahead_of_rows(lane, [&](int i, int row, int c) {
+            const int left = row0 + row < m ? n - col0 - c : 0;
+            const int64_t at = (int64_t)batch * m + row0 + row;
+            ahead.g[i].load(g + at * ldg + col0 + c, left, vec);
+            ahead.u[i].load(u + at * ldu + col0 + c, left, vec);
+        });
+    }
+    __device__ __forceinline__ void operator()(float (&v)[32], float (&)[32], const Ahead& ahead, float* stage, int lane, int batch, int row0, int col0) const
+    {
+        along_rows<true>(v, stage, lane, [&](int j, int row, int c, auto& dh) {
             const int left = n - col0 - c;
             if (row0 + row >= m || left <= 0) return;
-            const int64_t at = (int64_t)batch * m + row0 + row;
             float gv[8], uv[8];
-            const T* pg = g + at * ldg + col0 + c;
-            const T* pu = u + at * ldu + col0 + c;
-            if (vec) {
-                load_values<T, 8>(pg, left, gv);
-                load_values<T, 8>(pu, left, uv);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    gv[i] = i < left ? to_f32(pg[i]) : 0.f;
-                    uv[i] = i < left ? to_f32(pu[i]) : 0.f;
-                }
-            }
+            ahead.g[j].values(gv);
+            ahead.u[j].values(uv);
             float hv[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -125,31 +129,19 @@ struct GateGrad {
 template <class T>
 struct StoreRows {
     static constexpr bool kDual = false;
+    using Ahead = NothingAhead;
     T* out[2];
     int64_t ld[2], node[2];
     int32_t m, n, split, accumulate, vec;
 
+    __device__ __forceinline__ void load(Ahead&, int, int, int, int) const {}
     template <bool VEC>
     __device__ __forceinline__ void rows(const float (&v)[32], float* stage, int lane, int batch, int row0, int col0) const
     {
         const int which = batch >= split;
-        T* const base = out[which] + (batch - which * split) * node[which];
-        const int64_t stride = ld[which];
-        along_rows<VEC>(v, stage, lane, [&](int row, int c, auto& x) {
-            const int left = n - col0 - c;
-            if (row0 + row >= m || left <= 0) return;
-            T* const at = base + (row0 + row) * stride + col0 + c;
-            if (accumulate) {
-                constexpr int W = sizeof(x) / sizeof(float);
-                float old[W];
-                load_values(at, left, old);
-#pragma unroll
-                for (int i = 0; i < W; ++i) x[i] += old[i];
-            }
-            store_values(at, left, x);
-        });
+        store_rows<VEC>(v, out[which] + (batch - which * split) * node[which], ld[which], 1.f, accumulate, m, n, stage, lane, row0, col0);
     }
-    __device__ __forceinline__ void operator()(float (&v)[32], float (&)[32], float* stage, int lane, int batch, int row0, int col0) const
+    __device__ __forceinline__ void operator()(float (&v)[32], float (&)[32], const Ahead&, float* stage, int lane, int batch, int row0, int col0) const
     {
         if (vec)
             rows<true>(v, stage, lane, batch, row0, col0);
@@ -167,13 +159,12 @@ inline bool rows_on_16(const void* p, int64_t ld, int64_t rows, int64_t node, in
 template <int P, class Epi>
 cudaError_t launch_gemm(const GemmPlan& g, const Epi& epi, cudaStream_t stream)
 {
-    constexpr bool chunked = P > 1;
-    if (g.m <= 128) return launch_gemm_as<1, chunked>(g, 128, epi, stream);
-    return launch_gemm_as<2, chunked>(g, chunked ? 128 : 256, epi, stream);
+    if (g.m <= 128) return launch_gemm_as<Variant<1, 128, P>>(g, epi, stream);
+    return launch_gemm_as<Variant<2, 256, P>>(g, epi, stream);
 }
 
-template <class T>
-cudaError_t store_product(const GemmPlan& g, const Matrix& out, int64_t rows, const Matrix* second, bool accumulate, int pieces, cudaStream_t stream)
+template <class T, int P>
+cudaError_t store_product(const GemmPlan& g, const Matrix& out, int64_t rows, const Matrix* second, bool accumulate, cudaStream_t stream)
 {
     StoreRows<T> e;
     const Matrix& o2 = second ? *second : out;
@@ -188,7 +179,7 @@ cudaError_t store_product(const GemmPlan& g, const Matrix& out, int64_t rows, co
     e.split = (int32_t)(second ? g.batch / 2 : g.batch);
     e.accumulate = accumulate;
     e.vec = rows_on_16(out.p, out.ld, rows, out.node, g.batch, sizeof(T)) && rows_on_16(o2.p, o2.ld, rows, o2.node, g.batch, sizeof(T));
-    return pieces == 1 ? launch_gemm<1>(g, e, stream) : launch_gemm<3>(g, e, stream);
+    return launch_gemm<P>(g, e, stream);
 }
 
 }  // namespace gpga

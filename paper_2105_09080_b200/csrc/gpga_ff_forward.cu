@@ -60,7 +60,7 @@ cudaError_t forward(const FeedForwardParams& p, cudaStream_t stream)
     g.b[0] = q.down;
     g.n = p.d;
     g.k[0] = p.f;
-    return store_product<T>(g, p.y, p.nodes * p.rows, nullptr, false, P, stream);
+    return store_product<T, P>(g, p.y, p.nodes * p.rows, nullptr, false, stream);
 }
 
 }  // namespace

@@ -10,12 +10,13 @@
 //
 // A tile is 128 CG rows by bn columns on CG thread blocks.  Warp 0 loads, warp 1 of the leading block issues the matrix
 // instructions, warps 4 to 11 take finished tiles out of tensor memory (two accumulators: the next tile's sums run
-// meanwhile) and through shared memory, so that their accesses to global memory are along rows.
+// meanwhile) and through shared memory, so that their accesses to global memory are along rows.  Operands pass through a
+// ring of stages, each one piece of A and one of B, 64 deep in k.
 //
-// CHUNKED (operands in pieces): the matrix unit cuts what it adds to its fp32 accumulator off, it does not round, so that a
-// sum drifts towards zero by about 2^-26 of itself per instruction (K = 256 in 96 instructions: 1.6e-6 of the result).
-// Where the result is to be as good as fp32 gives, the large products (first pieces) and the small ones have an accumulator
-// each, the sum is cut into chunks of 128, and the epilogue's threads add the chunks' sums in registers.
+// CHUNKED (operands in pieces, P > 1): the matrix unit cuts what it adds to its fp32 accumulator off, it does not round, so
+// that a sum drifts towards zero by about 2^-26 of itself per instruction (K = 256 in 96 instructions: 1.6e-6 of the
+// result).  Where the result is to be as good as fp32 gives, the sum is cut into chunks of 64 or 128, the small products of
+// a chunk come first, and the epilogue's threads, which then have most of the block's registers, add the chunks' sums.
 //
 // Every wait has a limit (kWaitTries); when one runs out the block notes it in `gave_up`, all of its roles wind down, and
 // gpga_token_status reports it.
@@ -37,8 +38,7 @@ namespace gpga {
 
 constexpr int kGemmThreads = 384;
 constexpr int kTileK = 64;                                  // columns of k in a stage: 128 bytes
-constexpr int kStageLine = 36;                              // floats per staged row: 16-byte aligned, no bank conflicts
-constexpr int kStaging = 8 * 32 * kStageLine * 4;           // bytes: 32 rows x 32 columns for each epilogue warp
+constexpr int kStaging = 8 * 32 * 32 * 4;                   // bytes: 32 rows x 32 columns for each epilogue warp
 constexpr int kGemmHead = 1024;                             // barriers, before the operand stages
 constexpr int kGemmSmem = 227 * 1024;
 constexpr uint32_t kWaitTries = 1u << 20;                   // polls of up to some microseconds each: seconds
@@ -54,8 +54,6 @@ struct GemmParams {
     int32_t kblocks0, kblocks;    // steps of kTileK of the first segment; of both
     int32_t bmod;                 // B's batch index is batch % bmod
     int32_t tiles_m, tiles_n, tiles;
-    int32_t bn, stages, pieces, chunk;
-    uint32_t b_bytes;             // of a piece of B per stage and block
     uint32_t idesc;
     int32_t a_mn, b_mn;
 };
@@ -64,7 +62,7 @@ struct GemmTile {
     int32_t batch, m0, n0;
 };
 // Tiles of a batch in columns of eight row tiles, so that tiles that run together share operands in L2.
-__device__ __forceinline__ GemmTile gemm_tile(const GemmParams& p, int t, int rows)
+__device__ __forceinline__ GemmTile gemm_tile(const GemmParams& p, int t, int rows, int columns)
 {
     const int per = p.tiles_m * p.tiles_n;
     GemmTile g;
@@ -74,16 +72,26 @@ __device__ __forceinline__ GemmTile gemm_tile(const GemmParams& p, int t, int ro
     const int first = group * 8, height = min(8, p.tiles_m - first);
     r -= first * p.tiles_n;
     g.m0 = (first + r % height) * rows;
-    g.n0 = (r / height) * p.bn;
+    g.n0 = (r / height) * columns;
     return g;
 }
+
+// A place in a ring of N stages and the parity of its current round.
+template <uint32_t N>
+struct Ring {
+    uint32_t at = 0, parity = 0;
+    __device__ __forceinline__ void next()
+    {
+        if (++at == N) at = 0, parity ^= 1;
+    }
+};
 
 struct WaitState {
     volatile uint32_t* stop;
     __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) const
     {
         for (uint32_t t = 0; t < kWaitTries; ++t) {
-            if (try_wait_cluster(bar, parity)) return true;
+            if (try_wait(bar, parity)) return true;
             if (*stop) return false;
         }
         *stop = 1;
@@ -92,33 +100,41 @@ struct WaitState {
     }
 };
 
-// Columns n0 + c .. of a row, eight (or one, where rows do not all start on 16 bytes) to a call of f(row, c, v), rows side
-// by side on the lanes.  v: the warp's 32 x 32 values, thread l holding row l.
+// Columns c .. of a row, eight (or one, where rows do not all start on 16 bytes) to a call, rows side by side on the lanes.
+// v: the warp's 32 x 32 values, thread l holding row l; groups of four columns are staged at group ^ (row & 7), so that
+// neither the writes nor the reads meet in a bank.  VEC: the lane's i-th call of four is f(i, row, c, values).
 template <bool VEC, class F>
 __device__ __forceinline__ void along_rows(const float (&v)[32], float* stage, int lane, const F& f)
 {
     __syncwarp();
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-        *reinterpret_cast<float4*>(stage + lane * kStageLine + 4 * j) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+        *reinterpret_cast<float4*>(stage + lane * 32 + 4 * (j ^ (lane & 7))) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
     __syncwarp();
     if constexpr (VEC) {
         const int c = (lane & 3) * 8;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int row = i * 8 + (lane >> 2);
-            const float4 a = *reinterpret_cast<const float4*>(stage + row * kStageLine + c);
-            const float4 b = *reinterpret_cast<const float4*>(stage + row * kStageLine + c + 4);
+            const float4 a = *reinterpret_cast<const float4*>(stage + row * 32 + (c ^ (4 * (row & 7))));
+            const float4 b = *reinterpret_cast<const float4*>(stage + row * 32 + ((c + 4) ^ (4 * (row & 7))));
             float w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-            f(row, c, w);
+            f(i, row, c, w);
         }
     } else {
 #pragma unroll 4
         for (int row = 0; row < 32; ++row) {
-            float w[1] = {stage[row * kStageLine + lane]};
-            f(row, lane, w);
+            float w[1] = {stage[row * 32 + (lane ^ (4 * (row & 7)))]};
+            f(0, row, lane, w);
         }
     }
+}
+// Rows and columns of those calls, for what is read ahead of them: f(i, row, c).
+template <class F>
+__device__ __forceinline__ void ahead_of_rows(int lane, const F& f)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f(i, i * 8 + (lane >> 2), (lane & 3) * 8);
 }
 
 // W = 8 (aligned) or 1 values at p, of which n lie in the row.
@@ -148,6 +164,40 @@ __device__ __forceinline__ void load_values(const T* p, int n, float (&v)[W])
         }
     }
 }
+// Eight values as they lie in memory; zeros from the n-th on.
+template <class T>
+struct Raw {
+    uint32_t w[2 * sizeof(T)];
+    __device__ __forceinline__ void load(const T* p, int n, bool vec)
+    {
+        if (vec && n >= 8) {
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+                const uint4 q = reinterpret_cast<const uint4*>(p)[i];
+                w[4 * i] = q.x, w[4 * i + 1] = q.y, w[4 * i + 2] = q.z, w[4 * i + 3] = q.w;
+            }
+            return;
+        }
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = i < n ? reinterpret_cast<const uint32_t*>(p)[i] : 0;
+        } else {
+            const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = (2 * i < n ? h[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)h[2 * i + 1] << 16 : 0u);
+        }
+    }
+    __device__ __forceinline__ void values(float (&v)[8]) const
+    {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) unpack16(w[i], v[2 * i], v[2 * i + 1], T());
+        }
+    }
+};
 template <class T, int W>
 __device__ __forceinline__ void store_values(T* p, int n, const float (&v)[W])
 {
@@ -217,23 +267,61 @@ struct Pieces {
         for (int q = 0; q < P; ++q) *reinterpret_cast<uint4*>(at + q * piece) = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
     }
     template <int P>
-    __device__ __forceinline__ void load(int b, int row, int col, float (&v)[8]) const
+    __device__ __forceinline__ void load(int b, int row, int col, Raw<T16> (&r)[P]) const
     {
         const T16* at = base + b * batch + row * ld + col;
-        load_values<T16, 8>(at, 8, v);
 #pragma unroll
-        for (int q = 1; q < P; ++q) {
-            float r[8];
-            load_values<T16, 8>(at + q * piece, 8, r);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += r[i];
-        }
+        for (int q = 0; q < P; ++q) r[q].load(at + q * piece, 8, true);
     }
 };
 
-// Epi: kDual; operator()(v, w, stage, lane, batch, row0, col0): the warp's 32 rows from row0, 32 columns from col0 of the
-// product (kDual: v of the first array's columns, w of the second's).
-template <int CG, bool CHUNKED, class Epi>
+// factor v, added to what is there or not, into rows of the caller's.
+template <bool VEC, class T>
+__device__ __forceinline__ void store_rows(const float (&v)[32], T* base, int64_t ld, float factor, bool accumulate, int m, int n, float* stage, int lane,
+                                           int row0, int col0)
+{
+    Raw<T> old[4];
+    if (VEC && accumulate)
+        ahead_of_rows(lane, [&](int i, int row, int c) {
+            old[i].load(base + (row0 + row) * ld + col0 + c, row0 + row < m ? n - col0 - c : 0, true);
+        });
+    along_rows<VEC>(v, stage, lane, [&](int i, int row, int c, auto& x) {
+        const int left = n - col0 - c;
+        if (row0 + row >= m || left <= 0) return;
+        T* const at = base + (row0 + row) * ld + col0 + c;
+        if constexpr (VEC) {
+            float o[8];
+            if (accumulate) old[i].values(o);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = accumulate ? o[k] + factor * x[k] : factor * x[k];
+        } else {
+            x[0] = accumulate ? to_f32(*at) + factor * x[0] : factor * x[0];
+        }
+        store_values(at, left, x);
+    });
+}
+
+// Registers of the CHUNKED kernel's threads: warps 0 to 3, and the others.  128 x (64 + 2 x 208) are no more than a launch
+// of 384 threads with 168 (and with 160) has; the launch checks it.
+constexpr int kFewRegisters = 64, kManyRegisters = 208;
+
+// Epi: kDual; Ahead, what load() reads of a 32 x 32 block before its sums are there; operator()(v, w, ahead, stage, lane,
+// batch, row0, col0): the warp's 32 rows from row0, 32 columns from col0 of the product (kDual: v of the first array's
+// columns, w of the second's).
+struct NothingAhead {};
+
+// What a variant of the kernel has: tile columns (of a pair of blocks, where CG = 2), pieces, stages.
+template <int CG_, int BN_, int P_>
+struct Variant {
+    static constexpr int CG = CG_, BN = BN_, P = P_;
+    static constexpr bool chunked = P > 1;
+    static constexpr uint32_t a_bytes = 128 * kTileK * 2, b_bytes = BN / CG * kTileK * 2, stage_bytes = a_bytes + b_bytes;
+    static constexpr uint32_t room = (kGemmSmem - 1024 - kGemmHead - kStaging) / stage_bytes;
+    static constexpr uint32_t stages = room < 8 ? room : 8;
+    static constexpr int chunk = P == 3 ? 1 : 2;   // k-blocks of a chunk
+};
+
+template <class V, class Epi>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmParams p, const __grid_constant__ Epi epi)
 {
@@ -247,7 +335,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     volatile uint32_t* const stop = reinterpret_cast<volatile uint32_t*>(smem + 164);
     float* const staging = reinterpret_cast<float*>(smem + kGemmHead);
     const uint32_t operands = base + kGemmHead + kStaging;
-    const uint32_t a_bytes = 128 * kTileK * 2, stage_bytes = p.pieces * (a_bytes + p.b_bytes);
+    constexpr int CG = V::CG, BN = V::BN, P = V::P;
+    constexpr bool CHUNKED = V::chunked;
+    constexpr uint32_t a_bytes = V::a_bytes, stage_bytes = V::stage_bytes, stages = V::stages;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0;
@@ -255,7 +345,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     const WaitState w{stop};
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < p.stages; ++s) {
+        for (uint32_t s = 0; s < stages; ++s) {
             mbar_init(reinterpret_cast<uint64_t*>(smem + 8 * s), CG);
             mbar_init(reinterpret_cast<uint64_t*>(smem + 64 + 8 * s), 1);
         }
@@ -278,86 +368,90 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     grid_dependency_wait();
 
     uint32_t loaded = 0;   // stages filled by this block (warp 0)
-    if (warp == 0) {
-        if (lane == 0) {
-            const uint32_t nb = p.bn / CG;
-            for (int t = first; t < p.tiles; t += step) {
-                const GemmTile g = gemm_tile(p, t, 128 * CG);
-                const int m0 = g.m0 + (int)rank * 128;
-                const int bb = g.batch % p.bmod;
-                bool ok = true;
-                for (int kb = 0; kb < p.kblocks; ++kb, ++loaded) {
-                    const uint32_t s = loaded % p.stages;
-                    if (loaded >= (uint32_t)p.stages && !(ok = w.wait(empty + 8 * s, (loaded / p.stages - 1) & 1))) break;
+    if (warp < 4) {
+        if constexpr (CHUNKED) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegisters));
+        if (warp == 0 && lane == 0) {
+            constexpr int nb = BN / CG;
+            const uint32_t lead = CG == 2 ? map_shared(full, 0) : full;
+            const bool a_mn = p.a_mn, b_mn = p.b_mn;
+            Ring<stages> ring;
+            bool ok = true;
+            for (int t = first; t < p.tiles && ok; t += step) {
+                const GemmTile g = gemm_tile(p, t, 128 * CG, BN);
+                const int m0 = g.m0 + (int)rank * 128, bb = g.batch % p.bmod;
+                const int n0 = Epi::kDual ? g.n0 / 2 : g.n0 + (int)rank * nb;   // kDual: BN / 2 columns of each array
+                for (int kb = 0; kb < p.kblocks && ok; ++kb) {
                     const int seg = kb >= p.kblocks0, k0 = (kb - (seg ? p.kblocks0 : 0)) * kTileK;
-                    const uint32_t bar = CG == 2 ? map_shared(full + 8 * s, 0) : full + 8 * s;
-                    if constexpr (CG == 2)
-                        arrive_expect_cluster(bar, stage_bytes);
-                    else
-                        mbar_arrive_expect_tx(reinterpret_cast<uint64_t*>(smem + 8 * s), stage_bytes);
-                    uint32_t dst = operands + s * stage_bytes;
-                    for (int q = 0; q < p.pieces; ++q, dst += a_bytes) {
-                        if (p.a_mn) {
-                            load_box<CG>(dst, &maps.a[seg], m0, k0, g.batch, q, bar);
-                            load_box<CG>(dst + 8192, &maps.a[seg], m0 + 64, k0, g.batch, q, bar);
+                    const CUtensorMap* const ma = &maps.a[seg];
+                    const CUtensorMap* const mb = &maps.b[Epi::kDual ? (CG == 2 ? rank : 0) : seg];
+#pragma unroll
+                    for (int q = P - 1; q >= 0; --q, ring.next(), ++loaded) {
+                        if (loaded >= stages && !(ok = w.wait(empty + 8 * ring.at, ring.parity ^ 1))) break;
+                        const uint32_t bar = lead + 8 * ring.at;
+                        if constexpr (CG == 2)
+                            arrive_expect_cluster(bar, stage_bytes);
+                        else
+                            mbar_arrive_expect_tx(reinterpret_cast<uint64_t*>(smem + 8 * ring.at), stage_bytes);
+                        const uint32_t da = operands + ring.at * stage_bytes, db = da + a_bytes;
+                        if (a_mn) {
+                            load_box<CG>(da, ma, m0, k0, g.batch, q, bar);
+                            load_box<CG>(da + 8192, ma, m0 + 64, k0, g.batch, q, bar);
                         } else {
-                            load_box<CG>(dst, &maps.a[seg], k0, m0, g.batch, q, bar);
+                            load_box<CG>(da, ma, k0, m0, g.batch, q, bar);
                         }
-                    }
-                    for (int q = 0; q < p.pieces; ++q, dst += p.b_bytes) {
-                        if constexpr (Epi::kDual) {   // bn / 2 columns of each array
-                            const int n0 = g.n0 / 2;
-                            if constexpr (CG == 2) {
-                                load_box<CG>(dst, &maps.b[rank], k0, n0, bb, q, bar);
-                            } else {
-                                load_box<CG>(dst, &maps.b[0], k0, n0, bb, q, bar);
-                                load_box<CG>(dst + p.b_bytes / 2, &maps.b[1], k0, n0, bb, q, bar);
-                            }
-                        } else if (p.b_mn) {
-                            const int n0 = g.n0 + (int)(rank * nb);
-                            for (uint32_t c = 0; c < nb; c += 64) load_box<CG>(dst + c * 128, &maps.b[seg], n0 + (int)c, k0, bb, q, bar);
+                        if (!Epi::kDual && b_mn) {
+#pragma unroll
+                            for (int c = 0; c < nb; c += 64) load_box<CG>(db + c * 128, mb, n0 + c, k0, bb, q, bar);
                         } else {
-                            load_box<CG>(dst, &maps.b[seg], k0, g.n0 + (int)(rank * nb), bb, q, bar);
+                            load_box<CG>(db, mb, k0, n0, bb, q, bar);
+                            if constexpr (Epi::kDual && CG == 1) load_box<CG>(db + V::b_bytes / 2, &maps.b[1], k0, n0, bb, q, bar);
                         }
                     }
                 }
-                if (!ok) break;
             }
-        }
-        __syncwarp();
-    } else if (warp == 1) {
-        if (rank == 0 && lane == 0) {
-            const uint64_t a_step = p.a_mn ? 2048 >> 4 : 32 >> 4, b_step = p.b_mn ? 2048 >> 4 : 32 >> 4;
-            uint32_t used = 0, sums = 0;   // stages; accumulators
+        } else if (warp == 1 && rank == 0 && lane == 0) {
+            const uint32_t a_step = p.a_mn ? 2048 >> 4 : 32 >> 4, b_step = p.b_mn ? 2048 >> 4 : 32 >> 4;
+            const uint64_t a_first = tile_descriptor(operands, p.a_mn), b_first = tile_descriptor(operands + a_bytes, p.b_mn);
+            const uint32_t idesc = p.idesc;
+            Ring<stages> ring;
+            uint32_t sums = 0;   // accumulators filled
             bool ok = true;
             for (int t = first; t < p.tiles && ok; t += step) {
-                for (int k0 = 0; k0 < p.kblocks && ok; k0 += p.chunk, ++sums) {
+                const int chunk = CHUNKED ? V::chunk : p.kblocks;
+                for (int k0 = 0; k0 < p.kblocks && ok; k0 += chunk, ++sums) {
                     const uint32_t buf = sums & 1;
                     if (sums >= 2 && !(ok = w.wait(acc_empty + 8 * buf, (sums / 2 - 1) & 1))) break;
                     tmem_fence_after();
                     const uint32_t d = tmem + buf * 256;
-                    const int k1 = min(k0 + p.chunk, p.kblocks);
-                    uint32_t add[2] = {0, 0};
-                    for (int kb = k0; kb < k1; ++kb, ++used) {
-                        const uint32_t s = used % p.stages;
-                        if (!(ok = w.wait(full + 8 * s, (used / p.stages) & 1))) break;
-                        tmem_fence_after();
-                        const uint32_t at = operands + s * stage_bytes;
-                        const uint64_t a0 = tile_descriptor(at, p.a_mn);
-                        const uint64_t b0 = tile_descriptor(at + p.pieces * a_bytes, p.b_mn);
-                        for (int q = 0; q < p.pieces; ++q)
-                            for (int r = 0; q + r < p.pieces; ++r) {
-                                const uint64_t a = a0 + q * (a_bytes >> 4), b = b0 + r * (p.b_bytes >> 4);
-                                const int low = CHUNKED && q + r > 0;
-                                uint32_t go_on = add[low];
+                    const int count = min(chunk, p.kblocks - k0);
+                    for (int kb = 0; kb < count && ok; ++kb) {
+                        // The last pieces lie in the first stage of a k-block.  Small products first; a stage is free when its piece
+                        // has met all that it meets, which is in the stages' order.
+                        uint64_t a[P], b[P];
+                        uint32_t free[P];
 #pragma unroll
-                                for (int k = 0; k < kTileK / 16; ++k) {
-                                    mma_f16<CG>(d + low * 128, a + k * a_step, b + k * b_step, p.idesc, go_on);
-                                    go_on = 1;
-                                }
-                                add[low] = 1;
+                        for (int q = P - 1; q >= 0; --q, ring.next()) {
+                            if (!(ok = w.wait(full + 8 * ring.at, ring.parity))) break;
+                            a[q] = a_first + ring.at * (stage_bytes >> 4);
+                            b[q] = b_first + ring.at * (stage_bytes >> 4);
+                            free[q] = empty + 8 * ring.at;
+                        }
+                        if (!ok) break;
+                        tmem_fence_after();
+#pragma unroll
+                        for (int q = P - 1; q >= 0; --q) {   // products whose higher piece is q
+#pragma unroll
+                            for (int r = q; r >= 0; --r) {
+                                if (q + r >= P) continue;
+#pragma unroll
+                                for (int flip = 0; flip < (r < q ? 2 : 1); ++flip)
+#pragma unroll
+                                    for (int k = 0; k < kTileK / 16; ++k)
+                                        mma_f16<CG>(d, a[flip ? r : q] + k * a_step, b[flip ? q : r] + k * b_step, idesc,
+                                                    kb > 0 || k > 0 || flip > 0 || q < P - 1 || r < (P - 1) - q);
                             }
-                        mma_commit<CG>(empty + 8 * s);
+                            mma_commit<CG>(free[q]);
+                        }
                     }
                     if (!ok) break;
                     mma_commit<CG>(acc_full + 8 * buf);
@@ -365,78 +459,76 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             }
         }
         __syncwarp();
-    } else if (warp >= 4) {
+    } else {
+        if constexpr (CHUNKED) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegisters));
         const int quarter = warp & 3, half = (warp - 4) >> 2;
-        float* const stage = staging + (warp - 4) * 32 * kStageLine;
+        float* const stage = staging + (warp - 4) * 32 * 32;
         const uint32_t release = CG == 2 ? map_shared(acc_empty, 0) : acc_empty;
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
         uint32_t sums = 0;
         bool ok = true;
+        constexpr int width = BN / (Epi::kDual ? 4 : 2);   // columns of this warp (of each array)
         for (int t = first; t < p.tiles && ok; t += step) {
-            const GemmTile g = gemm_tile(p, t, 128 * CG);
-            const int row0 = g.m0 + (int)rank * 128 + quarter * 32;
-            if constexpr (CHUNKED) {   // bn = 128: 64 columns to a warp
-                float acc[64];
+            const GemmTile g = gemm_tile(p, t, 128 * CG, BN);
+            const int row0 = g.m0 + (int)rank * 128 + quarter * 32, from = (Epi::kDual ? g.n0 / 2 : g.n0) + half * width;
+            typename Epi::Ahead ahead;
+            if constexpr (CHUNKED) {
+                constexpr int slabs = BN / 64;   // kDual: those of the first array, then those of the second
+                float acc[slabs][32];
 #pragma unroll
-                for (int i = 0; i < 64; ++i) acc[i] = 0.f;
-                for (int k0 = 0; k0 < p.kblocks; k0 += p.chunk, ++sums) {
+                for (int j = 0; j < slabs; ++j)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) acc[j][i] = 0.f;
+                for (int k0 = 0; k0 < p.kblocks; k0 += V::chunk, ++sums) {
                     const uint32_t buf = sums & 1;
                     ok = __all_sync(~0u, w.wait(acc_full + 8 * buf, (sums / 2) & 1));
                     if (!ok) break;
                     tmem_fence_after();
-                    const uint32_t at = lanes + buf * 256 + half * (Epi::kDual ? 32 : 64);
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        float a[32], b[32];
-                        tmem_load32(at + j * (Epi::kDual ? 64 : 32), a);
-                        tmem_load32(at + j * (Epi::kDual ? 64 : 32) + 128, b);
+                    for (int j = 0; j < slabs; ++j) {
+                        const uint32_t at = lanes + buf * 256 + half * width + (Epi::kDual ? (j % (slabs / 2)) * 32 + j / (slabs / 2) * (BN / 2) : j * 32);
+                        float a[32];
+                        tmem_load32(at, a);
                         tmem_wait_load();
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) acc[32 * j + i] += a[i] + b[i];
+                        for (int i = 0; i < 32; ++i) acc[j][i] += a[i];
                     }
                     tmem_fence_before();
                     __syncwarp();
                     if (lane == 0) arrive_cluster(release + 8 * buf);
                 }
                 if (!ok) break;
-                if (row0 < p.m) {
-                    float a[32], b[32];
+                if (row0 >= p.m) continue;
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) a[i] = acc[i], b[i] = acc[32 + i];
-                    if constexpr (Epi::kDual) {
-                        const int col0 = g.n0 / 2 + half * 32;
-                        if (col0 < p.n) epi(a, b, stage, lane, g.batch, row0, col0);
-                    } else {
-                        const int col0 = g.n0 + half * 64;
-                        if (col0 < p.n) epi(a, a, stage, lane, g.batch, row0, col0);
-                        if (col0 + 32 < p.n) epi(b, b, stage, lane, g.batch, row0, col0 + 32);
-                    }
+                for (int j = 0; j < (Epi::kDual ? slabs / 2 : slabs); ++j) {
+                    const int col0 = from + 32 * j;
+                    if (col0 >= p.n) continue;
+                    epi.load(ahead, lane, g.batch, row0, col0);
+                    epi(acc[j], acc[Epi::kDual ? j + slabs / 2 : j], ahead, stage, lane, g.batch, row0, col0);
                 }
             } else {
                 const uint32_t buf = sums & 1;
+                if (row0 < p.m && from < p.n) epi.load(ahead, lane, g.batch, row0, from);
                 ok = __all_sync(~0u, w.wait(acc_full + 8 * buf, (sums / 2) & 1));
                 if (!ok) break;
                 ++sums;
                 tmem_fence_after();
-                const int width = p.bn / (Epi::kDual ? 4 : 2);   // columns of this warp
                 for (int c = 0; c < width; c += 32) {
                     float a[32], b[32];
                     const uint32_t at = lanes + buf * 256 + half * width + c;
                     tmem_load32(at, a);
-                    if constexpr (Epi::kDual) tmem_load32(at + p.bn / 2, b);
+                    if constexpr (Epi::kDual) tmem_load32(at + BN / 2, b);
                     tmem_wait_load();
                     if (c + 32 >= width) {
                         tmem_fence_before();
                         __syncwarp();
                         if (lane == 0) arrive_cluster(release + 8 * buf);
                     }
-                    const int col0 = (Epi::kDual ? g.n0 / 2 : g.n0) + half * width + c;
-                    if (row0 < p.m && col0 < p.n) {
-                        if constexpr (Epi::kDual)
-                            epi(a, b, stage, lane, g.batch, row0, col0);
-                        else
-                            epi(a, a, stage, lane, g.batch, row0, col0);
-                    }
+                    const int col0 = from + c;
+                    if (row0 >= p.m || col0 >= p.n) continue;
+                    const typename Epi::Ahead now = ahead;
+                    if (c + 32 < width && col0 + 32 < p.n) epi.load(ahead, lane, g.batch, row0, col0 + 32);
+                    epi(a, Epi::kDual ? b : a, now, stage, lane, g.batch, row0, col0);
                 }
             }
         }
@@ -446,8 +538,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     tmem_fence_before();
     __syncthreads();
     if (*stop && threadIdx.x == 0)
-        for (uint32_t i = loaded > (uint32_t)p.stages ? loaded - p.stages : 0; i < loaded; ++i)
-            for (uint32_t tries = 0; tries < 4096 && !try_wait_cluster(full + 8 * (i % p.stages), (i / p.stages) & 1); ++tries) {
+        for (uint32_t i = loaded > stages ? loaded - stages : 0; i < loaded; ++i)
+            for (uint32_t tries = 0; tries < 4096 && !try_wait(full + 8 * (i % stages), (i / stages) & 1); ++tries) {
             }
     __syncthreads();
     if constexpr (CG == 2) cluster_barrier();
@@ -482,12 +574,19 @@ struct GemmPlan {
 
 int sm_count();
 
-template <int CG, bool CHUNKED, class Epi>
-cudaError_t launch_gemm_as(const GemmPlan& g, int bn, const Epi& epi, cudaStream_t stream)
+template <class Kernel>
+int kernel_registers(Kernel kernel)
 {
+    cudaFuncAttributes a;
+    return cudaFuncGetAttributes(&a, kernel) == cudaSuccess ? a.numRegs : 0;
+}
+
+template <class V, class Epi>
+cudaError_t launch_gemm_as(const GemmPlan& g, const Epi& epi, cudaStream_t stream)
+{
+    constexpr int CG = V::CG, bn = V::BN;
     GemmParams p;
     GemmMaps maps;
-    const int pieces = (int)g.a[0].pieces;
     p.m = (int32_t)g.m;
     p.n = (int32_t)g.n;
     p.kblocks0 = (int32_t)((g.k[0] + kTileK - 1) / kTileK);
@@ -499,12 +598,6 @@ cudaError_t launch_gemm_as(const GemmPlan& g, int bn, const Epi& epi, cudaStream
     const int64_t tiles = g.batch * p.tiles_m * p.tiles_n;
     if (tiles >= (int64_t(1) << 31) - 65536) return cudaErrorInvalidValue;
     p.tiles = (int32_t)tiles;
-    p.bn = bn;
-    p.pieces = pieces;
-    p.b_bytes = (uint32_t)(bn / CG * kTileK * 2);
-    const int stage_bytes = pieces * (128 * kTileK * 2 + (int)p.b_bytes);
-    p.stages = std::min(8, (kGemmSmem - 1024 - kGemmHead - kStaging) / stage_bytes);
-    p.chunk = CHUNKED ? 2 : p.kblocks;
     p.a_mn = g.a[0].mn_major;
     p.b_mn = g.b[0].mn_major;
     p.idesc = 1u << 4 | (g.half ? 0u : 1u << 7 | 1u << 10) | (uint32_t)p.a_mn << 15 | (uint32_t)p.b_mn << 16 | (uint32_t)(bn >> 3) << 17 |
@@ -516,10 +609,14 @@ cudaError_t launch_gemm_as(const GemmPlan& g, int bn, const Epi& epi, cudaStream
         if (e == cudaSuccess) e = encode_map(maps.b[i], g.b[b_there ? i : 0], g.half, b_rows);
         if (e != cudaSuccess) return e;
     }
-    const auto kernel = gemm_kernel<CG, CHUNKED, Epi>;
+    const auto kernel = gemm_kernel<V, Epi>;
     static std::atomic<unsigned long long> limit_set{0};
     const cudaError_t e = ensure_smem_limit(kernel, kGemmSmem, limit_set);
     if (e != cudaSuccess) return e;
+    if (V::chunked) {
+        static const int registers = kernel_registers(kernel);
+        if (registers * kGemmThreads < 128 * (kFewRegisters + 2 * kManyRegisters)) return cudaErrorLaunchOutOfResources;
+    }
     const int64_t blocks = std::min<int64_t>(tiles, sm_count() / CG) * CG;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)blocks);

@@ -16,7 +16,7 @@ namespace gpga {
 namespace {
 
 constexpr float kScale = 2048.f;
-constexpr int kNormParts = 64;    // blocks per matrix of the sum of squares
+constexpr int kNormParts = 1024;  // blocks of the sum of squares, over all matrices
 
 // Sum of squares of a part of a matrix in fp64: no overflow, and the order is fixed.
 template <class T>
@@ -101,28 +101,44 @@ __global__ void __launch_bounds__(256) start_kernel(const T* m, int64_t ld, int6
 template <int P>
 struct KeepPieces {
     static constexpr bool kDual = false;
+    struct Ahead {
+        Raw<__half> r[4][P];
+    };
     Pieces<__half> out, r;
     const float* kappa;
     float factor, beta, diagonal;
     int32_t m, n, power, with_r;
 
-    __device__ __forceinline__ void operator()(float (&v)[32], float (&)[32], float* stage, int lane, int batch, int row0, int col0) const
+    __device__ __forceinline__ void load(Ahead& ahead, int lane, int batch, int row0, int col0) const
+    {
+        if (with_r)
+            ahead_of_rows(lane, [&](int i, int row, int c) {
+                if (row0 + row < m && col0 + c < n) r.template load<P>(batch, row0 + row, col0 + c, ahead.r[i]);
+            });
+    }
+    __device__ __forceinline__ void operator()(float (&v)[32], float (&)[32], const Ahead& ahead, float* stage, int lane, int batch, int row0, int col0) const
     {
         float a = factor;
         if (power) {
             const float k = kappa[batch];
             a *= power == 2 ? k * k : k;
         }
-        along_rows<true>(v, stage, lane, [&](int row, int c, auto& x) {
+        along_rows<true>(v, stage, lane, [&](int l, int row, int c, auto& x) {
             const int i = row0 + row, j = col0 + c;
             if (i >= m || j >= n) return;
 #pragma unroll
             for (int k = 0; k < 8; ++k) x[k] *= a;
             if (with_r) {
-                float s[8];
-                r.template load<P>(batch, i, j, s);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) x[k] += beta * s[k] + (i == j + k ? diagonal : 0.f);
+                for (int q = P - 1; q >= 0; --q) {
+                    float s[8];
+                    ahead.r[l][q].values(s);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) x[k] += beta * s[k];
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (i == j + k) x[k] += diagonal;
             }
             out.template store<P>(batch, i, j, n - j, x);
         });
@@ -133,35 +149,21 @@ struct KeepPieces {
 template <class T>
 struct LastStep {
     static constexpr bool kDual = false;
+    using Ahead = NothingAhead;
     T* out;
     int64_t ld, node;
     const float* kappa;
     float factor;
     int32_t m, n, power, accumulate, vec;
 
-    template <bool VEC>
-    __device__ __forceinline__ void rows(const float (&v)[32], float* stage, int lane, int batch, int row0, int col0) const
+    __device__ __forceinline__ void load(Ahead&, int, int, int, int) const {}
+    __device__ __forceinline__ void operator()(float (&v)[32], float (&)[32], const Ahead&, float* stage, int lane, int batch, int row0, int col0) const
     {
         const float a = power ? factor * kappa[batch] : factor;
-        T* const base = out + batch * node;
-        along_rows<VEC>(v, stage, lane, [&](int row, int c, auto& x) {
-            const int left = n - col0 - c;
-            if (row0 + row >= m || left <= 0) return;
-            T* const at = base + (row0 + row) * ld + col0 + c;
-            constexpr int W = sizeof(x) / sizeof(float);
-            float old[W];
-            if (accumulate) load_values(at, left, old);
-#pragma unroll
-            for (int i = 0; i < W; ++i) x[i] = accumulate ? old[i] + a * x[i] : a * x[i];
-            store_values(at, left, x);
-        });
-    }
-    __device__ __forceinline__ void operator()(float (&v)[32], float (&)[32], float* stage, int lane, int batch, int row0, int col0) const
-    {
         if (vec)
-            rows<true>(v, stage, lane, batch, row0, col0);
+            store_rows<true>(v, out + batch * node, ld, a, accumulate, m, n, stage, lane, row0, col0);
         else
-            rows<false>(v, stage, lane, batch, row0, col0);
+            store_rows<false>(v, out + batch * node, ld, a, accumulate, m, n, stage, lane, row0, col0);
     }
 };
 
@@ -182,7 +184,7 @@ OrthPlan plan_orth(const OrthParams& p)
 {
     OrthPlan q;
     const int64_t s = std::min(p.r, p.c);
-    q.count_parts = (int)std::max<int64_t>(1, std::min<int64_t>(kNormParts, p.r * p.c / 2048));
+    q.count_parts = (int)std::max<int64_t>(1, std::min<int64_t>(std::max<int64_t>(1, kNormParts / p.nodes), p.r * p.c / 2048));
     const auto array = [&](int64_t rows, int64_t cols) {
         Operand o;
         o.inner = cols;
@@ -207,8 +209,8 @@ OrthPlan plan_orth(const OrthParams& p)
 template <int P, class Epi>
 cudaError_t product(const GemmPlan& g, const Epi& e, cudaStream_t stream)
 {
-    if (g.m <= 128) return launch_gemm_as<1, P == 2>(g, 128, e, stream);
-    return launch_gemm_as<2, P == 2>(g, P == 2 ? 128 : 256, e, stream);
+    if (g.m <= 128) return launch_gemm_as<Variant<1, 128, P>>(g, e, stream);
+    return launch_gemm_as<Variant<2, 256, P>>(g, e, stream);
 }
 
 template <class T>
