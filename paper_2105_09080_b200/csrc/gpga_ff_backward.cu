@@ -65,7 +65,6 @@ cudaError_t backward(const FeedForwardParams& p, cudaStream_t stream)
     grad.dg = pieces_of<T16>(dg);
     grad.du = pieces_of<T16>(du);
     grad.m = (int32_t)p.rows;
-    grad.n = (int32_t)p.f;
     grad.kind = p.activation;
     grad.vec = rows_on_16(p.g.p, p.g.ld, p.nodes * p.rows, 0, 1, sizeof(T)) && rows_on_16(p.u.p, p.u.ld, p.nodes * p.rows, 0, 1, sizeof(T));
     if ((e = launch_gemm<P>(g, grad, stream)) != cudaSuccess) return e;

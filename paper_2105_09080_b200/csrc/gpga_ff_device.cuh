@@ -48,33 +48,23 @@ struct GateUp {
     T *g, *u;
     int64_t ldg, ldu;
     Pieces<T16> h;
-    int32_t m, n, kind, keep, vec;
+    int32_t m, kind, keeps, vec;
 
-    __device__ __forceinline__ void load(Ahead&, int, int, int, int) const {}
-
-    template <bool VEC>
-    __device__ __forceinline__ void keep_values(const float (&v)[32], T* to, int64_t ld, float* stage, int lane, int batch, int row0, int col0) const
+    __device__ __forceinline__ bool wide() const { return vec; }
+    __device__ __forceinline__ void keep(int which, float v, int batch, int row, int col) const
     {
-        along_rows<VEC>(v, stage, lane, [&](int, int row, int c, auto& x) {
-            if (row0 + row < m && col0 + c < n) store_values(to + ((int64_t)batch * m + row0 + row) * ld + col0 + c, n - col0 - c, x);
-        });
+        (which ? u : g)[((int64_t)batch * m + row) * (which ? ldu : ldg) + col] = from_f32<T>(v);
     }
-    __device__ __forceinline__ void operator()(float (&v)[32], float (&w)[32], const Ahead&, float* stage, int lane, int batch, int row0, int col0) const
+    __device__ __forceinline__ void eight(float (&v)[8], float (&w)[8], int batch, int row, int col, int left) const
     {
-        if (keep) {
-            if (vec) {
-                keep_values<true>(v, g, ldg, stage, lane, batch, row0, col0);
-                keep_values<true>(w, u, ldu, stage, lane, batch, row0, col0);
-            } else {
-                keep_values<false>(v, g, ldg, stage, lane, batch, row0, col0);
-                keep_values<false>(w, u, ldu, stage, lane, batch, row0, col0);
-            }
+        if (keeps && vec) {
+            const int64_t at = (int64_t)batch * m + row;
+            store8(g + at * ldg + col, left, v);
+            store8(u + at * ldu + col, left, w);
         }
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = act_value<sizeof(T) == 2>(v[i], kind) * w[i];
-        along_rows<true>(v, stage, lane, [&](int, int row, int c, auto& x) {
-            if (row0 + row < m && col0 + c < n) h.template store<P>(batch, row0 + row, col0 + c, n - col0 - c, x);
-        });
+        for (int i = 0; i < 8; ++i) v[i] = act_value<sizeof(T) == 2>(v[i], kind) * w[i];
+        h.template store<P>(batch, row, col, v);
     }
 };
 
@@ -85,43 +75,37 @@ struct GateGrad {
     using T16 = typename PiecesOf<T>::type;
     static constexpr int P = PiecesOf<T>::count;
     struct Ahead {
-        Raw<T> g[4], u[4];
+        Raw<T> g, u;
     };
     const T *g, *u;
     int64_t ldg, ldu;
     Pieces<T16> h, dg, du;
-    int32_t m, n, kind, vec;
+    int32_t m, kind, vec;
 
-    __device__ __forceinline__ void load(Ahead& ahead, int lane, int batch, int row0, int col0) const
+    __device__ __forceinline__ bool wide() const { return true; }
+    __device__ __forceinline__ void one(float, int, int, int) const {}
+    __device__ __forceinline__ void load(Ahead& ahead, int batch, int row, int col, int left) const
     {
-        ahead_of_rows(lane, [&](int i, int row, int c) {
-            const int left = row0 + row < m ? n - col0 - c : 0;
-            const int64_t at = (int64_t)batch * m + row0 + row;
-            ahead.g[i].load(g + at * ldg + col0 + c, left, vec);
-            ahead.u[i].load(u + at * ldu + col0 + c, left, vec);
-        });
+        const int64_t at = (int64_t)batch * m + row;
+        ahead.g.load(g + at * ldg + col, left, vec);
+        ahead.u.load(u + at * ldu + col, left, vec);
     }
-    __device__ __forceinline__ void operator()(float (&v)[32], float (&)[32], const Ahead& ahead, float* stage, int lane, int batch, int row0, int col0) const
+    __device__ __forceinline__ void eight(float (&dh)[8], const Ahead& now, int batch, int row, int col, int) const
     {
-        along_rows<true>(v, stage, lane, [&](int j, int row, int c, auto& dh) {
-            const int left = n - col0 - c;
-            if (row0 + row >= m || left <= 0) return;
-            float gv[8], uv[8];
-            ahead.g[j].values(gv);
-            ahead.u[j].values(uv);
-            float hv[8];
+        float a[8], s[8], gu[8];
+        now.g.values(gu);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float a, s;
-                act_slope<sizeof(T) == 2>(gv[i], kind, a, s);
-                hv[i] = a * uv[i];
-                gv[i] = dh[i] * uv[i] * s;
-                uv[i] = dh[i] * a;
-            }
-            h.template store<P>(batch, row0 + row, col0 + c, left, hv);
-            dg.template store<P>(batch, row0 + row, col0 + c, left, gv);
-            du.template store<P>(batch, row0 + row, col0 + c, left, uv);
-        });
+        for (int i = 0; i < 8; ++i) act_slope<sizeof(T) == 2>(gu[i], kind, a[i], s[i]);
+        now.u.values(gu);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] *= dh[i] * gu[i];
+        dg.template store<P>(batch, row, col, s);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) gu[i] *= a[i];
+        h.template store<P>(batch, row, col, gu);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a[i] *= dh[i];
+        du.template store<P>(batch, row, col, a);
     }
 };
 
@@ -129,25 +113,23 @@ struct GateGrad {
 template <class T>
 struct StoreRows {
     static constexpr bool kDual = false;
-    using Ahead = NothingAhead;
+    using Ahead = Raw<T>;
     T* out[2];
     int64_t ld[2], node[2];
-    int32_t m, n, split, accumulate, vec;
+    int32_t split, accumulate, vec;
 
-    __device__ __forceinline__ void load(Ahead&, int, int, int, int) const {}
-    template <bool VEC>
-    __device__ __forceinline__ void rows(const float (&v)[32], float* stage, int lane, int batch, int row0, int col0) const
+    __device__ __forceinline__ bool wide() const { return vec; }
+    __device__ __forceinline__ Rows<T> rows(int batch) const
     {
         const int which = batch >= split;
-        store_rows<VEC>(v, out[which] + (batch - which * split) * node[which], ld[which], 1.f, accumulate, m, n, stage, lane, row0, col0);
+        return {out[which] + (batch - which * split) * node[which], ld[which], 1.f, accumulate != 0};
     }
-    __device__ __forceinline__ void operator()(float (&v)[32], float (&)[32], const Ahead&, float* stage, int lane, int batch, int row0, int col0) const
+    __device__ __forceinline__ void load(Ahead& old, int batch, int row, int col, int left) const { rows(batch).ahead(old, row, col, left); }
+    __device__ __forceinline__ void eight(float (&v)[8], const Ahead& old, int batch, int row, int col, int left) const
     {
-        if (vec)
-            rows<true>(v, stage, lane, batch, row0, col0);
-        else
-            rows<false>(v, stage, lane, batch, row0, col0);
+        rows(batch).eight(v, old, row, col, left);
     }
+    __device__ __forceinline__ void one(float v, int batch, int row, int col) const { rows(batch).one(v, row, col); }
 };
 
 inline bool rows_on_16(const void* p, int64_t ld, int64_t rows, int64_t node, int64_t nodes, int size)
@@ -174,8 +156,6 @@ cudaError_t store_product(const GemmPlan& g, const Matrix& out, int64_t rows, co
     e.ld[1] = o2.ld;
     e.node[0] = out.node;
     e.node[1] = o2.node;
-    e.m = (int32_t)g.m;
-    e.n = (int32_t)g.n;
     e.split = (int32_t)(second ? g.batch / 2 : g.batch);
     e.accumulate = accumulate;
     e.vec = rows_on_16(out.p, out.ld, rows, out.node, g.batch, sizeof(T)) && rows_on_16(o2.p, o2.ld, rows, o2.node, g.batch, sizeof(T));

@@ -49,10 +49,9 @@ cudaError_t forward(const FeedForwardParams& p, cudaStream_t stream)
     up.ldu = p.u.ld;
     up.h = pieces_of<T16>(q.h);
     up.m = (int32_t)p.rows;
-    up.n = (int32_t)p.f;
     up.kind = p.activation;
-    up.keep = p.g.p != nullptr;
-    up.vec = !up.keep || (rows_on_16(p.g.p, p.g.ld, p.nodes * p.rows, 0, 1, sizeof(T)) && rows_on_16(p.u.p, p.u.ld, p.nodes * p.rows, 0, 1, sizeof(T)));
+    up.keeps = p.g.p != nullptr;
+    up.vec = !up.keeps || (rows_on_16(p.g.p, p.g.ld, p.nodes * p.rows, 0, 1, sizeof(T)) && rows_on_16(p.u.p, p.u.ld, p.nodes * p.rows, 0, 1, sizeof(T)));
     e = launch_gemm<P>(g, up, stream);
     if (e != cudaSuccess) return e;
     g.after = true;

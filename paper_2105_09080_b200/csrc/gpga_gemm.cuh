@@ -100,70 +100,24 @@ struct WaitState {
     }
 };
 
-// Columns c .. of a row, eight (or one, where rows do not all start on 16 bytes) to a call, rows side by side on the lanes.
-// v: the warp's 32 x 32 values, thread l holding row l; groups of four columns are staged at group ^ (row & 7), so that
-// neither the writes nor the reads meet in a bank.  VEC: the lane's i-th call of four is f(i, row, c, values).
-template <bool VEC, class F>
-__device__ __forceinline__ void along_rows(const float (&v)[32], float* stage, int lane, const F& f)
+// A warp's 32 x 32 values pass from thread l holding row l to eight columns of a row per lane: groups of four columns lie at
+// group ^ (row & 7), so that neither the writes nor the reads meet in a bank.
+__device__ __forceinline__ void stage_rows(const float (&v)[32], float* stage, int lane)
 {
     __syncwarp();
 #pragma unroll
     for (int j = 0; j < 8; ++j)
         *reinterpret_cast<float4*>(stage + lane * 32 + 4 * (j ^ (lane & 7))) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
     __syncwarp();
-    if constexpr (VEC) {
-        const int c = (lane & 3) * 8;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = i * 8 + (lane >> 2);
-            const float4 a = *reinterpret_cast<const float4*>(stage + row * 32 + (c ^ (4 * (row & 7))));
-            const float4 b = *reinterpret_cast<const float4*>(stage + row * 32 + ((c + 4) ^ (4 * (row & 7))));
-            float w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-            f(i, row, c, w);
-        }
-    } else {
-#pragma unroll 4
-        for (int row = 0; row < 32; ++row) {
-            float w[1] = {stage[row * 32 + (lane ^ (4 * (row & 7)))]};
-            f(0, row, lane, w);
-        }
-    }
 }
-// Rows and columns of those calls, for what is read ahead of them: f(i, row, c).
-template <class F>
-__device__ __forceinline__ void ahead_of_rows(int lane, const F& f)
+__device__ __forceinline__ void staged8(const float* stage, int row, int c, float (&v)[8])
 {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f(i, i * 8 + (lane >> 2), (lane & 3) * 8);
+    const float4 a = *reinterpret_cast<const float4*>(stage + row * 32 + (c ^ (4 * (row & 7))));
+    const float4 b = *reinterpret_cast<const float4*>(stage + row * 32 + ((c + 4) ^ (4 * (row & 7))));
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
 }
+__device__ __forceinline__ float staged1(const float* stage, int row, int c) { return stage[row * 32 + (c ^ (4 * (row & 7)))]; }
 
-// W = 8 (aligned) or 1 values at p, of which n lie in the row.
-template <class T, int W>
-__device__ __forceinline__ void load_values(const T* p, int n, float (&v)[W])
-{
-    if constexpr (W == 1) {
-        v[0] = n > 0 ? to_f32(*p) : 0.f;
-    } else {
-        if (n >= 8) {
-            uint32_t w[2 * sizeof(T)];
-#pragma unroll
-            for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-                const uint4 q = reinterpret_cast<const uint4*>(p)[i];
-                w[4 * i] = q.x, w[4 * i + 1] = q.y, w[4 * i + 2] = q.z, w[4 * i + 3] = q.w;
-            }
-            if constexpr (sizeof(T) == 4) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) unpack16(w[i], v[2 * i], v[2 * i + 1], T());
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = i < n ? to_f32(p[i]) : 0.f;
-        }
-    }
-}
 // Eight values as they lie in memory; zeros from the n-th on.
 template <class T>
 struct Raw {
@@ -198,70 +152,66 @@ struct Raw {
         }
     }
 };
-template <class T, int W>
-__device__ __forceinline__ void store_values(T* p, int n, const float (&v)[W])
+// Eight values to memory, the first n of them where the row ends.
+template <class T>
+__device__ __forceinline__ void store8(T* p, int n, const float (&v)[8])
 {
-    if constexpr (W == 1) {
-        if (n > 0) *p = from_f32<T>(v[0]);
+    uint32_t w[2 * sizeof(T)];
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(v[i]);
     } else {
-        if (n >= 8) {
-            uint32_t w[2 * sizeof(T)];
-            if constexpr (sizeof(T) == 4) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(v[i]);
-            } else {
+        for (int i = 0; i < 4; ++i) w[i] = pack16(v[2 * i], v[2 * i + 1], T());
+    }
+    if (n >= 8) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] = pack16(v[2 * i], v[2 * i + 1], T());
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+            reinterpret_cast<uint4*>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 7; ++i)
+            if (i < n) {
+                if constexpr (sizeof(T) == 4)
+                    reinterpret_cast<uint32_t*>(p)[i] = w[i];
+                else
+                    reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
             }
-#pragma unroll
-            for (int i = 0; i < (int)sizeof(T) / 2; ++i)
-                reinterpret_cast<uint4*>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < n) p[i] = from_f32<T>(v[i]);
-        }
     }
 }
 
-// The pieces of a value.  bfloat16: the upper 16 bits, the upper 16 of the rest, and what is left of it, which has eight
-// significant bits: the sum is exact (an infinity's rest is NaN).  half: rounded, then the rounded rest: 22 bits.
-template <class T16, int P>
-__device__ __forceinline__ void split(float v, T16 (&o)[P])
-{
-    if constexpr (P == 1) {
-        o[0] = from_f32<T16>(v);
-    } else if constexpr (P == 2) {
-        o[0] = from_f32<T16>(v);
-        o[1] = from_f32<T16>(v - to_f32(o[0]));
-    } else {
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-            const float h = __uint_as_float(__float_as_uint(v) & 0xFFFF0000u);
-            o[i] = from_f32<T16>(h);
-            v -= h;
-        }
-    }
-}
 // Where the pieces of an array of rows are (piece, batch, row, column; rows start on 16 bytes and are padded to eight).
+// bfloat16, P = 3: the upper 16 bits, the upper 16 of the rest, and what is left of it, which has eight significant bits:
+// the sum is exact (an infinity's rest is NaN).  half, P = 2: rounded, then the rounded rest: 22 bits.  P = 1: rounded.
 template <class T16>
 struct Pieces {
     T16* base;
     int64_t piece, batch, ld;
-    template <int P, int W>
-    __device__ __forceinline__ void store(int b, int row, int col, int n, const float (&v)[W]) const
+    template <int P>
+    __device__ __forceinline__ void store(int b, int row, int col, const float (&v)[8]) const
     {
-        static_assert(W == 8, "pieces are stored in chunks of eight columns");
         T16* at = base + b * batch + row * ld + col;
         uint32_t w[P][4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            T16 lo[P], hi[P];
-            split<T16, P>(2 * i < n ? v[2 * i] : 0.f, lo);
-            split<T16, P>(2 * i + 1 < n ? v[2 * i + 1] : 0.f, hi);
+            float x = v[2 * i], y = v[2 * i + 1];
+            if constexpr (P == 3) {
 #pragma unroll
-            for (int q = 0; q < P; ++q)
-                w[q][i] = (uint32_t)*reinterpret_cast<const uint16_t*>(&lo[q]) | (uint32_t)*reinterpret_cast<const uint16_t*>(&hi[q]) << 16;
+                for (int q = 0; q < 3; ++q) {
+                    w[q][i] = __byte_perm(__float_as_uint(x), __float_as_uint(y), 0x7632);
+                    if (q < 2) {
+                        x -= __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
+                        y -= __uint_as_float(__float_as_uint(y) & 0xFFFF0000u);
+                    }
+                }
+            } else {
+                w[0][i] = pack16(x, y, T16());
+                if constexpr (P == 2) {
+                    float hx, hy;
+                    unpack16(w[0][i], hx, hy, T16());
+                    w[1][i] = pack16(x - hx, y - hy, T16());
+                }
+            }
         }
 #pragma unroll
         for (int q = 0; q < P; ++q) *reinterpret_cast<uint4*>(at + q * piece) = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
@@ -275,39 +225,43 @@ struct Pieces {
     }
 };
 
-// factor v, added to what is there or not, into rows of the caller's.
-template <bool VEC, class T>
-__device__ __forceinline__ void store_rows(const float (&v)[32], T* base, int64_t ld, float factor, bool accumulate, int m, int n, float* stage, int lane,
-                                           int row0, int col0)
-{
-    Raw<T> old[4];
-    if (VEC && accumulate)
-        ahead_of_rows(lane, [&](int i, int row, int c) {
-            old[i].load(base + (row0 + row) * ld + col0 + c, row0 + row < m ? n - col0 - c : 0, true);
-        });
-    along_rows<VEC>(v, stage, lane, [&](int i, int row, int c, auto& x) {
-        const int left = n - col0 - c;
-        if (row0 + row >= m || left <= 0) return;
-        T* const at = base + (row0 + row) * ld + col0 + c;
-        if constexpr (VEC) {
-            float o[8];
-            if (accumulate) old[i].values(o);
+// Rows of the caller's that a product goes to: factor times it, added to what is there or not.
+template <class T>
+struct Rows {
+    T* base;
+    int64_t ld;
+    float factor;
+    bool accumulate;
+    __device__ __forceinline__ void ahead(Raw<T>& old, int row, int col, int left) const
+    {
+        if (accumulate) old.load(base + row * ld + col, left, true);
+    }
+    __device__ __forceinline__ void eight(float (&v)[8], const Raw<T>& old, int row, int col, int left) const
+    {
+        float o[8];
+        if (accumulate) old.values(o);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) x[k] = accumulate ? o[k] + factor * x[k] : factor * x[k];
-        } else {
-            x[0] = accumulate ? to_f32(*at) + factor * x[0] : factor * x[0];
-        }
-        store_values(at, left, x);
-    });
-}
+        for (int k = 0; k < 8; ++k) v[k] = accumulate ? o[k] + factor * v[k] : factor * v[k];
+        store8(base + row * ld + col, left, v);
+    }
+    __device__ __forceinline__ void one(float v, int row, int col) const
+    {
+        T* const at = base + row * ld + col;
+        *at = from_f32<T>(accumulate ? to_f32(*at) + factor * v : factor * v);
+    }
+};
 
 // Registers of the CHUNKED kernel's threads: warps 0 to 3, and the others.  128 x (64 + 2 x 208) are no more than a launch
 // of 384 threads with 168 (and with 160) has; the launch checks it.
 constexpr int kFewRegisters = 64, kManyRegisters = 208;
 
-// Epi: kDual; Ahead, what load() reads of a 32 x 32 block before its sums are there; operator()(v, w, ahead, stage, lane,
-// batch, row0, col0): the warp's 32 rows from row0, 32 columns from col0 of the product (kDual: v of the first array's
-// columns, w of the second's).
+// Epi, for a product's row and column (bounds are the kernel's care; `left` columns are there from col on):
+//   Ahead, load(ahead, batch, row, col, left): what is read of eight columns ahead of their sums;
+//   eight(v, ahead, batch, row, col, left): eight columns.  wide() false: one(v, batch, row, col) is called instead;
+//   kDual: eight(v, w, batch, row, col, left), v of the first array's columns, w of the second's.  wide() false: keep(which, v,
+//   batch, row, col) is called first for every single value.
+// The loops over eight columns are kept rolled: a warp goes through an epilogue once per tile, and unrolled it waits for
+// instructions (gradient epilogue, fp32: 147 us unrolled, see below for what it is now).
 struct NothingAhead {};
 
 // What a variant of the kernel has: tile columns (of a pair of blocks, where CG = 2), pieces, stages.
@@ -468,10 +422,62 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         uint32_t sums = 0;
         bool ok = true;
         constexpr int width = BN / (Epi::kDual ? 4 : 2);   // columns of this warp (of each array)
+        const int lane_row = lane >> 2, lane_col = (lane & 3) * 8;
         for (int t = first; t < p.tiles && ok; t += step) {
             const GemmTile g = gemm_tile(p, t, 128 * CG, BN);
             const int row0 = g.m0 + (int)rank * 128 + quarter * 32, from = (Epi::kDual ? g.n0 / 2 : g.n0) + half * width;
+            const int rows = p.m - row0;   // that are there
             typename Epi::Ahead ahead;
+            // A 32 x 32 block that is staged; `next`: whether the block to the right follows.
+            const auto block = [&](int col0, bool next) {
+                if constexpr (!Epi::kDual) {
+                if (!epi.wide()) {
+                    if (col0 + lane < p.n)
+#pragma unroll 1
+                        for (int r = 0; r < min(rows, 32); ++r) epi.one(staged1(stage, r, lane), g.batch, row0 + r, col0 + lane);
+                    return;
+                }
+#pragma unroll 1
+                for (int i = 0; i < 4; ++i) {
+                    const int r = i * 8 + lane_row, c = col0 + lane_col;
+                    const typename Epi::Ahead now = ahead;
+                    const int nr = i < 3 ? r + 8 : lane_row, nc = i < 3 ? c : c + 32;
+                    if (nr < rows && nc < p.n && (i < 3 || next)) epi.load(ahead, g.batch, row0 + nr, nc, p.n - nc);
+                    if (r < rows && c < p.n) {
+                        float v[8];
+                        staged8(stage, r, lane_col, v);
+                        epi.eight(v, now, g.batch, row0 + r, c, p.n - c);
+                    }
+                }
+                }
+            };
+            const auto start = [&] {
+                if constexpr (!Epi::kDual)
+                    if (epi.wide() && lane_row < rows && from + lane_col < p.n) epi.load(ahead, g.batch, row0 + lane_row, from + lane_col, p.n - from - lane_col);
+            };
+            // The same of two arrays.
+            const auto block2 = [&](const float(&a)[32], const float(&b)[32], int col0) {
+                if constexpr (Epi::kDual) {
+                stage_rows(a, stage, lane);
+                if (!epi.wide() && col0 + lane < p.n)
+#pragma unroll 1
+                    for (int r = 0; r < min(rows, 32); ++r) epi.keep(0, staged1(stage, r, lane), g.batch, row0 + r, col0 + lane);
+                float v[4][8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) staged8(stage, i * 8 + lane_row, lane_col, v[i]);
+                stage_rows(b, stage, lane);
+                if (!epi.wide() && col0 + lane < p.n)
+#pragma unroll 1
+                    for (int r = 0; r < min(rows, 32); ++r) epi.keep(1, staged1(stage, r, lane), g.batch, row0 + r, col0 + lane);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = i * 8 + lane_row, c = col0 + lane_col;
+                    float w[8];
+                    staged8(stage, r, lane_col, w);
+                    if (r < rows && c < p.n) epi.eight(v[i], w, g.batch, row0 + r, c, p.n - c);
+                }
+                }
+            };
             if constexpr (CHUNKED) {
                 constexpr int slabs = BN / 64;   // kDual: those of the first array, then those of the second
                 float acc[slabs][32];
@@ -498,21 +504,35 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                     if (lane == 0) arrive_cluster(release + 8 * buf);
                 }
                 if (!ok) break;
-                if (row0 >= p.m) continue;
-#pragma unroll
+                if (rows <= 0) continue;
+                if constexpr (!Epi::kDual) start();
+#pragma unroll 1
                 for (int j = 0; j < (Epi::kDual ? slabs / 2 : slabs); ++j) {
                     const int col0 = from + 32 * j;
-                    if (col0 >= p.n) continue;
-                    epi.load(ahead, lane, g.batch, row0, col0);
-                    epi(acc[j], acc[Epi::kDual ? j + slabs / 2 : j], ahead, stage, lane, g.batch, row0, col0);
+                    if (col0 >= p.n) break;
+                    if constexpr (Epi::kDual) {
+                        float a[32], b[32];
+#pragma unroll
+                        for (int q = 0; q < slabs / 2; ++q)
+                            if (q == j)
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) a[i] = acc[q][i], b[i] = acc[q + slabs / 2][i];
+                        block2(a, b, col0);
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < slabs; ++q)
+                            if (q == j) stage_rows(acc[q], stage, lane);
+                        block(col0, j + 1 < slabs);
+                    }
                 }
             } else {
                 const uint32_t buf = sums & 1;
-                if (row0 < p.m && from < p.n) epi.load(ahead, lane, g.batch, row0, from);
+                if constexpr (!Epi::kDual) start();
                 ok = __all_sync(~0u, w.wait(acc_full + 8 * buf, (sums / 2) & 1));
                 if (!ok) break;
                 ++sums;
                 tmem_fence_after();
+#pragma unroll 1
                 for (int c = 0; c < width; c += 32) {
                     float a[32], b[32];
                     const uint32_t at = lanes + buf * 256 + half * width + c;
@@ -525,10 +545,13 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                         if (lane == 0) arrive_cluster(release + 8 * buf);
                     }
                     const int col0 = from + c;
-                    if (row0 >= p.m || col0 >= p.n) continue;
-                    const typename Epi::Ahead now = ahead;
-                    if (c + 32 < width && col0 + 32 < p.n) epi.load(ahead, lane, g.batch, row0, col0 + 32);
-                    epi(a, Epi::kDual ? b : a, now, stage, lane, g.batch, row0, col0);
+                    if (rows <= 0 || col0 >= p.n) continue;
+                    if constexpr (Epi::kDual) {
+                        block2(a, b, col0);
+                    } else {
+                        stage_rows(a, stage, lane);
+                        block(col0, c + 32 < width);
+                    }
                 }
             }
         }

@@ -30,12 +30,9 @@ __global__ void __launch_bounds__(256) square_sum_kernel(const T* m, int64_t ld,
         const int col = (int)(i - r * chunks) * 8, n = (int)min((int64_t)8, cols - col);
         float v[8];
         const T* at = base + r * ld + col;
-        if (vec) {
-            load_values<T, 8>(at, n, v);
-        } else {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = k < n ? to_f32(at[k]) : 0.f;
-        }
+        Raw<T> x8;
+        x8.load(at, n, vec);
+        x8.values(v);
 #pragma unroll
         for (int k = 0; k < 8; ++k) sum += (double)v[k] * v[k];
     }
@@ -84,16 +81,13 @@ __global__ void __launch_bounds__(256) start_kernel(const T* m, int64_t ld, int6
         const int col = (int)(i - r * chunks) * 8, n = (int)min((int64_t)8, cols - col);
         float v[8];
         const T* at = base + r * ld + col;
-        if (vec) {
-            load_values<T, 8>(at, n, v);
-        } else {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = k < n ? to_f32(at[k]) : 0.f;
-        }
+        Raw<T> x8;
+        x8.load(at, n, vec);
+        x8.values(v);
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = (float)(v[k] * power);
         const Pieces<__half> to{x.base + blockIdx.y * x.batch + r * x.ld + col, x.piece, 0, 0};
-        to.template store<P>(0, 0, 0, 8, v);
+        to.template store<P>(0, 0, 0, v);
     }
 }
 
@@ -102,46 +96,41 @@ template <int P>
 struct KeepPieces {
     static constexpr bool kDual = false;
     struct Ahead {
-        Raw<__half> r[4][P];
+        Raw<__half> r[P];
     };
     Pieces<__half> out, r;
     const float* kappa;
     float factor, beta, diagonal;
-    int32_t m, n, power, with_r;
+    int32_t power, with_r;
 
-    __device__ __forceinline__ void load(Ahead& ahead, int lane, int batch, int row0, int col0) const
+    __device__ __forceinline__ bool wide() const { return true; }
+    __device__ __forceinline__ void one(float, int, int, int) const {}
+    __device__ __forceinline__ void load(Ahead& ahead, int batch, int row, int col, int) const
     {
-        if (with_r)
-            ahead_of_rows(lane, [&](int i, int row, int c) {
-                if (row0 + row < m && col0 + c < n) r.template load<P>(batch, row0 + row, col0 + c, ahead.r[i]);
-            });
+        if (with_r) r.template load<P>(batch, row, col, ahead.r);
     }
-    __device__ __forceinline__ void operator()(float (&v)[32], float (&)[32], const Ahead& ahead, float* stage, int lane, int batch, int row0, int col0) const
+    __device__ __forceinline__ void eight(float (&v)[8], const Ahead& now, int batch, int row, int col, int) const
     {
         float a = factor;
         if (power) {
             const float k = kappa[batch];
             a *= power == 2 ? k * k : k;
         }
-        along_rows<true>(v, stage, lane, [&](int l, int row, int c, auto& x) {
-            const int i = row0 + row, j = col0 + c;
-            if (i >= m || j >= n) return;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) x[k] *= a;
-            if (with_r) {
+        for (int k = 0; k < 8; ++k) v[k] *= a;
+        if (with_r) {
 #pragma unroll
-                for (int q = P - 1; q >= 0; --q) {
-                    float s[8];
-                    ahead.r[l][q].values(s);
+            for (int q = P - 1; q >= 0; --q) {
+                float s[8];
+                now.r[q].values(s);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) x[k] += beta * s[k];
-                }
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (i == j + k) x[k] += diagonal;
+                for (int k = 0; k < 8; ++k) v[k] += beta * s[k];
             }
-            out.template store<P>(batch, i, j, n - j, x);
-        });
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (row == col + k) v[k] += diagonal;
+        }
+        out.template store<P>(batch, row, col, v);
     }
 };
 
@@ -149,22 +138,24 @@ struct KeepPieces {
 template <class T>
 struct LastStep {
     static constexpr bool kDual = false;
-    using Ahead = NothingAhead;
+    using Ahead = Raw<T>;
     T* out;
     int64_t ld, node;
     const float* kappa;
     float factor;
-    int32_t m, n, power, accumulate, vec;
+    int32_t power, accumulate, vec;
 
-    __device__ __forceinline__ void load(Ahead&, int, int, int, int) const {}
-    __device__ __forceinline__ void operator()(float (&v)[32], float (&)[32], const Ahead&, float* stage, int lane, int batch, int row0, int col0) const
+    __device__ __forceinline__ bool wide() const { return vec; }
+    __device__ __forceinline__ Rows<T> rows(int batch) const
     {
-        const float a = power ? factor * kappa[batch] : factor;
-        if (vec)
-            store_rows<true>(v, out + batch * node, ld, a, accumulate, m, n, stage, lane, row0, col0);
-        else
-            store_rows<false>(v, out + batch * node, ld, a, accumulate, m, n, stage, lane, row0, col0);
+        return {out + batch * node, ld, power ? factor * kappa[batch] : factor, accumulate != 0};
     }
+    __device__ __forceinline__ void load(Ahead& old, int batch, int row, int col, int left) const { rows(batch).ahead(old, row, col, left); }
+    __device__ __forceinline__ void eight(float (&v)[8], const Ahead& old, int batch, int row, int col, int left) const
+    {
+        rows(batch).eight(v, old, row, col, left);
+    }
+    __device__ __forceinline__ void one(float v, int batch, int row, int col) const { rows(batch).one(v, row, col); }
 };
 
 bool on_16(const void* p, int64_t ld, int64_t rows, int64_t node, int64_t nodes, int size)
@@ -243,7 +234,6 @@ cudaError_t orth(const OrthParams& p, cudaStream_t stream)
         g.a[0].mn_major = g.b[0].mn_major = tall;
         g.m = g.n = s;
         g.k[0] = std::max(p.r, p.c);
-        keep.m = keep.n = (int32_t)s;
         keep.out = pieces_of<__half>(q.a);
         keep.factor = 1.f / kScale;
         keep.power = first ? 2 : 0;
@@ -269,8 +259,6 @@ cudaError_t orth(const OrthParams& p, cudaStream_t stream)
         g.n = p.c;
         g.k[0] = s;
         if (i + 1 < p.steps) {
-            keep.m = (int32_t)p.r;
-            keep.n = (int32_t)p.c;
             keep.out = pieces_of<__half>(next);
             keep.factor = 1.f / kScale;
             keep.power = first;
@@ -283,8 +271,6 @@ cudaError_t orth(const OrthParams& p, cudaStream_t stream)
             last.node = p.node_ldo;
             last.kappa = q.kappa;
             last.factor = (float)(p.scale / ((double)kScale * kScale));
-            last.m = (int32_t)p.r;
-            last.n = (int32_t)p.c;
             last.power = first;
             last.accumulate = p.accumulate;
             last.vec = on_16(p.out, p.ldo, p.r, p.node_ldo, p.nodes, sizeof(T));

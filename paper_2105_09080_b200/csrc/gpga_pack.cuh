@@ -39,24 +39,16 @@ __global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackJ
         float v[8];
         const int64_t from = b * j.batch + r * j.ld + col;
         if (j.src_f32) {
-            const float* s = static_cast<const float*>(j.src) + from;
-            if (j.vec) {
-                load_values<float, 8>(s, n, v);
-            } else {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = k < n ? s[k] : 0.f;
-            }
+            Raw<float> x;
+            x.load(static_cast<const float*>(j.src) + from, n, j.vec);
+            x.values(v);
         } else {
-            const T16* s = static_cast<const T16*>(j.src) + from;
-            if (j.vec) {
-                load_values<T16, 8>(s, n, v);
-            } else {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = k < n ? to_f32(s[k]) : 0.f;
-            }
+            Raw<T16> x;
+            x.load(static_cast<const T16*>(j.src) + from, n, j.vec);
+            x.values(v);
         }
         const Pieces<T16> dst{static_cast<T16*>(j.dst) + c * 8, j.dst_piece, 0, 0};
-        dst.template store<P>(0, 0, 0, 8, v);
+        dst.template store<P>(0, 0, 0, v);
     }
 }
 
