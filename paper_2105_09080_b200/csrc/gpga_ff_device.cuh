@@ -7,30 +7,71 @@ namespace gpga {
 
 enum { kSilu = 0, kGelu = 1, kRelu = 2 };
 
-// act(v).  fp32 results take CUDA's expf; the fast form's error (2^-21 of the value and more beyond |v| = 8) is below the
-// rounding of 16-bit ones.
-template <bool FAST>
-__device__ __forceinline__ float act_value(float v, int kind)
+// 2^x and 1 / x by the special-function unit (errors of about 2^-22), results below 2^-126 as zero.
+__device__ __forceinline__ float fast_exp2(float x)
 {
-    if (kind == kSilu) return FAST ? __fdividef(v, 1.f + __expf(-v)) : v / (1.f + expf(-v));
-    if (kind == kGelu) return 0.5f * v * (1.f + erff(v * 0.70710678118654752f));
-    return v <= 0.f ? 0.f : v;    // NaN stays
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
-// act(v) and act'(v).
+__device__ __forceinline__ float fast_reciprocal(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// 1 / (1 + e^-v) and e^(-v^2 / 2).  fp32 results take CUDA's expf and division; the fast forms' errors are below the rounding
+// of 16-bit ones.
 template <bool FAST>
-__device__ __forceinline__ void act_slope(float v, int kind, float& a, float& s)
+__device__ __forceinline__ float sigmoid(float v)
+{
+    return FAST ? fast_reciprocal(1.f + fast_exp2(-1.44269504f * v)) : 1.f / (1.f + expf(-v));
+}
+template <bool FAST>
+__device__ __forceinline__ float bell(float v)
+{
+    return FAST ? fast_exp2(-0.72134752f * v * v) : expf(-0.5f * v * v);
+}
+
+// v <- act(v).
+template <bool FAST, int N>
+__device__ __forceinline__ void act_values(float (&v)[N], int kind)
 {
     if (kind == kSilu) {
-        const float sig = FAST ? __fdividef(1.f, 1.f + __expf(-v)) : 1.f / (1.f + expf(-v));
-        a = v * sig;
-        s = sig * (1.f + v * (1.f - sig));
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] *= sigmoid<FAST>(v[i]);
     } else if (kind == kGelu) {
-        const float c = 0.5f * (1.f + erff(v * 0.70710678118654752f));
-        a = v * c;
-        s = c + v * 0.39894228040143268f * (FAST ? __expf(-0.5f * v * v) : expf(-0.5f * v * v));
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] *= 0.5f * (1.f + erff(v[i] * 0.70710678118654752f));
     } else {
-        a = v <= 0.f ? 0.f : v;
-        s = v > 0.f ? 1.f : 0.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = v[i] <= 0.f ? 0.f : v[i];    // NaN stays
+    }
+}
+// v <- act(v), s = act'(v).
+template <bool FAST, int N>
+__device__ __forceinline__ void act_slopes(float (&v)[N], float (&s)[N], int kind)
+{
+    if (kind == kSilu) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float sig = sigmoid<FAST>(v[i]), a = v[i] * sig;
+            s[i] = fmaf(a, 1.f - sig, sig);
+            v[i] = a;
+        }
+    } else if (kind == kGelu) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float c = 0.5f * (1.f + erff(v[i] * 0.70710678118654752f));
+            s[i] = fmaf(v[i] * 0.39894228040143268f, bell<FAST>(v[i]), c);
+            v[i] *= c;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            s[i] = v[i] > 0.f ? 1.f : 0.f;
+            v[i] = v[i] <= 0.f ? 0.f : v[i];
+        }
     }
 }
 
@@ -42,6 +83,7 @@ template <> struct PiecesOf<float> { using type = __nv_bfloat16; static constexp
 template <class T>
 struct GateUp {
     static constexpr bool kDual = true;
+    static constexpr int kWarps = 16;
     using T16 = typename PiecesOf<T>::type;
     static constexpr int P = PiecesOf<T>::count;
     using Ahead = NothingAhead;
@@ -62,8 +104,9 @@ struct GateUp {
             store8(g + at * ldg + col, left, v);
             store8(u + at * ldu + col, left, w);
         }
+        act_values<sizeof(T) == 2>(v, kind);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = act_value<sizeof(T) == 2>(v[i], kind) * w[i];
+        for (int i = 0; i < 8; ++i) v[i] *= w[i];
         h.template store<P>(batch, row, col, v);
     }
 };
@@ -72,6 +115,7 @@ struct GateUp {
 template <class T>
 struct GateGrad {
     static constexpr bool kDual = false;
+    static constexpr int kWarps = 16;
     using T16 = typename PiecesOf<T>::type;
     static constexpr int P = PiecesOf<T>::count;
     struct Ahead {
@@ -92,20 +136,21 @@ struct GateGrad {
     }
     __device__ __forceinline__ void eight(float (&dh)[8], const Ahead& now, int batch, int row, int col, int) const
     {
-        float a[8], s[8], gu[8];
-        now.g.values(gu);
+        float a[8], s[8], uv[8];
+        now.g.values(a);
+        now.u.values(uv);
+        act_slopes<sizeof(T) == 2>(a, s, kind);
+        const int64_t at = h.at(batch, row, col);    // of all three
 #pragma unroll
-        for (int i = 0; i < 8; ++i) act_slope<sizeof(T) == 2>(gu[i], kind, a[i], s[i]);
-        now.u.values(gu);
+        for (int i = 0; i < 8; ++i) s[i] *= dh[i] * uv[i];
+        dg.template store_at<P>(at, s);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[i] *= dh[i] * gu[i];
-        dg.template store<P>(batch, row, col, s);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) gu[i] *= a[i];
-        h.template store<P>(batch, row, col, gu);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) a[i] *= dh[i];
-        du.template store<P>(batch, row, col, a);
+        for (int i = 0; i < 8; ++i) {
+            dh[i] *= a[i];
+            a[i] *= uv[i];
+        }
+        h.template store_at<P>(at, a);
+        du.template store_at<P>(at, dh);
     }
 };
 
@@ -113,6 +158,7 @@ struct GateGrad {
 template <class T>
 struct StoreRows {
     static constexpr bool kDual = false;
+    static constexpr int kWarps = 8;
     using Ahead = Raw<T>;
     T* out[2];
     int64_t ld[2], node[2];
@@ -142,7 +188,7 @@ template <int P, class Epi>
 cudaError_t launch_gemm(const GemmPlan& g, const Epi& epi, cudaStream_t stream)
 {
     if (g.m <= 128) return launch_gemm_as<Variant<1, 128, P>>(g, epi, stream);
-    return launch_gemm_as<Variant<2, 256, P>>(g, epi, stream);
+    return launch_gemm_as<Variant<2, 256, P, P == 1 ? Epi::kWarps : 8>>(g, epi, stream);
 }
 
 template <class T, int P>

@@ -36,9 +36,8 @@
 
 namespace gpga {
 
-constexpr int kGemmThreads = 384;
 constexpr int kTileK = 64;                                  // columns of k in a stage: 128 bytes
-constexpr int kStaging = 8 * 32 * 32 * 4;                   // bytes: 32 rows x 32 columns for each epilogue warp
+constexpr int kStagingWarp = 32 * 32 * 4;                   // bytes: 32 rows x 32 columns for each epilogue warp
 constexpr int kGemmHead = 1024;                             // barriers, before the operand stages
 constexpr int kGemmSmem = 227 * 1024;
 constexpr uint32_t kWaitTries = 1u << 20;                   // polls of up to some microseconds each: seconds
@@ -187,10 +186,16 @@ template <class T16>
 struct Pieces {
     T16* base;
     int64_t piece, batch, ld;
+    __device__ __forceinline__ int64_t at(int b, int row, int col) const { return b * batch + row * ld + col; }
     template <int P>
     __device__ __forceinline__ void store(int b, int row, int col, const float (&v)[8]) const
     {
-        T16* at = base + b * batch + row * ld + col;
+        store_at<P>(at(b, row, col), v);
+    }
+    template <int P>
+    __device__ __forceinline__ void store_at(int64_t place, const float (&v)[8]) const
+    {
+        T16* const to = base + place;
         uint32_t w[P][4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -214,14 +219,14 @@ struct Pieces {
             }
         }
 #pragma unroll
-        for (int q = 0; q < P; ++q) *reinterpret_cast<uint4*>(at + q * piece) = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
+        for (int q = 0; q < P; ++q) *reinterpret_cast<uint4*>(to + q * piece) = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
     }
     template <int P>
     __device__ __forceinline__ void load(int b, int row, int col, Raw<T16> (&r)[P]) const
     {
-        const T16* at = base + b * batch + row * ld + col;
+        const T16* const from = base + at(b, row, col);
 #pragma unroll
-        for (int q = 0; q < P; ++q) r[q].load(at + q * piece, 8, true);
+        for (int q = 0; q < P; ++q) r[q].load(from + q * piece, 8, true);
     }
 };
 
@@ -264,19 +269,20 @@ constexpr int kFewRegisters = 64, kManyRegisters = 208;
 // instructions (gradient epilogue, fp32: 147 us unrolled, see below for what it is now).
 struct NothingAhead {};
 
-// What a variant of the kernel has: tile columns (of a pair of blocks, where CG = 2), pieces, stages.
-template <int CG_, int BN_, int P_>
+// What a variant of the kernel has: tile columns (of a pair of blocks, where CG = 2), pieces, warps of the epilogue, stages.
+template <int CG_, int BN_, int P_, int WARPS_ = 8>
 struct Variant {
-    static constexpr int CG = CG_, BN = BN_, P = P_;
+    static constexpr int CG = CG_, BN = BN_, P = P_, warps = WARPS_, threads = 128 + 32 * warps, staging = warps * kStagingWarp;
     static constexpr bool chunked = P > 1;
+    static_assert(!chunked || warps == 8, "the registers of a CHUNKED kernel are split for eight warps");
     static constexpr uint32_t a_bytes = 128 * kTileK * 2, b_bytes = BN / CG * kTileK * 2, stage_bytes = a_bytes + b_bytes;
-    static constexpr uint32_t room = (kGemmSmem - 1024 - kGemmHead - kStaging) / stage_bytes;
+    static constexpr uint32_t room = (kGemmSmem - 1024 - kGemmHead - staging) / stage_bytes;
     static constexpr uint32_t stages = room < 8 ? room : 8;
     static constexpr int chunk = P == 3 ? 1 : 2;   // k-blocks of a chunk
 };
 
 template <class V, class Epi>
-__global__ void __launch_bounds__(kGemmThreads, 1)
+__global__ void __launch_bounds__(V::threads, 1)
     gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmParams p, const __grid_constant__ Epi epi)
 {
     extern __shared__ __align__(1024) unsigned char smem_raw[];
@@ -288,7 +294,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     uint32_t* const tmem_at = reinterpret_cast<uint32_t*>(smem + 160);
     volatile uint32_t* const stop = reinterpret_cast<volatile uint32_t*>(smem + 164);
     float* const staging = reinterpret_cast<float*>(smem + kGemmHead);
-    const uint32_t operands = base + kGemmHead + kStaging;
+    const uint32_t operands = base + kGemmHead + V::staging;
     constexpr int CG = V::CG, BN = V::BN, P = V::P;
     constexpr bool CHUNKED = V::chunked;
     constexpr uint32_t a_bytes = V::a_bytes, stage_bytes = V::stage_bytes, stages = V::stages;
@@ -305,7 +311,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(reinterpret_cast<uint64_t*>(smem + 128 + 8 * i), 1);
-            mbar_init(reinterpret_cast<uint64_t*>(smem + 144 + 8 * i), 8 * CG);
+            mbar_init(reinterpret_cast<uint64_t*>(smem + 144 + 8 * i), V::warps * CG);
         }
         *stop = 0;
         mbar_init_fence();
@@ -415,19 +421,20 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         __syncwarp();
     } else {
         if constexpr (CHUNKED) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegisters));
-        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        const int quarter = warp & 3, part = (warp - 4) >> 2;   // lanes of tensor memory, columns
         float* const stage = staging + (warp - 4) * 32 * 32;
         const uint32_t release = CG == 2 ? map_shared(acc_empty, 0) : acc_empty;
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
         uint32_t sums = 0;
         bool ok = true;
-        constexpr int width = BN / (Epi::kDual ? 4 : 2);   // columns of this warp (of each array)
+        constexpr int width = BN / (V::warps / 4) / (Epi::kDual ? 2 : 1);   // columns of this warp (of each array)
         const int lane_row = lane >> 2, lane_col = (lane & 3) * 8;
         for (int t = first; t < p.tiles && ok; t += step) {
             const GemmTile g = gemm_tile(p, t, 128 * CG, BN);
-            const int row0 = g.m0 + (int)rank * 128 + quarter * 32, from = (Epi::kDual ? g.n0 / 2 : g.n0) + half * width;
+            const int row0 = g.m0 + (int)rank * 128 + quarter * 32, from = (Epi::kDual ? g.n0 / 2 : g.n0) + part * width;
             const int rows = p.m - row0;   // that are there
-            typename Epi::Ahead ahead;
+            constexpr int kAhead = CHUNKED ? 1 : 2;   // calls of eight() that are read ahead
+            typename Epi::Ahead ahead[kAhead];
             // A 32 x 32 block that is staged; `next`: whether the block to the right follows.
             const auto block = [&](int col0, bool next) {
                 if constexpr (!Epi::kDual) {
@@ -438,22 +445,29 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                     return;
                 }
 #pragma unroll 1
-                for (int i = 0; i < 4; ++i) {
-                    const int r = i * 8 + lane_row, c = col0 + lane_col;
-                    const typename Epi::Ahead now = ahead;
-                    const int nr = i < 3 ? r + 8 : lane_row, nc = i < 3 ? c : c + 32;
-                    if (nr < rows && nc < p.n && (i < 3 || next)) epi.load(ahead, g.batch, row0 + nr, nc, p.n - nc);
-                    if (r < rows && c < p.n) {
-                        float v[8];
-                        staged8(stage, r, lane_col, v);
-                        epi.eight(v, now, g.batch, row0 + r, c, p.n - c);
+                for (int i = 0; i < 4; i += kAhead) {
+#pragma unroll
+                    for (int j = 0; j < kAhead; ++j) {
+                        const int r = (i + j) * 8 + lane_row, c = col0 + lane_col;
+                        const typename Epi::Ahead now = ahead[j];
+                        const bool here = i + kAhead < 4;
+                        const int nr = here ? r + 8 * kAhead : j * 8 + lane_row, nc = here ? c : c + 32;
+                        if (nr < rows && nc < p.n && (here || next)) epi.load(ahead[j], g.batch, row0 + nr, nc, p.n - nc);
+                        if (r < rows && c < p.n) {
+                            float v[8];
+                            staged8(stage, r, lane_col, v);
+                            epi.eight(v, now, g.batch, row0 + r, c, p.n - c);
+                        }
                     }
                 }
                 }
             };
             const auto start = [&] {
                 if constexpr (!Epi::kDual)
-                    if (epi.wide() && lane_row < rows && from + lane_col < p.n) epi.load(ahead, g.batch, row0 + lane_row, from + lane_col, p.n - from - lane_col);
+#pragma unroll
+                    for (int j = 0; j < kAhead; ++j)
+                        if (epi.wide() && j * 8 + lane_row < rows && from + lane_col < p.n)
+                            epi.load(ahead[j], g.batch, row0 + j * 8 + lane_row, from + lane_col, p.n - from - lane_col);
             };
             // The same of two arrays.
             const auto block2 = [&](const float(&a)[32], const float(&b)[32], int col0) {
@@ -492,7 +506,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                     tmem_fence_after();
 #pragma unroll
                     for (int j = 0; j < slabs; ++j) {
-                        const uint32_t at = lanes + buf * 256 + half * width + (Epi::kDual ? (j % (slabs / 2)) * 32 + j / (slabs / 2) * (BN / 2) : j * 32);
+                        const uint32_t at = lanes + buf * 256 + part * width + (Epi::kDual ? (j % (slabs / 2)) * 32 + j / (slabs / 2) * (BN / 2) : j * 32);
                         float a[32];
                         tmem_load32(at, a);
                         tmem_wait_load();
@@ -535,7 +549,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 #pragma unroll 1
                 for (int c = 0; c < width; c += 32) {
                     float a[32], b[32];
-                    const uint32_t at = lanes + buf * 256 + half * width + c;
+                    const uint32_t at = lanes + buf * 256 + part * width + c;
                     tmem_load32(at, a);
                     if constexpr (Epi::kDual) tmem_load32(at + BN / 2, b);
                     tmem_wait_load();
@@ -638,12 +652,12 @@ cudaError_t launch_gemm_as(const GemmPlan& g, const Epi& epi, cudaStream_t strea
     if (e != cudaSuccess) return e;
     if (V::chunked) {
         static const int registers = kernel_registers(kernel);
-        if (registers * kGemmThreads < 128 * (kFewRegisters + 2 * kManyRegisters)) return cudaErrorLaunchOutOfResources;
+        if (registers * V::threads < 128 * (kFewRegisters + 2 * kManyRegisters)) return cudaErrorLaunchOutOfResources;
     }
     const int64_t blocks = std::min<int64_t>(tiles, sm_count() / CG) * CG;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)blocks);
-    cfg.blockDim = dim3(kGemmThreads);
+    cfg.blockDim = dim3(V::threads);
     cfg.dynamicSmemBytes = kGemmSmem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
