@@ -12,7 +12,7 @@ CSRC = PKG / "csrc"
 LIB = PKG / "libgpga.so"
 SOURCES = ["gpga_api.cu", "gpga_kernels.cu", "gpga_tile.cu", "gpga_logreg.cu", "gpga_logrun.cu", "gpga_noalloc.cu", "gpga_loss.cu", "gpga_shard.cu",
            "gpga_dropout.cu", "gpga_norm.cu", "gpga_norm_grad.cu", "gpga_embed.cu", "gpga_token_api.cu",
-           "gpga_gemm.cu", "gpga_ff_forward.cu", "gpga_ff_backward.cu", "gpga_orth.cu", "gpga_matrix_api.cu"]
+           "gpga_gemm.cu", "gpga_ff_forward.cu", "gpga_ff_few.cu", "gpga_ff_backward.cu", "gpga_orth.cu", "gpga_matrix_api.cu"]
 
 
 def nvcc_path() -> str:

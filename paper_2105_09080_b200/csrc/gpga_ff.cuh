@@ -19,6 +19,12 @@ struct FeedForwardParams {
     char* scratch = nullptr;
 };
 
+// Tokens per node up to which the forward pass reads the weights where they lie, without the tensor memory path: up to
+// there its time is that of reading them.
+inline bool ff_few(const FeedForwardParams& p) { return p.rows <= (p.dtype == 0 ? 8 : 32); }
+int64_t ff_few_scratch_bytes(const FeedForwardParams& p);
+cudaError_t launch_ff_few(const FeedForwardParams& p, cudaStream_t stream);
+
 int64_t ff_forward_scratch_bytes(const FeedForwardParams& p);
 int64_t ff_backward_scratch_bytes(const FeedForwardParams& p);
 cudaError_t launch_ff_forward(const FeedForwardParams& p, cudaStream_t stream);

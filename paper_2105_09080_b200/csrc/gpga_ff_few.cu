@@ -1,0 +1,391 @@
+// Gated feed-forward block of few tokens per node (a trained model answering): every weight is read once, straight from where it lies,
+// and that is what bounds it.
+//
+// Two launches, h = act(x Wg^T) (x Wu^T) and y = h Wd^T.  A cluster of up to eight blocks takes 16 rows of the weights (fp32:
+// 4), its warps a part of k each, so that all that is to be read is soon in flight; their sums are added through the
+// cluster's shared memory in a fixed order.  16-bit activations: the weights are the rows of
+// m16n8k16 matrix instructions and the tokens their columns; as a sum over k may run in any order, a lane takes eight
+// neighbouring k (128 or 256 bits of weights, 128 of x) and both operands use them in the same places of two instructions.
+// The tensor memory path would need its 128 rows through shared memory first; at up to 32 tokens the instructions are not
+// what bounds.  fp32 activations: fp32 arithmetic.  The second launch starts while the first runs and asks for its weights
+// to be brought into L2 meanwhile.
+#include <type_traits>
+
+#include "gpga_ff_device.cuh"
+
+namespace gpga {
+
+namespace {
+
+struct FewParams {
+    const void *x, *w1, *w2;        // w2: the second projection (nullptr: only one product)
+    int64_t ldx, ld1, node1, ld2, node2;
+    void *out, *g, *u;              // out: h or y
+    int64_t ldo, ldg, ldu;
+    int32_t tokens, rows, k, kind, vec_x, vec_w, after, blocks;   // rows: of the weights; blocks: of a cluster
+};
+
+template <class T>
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], const uint32_t (&b)[2])
+{
+    if constexpr (std::is_same<T, __half>::value)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+
+// Eight weights as four pairs of the activations' type.
+template <class T, class W>
+__device__ __forceinline__ void as_pairs(const Raw<W>& r, uint32_t (&o)[4])
+{
+    if constexpr (sizeof(W) == 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = r.w[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = pack16(__uint_as_float(r.w[2 * i]), __uint_as_float(r.w[2 * i + 1]), T());
+    }
+}
+
+// What is done with a finished sum of both projections (or of the one): g, u, h, or y.
+template <class T, class H, bool GATE>
+__device__ __forceinline__ void finish(const FewParams& p, int node, int token, int row, float a, float b)
+{
+    const int64_t t = (int64_t)node * p.tokens + token;
+    if constexpr (GATE) {
+        if (p.g) {
+            static_cast<T*>(p.g)[t * p.ldg + row] = from_f32<T>(a);
+            static_cast<T*>(p.u)[t * p.ldu + row] = from_f32<T>(b);
+        }
+        float v[1] = {a};
+        act_values<sizeof(T) == 2>(v, p.kind);
+        static_cast<H*>(p.out)[t * p.ldo + row] = from_f32<H>(v[0] * b);
+    } else {
+        static_cast<T*>(p.out)[t * p.ldo + row] = from_f32<T>(a);
+    }
+}
+
+// Asks for this warp's part of the weights while the kernel before it runs.
+template <class W, int ROWS>
+__device__ __forceinline__ void ask_ahead(const W* w, int64_t ld, int row0, int rows, int k0, int k1, int lane)
+{
+    if (k0 >= k1) return;
+    const int bytes = (k1 - k0) * (int)sizeof(W), lines = (bytes + 127) / 128 + 1;
+    for (int i = lane; i < ROWS * lines; i += 32) {
+        const int r = i / lines, l = i - r * lines;
+        if (row0 + r >= rows) break;
+        const char* const at = reinterpret_cast<const char*>(w + (row0 + r) * ld + k0);
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(at + min(l * 128, bytes - 1)));
+    }
+}
+
+constexpr int kFewWarps = 8;
+
+// Sum of value i of every warp of the cluster, in the order of k.  sums: this block's [warp][count].
+__device__ __forceinline__ float cluster_sum(const float* sums, int i, int count, uint32_t blocks)
+{
+    float s = 0.f;
+    for (uint32_t b = 0; b < blocks; ++b) {
+        const uint32_t at = map_shared(smem_u32(sums + i), b);
+#pragma unroll
+        for (int v = 0; v < kFewWarps; ++v) {
+            float x;
+            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(at + 4 * v * count));
+            s += x;
+        }
+    }
+    return s;
+}
+
+// NT tiles of eight tokens.
+template <class T, class W, int NT, bool GATE>
+__global__ void __launch_bounds__(kFewWarps * 32) few_tokens_kernel(const __grid_constant__ FewParams p)
+{
+    constexpr int M = GATE ? 2 : 1, R = 16, N = 8 * NT;
+    constexpr int S = R + 4;   // a token's rows in `sums`: no two lanes of a store meet in a bank
+    __shared__ __align__(16) float sums[kFewWarps * M * N * S];   // [warp][array][token][row]
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, node = blockIdx.y, row0 = (int)(blockIdx.x / p.blocks) * R;
+    const int group = lane >> 2, place = (lane & 3) * 8;
+    const uint32_t rank = cluster_rank();
+    const int parts = kFewWarps * p.blocks, steps = (p.k + 31) / 32, each = (steps + parts - 1) / parts;
+    const int k0 = min(((int)rank * kFewWarps + warp) * each * 32, p.k), k1 = min(k0 + each * 32, p.k);
+    const W* w[M];
+    int64_t ld[M];
+    w[0] = static_cast<const W*>(p.w1) + node * p.node1;
+    ld[0] = p.ld1;
+    if constexpr (GATE) {
+        w[1] = static_cast<const W*>(p.w2) + node * p.node2;
+        ld[1] = p.ld2;
+    }
+    grid_launch_dependents();
+    if (p.after) {
+        ask_ahead<W, R>(w[0], ld[0], row0, p.rows, k0, k1, lane);
+        grid_dependency_wait();
+    }
+    const T* const x = static_cast<const T*>(p.x) + (int64_t)node * p.tokens * p.ldx;
+
+    // Rows and tokens past the last are read as the last: their sums are dropped.
+    const W* wr[M][2];
+    const T* xr[NT];
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) wr[m][h] = w[m] + min(row0 + 8 * h + group, p.rows - 1) * ld[m] + place;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) xr[n] = x + min(8 * n + group, p.tokens - 1) * p.ldx + place;
+    float acc[M][NT][4] = {};
+    const auto multiply = [&](const Raw<W>(&wv)[M][2], const Raw<T>(&xv)[NT]) {
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            uint32_t lo[4], hi[4];
+            as_pairs<T>(wv[m][0], lo);
+            as_pairs<T>(wv[m][1], hi);
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const uint32_t a[4] = {lo[2 * s], hi[2 * s], lo[2 * s + 1], hi[2 * s + 1]};
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const uint32_t b[2] = {xv[n].w[2 * s], xv[n].w[2 * s + 1]};
+                    mma16816<T>(acc[m][n], a, b);
+                }
+            }
+        }
+    };
+    // Whole steps of aligned rows, U of them asked for at once; then what is left, or all of it.
+    constexpr int step_registers = M * 2 * 2 * (int)sizeof(W) + NT * 4, U = step_registers * 6 <= 80 ? 6 : step_registers * 4 <= 80 ? 4 : step_registers * 2 <= 80 ? 2 : 1;
+    int k = k0;
+    if (p.vec_w && p.vec_x) {
+        const int whole = min(k1, p.k / 32 * 32);
+        for (; k + 32 * U <= whole; k += 32 * U) {
+            Raw<W> wv[U][M][2];
+            Raw<T> xv[U][NT];
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+#pragma unroll
+                for (int m = 0; m < M; ++m)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) wv[j][m][h].load16(wr[m][h] + k + 32 * j);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) xv[j][n].load16(xr[n] + k + 32 * j);
+            }
+#pragma unroll
+            for (int j = 0; j < U; ++j) multiply(wv[j], xv[j]);
+        }
+    }
+#pragma unroll 1
+    for (; k < k1; k += 32) {
+        Raw<W> wv[M][2];
+        Raw<T> xv[NT];
+        const int left = p.k - k - place;
+#pragma unroll
+        for (int m = 0; m < M; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) wv[m][h].load(wr[m][h] + k, left, p.vec_w);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) xv[n].load(xr[n] + k, left, p.vec_x);
+        multiply(wv, xv);
+    }
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sums[((warp * M + m) * N + 8 * n + 2 * (lane & 3) + (e & 1)) * S + 8 * (e >> 1) + group] = acc[m][n][e];
+    cluster_barrier();
+    for (int i = (int)rank * kFewWarps * 32 + threadIdx.x; i < R * N; i += p.blocks * kFewWarps * 32) {
+        const int r = i % R, n = i / R;
+        if (row0 + r >= p.rows || n >= p.tokens) continue;
+        float s[M];
+#pragma unroll
+        for (int m = 0; m < M; ++m) s[m] = cluster_sum(sums, (m * N + n) * S + r, M * N * S, p.blocks);
+        finish<T, T, GATE>(p, node, n, row0 + r, s[0], s[M - 1]);
+    }
+    cluster_barrier();   // nobody goes while its sums are read
+}
+
+// fp32: R rows of the weights and N tokens to a block, its warps a part of k each.
+template <int N, bool GATE>
+__global__ void __launch_bounds__(kFewWarps * 32) few_tokens_f32_kernel(const __grid_constant__ FewParams p)
+{
+    constexpr int M = GATE ? 2 : 1, R = 4;
+    __shared__ __align__(16) float sums[kFewWarps * M * R * N];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, node = blockIdx.y, row0 = (int)(blockIdx.x / p.blocks) * R;
+    const uint32_t rank = cluster_rank();
+    const int parts = kFewWarps * p.blocks, steps = (p.k + 127) / 128, each = (steps + parts - 1) / parts;
+    const int k0 = min(((int)rank * kFewWarps + warp) * each * 128, p.k), k1 = min(k0 + each * 128, p.k);
+    const float* w[M];
+    int64_t ld[M];
+    w[0] = static_cast<const float*>(p.w1) + node * p.node1;
+    ld[0] = p.ld1;
+    if constexpr (GATE) {
+        w[1] = static_cast<const float*>(p.w2) + node * p.node2;
+        ld[1] = p.ld2;
+    }
+    grid_launch_dependents();
+    if (p.after) {
+        ask_ahead<float, R>(w[0], ld[0], row0, p.rows, k0, k1, lane);
+        grid_dependency_wait();
+    }
+    const float* const x = static_cast<const float*>(p.x) + (int64_t)node * p.tokens * p.ldx;
+    const auto four = [](const float* q, int n) {
+        if (n >= 4) return make_float4(q[0], q[1], q[2], q[3]);
+        return make_float4(n > 0 ? q[0] : 0.f, n > 1 ? q[1] : 0.f, n > 2 ? q[2] : 0.f, 0.f);
+    };
+    // Rows and tokens past the last are read as the last: their sums are dropped.
+    const float* wr[M][R];
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int r = 0; r < R; ++r) wr[m][r] = w[m] + min(row0 + r, p.rows - 1) * ld[m] + 4 * lane;
+    float acc[M][R][N] = {};
+    const auto multiply = [&](const float4(&wv)[M][R], int n, const float4& v) {
+#pragma unroll
+        for (int m = 0; m < M; ++m)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                acc[m][r][n] = fmaf(wv[m][r].w, v.w, fmaf(wv[m][r].z, v.z, fmaf(wv[m][r].y, v.y, fmaf(wv[m][r].x, v.x, acc[m][r][n]))));
+    };
+    int k = k0;
+    if (p.vec_w && p.vec_x)
+        for (; k + 128 <= min(k1, p.k); k += 128) {
+            float4 wv[M][R];
+#pragma unroll
+            for (int m = 0; m < M; ++m)
+#pragma unroll
+                for (int r = 0; r < R; ++r) wv[m][r] = *reinterpret_cast<const float4*>(wr[m][r] + k);
+#pragma unroll
+            for (int n = 0; n < N; ++n) multiply(wv, n, *reinterpret_cast<const float4*>(x + min(n, p.tokens - 1) * p.ldx + 4 * lane + k));
+        }
+#pragma unroll 1
+    for (; k < k1; k += 128) {
+        const int left = p.k - k - 4 * lane;
+        float4 wv[M][R];
+#pragma unroll
+        for (int m = 0; m < M; ++m)
+#pragma unroll
+            for (int r = 0; r < R; ++r) wv[m][r] = four(wr[m][r] + k, left);
+#pragma unroll
+        for (int n = 0; n < N; ++n) multiply(wv, n, four(x + min(n, p.tokens - 1) * p.ldx + 4 * lane + k, left));
+    }
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                float s = acc[m][r][n];
+#pragma unroll
+                for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(~0u, s, o);
+                if (lane == 0) sums[(warp * M * R + m * R + r) * N + n] = s;
+            }
+    cluster_barrier();
+    const int i = (int)rank * kFewWarps * 32 + threadIdx.x;
+    if (i < R * N) {
+        const int r = i % R, n = i / R;
+        if (row0 + r < p.rows && n < p.tokens) {
+            float s[M];
+#pragma unroll
+            for (int m = 0; m < M; ++m) s[m] = cluster_sum(sums, (m * R + r) * N + n, M * R * N, p.blocks);
+            finish<float, float, GATE>(p, node, n, row0 + r, s[0], s[M - 1]);
+        }
+    }
+    cluster_barrier();
+}
+
+// Blocks of a cluster: more while the launch has less than a block per SM and every warp still has two steps of k.
+cudaError_t launch_clusters(void (*kernel)(FewParams), FewParams p, int rows, int step, int64_t nodes, cudaStream_t stream)
+{
+    const int64_t tiles = (p.rows + rows - 1) / rows;
+    p.blocks = 1;
+    while (p.blocks < 8 && tiles * nodes * p.blocks < sm_count() && p.k >= p.blocks * 2 * kFewWarps * step * 2) p.blocks *= 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(tiles * p.blocks), (unsigned)nodes);
+    cfg.blockDim = dim3(kFewWarps * 32);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)p.blocks;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = p.after ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, p);
+}
+
+template <class T, class W, bool GATE>
+cudaError_t few16(const FewParams& p, int64_t nodes, cudaStream_t stream)
+{
+    const auto kernel = p.tokens <= 8 ? few_tokens_kernel<T, W, 1, GATE> : p.tokens <= 16 ? few_tokens_kernel<T, W, 2, GATE> : few_tokens_kernel<T, W, 4, GATE>;
+    return launch_clusters(kernel, p, 16, 32, nodes, stream);
+}
+
+template <bool GATE>
+cudaError_t few32(const FewParams& p, int64_t nodes, cudaStream_t stream)
+{
+    const auto kernel = p.tokens == 1 ? few_tokens_f32_kernel<1, GATE> : p.tokens <= 4 ? few_tokens_f32_kernel<4, GATE> : few_tokens_f32_kernel<8, GATE>;
+    return launch_clusters(kernel, p, 4, 128, nodes, stream);
+}
+
+template <bool GATE>
+cudaError_t few(const FeedForwardParams& q, const FewParams& p, cudaStream_t stream)
+{
+    if (q.dtype == 0) return few32<GATE>(p, q.nodes, stream);
+    if (q.dtype == 1) return q.weight_dtype == 0 ? few16<__nv_bfloat16, float, GATE>(p, q.nodes, stream) : few16<__nv_bfloat16, __nv_bfloat16, GATE>(p, q.nodes, stream);
+    return q.weight_dtype == 0 ? few16<__half, float, GATE>(p, q.nodes, stream) : few16<__half, __half, GATE>(p, q.nodes, stream);
+}
+
+}  // namespace
+
+int64_t ff_few_scratch_bytes(const FeedForwardParams& p) { return p.nodes * p.rows * ((p.f + 7) / 8 * 8) * (p.dtype == 0 ? 4 : 2); }
+
+cudaError_t launch_ff_few(const FeedForwardParams& q, cudaStream_t stream)
+{
+    const int size = q.dtype == 0 ? 4 : 2, wsize = q.weight_dtype == 0 ? 4 : 2;
+    const int64_t ldh = (q.f + 7) / 8 * 8;
+    FewParams p;
+    p.x = q.x.p;
+    p.ldx = q.x.ld;
+    p.vec_x = rows_on_16(q.x.p, q.x.ld, q.nodes * q.rows, 0, 1, size);
+    p.w1 = q.gate.p;
+    p.ld1 = q.gate.ld;
+    p.node1 = q.gate.node;
+    p.w2 = q.up.p;
+    p.ld2 = q.up.ld;
+    p.node2 = q.up.node;
+    p.vec_w = rows_on_16(q.gate.p, q.gate.ld, q.f, q.gate.node, q.nodes, wsize) && rows_on_16(q.up.p, q.up.ld, q.f, q.up.node, q.nodes, wsize);
+    p.out = q.scratch;
+    p.ldo = ldh;
+    p.g = q.g.p;
+    p.u = q.u.p;
+    p.ldg = q.g.ld;
+    p.ldu = q.u.ld;
+    p.tokens = (int32_t)q.rows;
+    p.rows = (int32_t)q.f;
+    p.k = (int32_t)q.d;
+    p.kind = q.activation;
+    p.after = 0;
+    const cudaError_t e = few<true>(q, p, stream);
+    if (e != cudaSuccess) return e;
+    p.x = q.scratch;
+    p.ldx = ldh;
+    p.vec_x = 1;
+    p.w1 = q.down.p;
+    p.ld1 = q.down.ld;
+    p.node1 = q.down.node;
+    p.vec_w = rows_on_16(q.down.p, q.down.ld, q.d, q.down.node, q.nodes, wsize);
+    p.out = q.y.p;
+    p.ldo = q.y.ld;
+    p.g = p.u = nullptr;
+    p.rows = (int32_t)q.d;
+    p.k = (int32_t)q.f;
+    p.after = 1;
+    return few<false>(q, p, stream);
+}
+
+}  // namespace gpga

@@ -70,10 +70,14 @@ unsigned int* ff_forward_gave_up()
     return cudaGetSymbolAddress(&at, gave_up) == cudaSuccess ? static_cast<unsigned int*>(at) : nullptr;
 }
 
-int64_t ff_forward_scratch_bytes(const FeedForwardParams& p) { return p.rows ? plan_forward(p).pack.scratch.bytes : 0; }
+int64_t ff_forward_scratch_bytes(const FeedForwardParams& p) 
+{
+    return !p.rows ? 0 : ff_few(p) ? ff_few_scratch_bytes(p) : plan_forward(p).pack.scratch.bytes;
+}
 
 cudaError_t launch_ff_forward(const FeedForwardParams& p, cudaStream_t stream)
 {
+    if (ff_few(p)) return launch_ff_few(p, stream);
     if (p.dtype == 0) return forward<float>(p, stream);
     if (p.dtype == 1) return forward<__nv_bfloat16>(p, stream);
     return forward<__half>(p, stream);

@@ -121,14 +121,18 @@ __device__ __forceinline__ float staged1(const float* stage, int row, int c) { r
 template <class T>
 struct Raw {
     uint32_t w[2 * sizeof(T)];
+    __device__ __forceinline__ void load16(const T* p)    // all eight, p on 16 bytes
+    {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+            const uint4 q = reinterpret_cast<const uint4*>(p)[i];
+            w[4 * i] = q.x, w[4 * i + 1] = q.y, w[4 * i + 2] = q.z, w[4 * i + 3] = q.w;
+        }
+    }
     __device__ __forceinline__ void load(const T* p, int n, bool vec)
     {
         if (vec && n >= 8) {
-#pragma unroll
-            for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-                const uint4 q = reinterpret_cast<const uint4*>(p)[i];
-                w[4 * i] = q.x, w[4 * i + 1] = q.y, w[4 * i + 2] = q.z, w[4 * i + 3] = q.w;
-            }
+            load16(p);
             return;
         }
         if constexpr (sizeof(T) == 4) {
