@@ -44,6 +44,12 @@ constexpr uint32_t kWaitTries = 1u << 20;                   // polls of up to so
 
 static __device__ unsigned int gave_up;                     // one per file that launches products
 
+// Instruction descriptor: fp32 accumulator, A and B fp16 or bfloat16.
+__host__ __device__ constexpr uint32_t mma_descriptor(int m, int n, bool half, bool a_mn, bool b_mn)
+{
+    return 1u << 4 | (half ? 0u : 1u << 7 | 1u << 10) | (uint32_t)a_mn << 15 | (uint32_t)b_mn << 16 | (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24;
+}
+
 struct GemmMaps {
     CUtensorMap a[2], b[2];
 };
@@ -641,8 +647,7 @@ cudaError_t launch_gemm_as(const GemmPlan& g, const Epi& epi, cudaStream_t strea
     p.tiles = (int32_t)tiles;
     p.a_mn = g.a[0].mn_major;
     p.b_mn = g.b[0].mn_major;
-    p.idesc = 1u << 4 | (g.half ? 0u : 1u << 7 | 1u << 10) | (uint32_t)p.a_mn << 15 | (uint32_t)p.b_mn << 16 | (uint32_t)(bn >> 3) << 17 |
-              (uint32_t)(128 * CG >> 4) << 24;
+    p.idesc = mma_descriptor(128 * CG, bn, g.half, p.a_mn, p.b_mn);
     const int b_rows = p.b_mn ? 64 : Epi::kDual ? bn / 2 : bn / CG;
     for (int i = 0; i < 2; ++i) {
         const bool b_there = i == 0 || g.segments > 1 || Epi::kDual;

@@ -46,6 +46,16 @@ __global__ void __launch_bounds__(256) square_sum_kernel(const T* m, int64_t ld,
     }
 }
 
+// What M is multiplied by to be S X_0: S / norm, or the power of two below it.  An infinity or NaN in M makes it NaN.
+__device__ __forceinline__ double start_factor(double norm, bool whole)
+{
+    if (norm == 0) return 1;                   // M = 0 and eps = 0
+    if (!(norm <= 1e300)) return whole ? nan("") : 1;
+    int e;
+    frexp(kScale / norm, &e);
+    return whole ? kScale / norm : ldexp(0.5, e);
+}
+
 // M times a power of two as fp16 pieces, and kappa.
 template <class T, int P>
 __global__ void __launch_bounds__(256) start_kernel(const T* m, int64_t ld, int64_t node, int64_t rows, int64_t cols, int vec, const double* parts,
@@ -59,17 +69,8 @@ __global__ void __launch_bounds__(256) start_kernel(const T* m, int64_t ld, int6
         for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
         if (threadIdx.x == 0) {
             const double norm = sqrt(sum) + eps;
-            double power = 1, rest = 1;
-            if (norm > 0 && norm <= 1e300) {
-                int e;
-                const double f = frexp(kScale / norm, &e);   // f in [1/2, 1)
-                power = ldexp(0.5, e);
-                rest = 2 * f;
-            } else if (norm != 0) {
-                rest = nan("");                              // an infinity or NaN in M
-            }
-            factor = power;
-            if (blockIdx.x == 0) kappa[blockIdx.y] = (float)rest;
+            factor = start_factor(norm, false);
+            if (blockIdx.x == 0) kappa[blockIdx.y] = (float)(start_factor(norm, true) / factor);
         }
     }
     __syncthreads();
@@ -197,6 +198,284 @@ OrthPlan plan_orth(const OrthParams& p)
     return q;
 }
 
+// Small matrices: one thread block does all of it, X and A (then B) in shared memory, the sums in tensor memory.  X lies as
+// [smaller side, padded to 128] x [larger side, in chunks of 64]: chunk after chunk of 128 rows of 128 bytes, swizzled,
+// which is an operand with rows along k for X X^T and one with rows along n for B X.  What a launch per product costs
+// (about 5 us each, fifteen of them and two before) is left out: 64 x 128 fp32, 97 us that way.
+constexpr int kSmallSide = 128, kSmallChunk = 128 * 128;   // rows; bytes
+constexpr int kSmallHead = 1024;
+bool small_enough(const OrthParams& p)
+{
+    const int64_t s = std::min(p.r, p.c), l = std::max(p.r, p.c), pieces = p.dtype == 0 ? 2 : 1;
+    return s <= kSmallSide && l <= 512 && pieces * ((l + 63) / 64 + 2) * kSmallChunk + kSmallHead + 1024 <= kGemmSmem;
+}
+
+struct SmallParams {
+    const void* m;
+    void* out;
+    int64_t ldm, node_ldm, ldo, node_ldo;
+    double eps;
+    float c1, c3, c5, scale;
+    int32_t r, c, steps, accumulate, vec;   // vec: M's rows start on 16 bytes
+};
+
+// Eight values of a row to a swizzled chunk array, as pieces.
+template <int P>
+__device__ __forceinline__ void put8(unsigned char* to, uint32_t piece_bytes, int row, int col, const float (&v)[8])
+{
+    unsigned char* const at = to + (col >> 6) * kSmallChunk + row * 128 + ((((col & 63) >> 3) ^ (row & 7)) << 4);
+    uint32_t w[P][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        w[0][i] = pack16(v[2 * i], v[2 * i + 1], __half());
+        if constexpr (P == 2) {
+            float a, b;
+            unpack16(w[0][i], a, b, __half());
+            w[1][i] = pack16(v[2 * i] - a, v[2 * i + 1] - b, __half());
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < P; ++q) *reinterpret_cast<uint4*>(at + q * piece_bytes) = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
+}
+template <int P>
+__device__ __forceinline__ void get8(const unsigned char* from, uint32_t piece_bytes, int row, int col, float (&v)[8])
+{
+    const unsigned char* const at = from + (col >> 6) * kSmallChunk + row * 128 + ((((col & 63) >> 3) ^ (row & 7)) << 4);
+#pragma unroll
+    for (int q = P - 1; q >= 0; --q) {
+        const uint4 w = *reinterpret_cast<const uint4*>(at + q * piece_bytes);
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float a, b;
+            unpack16(u[i], a, b, __half());
+            v[2 * i] = q == P - 1 ? a : v[2 * i] + a;
+            v[2 * i + 1] = q == P - 1 ? b : v[2 * i + 1] + b;
+        }
+    }
+}
+
+template <class T>
+__global__ void __launch_bounds__(256, 1) orth_small_kernel(const __grid_constant__ SmallParams p)
+{
+    constexpr int P = sizeof(T) == 4 ? 2 : 1;
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    unsigned char* const smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+    uint64_t* const bar = reinterpret_cast<uint64_t*>(smem);
+    uint32_t* const tmem_at = reinterpret_cast<uint32_t*>(smem + 8);
+    volatile uint32_t* const stop = reinterpret_cast<volatile uint32_t*>(smem + 12);
+    double* const parts = reinterpret_cast<double*>(smem + 16);   // [8]
+    const bool tall = p.r > p.c;
+    const int s = min(p.r, p.c), l = max(p.r, p.c), chunks = (l + 63) >> 6;
+    unsigned char* const x = smem + kSmallHead;
+    const uint32_t x_piece = chunks * kSmallChunk, a_piece = 2 * kSmallChunk;
+    unsigned char* const a = x + P * x_piece;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const T* const m = static_cast<const T*>(p.m) + blockIdx.x * p.node_ldm;
+
+    if (tid == 0) {
+        mbar_init(bar, 1);
+        mbar_init_fence();
+        *stop = 0;
+    }
+    if (warp == 0) tmem_alloc<1>(smem_u32(tmem_at), 512);
+
+    // Eight values of X's i-th chunk, lanes along M's rows; false outside of X.
+    const auto chunk = [&](int i, int& row, int& col, float(&v)[8]) {
+        if (tall)
+            row = i & 127, col = (i >> 7) * 8;
+        else
+            row = i / (chunks * 8), col = (i - row * chunks * 8) * 8;
+        const bool in = row < s && col < l;
+        if (!tall) {
+            Raw<T> r;
+            r.load(m + row * p.ldm + col, in ? l - col : 0, p.vec);
+            r.values(v);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = row < s && col + k < l ? to_f32(m[(col + k) * p.ldm + row]) : 0.f;
+        }
+    };
+    // |M|, in fp64 and a fixed order
+    double sum = 0;
+#pragma unroll 4
+    for (int i = tid; i < 128 * chunks * 8; i += 256) {
+        int row, col;
+        float v[8];
+        chunk(i, row, col, v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum += (double)v[k] * v[k];
+    }
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+    if (lane == 0) parts[warp] = sum;
+    tmem_fence_before();
+    __syncthreads();
+    tmem_fence_after();
+    const uint32_t tmem = *tmem_at;
+    sum = 0;
+    for (int i = 0; i < 8; ++i) sum += parts[i];
+    const double factor = start_factor(sqrt(sum) + p.eps, true);
+
+    // X_0, zeros around it
+#pragma unroll 4
+    for (int i = tid; i < 128 * chunks * 8; i += 256) {
+        int row, col;
+        float v[8];
+        chunk(i, row, col, v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = (float)(v[k] * factor);
+        put8<P>(x, x_piece, row, col, v);
+    }
+
+    const WaitState w{stop};
+    const int quarter = warp & 3, half = warp >> 2, row = quarter * 32 + lane;
+    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
+    uint32_t parity = 0;
+    // D = A B over `count` k-steps of 16; small products of pieces first.  k-steps of A: 32 bytes, the next chunk after four.
+    const auto multiply = [&](uint32_t d, uint32_t at_a, uint32_t pa, uint32_t at_b, uint32_t pb, bool b_mn, int n, int count) {
+        const uint32_t idesc = mma_descriptor(128, n, true, false, b_mn);
+        uint32_t add = 0;
+        for (int q = P - 1; q >= 0; --q)
+            for (int r = P - 1 - q; r >= 0; --r) {
+                if (P > 1 && q == 0 && r == 0) continue;
+                for (int k = 0; k < count; ++k, add = 1) {
+                    const uint64_t da = tile_descriptor(at_a + q * pa + (k >> 2) * kSmallChunk + (k & 3) * 32, false);
+                    const uint64_t db = b_mn ? tile_descriptor(at_b + r * pb + k * 2048, true, kSmallChunk)
+                                             : tile_descriptor(at_b + r * pb + (k >> 2) * kSmallChunk + (k & 3) * 32, false);
+                    mma_f16<1>(d, da, db, idesc, add);
+                }
+            }
+        if (P > 1)
+            for (int k = 0; k < count; ++k) {
+                const uint64_t da = tile_descriptor(at_a + (k >> 2) * kSmallChunk + (k & 3) * 32, false);
+                const uint64_t db = b_mn ? tile_descriptor(at_b + k * 2048, true, kSmallChunk)
+                                         : tile_descriptor(at_b + (k >> 2) * kSmallChunk + (k & 3) * 32, false);
+                mma_f16<1>(d, da, db, idesc, 1);
+            }
+    };
+    // What the block has written to shared memory is there for the matrix unit, and what it has read of tensor memory is read.
+    const auto hand_over = [&] {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        tmem_fence_before();
+        __syncthreads();
+        tmem_fence_after();
+    };
+    const auto finished = [&] {
+        w.wait(smem_u32(bar), parity);
+        parity ^= 1;
+        tmem_fence_after();
+    };
+    const uint32_t xs = smem_u32(x), as = smem_u32(a);
+    const int side = (s + 15) >> 4, wide = chunks * 64;
+    for (int step = 0; step < p.steps; ++step) {
+        hand_over();
+        if (tid == 0) {                                       // A = X X^T
+            multiply(tmem, xs, x_piece, xs, x_piece, false, 128, (l + 15) >> 4);
+            mma_commit<1>(smem_u32(bar));
+        }
+        finished();
+#pragma unroll 1
+        for (int c = 64 * half; c < 64 * half + 64; c += 32) {
+            float v[32];
+            tmem_load32(lanes + c, v);
+            tmem_wait_load();
+#pragma unroll
+            for (int j = 0; j < 32; j += 8) {
+                float o[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) o[k] = v[j + k] * (1.f / kScale);
+                put8<P>(a, a_piece, row, c + j, o);
+            }
+        }
+        hand_over();
+        if (tid == 0) {                                       // B = c1 I + c3 A + c5 A A, in A's place
+            multiply(tmem, as, a_piece, as, a_piece, false, 128, side);
+            mma_commit<1>(smem_u32(bar));
+        }
+        finished();
+#pragma unroll 1
+        for (int c = 64 * half; c < 64 * half + 64; c += 32) {
+            float v[32];
+            tmem_load32(lanes + c, v);
+            tmem_wait_load();
+#pragma unroll
+            for (int j = 0; j < 32; j += 8) {
+                float o[8];
+                get8<P>(a, a_piece, row, c + j, o);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) o[k] = p.c5 * (1.f / kScale) * v[j + k] + p.c3 * o[k] + (row == c + j + k ? p.c1 * kScale : 0.f);
+                put8<P>(a, a_piece, row, c + j, o);
+            }
+        }
+        hand_over();
+        if (tid == 0) {                                       // B X, 256 columns to an instruction
+            for (int n = 0; n < wide; n += 256)
+                multiply(tmem + n, as, a_piece, xs + (n >> 6) * kSmallChunk, x_piece, true, min(256, wide - n), side);
+            mma_commit<1>(smem_u32(bar));
+        }
+        finished();
+        const bool last = step + 1 == p.steps;
+#pragma unroll 1
+        for (int c = 32 * half; c < wide; c += 64) {
+            float v[32];
+            tmem_load32(lanes + c, v);
+            tmem_wait_load();
+            if (!last) {
+#pragma unroll
+                for (int j = 0; j < 32; j += 8) {
+                    float o[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) o[k] = v[j + k] * (1.f / kScale);
+                    put8<P>(x, x_piece, row, c + j, o);
+                }
+            } else if (row < s) {
+                T* const out = static_cast<T*>(p.out) + blockIdx.x * p.node_ldo;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    if (c + j >= l) break;
+                    T* const at = out + (tall ? (c + j) * p.ldo + row : row * p.ldo + c + j);
+                    const float o = v[j] * (p.scale / (kScale * kScale));
+                    *at = from_f32<T>(p.accumulate ? to_f32(*at) + o : o);
+                }
+            }
+        }
+    }
+    tmem_fence_before();
+    __syncthreads();
+    if (warp == 0) {
+        tmem_fence_after();
+        tmem_free<1>(tmem, 512);
+    }
+}
+
+template <class T>
+cudaError_t orth_small(const OrthParams& p, cudaStream_t stream)
+{
+    SmallParams q;
+    q.m = p.m;
+    q.out = p.out;
+    q.ldm = p.ldm;
+    q.node_ldm = p.node_ldm;
+    q.ldo = p.ldo;
+    q.node_ldo = p.node_ldo;
+    q.eps = p.eps;
+    q.c1 = (float)p.c1;
+    q.c3 = (float)p.c3;
+    q.c5 = (float)p.c5;
+    q.scale = (float)p.scale;
+    q.r = (int32_t)p.r;
+    q.c = (int32_t)p.c;
+    q.steps = (int32_t)p.steps;
+    q.accumulate = p.accumulate;
+    q.vec = on_16(p.m, p.ldm, p.r, p.node_ldm, p.nodes, sizeof(T));
+    static std::atomic<unsigned long long> limit_set{0};
+    const cudaError_t e = ensure_smem_limit(orth_small_kernel<T>, kGemmSmem, limit_set);
+    if (e != cudaSuccess) return e;
+    const int64_t chunks = (std::max(p.r, p.c) + 63) / 64, pieces = sizeof(T) == 4 ? 2 : 1;
+    orth_small_kernel<T><<<(unsigned)p.nodes, 256, (size_t)(pieces * (chunks + 2) * kSmallChunk + kSmallHead + 1024), stream>>>(q);
+    return cudaGetLastError();
+}
+
 template <int P, class Epi>
 cudaError_t product(const GemmPlan& g, const Epi& e, cudaStream_t stream)
 {
@@ -288,13 +567,14 @@ unsigned int* orth_gave_up()
     return cudaGetSymbolAddress(&at, gave_up) == cudaSuccess ? static_cast<unsigned int*>(at) : nullptr;
 }
 
-int64_t orth_scratch_bytes(const OrthParams& p) { return plan_orth(p).scratch.bytes; }
+int64_t orth_scratch_bytes(const OrthParams& p) { return small_enough(p) ? 0 : plan_orth(p).scratch.bytes; }
 
 cudaError_t launch_orth(const OrthParams& p, cudaStream_t stream)
 {
-    if (p.dtype == 0) return orth<float>(p, stream);
-    if (p.dtype == 1) return orth<__nv_bfloat16>(p, stream);
-    return orth<__half>(p, stream);
+    const bool small = small_enough(p);
+    if (p.dtype == 0) return small ? orth_small<float>(p, stream) : orth<float>(p, stream);
+    if (p.dtype == 1) return small ? orth_small<__nv_bfloat16>(p, stream) : orth<__nv_bfloat16>(p, stream);
+    return small ? orth_small<__half>(p, stream) : orth<__half>(p, stream);
 }
 
 }  // namespace gpga

@@ -148,10 +148,10 @@ __device__ __forceinline__ void tmem_load16(uint32_t at, float (&v)[16])
 
 // Descriptor of an operand tile in shared memory with the 128-byte swizzle (rows of 128 bytes, eight of them a 1024-byte
 // atom; the tile starts on 1024 bytes).  Rows run along the sum's axis (mn_major: the other way round, in chunks of 64 rows
-// or columns, one 64-deep chunk 8192 bytes after the other).
-__device__ __forceinline__ uint64_t tile_descriptor(uint32_t addr, bool mn_major)
+// or columns that lie chunk_bytes apart).
+__device__ __forceinline__ uint64_t tile_descriptor(uint32_t addr, bool mn_major, uint32_t chunk_bytes = 8192)
 {
-    const uint64_t lead = mn_major ? 8192 >> 4 : 1, step = 1024 >> 4;
+    const uint64_t lead = mn_major ? chunk_bytes >> 4 : 1, step = 1024 >> 4;
     return (uint64_t)((addr >> 4) & 0x3FFF) | lead << 16 | step << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
 
