@@ -150,6 +150,16 @@ struct Raw {
             for (int i = 0; i < 4; ++i) w[i] = (2 * i < n ? h[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)h[2 * i + 1] << 16 : 0u);
         }
     }
+    __device__ __forceinline__ void set(const float (&v)[8])
+    {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(v[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = pack16(v[2 * i], v[2 * i + 1], T());
+        }
+    }
     __device__ __forceinline__ void values(float (&v)[8]) const
     {
         if constexpr (sizeof(T) == 4) {

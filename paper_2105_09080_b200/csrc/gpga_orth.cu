@@ -2,23 +2,43 @@
 //
 //     X_0 = M / (|M| + eps),   X <- (a I + b A + c A^2) X with A = X X^T     (M with more rows than columns: X^T X, from the right)
 //
-// Three products a step: the Gram matrix A, the polynomial B = a I + b A + c A A, and B X.  A and B are symmetric, so
-// every operand is read as it lies.  The matrices are held as S times their value in fp16: with |X| about 1 their entries
-// lie between 1/columns and a few units, for which fp16 has its full 11 bits (S = 2^11 moves its range down to 2^-25 and
-// leaves 2^5 above one).  16-bit updates take one fp16 value (rounding 2^-12, bfloat16's is 2^-9); fp32 updates two, 22
-// bits, and three products of fp16 for one, summed as fp32 would be.  X_0 is M times a power of two (nothing is lost), the
+// Three products a step: the Gram matrix A, the polynomial B = a I + b A + c A A, and B X.  A and B are symmetric, so every
+// operand is read as it lies.  The matrices are held as S times their value in fp16: with |X| about 1 their entries lie
+// between 1 / columns and a few units, for which fp16 has its full 11 bits (S = 2^11 moves its range down to 2^-25 and
+// leaves 2^5 above one).  fp32 and fp16 updates take two fp16 values for each (22 bits and more) and three products of fp16
+// for one, summed as fp32 would be.  bfloat16 updates of more than 128 rows and columns take one value and one product, a
+// third of the time: the result is off by 1.2 to 1.4 times its own rounding.  Smaller ones, in which the rounding of X on
+// the way weighs more (500 x 33: 2 times), are computed like fp32.  X_0 is M times a power of two (nothing is lost), the
 // rest of the norm, kappa in [1, 2), is a factor in the first step's epilogues.
 #include "gpga_orth.cuh"
+
+#include <type_traits>
+
 #include "gpga_pack.cuh"
 
 namespace gpga {
 
 namespace {
 
+constexpr int GPGA_BF16 = 1;     // the type's code
 constexpr float kScale = 2048.f;
+constexpr int kSmallSide = 128;
 constexpr int kNormParts = 1024;  // blocks of the sum of squares, over all matrices
 
-// Sum of squares of a part of a matrix in fp64: no overflow, and the order is fixed.
+// Sum of eight squares, in fp32 where that neither overflows nor vanishes.
+__device__ __forceinline__ double squares(const float (&v)[8])
+{
+    float q = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) q = fmaf(v[k], v[k], q);
+    if (q > 1e-30f && q < 1e38f) return q;
+    double d = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) d += (double)v[k] * v[k];
+    return d;
+}
+
+// Sum of squares of a part of a matrix: no overflow, and the order is fixed.
 template <class T>
 __global__ void __launch_bounds__(256) square_sum_kernel(const T* m, int64_t ld, int64_t node, int64_t rows, int64_t cols, int vec, double* parts)
 {
@@ -33,8 +53,7 @@ __global__ void __launch_bounds__(256) square_sum_kernel(const T* m, int64_t ld,
         Raw<T> x8;
         x8.load(at, n, vec);
         x8.values(v);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) sum += (double)v[k] * v[k];
+        sum += squares(v);
     }
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
     __shared__ double warps[8];
@@ -92,7 +111,7 @@ __global__ void __launch_bounds__(256) start_kernel(const T* m, int64_t ld, int6
     }
 }
 
-// factor kappa^power acc + beta R (+ diagonal), as pieces.
+// kappa^power factor acc + beta R (+ diagonal), as P pieces (R in as many).
 template <int P>
 struct KeepPieces {
     static constexpr bool kDual = false;
@@ -125,7 +144,7 @@ struct KeepPieces {
                 float s[8];
                 now.r[q].values(s);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] += beta * s[k];
+                for (int k = 0; k < 8; ++k) v[k] = fmaf(beta, s[k], v[k]);
             }
 #pragma unroll
             for (int k = 0; k < 8; ++k)
@@ -135,7 +154,7 @@ struct KeepPieces {
     }
 };
 
-// The last step: factor kappa^power acc, added to what is there or not, in the caller's type.
+// The last step: kappa^power factor acc, added to what is there or not, in the caller's type.
 template <class T>
 struct LastStep {
     static constexpr bool kDual = false;
@@ -164,6 +183,9 @@ bool on_16(const void* p, int64_t ld, int64_t rows, int64_t node, int64_t nodes,
     return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (rows <= 1 || ld * size % 16 == 0) && (nodes <= 1 || node * size % 16 == 0);
 }
 
+// fp16 values that a matrix is held in.
+int pieces_for(const OrthParams& p) { return p.dtype == GPGA_BF16 && std::min(p.r, p.c) > kSmallSide ? 1 : 2; }
+
 struct OrthPlan {
     ScratchPlan scratch;
     Operand x[2], a, b;
@@ -182,7 +204,7 @@ OrthPlan plan_orth(const OrthParams& p)
         o.inner = cols;
         o.outer = rows;
         o.batches = p.nodes;
-        o.pieces = p.dtype == 0 ? 2 : 1;
+        o.pieces = pieces_for(p);
         o.ld = (cols + 7) / 8 * 8;
         o.batch = rows * o.ld;
         o.piece = p.nodes * o.batch;
@@ -202,12 +224,13 @@ OrthPlan plan_orth(const OrthParams& p)
 // [smaller side, padded to 128] x [larger side, in chunks of 64]: chunk after chunk of 128 rows of 128 bytes, swizzled,
 // which is an operand with rows along k for X X^T and one with rows along n for B X.  What a launch per product costs
 // (about 5 us each, fifteen of them and two before) is left out: 64 x 128 fp32, 97 us that way.
-constexpr int kSmallSide = 128, kSmallChunk = 128 * 128;   // rows; bytes
+constexpr int kSmallChunk = 128 * 128;   // bytes
 constexpr int kSmallHead = 1024;
+// Shared memory: two pieces of X and of A.
+int64_t small_bytes(const OrthParams& p) { return 2 * ((std::max(p.r, p.c) + 63) / 64 + 2) * kSmallChunk + kSmallHead + 1024; }
 bool small_enough(const OrthParams& p)
 {
-    const int64_t s = std::min(p.r, p.c), l = std::max(p.r, p.c), pieces = p.dtype == 0 ? 2 : 1;
-    return s <= kSmallSide && l <= 512 && pieces * ((l + 63) / 64 + 2) * kSmallChunk + kSmallHead + 1024 <= kGemmSmem;
+    return std::min(p.r, p.c) <= kSmallSide && std::max(p.r, p.c) <= 320 && small_bytes(p) <= kGemmSmem;
 }
 
 struct SmallParams {
@@ -219,46 +242,39 @@ struct SmallParams {
     int32_t r, c, steps, accumulate, vec;   // vec: M's rows start on 16 bytes
 };
 
-// Eight values of a row to a swizzled chunk array, as pieces.
-template <int P>
+// Eight values of a row to a swizzled chunk array and back, as two pieces.
 __device__ __forceinline__ void put8(unsigned char* to, uint32_t piece_bytes, int row, int col, const float (&v)[8])
 {
     unsigned char* const at = to + (col >> 6) * kSmallChunk + row * 128 + ((((col & 63) >> 3) ^ (row & 7)) << 4);
-    uint32_t w[P][4];
+    uint32_t hi[4], lo[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        w[0][i] = pack16(v[2 * i], v[2 * i + 1], __half());
-        if constexpr (P == 2) {
-            float a, b;
-            unpack16(w[0][i], a, b, __half());
-            w[1][i] = pack16(v[2 * i] - a, v[2 * i + 1] - b, __half());
-        }
+        float a, b;
+        hi[i] = pack16(v[2 * i], v[2 * i + 1], __half());
+        unpack16(hi[i], a, b, __half());
+        lo[i] = pack16(v[2 * i] - a, v[2 * i + 1] - b, __half());
     }
-#pragma unroll
-    for (int q = 0; q < P; ++q) *reinterpret_cast<uint4*>(at + q * piece_bytes) = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
+    *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    *reinterpret_cast<uint4*>(at + piece_bytes) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
 }
-template <int P>
 __device__ __forceinline__ void get8(const unsigned char* from, uint32_t piece_bytes, int row, int col, float (&v)[8])
 {
     const unsigned char* const at = from + (col >> 6) * kSmallChunk + row * 128 + ((((col & 63) >> 3) ^ (row & 7)) << 4);
+    const uint4 h = *reinterpret_cast<const uint4*>(at), o = *reinterpret_cast<const uint4*>(at + piece_bytes);
+    const uint32_t hi[4] = {h.x, h.y, h.z, h.w}, lo[4] = {o.x, o.y, o.z, o.w};
 #pragma unroll
-    for (int q = P - 1; q >= 0; --q) {
-        const uint4 w = *reinterpret_cast<const uint4*>(at + q * piece_bytes);
-        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float a, b;
-            unpack16(u[i], a, b, __half());
-            v[2 * i] = q == P - 1 ? a : v[2 * i] + a;
-            v[2 * i + 1] = q == P - 1 ? b : v[2 * i + 1] + b;
-        }
+    for (int i = 0; i < 4; ++i) {
+        float a, b, c, d;
+        unpack16(hi[i], a, b, __half());
+        unpack16(lo[i], c, d, __half());
+        v[2 * i] = a + c;
+        v[2 * i + 1] = b + d;
     }
 }
 
 template <class T>
 __global__ void __launch_bounds__(256, 1) orth_small_kernel(const __grid_constant__ SmallParams p)
 {
-    constexpr int P = sizeof(T) == 4 ? 2 : 1;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* const smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     uint64_t* const bar = reinterpret_cast<uint64_t*>(smem);
@@ -269,7 +285,7 @@ __global__ void __launch_bounds__(256, 1) orth_small_kernel(const __grid_constan
     const int s = min(p.r, p.c), l = max(p.r, p.c), chunks = (l + 63) >> 6;
     unsigned char* const x = smem + kSmallHead;
     const uint32_t x_piece = chunks * kSmallChunk, a_piece = 2 * kSmallChunk;
-    unsigned char* const a = x + P * x_piece;
+    unsigned char* const a = x + 2 * x_piece;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const T* const m = static_cast<const T*>(p.m) + blockIdx.x * p.node_ldm;
 
@@ -280,32 +296,37 @@ __global__ void __launch_bounds__(256, 1) orth_small_kernel(const __grid_constan
     }
     if (warp == 0) tmem_alloc<1>(smem_u32(tmem_at), 512);
 
-    // Eight values of X's i-th chunk, lanes along M's rows; false outside of X.
-    const auto chunk = [&](int i, int& row, int& col, float(&v)[8]) {
-        if (tall)
-            row = i & 127, col = (i >> 7) * 8;
-        else
-            row = i / (chunks * 8), col = (i - row * chunks * 8) * 8;
-        const bool in = row < s && col < l;
-        if (!tall) {
-            Raw<T> r;
-            r.load(m + row * p.ldm + col, in ? l - col : 0, p.vec);
-            r.values(v);
-        } else {
+    // X's chunks of eight values, four of them to a thread at once, lanes along M's rows; f(row, column, values).
+    const auto each_chunk = [&](const auto& f) {
+        for (int i0 = tid; i0 < 128 * chunks * 8; i0 += 4 * 256) {
+            Raw<T> raw[4];
+            int row[4], col[4];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = row < s && col + k < l ? to_f32(m[(col + k) * p.ldm + row]) : 0.f;
+            for (int j = 0; j < 4; ++j) {
+                const int i = i0 + 256 * j;
+                row[j] = tall ? i & 127 : i / (chunks * 8);
+                col[j] = (tall ? i >> 7 : i - row[j] * chunks * 8) * 8;
+                const bool in = row[j] < s && col[j] < l;
+                if (!tall && p.vec && in && col[j] + 8 <= l) {
+                    raw[j].load16(m + row[j] * p.ldm + col[j]);
+                } else {
+                    float v[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[k] = in && col[j] + k < l ? to_f32(tall ? m[(col[j] + k) * p.ldm + row[j]] : m[row[j] * p.ldm + col[j] + k]) : 0.f;
+                    raw[j].set(v);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float v[8];
+                raw[j].values(v);
+                if (row[j] < 128) f(row[j], col[j], v);
+            }
         }
     };
-    // |M|, in fp64 and a fixed order
+    // |M|, in a fixed order
     double sum = 0;
-#pragma unroll 4
-    for (int i = tid; i < 128 * chunks * 8; i += 256) {
-        int row, col;
-        float v[8];
-        chunk(i, row, col, v);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) sum += (double)v[k] * v[k];
-    }
+    each_chunk([&](int, int, const float(&v)[8]) { sum += squares(v); });
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
     if (lane == 0) parts[warp] = sum;
     tmem_fence_before();
@@ -317,41 +338,33 @@ __global__ void __launch_bounds__(256, 1) orth_small_kernel(const __grid_constan
     const double factor = start_factor(sqrt(sum) + p.eps, true);
 
     // X_0, zeros around it
-#pragma unroll 4
-    for (int i = tid; i < 128 * chunks * 8; i += 256) {
-        int row, col;
-        float v[8];
-        chunk(i, row, col, v);
+    each_chunk([&](int row, int col, float(&v)[8]) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = (float)(v[k] * factor);
-        put8<P>(x, x_piece, row, col, v);
-    }
+        put8(x, x_piece, row, col, v);
+    });
 
     const WaitState w{stop};
     const int quarter = warp & 3, half = warp >> 2, row = quarter * 32 + lane;
     const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
     uint32_t parity = 0;
-    // D = A B over `count` k-steps of 16; small products of pieces first.  k-steps of A: 32 bytes, the next chunk after four.
-    const auto multiply = [&](uint32_t d, uint32_t at_a, uint32_t pa, uint32_t at_b, uint32_t pb, bool b_mn, int n, int count) {
-        const uint32_t idesc = mma_descriptor(128, n, true, false, b_mn);
+    // D = A B over `count` k-steps of 16, the small products of pieces first.  A's rows run along k (32 bytes a step, a chunk
+    // after four), B's too or (b_mn) along n.
+    const auto multiply = [&](uint32_t d, uint64_t a0, uint32_t pa, uint64_t b0, uint32_t pb, bool b_mn, int n, int count) {
+        const uint32_t idesc = mma_descriptor(128, n, true, false, b_mn), b_step = b_mn ? 2048 >> 4 : 32 >> 4, b_chunk = b_mn ? 8192 >> 4 : kSmallChunk >> 4;
         uint32_t add = 0;
-        for (int q = P - 1; q >= 0; --q)
-            for (int r = P - 1 - q; r >= 0; --r) {
-                if (P > 1 && q == 0 && r == 0) continue;
-                for (int k = 0; k < count; ++k, add = 1) {
-                    const uint64_t da = tile_descriptor(at_a + q * pa + (k >> 2) * kSmallChunk + (k & 3) * 32, false);
-                    const uint64_t db = b_mn ? tile_descriptor(at_b + r * pb + k * 2048, true, kSmallChunk)
-                                             : tile_descriptor(at_b + r * pb + (k >> 2) * kSmallChunk + (k & 3) * 32, false);
-                    mma_f16<1>(d, da, db, idesc, add);
-                }
-            }
-        if (P > 1)
-            for (int k = 0; k < count; ++k) {
-                const uint64_t da = tile_descriptor(at_a + (k >> 2) * kSmallChunk + (k & 3) * 32, false);
-                const uint64_t db = b_mn ? tile_descriptor(at_b + k * 2048, true, kSmallChunk)
-                                         : tile_descriptor(at_b + (k >> 2) * kSmallChunk + (k & 3) * 32, false);
-                mma_f16<1>(d, da, db, idesc, 1);
-            }
+#pragma unroll 1
+        for (int q = 0; q < 3; ++q) {     // (1, 0), (0, 1), (0, 0)
+            uint64_t da = a0 + (q == 0 ? pa >> 4 : 0), db = b0 + (q == 1 ? pb >> 4 : 0);
+#pragma unroll 1
+            for (int k = 0; k < count; k += 4, da += kSmallChunk >> 4, db += b_chunk)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (k + j < count) {
+                        mma_f16<1>(d, da + j * (32 >> 4), db + j * b_step, idesc, add);
+                        add = 1;
+                    }
+        }
     };
     // What the block has written to shared memory is there for the matrix unit, and what it has read of tensor memory is read.
     const auto hand_over = [&] {
@@ -366,16 +379,17 @@ __global__ void __launch_bounds__(256, 1) orth_small_kernel(const __grid_constan
         tmem_fence_after();
     };
     const uint32_t xs = smem_u32(x), as = smem_u32(a);
-    const int side = (s + 15) >> 4, wide = chunks * 64;
+    const uint64_t xk = tile_descriptor(xs, false), xn = tile_descriptor(xs, true, kSmallChunk), ak = tile_descriptor(as, false);
+    const int side = (s + 15) >> 4, square = side * 16, wide = chunks * 64;   // columns of A and B that are used; of X
     for (int step = 0; step < p.steps; ++step) {
         hand_over();
         if (tid == 0) {                                       // A = X X^T
-            multiply(tmem, xs, x_piece, xs, x_piece, false, 128, (l + 15) >> 4);
+            multiply(tmem, xk, x_piece, xk, x_piece, false, square, (l + 15) >> 4);
             mma_commit<1>(smem_u32(bar));
         }
         finished();
 #pragma unroll 1
-        for (int c = 64 * half; c < 64 * half + 64; c += 32) {
+        for (int c = 32 * half; c < square; c += 64) {
             float v[32];
             tmem_load32(lanes + c, v);
             tmem_wait_load();
@@ -384,33 +398,33 @@ __global__ void __launch_bounds__(256, 1) orth_small_kernel(const __grid_constan
                 float o[8];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) o[k] = v[j + k] * (1.f / kScale);
-                put8<P>(a, a_piece, row, c + j, o);
+                put8(a, a_piece, row, c + j, o);
             }
         }
         hand_over();
         if (tid == 0) {                                       // B = c1 I + c3 A + c5 A A, in A's place
-            multiply(tmem, as, a_piece, as, a_piece, false, 128, side);
+            multiply(tmem, ak, a_piece, ak, a_piece, false, square, side);
             mma_commit<1>(smem_u32(bar));
         }
         finished();
 #pragma unroll 1
-        for (int c = 64 * half; c < 64 * half + 64; c += 32) {
+        for (int c = 32 * half; c < square; c += 64) {
             float v[32];
             tmem_load32(lanes + c, v);
             tmem_wait_load();
 #pragma unroll
             for (int j = 0; j < 32; j += 8) {
                 float o[8];
-                get8<P>(a, a_piece, row, c + j, o);
+                get8(a, a_piece, row, c + j, o);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) o[k] = p.c5 * (1.f / kScale) * v[j + k] + p.c3 * o[k] + (row == c + j + k ? p.c1 * kScale : 0.f);
-                put8<P>(a, a_piece, row, c + j, o);
+                put8(a, a_piece, row, c + j, o);
             }
         }
         hand_over();
         if (tid == 0) {                                       // B X, 256 columns to an instruction
             for (int n = 0; n < wide; n += 256)
-                multiply(tmem + n, as, a_piece, xs + (n >> 6) * kSmallChunk, x_piece, true, min(256, wide - n), side);
+                multiply(tmem + n, ak, a_piece, xn + (n >> 6) * (kSmallChunk >> 4), x_piece, true, min(256, wide - n), side);
             mma_commit<1>(smem_u32(bar));
         }
         finished();
@@ -420,15 +434,14 @@ __global__ void __launch_bounds__(256, 1) orth_small_kernel(const __grid_constan
             float v[32];
             tmem_load32(lanes + c, v);
             tmem_wait_load();
-            if (!last) {
 #pragma unroll
-                for (int j = 0; j < 32; j += 8) {
-                    float o[8];
+            for (int j = 0; j < 32; j += 8) {
+                float o[8];
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) o[k] = v[j + k] * (1.f / kScale);
-                    put8<P>(x, x_piece, row, c + j, o);
-                }
-            } else if (row < s) {
+                for (int k = 0; k < 8; ++k) o[k] = v[j + k] * (1.f / kScale);
+                if (!last) put8(x, x_piece, row, c + j, o);
+            }
+            if (last && row < s) {
                 T* const out = static_cast<T*>(p.out) + blockIdx.x * p.node_ldo;
 #pragma unroll
                 for (int j = 0; j < 32; ++j) {
@@ -471,8 +484,7 @@ cudaError_t orth_small(const OrthParams& p, cudaStream_t stream)
     static std::atomic<unsigned long long> limit_set{0};
     const cudaError_t e = ensure_smem_limit(orth_small_kernel<T>, kGemmSmem, limit_set);
     if (e != cudaSuccess) return e;
-    const int64_t chunks = (std::max(p.r, p.c) + 63) / 64, pieces = sizeof(T) == 4 ? 2 : 1;
-    orth_small_kernel<T><<<(unsigned)p.nodes, 256, (size_t)(pieces * (chunks + 2) * kSmallChunk + kSmallHead + 1024), stream>>>(q);
+    orth_small_kernel<T><<<(unsigned)p.nodes, 256, (size_t)small_bytes(p), stream>>>(q);
     return cudaGetLastError();
 }
 
@@ -483,10 +495,9 @@ cudaError_t product(const GemmPlan& g, const Epi& e, cudaStream_t stream)
     return launch_gemm_as<Variant<2, 256, P>>(g, e, stream);
 }
 
-template <class T>
+template <class T, int P>
 cudaError_t orth(const OrthParams& p, cudaStream_t stream)
 {
-    constexpr int P = sizeof(T) == 4 ? 2 : 1;
     const OrthPlan q = plan_orth(p);
     const T* m = static_cast<const T*>(p.m);
     const int vec = on_16(p.m, p.ldm, p.r, p.node_ldm, p.nodes, sizeof(T));
@@ -495,13 +506,11 @@ cudaError_t orth(const OrthParams& p, cudaStream_t stream)
     if (e != cudaSuccess) return e;
     const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>((p.r * ((p.c + 7) / 8) + 255) / 256, (int64_t)sm_count() * 8 / std::min<int64_t>(p.nodes, 64)));
     start_kernel<T, P><<<dim3((unsigned)blocks, (unsigned)p.nodes), 256, 0, stream>>>(m, p.ldm, p.node_ldm, p.r, p.c, vec, q.parts, q.count_parts, p.eps,
-                                                                                 pieces_of<__half>(q.x[0]), q.kappa);
+                                                                              pieces_of<__half>(q.x[0]), q.kappa);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
 
     const bool tall = p.r > p.c;
     const int64_t s = std::min(p.r, p.c);
-    KeepPieces<P> keep;
-    keep.kappa = q.kappa;
     GemmPlan g;
     g.half = true;
     g.batch = g.bmod = p.nodes;
@@ -509,21 +518,22 @@ cudaError_t orth(const OrthParams& p, cudaStream_t stream)
     for (int64_t i = 0; i < p.steps; ++i) {
         const Operand &x = q.x[i & 1], &next = q.x[~i & 1];
         const int first = i == 0;
+        KeepPieces<P> keep;
+        keep.kappa = q.kappa;
         g.a[0] = g.b[0] = x;                            // A
         g.a[0].mn_major = g.b[0].mn_major = tall;
         g.m = g.n = s;
         g.k[0] = std::max(p.r, p.c);
-        keep.out = pieces_of<__half>(q.a);
+        keep.out = keep.r = pieces_of<__half>(q.a);
         keep.factor = 1.f / kScale;
+        keep.beta = keep.diagonal = 0.f;
         keep.power = first ? 2 : 0;
         keep.with_r = 0;
-        keep.r = keep.out;
         if ((e = product<P>(g, keep, stream)) != cudaSuccess) return e;
         g.a[0] = g.b[0] = q.a;                          // B = a I + b A + c A A
         g.a[0].mn_major = g.b[0].mn_major = false;
         g.k[0] = s;
         keep.out = pieces_of<__half>(q.b);
-        keep.r = pieces_of<__half>(q.a);
         keep.factor = (float)(p.c5 / kScale);
         keep.beta = (float)p.c3;
         keep.diagonal = (float)(p.c1 * kScale);
@@ -572,9 +582,10 @@ int64_t orth_scratch_bytes(const OrthParams& p) { return small_enough(p) ? 0 : p
 cudaError_t launch_orth(const OrthParams& p, cudaStream_t stream)
 {
     const bool small = small_enough(p);
-    if (p.dtype == 0) return small ? orth_small<float>(p, stream) : orth<float>(p, stream);
-    if (p.dtype == 1) return small ? orth_small<__nv_bfloat16>(p, stream) : orth<__nv_bfloat16>(p, stream);
-    return small ? orth_small<__half>(p, stream) : orth<__half>(p, stream);
+    if (p.dtype == 0) return small ? orth_small<float>(p, stream) : orth<float, 2>(p, stream);
+    if (p.dtype == 2) return small ? orth_small<__half>(p, stream) : orth<__half, 2>(p, stream);
+    if (small) return orth_small<__nv_bfloat16>(p, stream);
+    return pieces_for(p) == 1 ? orth<__nv_bfloat16, 1>(p, stream) : orth<__nv_bfloat16, 2>(p, stream);
 }
 
 }  // namespace gpga
