@@ -16,11 +16,11 @@ BackwardPlan plan_backward(const FeedForwardParams& p)
     const bool f32 = p.dtype == 0, wf32 = p.weight_dtype == 0;
     q.pack.base = p.scratch;
     q.pack.pieces = f32 ? 3 : 1;
-    q.dy = q.pack.operand(p.dy.p, p.dy.ld, p.rows * p.dy.ld, p.rows, p.d, p.nodes, f32, false);
-    q.down = q.pack.operand(p.down.p, p.down.ld, p.down.node, p.d, p.f, p.nodes, wf32, true);
-    q.x = q.pack.operand(p.x.p, p.x.ld, p.rows * p.x.ld, p.rows, p.d, p.nodes, f32, true);
-    q.gate = q.pack.operand(p.gate.p, p.gate.ld, p.gate.node, p.f, p.d, p.nodes, wf32, true);
-    q.up = q.pack.operand(p.up.p, p.up.ld, p.up.node, p.f, p.d, p.nodes, wf32, true);
+    q.dy = q.pack.operand(p.dy.p, p.dy.ld, p.rows * p.dy.ld, p.rows, p.d, p.nodes, f32, false, q.pack.pieces);
+    q.down = q.pack.weights(p.down.p, p.down.ld, p.down.node, p.d, p.f, p.nodes, wf32, true);
+    q.x = q.pack.operand(p.x.p, p.x.ld, p.rows * p.x.ld, p.rows, p.d, p.nodes, f32, true, q.pack.pieces);
+    q.gate = q.pack.weights(p.gate.p, p.gate.ld, p.gate.node, p.f, p.d, p.nodes, wf32, true);
+    q.up = q.pack.weights(p.up.p, p.up.ld, p.up.node, p.f, p.d, p.nodes, wf32, true);
     q.h = q.pack.written(p.rows, p.f, p.nodes, true);
     q.dgu = q.pack.written(p.rows, p.f, 2 * p.nodes, true);   // dg of all nodes, then du
     return q;
@@ -41,7 +41,7 @@ cudaError_t backward(const FeedForwardParams& p, cudaStream_t stream)
     constexpr int P = PiecesOf<T>::count;
     using T16 = typename PiecesOf<T>::type;
     const BackwardPlan q = plan_backward(p);
-    cudaError_t e = q.pack.launch<T16, P>(stream);
+    cudaError_t e = q.pack.launch<T16>(stream);
     if (e != cudaSuccess) return e;
     Operand dg = q.dgu, du = q.dgu;    // halves of one array
     dg.batches = du.batches = p.nodes;
@@ -55,7 +55,7 @@ cudaError_t backward(const FeedForwardParams& p, cudaStream_t stream)
     g.b[0] = q.down;
     g.m = p.rows;
     g.n = p.f;
-    g.k[0] = p.d;
+    g.k = p.d;
     GateGrad<T> grad;
     grad.g = static_cast<const T*>(p.g.p);
     grad.u = static_cast<const T*>(p.u.p);
@@ -75,7 +75,7 @@ cudaError_t backward(const FeedForwardParams& p, cudaStream_t stream)
     g.b[0] = q.h;
     g.m = p.d;
     g.n = p.f;
-    g.k[0] = p.rows;
+    g.k = p.rows;
     if ((e = weight_gradient<T>(g, p, p.ddown, p.d, nullptr, stream)) != cudaSuccess) return e;
 
     g.a[0] = q.dgu;                     // dWg = dg^T x, dWu = du^T x
@@ -85,7 +85,7 @@ cudaError_t backward(const FeedForwardParams& p, cudaStream_t stream)
     g.batch = 2 * p.nodes;
     if ((e = weight_gradient<T>(g, p, p.dgate, p.f, &p.dup, stream)) != cudaSuccess) return e;
 
-    g.segments = 2;                     // dx = dg Wg + du Wu, last: it may take dy's or x's place
+    g.pairs = 2;                        // dx = dg Wg + du Wu, last: it may take dy's or x's place
     g.batch = p.nodes;
     g.a[0] = dg;
     g.a[1] = du;
@@ -94,7 +94,7 @@ cudaError_t backward(const FeedForwardParams& p, cudaStream_t stream)
     g.b[1] = q.up;
     g.m = p.rows;
     g.n = p.d;
-    g.k[0] = g.k[1] = p.f;
+    g.k = p.f;
     return store_product<T, P>(g, p.dx, p.nodes * p.rows, nullptr, false, stream);
 }
 

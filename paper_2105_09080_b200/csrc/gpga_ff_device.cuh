@@ -82,7 +82,7 @@ template <> struct PiecesOf<float> { using type = __nv_bfloat16; static constexp
 // g, u -> h = act(g) u as pieces; g and u themselves where they are kept.
 template <class T>
 struct GateUp {
-    static constexpr bool kDual = true;
+    static constexpr bool kDual = true, kMirror = false;
     static constexpr int kWarps = 16;
     using T16 = typename PiecesOf<T>::type;
     static constexpr int P = PiecesOf<T>::count;
@@ -114,7 +114,7 @@ struct GateUp {
 // acc = dh; g, u -> h = act(g) u, du = dh act(g), dg = dh u act'(g), all as pieces.
 template <class T>
 struct GateGrad {
-    static constexpr bool kDual = false;
+    static constexpr bool kDual = false, kMirror = false;
     static constexpr int kWarps = 16;
     using T16 = typename PiecesOf<T>::type;
     static constexpr int P = PiecesOf<T>::count;
@@ -157,7 +157,7 @@ struct GateGrad {
 // acc -> an array of the caller's; batches from `split` on go to the second one.
 template <class T>
 struct StoreRows {
-    static constexpr bool kDual = false;
+    static constexpr bool kDual = false, kMirror = false;
     static constexpr int kWarps = 8;
     using Ahead = Raw<T>;
     T* out[2];
@@ -181,14 +181,6 @@ struct StoreRows {
 inline bool rows_on_16(const void* p, int64_t ld, int64_t rows, int64_t node, int64_t nodes, int size)
 {
     return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (rows <= 1 || ld * size % 16 == 0) && (nodes <= 1 || node * size % 16 == 0);
-}
-
-// One block a tile where rows are few, pairs of blocks otherwise.
-template <int P, class Epi>
-cudaError_t launch_gemm(const GemmPlan& g, const Epi& epi, cudaStream_t stream)
-{
-    if (g.m <= 128) return launch_gemm_as<Variant<1, 128, P>>(g, epi, stream);
-    return launch_gemm_as<Variant<2, 256, P, P == 1 ? Epi::kWarps : 8>>(g, epi, stream);
 }
 
 template <class T, int P>

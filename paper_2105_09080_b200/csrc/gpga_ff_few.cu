@@ -38,16 +38,21 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
 }
 
-// Eight weights as four pairs of the activations' type.
-template <class T, class W>
-__device__ __forceinline__ void as_pairs(const Raw<W>& r, uint32_t (&o)[4])
+// Eight weights as four pairs of the activations' type; fp32 ones as the sum of two (16 bits more than make a difference).
+template <class T, class W, int Q>
+__device__ __forceinline__ void as_pairs(const Raw<W>& r, uint32_t (&o)[Q][4])
 {
-    if constexpr (sizeof(W) == 2) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = r.w[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = pack16(__uint_as_float(r.w[2 * i]), __uint_as_float(r.w[2 * i + 1]), T());
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(W) == 2) {
+            o[0][i] = r.w[i];
+        } else {
+            const float x = __uint_as_float(r.w[2 * i]), y = __uint_as_float(r.w[2 * i + 1]);
+            float a, b;
+            o[0][i] = pack16(x, y, T());
+            unpack16(o[0][i], a, b, T());
+            o[1][i] = pack16(x - a, y - b, T());
+        }
     }
 }
 
@@ -141,18 +146,21 @@ __global__ void __launch_bounds__(kFewWarps * 32) few_tokens_kernel(const __grid
     const auto multiply = [&](const Raw<W>(&wv)[M][2], const Raw<T>(&xv)[NT]) {
 #pragma unroll
         for (int m = 0; m < M; ++m) {
-            uint32_t lo[4], hi[4];
+            constexpr int Q = sizeof(W) / 2;
+            uint32_t lo[Q][4], hi[Q][4];
             as_pairs<T>(wv[m][0], lo);
             as_pairs<T>(wv[m][1], hi);
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const uint32_t a[4] = {lo[2 * s], hi[2 * s], lo[2 * s + 1], hi[2 * s + 1]};
+            for (int q = Q - 1; q >= 0; --q)
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const uint32_t b[2] = {xv[n].w[2 * s], xv[n].w[2 * s + 1]};
-                    mma16816<T>(acc[m][n], a, b);
+                for (int s = 0; s < 2; ++s) {
+                    const uint32_t a[4] = {lo[q][2 * s], hi[q][2 * s], lo[q][2 * s + 1], hi[q][2 * s + 1]};
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const uint32_t b[2] = {xv[n].w[2 * s], xv[n].w[2 * s + 1]};
+                        mma16816<T>(acc[m][n], a, b);
+                    }
                 }
-            }
         }
     };
     // Whole steps of aligned rows, U of them asked for at once; then what is left, or all of it.

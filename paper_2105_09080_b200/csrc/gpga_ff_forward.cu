@@ -16,10 +16,10 @@ ForwardPlan plan_forward(const FeedForwardParams& p)
     const bool f32 = p.dtype == 0, wf32 = p.weight_dtype == 0;
     q.pack.base = p.scratch;
     q.pack.pieces = f32 ? 3 : 1;
-    q.x = q.pack.operand(p.x.p, p.x.ld, p.rows * p.x.ld, p.rows, p.d, p.nodes, f32, false);
-    q.gate = q.pack.operand(p.gate.p, p.gate.ld, p.gate.node, p.f, p.d, p.nodes, wf32, false);
-    q.up = q.pack.operand(p.up.p, p.up.ld, p.up.node, p.f, p.d, p.nodes, wf32, false);
-    q.down = q.pack.operand(p.down.p, p.down.ld, p.down.node, p.d, p.f, p.nodes, wf32, false);
+    q.x = q.pack.operand(p.x.p, p.x.ld, p.rows * p.x.ld, p.rows, p.d, p.nodes, f32, false, q.pack.pieces);
+    q.gate = q.pack.weights(p.gate.p, p.gate.ld, p.gate.node, p.f, p.d, p.nodes, wf32, false);
+    q.up = q.pack.weights(p.up.p, p.up.ld, p.up.node, p.f, p.d, p.nodes, wf32, false);
+    q.down = q.pack.weights(p.down.p, p.down.ld, p.down.node, p.d, p.f, p.nodes, wf32, false);
     q.h = q.pack.written(p.rows, p.f, p.nodes, false);
     return q;
 }
@@ -30,7 +30,7 @@ cudaError_t forward(const FeedForwardParams& p, cudaStream_t stream)
     constexpr int P = PiecesOf<T>::count;
     using T16 = typename PiecesOf<T>::type;
     const ForwardPlan q = plan_forward(p);
-    cudaError_t e = q.pack.launch<T16, P>(stream);
+    cudaError_t e = q.pack.launch<T16>(stream);
     if (e != cudaSuccess) return e;
     GemmPlan g;
     g.half = std::is_same<T16, __half>::value;
@@ -41,7 +41,7 @@ cudaError_t forward(const FeedForwardParams& p, cudaStream_t stream)
     g.b[1] = q.up;
     g.m = p.rows;
     g.n = p.f;
-    g.k[0] = p.d;
+    g.k = p.d;
     GateUp<T> up;
     up.g = static_cast<T*>(p.g.p);
     up.u = static_cast<T*>(p.u.p);
@@ -58,7 +58,7 @@ cudaError_t forward(const FeedForwardParams& p, cudaStream_t stream)
     g.a[0] = q.h;
     g.b[0] = q.down;
     g.n = p.d;
-    g.k[0] = p.f;
+    g.k = p.f;
     return store_product<T, P>(g, p.y, p.nodes * p.rows, nullptr, false, stream);
 }
 

@@ -5,8 +5,9 @@
 // Operands are 16-bit arrays that tiled asynchronous copies bring to shared memory: rows along k, or (mn_major) rows along i
 // or j, so no operand is ever transposed in memory.  An operand may be the sum of P arrays of 16 bits ("pieces": a float32
 // value is exactly three bfloat16 values); then the products of pieces p + q < P are summed, six of them for P = 3.
-// A sum may run over two pairs of operands (segments), and a tile's columns may come from two arrays (DUAL: the left half
-// from B[0], the right half from B[1]), so that both projections of a gate end in one thread's registers.
+// A sum may run over two pairs of operands, and over two pieces of B with one of A (segments), and a tile's columns may
+// come from two arrays (DUAL: the left half from B[0], the right half from B[1]), so that both projections of a gate end in
+// one thread's registers.  A symmetric product is computed on and above the diagonal and stored twice.
 //
 // A tile is 128 CG rows by bn columns on CG thread blocks.  Warp 0 loads, warp 1 of the leading block issues the matrix
 // instructions, warps 4 to 11 take finished tiles out of tensor memory (two accumulators: the next tile's sums run
@@ -17,6 +18,9 @@
 // that a sum drifts towards zero by about 2^-26 of itself per instruction (K = 256 in 96 instructions: 1.6e-6 of the
 // result).  Where the result is to be as good as fp32 gives, the sum is cut into chunks of 64 or 128, the small products of
 // a chunk come first, and the epilogue's threads, which then have most of the block's registers, add the chunks' sums.
+//
+// SPLIT: where there are fewer tiles than SMs, a cluster of blocks takes parts of k of one 128 x 128 tile each; their sums
+// lie in shared memory then, and every block adds a part of the columns from all of them, in the order of k.
 //
 // Every wait has a limit (kWaitTries); when one runs out the block notes it in `gave_up`, all of its roles wind down, and
 // gpga_token_status reports it.
@@ -56,9 +60,12 @@ struct GemmMaps {
 
 struct GemmParams {
     int32_t m, n;                 // of one batch
-    int32_t kblocks0, kblocks;    // steps of kTileK of the first segment; of both
+    int32_t kblocks1, kblocks;    // steps of kTileK of a segment; of all
+    int32_t pairs;                // operands that the segments go through, again for every piece of B (GemmPlan)
     int32_t bmod;                 // B's batch index is batch % bmod
-    int32_t tiles_m, tiles_n, tiles;
+    int32_t tiles_m, tiles_n, per_batch, tiles;
+    int32_t symmetric;            // only tiles on and above the diagonal; the others are their mirror images
+    int32_t splits;               // SPLIT: blocks of a cluster, which share a tile's sum
     uint32_t idesc;
     int32_t a_mn, b_mn;
 };
@@ -69,10 +76,17 @@ struct GemmTile {
 // Tiles of a batch in columns of eight row tiles, so that tiles that run together share operands in L2.
 __device__ __forceinline__ GemmTile gemm_tile(const GemmParams& p, int t, int rows, int columns)
 {
-    const int per = p.tiles_m * p.tiles_n;
     GemmTile g;
-    g.batch = t / per;
-    int r = t - g.batch * per;
+    g.batch = t / p.per_batch;
+    int r = t - g.batch * p.per_batch;
+    if (p.symmetric) {   // column j has j + 1 tiles
+        int j = (int)((sqrtf(8.f * r + 1.f) - 1.f) * 0.5f);
+        while ((int64_t)j * (j + 1) / 2 > r) --j;
+        while ((int64_t)(j + 1) * (j + 2) / 2 <= r) ++j;
+        g.m0 = (int)(r - (int64_t)j * (j + 1) / 2) * rows;
+        g.n0 = j * columns;
+        return g;
+    }
     const int group = r / (8 * p.tiles_n);
     const int first = group * 8, height = min(8, p.tiles_m - first);
     r -= first * p.tiles_n;
@@ -120,6 +134,11 @@ __device__ __forceinline__ void staged8(const float* stage, int row, int c, floa
     const float4 a = *reinterpret_cast<const float4*>(stage + row * 32 + (c ^ (4 * (row & 7))));
     const float4 b = *reinterpret_cast<const float4*>(stage + row * 32 + ((c + 4) ^ (4 * (row & 7))));
     v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+}
+__device__ __forceinline__ void stage8(float* stage, int row, int c, const float (&v)[8])
+{
+    *reinterpret_cast<float4*>(stage + row * 32 + (c ^ (4 * (row & 7)))) = make_float4(v[0], v[1], v[2], v[3]);
+    *reinterpret_cast<float4*>(stage + row * 32 + ((c + 4) ^ (4 * (row & 7)))) = make_float4(v[4], v[5], v[6], v[7]);
 }
 __device__ __forceinline__ float staged1(const float* stage, int row, int c) { return stage[row * 32 + (c ^ (4 * (row & 7)))]; }
 
@@ -285,21 +304,36 @@ constexpr int kFewRegisters = 64, kManyRegisters = 208;
 //   eight(v, ahead, batch, row, col, left): eight columns.  wide() false: one(v, batch, row, col) is called instead;
 //   kDual: eight(v, w, batch, row, col, left), v of the first array's columns, w of the second's.  wide() false: keep(which, v,
 //   batch, row, col) is called first for every single value.
+//   kMirror: eight() leaves in v what it has stored; put(v, batch, row, col) stores it again at its mirror place.
 // The loops over eight columns are kept rolled: a warp goes through an epilogue once per tile, and unrolled it waits for
 // instructions (gradient epilogue, fp32: 147 us unrolled, see below for what it is now).
 struct NothingAhead {};
 
+// v[k] for a k that is not known when compiling.
+__device__ __forceinline__ float pick(const float (&v)[8], int k)
+{
+    float x = v[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) x = k == i ? v[i] : x;
+    return x;
+}
+
 // What a variant of the kernel has: tile columns (of a pair of blocks, where CG = 2), pieces, warps of the epilogue, stages.
-template <int CG_, int BN_, int P_, int WARPS_ = 8>
+template <int CG_, int BN_, int P_, int WARPS_ = 8, bool SPLIT_ = false>
 struct Variant {
-    static constexpr int CG = CG_, BN = BN_, P = P_, warps = WARPS_, threads = 128 + 32 * warps, staging = warps * kStagingWarp;
-    static constexpr bool chunked = P > 1;
+    static constexpr int CG = CG_, BN = BN_, P = P_, warps = WARPS_, threads = 128 + 32 * warps;
+    static constexpr bool chunked = P > 1, split = SPLIT_;
+    static constexpr int staging = split ? 0 : warps * kStagingWarp;
     static_assert(!chunked || warps == 8, "the registers of a CHUNKED kernel are split for eight warps");
+    static_assert(!split || (CG == 1 && BN == 128 && warps == 8), "a SPLIT tile is 128 x 128");
     static constexpr uint32_t a_bytes = 128 * kTileK * 2, b_bytes = BN / CG * kTileK * 2, stage_bytes = a_bytes + b_bytes;
     static constexpr uint32_t room = (kGemmSmem - 1024 - kGemmHead - staging) / stage_bytes;
     static constexpr uint32_t stages = room < 8 ? room : 8;
     static constexpr int chunk = P == 3 ? 1 : 2;   // k-blocks of a chunk
 };
+
+// Four columns of a SPLIT tile's row, 512 bytes to a row.
+__device__ __forceinline__ uint32_t split_place(int row, int group) { return row * 512 + ((group ^ (row & 7)) << 4); }
 
 template <class V, class Epi>
 __global__ void __launch_bounds__(V::threads, 1)
@@ -316,12 +350,14 @@ __global__ void __launch_bounds__(V::threads, 1)
     float* const staging = reinterpret_cast<float*>(smem + kGemmHead);
     const uint32_t operands = base + kGemmHead + V::staging;
     constexpr int CG = V::CG, BN = V::BN, P = V::P;
-    constexpr bool CHUNKED = V::chunked;
+    constexpr bool CHUNKED = V::chunked, SPLIT = V::split;
     constexpr uint32_t a_bytes = V::a_bytes, stage_bytes = V::stage_bytes, stages = V::stages;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = CG == 2 ? cluster_rank() : 0;
-    const int first = blockIdx.x / CG, step = gridDim.x / CG;
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0, part_of_k = SPLIT ? cluster_rank() : 0;
+    const int group = SPLIT ? p.splits : CG, first = blockIdx.x / group, step = gridDim.x / group;
+    const int kb_first = SPLIT ? (int)((int64_t)p.kblocks * part_of_k / p.splits) : 0;
+    const int kb_count = SPLIT ? (int)((int64_t)p.kblocks * (part_of_k + 1) / p.splits) - kb_first : p.kblocks;
     const WaitState w{stop};
 
     if (threadIdx.x == 0) {
@@ -360,10 +396,11 @@ __global__ void __launch_bounds__(V::threads, 1)
                 const GemmTile g = gemm_tile(p, t, 128 * CG, BN);
                 const int m0 = g.m0 + (int)rank * 128, bb = g.batch % p.bmod;
                 const int n0 = Epi::kDual ? g.n0 / 2 : g.n0 + (int)rank * nb;   // kDual: BN / 2 columns of each array
-                for (int kb = 0; kb < p.kblocks && ok; ++kb) {
-                    const int seg = kb >= p.kblocks0, k0 = (kb - (seg ? p.kblocks0 : 0)) * kTileK;
-                    const CUtensorMap* const ma = &maps.a[seg];
-                    const CUtensorMap* const mb = &maps.b[Epi::kDual ? (CG == 2 ? rank : 0) : seg];
+                const int segment = kb_first / p.kblocks1;
+                int pair = segment % p.pairs, piece = segment / p.pairs, k0 = (kb_first - segment * p.kblocks1) * kTileK;
+                for (int kb = 0; kb < kb_count && ok; ++kb) {
+                    const CUtensorMap* const ma = &maps.a[pair];
+                    const CUtensorMap* const mb = &maps.b[Epi::kDual ? (CG == 2 ? rank : 0) : pair];
 #pragma unroll
                     for (int q = P - 1; q >= 0; --q, ring.next(), ++loaded) {
                         if (loaded >= stages && !(ok = w.wait(empty + 8 * ring.at, ring.parity ^ 1))) break;
@@ -381,11 +418,15 @@ __global__ void __launch_bounds__(V::threads, 1)
                         }
                         if (!Epi::kDual && b_mn) {
 #pragma unroll
-                            for (int c = 0; c < nb; c += 64) load_box<CG>(db + c * 128, mb, n0 + c, k0, bb, q, bar);
+                            for (int c = 0; c < nb; c += 64) load_box<CG>(db + c * 128, mb, n0 + c, k0, bb, q + piece, bar);
                         } else {
-                            load_box<CG>(db, mb, k0, n0, bb, q, bar);
-                            if constexpr (Epi::kDual && CG == 1) load_box<CG>(db + V::b_bytes / 2, &maps.b[1], k0, n0, bb, q, bar);
+                            load_box<CG>(db, mb, k0, n0, bb, q + piece, bar);
+                            if constexpr (Epi::kDual && CG == 1) load_box<CG>(db + V::b_bytes / 2, &maps.b[1], k0, n0, bb, q + piece, bar);
                         }
+                    }
+                    if ((k0 += kTileK) >= p.kblocks1 * kTileK) {
+                        k0 = 0;
+                        if (++pair == p.pairs) pair = 0, ++piece;
                     }
                 }
             }
@@ -397,13 +438,13 @@ __global__ void __launch_bounds__(V::threads, 1)
             uint32_t sums = 0;   // accumulators filled
             bool ok = true;
             for (int t = first; t < p.tiles && ok; t += step) {
-                const int chunk = CHUNKED ? V::chunk : p.kblocks;
-                for (int k0 = 0; k0 < p.kblocks && ok; k0 += chunk, ++sums) {
+                const int chunk = CHUNKED ? V::chunk : kb_count;
+                for (int k0 = 0; k0 < kb_count && ok; k0 += chunk, ++sums) {
                     const uint32_t buf = sums & 1;
                     if (sums >= 2 && !(ok = w.wait(acc_empty + 8 * buf, (sums / 2 - 1) & 1))) break;
                     tmem_fence_after();
                     const uint32_t d = tmem + buf * 256;
-                    const int count = min(chunk, p.kblocks - k0);
+                    const int count = min(chunk, kb_count - k0);
                     for (int kb = 0; kb < count && ok; ++kb) {
                         // The last pieces lie in the first stage of a k-block.  Small products first; a stage is free when its piece
                         // has met all that it meets, which is in the stages' order.
@@ -453,8 +494,16 @@ __global__ void __launch_bounds__(V::threads, 1)
             const GemmTile g = gemm_tile(p, t, 128 * CG, BN);
             const int row0 = g.m0 + (int)rank * 128 + quarter * 32, from = (Epi::kDual ? g.n0 / 2 : g.n0) + part * width;
             const int rows = p.m - row0;   // that are there
+            const bool mirror = p.symmetric && g.m0 != g.n0;
             constexpr int kAhead = CHUNKED ? 1 : 2;   // calls of eight() that are read ahead
             typename Epi::Ahead ahead[kAhead];
+            // SPLIT: 32 columns of this block's sum, where the operands were.
+            const auto put_partial = [&](const float(&v)[32], int col) {
+                const int r = quarter * 32 + lane;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    *reinterpret_cast<float4*>(smem + kGemmHead + split_place(r, col / 4 + j)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+            };
             // A 32 x 32 block that is staged; `next`: whether the block to the right follows.
             const auto block = [&](int col0, bool next) {
                 if constexpr (!Epi::kDual) {
@@ -477,9 +526,23 @@ __global__ void __launch_bounds__(V::threads, 1)
                             float v[8];
                             staged8(stage, r, lane_col, v);
                             epi.eight(v, now, g.batch, row0 + r, c, p.n - c);
+                            if constexpr (Epi::kMirror)
+                                if (mirror) stage8(stage, r, lane_col, v);
                         }
                     }
                 }
+                if constexpr (Epi::kMirror)
+                    if (mirror) {
+                        __syncwarp();
+#pragma unroll 1
+                        for (int i = 0; i < 4; ++i) {
+                            const int c = i * 8 + lane_row, r = lane_col;
+                            float v[8];
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) v[k] = staged1(stage, r + k, c);
+                            if (col0 + c < p.n && r < rows) epi.put(v, g.batch, col0 + c, row0 + r);
+                        }
+                    }
                 }
             };
             const auto start = [&] {
@@ -519,7 +582,7 @@ __global__ void __launch_bounds__(V::threads, 1)
                 for (int j = 0; j < slabs; ++j)
 #pragma unroll
                     for (int i = 0; i < 32; ++i) acc[j][i] = 0.f;
-                for (int k0 = 0; k0 < p.kblocks; k0 += V::chunk, ++sums) {
+                for (int k0 = 0; k0 < kb_count; k0 += V::chunk, ++sums) {
                     const uint32_t buf = sums & 1;
                     ok = __all_sync(~0u, w.wait(acc_full + 8 * buf, (sums / 2) & 1));
                     if (!ok) break;
@@ -538,6 +601,12 @@ __global__ void __launch_bounds__(V::threads, 1)
                     if (lane == 0) arrive_cluster(release + 8 * buf);
                 }
                 if (!ok) break;
+                if constexpr (SPLIT) {
+#pragma unroll
+                    for (int j = 0; j < slabs; ++j)
+                        put_partial(acc[j], part * width + (Epi::kDual ? j * (BN / 2) : j * 32));
+                    continue;
+                }
                 if (rows <= 0) continue;
                 if constexpr (!Epi::kDual) start();
 #pragma unroll 1
@@ -561,7 +630,7 @@ __global__ void __launch_bounds__(V::threads, 1)
                 }
             } else {
                 const uint32_t buf = sums & 1;
-                if constexpr (!Epi::kDual) start();
+                if constexpr (!Epi::kDual && !SPLIT) start();
                 ok = __all_sync(~0u, w.wait(acc_full + 8 * buf, (sums / 2) & 1));
                 if (!ok) break;
                 ++sums;
@@ -579,6 +648,11 @@ __global__ void __launch_bounds__(V::threads, 1)
                         if (lane == 0) arrive_cluster(release + 8 * buf);
                     }
                     const int col0 = from + c;
+                    if constexpr (SPLIT) {
+                        put_partial(a, part * width + c);
+                        if constexpr (Epi::kDual) put_partial(b, part * width + c + BN / 2);
+                        continue;
+                    }
                     if (rows <= 0 || col0 >= p.n) continue;
                     if constexpr (Epi::kDual) {
                         block2(a, b, col0);
@@ -591,6 +665,75 @@ __global__ void __launch_bounds__(V::threads, 1)
         }
     }
 
+    if constexpr (SPLIT) {
+        cluster_barrier();
+        if (warp >= 4 && !*stop) {
+            const GemmTile g = gemm_tile(p, first, 128, BN);
+            const int thread = threadIdx.x - 128, per = (Epi::kDual ? BN / 2 : BN) / 8 / p.splits;   // chunks of eight columns of this block
+            const int n0 = Epi::kDual ? g.n0 / 2 : g.n0;
+            const bool mirror = p.symmetric && g.m0 != g.n0;
+            const auto total = [&](int row, int group, float(&v)[8]) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = 0.f;
+                for (int b = 0; b < p.splits; ++b) {
+                    const uint32_t from = map_shared(operands, b);
+                    float x[8];
+                    load_shared_cluster(from + split_place(row, group), x[0], x[1], x[2], x[3]);
+                    load_shared_cluster(from + split_place(row, group + 1), x[4], x[5], x[6], x[7]);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[k] += x[k];
+                }
+            };
+#pragma unroll 1
+            for (int u = thread; u < 128 * per; u += 256) {
+                const int row = u / per, c = ((int)part_of_k * per + u - row * per) * 8;   // in the tile
+                const int r = g.m0 + row, col = n0 + c, left = p.n - col;
+                if (r >= p.m || left <= 0) continue;
+                float v[8];
+                if constexpr (Epi::kDual) {
+                    float x[8];
+                    total(row, c / 4, v);
+                    total(row, (c + BN / 2) / 4, x);
+                    if (!epi.wide())
+#pragma unroll 1
+                        for (int k = 0; k < min(left, 8); ++k) {
+                            epi.keep(0, pick(v, k), g.batch, r, col + k);
+                            epi.keep(1, pick(x, k), g.batch, r, col + k);
+                        }
+                    epi.eight(v, x, g.batch, r, col, left);
+                } else {
+                    typename Epi::Ahead ahead;
+                    if (epi.wide()) epi.load(ahead, g.batch, r, col, left);
+                    total(row, c / 4, v);
+                    if (epi.wide()) {
+                        epi.eight(v, ahead, g.batch, r, col, left);
+                    } else {
+#pragma unroll 1
+                        for (int k = 0; k < min(left, 8); ++k) epi.one(pick(v, k), g.batch, r, col + k);
+                    }
+                    if constexpr (Epi::kMirror)
+                        if (mirror) {   // nobody else reads these columns here
+                            *reinterpret_cast<float4*>(smem + kGemmHead + split_place(row, c / 4)) = make_float4(v[0], v[1], v[2], v[3]);
+                            *reinterpret_cast<float4*>(smem + kGemmHead + split_place(row, c / 4 + 1)) = make_float4(v[4], v[5], v[6], v[7]);
+                        }
+                }
+            }
+            if constexpr (Epi::kMirror)
+                if (mirror) {
+                    asm volatile("bar.sync 1, 256;" ::: "memory");
+#pragma unroll 1
+                    for (int u = thread; u < 16 * 8 * per; u += 256) {
+                        const int c = (int)part_of_k * per * 8 + u / 16, row = (u & 15) * 8;
+                        if (n0 + c >= p.n || g.m0 + row >= p.m) continue;
+                        float v[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) v[k] = reinterpret_cast<const float*>(smem + kGemmHead + split_place(row + k, c / 4))[c & 3];
+                        epi.put(v, g.batch, n0 + c, g.m0 + row);
+                    }
+                }
+        }
+    }
+
     // Everybody is done, or has given up; copies in flight must land before the block goes.
     tmem_fence_before();
     __syncthreads();
@@ -599,7 +742,7 @@ __global__ void __launch_bounds__(V::threads, 1)
             for (uint32_t tries = 0; tries < 4096 && !try_wait(full + 8 * (i % stages), (i / stages) & 1); ++tries) {
             }
     __syncthreads();
-    if constexpr (CG == 2) cluster_barrier();
+    if constexpr (CG == 2 || SPLIT) cluster_barrier();
     if (warp == 2) {
         tmem_fence_after();
         tmem_free<CG>(tmem, 512);
@@ -622,11 +765,13 @@ bool operand_fits(const void* base, int64_t ld, int64_t batch);   // whether a t
 cudaError_t encode_map(CUtensorMap& map, const Operand& o, bool half, int box_rows);
 
 struct GemmPlan {
+    // The sum runs over the pairs, for every piece of B beyond those that A has too (their number is a[0].pieces).
     Operand a[2], b[2];
-    int segments = 1;
-    int64_t m = 0, n = 0, k[2] = {0, 0}, batch = 1, bmod = 1;
-    bool half = false;   // fp16 operands (otherwise bfloat16)
-    bool after = false;  // the kernel before it on the stream is one of the same call
+    int pairs = 1;
+    int64_t m = 0, n = 0, k = 0, batch = 1, bmod = 1;
+    bool half = false;        // fp16 operands (otherwise bfloat16)
+    bool after = false;       // the kernel before it on the stream is one of the same call
+    bool symmetric = false;
 };
 
 int sm_count();
@@ -639,31 +784,39 @@ int kernel_registers(Kernel kernel)
 }
 
 template <class V, class Epi>
-cudaError_t launch_gemm_as(const GemmPlan& g, const Epi& epi, cudaStream_t stream)
+cudaError_t launch_gemm_as(const GemmPlan& g, int splits, const Epi& epi, cudaStream_t stream)
 {
     constexpr int CG = V::CG, bn = V::BN;
     GemmParams p;
     GemmMaps maps;
     p.m = (int32_t)g.m;
     p.n = (int32_t)g.n;
-    p.kblocks0 = (int32_t)((g.k[0] + kTileK - 1) / kTileK);
-    p.kblocks = p.kblocks0 + (g.segments > 1 ? (int32_t)((g.k[1] + kTileK - 1) / kTileK) : 0);
+    p.pairs = g.pairs;
+    p.kblocks1 = (int32_t)((g.k + kTileK - 1) / kTileK);
+    p.kblocks = p.kblocks1 * g.pairs * (int32_t)(g.b[0].pieces - g.a[0].pieces + 1);
     p.bmod = (int32_t)g.bmod;
     p.tiles_m = (int32_t)((g.m + 128 * CG - 1) / (128 * CG));
     const int columns = Epi::kDual ? bn / 2 : bn;
     p.tiles_n = (int32_t)((g.n + columns - 1) / columns);
-    const int64_t tiles = g.batch * p.tiles_m * p.tiles_n;
-    if (tiles >= (int64_t(1) << 31) - 65536) return cudaErrorInvalidValue;
+    p.symmetric = g.symmetric;
+    p.per_batch = g.symmetric ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n;
+    p.splits = splits;
+    const int64_t tiles = g.batch * p.per_batch;
+    if (tiles * splits >= (int64_t(1) << 31) - 65536) return cudaErrorInvalidValue;
     p.tiles = (int32_t)tiles;
     p.a_mn = g.a[0].mn_major;
     p.b_mn = g.b[0].mn_major;
     p.idesc = mma_descriptor(128 * CG, bn, g.half, p.a_mn, p.b_mn);
     const int b_rows = p.b_mn ? 64 : Epi::kDual ? bn / 2 : bn / CG;
     for (int i = 0; i < 2; ++i) {
-        const bool b_there = i == 0 || g.segments > 1 || Epi::kDual;
-        cudaError_t e = encode_map(maps.a[i], g.a[i < g.segments ? i : 0], g.half, p.a_mn ? 64 : 128);
-        if (e == cudaSuccess) e = encode_map(maps.b[i], g.b[b_there ? i : 0], g.half, b_rows);
+        cudaError_t e = encode_map(maps.a[i], g.a[i < g.pairs ? i : 0], g.half, p.a_mn ? 64 : 128);
+        if (e == cudaSuccess) e = encode_map(maps.b[i], g.b[i < g.pairs || Epi::kDual ? i : 0], g.half, b_rows);
         if (e != cudaSuccess) return e;
+        if (g.pairs == 1 && !Epi::kDual) {
+            maps.a[1] = maps.a[0];
+            maps.b[1] = maps.b[0];
+            break;
+        }
     }
     const auto kernel = gemm_kernel<V, Epi>;
     static std::atomic<unsigned long long> limit_set{0};
@@ -673,7 +826,8 @@ cudaError_t launch_gemm_as(const GemmPlan& g, const Epi& epi, cudaStream_t strea
         static const int registers = kernel_registers(kernel);
         if (registers * V::threads < 128 * (kFewRegisters + 2 * kManyRegisters)) return cudaErrorLaunchOutOfResources;
     }
-    const int64_t blocks = std::min<int64_t>(tiles, sm_count() / CG) * CG;
+    const int cluster = V::split ? splits : CG;
+    const int64_t blocks = (V::split ? tiles : std::min<int64_t>(tiles, sm_count() / CG)) * cluster;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)blocks);
     cfg.blockDim = dim3(V::threads);
@@ -681,9 +835,9 @@ cudaError_t launch_gemm_as(const GemmPlan& g, const Epi& epi, cudaStream_t strea
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     int n = 0;
-    if (CG == 2) {
+    if (cluster > 1) {
         attr[n].id = cudaLaunchAttributeClusterDimension;
-        attr[n].val.clusterDim.x = 2;
+        attr[n].val.clusterDim.x = (unsigned)cluster;
         attr[n].val.clusterDim.y = 1;
         attr[n].val.clusterDim.z = 1;
         ++n;
@@ -696,6 +850,35 @@ cudaError_t launch_gemm_as(const GemmPlan& g, const Epi& epi, cudaStream_t strea
     cfg.attrs = attr;
     cfg.numAttrs = n;
     return cudaLaunchKernelEx(&cfg, kernel, maps, p, epi);
+}
+
+// Microseconds that a product takes as 256 x 256 tiles on pairs of SMs (splits = 0), or as 128 x 128 tiles on clusters of
+// `splits` blocks: waves of tiles, k-blocks of a tile, and what a tile costs besides.  A k-block of a 256 x 256 tile
+// takes 0.27 us per product of pieces, one of a 128 x 128 tile 0.18 us (more than a quarter of it on two SMs: each
+// operand byte is used half as often).
+inline double gemm_microseconds(int64_t m, int64_t n, int64_t kblocks, int64_t batch, int products, bool symmetric, int splits, int sms)
+{
+    const int64_t side = splits ? 128 : 256, tm = (m + side - 1) / side, tn = (n + side - 1) / side;
+    const int64_t tiles = batch * (symmetric ? tm * (tm + 1) / 2 : tm * tn);
+    if (!splits) return (double)((tiles + sms / 2 - 1) / (sms / 2)) * (0.27 * products * kblocks + 0.3) + 3.0;
+    const int64_t waves = (tiles * splits + sms - 1) / sms;
+    return waves * (0.18 * products * ((kblocks + splits - 1) / splits) + 3.0) + (splits > 1 ? 1.0 : 0.0);
+}
+
+// The variant that should take the least time.
+template <int P, class Epi>
+cudaError_t launch_gemm(const GemmPlan& g, const Epi& epi, cudaStream_t stream)
+{
+    const int products = P * (P + 1) / 2;
+    const int64_t n = Epi::kDual ? 2 * g.n : g.n, kblocks = (g.k + kTileK - 1) / kTileK * g.pairs * (g.b[0].pieces - g.a[0].pieces + 1);
+    int best = 0;
+    double least = gemm_microseconds(g.m, n, kblocks, g.batch, products, g.symmetric, 0, sm_count());
+    for (int splits = 1; splits <= 8 && splits <= kblocks; splits *= 2) {
+        const double t = gemm_microseconds(g.m, n, kblocks, g.batch, products, g.symmetric, splits, sm_count());
+        if (t < least) least = t, best = splits;
+    }
+    if (best) return launch_gemm_as<Variant<1, 128, P, 8, true>>(g, best, epi, stream);
+    return launch_gemm_as<Variant<2, 256, P, P == 1 ? Epi::kWarps : 8>>(g, 1, epi, stream);
 }
 
 }  // namespace gpga

@@ -114,7 +114,8 @@ __global__ void __launch_bounds__(256) start_kernel(const T* m, int64_t ld, int6
 // kappa^power factor acc + beta R (+ diagonal), as P pieces (R in as many).
 template <int P>
 struct KeepPieces {
-    static constexpr bool kDual = false;
+    static constexpr bool kDual = false, kMirror = true;
+    static constexpr int kWarps = 8;
     struct Ahead {
         Raw<__half> r[P];
     };
@@ -152,12 +153,14 @@ struct KeepPieces {
         }
         out.template store<P>(batch, row, col, v);
     }
+    __device__ __forceinline__ void put(const float (&v)[8], int batch, int row, int col) const { out.template store<P>(batch, row, col, v); }
 };
 
 // The last step: kappa^power factor acc, added to what is there or not, in the caller's type.
 template <class T>
 struct LastStep {
-    static constexpr bool kDual = false;
+    static constexpr bool kDual = false, kMirror = false;
+    static constexpr int kWarps = 8;
     using Ahead = Raw<T>;
     T* out;
     int64_t ld, node;
@@ -488,13 +491,6 @@ cudaError_t orth_small(const OrthParams& p, cudaStream_t stream)
     return cudaGetLastError();
 }
 
-template <int P, class Epi>
-cudaError_t product(const GemmPlan& g, const Epi& e, cudaStream_t stream)
-{
-    if (g.m <= 128) return launch_gemm_as<Variant<1, 128, P>>(g, e, stream);
-    return launch_gemm_as<Variant<2, 256, P>>(g, e, stream);
-}
-
 template <class T, int P>
 cudaError_t orth(const OrthParams& p, cudaStream_t stream)
 {
@@ -523,36 +519,38 @@ cudaError_t orth(const OrthParams& p, cudaStream_t stream)
         g.a[0] = g.b[0] = x;                            // A
         g.a[0].mn_major = g.b[0].mn_major = tall;
         g.m = g.n = s;
-        g.k[0] = std::max(p.r, p.c);
+        g.k = std::max(p.r, p.c);
+        g.symmetric = true;
         keep.out = keep.r = pieces_of<__half>(q.a);
         keep.factor = 1.f / kScale;
         keep.beta = keep.diagonal = 0.f;
         keep.power = first ? 2 : 0;
         keep.with_r = 0;
-        if ((e = product<P>(g, keep, stream)) != cudaSuccess) return e;
+        if ((e = launch_gemm<P>(g, keep, stream)) != cudaSuccess) return e;
         g.a[0] = g.b[0] = q.a;                          // B = a I + b A + c A A
         g.a[0].mn_major = g.b[0].mn_major = false;
-        g.k[0] = s;
+        g.k = s;
         keep.out = pieces_of<__half>(q.b);
         keep.factor = (float)(p.c5 / kScale);
         keep.beta = (float)p.c3;
         keep.diagonal = (float)(p.c1 * kScale);
         keep.power = 0;
         keep.with_r = 1;
-        if ((e = product<P>(g, keep, stream)) != cudaSuccess) return e;
+        if ((e = launch_gemm<P>(g, keep, stream)) != cudaSuccess) return e;
         g.a[0] = tall ? x : q.b;                        // B X or X B
         g.b[0] = tall ? q.b : x;
         g.a[0].mn_major = false;
         g.b[0].mn_major = !tall;
         g.m = p.r;
         g.n = p.c;
-        g.k[0] = s;
+        g.k = s;
+        g.symmetric = false;
         if (i + 1 < p.steps) {
             keep.out = pieces_of<__half>(next);
             keep.factor = 1.f / kScale;
             keep.power = first;
             keep.with_r = 0;
-            if ((e = product<P>(g, keep, stream)) != cudaSuccess) return e;
+            if ((e = launch_gemm<P>(g, keep, stream)) != cudaSuccess) return e;
         } else {
             LastStep<T> last;
             last.out = static_cast<T*>(p.out);
@@ -563,7 +561,7 @@ cudaError_t orth(const OrthParams& p, cudaStream_t stream)
             last.power = first;
             last.accumulate = p.accumulate;
             last.vec = on_16(p.out, p.ldo, p.r, p.node_ldo, p.nodes, sizeof(T));
-            if ((e = product<P>(g, last, stream)) != cudaSuccess) return e;
+            if ((e = launch_gemm<P>(g, last, stream)) != cudaSuccess) return e;
         }
     }
     return cudaSuccess;

@@ -12,6 +12,7 @@ struct PackJob {
     int64_t first;            // first of the launch's chunks that belongs to this job
     int vec;                  // every source row starts on 16 bytes
     int src_f32;              // otherwise the type of the pieces
+    int pieces;
     void* dst;
     int64_t dst_piece;
 };
@@ -24,7 +25,7 @@ struct PackJobs {
 
 // A thread takes a chunk of eight columns: one pass over the source, bound by memory (fp32 to three pieces: 4 bytes read,
 // 6 written per value).
-template <class T16, int P>
+template <class T16>
 __global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackJobs jobs)
 {
     grid_launch_dependents();
@@ -48,7 +49,12 @@ __global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackJ
             x.values(v);
         }
         const Pieces<T16> dst{static_cast<T16*>(j.dst) + c * 8, j.dst_piece, 0, 0};
-        dst.template store<P>(0, 0, 0, v);
+        if (j.pieces == 1)
+            dst.template store<1>(0, 0, 0, v);
+        else if (j.pieces == 2)
+            dst.template store<2>(0, 0, 0, v);
+        else
+            dst.template store<3>(0, 0, 0, v);
     }
 }
 
@@ -68,9 +74,14 @@ struct PackPlan {
     PackJobs jobs{};
     ScratchPlan scratch;
     char* base = nullptr;     // nullptr: only the sizes are wanted
-    int pieces = 1;
+    int pieces = 1;           // of activations
 
-    Operand operand(const void* p, int64_t ld, int64_t batch, int64_t rows, int64_t cols, int64_t batches, bool f32, bool mn_major)
+    // Weights: fp32 beside 16-bit activations are two pieces of their type.
+    Operand weights(const void* p, int64_t ld, int64_t batch, int64_t rows, int64_t cols, int64_t batches, bool f32, bool mn_major)
+    {
+        return operand(p, ld, batch, rows, cols, batches, f32, mn_major, f32 && pieces == 1 ? 2 : pieces);
+    }
+    Operand operand(const void* p, int64_t ld, int64_t batch, int64_t rows, int64_t cols, int64_t batches, bool f32, bool mn_major, int pieces)
     {
         Operand o;
         o.inner = cols;
@@ -102,6 +113,7 @@ struct PackPlan {
         j.first = jobs.chunks;
         j.vec = (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (rows == 1 || ld * size % 16 == 0) && (batches == 1 || batch * size % 16 == 0);
         j.src_f32 = f32;
+        j.pieces = pieces;
         j.dst = base + at;
         j.dst_piece = o.piece;
         ++jobs.count;
@@ -123,12 +135,12 @@ struct PackPlan {
         o.base = base + scratch.take(pieces * o.piece * 2);
         return o;
     }
-    template <class T16, int P>
+    template <class T16>
     cudaError_t launch(cudaStream_t stream) const
     {
         if (!jobs.count) return cudaSuccess;
         const int64_t blocks = std::min<int64_t>((jobs.chunks + 255) / 256, (int64_t)sm_count() * 8);
-        pack_kernel<T16, P><<<(unsigned)blocks, 256, 0, stream>>>(jobs);
+        pack_kernel<T16><<<(unsigned)blocks, 256, 0, stream>>>(jobs);
         return cudaGetLastError();
     }
 };

@@ -27,6 +27,10 @@ __device__ __forceinline__ uint32_t map_shared(uint32_t addr, uint32_t rank)
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
+__device__ __forceinline__ void load_shared_cluster(uint32_t addr, float& a, float& b, float& c, float& d)
+{
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(a), "=f"(b), "=f"(c), "=f"(d) : "r"(addr) : "memory");
+}
 // Arrivals on a barrier anywhere in the cluster.  What they announce is ordered by other means (asynchronous copies count
 // their own bytes, tensor memory has its own fences), so they need no cluster-wide release: with one per stage a product
 // ran at a third of its speed.
