@@ -621,18 +621,21 @@ int64_t gpga_layer_norm_scratch_bytes(int64_t nodes, int64_t rows, int64_t d);
  * the token-block operators hold, and these:
  *
  *  - A matrix of node i is row-major and starts at p + i * node_p, its rows ld_p apart (elements).  Weights are fp32 (slices of
- *    X) or of the activations' type; fp32 weights beside 16-bit activations are rounded to that type once per call.
+ *    X) or of the activations' type.
  *  - fp32 operands (all of a call with fp32 activations) are taken as exact sums of three bfloat16 values, so that results
- *    are as good as fp32 arithmetic gives; an infinity among them gives NaN in what it reaches.  16-bit operands are taken as
- *    they are.  Sums are fp32.  What passes from one product to the next (h, dg, du) has the activations' type.
+ *    are as good as fp32 arithmetic gives; an infinity among them may give NaN in what it reaches.  16-bit operands are taken
+ *    as they are, fp32 weights beside them as the sum of two values of their type (16 significant bits for bfloat16; for
+ *    fp16 22, and 2^-25 at least).  Sums are fp32.  What passes from one product to the next (h, dg, du) has the activations'
+ *    type.
  *  - Scratch: the _scratch_bytes function of an entry, given the entry's own argument struct (its scratch members are not
  *    looked at), says how much it needs; 0 also where the arguments are wrong.
  *  - Waits inside the kernels are bounded.  One that gives up (which takes seconds and does not happen in a sound run) ends
- *    the call's kernels with undefined results; gpga_token_status, which waits for the stream, then returns TIMEOUT, from
- *    then on and for the current device.
+ *    the call's kernels with undefined results; gpga_token_status, which waits for the stream, then returns TIMEOUT, once,
+ *    for the current device.  gpga_selftest_token_wait lets a wait on `stream` run out.
  */
 enum { GPGA_ACTIVATION_SILU = 0, GPGA_ACTIVATION_GELU = 1, GPGA_ACTIVATION_RELU = 2 };
 int32_t gpga_token_status(void* stream);
+int32_t gpga_selftest_token_wait(void* stream);
 
 /*
  * Gated feed-forward block, per node (gate, up: f x d; down: d x f):
@@ -670,8 +673,10 @@ int64_t gpga_feed_forward_backward_scratch_bytes(const gpga_feed_forward_backwar
  *     X = M / (|M| + eps)  (Frobenius norm),  then `steps` times  X <- c1 X + c3 (X X^T) X + c5 (X X^T)^2 X,
  *     out = scale X, or out + scale X where accumulate is not 0 (a local update x - gamma X is scale = -gamma).
  * A singular value s of M / |M| becomes p(p(...p(s))) with p(s) = c1 s + c3 s^3 + c5 s^5; singular vectors stay.  Coefficients
- * must keep p(s) within [-8, 8] on the way (fp16 range of the products).  M and out have type dtype; fp32 is computed with
- * 22 significant bits, the 16-bit types with 11.  Zero gives zero (eps > 0); an infinity or NaN in M makes its node NaN.
+ * must keep p(s) and c1 + c3 s^2 + c5 s^4 within [-8, 8] on the way (fp16 range of the products).  M and out have type dtype.
+ * fp32 and fp16 are computed with 22 significant bits and fp32 sums; so is bfloat16 where a side has at most 128 rows or
+ * columns, and with 11 bits otherwise (the result is off by 1.2 to 1.4 times its own rounding).  Zero gives zero; an
+ * infinity or NaN in M makes its node NaN.
  * 1 <= r, c <= 2^20, nodes * r * c <= 2^40, 1 <= steps <= 1000.  out may be M itself.
  */
 typedef struct gpga_orthogonalize_args {

@@ -95,6 +95,7 @@ SIGNATURES = {
     "gpga_orthogonalize": (_i32, [_P, _P]),
     "gpga_orthogonalize_scratch_bytes": (_i64, [_P]),
     "gpga_token_status": (_i32, [_P]),
+    "gpga_selftest_token_wait": (_i32, [_P]),
 }
 
 GPGA_NOALLOC_SCRATCH_BYTES = 4 * 1024 * 1024

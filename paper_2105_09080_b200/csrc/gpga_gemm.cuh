@@ -107,9 +107,10 @@ struct Ring {
 
 struct WaitState {
     volatile uint32_t* stop;
+    uint32_t tries = kWaitTries;
     __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) const
     {
-        for (uint32_t t = 0; t < kWaitTries; ++t) {
+        for (uint32_t t = 0; t < tries; ++t) {
             if (try_wait(bar, parity)) return true;
             if (*stop) return false;
         }
@@ -854,15 +855,18 @@ cudaError_t launch_gemm_as(const GemmPlan& g, int splits, const Epi& epi, cudaSt
 
 // Microseconds that a product takes as 256 x 256 tiles on pairs of SMs (splits = 0), or as 128 x 128 tiles on clusters of
 // `splits` blocks: waves of tiles, k-blocks of a tile, and what a tile costs besides.  A k-block of a 256 x 256 tile
-// takes 0.27 us per product of pieces, one of a 128 x 128 tile 0.18 us (more than a quarter of it on two SMs: each
-// operand byte is used half as often).
+// takes 0.27 us per product of pieces, one of a 128 x 128 tile on its one SM 0.25 us (a quarter of the work on half of the
+// SMs: each operand byte is used half as often); a 128 x 128 tile is a block's only one, so nothing hides its start and
+// end.  Measured, all of a call with either: 512 x 512 fp32, two steps, 117 us and (4 blocks) 68 us; 8 x 1024 x 2816
+// bfloat16 256 us and (1 block) 461 us; gradient of 8000 tokens x 128 x 300, bf16, 146 us and (4 blocks) 91 us.
 inline double gemm_microseconds(int64_t m, int64_t n, int64_t kblocks, int64_t batch, int products, bool symmetric, int splits, int sms)
 {
     const int64_t side = splits ? 128 : 256, tm = (m + side - 1) / side, tn = (n + side - 1) / side;
     const int64_t tiles = batch * (symmetric ? tm * (tm + 1) / 2 : tm * tn);
-    if (!splits) return (double)((tiles + sms / 2 - 1) / (sms / 2)) * (0.27 * products * kblocks + 0.3) + 3.0;
-    const int64_t waves = (tiles * splits + sms - 1) / sms;
-    return waves * (0.18 * products * ((kblocks + splits - 1) / splits) + 3.0) + (splits > 1 ? 1.0 : 0.0);
+    if (!splits) return (double)((tiles + sms / 2 - 1) / (sms / 2)) * (0.27 * products * kblocks + 0.3) + 4.0;
+    const int64_t room = splits == 8 ? sms * 3 / 4 : splits == 4 ? sms * 9 / 10 : sms;   // SMs of whole clusters
+    const int64_t waves = (tiles * splits + room - 1) / room;
+    return waves * (0.25 * products * ((kblocks + splits - 1) / splits) + 4.0) + (splits == 1 ? 0.0 : splits == 2 ? 0.5 : splits == 4 ? 1.0 : 3.5);
 }
 
 // The variant that should take the least time.

@@ -252,6 +252,11 @@ int32_t gpga_orthogonalize(const gpga_orthogonalize_args_t* a, void* stream)
     return launched(launch_orth(q, static_cast<cudaStream_t>(stream)), "gpga_orthogonalize");
 }
 
+int32_t gpga_selftest_token_wait(void* stream)
+{
+    return launched(launch_wait_selftest(static_cast<cudaStream_t>(stream)), "gpga_selftest_token_wait");
+}
+
 int32_t gpga_token_status(void* stream)
 {
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -262,6 +267,7 @@ int32_t gpga_token_status(void* stream)
         unsigned int v = 0;
         cudaError_t e = cudaMemcpyAsync(&v, f, sizeof v, cudaMemcpyDeviceToHost, s);
         if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+        if (e == cudaSuccess && v) e = cudaMemsetAsync(f, 0, sizeof v, s);
         if (e != cudaSuccess) return launched(e, "gpga_token_status");
         any |= v;
     }

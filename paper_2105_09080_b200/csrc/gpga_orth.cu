@@ -464,6 +464,18 @@ __global__ void __launch_bounds__(256, 1) orth_small_kernel(const __grid_constan
     }
 }
 
+// A wait that runs out: nothing arrives at its barrier.
+__global__ void wait_selftest_kernel()
+{
+    __shared__ __align__(8) uint64_t bar;
+    __shared__ uint32_t stop;
+    mbar_init(&bar, 1);
+    mbar_init_fence();
+    stop = 0;
+    const WaitState w{&stop, 64};
+    w.wait(smem_u32(&bar), 0);
+}
+
 template <class T>
 cudaError_t orth_small(const OrthParams& p, cudaStream_t stream)
 {
@@ -573,6 +585,12 @@ unsigned int* orth_gave_up()
 {
     void* at = nullptr;
     return cudaGetSymbolAddress(&at, gave_up) == cudaSuccess ? static_cast<unsigned int*>(at) : nullptr;
+}
+
+cudaError_t launch_wait_selftest(cudaStream_t stream)
+{
+    wait_selftest_kernel<<<1, 1, 0, stream>>>();
+    return cudaGetLastError();
 }
 
 int64_t orth_scratch_bytes(const OrthParams& p) { return small_enough(p) ? 0 : plan_orth(p).scratch.bytes; }

@@ -19,5 +19,6 @@ struct OrthParams {
 int64_t orth_scratch_bytes(const OrthParams& p);
 cudaError_t launch_orth(const OrthParams& p, cudaStream_t stream);
 unsigned int* orth_gave_up();
+cudaError_t launch_wait_selftest(cudaStream_t stream);
 
 }  // namespace gpga
