@@ -83,6 +83,7 @@ template <> struct PiecesOf<float> { using type = __nv_bfloat16; static constexp
 template <class T>
 struct GateUp {
     static constexpr bool kDual = true, kMirror = false;
+    static constexpr double kTail = 3.0;
     static constexpr int kWarps = 16;
     using T16 = typename PiecesOf<T>::type;
     static constexpr int P = PiecesOf<T>::count;
@@ -115,6 +116,7 @@ struct GateUp {
 template <class T>
 struct GateGrad {
     static constexpr bool kDual = false, kMirror = false;
+    static constexpr double kTail = 6.0;
     static constexpr int kWarps = 16;
     using T16 = typename PiecesOf<T>::type;
     static constexpr int P = PiecesOf<T>::count;
@@ -158,6 +160,7 @@ struct GateGrad {
 template <class T>
 struct StoreRows {
     static constexpr bool kDual = false, kMirror = false;
+    static constexpr double kTail = 1.0;
     static constexpr int kWarps = 8;
     using Ahead = Raw<T>;
     T* out[2];

@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(kFewWarps * 32) few_tokens_kernel(const __grid
         for (int m = 0; m < M; ++m) s[m] = cluster_sum(sums, (m * N + n) * S + r, M * N * S, p.blocks);
         finish<T, T, GATE>(p, node, n, row0 + r, s[0], s[M - 1]);
     }
-    cluster_barrier();   // nobody goes while its sums are read
+    cluster_farewell();   // nobody goes while its sums are read
 }
 
 // fp32: R rows of the weights and N tokens to a block, its warps a part of k each.

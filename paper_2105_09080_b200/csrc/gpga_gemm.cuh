@@ -19,8 +19,9 @@
 // result).  Where the result is to be as good as fp32 gives, the sum is cut into chunks of 64 or 128, the small products of
 // a chunk come first, and the epilogue's threads, which then have most of the block's registers, add the chunks' sums.
 //
-// SPLIT: where there are fewer tiles than SMs, a cluster of blocks takes parts of k of one 128 x 128 tile each; their sums
-// lie in shared memory then, and every block adds a part of the columns from all of them, in the order of k.
+// SPLIT: where there are fewer tiles than SMs, a cluster of blocks takes parts of k of one 128 x 128 tile each.  Every block
+// has a part of the columns to finish: it gets the others' sums for them by bulk copies between shared memories, and adds
+// in the order of k.
 //
 // Every wait has a limit (kWaitTries); when one runs out the block notes it in `gave_up`, all of its roles wind down, and
 // gpga_token_status reports it.
@@ -305,10 +306,16 @@ constexpr int kFewRegisters = 64, kManyRegisters = 208;
 //   eight(v, ahead, batch, row, col, left): eight columns.  wide() false: one(v, batch, row, col) is called instead;
 //   kDual: eight(v, w, batch, row, col, left), v of the first array's columns, w of the second's.  wide() false: keep(which, v,
 //   batch, row, col) is called first for every single value.
+//   kTail: microseconds of 128 x 256 columns, for the choice of the variant.
 //   kMirror: eight() leaves in v what it has stored; put(v, batch, row, col) stores it again at its mirror place.
 // The loops over eight columns are kept rolled: a warp goes through an epilogue once per tile, and unrolled it waits for
 // instructions (gradient epilogue, fp32: 147 us unrolled, see below for what it is now).
 struct NothingAhead {};
+
+// A SPLIT tile's sums: eight columns after eight columns (the block that finishes them has them one after the other), 128 rows of
+// 32 bytes and 64 bytes between; the halves of a row change places every four rows, for the banks.
+constexpr int kSplitChunk = 128 * 32 + 64;
+__device__ __forceinline__ uint32_t split_place(int chunk, int row, int half) { return chunk * kSplitChunk + row * 32 + ((half ^ (row >> 2 & 1)) << 4); }
 
 // v[k] for a k that is not known when compiling.
 __device__ __forceinline__ float pick(const float (&v)[8], int k)
@@ -324,7 +331,7 @@ template <int CG_, int BN_, int P_, int WARPS_ = 8, bool SPLIT_ = false>
 struct Variant {
     static constexpr int CG = CG_, BN = BN_, P = P_, warps = WARPS_, threads = 128 + 32 * warps;
     static constexpr bool chunked = P > 1, split = SPLIT_;
-    static constexpr int staging = split ? 0 : warps * kStagingWarp;
+    static constexpr int staging = split ? 16 * kSplitChunk : warps * kStagingWarp;   // split: the other blocks' sums
     static_assert(!chunked || warps == 8, "the registers of a CHUNKED kernel are split for eight warps");
     static_assert(!split || (CG == 1 && BN == 128 && warps == 8), "a SPLIT tile is 128 x 128");
     static constexpr uint32_t a_bytes = 128 * kTileK * 2, b_bytes = BN / CG * kTileK * 2, stage_bytes = a_bytes + b_bytes;
@@ -332,9 +339,6 @@ struct Variant {
     static constexpr uint32_t stages = room < 8 ? room : 8;
     static constexpr int chunk = P == 3 ? 1 : 2;   // k-blocks of a chunk
 };
-
-// Four columns of a SPLIT tile's row, 512 bytes to a row.
-__device__ __forceinline__ uint32_t split_place(int row, int group) { return row * 512 + ((group ^ (row & 7)) << 4); }
 
 template <class V, class Epi>
 __global__ void __launch_bounds__(V::threads, 1)
@@ -344,10 +348,11 @@ __global__ void __launch_bounds__(V::threads, 1)
     const uint32_t raw = smem_u32(smem_raw);
     unsigned char* const smem = smem_raw + ((1024 - (raw & 1023)) & 1023);
     const uint32_t base = smem_u32(smem);
-    // head: full[8], empty[8], acc_full[2], acc_empty[2], tensor memory address, stop flag
+    // head: full[8], empty[8], acc_full[2], acc_empty[2], tensor memory address, stop flag, SPLIT's copies
     const uint32_t full = base, empty = base + 64, acc_full = base + 128, acc_empty = base + 144;
     uint32_t* const tmem_at = reinterpret_cast<uint32_t*>(smem + 160);
     volatile uint32_t* const stop = reinterpret_cast<volatile uint32_t*>(smem + 164);
+    uint64_t* const copies = reinterpret_cast<uint64_t*>(smem + 168);
     float* const staging = reinterpret_cast<float*>(smem + kGemmHead);
     const uint32_t operands = base + kGemmHead + V::staging;
     constexpr int CG = V::CG, BN = V::BN, P = V::P;
@@ -360,6 +365,14 @@ __global__ void __launch_bounds__(V::threads, 1)
     const int kb_first = SPLIT ? (int)((int64_t)p.kblocks * part_of_k / p.splits) : 0;
     const int kb_count = SPLIT ? (int)((int64_t)p.kblocks * (part_of_k + 1) / p.splits) - kb_first : p.kblocks;
     const WaitState w{stop};
+    // SPLIT: this block's sums, in the order of the blocks that finish them; the place there of the tile's c-th eight columns.
+    unsigned char* const sums_at = smem + kGemmHead + V::staging;
+    constexpr int columns8 = (Epi::kDual ? BN / 2 : BN) / 8;
+    const auto split_chunk = [&](int c) {
+        if (!Epi::kDual) return c;
+        const int per = columns8 / p.splits, i = c % columns8;   // of both arrays side by side
+        return (i / per * 2 + c / columns8) * per + i % per;
+    };
 
     if (threadIdx.x == 0) {
         for (uint32_t s = 0; s < stages; ++s) {
@@ -371,6 +384,10 @@ __global__ void __launch_bounds__(V::threads, 1)
             mbar_init(reinterpret_cast<uint64_t*>(smem + 144 + 8 * i), V::warps * CG);
         }
         *stop = 0;
+        if constexpr (SPLIT) {
+            mbar_init(copies, 1);
+            if (p.splits > 1) mbar_arrive_expect_tx(copies, (p.splits - 1) * (16 / p.splits) * kSplitChunk);
+        }
         mbar_init_fence();
         prefetch_map(&maps.a[0]);
         prefetch_map(&maps.b[0]);
@@ -378,7 +395,7 @@ __global__ void __launch_bounds__(V::threads, 1)
     if (warp == 2) tmem_alloc<CG>(smem_u32(tmem_at), 512);
     tmem_fence_before();
     __syncthreads();
-    if constexpr (CG == 2) cluster_barrier();
+    if constexpr (CG == 2 || SPLIT) cluster_barrier();
     tmem_fence_after();
     const uint32_t tmem = *tmem_at;
     grid_launch_dependents();
@@ -503,7 +520,7 @@ __global__ void __launch_bounds__(V::threads, 1)
                 const int r = quarter * 32 + lane;
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    *reinterpret_cast<float4*>(smem + kGemmHead + split_place(r, col / 4 + j)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                    *reinterpret_cast<float4*>(sums_at + split_place(split_chunk(col / 8 + j / 2), r, j & 1)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
             };
             // A 32 x 32 block that is staged; `next`: whether the block to the right follows.
             const auto block = [&](int col0, bool next) {
@@ -667,34 +684,42 @@ __global__ void __launch_bounds__(V::threads, 1)
     }
 
     if constexpr (SPLIT) {
-        cluster_barrier();
         if (warp >= 4 && !*stop) {
+            const int thread = threadIdx.x - 128, per = columns8 / p.splits, shift = __ffs(per) - 1;   // chunks of this block: a power of two
+            const uint32_t slice = (Epi::kDual ? 2 : 1) * per * kSplitChunk;
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            if (thread == 0)
+                for (int b = 0; b < p.splits; ++b)
+                    if (b != (int)part_of_k)
+                        copy_to_block(map_shared(smem_u32(staging) + part_of_k * slice, b), smem_u32(sums_at) + b * slice, slice, map_shared(smem_u32(copies), b));
             const GemmTile g = gemm_tile(p, first, 128, BN);
-            const int thread = threadIdx.x - 128, per = (Epi::kDual ? BN / 2 : BN) / 8 / p.splits;   // chunks of eight columns of this block
             const int n0 = Epi::kDual ? g.n0 / 2 : g.n0;
             const bool mirror = p.symmetric && g.m0 != g.n0;
-            const auto total = [&](int row, int group, float(&v)[8]) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = 0.f;
+            unsigned char* const own = sums_at + part_of_k * slice;
+            if (p.splits > 1) w.wait(smem_u32(copies), 0);
+            // Eight columns' sums over the blocks, in the order of k.
+            const auto total = [&](int chunk, int row, float(&v)[8]) {
+                const uint32_t lo = split_place(chunk, row, 0), hi = split_place(chunk, row, 1);
+#pragma unroll 2
                 for (int b = 0; b < p.splits; ++b) {
-                    const uint32_t from = map_shared(operands, b);
-                    float x[8];
-                    load_shared_cluster(from + split_place(row, group), x[0], x[1], x[2], x[3]);
-                    load_shared_cluster(from + split_place(row, group + 1), x[4], x[5], x[6], x[7]);
+                    const unsigned char* const from = b == (int)part_of_k ? own : reinterpret_cast<const unsigned char*>(staging) + b * slice;
+                    const float4 x = *reinterpret_cast<const float4*>(from + lo), y = *reinterpret_cast<const float4*>(from + hi);
+                    const float z[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) v[k] += x[k];
+                    for (int k = 0; k < 8; ++k) v[k] = b ? v[k] + z[k] : z[k];
                 }
             };
 #pragma unroll 1
             for (int u = thread; u < 128 * per; u += 256) {
-                const int row = u / per, c = ((int)part_of_k * per + u - row * per) * 8;   // in the tile
+                const int row = u >> shift, chunk = u & (per - 1), c = (int)((part_of_k << shift) + chunk) * 8;
                 const int r = g.m0 + row, col = n0 + c, left = p.n - col;
                 if (r >= p.m || left <= 0) continue;
                 float v[8];
                 if constexpr (Epi::kDual) {
                     float x[8];
-                    total(row, c / 4, v);
-                    total(row, (c + BN / 2) / 4, x);
+                    total(chunk, row, v);
+                    total(chunk + per, row, x);
                     if (!epi.wide())
 #pragma unroll 1
                         for (int k = 0; k < min(left, 8); ++k) {
@@ -705,7 +730,7 @@ __global__ void __launch_bounds__(V::threads, 1)
                 } else {
                     typename Epi::Ahead ahead;
                     if (epi.wide()) epi.load(ahead, g.batch, r, col, left);
-                    total(row, c / 4, v);
+                    total(chunk, row, v);
                     if (epi.wide()) {
                         epi.eight(v, ahead, g.batch, r, col, left);
                     } else {
@@ -713,9 +738,9 @@ __global__ void __launch_bounds__(V::threads, 1)
                         for (int k = 0; k < min(left, 8); ++k) epi.one(pick(v, k), g.batch, r, col + k);
                     }
                     if constexpr (Epi::kMirror)
-                        if (mirror) {   // nobody else reads these columns here
-                            *reinterpret_cast<float4*>(smem + kGemmHead + split_place(row, c / 4)) = make_float4(v[0], v[1], v[2], v[3]);
-                            *reinterpret_cast<float4*>(smem + kGemmHead + split_place(row, c / 4 + 1)) = make_float4(v[4], v[5], v[6], v[7]);
+                        if (mirror) {   // this block's own sums of these columns are not needed again
+                            *reinterpret_cast<float4*>(own + split_place(chunk, row, 0)) = make_float4(v[0], v[1], v[2], v[3]);
+                            *reinterpret_cast<float4*>(own + split_place(chunk, row, 1)) = make_float4(v[4], v[5], v[6], v[7]);
                         }
                 }
             }
@@ -724,11 +749,11 @@ __global__ void __launch_bounds__(V::threads, 1)
                     asm volatile("bar.sync 1, 256;" ::: "memory");
 #pragma unroll 1
                     for (int u = thread; u < 16 * 8 * per; u += 256) {
-                        const int c = (int)part_of_k * per * 8 + u / 16, row = (u & 15) * 8;
+                        const int mine = u / 16, row = (u & 15) * 8, c = (int)(part_of_k << shift) * 8 + mine;
                         if (n0 + c >= p.n || g.m0 + row >= p.m) continue;
                         float v[8];
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) v[k] = reinterpret_cast<const float*>(smem + kGemmHead + split_place(row + k, c / 4))[c & 3];
+                        for (int k = 0; k < 8; ++k) v[k] = reinterpret_cast<const float*>(own + split_place(mine >> 3, row + k, mine >> 2 & 1))[mine & 3];
                         epi.put(v, g.batch, n0 + c, g.m0 + row);
                     }
                 }
@@ -743,7 +768,7 @@ __global__ void __launch_bounds__(V::threads, 1)
             for (uint32_t tries = 0; tries < 4096 && !try_wait(full + 8 * (i % stages), (i / stages) & 1); ++tries) {
             }
     __syncthreads();
-    if constexpr (CG == 2 || SPLIT) cluster_barrier();
+    if constexpr (CG == 2 || SPLIT) cluster_farewell();
     if (warp == 2) {
         tmem_fence_after();
         tmem_free<CG>(tmem, 512);
@@ -857,16 +882,16 @@ cudaError_t launch_gemm_as(const GemmPlan& g, int splits, const Epi& epi, cudaSt
 // `splits` blocks: waves of tiles, k-blocks of a tile, and what a tile costs besides.  A k-block of a 256 x 256 tile
 // takes 0.27 us per product of pieces, one of a 128 x 128 tile on its one SM 0.25 us (a quarter of the work on half of the
 // SMs: each operand byte is used half as often); a 128 x 128 tile is a block's only one, so nothing hides its start and
-// end.  Measured, all of a call with either: 512 x 512 fp32, two steps, 117 us and (4 blocks) 68 us; 8 x 1024 x 2816
-// bfloat16 256 us and (1 block) 461 us; gradient of 8000 tokens x 128 x 300, bf16, 146 us and (4 blocks) 91 us.
-inline double gemm_microseconds(int64_t m, int64_t n, int64_t kblocks, int64_t batch, int products, bool symmetric, int splits, int sms)
+// end.  tail: the epilogue of a block's 128 x 256 part of the last tile.  Measured, all of a call with either: 512 x 512 fp32, two steps, 117 us and (4 blocks) 60 us; 8 x 1024 x 2816
+// bfloat16 255 us and (1 block) 456 us; gradient of 8000 tokens x 128 x 300, bf16, 145 us and (4 blocks) 84 us.
+inline double gemm_microseconds(int64_t m, int64_t n, int64_t kblocks, int64_t batch, int products, double tail, bool symmetric, int splits, int sms)
 {
     const int64_t side = splits ? 128 : 256, tm = (m + side - 1) / side, tn = (n + side - 1) / side;
     const int64_t tiles = batch * (symmetric ? tm * (tm + 1) / 2 : tm * tn);
-    if (!splits) return (double)((tiles + sms / 2 - 1) / (sms / 2)) * (0.27 * products * kblocks + 0.3) + 4.0;
+    if (!splits) return (double)((tiles + sms / 2 - 1) / (sms / 2)) * (0.27 * products * kblocks + 0.3) + (products > 1 ? 5.0 : 3.0) + tail;
     const int64_t room = splits == 8 ? sms * 3 / 4 : splits == 4 ? sms * 9 / 10 : sms;   // SMs of whole clusters
     const int64_t waves = (tiles * splits + room - 1) / room;
-    return waves * (0.25 * products * ((kblocks + splits - 1) / splits) + 4.0) + (splits == 1 ? 0.0 : splits == 2 ? 0.5 : splits == 4 ? 1.0 : 3.5);
+    return waves * (0.25 * products * ((kblocks + splits - 1) / splits) + 2.6 + (1.4 + 0.5 * tail) / splits + (splits > 1 ? 0.5 : 0.0));
 }
 
 // The variant that should take the least time.
@@ -876,9 +901,9 @@ cudaError_t launch_gemm(const GemmPlan& g, const Epi& epi, cudaStream_t stream)
     const int products = P * (P + 1) / 2;
     const int64_t n = Epi::kDual ? 2 * g.n : g.n, kblocks = (g.k + kTileK - 1) / kTileK * g.pairs * (g.b[0].pieces - g.a[0].pieces + 1);
     int best = 0;
-    double least = gemm_microseconds(g.m, n, kblocks, g.batch, products, g.symmetric, 0, sm_count());
+    double least = gemm_microseconds(g.m, n, kblocks, g.batch, products, Epi::kTail, g.symmetric, 0, sm_count());
     for (int splits = 1; splits <= 8 && splits <= kblocks; splits *= 2) {
-        const double t = gemm_microseconds(g.m, n, kblocks, g.batch, products, g.symmetric, splits, sm_count());
+        const double t = gemm_microseconds(g.m, n, kblocks, g.batch, products, Epi::kTail, g.symmetric, splits, sm_count());
         if (t < least) least = t, best = splits;
     }
     if (best) return launch_gemm_as<Variant<1, 128, P, 8, true>>(g, best, epi, stream);

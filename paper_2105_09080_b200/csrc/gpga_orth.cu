@@ -115,6 +115,7 @@ __global__ void __launch_bounds__(256) start_kernel(const T* m, int64_t ld, int6
 template <int P>
 struct KeepPieces {
     static constexpr bool kDual = false, kMirror = true;
+    static constexpr double kTail = 1.0;
     static constexpr int kWarps = 8;
     struct Ahead {
         Raw<__half> r[P];
@@ -160,6 +161,7 @@ struct KeepPieces {
 template <class T>
 struct LastStep {
     static constexpr bool kDual = false, kMirror = false;
+    static constexpr double kTail = 1.0;
     static constexpr int kWarps = 8;
     using Ahead = Raw<T>;
     T* out;

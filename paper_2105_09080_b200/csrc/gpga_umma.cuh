@@ -20,6 +20,11 @@ __device__ __forceinline__ void cluster_barrier()
 {
     asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
+// The last one, after which nobody's shared memory is touched: it does not wait for stores to global memory.
+__device__ __forceinline__ void cluster_farewell()
+{
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
 // Address of this block's shared variable at `addr` as it lies in block `rank` of the cluster.
 __device__ __forceinline__ uint32_t map_shared(uint32_t addr, uint32_t rank)
 {
@@ -27,9 +32,11 @@ __device__ __forceinline__ uint32_t map_shared(uint32_t addr, uint32_t rank)
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
-__device__ __forceinline__ void load_shared_cluster(uint32_t addr, float& a, float& b, float& c, float& d)
+// Bytes of this block's shared memory to another block of the cluster; they are counted at `bar`, which lies there.
+__device__ __forceinline__ void copy_to_block(uint32_t dst, uint32_t src, uint32_t bytes, uint32_t bar)
 {
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(a), "=f"(b), "=f"(c), "=f"(d) : "r"(addr) : "memory");
+    asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "r"(src), "r"(bytes), "r"(bar)
+                 : "memory");
 }
 // Arrivals on a barrier anywhere in the cluster.  What they announce is ordered by other means (asynchronous copies count
 // their own bytes, tensor memory has its own fences), so they need no cluster-wide release: with one per stage a product
