@@ -19,9 +19,14 @@ struct FeedForwardParams {
     char* scratch = nullptr;
 };
 
-// Tokens per node up to which the forward pass reads the weights where they lie, without the tensor memory path: up to
-// there its time is that of reading them.
-inline bool ff_few(const FeedForwardParams& p) { return p.rows <= (p.dtype == 0 ? 8 : 32); }
+// Whether the forward pass reads the weights where they lie, without the tensor memory path: for few tokens its time is
+// that of reading them.  Measured with either: 32 tokens, 2048 x 5632, 16-bit weights 30 us and 33 us, fp32 weights 38 us
+// and 94 us; 24 tokens, 4096 x 11008, 16-bit weights 94 us and 81 us, 16 tokens 81 us and 81 us.
+inline bool ff_few(const FeedForwardParams& p)
+{
+    if (p.dtype == 0) return p.rows <= 8;
+    return p.rows <= 16 || (p.rows <= 32 && (p.weight_dtype == 0 || p.d * p.f <= 20'000'000));
+}
 int64_t ff_few_scratch_bytes(const FeedForwardParams& p);
 cudaError_t launch_ff_few(const FeedForwardParams& p, cudaStream_t stream);
 

@@ -1,14 +1,18 @@
 // Gated feed-forward block of few tokens per node (a trained model answering): every weight is read once, straight from where it lies,
 // and that is what bounds it.
 //
-// Two launches, h = act(x Wg^T) (x Wu^T) and y = h Wd^T.  A cluster of up to eight blocks takes 16 rows of the weights (fp32:
-// 4), its warps a part of k each, so that all that is to be read is soon in flight; their sums are added through the
-// cluster's shared memory in a fixed order.  16-bit activations: the weights are the rows of
-// m16n8k16 matrix instructions and the tokens their columns; as a sum over k may run in any order, a lane takes eight
-// neighbouring k (128 or 256 bits of weights, 128 of x) and both operands use them in the same places of two instructions.
-// The tensor memory path would need its 128 rows through shared memory first; at up to 32 tokens the instructions are not
-// what bounds.  fp32 activations: fp32 arithmetic.  The second launch starts while the first runs and asks for its weights
-// to be brought into L2 meanwhile.
+// Two launches, h = act(x Wg^T) (x Wu^T) and y = h Wd^T.  16-bit activations: the weights are the rows of m16n8k16 matrix
+// instructions (eight of the gate and the same eight of the other projection, or sixteen of Wd) and the tokens their
+// columns; as a sum over k may run in any order, a lane takes eight neighbouring k and both operands use them in the same
+// places of two instructions.  The tensor memory path would need 128 rows at a time; at up to 32 tokens the instructions
+// are not what bounds.  A block's warps take a part of k each and add up through shared memory, in a fixed order.
+//
+// Rows on 16 bytes are streamed: every warp has 12 to 14 KB of its part on the way to its own ring in shared memory all the time,
+// across the tiles that a block goes through (24 tokens, 2048 x 5632, fp32 weights, 138 MB: 45 us with loads to registers,
+// 36 us streamed; one token 26.7 us, 5.2 TB/s).  With more tokens the reading of x for every tile (from L2) adds 3 us for
+// each eight of them.
+// Others are loaded as they lie, on clusters of blocks where there are few tiles.  fp32 activations: fp32 arithmetic.  The
+// second launch begins to read its weights while the first runs.
 #include <type_traits>
 
 #include "gpga_ff_device.cuh"
@@ -163,29 +167,8 @@ __global__ void __launch_bounds__(kFewWarps * 32) few_tokens_kernel(const __grid
                 }
         }
     };
-    // Whole steps of aligned rows, U of them asked for at once; then what is left, or all of it.
-    constexpr int step_registers = M * 2 * 2 * (int)sizeof(W) + NT * 4, U = step_registers * 6 <= 80 ? 6 : step_registers * 4 <= 80 ? 4 : step_registers * 2 <= 80 ? 2 : 1;
-    int k = k0;
-    if (p.vec_w && p.vec_x) {
-        const int whole = min(k1, p.k / 32 * 32);
-        for (; k + 32 * U <= whole; k += 32 * U) {
-            Raw<W> wv[U][M][2];
-            Raw<T> xv[U][NT];
-#pragma unroll
-            for (int j = 0; j < U; ++j) {
-#pragma unroll
-                for (int m = 0; m < M; ++m)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) wv[j][m][h].load16(wr[m][h] + k + 32 * j);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) xv[j][n].load16(xr[n] + k + 32 * j);
-            }
-#pragma unroll
-            for (int j = 0; j < U; ++j) multiply(wv[j], xv[j]);
-        }
-    }
 #pragma unroll 1
-    for (; k < k1; k += 32) {
+    for (int k = k0; k < k1; k += 32) {
         Raw<W> wv[M][2];
         Raw<T> xv[NT];
         const int left = p.k - k - place;
@@ -213,6 +196,147 @@ __global__ void __launch_bounds__(kFewWarps * 32) few_tokens_kernel(const __grid
         finish<T, T, GATE>(p, node, n, row0 + r, s[0], s[M - 1]);
     }
     cluster_farewell();   // nobody goes while its sums are read
+}
+
+// Streamed: 16 rows of weights and 64 of k to a stage.
+constexpr int kStreamK = 64;
+template <class W> constexpr int kStreamStages = sizeof(W) == 4 ? 4 : 8;
+template <class W> constexpr int kStreamStage = 16 * kStreamK * (int)sizeof(W);   // bytes
+
+template <class T, class W, int NT, bool GATE>
+__global__ void __launch_bounds__(kFewWarps * 32) few_streamed_kernel(const __grid_constant__ FewParams p)
+{
+    constexpr int N = 8 * NT, S = 16 + 4, stages = kStreamStages<W>, stage_bytes = kStreamStage<W>;
+    constexpr int G = kStreamK * (int)sizeof(W) / 16;    // 16-byte groups of a row
+    extern __shared__ __align__(16) unsigned char shared[];
+    float* const sums = reinterpret_cast<float*>(shared + kFewWarps * stages * stage_bytes);   // [tile & 1][warp][token][row]
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, node = blockIdx.y;
+    const int group = lane >> 2, quad = lane & 3;
+    unsigned char* const ring = shared + warp * stages * stage_bytes;
+    const int tiles = GATE ? (p.rows + 7) / 8 : (p.rows + 15) / 16;
+    const int steps = (p.k + kStreamK - 1) / kStreamK, each = (steps + kFewWarps - 1) / kFewWarps;
+    const int s0 = min(warp * each, steps), mine = min(each, steps - s0);   // steps of k of this warp
+    const W* const w1 = static_cast<const W*>(p.w1) + node * p.node1;
+    const W* const w2 = GATE ? static_cast<const W*>(p.w2) + node * p.node2 : nullptr;
+    grid_launch_dependents();
+
+    // rows 0 to 7 of a stage: of the gate, 8 to 15 of the other (or 16 of the one); neighbouring rows' groups change places
+    const auto swizzle = [](int r) { return sizeof(W) == 4 ? r & 7 : 4 * (r & 1); };
+    int ask_tile = blockIdx.x, ask_step = 0, ask_slot = 0;
+    const auto ask = [&] {
+        if (mine > 0 && ask_tile < tiles) {
+            const int k0 = (s0 + ask_step) * kStreamK;
+#pragma unroll
+            for (int i = 0; i < 16 * G / 32; ++i) {
+                const int at = i * 32 + lane, r = at / G, g = at % G;
+                const int row = GATE ? min(ask_tile * 8 + (r & 7), p.rows - 1) : min(ask_tile * 16 + r, p.rows - 1);
+                const int k = k0 + g * (16 / (int)sizeof(W)), bytes = max(0, min(16, (p.k - k) * (int)sizeof(W)));
+                const W* const from = GATE && r >= 8 ? w2 + row * p.ld2 : w1 + row * p.ld1;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(ring + ask_slot * stage_bytes + r * (G * 16) + ((g ^ swizzle(r)) << 4))),
+                             "l"(from + (bytes ? k : 0)), "r"(bytes)
+                             : "memory");
+            }
+            if (++ask_step == mine) ask_step = 0, ask_tile += gridDim.x;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (++ask_slot == stages) ask_slot = 0;
+    };
+#pragma unroll 1
+    for (int i = 0; i < stages - 1; ++i) ask();
+    if (p.after) grid_dependency_wait();
+
+    const T* const x = static_cast<const T*>(p.x) + (int64_t)node * p.tokens * p.ldx + quad * 8;
+    const T* xr[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) xr[n] = x + min(8 * n + group, p.tokens - 1) * p.ldx;
+    int slot = 0, turn = 0;
+#pragma unroll 1
+    for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x, turn ^= 1) {
+        float acc[NT][4] = {};
+#pragma unroll 1
+        for (int step = 0; step < mine; ++step) {
+            const int k0 = (s0 + step) * kStreamK;
+            Raw<T> xv[2][NT];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const int k = k0 + 32 * h, left = p.k - k - quad * 8;
+                    if (left >= 8)
+                        xv[h][n].load16(xr[n] + k);
+                    else
+                        xv[h][n].load(xr[n] + k, left, false);
+                }
+            asm volatile("cp.async.wait_group %0;" ::"n"(stages - 2) : "memory");
+            __syncwarp();
+            ask();      // into the slot that the step before this one was read from
+            const unsigned char* const stage = ring + slot * stage_bytes;
+            if (++slot == stages) slot = 0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                constexpr int Q = sizeof(W) / 2;
+                uint32_t lo[Q][4], hi[Q][4];
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int r = group + 8 * half;
+                    Raw<W> wv;
+#pragma unroll
+                    for (int i = 0; i < Q; ++i) {
+                        const int g = (32 * h + 8 * quad) * (int)sizeof(W) / 16 + i;
+                        const uint4 v = *reinterpret_cast<const uint4*>(stage + r * (G * 16) + ((g ^ swizzle(r)) << 4));
+                        wv.w[4 * i] = v.x, wv.w[4 * i + 1] = v.y, wv.w[4 * i + 2] = v.z, wv.w[4 * i + 3] = v.w;
+                    }
+                    if (half)
+                        as_pairs<T>(wv, hi);
+                    else
+                        as_pairs<T>(wv, lo);
+                }
+#pragma unroll
+                for (int q = Q - 1; q >= 0; --q)
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        const uint32_t a[4] = {lo[q][2 * s], hi[q][2 * s], lo[q][2 * s + 1], hi[q][2 * s + 1]};
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            const uint32_t b[2] = {xv[h][n].w[2 * s], xv[h][n].w[2 * s + 1]};
+                            mma16816<T>(acc[n], a, b);
+                        }
+                    }
+            }
+            __syncwarp();
+        }
+        float* const here = sums + turn * kFewWarps * N * S;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) here[(warp * N + 8 * n + 2 * quad + (e & 1)) * S + 8 * (e >> 1) + group] = acc[n][e];
+        __syncthreads();
+        constexpr int R = GATE ? 8 : 16;
+        for (int i = threadIdx.x; i < R * N; i += kFewWarps * 32) {
+            const int r = i % R, n = i / R, row = tile * R + r;
+            if (row >= p.rows || n >= p.tokens) continue;
+            float a = 0.f, b = 0.f;
+#pragma unroll
+            for (int v = 0; v < kFewWarps; ++v) {
+                a += here[(v * N + n) * S + r];
+                if constexpr (GATE) b += here[(v * N + n) * S + r + 8];
+            }
+            finish<T, T, GATE>(p, node, n, row, a, b);
+        }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+}
+
+template <class T, class W, int NT, bool GATE>
+cudaError_t launch_streamed(FewParams p, int64_t nodes, cudaStream_t stream)
+{
+    constexpr int bytes = kFewWarps * (kStreamStages<W> * kStreamStage<W> + 2 * 8 * NT * 20 * 4);
+    const auto kernel = few_streamed_kernel<T, W, NT, GATE>;
+    static std::atomic<unsigned long long> limit_set{0};
+    const cudaError_t e = ensure_smem_limit(kernel, bytes, limit_set);
+    if (e != cudaSuccess) return e;
+    const int64_t tiles = (p.rows + (GATE ? 7 : 15)) / (GATE ? 8 : 16), blocks = std::max<int64_t>(1, std::min<int64_t>(tiles, (sm_count() + nodes - 1) / nodes));
+    return launch_after_trigger(kernel, dim3((unsigned)blocks, (unsigned)nodes), dim3(kFewWarps * 32), bytes, stream, p.after != 0, p);
 }
 
 // fp32: R rows of the weights and N tokens to a block, its warps a part of k each.
@@ -329,6 +453,9 @@ cudaError_t launch_clusters(void (*kernel)(FewParams), FewParams p, int rows, in
 template <class T, class W, bool GATE>
 cudaError_t few16(const FewParams& p, int64_t nodes, cudaStream_t stream)
 {
+    if (p.vec_w && p.vec_x)
+        return p.tokens <= 8 ? launch_streamed<T, W, 1, GATE>(p, nodes, stream) : p.tokens <= 16 ? launch_streamed<T, W, 2, GATE>(p, nodes, stream)
+                                                                                                : launch_streamed<T, W, 4, GATE>(p, nodes, stream);
     const auto kernel = p.tokens <= 8 ? few_tokens_kernel<T, W, 1, GATE> : p.tokens <= 16 ? few_tokens_kernel<T, W, 2, GATE> : few_tokens_kernel<T, W, 4, GATE>;
     return launch_clusters(kernel, p, 16, 32, nodes, stream);
 }
