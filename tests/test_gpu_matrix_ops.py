@@ -264,6 +264,21 @@ def test_slices_of_the_state_matrix(dtype):
     assert torch.equal(G[:, :lead], before[:, :lead]) and torch.equal(G[:, lead + 3 * s:], before[:, lead + 3 * s:])
 
 
+@pytest.mark.parametrize("size", [(2, 30, 24, 40), (1, 300, 129, 77)], ids=str)
+def test_16_bit_gradients_added_to(size):
+    """Sums of whole numbers below 2^11 (fp16): the sum of old and new is rounded once."""
+    n, t, d, f = size
+    x, gate, up, down = whole_inputs(*size, F16, F16, seed=18)
+    gen = generator(19)
+    y, g, u = pkg.feed_forward_forward(x, gate, up, down, activation="relu")
+    grads = pkg.feed_forward_backward(x, x, g, u, gate, up, down, activation="relu")[1:]
+    old = [whole(w.shape, gen, F16) for w in grads]
+    new = [w.clone() for w in old]
+    pkg.feed_forward_backward(x, x, g, u, gate, up, down, activation="relu", dgate=new[0], dup=new[1], ddown=new[2], accumulate=True)
+    exact = whole_backward(x, x, g, u, gate, up, down)[1:]
+    assert all(torch.equal(a, (b.double() + c).to(F16)) for a, b, c in zip(new, old, exact))
+
+
 @pytest.mark.parametrize("rows", [3, 20, 200])
 def test_outputs_in_the_place_of_inputs(rows):
     x, gate, up, down = whole_inputs(2, rows, 40, 56, BF16, BF16, seed=10)
