@@ -27,6 +27,12 @@ inline bool ff_few(const FeedForwardParams& p)
     if (p.dtype == 0) return p.rows <= 8;
     return p.rows <= 16 || (p.rows <= 32 && (p.weight_dtype == 0 || p.d * p.f <= 20'000'000));
 }
+// Whether fp32 operands are taken as pairs of fp16 values (three products of pieces, with a pass over every array for its largest
+// value) and not as three bfloat16 values (six products): where the products take long enough for the passes.
+inline bool ff_pairs(const FeedForwardParams& p, bool backward)
+{
+    return p.dtype == 0 && (double)p.nodes * p.rows * p.d * p.f * (backward ? 12 : 6) >= 1.3e10;
+}
 int64_t ff_few_scratch_bytes(const FeedForwardParams& p);
 cudaError_t launch_ff_few(const FeedForwardParams& p, cudaStream_t stream);
 

@@ -30,8 +30,8 @@ template <class T>
 cudaError_t weight_gradient(const GemmPlan& g, const FeedForwardParams& p, const Matrix& out, int64_t rows, const Matrix* second, cudaStream_t stream)
 {
     constexpr int P = PiecesOf<T>::count;
-    if (p.grad_dtype == 0) return store_product<float, P>(g, out, rows, second, p.accumulate, stream);
-    if constexpr (P == 1) return store_product<T, P>(g, out, rows, second, p.accumulate, stream);
+    if (p.grad_dtype == 0) return store_product<float, P>(g, out, rows, second, p.accumulate, Exponents(), stream);
+    if constexpr (P == 1) return store_product<T, P>(g, out, rows, second, p.accumulate, Exponents(), stream);
     return cudaErrorInvalidValue;
 }
 
@@ -95,7 +95,108 @@ cudaError_t backward(const FeedForwardParams& p, cudaStream_t stream)
     g.m = p.rows;
     g.n = p.d;
     g.k = p.f;
-    return store_product<T, P>(g, p.dx, p.nodes * p.rows, nullptr, false, stream);
+    return store_product<T, P>(g, p.dx, p.nodes * p.rows, nullptr, false, Exponents(), stream);
+}
+
+// fp32 as pairs of fp16.
+struct PairsPlan {
+    PackPlan in, between;
+    Operand x, dy, gate, up, down, h, dgu;
+    float *hf, *dguf;
+    int64_t ldh;
+    uint32_t *parts, *peaks;     // of dy, down, x, gate, up (kPeakParts each); of h, of dg and du
+    int32_t* exponents;          // of dy, down, x, gate and up, up again, h, dg and du
+};
+
+PairsPlan plan_pairs(const FeedForwardParams& p)
+{
+    PairsPlan q;
+    q.in.base = q.between.base = p.scratch;
+    q.in.pieces = q.between.pieces = 2;
+    ScratchPlan& s = q.in.scratch;
+    q.parts = reinterpret_cast<uint32_t*>(p.scratch + s.take(5 * kPeakParts * 4));
+    q.peaks = reinterpret_cast<uint32_t*>(p.scratch + s.take(8));
+    q.exponents = reinterpret_cast<int32_t*>(p.scratch + s.take(7 * 4));
+    q.dy = q.in.operand(p.dy.p, p.dy.ld, p.rows * p.dy.ld, p.rows, p.d, p.nodes, true, false, 2);
+    q.in.scaled(q.parts, kPeakParts, q.exponents);
+    q.down = q.in.operand(p.down.p, p.down.ld, p.down.node, p.d, p.f, p.nodes, true, true, 2);
+    q.in.scaled(q.parts + kPeakParts, kPeakParts, q.exponents + 1);
+    q.x = q.in.operand(p.x.p, p.x.ld, p.rows * p.x.ld, p.rows, p.d, p.nodes, true, true, 2);
+    q.in.scaled(q.parts + 2 * kPeakParts, kPeakParts, q.exponents + 2);
+    q.gate = q.in.operand(p.gate.p, p.gate.ld, p.gate.node, p.f, p.d, p.nodes, true, true, 2);
+    q.in.scaled(q.parts + 3 * kPeakParts, 2 * kPeakParts, q.exponents + 3);   // one power for both: their products are one sum
+    q.up = q.in.operand(p.up.p, p.up.ld, p.up.node, p.f, p.d, p.nodes, true, true, 2);
+    q.in.scaled(q.parts + 3 * kPeakParts, 2 * kPeakParts, q.exponents + 4);
+    q.ldh = (p.f + 7) / 8 * 8;
+    q.hf = reinterpret_cast<float*>(p.scratch + s.take(p.nodes * p.rows * q.ldh * 4));
+    q.dguf = reinterpret_cast<float*>(p.scratch + s.take(2 * p.nodes * p.rows * q.ldh * 4));
+    q.between.scratch = s;
+    q.h = q.between.operand(q.hf, q.ldh, p.rows * q.ldh, p.rows, p.f, p.nodes, true, true, 2);
+    q.between.scaled(q.peaks, 1, q.exponents + 5);
+    q.dgu = q.between.operand(q.dguf, q.ldh, p.rows * q.ldh, p.rows, p.f, 2 * p.nodes, true, true, 2);   // dg of all nodes, then du
+    q.between.scaled(q.peaks + 1, 1, q.exponents + 6);
+    return q;
+}
+
+cudaError_t backward_pairs(const FeedForwardParams& p, cudaStream_t stream)
+{
+    const PairsPlan q = plan_pairs(p);
+    cudaError_t e = q.in.launch_peaks(q.parts, q.peaks, stream);
+    if (e == cudaSuccess) e = q.in.launch<__half>(stream);
+    if (e != cudaSuccess) return e;
+    GemmPlan g;
+    g.half = true;
+    g.batch = g.bmod = p.nodes;
+    g.after = true;
+    g.a[0] = q.dy;
+    g.b[0] = q.down;
+    g.m = p.rows;
+    g.n = p.f;
+    g.k = p.d;
+    GateGrad<float, true> grad;
+    grad.g = static_cast<const float*>(p.g.p);
+    grad.u = static_cast<const float*>(p.u.p);
+    grad.ldg = p.g.ld;
+    grad.ldu = p.u.ld;
+    grad.h = {q.hf, q.ldh, p.rows * q.ldh};
+    grad.dg = {q.dguf, q.ldh, p.rows * q.ldh};
+    grad.du = {q.dguf + p.nodes * p.rows * q.ldh, q.ldh, p.rows * q.ldh};
+    grad.exponents = {q.exponents, q.exponents + 1};
+    grad.peaks = q.peaks;
+    grad.m = (int32_t)p.rows;
+    grad.kind = p.activation;
+    grad.vec = rows_on_16(p.g.p, p.g.ld, p.nodes * p.rows, 0, 1, 4) && rows_on_16(p.u.p, p.u.ld, p.nodes * p.rows, 0, 1, 4);
+    e = launch_gemm<2>(g, grad, stream);
+    if (e == cudaSuccess) e = q.between.launch<__half>(stream);
+    if (e != cudaSuccess) return e;
+
+    g.a[0] = q.dy;                      // dWd
+    g.a[0].mn_major = true;
+    g.b[0] = q.h;
+    g.m = p.d;
+    g.n = p.f;
+    g.k = p.rows;
+    if ((e = store_product<float, 2>(g, p.ddown, p.d, nullptr, p.accumulate, {q.exponents, q.exponents + 5}, stream)) != cudaSuccess) return e;
+    g.a[0] = q.dgu;                     // dWg, dWu
+    g.b[0] = q.x;
+    g.m = p.f;
+    g.n = p.d;
+    g.batch = 2 * p.nodes;
+    if ((e = store_product<float, 2>(g, p.dgate, p.f, &p.dup, p.accumulate, {q.exponents + 6, q.exponents + 2}, stream)) != cudaSuccess) return e;
+    Operand dg = q.dgu, du = q.dgu;
+    dg.batches = du.batches = p.nodes;
+    du.base = static_cast<const __half*>(du.base) + p.nodes * du.batch;
+    g.pairs = 2;                        // dx
+    g.batch = p.nodes;
+    g.a[0] = dg;
+    g.a[1] = du;
+    g.a[0].mn_major = g.a[1].mn_major = false;
+    g.b[0] = q.gate;
+    g.b[1] = q.up;
+    g.m = p.rows;
+    g.n = p.d;
+    g.k = p.f;
+    return store_product<float, 2>(g, p.dx, p.nodes * p.rows, nullptr, false, {q.exponents + 6, q.exponents + 3}, stream);
 }
 
 template <class T>
@@ -135,11 +236,12 @@ unsigned int* ff_backward_gave_up()
     return cudaGetSymbolAddress(&at, gave_up) == cudaSuccess ? static_cast<unsigned int*>(at) : nullptr;
 }
 
-int64_t ff_backward_scratch_bytes(const FeedForwardParams& p) { return p.rows ? plan_backward(p).pack.scratch.bytes : 0; }
+int64_t ff_backward_scratch_bytes(const FeedForwardParams& p) { return !p.rows ? 0 : ff_pairs(p, true) ? plan_pairs(p).between.scratch.bytes : plan_backward(p).pack.scratch.bytes; }
 
 cudaError_t launch_ff_backward(const FeedForwardParams& p, cudaStream_t stream)
 {
     if (p.rows == 0) return no_tokens(p, stream);
+    if (ff_pairs(p, true)) return backward_pairs(p, stream);
     if (p.dtype == 0) return backward<float>(p, stream);
     if (p.dtype == 1) return backward<__nv_bfloat16>(p, stream);
     return backward<__half>(p, stream);

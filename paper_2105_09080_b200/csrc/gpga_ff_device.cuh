@@ -1,5 +1,7 @@
 // Gated feed-forward block: the activation and its slope, and what the products' epilogues do with them.
 #pragma once
+#include <type_traits>
+
 #include "gpga_ff.cuh"
 #include "gpga_pack.cuh"
 
@@ -20,12 +22,12 @@ __device__ __forceinline__ float fast_reciprocal(float x)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// 1 / (1 + e^-v) and e^(-v^2 / 2).  fp32 results take CUDA's expf and division; the fast forms' errors are below the rounding
-// of 16-bit ones.
+// 1 / (1 + e^-v) and e^(-v^2 / 2).  fp32 results take CUDA's expf and its division to two steps (2^-22); the fast forms' errors
+// are below the rounding of 16-bit ones.
 template <bool FAST>
 __device__ __forceinline__ float sigmoid(float v)
 {
-    return FAST ? fast_reciprocal(1.f + fast_exp2(-1.44269504f * v)) : 1.f / (1.f + expf(-v));
+    return FAST ? fast_reciprocal(1.f + fast_exp2(-1.44269504f * v)) : __fdividef(1.f, 1.f + expf(-v));
 }
 template <bool FAST>
 __device__ __forceinline__ float bell(float v)
@@ -79,8 +81,39 @@ __device__ __forceinline__ void act_slopes(float (&v)[N], float (&s)[N], int kin
 template <class T> struct PiecesOf { using type = T; static constexpr int count = 1; };
 template <> struct PiecesOf<float> { using type = __nv_bfloat16; static constexpr int count = 3; };
 
-// g, u -> h = act(g) u as pieces; g and u themselves where they are kept.
-template <class T>
+// fp32 operands as pairs of fp16 (ff_pairs): a product is 2^exponent times the product of what was packed, whose arrays have
+// an exponent each.  Two factors, as one may be beyond fp32's range.
+struct Exponents {
+    const int32_t *a = nullptr, *b = nullptr;
+    __device__ __forceinline__ void factors(float& f, float& g) const
+    {
+        f = g = 1.f;
+        if (!a) return;
+        const int e = max(-250, min(250, *a + *b)), h = e >> 1;
+        f = __int_as_float((h + 127) << 23);
+        g = __int_as_float((e - h + 127) << 23);
+    }
+};
+// An array between two products that is packed after the first: fp32 rows, and the bits of its largest finite value.
+struct Between {
+    float* base = nullptr;
+    int64_t ld = 0, batch = 0;
+    __device__ __forceinline__ void store(int64_t place, const float (&v)[8]) const
+    {
+        reinterpret_cast<float4*>(base + place)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4*>(base + place)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    }
+};
+__device__ __forceinline__ void note_peak(int which, const float (&v)[8], int left)
+{
+    uint32_t peak = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) peak = max(peak, i < left ? finite_bits(v[i]) : 0u);
+    if (peak > block_peaks()[which]) atomicMax(block_peaks() + which, peak);
+}
+
+// g, u -> h = act(g) u as pieces (PAIRS: as fp32); g and u themselves where they are kept.
+template <class T, bool PAIRS = false>
 struct GateUp {
     static constexpr bool kDual = true, kMirror = false;
     static constexpr double kTail = 3.0;
@@ -88,18 +121,32 @@ struct GateUp {
     using T16 = typename PiecesOf<T>::type;
     static constexpr int P = PiecesOf<T>::count;
     using Ahead = NothingAhead;
+    static constexpr int kPeaks = PAIRS ? 1 : 0;
     T *g, *u;
     int64_t ldg, ldu;
-    Pieces<T16> h;
+    std::conditional_t<PAIRS, Between, Pieces<T16>> h;
+    Exponents exponents;
+    uint32_t* peaks;
     int32_t m, kind, keeps, vec;
 
     __device__ __forceinline__ bool wide() const { return vec; }
     __device__ __forceinline__ void keep(int which, float v, int batch, int row, int col) const
     {
+        if constexpr (PAIRS) {
+            float e, f;
+            exponents.factors(e, f);
+            v = v * e * f;
+        }
         (which ? u : g)[((int64_t)batch * m + row) * (which ? ldu : ldg) + col] = from_f32<T>(v);
     }
     __device__ __forceinline__ void eight(float (&v)[8], float (&w)[8], int batch, int row, int col, int left) const
     {
+        if constexpr (PAIRS) {
+            float e, f;
+            exponents.factors(e, f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = v[i] * e * f, w[i] = w[i] * e * f;
+        }
         if (keeps && vec) {
             const int64_t at = (int64_t)batch * m + row;
             store8(g + at * ldg + col, left, v);
@@ -108,12 +155,17 @@ struct GateUp {
         act_values<sizeof(T) == 2>(v, kind);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] *= w[i];
-        h.template store<P>(batch, row, col, v);
+        if constexpr (PAIRS) {
+            note_peak(0, v, left);
+            h.store(batch * h.batch + row * h.ld + col, v);
+        } else {
+            h.template store<P>(batch, row, col, v);
+        }
     }
 };
 
-// acc = dh; g, u -> h = act(g) u, du = dh act(g), dg = dh u act'(g), all as pieces.
-template <class T>
+// acc = dh; g, u -> h = act(g) u, du = dh act(g), dg = dh u act'(g), all as pieces (PAIRS: as fp32).
+template <class T, bool PAIRS = false>
 struct GateGrad {
     static constexpr bool kDual = false, kMirror = false;
     static constexpr double kTail = 6.0;
@@ -123,9 +175,12 @@ struct GateGrad {
     struct Ahead {
         Raw<T> g, u;
     };
+    static constexpr int kPeaks = PAIRS ? 2 : 0;
     const T *g, *u;
     int64_t ldg, ldu;
-    Pieces<T16> h, dg, du;
+    std::conditional_t<PAIRS, Between, Pieces<T16>> h, dg, du;
+    Exponents exponents;
+    uint32_t* peaks;      // of h; of dg and du
     int32_t m, kind, vec;
 
     __device__ __forceinline__ bool wide() const { return true; }
@@ -136,23 +191,38 @@ struct GateGrad {
         ahead.g.load(g + at * ldg + col, left, vec);
         ahead.u.load(u + at * ldu + col, left, vec);
     }
-    __device__ __forceinline__ void eight(float (&dh)[8], const Ahead& now, int batch, int row, int col, int) const
+    __device__ __forceinline__ void put(const std::conditional_t<PAIRS, Between, Pieces<T16>>& to, int64_t at, const float (&v)[8], int which, int left) const
+    {
+        if constexpr (PAIRS) {
+            note_peak(which, v, left);
+            to.store(at, v);
+        } else {
+            to.template store_at<P>(at, v);
+        }
+    }
+    __device__ __forceinline__ void eight(float (&dh)[8], const Ahead& now, int batch, int row, int col, int left) const
     {
         float a[8], s[8], uv[8];
+        if constexpr (PAIRS) {
+            float e, f;
+            exponents.factors(e, f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dh[i] = dh[i] * e * f;
+        }
         now.g.values(a);
         now.u.values(uv);
         act_slopes<sizeof(T) == 2>(a, s, kind);
-        const int64_t at = h.at(batch, row, col);    // of all three
+        const int64_t at = batch * h.batch + row * h.ld + col;    // of all three
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[i] *= dh[i] * uv[i];
-        dg.template store_at<P>(at, s);
+        put(dg, at, s, 1, left);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             dh[i] *= a[i];
             a[i] *= uv[i];
         }
-        h.template store_at<P>(at, a);
-        du.template store_at<P>(at, dh);
+        put(h, at, a, 0, left);
+        put(du, at, dh, 1, left);
     }
 };
 
@@ -162,9 +232,11 @@ struct StoreRows {
     static constexpr bool kDual = false, kMirror = false;
     static constexpr double kTail = 1.0;
     static constexpr int kWarps = 8;
+    static constexpr int kPeaks = 0;
     using Ahead = Raw<T>;
     T* out[2];
     int64_t ld[2], node[2];
+    Exponents exponents;
     int32_t split, accumulate, vec;
 
     __device__ __forceinline__ bool wide() const { return vec; }
@@ -176,9 +248,18 @@ struct StoreRows {
     __device__ __forceinline__ void load(Ahead& old, int batch, int row, int col, int left) const { rows(batch).ahead(old, row, col, left); }
     __device__ __forceinline__ void eight(float (&v)[8], const Ahead& old, int batch, int row, int col, int left) const
     {
+        float e, f;
+        exponents.factors(e, f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = v[i] * e * f;
         rows(batch).eight(v, old, row, col, left);
     }
-    __device__ __forceinline__ void one(float v, int batch, int row, int col) const { rows(batch).one(v, row, col); }
+    __device__ __forceinline__ void one(float v, int batch, int row, int col) const
+    {
+        float e, f;
+        exponents.factors(e, f);
+        rows(batch).one(v * e * f, row, col);
+    }
 };
 
 inline bool rows_on_16(const void* p, int64_t ld, int64_t rows, int64_t node, int64_t nodes, int size)
@@ -187,9 +268,10 @@ inline bool rows_on_16(const void* p, int64_t ld, int64_t rows, int64_t node, in
 }
 
 template <class T, int P>
-cudaError_t store_product(const GemmPlan& g, const Matrix& out, int64_t rows, const Matrix* second, bool accumulate, cudaStream_t stream)
+cudaError_t store_product(const GemmPlan& g, const Matrix& out, int64_t rows, const Matrix* second, bool accumulate, const Exponents& exponents, cudaStream_t stream)
 {
     StoreRows<T> e;
+    e.exponents = exponents;
     const Matrix& o2 = second ? *second : out;
     e.out[0] = static_cast<T*>(out.p);
     e.out[1] = static_cast<T*>(o2.p);

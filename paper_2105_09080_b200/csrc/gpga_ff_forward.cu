@@ -59,7 +59,80 @@ cudaError_t forward(const FeedForwardParams& p, cudaStream_t stream)
     g.b[0] = q.down;
     g.n = p.d;
     g.k = p.f;
-    return store_product<T, P>(g, p.y, p.nodes * p.rows, nullptr, false, stream);
+    return store_product<T, P>(g, p.y, p.nodes * p.rows, nullptr, false, Exponents(), stream);
+}
+
+// fp32 as pairs of fp16.
+struct PairsPlan {
+    PackPlan in, between;
+    Operand x, gate, up, down, h;
+    float* hf;
+    int64_t ldh;
+    uint32_t *parts, *peaks;     // of x, gate, up, down (kPeakParts each); of h and nothing
+    int32_t* exponents;          // of x, gate and up, up again, down, h
+};
+
+PairsPlan plan_pairs(const FeedForwardParams& p)
+{
+    PairsPlan q;
+    q.in.base = q.between.base = p.scratch;
+    q.in.pieces = q.between.pieces = 2;
+    ScratchPlan& s = q.in.scratch;
+    q.parts = reinterpret_cast<uint32_t*>(p.scratch + s.take(4 * kPeakParts * 4));
+    q.peaks = reinterpret_cast<uint32_t*>(p.scratch + s.take(8));
+    q.exponents = reinterpret_cast<int32_t*>(p.scratch + s.take(5 * 4));
+    q.x = q.in.operand(p.x.p, p.x.ld, p.rows * p.x.ld, p.rows, p.d, p.nodes, true, false, 2);
+    q.in.scaled(q.parts, kPeakParts, q.exponents);
+    q.gate = q.in.operand(p.gate.p, p.gate.ld, p.gate.node, p.f, p.d, p.nodes, true, false, 2);
+    q.in.scaled(q.parts + kPeakParts, 2 * kPeakParts, q.exponents + 1);   // one power for both
+    q.up = q.in.operand(p.up.p, p.up.ld, p.up.node, p.f, p.d, p.nodes, true, false, 2);
+    q.in.scaled(q.parts + kPeakParts, 2 * kPeakParts, q.exponents + 2);
+    q.down = q.in.operand(p.down.p, p.down.ld, p.down.node, p.d, p.f, p.nodes, true, false, 2);
+    q.in.scaled(q.parts + 3 * kPeakParts, kPeakParts, q.exponents + 3);
+    q.ldh = (p.f + 7) / 8 * 8;
+    q.hf = reinterpret_cast<float*>(p.scratch + s.take(p.nodes * p.rows * q.ldh * 4));
+    q.between.scratch = s;
+    q.h = q.between.operand(q.hf, q.ldh, p.rows * q.ldh, p.rows, p.f, p.nodes, true, false, 2);
+    q.between.scaled(q.peaks, 1, q.exponents + 4);
+    return q;
+}
+
+cudaError_t forward_pairs(const FeedForwardParams& p, cudaStream_t stream)
+{
+    const PairsPlan q = plan_pairs(p);
+    cudaError_t e = q.in.launch_peaks(q.parts, q.peaks, stream);
+    if (e == cudaSuccess) e = q.in.launch<__half>(stream);
+    if (e != cudaSuccess) return e;
+    GemmPlan g;
+    g.half = true;
+    g.batch = g.bmod = p.nodes;
+    g.after = true;
+    g.a[0] = q.x;
+    g.b[0] = q.gate;
+    g.b[1] = q.up;
+    g.m = p.rows;
+    g.n = p.f;
+    g.k = p.d;
+    GateUp<float, true> up;
+    up.g = static_cast<float*>(p.g.p);
+    up.u = static_cast<float*>(p.u.p);
+    up.ldg = p.g.ld;
+    up.ldu = p.u.ld;
+    up.h = {q.hf, q.ldh, p.rows * q.ldh};
+    up.exponents = {q.exponents, q.exponents + 1};
+    up.peaks = q.peaks;
+    up.m = (int32_t)p.rows;
+    up.kind = p.activation;
+    up.keeps = p.g.p != nullptr;
+    up.vec = !up.keeps || (rows_on_16(p.g.p, p.g.ld, p.nodes * p.rows, 0, 1, 4) && rows_on_16(p.u.p, p.u.ld, p.nodes * p.rows, 0, 1, 4));
+    e = launch_gemm<2>(g, up, stream);
+    if (e == cudaSuccess) e = q.between.launch<__half>(stream);
+    if (e != cudaSuccess) return e;
+    g.a[0] = q.h;
+    g.b[0] = q.down;
+    g.n = p.d;
+    g.k = p.f;
+    return store_product<float, 2>(g, p.y, p.nodes * p.rows, nullptr, false, {q.exponents + 4, q.exponents + 3}, stream);
 }
 
 }  // namespace
@@ -72,12 +145,13 @@ unsigned int* ff_forward_gave_up()
 
 int64_t ff_forward_scratch_bytes(const FeedForwardParams& p) 
 {
-    return !p.rows ? 0 : ff_few(p) ? ff_few_scratch_bytes(p) : plan_forward(p).pack.scratch.bytes;
+    return !p.rows ? 0 : ff_few(p) ? ff_few_scratch_bytes(p) : ff_pairs(p, false) ? plan_pairs(p).between.scratch.bytes : plan_forward(p).pack.scratch.bytes;
 }
 
 cudaError_t launch_ff_forward(const FeedForwardParams& p, cudaStream_t stream)
 {
     if (ff_few(p)) return launch_ff_few(p, stream);
+    if (ff_pairs(p, false)) return forward_pairs(p, stream);
     if (p.dtype == 0) return forward<float>(p, stream);
     if (p.dtype == 1) return forward<__nv_bfloat16>(p, stream);
     return forward<__half>(p, stream);

@@ -306,11 +306,21 @@ constexpr int kFewRegisters = 64, kManyRegisters = 208;
 //   eight(v, ahead, batch, row, col, left): eight columns.  wide() false: one(v, batch, row, col) is called instead;
 //   kDual: eight(v, w, batch, row, col, left), v of the first array's columns, w of the second's.  wide() false: keep(which, v,
 //   batch, row, col) is called first for every single value.
+//   kPeaks: largest values that the block notes (block_peaks) and adds to those at `peaks` in the end.
 //   kTail: microseconds of 128 x 256 columns, for the choice of the variant.
 //   kMirror: eight() leaves in v what it has stored; put(v, batch, row, col) stores it again at its mirror place.
 // The loops over eight columns are kept rolled: a warp goes through an epilogue once per tile, and unrolled it waits for
 // instructions (gradient epilogue of 2048 x 768 x 2048, fp32: 147 us unrolled, 60 us rolled).
 struct NothingAhead {};
+
+// The kernel's shared memory from the first 1024-byte boundary on.
+__device__ __forceinline__ unsigned char* gemm_shared()
+{
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    return smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+}
+// The block's largest values so far (two arrays); the kernel adds them to the call's when it ends.
+__device__ __forceinline__ uint32_t* block_peaks() { return reinterpret_cast<uint32_t*>(gemm_shared() + 176); }
 
 // A SPLIT tile's sums: eight columns after eight columns (the block that finishes them has them one after the other), 128 rows of
 // 32 bytes and 64 bytes between; the halves of a row change places every four rows, for the banks.
@@ -344,11 +354,9 @@ template <class V, class Epi>
 __global__ void __launch_bounds__(V::threads, 1)
     gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmParams p, const __grid_constant__ Epi epi)
 {
-    extern __shared__ __align__(1024) unsigned char smem_raw[];
-    const uint32_t raw = smem_u32(smem_raw);
-    unsigned char* const smem = smem_raw + ((1024 - (raw & 1023)) & 1023);
+    unsigned char* const smem = gemm_shared();
     const uint32_t base = smem_u32(smem);
-    // head: full[8], empty[8], acc_full[2], acc_empty[2], tensor memory address, stop flag, SPLIT's copies
+    // head: full[8], empty[8], acc_full[2], acc_empty[2], tensor memory address, stop flag, SPLIT's copies, block_peaks
     const uint32_t full = base, empty = base + 64, acc_full = base + 128, acc_empty = base + 144;
     uint32_t* const tmem_at = reinterpret_cast<uint32_t*>(smem + 160);
     volatile uint32_t* const stop = reinterpret_cast<volatile uint32_t*>(smem + 164);
@@ -384,6 +392,7 @@ __global__ void __launch_bounds__(V::threads, 1)
             mbar_init(reinterpret_cast<uint64_t*>(smem + 144 + 8 * i), V::warps * CG);
         }
         *stop = 0;
+        for (int i = 0; i < Epi::kPeaks; ++i) block_peaks()[i] = 0;
         if constexpr (SPLIT) {
             mbar_init(copies, 1);
             if (p.splits > 1) mbar_arrive_expect_tx(copies, (p.splits - 1) * (16 / p.splits) * kSplitChunk);
@@ -767,6 +776,8 @@ __global__ void __launch_bounds__(V::threads, 1)
     // Everybody is done, or has given up; copies in flight must land before the block goes.
     tmem_fence_before();
     __syncthreads();
+    if constexpr (Epi::kPeaks > 0)
+        if (threadIdx.x < Epi::kPeaks) atomicMax(epi.peaks + threadIdx.x, block_peaks()[threadIdx.x]);
     if (*stop && threadIdx.x == 0)
         for (uint32_t i = loaded > stages ? loaded - stages : 0; i < loaded; ++i)
             for (uint32_t tries = 0; tries < 4096 && !try_wait(full + 8 * (i % stages), (i / stages) & 1); ++tries) {
@@ -895,7 +906,8 @@ inline double gemm_microseconds(int64_t m, int64_t n, int64_t kblocks, int64_t b
     if (!splits) return (double)((tiles + sms / 2 - 1) / (sms / 2)) * (0.27 * products * kblocks + 0.3) + (products > 1 ? 5.0 : 3.0) + tail;
     const int64_t room = splits == 8 ? sms * 3 / 4 : splits == 4 ? sms * 9 / 10 : sms;   // SMs of whole clusters
     const int64_t waves = (tiles * splits + room - 1) / room;
-    return waves * (0.25 * products * ((kblocks + splits - 1) / splits) + 2.6 + (1.4 + 0.5 * tail) / splits + (splits > 1 ? 0.5 : 0.0));
+    // a wave after the first waits for the blocks before it to leave
+    return waves * (0.25 * products * ((kblocks + splits - 1) / splits) + 2.6 + (1.4 + 0.5 * tail) / splits + (splits > 1 ? 0.5 : 0.0)) + (1.0 + 1.25 * splits) * (waves - 1);
 }
 
 // The variant that should take the least time.

@@ -116,6 +116,7 @@ template <int P>
 struct KeepPieces {
     static constexpr bool kDual = false, kMirror = true;
     static constexpr double kTail = 1.0;
+    static constexpr int kPeaks = 0;
     static constexpr int kWarps = 8;
     struct Ahead {
         Raw<__half> r[P];
@@ -162,6 +163,7 @@ template <class T>
 struct LastStep {
     static constexpr bool kDual = false, kMirror = false;
     static constexpr double kTail = 1.0;
+    static constexpr int kPeaks = 0;
     static constexpr int kWarps = 8;
     using Ahead = Raw<T>;
     T* out;

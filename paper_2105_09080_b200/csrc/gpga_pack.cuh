@@ -15,6 +15,11 @@ struct PackJob {
     int pieces;
     void* dst;
     int64_t dst_piece;
+    // Where the pieces are of the source times a power of two: bits of the largest values of its parts, and where the power's
+    // exponent goes, negated.
+    const uint32_t* peaks;
+    int peak_count;
+    int32_t* exponent;
 };
 constexpr int kPackJobs = 5;
 struct PackJobs {
@@ -23,29 +28,86 @@ struct PackJobs {
     int64_t chunks;
 };
 
+__device__ __forceinline__ void pack_load(const PackJob& j, int64_t c, float (&v)[8])
+{
+    const int64_t row = c / j.chunks, b = row / j.rows, r = row - b * j.rows;
+    const int col = (int)(c - row * j.chunks) * 8;
+    Raw<float> x;
+    x.load(static_cast<const float*>(j.src) + b * j.batch + r * j.ld + col, (int)min((int64_t)8, j.cols - col), j.vec);
+    x.values(v);
+}
+
+// Largest finite value of an array, as bits.
+__device__ __forceinline__ uint32_t finite_bits(float v)
+{
+    const uint32_t b = __float_as_uint(v) & 0x7FFFFFFFu;
+    return b < 0x7F800000u ? b : 0;
+}
+constexpr int kPeakParts = 128;   // blocks per array
+
+// Block x of job y: its part of the array.  `cleared`: peaks that a product of the call will find.
+static __global__ void __launch_bounds__(256) peak_kernel(const __grid_constant__ PackJobs jobs, uint32_t* parts, uint32_t* cleared)
+{
+    const PackJob& j = jobs.job[blockIdx.y];
+    const int64_t count = j.batches * j.rows * j.chunks;
+    uint32_t peak = 0;
+#pragma unroll 4
+    for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < count; c += kPeakParts * 256) {
+        float v[8];
+        pack_load(j, c, v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) peak = max(peak, finite_bits(v[k]));
+    }
+    peak = __reduce_max_sync(~0u, peak);
+    __shared__ uint32_t warps[8];
+    if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = peak;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 8; ++i) peak = max(peak, warps[i]);
+        parts[blockIdx.y * kPeakParts + blockIdx.x] = peak;
+        if (blockIdx.x == 0 && blockIdx.y == 0) cleared[0] = cleared[1] = 0;
+    }
+}
+
 // A thread takes a chunk of eight columns: one pass over the source, bound by memory (fp32 to three pieces: 4 bytes read,
 // 6 written per value).
 template <class T16>
 __global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackJobs jobs)
 {
     grid_launch_dependents();
+    __shared__ float scale[kPackJobs];
+    if (jobs.job[0].peaks) {
+        const int i = threadIdx.x >> 5;
+        if (i < jobs.count) {
+            const PackJob& j = jobs.job[i];
+            uint32_t peak = 0;
+            for (int k = threadIdx.x & 31; k < j.peak_count; k += 32) peak = max(peak, j.peaks[k]);
+            peak = __reduce_max_sync(~0u, peak);
+            // the largest value to 2^14 .. 2^15; an array of zeros as it is
+            const int e = peak ? min(14 + 127 - (int)(peak >> 23), 120) : 0;
+            if ((threadIdx.x & 31) == 0) {
+                scale[i] = __int_as_float((e + 127) << 23);
+                if (blockIdx.x == 0) *j.exponent = -e;
+            }
+        }
+        __syncthreads();
+    }
     for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < jobs.chunks; at += (int64_t)gridDim.x * 256) {
         int i = 0;
         while (i + 1 < jobs.count && at >= jobs.job[i + 1].first) ++i;
         const PackJob& j = jobs.job[i];
-        const int64_t c = at - j.first, row = c / j.chunks;
-        const int col = (int)(c - row * j.chunks) * 8;
-        const int64_t b = row / j.rows, r = row - b * j.rows;
-        const int n = (int)min((int64_t)8, j.cols - col);
+        const int64_t c = at - j.first;
         float v[8];
-        const int64_t from = b * j.batch + r * j.ld + col;
         if (j.src_f32) {
-            Raw<float> x;
-            x.load(static_cast<const float*>(j.src) + from, n, j.vec);
-            x.values(v);
+            pack_load(j, c, v);
+            if (j.peaks)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] *= scale[i];
         } else {
+            const int64_t row = c / j.chunks, b = row / j.rows, r = row - b * j.rows;
+            const int col = (int)(c - row * j.chunks) * 8;
             Raw<T16> x;
-            x.load(static_cast<const T16*>(j.src) + from, n, j.vec);
+            x.load(static_cast<const T16*>(j.src) + b * j.batch + r * j.ld + col, (int)min((int64_t)8, j.cols - col), j.vec);
             x.values(v);
         }
         const Pieces<T16> dst{static_cast<T16*>(j.dst) + c * 8, j.dst_piece, 0, 0};
@@ -134,6 +196,19 @@ struct PackPlan {
         o.piece = batches * o.batch;
         o.base = base + scratch.take(pieces * o.piece * 2);
         return o;
+    }
+    // The last operand is packed times a power of two.
+    void scaled(const uint32_t* peaks, int count, int32_t* exponent)
+    {
+        PackJob& j = jobs.job[jobs.count - 1];
+        j.peaks = peaks;
+        j.peak_count = count;
+        j.exponent = exponent;
+    }
+    cudaError_t launch_peaks(uint32_t* parts, uint32_t* cleared, cudaStream_t stream) const
+    {
+        peak_kernel<<<dim3(kPeakParts, jobs.count), 256, 0, stream>>>(jobs, parts, cleared);
+        return cudaGetLastError();
     }
     template <class T16>
     cudaError_t launch(cudaStream_t stream) const

@@ -311,6 +311,73 @@ def test_a_bad_token_stays_alone(dtype, rows):
             assert not a[0, 4].isfinite().all()
 
 
+LARGE = [(1, 3000, 1030, 1100), (3, 1501, 700, 780)]      # fp32 as pairs of fp16 values
+
+
+@pytest.mark.parametrize("size", LARGE, ids=str)
+def test_large_fp32_products_of_whole_numbers(size):
+    """Powers of two before and after the products change nothing: still exact, off the alignment too, and added to."""
+    x, gate, up, down = whole_inputs(*size, F32, F32, seed=20)
+    dy = whole(x.shape, generator(21), F32)
+    want = whole_forward(x, gate, up, down)
+    got = pkg.feed_forward_forward(x, gate, up, down, activation="relu")
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert torch.equal(pkg.feed_forward_forward(x, gate, up, down, activation="relu", keep=False)[0], want[0])
+    ref = whole_backward(dy, x, got[1], got[2], gate, up, down)
+    grads = pkg.feed_forward_backward(dy, x, got[1], got[2], gate, up, down, activation="relu")
+    assert all(torch.equal(a, b.float()) for a, b in zip(grads, ref))
+    wide = [strided(v, 3, 1)[0] for v in (x, gate, up, down)]
+    outs = [strided(v, 3, 1) for v in want]
+    pkg.feed_forward_forward(*wide, activation="relu", out=outs[0][0], g=outs[1][0], u=outs[2][0])
+    assert all(torch.equal(view, v) and (~buf.isnan()).sum() == v.numel() for (view, buf), v in zip(outs, want))
+    new = [torch.ones_like(w) for w in (gate, up, down)]
+    pkg.feed_forward_backward(dy, wide[0], outs[1][0], outs[2][0], *wide[1:], activation="relu", dgate=new[0], dup=new[1], ddown=new[2], accumulate=True)
+    assert all(torch.equal(a, (1 + b).float()) for a, b in zip(new, ref[1:]))
+    assert all(torch.equal(a, b) for a, b in zip(pkg.feed_forward_backward(dy, x, got[1], got[2], gate, up, down, activation="relu"), grads))
+
+
+@pytest.mark.parametrize("spread", [0, 12])
+def test_large_fp32_products_against_64_bits(spread):
+    """Tokens whose sizes differ by 2^12: every element within the bound of its own row.  Two fp16 values hold 24 bits of what
+    is at least 2^-17 of an array's largest value, and 2^-40 of that below; the largest of some million normal numbers is
+    below 8, so a value 2^-12 times a normal one keeps 2^-24 beside 2^-37 absolute, which the bound's 40 steps of the row's own sums cover
+    where those are above 2^-14: with 1030 terms of 2^-12 they are."""
+    x, gate, up, down = normal_inputs(1, 3000, 1030, 1100, F32, F32, seed=22)
+    x = x * torch.exp2(-torch.arange(3000, device="cuda") % (spread + 1)).float()[None, :, None]
+    for kind in ("silu", "gelu"):
+        for got, (want, bound) in zip(pkg.feed_forward_forward(x, gate, up, down, activation=kind)[1:], block_bound(x, gate, up, down, kind)[1:]):
+            assert ((got.double() - want).abs() <= bound).all()
+    if spread == 0:
+        (want, bound), *_ = block_bound(x, gate, up, down, "silu")
+        assert ((pkg.feed_forward_forward(x, gate, up, down)[0].double() - want).abs() <= bound).all()
+
+
+def test_large_fp32_products_leave_bad_tokens_alone():
+    x, gate, up, down = normal_inputs(1, 3000, 1030, 1100, F32, F32, seed=23)
+    clean = pkg.feed_forward_forward(x, gate, up, down)
+    dclean = pkg.feed_forward_backward(x, x, clean[1], clean[2], gate, up, down)[0]
+    z = x.clone()
+    z[0, 4, 3], z[0, 2900, 1000] = float("inf"), float("nan")
+    got = pkg.feed_forward_forward(z, gate, up, down)
+    dx = pkg.feed_forward_backward(z, x, clean[1], clean[2], gate, up, down)[0]
+    others = [i for i in range(3000) if i not in (4, 2900)]
+    # the largest finite value may be another one than before, so the powers of two may differ, and with them the last bits
+    for a, b in zip((*got, dx), (*clean, dclean)):
+        assert (a[:, others] - b[:, others]).abs().max() <= 2.0 ** -18 * b.abs().max()
+        assert not a[0, 4].isfinite().all() and not a[0, 2900].isfinite().all()
+    zero = pkg.feed_forward_forward(x * 0, gate, up, down)
+    assert all((v == 0).all() for v in zero)
+
+
+@pytest.mark.parametrize("factor", [2.0 ** 60, 2.0 ** -60, 2.0 ** 100])
+def test_large_fp32_products_of_extreme_numbers(factor):
+    """Powers of two on inputs pass through g and u exactly, far from one too."""
+    x, gate, up, down = normal_inputs(1, 3000, 1030, 1100, F32, F32, seed=24)
+    _, g, u = pkg.feed_forward_forward(x, gate, up, down, activation="relu")
+    _, g2, u2 = pkg.feed_forward_forward(x * factor, gate, up, down, activation="relu")
+    assert torch.equal(g2, g * factor) and torch.equal(u2, u * factor)
+
+
 def test_no_tokens():
     gate, up, down = (torch.ones(s, device="cuda", dtype=BF16) for s in ((2, 12, 8), (2, 12, 8), (2, 8, 12)))
     x = torch.empty((2, 0, 8), device="cuda", dtype=BF16)
