@@ -850,14 +850,16 @@ cudaError_t launch_gemm_as(const GemmPlan& g, int splits, const Epi& epi, cudaSt
     p.idesc = mma_descriptor(128 * CG, bn, g.half, p.a_mn, p.b_mn);
     const int b_rows = p.b_mn ? 64 : Epi::kDual ? bn / 2 : bn / CG;
     for (int i = 0; i < 2; ++i) {
-        cudaError_t e = encode_map(maps.a[i], g.a[i < g.pairs ? i : 0], g.half, p.a_mn ? 64 : 128);
-        if (e == cudaSuccess) e = encode_map(maps.b[i], g.b[i < g.pairs || Epi::kDual ? i : 0], g.half, b_rows);
+        cudaError_t e = cudaSuccess;
+        if (i < g.pairs)
+            e = encode_map(maps.a[i], g.a[i], g.half, p.a_mn ? 64 : 128);
+        else
+            maps.a[i] = maps.a[0];
+        if (e == cudaSuccess && (i < g.pairs || Epi::kDual))
+            e = encode_map(maps.b[i], g.b[i], g.half, b_rows);
+        else
+            maps.b[i] = maps.b[0];
         if (e != cudaSuccess) return e;
-        if (g.pairs == 1 && !Epi::kDual) {
-            maps.a[1] = maps.a[0];
-            maps.b[1] = maps.b[0];
-            break;
-        }
     }
     const auto kernel = gemm_kernel<V, Epi>;
     static std::atomic<unsigned long long> limit_set{0};

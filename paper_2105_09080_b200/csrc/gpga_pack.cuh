@@ -46,13 +46,14 @@ __device__ __forceinline__ uint32_t finite_bits(float v)
 constexpr int kPeakParts = 128;   // blocks per array
 
 // Block x of job y: its part of the array.  `cleared`: peaks that a product of the call will find.
-static __global__ void __launch_bounds__(256) peak_kernel(const __grid_constant__ PackJobs jobs, uint32_t* parts, uint32_t* cleared)
+template <int PARTS>
+__global__ void __launch_bounds__(256) peak_kernel(const __grid_constant__ PackJobs jobs, uint32_t* parts, uint32_t* cleared)
 {
     const PackJob& j = jobs.job[blockIdx.y];
     const int64_t count = j.batches * j.rows * j.chunks;
     uint32_t peak = 0;
 #pragma unroll 4
-    for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < count; c += kPeakParts * 256) {
+    for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < count; c += PARTS * 256) {
         float v[8];
         pack_load(j, c, v);
 #pragma unroll
@@ -64,7 +65,7 @@ static __global__ void __launch_bounds__(256) peak_kernel(const __grid_constant_
     __syncthreads();
     if (threadIdx.x == 0) {
         for (int i = 1; i < 8; ++i) peak = max(peak, warps[i]);
-        parts[blockIdx.y * kPeakParts + blockIdx.x] = peak;
+        parts[blockIdx.y * PARTS + blockIdx.x] = peak;
         if (blockIdx.x == 0 && blockIdx.y == 0) cleared[0] = cleared[1] = 0;
     }
 }
@@ -207,7 +208,7 @@ struct PackPlan {
     }
     cudaError_t launch_peaks(uint32_t* parts, uint32_t* cleared, cudaStream_t stream) const
     {
-        peak_kernel<<<dim3(kPeakParts, jobs.count), 256, 0, stream>>>(jobs, parts, cleared);
+        peak_kernel<kPeakParts><<<dim3(kPeakParts, jobs.count), 256, 0, stream>>>(jobs, parts, cleared);
         return cudaGetLastError();
     }
     template <class T16>

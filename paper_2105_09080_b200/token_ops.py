@@ -359,23 +359,30 @@ def _matrix(t, what, dtypes, device, nodes=None, rows=None, cols=None):
     return n, r, c, ld, stride[0] if n > 1 else r * ld
 
 
-@functools.lru_cache(maxsize=None)
-def _scratch_entry(name):
-    fn, pack = getattr(lib(), name + "_scratch_bytes"), ARGS[name].pack
+_SCRATCH = struct.Struct("=Qq")
 
-    def need(pointers, *members):
-        try:
-            return fn(pack(*pointers, 0, 0, *members))
-        except struct.error as e:
-            _bad(f"argument out of range: {e}")
-    return need
+
+@functools.lru_cache(maxsize=None)
+def _scratch_entry(name, pointers):
+    """(C function that says how much scratch a call needs, packing of its struct, offset of scratch and its size in it)."""
+    return getattr(lib(), name + "_scratch_bytes"), ARGS[name].pack, 8 * pointers, getattr(lib(), name)
 
 
 def _run_with_scratch(name, device, like, scratch, pointers, members):
     """Calls an entry whose struct is pointers, scratch, scratch bytes, members."""
-    need = _scratch_entry(name)(pointers, *members)
-    scratch, scratch_p, scratch_bytes = _scratch(scratch, need, like, device)
-    _entry(name)(device, *pointers, scratch_p, scratch_bytes, *members)
+    need, pack, at, fn = _scratch_entry(name, len(pointers))
+    if device != _current_device():
+        _bad(f"tensors live on cuda:{device} but cuda:{_current_device()} is current")
+    try:
+        args = pack(*pointers, 0, 0, *members)
+    except struct.error as e:
+        _bad(f"argument out of range: {e}")
+    scratch, scratch_p, scratch_bytes = _scratch(scratch, need(args), like, device)
+    if scratch_p:
+        args = args[:at] + _SCRATCH.pack(scratch_p, scratch_bytes) + args[at + 16:]
+    st = fn(args, _raw_stream(device))
+    if st != GPGA_OK:
+        raise GpgaError(st, lib().gpga_last_error(None).decode())
 
 
 def _activation(name):
@@ -388,6 +395,14 @@ def _weights(x, gate, up, down):
     """Checks of a block's input and weights: (shape, type, its code, device, d, nodes, rows, f, weight type, strides)."""
     dtype = x.dtype
     wtype = gate.dtype
+    shape = gate.shape
+    if (len(shape) == 3 and up.shape == shape and down.shape == (shape[0], shape[2], shape[1]) and up.dtype is wtype and down.dtype is wtype
+            and gate.is_contiguous() and up.is_contiguous() and down.is_contiguous() and shape.numel() and (wtype is torch.float32 or wtype is dtype)
+            and gate.get_device() == up.get_device() == down.get_device() == x.get_device()):
+        nodes, f, d = shape       # the plain case, in a few comparisons
+        shape, dtype, code, device, dx, rows = _vectors(x, nodes)
+        if dx == d:
+            return shape, dtype, code, device, d, nodes, rows, f, _DTYPE[wtype], (d, f * d, d, f * d, f, f * d)
     if wtype is not torch.float32 and wtype is not dtype:
         _bad(f"weights must be float32 or of the activations' type, got {wtype} beside {dtype}")
     device = x.get_device()
