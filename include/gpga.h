@@ -628,7 +628,7 @@ int64_t gpga_layer_norm_scratch_bytes(int64_t nodes, int64_t rows, int64_t d);
  *    theirs): results are as good as fp32 arithmetic gives.  An infinity among them may give NaN in what it reaches.  16-bit
  *    operands are taken as they are, fp32 weights beside them as the sum of two values of their type (16 significant bits for
  *    bfloat16; for fp16 22, and 2^-25 at least).  Sums are fp32.  What passes from one product to the next (h, dg, du) has the
- *    activations' type.
+ *    activations' type (forward calls of up to eight tokens per node: 16 bits more).
  *  - Scratch: the _scratch_bytes function of an entry, given the entry's own argument struct (its scratch members are not
  *    looked at), says how much it needs; 0 also where the arguments are wrong.
  *  - Waits inside the kernels are bounded.  One that gives up (which takes seconds and does not happen in a sound run) ends

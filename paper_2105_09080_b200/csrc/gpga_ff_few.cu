@@ -26,6 +26,7 @@ struct FewParams {
     int64_t ldx, ld1, node1, ld2, node2;
     void *out, *g, *u;              // out: h or y
     int64_t ldo, ldg, ldu;
+    int64_t lo;                     // h: elements from its values to the rests of their rounding (0: not kept)
     int32_t tokens, rows, k, kind, vec_x, vec_w, after, blocks;   // rows: of the weights; blocks: of a cluster
 };
 
@@ -72,7 +73,10 @@ __device__ __forceinline__ void finish(const FewParams& p, int node, int token, 
         }
         float v[1] = {a};
         act_values<sizeof(T) == 2>(v, p.kind);
-        static_cast<H*>(p.out)[t * p.ldo + row] = from_f32<H>(v[0] * b);
+        const float h = v[0] * b;
+        H* const at = static_cast<H*>(p.out) + t * p.ldo + row;
+        *at = from_f32<H>(h);
+        if (sizeof(H) == 2 && p.lo) at[p.lo] = from_f32<H>(h - to_f32(*at));
     } else {
         static_cast<T*>(p.out)[t * p.ldo + row] = from_f32<T>(a);
     }
@@ -110,8 +114,8 @@ __device__ __forceinline__ float cluster_sum(const float* sums, int i, int count
     return s;
 }
 
-// NT tiles of eight tokens.
-template <class T, class W, int NT, bool GATE>
+// NT tiles of eight tokens; XP = 2: x is h with the rests of its rounding.
+template <class T, class W, int NT, bool GATE, int XP>
 __global__ void __launch_bounds__(kFewWarps * 32) few_tokens_kernel(const __grid_constant__ FewParams p)
 {
     constexpr int M = GATE ? 2 : 1, R = 16, N = 8 * NT;
@@ -147,7 +151,7 @@ __global__ void __launch_bounds__(kFewWarps * 32) few_tokens_kernel(const __grid
 #pragma unroll
     for (int n = 0; n < NT; ++n) xr[n] = x + min(8 * n + group, p.tokens - 1) * p.ldx + place;
     float acc[M][NT][4] = {};
-    const auto multiply = [&](const Raw<W>(&wv)[M][2], const Raw<T>(&xv)[NT]) {
+    const auto multiply = [&](const Raw<W>(&wv)[M][2], const Raw<T>(&xv)[XP][NT]) {
 #pragma unroll
         for (int m = 0; m < M; ++m) {
             constexpr int Q = sizeof(W) / 2;
@@ -157,12 +161,16 @@ __global__ void __launch_bounds__(kFewWarps * 32) few_tokens_kernel(const __grid
 #pragma unroll
             for (int q = Q - 1; q >= 0; --q)
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    const uint32_t a[4] = {lo[q][2 * s], hi[q][2 * s], lo[q][2 * s + 1], hi[q][2 * s + 1]};
+                for (int z = XP - 1; z >= 0; --z) {
+                    if (q + z > 1) continue;
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        const uint32_t b[2] = {xv[n].w[2 * s], xv[n].w[2 * s + 1]};
-                        mma16816<T>(acc[m][n], a, b);
+                    for (int s = 0; s < 2; ++s) {
+                        const uint32_t a[4] = {lo[q][2 * s], hi[q][2 * s], lo[q][2 * s + 1], hi[q][2 * s + 1]};
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            const uint32_t b[2] = {xv[z][n].w[2 * s], xv[z][n].w[2 * s + 1]};
+                            mma16816<T>(acc[m][n], a, b);
+                        }
                     }
                 }
         }
@@ -170,14 +178,16 @@ __global__ void __launch_bounds__(kFewWarps * 32) few_tokens_kernel(const __grid
 #pragma unroll 1
     for (int k = k0; k < k1; k += 32) {
         Raw<W> wv[M][2];
-        Raw<T> xv[NT];
+        Raw<T> xv[XP][NT];
         const int left = p.k - k - place;
 #pragma unroll
         for (int m = 0; m < M; ++m)
 #pragma unroll
             for (int h = 0; h < 2; ++h) wv[m][h].load(wr[m][h] + k, left, p.vec_w);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) xv[n].load(xr[n] + k, left, p.vec_x);
+        for (int z = 0; z < XP; ++z)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) xv[z][n].load(xr[n] + z * p.lo + k, left, p.vec_x);
         multiply(wv, xv);
     }
 #pragma unroll
@@ -203,7 +213,7 @@ constexpr int kStreamK = 64;
 template <class W> constexpr int kStreamStages = sizeof(W) == 4 ? 4 : 8;
 template <class W> constexpr int kStreamStage = 16 * kStreamK * (int)sizeof(W);   // bytes
 
-template <class T, class W, int NT, bool GATE>
+template <class T, class W, int NT, bool GATE, int XP>
 __global__ void __launch_bounds__(kFewWarps * 32) few_streamed_kernel(const __grid_constant__ FewParams p)
 {
     constexpr int N = 8 * NT, S = 16 + 4, stages = kStreamStages<W>, stage_bytes = kStreamStage<W>;
@@ -256,17 +266,19 @@ __global__ void __launch_bounds__(kFewWarps * 32) few_streamed_kernel(const __gr
 #pragma unroll 1
         for (int step = 0; step < mine; ++step) {
             const int k0 = (s0 + step) * kStreamK;
-            Raw<T> xv[2][NT];
+            Raw<T> xv[2][XP][NT];
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const int k = k0 + 32 * h, left = p.k - k - quad * 8;
-                    if (left >= 8)
-                        xv[h][n].load16(xr[n] + k);
-                    else
-                        xv[h][n].load(xr[n] + k, left, false);
-                }
+                for (int z = 0; z < XP; ++z)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const int k = k0 + 32 * h, left = p.k - k - quad * 8;
+                        if (left >= 8)
+                            xv[h][z][n].load16(xr[n] + z * p.lo + k);
+                        else
+                            xv[h][z][n].load(xr[n] + z * p.lo + k, left, false);
+                    }
             asm volatile("cp.async.wait_group %0;" ::"n"(stages - 2) : "memory");
             __syncwarp();
             ask();      // into the slot that the step before this one was read from
@@ -294,12 +306,16 @@ __global__ void __launch_bounds__(kFewWarps * 32) few_streamed_kernel(const __gr
 #pragma unroll
                 for (int q = Q - 1; q >= 0; --q)
 #pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        const uint32_t a[4] = {lo[q][2 * s], hi[q][2 * s], lo[q][2 * s + 1], hi[q][2 * s + 1]};
+                    for (int z = XP - 1; z >= 0; --z) {
+                        if (q + z > 1) continue;
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            const uint32_t b[2] = {xv[h][n].w[2 * s], xv[h][n].w[2 * s + 1]};
-                            mma16816<T>(acc[n], a, b);
+                        for (int s = 0; s < 2; ++s) {
+                            const uint32_t a[4] = {lo[q][2 * s], hi[q][2 * s], lo[q][2 * s + 1], hi[q][2 * s + 1]};
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) {
+                                const uint32_t b[2] = {xv[h][z][n].w[2 * s], xv[h][z][n].w[2 * s + 1]};
+                                mma16816<T>(acc[n], a, b);
+                            }
                         }
                     }
             }
@@ -327,11 +343,11 @@ __global__ void __launch_bounds__(kFewWarps * 32) few_streamed_kernel(const __gr
     asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
-template <class T, class W, int NT, bool GATE>
+template <class T, class W, int NT, bool GATE, int XP = 1>
 cudaError_t launch_streamed(FewParams p, int64_t nodes, cudaStream_t stream)
 {
     constexpr int bytes = kFewWarps * (kStreamStages<W> * kStreamStage<W> + 2 * 8 * NT * 20 * 4);
-    const auto kernel = few_streamed_kernel<T, W, NT, GATE>;
+    const auto kernel = few_streamed_kernel<T, W, NT, GATE, XP>;
     static std::atomic<unsigned long long> limit_set{0};
     const cudaError_t e = ensure_smem_limit(kernel, bytes, limit_set);
     if (e != cudaSuccess) return e;
@@ -453,10 +469,11 @@ cudaError_t launch_clusters(void (*kernel)(FewParams), FewParams p, int rows, in
 template <class T, class W, bool GATE>
 cudaError_t few16(const FewParams& p, int64_t nodes, cudaStream_t stream)
 {
+    constexpr int XP = GATE ? 1 : 2;   // up to eight tokens h comes with the rests of its rounding
     if (p.vec_w && p.vec_x)
-        return p.tokens <= 8 ? launch_streamed<T, W, 1, GATE>(p, nodes, stream) : p.tokens <= 16 ? launch_streamed<T, W, 2, GATE>(p, nodes, stream)
-                                                                                                : launch_streamed<T, W, 4, GATE>(p, nodes, stream);
-    const auto kernel = p.tokens <= 8 ? few_tokens_kernel<T, W, 1, GATE> : p.tokens <= 16 ? few_tokens_kernel<T, W, 2, GATE> : few_tokens_kernel<T, W, 4, GATE>;
+        return p.tokens <= 8 ? launch_streamed<T, W, 1, GATE, XP>(p, nodes, stream) : p.tokens <= 16 ? launch_streamed<T, W, 2, GATE>(p, nodes, stream)
+                                                                                                    : launch_streamed<T, W, 4, GATE>(p, nodes, stream);
+    const auto kernel = p.tokens <= 8 ? few_tokens_kernel<T, W, 1, GATE, XP> : p.tokens <= 16 ? few_tokens_kernel<T, W, 2, GATE, 1> : few_tokens_kernel<T, W, 4, GATE, 1>;
     return launch_clusters(kernel, p, 16, 32, nodes, stream);
 }
 
@@ -477,7 +494,9 @@ cudaError_t few(const FeedForwardParams& q, const FewParams& p, cudaStream_t str
 
 }  // namespace
 
-int64_t ff_few_scratch_bytes(const FeedForwardParams& p) { return p.nodes * p.rows * ((p.f + 7) / 8 * 8) * (p.dtype == 0 ? 4 : 2); }
+// h: fp32, or 16 bits, of up to eight tokens with the rests of its rounding (the second launch is bound by its weights, and y is
+// rounded once then).
+int64_t ff_few_scratch_bytes(const FeedForwardParams& p) { return p.nodes * p.rows * ((p.f + 7) / 8 * 8) * (p.dtype == 0 || p.rows <= 8 ? 4 : 2); }
 
 cudaError_t launch_ff_few(const FeedForwardParams& q, cudaStream_t stream)
 {
@@ -496,6 +515,7 @@ cudaError_t launch_ff_few(const FeedForwardParams& q, cudaStream_t stream)
     p.vec_w = rows_on_16(q.gate.p, q.gate.ld, q.f, q.gate.node, q.nodes, wsize) && rows_on_16(q.up.p, q.up.ld, q.f, q.up.node, q.nodes, wsize);
     p.out = q.scratch;
     p.ldo = ldh;
+    p.lo = q.dtype != 0 && q.rows <= 8 ? q.nodes * q.rows * ldh : 0;
     p.g = q.g.p;
     p.u = q.u.p;
     p.ldg = q.g.ld;

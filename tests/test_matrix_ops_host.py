@@ -124,7 +124,8 @@ def test_scratch_is_what_the_arguments_need(L):
     pieces = 3 * 2 * (n * 100 * (d + f) + 3 * n * f * d)     # all fp32: three pieces each
     assert pieces <= scratch(L, "gpga_feed_forward_forward", dtype=F32, weight_dtype=F32, **big) < pieces + 5 * 256
     few = n * 8 * f
-    assert scratch(L, "gpga_feed_forward_forward", rows=8) == few * 2
+    assert scratch(L, "gpga_feed_forward_forward", rows=8) == few * 4          # h and the rests of its rounding
+    assert scratch(L, "gpga_feed_forward_forward", rows=9) == n * 9 * f * 2
     assert scratch(L, "gpga_feed_forward_forward", rows=8, dtype=F32, weight_dtype=F32) == few * 4
     assert scratch(L, "gpga_feed_forward_forward", rows=0) == 0
     between = 3 * n * t * f * 2 + weights
