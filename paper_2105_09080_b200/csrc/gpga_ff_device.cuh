@@ -169,7 +169,7 @@ template <class T, bool PAIRS = false>
 struct GateGrad {
     static constexpr bool kDual = false, kMirror = false;
     static constexpr double kTail = 6.0;
-    static constexpr int kWarps = 16;
+    static constexpr int kWarps = PAIRS ? 8 : 16;
     using T16 = typename PiecesOf<T>::type;
     static constexpr int P = PiecesOf<T>::count;
     struct Ahead {

@@ -327,22 +327,13 @@ __device__ __forceinline__ uint32_t* block_peaks() { return reinterpret_cast<uin
 constexpr int kSplitChunk = 128 * 32 + 64;
 __device__ __forceinline__ uint32_t split_place(int chunk, int row, int half) { return chunk * kSplitChunk + row * 32 + ((half ^ (row >> 2 & 1)) << 4); }
 
-// v[k] for a k that is not known when compiling.
-__device__ __forceinline__ float pick(const float (&v)[8], int k)
-{
-    float x = v[0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) x = k == i ? v[i] : x;
-    return x;
-}
-
 // What a variant of the kernel has: tile columns (of a pair of blocks, where CG = 2), pieces, warps of the epilogue, stages.
 template <int CG_, int BN_, int P_, int WARPS_ = 8, bool SPLIT_ = false>
 struct Variant {
     static constexpr int CG = CG_, BN = BN_, P = P_, warps = WARPS_, threads = 128 + 32 * warps;
     static constexpr bool chunked = P > 1, split = SPLIT_;
     static constexpr int staging = split ? 16 * kSplitChunk : warps * kStagingWarp;   // split: the other blocks' sums
-    static_assert(!chunked || warps == 8, "the registers of a CHUNKED kernel are split for eight warps");
+    static constexpr bool split_registers = chunked && warps == 8;    // sixteen have few enough sums each
     static_assert(!split || (CG == 1 && BN == 128 && warps == 8), "a SPLIT tile is 128 x 128");
     static constexpr uint32_t a_bytes = 128 * kTileK * 2, b_bytes = BN / CG * kTileK * 2, stage_bytes = a_bytes + b_bytes;
     static constexpr uint32_t room = (kGemmSmem - 1024 - kGemmHead - staging) / stage_bytes;
@@ -412,7 +403,7 @@ __global__ void __launch_bounds__(V::threads, 1)
 
     uint32_t loaded = 0;   // stages filled by this block (warp 0)
     if (warp < 4) {
-        if constexpr (CHUNKED) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegisters));
+        if constexpr (V::split_registers) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegisters));
         if (warp == 0 && lane == 0) {
             constexpr int nb = BN / CG;
             const uint32_t lead = CG == 2 ? map_shared(full, 0) : full;
@@ -509,7 +500,7 @@ __global__ void __launch_bounds__(V::threads, 1)
         }
         __syncwarp();
     } else {
-        if constexpr (CHUNKED) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegisters));
+        if constexpr (V::split_registers) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegisters));
         const int quarter = warp & 3, part = (warp - 4) >> 2;   // lanes of tensor memory, columns
         float* const stage = staging + (warp - 4) * 32 * 32;
         const uint32_t release = CG == 2 ? map_shared(acc_empty, 0) : acc_empty;
@@ -604,7 +595,7 @@ __global__ void __launch_bounds__(V::threads, 1)
                 }
             };
             if constexpr (CHUNKED) {
-                constexpr int slabs = BN / 64;   // kDual: those of the first array, then those of the second
+                constexpr int slabs = BN / (V::warps / 4) / 32;   // kDual: those of the first array, then those of the second
                 float acc[slabs][32];
 #pragma unroll
                 for (int j = 0; j < slabs; ++j)
@@ -734,11 +725,12 @@ __global__ void __launch_bounds__(V::threads, 1)
                     total(chunk, row, v);
                     total(chunk + per, row, x);
                     if (!epi.wide())
-#pragma unroll 1
-                        for (int k = 0; k < min(left, 8); ++k) {
-                            epi.keep(0, pick(v, k), g.batch, r, col + k);
-                            epi.keep(1, pick(x, k), g.batch, r, col + k);
-                        }
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            if (k < left) {
+                                epi.keep(0, v[k], g.batch, r, col + k);
+                                epi.keep(1, x[k], g.batch, r, col + k);
+                            }
                     epi.eight(v, x, g.batch, r, col, left);
                 } else {
                     typename Epi::Ahead ahead;
@@ -747,8 +739,9 @@ __global__ void __launch_bounds__(V::threads, 1)
                     if (epi.wide()) {
                         epi.eight(v, ahead, g.batch, r, col, left);
                     } else {
-#pragma unroll 1
-                        for (int k = 0; k < min(left, 8); ++k) epi.one(pick(v, k), g.batch, r, col + k);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            if (k < left) epi.one(v[k], g.batch, r, col + k);
                     }
                     if constexpr (Epi::kMirror)
                         if (mirror) {   // this block's own sums of these columns are not needed again
@@ -865,7 +858,7 @@ cudaError_t launch_gemm_as(const GemmPlan& g, int splits, const Epi& epi, cudaSt
     static std::atomic<unsigned long long> limit_set{0};
     const cudaError_t e = ensure_smem_limit(kernel, kGemmSmem, limit_set);
     if (e != cudaSuccess) return e;
-    if (V::chunked) {
+    if (V::split_registers) {
         static const int registers = kernel_registers(kernel);
         if (registers * V::threads < 128 * (kFewRegisters + 2 * kManyRegisters)) return cudaErrorLaunchOutOfResources;
     }
@@ -925,7 +918,7 @@ cudaError_t launch_gemm(const GemmPlan& g, const Epi& epi, cudaStream_t stream)
         if (t < least) least = t, best = splits;
     }
     if (best) return launch_gemm_as<Variant<1, 128, P, 8, true>>(g, best, epi, stream);
-    return launch_gemm_as<Variant<2, 256, P, P == 1 ? Epi::kWarps : 8>>(g, 1, epi, stream);
+    return launch_gemm_as<Variant<2, 256, P, P <= 2 ? Epi::kWarps : 8>>(g, 1, epi, stream);
 }
 
 }  // namespace gpga
