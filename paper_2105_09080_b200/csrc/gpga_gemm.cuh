@@ -64,7 +64,8 @@ struct GemmParams {
     int32_t kblocks1, kblocks;    // steps of kTileK of a segment; of all
     int32_t pairs;                // operands that the segments go through, again for every piece of B (GemmPlan)
     int32_t bmod;                 // B's batch index is batch % bmod
-    int32_t tiles_m, tiles_n, per_batch, tiles;
+    int32_t tiles_m, tiles_n, per_batch;
+    int32_t tile0, tiles;         // tiles tile0 to tiles - 1 are this launch's
     int32_t symmetric;            // only tiles on and above the diagonal; the others are their mirror images
     int32_t splits;               // SPLIT: blocks of a cluster, which share a tile's sum
     uint32_t idesc;
@@ -360,7 +361,7 @@ __global__ void __launch_bounds__(V::threads, 1)
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0, part_of_k = SPLIT ? cluster_rank() : 0;
-    const int group = SPLIT ? p.splits : CG, first = blockIdx.x / group, step = gridDim.x / group;
+    const int group = SPLIT ? p.splits : CG, first = p.tile0 + blockIdx.x / group, step = gridDim.x / group;
     const int kb_first = SPLIT ? (int)((int64_t)p.kblocks * part_of_k / p.splits) : 0;
     const int kb_count = SPLIT ? (int)((int64_t)p.kblocks * (part_of_k + 1) / p.splits) - kb_first : p.kblocks;
     const WaitState w{stop};
@@ -817,8 +818,9 @@ int kernel_registers(Kernel kernel)
     return cudaFuncGetAttributes(&a, kernel) == cudaSuccess ? a.numRegs : 0;
 }
 
+// The tiles from tile0 up to, but not, tile1 (0: the end).
 template <class V, class Epi>
-cudaError_t launch_gemm_as(const GemmPlan& g, int splits, const Epi& epi, cudaStream_t stream)
+cudaError_t launch_gemm_as(const GemmPlan& g, int splits, int64_t tile0, int64_t tile1, const Epi& epi, cudaStream_t stream)
 {
     constexpr int CG = V::CG, bn = V::BN;
     GemmParams p;
@@ -835,9 +837,11 @@ cudaError_t launch_gemm_as(const GemmPlan& g, int splits, const Epi& epi, cudaSt
     p.symmetric = g.symmetric;
     p.per_batch = g.symmetric ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n;
     p.splits = splits;
-    const int64_t tiles = g.batch * p.per_batch;
-    if (tiles * splits >= (int64_t(1) << 31) - 65536) return cudaErrorInvalidValue;
-    p.tiles = (int32_t)tiles;
+    if (!tile1) tile1 = g.batch * p.per_batch;
+    const int64_t tiles = tile1 - tile0;
+    if (tile1 * splits >= (int64_t(1) << 31) - 65536) return cudaErrorInvalidValue;
+    p.tile0 = (int32_t)tile0;
+    p.tiles = (int32_t)tile1;
     p.a_mn = g.a[0].mn_major;
     p.b_mn = g.b[0].mn_major;
     p.idesc = mma_descriptor(128 * CG, bn, g.half, p.a_mn, p.b_mn);
@@ -888,16 +892,22 @@ cudaError_t launch_gemm_as(const GemmPlan& g, int splits, const Epi& epi, cudaSt
     return cudaLaunchKernelEx(&cfg, kernel, maps, p, epi);
 }
 
-// Microseconds that a product takes as 256 x 256 tiles on pairs of SMs (splits = 0), or as 128 x 128 tiles on clusters of
-// `splits` blocks: waves of tiles, k-blocks of a tile, and what a tile costs besides.  A k-block of a 256 x 256 tile
+// Tiles of `side` rows and columns.
+inline int64_t gemm_tiles(const GemmPlan& g, int64_t n, int side)
+{
+    const int64_t tm = (g.m + side - 1) / side, tn = (n + side - 1) / side;
+    return g.symmetric ? tm * (tm + 1) / 2 : tm * tn;
+}
+
+// Microseconds that 256 x 256 tiles take on pairs of SMs (splits = 0), or 128 x 128 tiles on clusters of `splits` blocks:
+// waves of tiles, k-blocks of a tile, and what a tile costs besides.  A k-block of a 256 x 256 tile
 // takes 0.27 us per product of pieces, one of a 128 x 128 tile on its one SM 0.25 us (a quarter of the work on half of the
 // SMs: each operand byte is used half as often); a 128 x 128 tile is a block's only one, so nothing hides its start and
-// end.  tail: the epilogue of a block's 128 x 256 part of the last tile.  Measured, all of a call with either: 512 x 512 fp32, two steps, 117 us and (4 blocks) 60 us; 8 x 1024 x 2816
-// bfloat16 255 us and (1 block) 456 us; gradient of 8000 tokens x 128 x 300, bf16, 145 us and (4 blocks) 84 us.
-inline double gemm_microseconds(int64_t m, int64_t n, int64_t kblocks, int64_t batch, int products, double tail, bool symmetric, int splits, int sms)
+// end.  tail: the epilogue of a block's 128 x 256 part of the last tile.  Measured, all of a call with either: 512 x 512 fp32,
+// two steps, 117 us and (4 blocks) 60 us; 8 x 1024 x 2816 bfloat16 255 us and (1 block) 456 us; gradient of 8000 tokens x
+// 128 x 300, bf16, 145 us and (4 blocks) 84 us.
+inline double gemm_microseconds(int64_t tiles, int64_t kblocks, int products, double tail, int splits, int sms)
 {
-    const int64_t side = splits ? 128 : 256, tm = (m + side - 1) / side, tn = (n + side - 1) / side;
-    const int64_t tiles = batch * (symmetric ? tm * (tm + 1) / 2 : tm * tn);
     if (!splits) return (double)((tiles + sms / 2 - 1) / (sms / 2)) * (0.27 * products * kblocks + 0.3) + (products > 1 ? 5.0 : 3.0) + tail;
     const int64_t room = splits == 8 ? sms * 3 / 4 : splits == 4 ? sms * 9 / 10 : sms;   // SMs of whole clusters
     const int64_t waves = (tiles * splits + room - 1) / room;
@@ -905,20 +915,53 @@ inline double gemm_microseconds(int64_t m, int64_t n, int64_t kblocks, int64_t b
     return waves * (0.25 * products * ((kblocks + splits - 1) / splits) + 2.6 + (1.4 + 0.5 * tail) / splits + (splits > 1 ? 0.5 : 0.0)) + (1.0 + 1.25 * splits) * (waves - 1);
 }
 
-// The variant that should take the least time.
+// The last place, at most `limit` 256 x 256 tiles from the start, where the order of those tiles and that of 128 x 128 tiles
+// can be cut alike: between batches, columns of a symmetric one, and groups of eight rows of tiles (sixteen) of another.
+inline void gemm_cut(const GemmPlan& g, int64_t n, int64_t limit, int64_t& large, int64_t& small)
+{
+    const int64_t per = gemm_tiles(g, n, 256), batch = limit / per, left = limit - batch * per;
+    large = batch * per;
+    small = batch * gemm_tiles(g, n, 128);
+    if (g.symmetric) {
+        int64_t j = 0;
+        while ((j + 1) * (j + 2) / 2 <= left) ++j;
+        large += j * (j + 1) / 2;
+        small += j * (2 * j + 1);
+    } else {
+        const int64_t tn = (n + 255) / 256, i = left / (8 * tn);
+        large += 8 * i * tn;
+        small += 16 * i * ((n + 127) / 128);
+    }
+}
+
+// The variant that should take the least time.  Where whole waves of large tiles leave a few over, those may go to clusters
+// of blocks in a second launch (3 us): X X^T of 8 x 1024 x 2816, fp32, has 80 tiles for 74 pairs of SMs.
 template <int P, class Epi>
 cudaError_t launch_gemm(const GemmPlan& g, const Epi& epi, cudaStream_t stream)
 {
-    const int products = P * (P + 1) / 2;
+    const int products = P * (P + 1) / 2, sms = sm_count(), pairs = sms / 2;
     const int64_t n = Epi::kDual ? 2 * g.n : g.n, kblocks = (g.k + kTileK - 1) / kTileK * g.pairs * (g.b[0].pieces - g.a[0].pieces + 1);
+    const int64_t tiles = g.batch * gemm_tiles(g, n, 256), tiles1 = g.batch * gemm_tiles(g, n, 128);
     int best = 0;
-    double least = gemm_microseconds(g.m, n, kblocks, g.batch, products, Epi::kTail, g.symmetric, 0, sm_count());
+    int64_t large = tiles, small = 0;   // large tiles before the cut, small ones
+    double least = gemm_microseconds(tiles, kblocks, products, Epi::kTail, 0, sms);
+    int64_t large_cut = 0, small_cut = 0;
+    if (tiles > pairs) gemm_cut(g, n, tiles / pairs * pairs, large_cut, small_cut);
+    const double before = large_cut ? gemm_microseconds(large_cut, kblocks, products, Epi::kTail, 0, sms) + 3.0 : 0;
     for (int splits = 1; splits <= 8 && splits <= kblocks; splits *= 2) {
-        const double t = gemm_microseconds(g.m, n, kblocks, g.batch, products, Epi::kTail, g.symmetric, splits, sm_count());
-        if (t < least) least = t, best = splits;
+        double t = gemm_microseconds(tiles1, kblocks, products, Epi::kTail, splits, sms);
+        if (t < least) least = t, best = splits, large = small = 0;
+        if (!large_cut || large_cut == tiles) continue;
+        t = before + gemm_microseconds(tiles1 - small_cut, kblocks, products, Epi::kTail, splits, sms);
+        if (t < least) least = t, best = splits, large = large_cut, small = small_cut;
     }
-    if (best) return launch_gemm_as<Variant<1, 128, P, 8, true>>(g, best, epi, stream);
-    return launch_gemm_as<Variant<2, 256, P, P <= 2 ? Epi::kWarps : 8>>(g, 1, epi, stream);
+    GemmPlan rest = g;
+    if (large) {
+        const cudaError_t e = launch_gemm_as<Variant<2, 256, P, P <= 2 ? Epi::kWarps : 8>>(g, 1, 0, large, epi, stream);
+        if (e != cudaSuccess || !best) return e;
+        rest.after = true;
+    }
+    return launch_gemm_as<Variant<1, 128, P, 8, true>>(rest, best, small, 0, epi, stream);
 }
 
 }  // namespace gpga
