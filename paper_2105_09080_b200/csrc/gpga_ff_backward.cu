@@ -102,8 +102,8 @@ cudaError_t backward(const FeedForwardParams& p, cudaStream_t stream)
 struct PairsPlan {
     PackPlan in, between;
     Operand x, dy, gate, up, down, h, dgu;
-    float *hf, *dguf;
-    int64_t ldh;
+    float *hf, *dguf, *sums;
+    int64_t ldh, bytes;
     uint32_t *parts, *peaks;     // of dy, down, x, gate, up (kPeakParts each); of h, of dg and du
     int32_t* exponents;          // of dy, down, x, gate and up, up again, h, dg and du
 };
@@ -135,6 +135,10 @@ PairsPlan plan_pairs(const FeedForwardParams& p)
     q.between.scaled(q.peaks, 1, q.exponents + 5);
     q.dgu = q.between.operand(q.dguf, q.ldh, p.rows * q.ldh, p.rows, p.f, 2 * p.nodes, true, true, 2);   // dg of all nodes, then du
     q.between.scaled(q.peaks + 1, 1, q.exponents + 6);
+    ScratchPlan all = q.between.scratch;
+    const int64_t parts = std::max({parts_bytes(p.d, p.f, p.rows, p.nodes, 1), parts_bytes(p.f, p.d, p.rows, 2 * p.nodes, 1), parts_bytes(p.rows, p.d, p.f, p.nodes, 2)});
+    q.sums = reinterpret_cast<float*>(p.scratch + all.take(parts));
+    q.bytes = all.bytes;
     return q;
 }
 
@@ -176,13 +180,13 @@ cudaError_t backward_pairs(const FeedForwardParams& p, cudaStream_t stream)
     g.m = p.d;
     g.n = p.f;
     g.k = p.rows;
-    if ((e = store_product<float, 2>(g, p.ddown, p.d, nullptr, p.accumulate, {q.exponents, q.exponents + 5}, stream)) != cudaSuccess) return e;
+    if ((e = store_product<float, 2>(g, p.ddown, p.d, nullptr, p.accumulate, {q.exponents, q.exponents + 5}, stream, q.sums)) != cudaSuccess) return e;
     g.a[0] = q.dgu;                     // dWg, dWu
     g.b[0] = q.x;
     g.m = p.f;
     g.n = p.d;
     g.batch = 2 * p.nodes;
-    if ((e = store_product<float, 2>(g, p.dgate, p.f, &p.dup, p.accumulate, {q.exponents + 6, q.exponents + 2}, stream)) != cudaSuccess) return e;
+    if ((e = store_product<float, 2>(g, p.dgate, p.f, &p.dup, p.accumulate, {q.exponents + 6, q.exponents + 2}, stream, q.sums)) != cudaSuccess) return e;
     Operand dg = q.dgu, du = q.dgu;
     dg.batches = du.batches = p.nodes;
     du.base = static_cast<const __half*>(du.base) + p.nodes * du.batch;
@@ -196,7 +200,7 @@ cudaError_t backward_pairs(const FeedForwardParams& p, cudaStream_t stream)
     g.m = p.rows;
     g.n = p.d;
     g.k = p.f;
-    return store_product<float, 2>(g, p.dx, p.nodes * p.rows, nullptr, false, {q.exponents + 6, q.exponents + 3}, stream);
+    return store_product<float, 2>(g, p.dx, p.nodes * p.rows, nullptr, false, {q.exponents + 6, q.exponents + 3}, stream, q.sums);
 }
 
 template <class T>
@@ -236,7 +240,7 @@ unsigned int* ff_backward_gave_up()
     return cudaGetSymbolAddress(&at, gave_up) == cudaSuccess ? static_cast<unsigned int*>(at) : nullptr;
 }
 
-int64_t ff_backward_scratch_bytes(const FeedForwardParams& p) { return !p.rows ? 0 : ff_pairs(p, true) ? plan_pairs(p).between.scratch.bytes : plan_backward(p).pack.scratch.bytes; }
+int64_t ff_backward_scratch_bytes(const FeedForwardParams& p) { return !p.rows ? 0 : ff_pairs(p, true) ? plan_pairs(p).bytes : plan_backward(p).pack.scratch.bytes; }
 
 cudaError_t launch_ff_backward(const FeedForwardParams& p, cudaStream_t stream)
 {

@@ -267,8 +267,53 @@ inline bool rows_on_16(const void* p, int64_t ld, int64_t rows, int64_t node, in
     return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (rows <= 1 || ld * size % 16 == 0) && (nodes <= 1 || node * size % 16 == 0);
 }
 
+// The sums of a product left in parts: [batch][part][m][ld], added in the order of k.  A thread takes eight columns.
+template <class T>
+__global__ void __launch_bounds__(256) sum_parts_kernel(const float* sums, int parts, int m, int n, int64_t ld, int64_t chunks, const __grid_constant__ StoreRows<T> out)
+{
+    grid_launch_dependents();
+    grid_dependency_wait();
+    const int per = (int)(ld / 8);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < chunks; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / per;
+        const int col = (int)(i - r * per) * 8, batch = (int)(r / m), row = (int)(r - (int64_t)batch * m);
+        Raw<T> old;
+        if (out.wide()) out.load(old, batch, row, col, n - col);
+        const float* from = sums + ((int64_t)batch * parts * m + row) * ld + col;
+        float v[8] = {};
+#pragma unroll 4
+        for (int q = 0; q < parts; ++q, from += m * ld) {
+            const float4 x = *reinterpret_cast<const float4*>(from), y = *reinterpret_cast<const float4*>(from + 4);
+            const float z[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] += z[k];
+        }
+        if (out.wide()) {
+            out.eight(v, old, batch, row, col, n - col);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (col + k < n) out.one(v[k], batch, row, col + k);
+        }
+    }
+}
+
+// Bytes of the parts of a product of pairs, if store_product leaves its sums in parts.
+inline int64_t parts_bytes(int64_t m, int64_t n, int64_t k, int64_t batch, int pairs)
+{
+    GemmPlan g;
+    g.m = m;
+    g.n = n;
+    g.k = k;
+    g.batch = batch;
+    g.pairs = pairs;
+    const int parts = gemm_parts(g, 3, StoreRows<float>::kTail);
+    return parts > 1 ? parts * batch * m * ((n + 7) / 8 * 8) * 4 : 0;
+}
+
+// A product stored at its place.  sums: room for parts_bytes(), where the sums may be left in parts.
 template <class T, int P>
-cudaError_t store_product(const GemmPlan& g, const Matrix& out, int64_t rows, const Matrix* second, bool accumulate, const Exponents& exponents, cudaStream_t stream)
+cudaError_t store_product(const GemmPlan& g, const Matrix& out, int64_t rows, const Matrix* second, bool accumulate, const Exponents& exponents, cudaStream_t stream, float* sums = nullptr)
 {
     StoreRows<T> e;
     e.exponents = exponents;
@@ -282,6 +327,24 @@ cudaError_t store_product(const GemmPlan& g, const Matrix& out, int64_t rows, co
     e.split = (int32_t)(second ? g.batch / 2 : g.batch);
     e.accumulate = accumulate;
     e.vec = rows_on_16(out.p, out.ld, rows, out.node, g.batch, sizeof(T)) && rows_on_16(o2.p, o2.ld, rows, o2.node, g.batch, sizeof(T));
+    if constexpr (P == 2 && std::is_same<T, float>::value) {
+        const int parts = sums ? gemm_parts(g, P * (P + 1) / 2, StoreRows<float>::kTail) : 1;
+        if (parts > 1) {
+            StoreRows<float> to;
+            const int64_t ld = (g.n + 7) / 8 * 8;
+            to.exponents = Exponents();
+            to.out[0] = to.out[1] = sums;
+            to.ld[0] = to.ld[1] = ld;
+            to.node[0] = to.node[1] = g.m * ld;
+            to.split = INT32_MAX;
+            to.accumulate = 0;
+            to.vec = 1;
+            const cudaError_t r = launch_gemm_as<Variant<2, 256, P, 8, false, true>>(g, parts, 0, 0, to, stream);
+            if (r != cudaSuccess) return r;
+            const int64_t chunks = g.batch * g.m * (ld / 8);
+            return launch_after_trigger(sum_parts_kernel<T>, dim3((unsigned)std::min<int64_t>((chunks + 255) / 256, (int64_t)sm_count() * 8)), dim3(256), 0, stream, true, sums, parts, (int)g.m, (int)g.n, ld, chunks, e);
+        }
+    }
     return launch_gemm<P>(g, e, stream);
 }
 

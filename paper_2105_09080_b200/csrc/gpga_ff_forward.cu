@@ -66,8 +66,8 @@ cudaError_t forward(const FeedForwardParams& p, cudaStream_t stream)
 struct PairsPlan {
     PackPlan in, between;
     Operand x, gate, up, down, h;
-    float* hf;
-    int64_t ldh;
+    float *hf, *sums;
+    int64_t ldh, bytes;
     uint32_t *parts, *peaks;     // of x, gate, up, down (kPeakParts each); of h and nothing
     int32_t* exponents;          // of x, gate and up, up again, down, h
 };
@@ -94,6 +94,9 @@ PairsPlan plan_pairs(const FeedForwardParams& p)
     q.between.scratch = s;
     q.h = q.between.operand(q.hf, q.ldh, p.rows * q.ldh, p.rows, p.f, p.nodes, true, false, 2);
     q.between.scaled(q.peaks, 1, q.exponents + 4);
+    ScratchPlan all = q.between.scratch;
+    q.sums = reinterpret_cast<float*>(p.scratch + all.take(parts_bytes(p.rows, p.d, p.f, p.nodes, 1)));
+    q.bytes = all.bytes;
     return q;
 }
 
@@ -132,7 +135,7 @@ cudaError_t forward_pairs(const FeedForwardParams& p, cudaStream_t stream)
     g.b[0] = q.down;
     g.n = p.d;
     g.k = p.f;
-    return store_product<float, 2>(g, p.y, p.nodes * p.rows, nullptr, false, {q.exponents + 4, q.exponents + 3}, stream);
+    return store_product<float, 2>(g, p.y, p.nodes * p.rows, nullptr, false, {q.exponents + 4, q.exponents + 3}, stream, q.sums);
 }
 
 }  // namespace
@@ -145,7 +148,7 @@ unsigned int* ff_forward_gave_up()
 
 int64_t ff_forward_scratch_bytes(const FeedForwardParams& p) 
 {
-    return !p.rows ? 0 : ff_few(p) ? ff_few_scratch_bytes(p) : ff_pairs(p, false) ? plan_pairs(p).between.scratch.bytes : plan_forward(p).pack.scratch.bytes;
+    return !p.rows ? 0 : ff_few(p) ? ff_few_scratch_bytes(p) : ff_pairs(p, false) ? plan_pairs(p).bytes : plan_forward(p).pack.scratch.bytes;
 }
 
 cudaError_t launch_ff_forward(const FeedForwardParams& p, cudaStream_t stream)

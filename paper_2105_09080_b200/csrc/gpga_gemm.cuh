@@ -67,7 +67,7 @@ struct GemmParams {
     int32_t tiles_m, tiles_n, per_batch;
     int32_t tile0, tiles;         // tiles tile0 to tiles - 1 are this launch's
     int32_t symmetric;            // only tiles on and above the diagonal; the others are their mirror images
-    int32_t splits;               // SPLIT: blocks of a cluster, which share a tile's sum
+    int32_t splits;               // SPLIT: blocks of a cluster, which share a tile's sum; PARTS: parts that its sum is left in
     uint32_t idesc;
     int32_t a_mn, b_mn;
 };
@@ -329,10 +329,11 @@ constexpr int kSplitChunk = 128 * 32 + 64;
 __device__ __forceinline__ uint32_t split_place(int chunk, int row, int half) { return chunk * kSplitChunk + row * 32 + ((half ^ (row >> 2 & 1)) << 4); }
 
 // What a variant of the kernel has: tile columns (of a pair of blocks, where CG = 2), pieces, warps of the epilogue, stages.
-template <int CG_, int BN_, int P_, int WARPS_ = 8, bool SPLIT_ = false>
+// PARTS: batch b of the epilogue is part b % splits of the sums of batch b / splits.
+template <int CG_, int BN_, int P_, int WARPS_ = 8, bool SPLIT_ = false, bool PARTS_ = false>
 struct Variant {
     static constexpr int CG = CG_, BN = BN_, P = P_, warps = WARPS_, threads = 128 + 32 * warps;
-    static constexpr bool chunked = P > 1, split = SPLIT_;
+    static constexpr bool chunked = P > 1, split = SPLIT_, parts = PARTS_;
     static constexpr int staging = split ? 16 * kSplitChunk : warps * kStagingWarp;   // split: the other blocks' sums
     static constexpr bool split_registers = chunked && warps == 8;    // sixteen have few enough sums each
     static_assert(!split || (CG == 1 && BN == 128 && warps == 8), "a SPLIT tile is 128 x 128");
@@ -362,8 +363,13 @@ __global__ void __launch_bounds__(V::threads, 1)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0, part_of_k = SPLIT ? cluster_rank() : 0;
     const int group = SPLIT ? p.splits : CG, first = p.tile0 + blockIdx.x / group, step = gridDim.x / group;
-    const int kb_first = SPLIT ? (int)((int64_t)p.kblocks * part_of_k / p.splits) : 0;
-    const int kb_count = SPLIT ? (int)((int64_t)p.kblocks * (part_of_k + 1) / p.splits) - kb_first : p.kblocks;
+    const auto k_start = [&](int part) { return (int)((int64_t)p.kblocks * part / p.splits); };
+    int kb_first = SPLIT ? k_start(part_of_k) : 0, kb_count = SPLIT ? k_start(part_of_k + 1) - kb_first : p.kblocks;
+    const auto take_part = [&](int batch) {
+        const int part = batch % p.splits;
+        kb_first = k_start(part);
+        kb_count = k_start(part + 1) - kb_first;
+    };
     const WaitState w{stop};
     // SPLIT: this block's sums, in the order of the blocks that finish them; the place there of the tile's c-th eight columns.
     unsigned char* const sums_at = smem + kGemmHead + V::staging;
@@ -412,7 +418,8 @@ __global__ void __launch_bounds__(V::threads, 1)
             Ring<stages> ring;
             bool ok = true;
             for (int t = first; t < p.tiles && ok; t += step) {
-                const GemmTile g = gemm_tile(p, t, 128 * CG, BN);
+                GemmTile g = gemm_tile(p, t, 128 * CG, BN);
+                if constexpr (V::parts) take_part(g.batch), g.batch /= p.splits;
                 const int m0 = g.m0 + (int)rank * 128, bb = g.batch % p.bmod;
                 const int n0 = Epi::kDual ? g.n0 / 2 : g.n0 + (int)rank * nb;   // kDual: BN / 2 columns of each array
                 const int segment = kb_first / p.kblocks1;
@@ -458,6 +465,7 @@ __global__ void __launch_bounds__(V::threads, 1)
             uint32_t sums = 0;   // accumulators filled
             bool ok = true;
             for (int t = first; t < p.tiles && ok; t += step) {
+                if constexpr (V::parts) take_part(t / p.per_batch);
                 const int chunk = CHUNKED ? V::chunk : kb_count;
                 for (int k0 = 0; k0 < kb_count && ok; k0 += chunk, ++sums) {
                     const uint32_t buf = sums & 1;
@@ -512,6 +520,7 @@ __global__ void __launch_bounds__(V::threads, 1)
         const int lane_row = lane >> 2, lane_col = (lane & 3) * 8;
         for (int t = first; t < p.tiles && ok; t += step) {
             const GemmTile g = gemm_tile(p, t, 128 * CG, BN);
+            if constexpr (V::parts) take_part(g.batch);
             const int row0 = g.m0 + (int)rank * 128 + quarter * 32, from = (Epi::kDual ? g.n0 / 2 : g.n0) + part * width;
             const int rows = p.m - row0;   // that are there
             const bool mirror = p.symmetric && g.m0 != g.n0;
@@ -837,7 +846,7 @@ cudaError_t launch_gemm_as(const GemmPlan& g, int splits, int64_t tile0, int64_t
     p.symmetric = g.symmetric;
     p.per_batch = g.symmetric ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n;
     p.splits = splits;
-    if (!tile1) tile1 = g.batch * p.per_batch;
+    if (!tile1) tile1 = g.batch * p.per_batch * (V::parts ? splits : 1);
     const int64_t tiles = tile1 - tile0;
     if (tile1 * splits >= (int64_t(1) << 31) - 65536) return cudaErrorInvalidValue;
     p.tile0 = (int32_t)tile0;
@@ -934,34 +943,59 @@ inline void gemm_cut(const GemmPlan& g, int64_t n, int64_t limit, int64_t& large
     }
 }
 
-// The variant that should take the least time.  Where whole waves of large tiles leave a few over, those may go to clusters
-// of blocks in a second launch (3 us): X X^T of 8 x 1024 x 2816, fp32, has 80 tiles for 74 pairs of SMs.
+// The variant that should take the least time, of large tiles before the cut and clusters of `splits` blocks (0: none) after it.
+struct GemmChoice {
+    double microseconds;
+    int64_t large, small;   // large tiles before the cut, small ones
+    int splits;
+};
+inline GemmChoice choose_gemm(const GemmPlan& g, int64_t n, int64_t kblocks, int products, double tail)
+{
+    const int sms = sm_count(), pairs = sms / 2;
+    const int64_t large = g.batch * gemm_tiles(g, n, 256), small = g.batch * gemm_tiles(g, n, 128);
+    GemmChoice c{gemm_microseconds(large, kblocks, products, tail, 0, sms), large, small, 0};
+    int64_t large_cut = 0, small_cut = 0;
+    if (large > pairs) gemm_cut(g, n, large / pairs * pairs, large_cut, small_cut);
+    const double before = large_cut ? gemm_microseconds(large_cut, kblocks, products, tail, 0, sms) + 3.0 : 0;
+    for (int splits = 1; splits <= 8 && splits <= kblocks; splits *= 2) {
+        double t = gemm_microseconds(small, kblocks, products, tail, splits, sms);
+        if (t < c.microseconds) c = {t, 0, 0, splits};
+        if (!large_cut || large_cut == large) continue;
+        t = before + gemm_microseconds(small - small_cut, kblocks, products, tail, splits, sms);
+        if (t < c.microseconds) c = {t, large_cut, small_cut, splits};
+    }
+    return c;
+}
+inline int64_t gemm_kblocks(const GemmPlan& g) { return (g.k + kTileK - 1) / kTileK * g.pairs * (g.b[0].pieces - g.a[0].pieces + 1); }
+
+// Where whole waves of large tiles leave a few over, those may go to clusters of blocks in a second launch (3 us): X X^T of
+// 8 x 1024 x 2816, fp32, has 80 tiles for 74 pairs of SMs (89 us instead of 107 us).
 template <int P, class Epi>
 cudaError_t launch_gemm(const GemmPlan& g, const Epi& epi, cudaStream_t stream)
 {
-    const int products = P * (P + 1) / 2, sms = sm_count(), pairs = sms / 2;
-    const int64_t n = Epi::kDual ? 2 * g.n : g.n, kblocks = (g.k + kTileK - 1) / kTileK * g.pairs * (g.b[0].pieces - g.a[0].pieces + 1);
-    const int64_t tiles = g.batch * gemm_tiles(g, n, 256), tiles1 = g.batch * gemm_tiles(g, n, 128);
-    int best = 0;
-    int64_t large = tiles, small = 0;   // large tiles before the cut, small ones
-    double least = gemm_microseconds(tiles, kblocks, products, Epi::kTail, 0, sms);
-    int64_t large_cut = 0, small_cut = 0;
-    if (tiles > pairs) gemm_cut(g, n, tiles / pairs * pairs, large_cut, small_cut);
-    const double before = large_cut ? gemm_microseconds(large_cut, kblocks, products, Epi::kTail, 0, sms) + 3.0 : 0;
-    for (int splits = 1; splits <= 8 && splits <= kblocks; splits *= 2) {
-        double t = gemm_microseconds(tiles1, kblocks, products, Epi::kTail, splits, sms);
-        if (t < least) least = t, best = splits, large = small = 0;
-        if (!large_cut || large_cut == tiles) continue;
-        t = before + gemm_microseconds(tiles1 - small_cut, kblocks, products, Epi::kTail, splits, sms);
-        if (t < least) least = t, best = splits, large = large_cut, small = small_cut;
-    }
+    const GemmChoice c = choose_gemm(g, Epi::kDual ? 2 * g.n : g.n, gemm_kblocks(g), P * (P + 1) / 2, Epi::kTail);
     GemmPlan rest = g;
-    if (large) {
-        const cudaError_t e = launch_gemm_as<Variant<2, 256, P, P <= 2 ? Epi::kWarps : 8>>(g, 1, 0, large, epi, stream);
-        if (e != cudaSuccess || !best) return e;
+    if (c.large) {
+        const cudaError_t e = launch_gemm_as<Variant<2, 256, P, P <= 2 ? Epi::kWarps : 8>>(g, 1, 0, c.large, epi, stream);
+        if (e != cudaSuccess || !c.splits) return e;
         rest.after = true;
     }
-    return launch_gemm_as<Variant<1, 128, P, 8, true>>(rest, best, small, 0, epi, stream);
+    return launch_gemm_as<Variant<1, 128, P, 8, true>>(rest, c.splits, c.small, 0, epi, stream);
+}
+
+// Parts that the sums of a product with few large tiles are cut into, so that all pairs of SMs have some; a second launch adds
+// them (fp32, 2048 x 4096 x 768: see store_product).  1: none.
+inline int gemm_parts(const GemmPlan& g, int products, double tail)
+{
+    const int64_t tiles = g.batch * gemm_tiles(g, g.n, 256), kblocks = gemm_kblocks(g);
+    double least = choose_gemm(g, g.n, kblocks, products, tail).microseconds;
+    int best = 1;
+    for (int parts = 2; parts <= 8 && parts <= kblocks && tiles * parts <= sm_count() / 2; ++parts) {
+        // the parts pass through L2
+        const double t = gemm_microseconds(tiles * parts, (kblocks + parts - 1) / parts, products, 1.0, 0, sm_count()) + 4.0 + parts * g.batch * g.m * g.n * 4 / 4e6;
+        if (t < least) least = t, best = parts;
+    }
+    return best;
 }
 
 }  // namespace gpga
