@@ -98,11 +98,13 @@ cudaError_t backward(const FeedForwardParams& p, cudaStream_t stream)
     return store_product<T, P>(g, p.dx, p.nodes * p.rows, nullptr, false, Exponents(), stream);
 }
 
-// fp32 as pairs of fp16.
+// fp32 as pairs of fp16.  What follows dh is not its product's epilogue: a tile's sums take the registers of its few warps, which
+// then wait for g and u and for the activation.  Two passes with all warps take less: one for the largest values of h, and of dg
+// and du, one that makes their pieces (2048 x 2048 values: product 46 us with h, dg, du as fp32 and 18 us for their pieces).
 struct PairsPlan {
-    PackPlan in, between;
+    PackPlan in;
     Operand x, dy, gate, up, down, h, dgu;
-    float *hf, *dguf, *sums;
+    float *dh, *sums;
     int64_t ldh, bytes;
     uint32_t *parts, *peaks;     // of dy, down, x, gate, up (kPeakParts each); of h, of dg and du
     int32_t* exponents;          // of dy, down, x, gate and up, up again, h, dg and du
@@ -111,8 +113,8 @@ struct PairsPlan {
 PairsPlan plan_pairs(const FeedForwardParams& p)
 {
     PairsPlan q;
-    q.in.base = q.between.base = p.scratch;
-    q.in.pieces = q.between.pieces = 2;
+    q.in.base = p.scratch;
+    q.in.pieces = 2;
     ScratchPlan& s = q.in.scratch;
     q.parts = reinterpret_cast<uint32_t*>(p.scratch + s.take(5 * kPeakParts * 4));
     q.peaks = reinterpret_cast<uint32_t*>(p.scratch + s.take(8));
@@ -128,18 +130,75 @@ PairsPlan plan_pairs(const FeedForwardParams& p)
     q.up = q.in.operand(p.up.p, p.up.ld, p.up.node, p.f, p.d, p.nodes, true, true, 2);
     q.in.scaled(q.parts + 3 * kPeakParts, 2 * kPeakParts, q.exponents + 4);
     q.ldh = (p.f + 7) / 8 * 8;
-    q.hf = reinterpret_cast<float*>(p.scratch + s.take(p.nodes * p.rows * q.ldh * 4));
-    q.dguf = reinterpret_cast<float*>(p.scratch + s.take(2 * p.nodes * p.rows * q.ldh * 4));
-    q.between.scratch = s;
-    q.h = q.between.operand(q.hf, q.ldh, p.rows * q.ldh, p.rows, p.f, p.nodes, true, true, 2);
-    q.between.scaled(q.peaks, 1, q.exponents + 5);
-    q.dgu = q.between.operand(q.dguf, q.ldh, p.rows * q.ldh, p.rows, p.f, 2 * p.nodes, true, true, 2);   // dg of all nodes, then du
-    q.between.scaled(q.peaks + 1, 1, q.exponents + 6);
-    ScratchPlan all = q.between.scratch;
-    const int64_t parts = std::max({parts_bytes(p.d, p.f, p.rows, p.nodes, 1), parts_bytes(p.f, p.d, p.rows, 2 * p.nodes, 1), parts_bytes(p.rows, p.d, p.f, p.nodes, 2)});
-    q.sums = reinterpret_cast<float*>(p.scratch + all.take(parts));
-    q.bytes = all.bytes;
+    q.dh = reinterpret_cast<float*>(p.scratch + s.take(p.nodes * p.rows * q.ldh * 4));
+    q.h = q.in.written(p.rows, p.f, p.nodes, true);
+    q.dgu = q.in.written(p.rows, p.f, 2 * p.nodes, true);   // dg of all nodes, then du
+    const int64_t parts = std::max({parts_bytes(p.rows, p.f, p.d, p.nodes, 1), parts_bytes(p.d, p.f, p.rows, p.nodes, 1),
+                                    parts_bytes(p.f, p.d, p.rows, 2 * p.nodes, 1), parts_bytes(p.rows, p.d, p.f, p.nodes, 2)});
+    q.sums = reinterpret_cast<float*>(p.scratch + s.take(parts));
+    q.bytes = s.bytes;
     return q;
+}
+
+struct SlopeParams {
+    const float *g, *u, *dh;
+    int64_t ldg, ldu, ldh;
+    int64_t chunks;           // of eight columns, all rows
+    int32_t f, kind, vec;
+    Pieces<__half> h, dg, du;
+    uint32_t* peaks;          // of h; of dg and du
+    int32_t* exponents;
+};
+
+// PACK: the pieces of h, dg and du; otherwise their largest values.  Bound by memory (12 bytes read per value, 12 written).
+template <bool PACK>
+__global__ void __launch_bounds__(256) slopes_kernel(const __grid_constant__ SlopeParams p)
+{
+    grid_launch_dependents();
+    grid_dependency_wait();
+    float scale[2] = {1.f, 1.f};
+    if constexpr (PACK)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int e = scale_exponent(p.peaks[i]);
+            scale[i] = __int_as_float((e + 127) << 23);
+            if (blockIdx.x == 0 && threadIdx.x == 0) p.exponents[i] = -e;
+        }
+    const int per = (int)(p.ldh / 8);
+    uint32_t peak[2] = {0, 0};
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < p.chunks; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / per;
+        const int col = (int)(i - row * per) * 8, left = min(8, p.f - col);
+        Raw<float> rg, ru, rd;
+        rg.load(p.g + row * p.ldg + col, left, p.vec);
+        ru.load(p.u + row * p.ldu + col, left, p.vec);
+        rd.load(p.dh + row * p.ldh + col, left, true);
+        float v[8], w[8], dh[8], dg[8];
+        rg.values(v);
+        ru.values(w);
+        rd.values(dh);
+        block_slopes<false>(v, w, dh, dg, p.kind);
+        if constexpr (PACK) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] *= scale[0], dg[k] *= scale[1], dh[k] *= scale[1];
+            p.h.store_at<2>(i * 8, v);
+            p.dg.store_at<2>(i * 8, dg);
+            p.du.store_at<2>(i * 8, dh);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (k < left) {
+                    peak[0] = max(peak[0], finite_bits(v[k]));
+                    peak[1] = max(peak[1], max(finite_bits(dg[k]), finite_bits(dh[k])));
+                }
+        }
+    }
+    if constexpr (!PACK)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            peak[i] = __reduce_max_sync(~0u, peak[i]);
+            if ((threadIdx.x & 31) == 0 && peak[i] > *reinterpret_cast<volatile uint32_t*>(p.peaks + i)) atomicMax(p.peaks + i, peak[i]);
+        }
 }
 
 cudaError_t backward_pairs(const FeedForwardParams& p, cudaStream_t stream)
@@ -157,21 +216,31 @@ cudaError_t backward_pairs(const FeedForwardParams& p, cudaStream_t stream)
     g.m = p.rows;
     g.n = p.f;
     g.k = p.d;
-    GateGrad<float, true> grad;
-    grad.g = static_cast<const float*>(p.g.p);
-    grad.u = static_cast<const float*>(p.u.p);
-    grad.ldg = p.g.ld;
-    grad.ldu = p.u.ld;
-    grad.h = {q.hf, q.ldh, p.rows * q.ldh};
-    grad.dg = {q.dguf, q.ldh, p.rows * q.ldh};
-    grad.du = {q.dguf + p.nodes * p.rows * q.ldh, q.ldh, p.rows * q.ldh};
-    grad.exponents = {q.exponents, q.exponents + 1};
-    grad.peaks = q.peaks;
-    grad.m = (int32_t)p.rows;
-    grad.kind = p.activation;
-    grad.vec = rows_on_16(p.g.p, p.g.ld, p.nodes * p.rows, 0, 1, 4) && rows_on_16(p.u.p, p.u.ld, p.nodes * p.rows, 0, 1, 4);
-    e = launch_gemm<2>(g, grad, stream);
-    if (e == cudaSuccess) e = q.between.launch<__half>(stream);
+    const Matrix dh{q.dh, q.ldh, p.rows * q.ldh};
+    e = store_product<float, 2>(g, dh, p.nodes * p.rows, nullptr, false, {q.exponents, q.exponents + 1}, stream, q.sums);
+    if (e != cudaSuccess) return e;
+    Operand dg = q.dgu, du = q.dgu;     // halves of one array
+    dg.batches = du.batches = p.nodes;
+    du.base = static_cast<const __half*>(du.base) + p.nodes * du.batch;
+    SlopeParams s;
+    s.g = static_cast<const float*>(p.g.p);
+    s.u = static_cast<const float*>(p.u.p);
+    s.dh = q.dh;
+    s.ldg = p.g.ld;
+    s.ldu = p.u.ld;
+    s.ldh = q.ldh;
+    s.chunks = p.nodes * p.rows * (q.ldh / 8);
+    s.f = (int32_t)p.f;
+    s.kind = p.activation;
+    s.vec = rows_on_16(p.g.p, p.g.ld, p.nodes * p.rows, 0, 1, 4) && rows_on_16(p.u.p, p.u.ld, p.nodes * p.rows, 0, 1, 4);
+    s.h = pieces_of<__half>(q.h);
+    s.dg = pieces_of<__half>(dg);
+    s.du = pieces_of<__half>(du);
+    s.peaks = q.peaks;
+    s.exponents = q.exponents + 5;
+    const dim3 blocks((unsigned)std::min<int64_t>((s.chunks + 255) / 256, (int64_t)sm_count() * 8));
+    e = launch_after_trigger(slopes_kernel<false>, blocks, dim3(256), 0, stream, true, s);
+    if (e == cudaSuccess) e = launch_after_trigger(slopes_kernel<true>, blocks, dim3(256), 0, stream, true, s);
     if (e != cudaSuccess) return e;
 
     g.a[0] = q.dy;                      // dWd
@@ -187,9 +256,6 @@ cudaError_t backward_pairs(const FeedForwardParams& p, cudaStream_t stream)
     g.n = p.d;
     g.batch = 2 * p.nodes;
     if ((e = store_product<float, 2>(g, p.dgate, p.f, &p.dup, p.accumulate, {q.exponents + 6, q.exponents + 2}, stream, q.sums)) != cudaSuccess) return e;
-    Operand dg = q.dgu, du = q.dgu;
-    dg.batches = du.batches = p.nodes;
-    du.base = static_cast<const __half*>(du.base) + p.nodes * du.batch;
     g.pairs = 2;                        // dx
     g.batch = p.nodes;
     g.a[0] = dg;

@@ -164,23 +164,34 @@ struct GateUp {
     }
 };
 
-// acc = dh; g, u -> h = act(g) u, du = dh act(g), dg = dh u act'(g), all as pieces (PAIRS: as fp32).
-template <class T, bool PAIRS = false>
+// v = g, w = u, dh -> v = h = act(g) u, dg = dh u act'(g), dh = du = dh act(g).
+template <bool FAST>
+__device__ __forceinline__ void block_slopes(float (&v)[8], const float (&w)[8], float (&dh)[8], float (&dg)[8], int kind)
+{
+    act_slopes<FAST>(v, dg, kind);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        dg[i] *= dh[i] * w[i];
+        dh[i] *= v[i];
+        v[i] *= w[i];
+    }
+}
+
+// acc = dh; g, u -> h = act(g) u, du = dh act(g), dg = dh u act'(g), all as pieces.
+template <class T>
 struct GateGrad {
     static constexpr bool kDual = false, kMirror = false;
     static constexpr double kTail = 6.0;
-    static constexpr int kWarps = PAIRS ? 8 : 16;
+    static constexpr int kWarps = 16;
     using T16 = typename PiecesOf<T>::type;
     static constexpr int P = PiecesOf<T>::count;
     struct Ahead {
         Raw<T> g, u;
     };
-    static constexpr int kPeaks = PAIRS ? 2 : 0;
+    static constexpr int kPeaks = 0;
     const T *g, *u;
     int64_t ldg, ldu;
-    std::conditional_t<PAIRS, Between, Pieces<T16>> h, dg, du;
-    Exponents exponents;
-    uint32_t* peaks;      // of h; of dg and du
+    Pieces<T16> h, dg, du;
     int32_t m, kind, vec;
 
     __device__ __forceinline__ bool wide() const { return true; }
@@ -191,38 +202,16 @@ struct GateGrad {
         ahead.g.load(g + at * ldg + col, left, vec);
         ahead.u.load(u + at * ldu + col, left, vec);
     }
-    __device__ __forceinline__ void put(const std::conditional_t<PAIRS, Between, Pieces<T16>>& to, int64_t at, const float (&v)[8], int which, int left) const
-    {
-        if constexpr (PAIRS) {
-            note_peak(which, v, left);
-            to.store(at, v);
-        } else {
-            to.template store_at<P>(at, v);
-        }
-    }
     __device__ __forceinline__ void eight(float (&dh)[8], const Ahead& now, int batch, int row, int col, int left) const
     {
         float a[8], s[8], uv[8];
-        if constexpr (PAIRS) {
-            float e, f;
-            exponents.factors(e, f);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) dh[i] = dh[i] * e * f;
-        }
         now.g.values(a);
         now.u.values(uv);
-        act_slopes<sizeof(T) == 2>(a, s, kind);
+        block_slopes<sizeof(T) == 2>(a, uv, dh, s, kind);
         const int64_t at = batch * h.batch + row * h.ld + col;    // of all three
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s[i] *= dh[i] * uv[i];
-        put(dg, at, s, 1, left);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            dh[i] *= a[i];
-            a[i] *= uv[i];
-        }
-        put(h, at, a, 0, left);
-        put(du, at, dh, 1, left);
+        dg.template store_at<P>(at, s);
+        h.template store_at<P>(at, a);
+        du.template store_at<P>(at, dh);
     }
 };
 

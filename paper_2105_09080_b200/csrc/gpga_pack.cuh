@@ -70,6 +70,9 @@ __global__ void __launch_bounds__(256) peak_kernel(const __grid_constant__ PackJ
     }
 }
 
+// Exponent of the power of two that brings the largest value to 2^14 .. 2^15; an array of zeros stays as it is.
+__device__ __forceinline__ int scale_exponent(uint32_t peak) { return peak ? min(14 + 127 - (int)(peak >> 23), 120) : 0; }
+
 // A thread takes a chunk of eight columns: one pass over the source, bound by memory (fp32 to three pieces: 4 bytes read,
 // 6 written per value).
 template <class T16>
@@ -84,8 +87,7 @@ __global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackJ
             uint32_t peak = 0;
             for (int k = threadIdx.x & 31; k < j.peak_count; k += 32) peak = max(peak, j.peaks[k]);
             peak = __reduce_max_sync(~0u, peak);
-            // the largest value to 2^14 .. 2^15; an array of zeros as it is
-            const int e = peak ? min(14 + 127 - (int)(peak >> 23), 120) : 0;
+            const int e = scale_exponent(peak);
             if ((threadIdx.x & 31) == 0) {
                 scale[i] = __int_as_float((e + 127) << 23);
                 if (blockIdx.x == 0) *j.exponent = -e;
