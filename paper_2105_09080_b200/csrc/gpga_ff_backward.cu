@@ -8,7 +8,17 @@ namespace {
 struct BackwardPlan {
     PackPlan pack;
     Operand x, dy, gate, up, down, h, dgu;
+    float* sums;
+    int64_t bytes;
 };
+
+// Room for the parts of the three products behind dh (store_product).
+template <int P>
+int64_t all_parts_bytes(const FeedForwardParams& p, int64_t weight_pieces)
+{
+    return std::max({parts_bytes<P>(p.d, p.f, p.rows, p.nodes, 1, P), parts_bytes<P>(p.f, p.d, p.rows, 2 * p.nodes, 1, P),
+                     parts_bytes<P>(p.rows, p.d, p.f, p.nodes, 2, weight_pieces)});
+}
 
 BackwardPlan plan_backward(const FeedForwardParams& p)
 {
@@ -23,15 +33,18 @@ BackwardPlan plan_backward(const FeedForwardParams& p)
     q.up = q.pack.weights(p.up.p, p.up.ld, p.up.node, p.f, p.d, p.nodes, wf32, true);
     q.h = q.pack.written(p.rows, p.f, p.nodes, true);
     q.dgu = q.pack.written(p.rows, p.f, 2 * p.nodes, true);   // dg of all nodes, then du
+    const int64_t parts = f32 ? all_parts_bytes<3>(p, 3) : all_parts_bytes<1>(p, q.gate.pieces);
+    q.sums = reinterpret_cast<float*>(p.scratch + q.pack.scratch.take(parts));
+    q.bytes = q.pack.scratch.bytes;
     return q;
 }
 
 template <class T>
-cudaError_t weight_gradient(const GemmPlan& g, const FeedForwardParams& p, const Matrix& out, int64_t rows, const Matrix* second, cudaStream_t stream)
+cudaError_t weight_gradient(const GemmPlan& g, const FeedForwardParams& p, const Matrix& out, int64_t rows, const Matrix* second, float* sums, cudaStream_t stream)
 {
     constexpr int P = PiecesOf<T>::count;
-    if (p.grad_dtype == 0) return store_product<float, P>(g, out, rows, second, p.accumulate, Exponents(), stream);
-    if constexpr (P == 1) return store_product<T, P>(g, out, rows, second, p.accumulate, Exponents(), stream);
+    if (p.grad_dtype == 0) return store_product<float, P>(g, out, rows, second, p.accumulate, Exponents(), sums, stream);
+    if constexpr (P == 1) return store_product<T, P>(g, out, rows, second, p.accumulate, Exponents(), sums, stream);
     return cudaErrorInvalidValue;
 }
 
@@ -76,14 +89,14 @@ cudaError_t backward(const FeedForwardParams& p, cudaStream_t stream)
     g.m = p.d;
     g.n = p.f;
     g.k = p.rows;
-    if ((e = weight_gradient<T>(g, p, p.ddown, p.d, nullptr, stream)) != cudaSuccess) return e;
+    if ((e = weight_gradient<T>(g, p, p.ddown, p.d, nullptr, q.sums, stream)) != cudaSuccess) return e;
 
     g.a[0] = q.dgu;                     // dWg = dg^T x, dWu = du^T x
     g.b[0] = q.x;
     g.m = p.f;
     g.n = p.d;
     g.batch = 2 * p.nodes;
-    if ((e = weight_gradient<T>(g, p, p.dgate, p.f, &p.dup, stream)) != cudaSuccess) return e;
+    if ((e = weight_gradient<T>(g, p, p.dgate, p.f, &p.dup, q.sums, stream)) != cudaSuccess) return e;
 
     g.pairs = 2;                        // dx = dg Wg + du Wu, last: it may take dy's or x's place
     g.batch = p.nodes;
@@ -95,7 +108,7 @@ cudaError_t backward(const FeedForwardParams& p, cudaStream_t stream)
     g.m = p.rows;
     g.n = p.d;
     g.k = p.f;
-    return store_product<T, P>(g, p.dx, p.nodes * p.rows, nullptr, false, Exponents(), stream);
+    return store_product<T, P>(g, p.dx, p.nodes * p.rows, nullptr, false, Exponents(), q.sums, stream);
 }
 
 // fp32 as pairs of fp16.  What follows dh is not its product's epilogue: a tile's sums take the registers of its few warps, which
@@ -133,8 +146,7 @@ PairsPlan plan_pairs(const FeedForwardParams& p)
     q.dh = reinterpret_cast<float*>(p.scratch + s.take(p.nodes * p.rows * q.ldh * 4));
     q.h = q.in.written(p.rows, p.f, p.nodes, true);
     q.dgu = q.in.written(p.rows, p.f, 2 * p.nodes, true);   // dg of all nodes, then du
-    const int64_t parts = std::max({parts_bytes(p.rows, p.f, p.d, p.nodes, 1), parts_bytes(p.d, p.f, p.rows, p.nodes, 1),
-                                    parts_bytes(p.f, p.d, p.rows, 2 * p.nodes, 1), parts_bytes(p.rows, p.d, p.f, p.nodes, 2)});
+    const int64_t parts = std::max(parts_bytes<2>(p.rows, p.f, p.d, p.nodes, 1, 2), all_parts_bytes<2>(p, 2));
     q.sums = reinterpret_cast<float*>(p.scratch + s.take(parts));
     q.bytes = s.bytes;
     return q;
@@ -217,7 +229,7 @@ cudaError_t backward_pairs(const FeedForwardParams& p, cudaStream_t stream)
     g.n = p.f;
     g.k = p.d;
     const Matrix dh{q.dh, q.ldh, p.rows * q.ldh};
-    e = store_product<float, 2>(g, dh, p.nodes * p.rows, nullptr, false, {q.exponents, q.exponents + 1}, stream, q.sums);
+    e = store_product<float, 2>(g, dh, p.nodes * p.rows, nullptr, false, {q.exponents, q.exponents + 1}, q.sums, stream);
     if (e != cudaSuccess) return e;
     Operand dg = q.dgu, du = q.dgu;     // halves of one array
     dg.batches = du.batches = p.nodes;
@@ -249,13 +261,13 @@ cudaError_t backward_pairs(const FeedForwardParams& p, cudaStream_t stream)
     g.m = p.d;
     g.n = p.f;
     g.k = p.rows;
-    if ((e = store_product<float, 2>(g, p.ddown, p.d, nullptr, p.accumulate, {q.exponents, q.exponents + 5}, stream, q.sums)) != cudaSuccess) return e;
+    if ((e = store_product<float, 2>(g, p.ddown, p.d, nullptr, p.accumulate, {q.exponents, q.exponents + 5}, q.sums, stream)) != cudaSuccess) return e;
     g.a[0] = q.dgu;                     // dWg, dWu
     g.b[0] = q.x;
     g.m = p.f;
     g.n = p.d;
     g.batch = 2 * p.nodes;
-    if ((e = store_product<float, 2>(g, p.dgate, p.f, &p.dup, p.accumulate, {q.exponents + 6, q.exponents + 2}, stream, q.sums)) != cudaSuccess) return e;
+    if ((e = store_product<float, 2>(g, p.dgate, p.f, &p.dup, p.accumulate, {q.exponents + 6, q.exponents + 2}, q.sums, stream)) != cudaSuccess) return e;
     g.pairs = 2;                        // dx
     g.batch = p.nodes;
     g.a[0] = dg;
@@ -266,7 +278,7 @@ cudaError_t backward_pairs(const FeedForwardParams& p, cudaStream_t stream)
     g.m = p.rows;
     g.n = p.d;
     g.k = p.f;
-    return store_product<float, 2>(g, p.dx, p.nodes * p.rows, nullptr, false, {q.exponents + 6, q.exponents + 3}, stream, q.sums);
+    return store_product<float, 2>(g, p.dx, p.nodes * p.rows, nullptr, false, {q.exponents + 6, q.exponents + 3}, q.sums, stream);
 }
 
 template <class T>
@@ -306,7 +318,7 @@ unsigned int* ff_backward_gave_up()
     return cudaGetSymbolAddress(&at, gave_up) == cudaSuccess ? static_cast<unsigned int*>(at) : nullptr;
 }
 
-int64_t ff_backward_scratch_bytes(const FeedForwardParams& p) { return !p.rows ? 0 : ff_pairs(p, true) ? plan_pairs(p).bytes : plan_backward(p).pack.scratch.bytes; }
+int64_t ff_backward_scratch_bytes(const FeedForwardParams& p) { return !p.rows ? 0 : ff_pairs(p, true) ? plan_pairs(p).bytes : plan_backward(p).bytes; }
 
 cudaError_t launch_ff_backward(const FeedForwardParams& p, cudaStream_t stream)
 {

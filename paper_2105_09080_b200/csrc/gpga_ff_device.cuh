@@ -287,8 +287,9 @@ __global__ void __launch_bounds__(256) sum_parts_kernel(const float* sums, int p
     }
 }
 
-// Bytes of the parts of a product of pairs, if store_product leaves its sums in parts.
-inline int64_t parts_bytes(int64_t m, int64_t n, int64_t k, int64_t batch, int pairs)
+// Bytes of the parts of a product of P pieces, if store_product leaves its sums in parts.
+template <int P>
+int64_t parts_bytes(int64_t m, int64_t n, int64_t k, int64_t batch, int pairs, int64_t b_pieces)
 {
     GemmPlan g;
     g.m = m;
@@ -296,13 +297,15 @@ inline int64_t parts_bytes(int64_t m, int64_t n, int64_t k, int64_t batch, int p
     g.k = k;
     g.batch = batch;
     g.pairs = pairs;
-    const int parts = gemm_parts(g, 3, StoreRows<float>::kTail);
+    g.a[0].pieces = P;
+    g.b[0].pieces = b_pieces;
+    const int parts = gemm_parts(g, P * (P + 1) / 2, StoreRows<float>::kTail);
     return parts > 1 ? parts * batch * m * ((n + 7) / 8 * 8) * 4 : 0;
 }
 
-// A product stored at its place.  sums: room for parts_bytes(), where the sums may be left in parts.
+// A product stored at its place.  sums: room for parts_bytes().
 template <class T, int P>
-cudaError_t store_product(const GemmPlan& g, const Matrix& out, int64_t rows, const Matrix* second, bool accumulate, const Exponents& exponents, cudaStream_t stream, float* sums = nullptr)
+cudaError_t store_product(const GemmPlan& g, const Matrix& out, int64_t rows, const Matrix* second, bool accumulate, const Exponents& exponents, float* sums, cudaStream_t stream)
 {
     StoreRows<T> e;
     e.exponents = exponents;
@@ -316,25 +319,21 @@ cudaError_t store_product(const GemmPlan& g, const Matrix& out, int64_t rows, co
     e.split = (int32_t)(second ? g.batch / 2 : g.batch);
     e.accumulate = accumulate;
     e.vec = rows_on_16(out.p, out.ld, rows, out.node, g.batch, sizeof(T)) && rows_on_16(o2.p, o2.ld, rows, o2.node, g.batch, sizeof(T));
-    if constexpr (P == 2 && std::is_same<T, float>::value) {
-        const int parts = sums ? gemm_parts(g, P * (P + 1) / 2, StoreRows<float>::kTail) : 1;
-        if (parts > 1) {
-            StoreRows<float> to;
-            const int64_t ld = (g.n + 7) / 8 * 8;
-            to.exponents = Exponents();
-            to.out[0] = to.out[1] = sums;
-            to.ld[0] = to.ld[1] = ld;
-            to.node[0] = to.node[1] = g.m * ld;
-            to.split = INT32_MAX;
-            to.accumulate = 0;
-            to.vec = 1;
-            const cudaError_t r = launch_gemm_as<Variant<2, 256, P, 8, false, true>>(g, parts, 0, 0, to, stream);
-            if (r != cudaSuccess) return r;
-            const int64_t chunks = g.batch * g.m * (ld / 8);
-            return launch_after_trigger(sum_parts_kernel<T>, dim3((unsigned)std::min<int64_t>((chunks + 255) / 256, (int64_t)sm_count() * 8)), dim3(256), 0, stream, true, sums, parts, (int)g.m, (int)g.n, ld, chunks, e);
-        }
-    }
-    return launch_gemm<P>(g, e, stream);
+    const int parts = gemm_parts(g, P * (P + 1) / 2, StoreRows<float>::kTail);
+    if (parts == 1) return launch_gemm<P>(g, e, stream);
+    StoreRows<float> to;
+    const int64_t ld = (g.n + 7) / 8 * 8, chunks = g.batch * g.m * (ld / 8);
+    to.exponents = Exponents();
+    to.out[0] = to.out[1] = sums;
+    to.ld[0] = to.ld[1] = ld;
+    to.node[0] = to.node[1] = g.m * ld;
+    to.split = INT32_MAX;
+    to.accumulate = 0;
+    to.vec = 1;
+    const cudaError_t r = launch_gemm_as<Variant<2, 256, P, 8, false, true>>(g, parts, 0, 0, to, stream);
+    if (r != cudaSuccess) return r;
+    const dim3 blocks((unsigned)std::min<int64_t>((chunks + 255) / 256, (int64_t)sm_count() * 8));
+    return launch_after_trigger(sum_parts_kernel<T>, blocks, dim3(256), 0, stream, true, sums, parts, (int)g.m, (int)g.n, ld, chunks, e);
 }
 
 }  // namespace gpga

@@ -8,6 +8,8 @@ namespace {
 struct ForwardPlan {
     PackPlan pack;
     Operand x, gate, up, down, h;
+    float* sums;
+    int64_t bytes;
 };
 
 ForwardPlan plan_forward(const FeedForwardParams& p)
@@ -21,6 +23,9 @@ ForwardPlan plan_forward(const FeedForwardParams& p)
     q.up = q.pack.weights(p.up.p, p.up.ld, p.up.node, p.f, p.d, p.nodes, wf32, false);
     q.down = q.pack.weights(p.down.p, p.down.ld, p.down.node, p.d, p.f, p.nodes, wf32, false);
     q.h = q.pack.written(p.rows, p.f, p.nodes, false);
+    const int64_t parts = f32 ? parts_bytes<3>(p.rows, p.d, p.f, p.nodes, 1, 3) : parts_bytes<1>(p.rows, p.d, p.f, p.nodes, 1, q.down.pieces);
+    q.sums = reinterpret_cast<float*>(p.scratch + q.pack.scratch.take(parts));
+    q.bytes = q.pack.scratch.bytes;
     return q;
 }
 
@@ -59,7 +64,7 @@ cudaError_t forward(const FeedForwardParams& p, cudaStream_t stream)
     g.b[0] = q.down;
     g.n = p.d;
     g.k = p.f;
-    return store_product<T, P>(g, p.y, p.nodes * p.rows, nullptr, false, Exponents(), stream);
+    return store_product<T, P>(g, p.y, p.nodes * p.rows, nullptr, false, Exponents(), q.sums, stream);
 }
 
 // fp32 as pairs of fp16.
@@ -95,7 +100,7 @@ PairsPlan plan_pairs(const FeedForwardParams& p)
     q.h = q.between.operand(q.hf, q.ldh, p.rows * q.ldh, p.rows, p.f, p.nodes, true, false, 2);
     q.between.scaled(q.peaks, 1, q.exponents + 4);
     ScratchPlan all = q.between.scratch;
-    q.sums = reinterpret_cast<float*>(p.scratch + all.take(parts_bytes(p.rows, p.d, p.f, p.nodes, 1)));
+    q.sums = reinterpret_cast<float*>(p.scratch + all.take(parts_bytes<2>(p.rows, p.d, p.f, p.nodes, 1, 2)));
     q.bytes = all.bytes;
     return q;
 }
@@ -135,7 +140,7 @@ cudaError_t forward_pairs(const FeedForwardParams& p, cudaStream_t stream)
     g.b[0] = q.down;
     g.n = p.d;
     g.k = p.f;
-    return store_product<float, 2>(g, p.y, p.nodes * p.rows, nullptr, false, {q.exponents + 4, q.exponents + 3}, stream, q.sums);
+    return store_product<float, 2>(g, p.y, p.nodes * p.rows, nullptr, false, {q.exponents + 4, q.exponents + 3}, q.sums, stream);
 }
 
 }  // namespace
@@ -148,7 +153,7 @@ unsigned int* ff_forward_gave_up()
 
 int64_t ff_forward_scratch_bytes(const FeedForwardParams& p) 
 {
-    return !p.rows ? 0 : ff_few(p) ? ff_few_scratch_bytes(p) : ff_pairs(p, false) ? plan_pairs(p).bytes : plan_forward(p).pack.scratch.bytes;
+    return !p.rows ? 0 : ff_few(p) ? ff_few_scratch_bytes(p) : ff_pairs(p, false) ? plan_pairs(p).bytes : plan_forward(p).bytes;
 }
 
 cudaError_t launch_ff_forward(const FeedForwardParams& p, cudaStream_t stream)
