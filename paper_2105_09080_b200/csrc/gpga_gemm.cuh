@@ -984,15 +984,16 @@ cudaError_t launch_gemm(const GemmPlan& g, const Epi& epi, cudaStream_t stream)
 }
 
 // Parts that the sums of a product with few large tiles are cut into, so that all pairs of SMs have some; a second launch adds
-// them (fp32, 2048 x 4096 x 768: see store_product).  1: none.
+// them.  1: none.  Measured without and with them, all of a gradient: 14583 tokens x 308 x 683, bfloat16, 199 us and 170 us,
+// fp32 373 us and 312 us; 1278 x 934 x 1694 105 us and 96 us, 204 us and 180 us.
 inline int gemm_parts(const GemmPlan& g, int products, double tail)
 {
     const int64_t tiles = g.batch * gemm_tiles(g, g.n, 256), kblocks = gemm_kblocks(g);
     double least = choose_gemm(g, g.n, kblocks, products, tail).microseconds;
     int best = 1;
     for (int parts = 2; parts <= 8 && parts <= kblocks && tiles * parts <= sm_count() / 2; ++parts) {
-        // the parts pass through L2
-        const double t = gemm_microseconds(tiles * parts, (kblocks + parts - 1) / parts, products, 1.0, 0, sm_count()) + 4.0 + parts * g.batch * g.m * g.n * 4 / 4e6;
+        // the second launch, fp32 sums that are not hidden by the next tile's, and the parts' way through L2
+        const double t = gemm_microseconds(tiles * parts, (kblocks + parts - 1) / parts, products, 1.0, 0, sm_count()) + (products > 1 ? 9.0 : 4.0) + parts * g.batch * g.m * g.n * 4 / 4e6;
         if (t < least) least = t, best = parts;
     }
     return best;
