@@ -993,7 +993,7 @@ inline int gemm_parts(const GemmPlan& g, int products, double tail)
     int best = 1;
     for (int parts = 2; parts <= 8 && parts <= kblocks && tiles * parts <= sm_count() / 2; ++parts) {
         // the second launch, fp32 sums that are not hidden by the next tile's, and the parts' way through L2
-        const double t = gemm_microseconds(tiles * parts, (kblocks + parts - 1) / parts, products, 1.0, 0, sm_count()) + (products > 1 ? 9.0 : 4.0) + parts * g.batch * g.m * g.n * 4 / 4e6;
+        const double t = gemm_microseconds(tiles * parts, (kblocks + parts - 1) / parts, products, 1.0, 0, sm_count()) + (products > 1 ? 6.0 : 4.0) + parts * g.batch * g.m * g.n * 4 / 4e6;
         if (t < least) least = t, best = parts;
     }
     return best;
