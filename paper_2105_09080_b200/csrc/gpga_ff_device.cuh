@@ -115,7 +115,7 @@ __device__ __forceinline__ void note_peak(int which, const float (&v)[8], int le
 // g, u -> h = act(g) u as pieces (PAIRS: as fp32); g and u themselves where they are kept.
 template <class T, bool PAIRS = false>
 struct GateUp {
-    static constexpr bool kDual = true, kMirror = false;
+    static constexpr bool kDual = true, kMirror = false, kPair = false;
     static constexpr double kTail = 3.0;
     static constexpr int kWarps = 16;
     using T16 = typename PiecesOf<T>::type;
@@ -180,7 +180,7 @@ __device__ __forceinline__ void block_slopes(float (&v)[8], const float (&w)[8],
 // acc = dh; g, u -> h = act(g) u, du = dh act(g), dg = dh u act'(g), all as pieces.
 template <class T>
 struct GateGrad {
-    static constexpr bool kDual = false, kMirror = false;
+    static constexpr bool kDual = false, kMirror = false, kPair = sizeof(T) == 2;
     static constexpr double kTail = 6.0;
     static constexpr int kWarps = 16;
     using T16 = typename PiecesOf<T>::type;
@@ -218,7 +218,7 @@ struct GateGrad {
 // acc -> an array of the caller's; batches from `split` on go to the second one.
 template <class T>
 struct StoreRows {
-    static constexpr bool kDual = false, kMirror = false;
+    static constexpr bool kDual = false, kMirror = false, kPair = false;
     static constexpr double kTail = 1.0;
     static constexpr int kWarps = 8;
     static constexpr int kPeaks = 0;

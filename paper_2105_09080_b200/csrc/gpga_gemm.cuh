@@ -145,6 +145,30 @@ __device__ __forceinline__ void stage8(float* stage, int row, int c, const float
 }
 __device__ __forceinline__ float staged1(const float* stage, int row, int c) { return stage[row * 32 + (c ^ (4 * (row & 7)))]; }
 
+// The same for two warps side by side, each with 32 columns of the same rows: rows of 64, so that a store of 16-bit values to
+// memory has whole lines.  `half`: which one this warp is; `id`: of the pair's barrier.
+__device__ __forceinline__ void pair_sync(int id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ bool pair_all(int id, bool ok)
+{
+    uint32_t all;
+    asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 p, %2, 0;\nbar.red.and.pred q, %1, 64, p;\nselp.u32 %0, 1, 0, q;\n}" : "=r"(all) : "r"(id), "r"((uint32_t)ok) : "memory");
+    return all;
+}
+__device__ __forceinline__ int pair_place(int row, int c) { return row * 64 + (c & 32) + ((c & 31) ^ (4 * ((row & 7) ^ (c >> 5)))); }
+__device__ __forceinline__ void pair_staged8(const float* stage, int row, int c, float (&v)[8])
+{
+    const float4 a = *reinterpret_cast<const float4*>(stage + pair_place(row, c)), b = *reinterpret_cast<const float4*>(stage + pair_place(row, c + 4));
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+}
+__device__ __forceinline__ void stage_pair(const float (&v)[32], float* stage, int lane, int half, int id)
+{
+    pair_sync(id);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        *reinterpret_cast<float4*>(stage + pair_place(lane, half * 32 + 4 * j)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+    pair_sync(id);
+}
+
 // Eight values as they lie in memory; zeros from the n-th on.
 template <class T>
 struct Raw {
@@ -308,6 +332,7 @@ constexpr int kFewRegisters = 64, kManyRegisters = 208;
 //   kDual: eight(v, w, batch, row, col, left), v of the first array's columns, w of the second's.  wide() false: keep(which, v,
 //   batch, row, col) is called first for every single value.
 //   kPeaks: largest values that the block notes (block_peaks) and adds to those at `peaks` in the end.
+//   kPair: 16-bit values that are read and stored pass in whole lines of 64 columns, two warps together (wide() is true).
 //   kTail: microseconds of 128 x 256 columns, for the choice of the variant.
 //   kMirror: eight() leaves in v what it has stored; put(v, batch, row, col) stores it again at its mirror place.
 // The loops over eight columns are kept rolled: a warp goes through an epilogue once per tile, and unrolled it waits for
@@ -511,17 +536,23 @@ __global__ void __launch_bounds__(V::threads, 1)
     } else {
         if constexpr (V::split_registers) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegisters));
         const int quarter = warp & 3, part = (warp - 4) >> 2;   // lanes of tensor memory, columns
-        float* const stage = staging + (warp - 4) * 32 * 32;
+        // Two warps of a quarter stage 64 columns together where that gives whole lines.
+        constexpr bool PAIR = Epi::kPair && !CHUNKED && !SPLIT;
+        static_assert(!Epi::kPair || (!Epi::kDual && !Epi::kMirror), "whole lines of one array, which takes eight()");
+        const int half = part & 1, pair = quarter + 4 * (part >> 1), pair_id = 1 + pair;
+        float* const stage = PAIR ? staging + pair * 64 * 32 : staging + (warp - 4) * 32 * 32;
         const uint32_t release = CG == 2 ? map_shared(acc_empty, 0) : acc_empty;
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
         uint32_t sums = 0;
         bool ok = true;
         constexpr int width = BN / (V::warps / 4) / (Epi::kDual ? 2 : 1);   // columns of this warp (of each array)
-        const int lane_row = lane >> 2, lane_col = (lane & 3) * 8;
+        constexpr int kRows = PAIR ? 4 : 8, kColumns = PAIR ? 64 : 32;   // of a pass over what is staged
+        const int lane_row = PAIR ? half * 16 + (lane >> 3) : lane >> 2, lane_col = PAIR ? (lane & 7) * 8 : (lane & 3) * 8;
+        const int first_column = PAIR ? (part >> 1) * 2 * width : part * width;
         for (int t = first; t < p.tiles && ok; t += step) {
             const GemmTile g = gemm_tile(p, t, 128 * CG, BN);
             if constexpr (V::parts) take_part(g.batch);
-            const int row0 = g.m0 + (int)rank * 128 + quarter * 32, from = (Epi::kDual ? g.n0 / 2 : g.n0) + part * width;
+            const int row0 = g.m0 + (int)rank * 128 + quarter * 32, from = (Epi::kDual ? g.n0 / 2 : g.n0) + first_column;
             const int rows = p.m - row0;   // that are there
             const bool mirror = p.symmetric && g.m0 != g.n0;
             constexpr int kAhead = CHUNKED ? 1 : 2;   // calls of eight() that are read ahead
@@ -533,7 +564,7 @@ __global__ void __launch_bounds__(V::threads, 1)
                 for (int j = 0; j < 8; ++j)
                     *reinterpret_cast<float4*>(sums_at + split_place(split_chunk(col / 8 + j / 2), r, j & 1)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
             };
-            // A 32 x 32 block that is staged; `next`: whether the block to the right follows.
+            // A 32 x 32 block that is staged (PAIR: 16 x 64); `next`: whether the block to the right follows.
             const auto block = [&](int col0, bool next) {
                 if constexpr (!Epi::kDual) {
                 if (!epi.wide()) {
@@ -546,14 +577,17 @@ __global__ void __launch_bounds__(V::threads, 1)
                 for (int i = 0; i < 4; i += kAhead) {
 #pragma unroll
                     for (int j = 0; j < kAhead; ++j) {
-                        const int r = (i + j) * 8 + lane_row, c = col0 + lane_col;
+                        const int r = (i + j) * kRows + lane_row, c = col0 + lane_col;
                         const typename Epi::Ahead now = ahead[j];
                         const bool here = i + kAhead < 4;
-                        const int nr = here ? r + 8 * kAhead : j * 8 + lane_row, nc = here ? c : c + 32;
+                        const int nr = here ? r + kRows * kAhead : j * kRows + lane_row, nc = here ? c : c + kColumns;
                         if (nr < rows && nc < p.n && (here || next)) epi.load(ahead[j], g.batch, row0 + nr, nc, p.n - nc);
                         if (r < rows && c < p.n) {
                             float v[8];
-                            staged8(stage, r, lane_col, v);
+                            if constexpr (PAIR)
+                                pair_staged8(stage, r, lane_col, v);
+                            else
+                                staged8(stage, r, lane_col, v);
                             epi.eight(v, now, g.batch, row0 + r, c, p.n - c);
                             if constexpr (Epi::kMirror)
                                 if (mirror) stage8(stage, r, lane_col, v);
@@ -578,8 +612,8 @@ __global__ void __launch_bounds__(V::threads, 1)
                 if constexpr (!Epi::kDual)
 #pragma unroll
                     for (int j = 0; j < kAhead; ++j)
-                        if (epi.wide() && j * 8 + lane_row < rows && from + lane_col < p.n)
-                            epi.load(ahead[j], g.batch, row0 + j * 8 + lane_row, from + lane_col, p.n - from - lane_col);
+                        if (epi.wide() && j * kRows + lane_row < rows && from + lane_col < p.n)
+                            epi.load(ahead[j], g.batch, row0 + j * kRows + lane_row, from + lane_col, p.n - from - lane_col);
             };
             // The same of two arrays.
             const auto block2 = [&](const float(&a)[32], const float(&b)[32], int col0) {
@@ -661,13 +695,14 @@ __global__ void __launch_bounds__(V::threads, 1)
                 const uint32_t buf = sums & 1;
                 if constexpr (!Epi::kDual && !SPLIT) start();
                 ok = __all_sync(~0u, w.wait(acc_full + 8 * buf, (sums / 2) & 1));
+                if constexpr (PAIR) ok = pair_all(pair_id, ok);   // both go on, or neither
                 if (!ok) break;
                 ++sums;
                 tmem_fence_after();
 #pragma unroll 1
                 for (int c = 0; c < width; c += 32) {
                     float a[32], b[32];
-                    const uint32_t at = lanes + buf * 256 + part * width + c;
+                    const uint32_t at = lanes + buf * 256 + first_column + (PAIR ? 2 * c + half * 32 : c);
                     tmem_load32(at, a);
                     if constexpr (Epi::kDual) tmem_load32(at + BN / 2, b);
                     tmem_wait_load();
@@ -676,7 +711,7 @@ __global__ void __launch_bounds__(V::threads, 1)
                         __syncwarp();
                         if (lane == 0) arrive_cluster(release + 8 * buf);
                     }
-                    const int col0 = from + c;
+                    const int col0 = from + (PAIR ? 2 * c : c);
                     if constexpr (SPLIT) {
                         put_partial(a, part * width + c);
                         if constexpr (Epi::kDual) put_partial(b, part * width + c + BN / 2);
@@ -686,7 +721,10 @@ __global__ void __launch_bounds__(V::threads, 1)
                     if constexpr (Epi::kDual) {
                         block2(a, b, col0);
                     } else {
-                        stage_rows(a, stage, lane);
+                        if constexpr (PAIR)
+                            stage_pair(a, stage, lane, half, pair_id);
+                        else
+                            stage_rows(a, stage, lane);
                         block(col0, c + 32 < width);
                     }
                 }

@@ -114,7 +114,7 @@ __global__ void __launch_bounds__(256) start_kernel(const T* m, int64_t ld, int6
 // kappa^power factor acc + beta R (+ diagonal), as P pieces (R in as many).
 template <int P>
 struct KeepPieces {
-    static constexpr bool kDual = false, kMirror = true;
+    static constexpr bool kDual = false, kMirror = true, kPair = false;
     static constexpr double kTail = 1.0;
     static constexpr int kPeaks = 0;
     static constexpr int kWarps = 8;
@@ -161,7 +161,7 @@ struct KeepPieces {
 // The last step: kappa^power factor acc, added to what is there or not, in the caller's type.
 template <class T>
 struct LastStep {
-    static constexpr bool kDual = false, kMirror = false;
+    static constexpr bool kDual = false, kMirror = false, kPair = false;
     static constexpr double kTail = 1.0;
     static constexpr int kPeaks = 0;
     static constexpr int kWarps = 8;
