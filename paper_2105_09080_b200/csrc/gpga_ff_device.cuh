@@ -177,7 +177,8 @@ __device__ __forceinline__ void block_slopes(float (&v)[8], const float (&w)[8],
     }
 }
 
-// acc = dh; g, u -> h = act(g) u, du = dh act(g), dg = dh u act'(g), all as pieces.
+// acc = dh; g, u -> h = act(g) u, du = dh act(g), dg = dh u act'(g), all as pieces.  What it reads and stores per tile bounds it: 16-bit
+// values in whole lines (8 x 4096 tokens, 1024 x 2816: 236 us, 268 us in half lines).
 template <class T>
 struct GateGrad {
     static constexpr bool kDual = false, kMirror = false, kPair = sizeof(T) == 2;
