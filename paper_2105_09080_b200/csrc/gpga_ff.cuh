@@ -28,10 +28,12 @@ inline bool ff_few(const FeedForwardParams& p)
     return p.rows <= 16 || (p.rows <= 32 && (p.weight_dtype == 0 || p.d * p.f <= 20'000'000));
 }
 // Whether fp32 operands are taken as pairs of fp16 values (three products of pieces, with a pass over every array for its largest
-// value) and not as three bfloat16 values (six products): where the products take long enough for the passes.
+// value) and not as three bfloat16 values (six products): where the products take long enough for the passes.  Measured with
+// three values and with pairs: forward 442 x 221 x 602 on 3 nodes 41 us and 47 us, 2681 x 361 x 666 54 us both, 1151 x 743 x 1901
+// 119 us and 99 us; gradient 550 x 406 x 747 66 us and 70 us, 536 x 378 x 1276 72 us both, 2939 x 284 x 976 141 us and 115 us.
 inline bool ff_pairs(const FeedForwardParams& p, bool backward)
 {
-    return p.dtype == 0 && (double)p.nodes * p.rows * p.d * p.f * (backward ? 12 : 6) >= 1.3e10;
+    return p.dtype == 0 && (double)p.nodes * p.rows * p.d * p.f * (backward ? 12 : 6) >= (backward ? 3e9 : 4e9);
 }
 int64_t ff_few_scratch_bytes(const FeedForwardParams& p);
 cudaError_t launch_ff_few(const FeedForwardParams& p, cudaStream_t stream);
