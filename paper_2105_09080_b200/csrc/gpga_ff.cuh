@@ -27,13 +27,14 @@ inline bool ff_few(const FeedForwardParams& p)
     if (p.dtype == 0) return p.rows <= 8;
     return p.rows <= 16 || (p.rows <= 32 && (p.weight_dtype == 0 || p.d * p.f <= 20'000'000));
 }
-// Whether fp32 operands are taken as pairs of fp16 values (three products of pieces, with a pass over every array for its largest
-// value) and not as three bfloat16 values (six products): where the products take long enough for the passes.  Measured with
-// three values and with pairs: forward 442 x 221 x 602 on 3 nodes 41 us and 47 us, 2681 x 361 x 666 54 us both, 1151 x 743 x 1901
-// 119 us and 99 us; gradient 550 x 406 x 747 66 us and 70 us, 536 x 378 x 1276 72 us both, 2939 x 284 x 976 141 us and 115 us.
+// Whether fp32 operands are taken as pairs of fp16 values (three products of pieces, with passes for the powers of two of rows and
+// columns) and not as three bfloat16 values (six products): where the products take long enough for the passes.  Measured with
+// three values and with pairs: forward 442 x 221 x 602 on 3 nodes 41 us and 54 us, 4096 x 256 x 688 56 us and 57 us, 700 x 700 x
+// 1500 60 us and 53 us, 1151 x 743 x 1901 118 us and 102 us; gradient 1151 x 743 x 1901 182 us and 198 us, 1024 x 1024 x 1024 on 2
+// nodes 184 us and 175 us, 2048 x 768 x 2048 229 us and 197 us.
 inline bool ff_pairs(const FeedForwardParams& p, bool backward)
 {
-    return p.dtype == 0 && (double)p.nodes * p.rows * p.d * p.f * (backward ? 12 : 6) >= (backward ? 3e9 : 4e9);
+    return p.dtype == 0 && (double)p.nodes * p.rows * p.d * p.f * (backward ? 12 : 6) >= (backward ? 24e9 : 4e9);
 }
 int64_t ff_few_scratch_bytes(const FeedForwardParams& p);
 cudaError_t launch_ff_few(const FeedForwardParams& p, cudaStream_t stream);

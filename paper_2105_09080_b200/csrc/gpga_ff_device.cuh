@@ -81,20 +81,47 @@ __device__ __forceinline__ void act_slopes(float (&v)[N], float (&s)[N], int kin
 template <class T> struct PiecesOf { using type = T; static constexpr int count = 1; };
 template <> struct PiecesOf<float> { using type = __nv_bfloat16; static constexpr int count = 3; };
 
-// fp32 operands as pairs of fp16 (ff_pairs): a product is 2^exponent times the product of what was packed, whose arrays have
-// an exponent each.  Two factors, as one may be beyond fp32's range.
+// fp32 operands as pairs of fp16 (ff_pairs): a product's element is 2^(a + b) times the product of what was packed, with an
+// exponent a of its row and one b of its column.  (A value is 2^-23 of itself off in a pair, or 2^-40 of the largest one that
+// shares its power; the product of two rests, at most 2^-22 of a term, is left out.)
 struct Exponents {
-    const int32_t *a = nullptr, *b = nullptr;
-    __device__ __forceinline__ void factors(float& f, float& g) const
+    const int8_t *a = nullptr, *b = nullptr;
+    int64_t a_batch = 0, b_batch = 0;
+    int32_t b_mod = 1;        // batches of b, which come twice at most
+    __device__ __forceinline__ int row(int batch, int r) const { return a[batch * a_batch + r]; }
+    __device__ __forceinline__ const int8_t* column(int batch, int c) const { return b + (batch >= b_mod ? batch - b_mod : batch) * b_batch + c; }
+    using Columns = uint2;    // of eight columns, as they lie in memory
+    __device__ __forceinline__ Columns columns(int batch, int c) const { return *reinterpret_cast<const uint2*>(column(batch, c)); }
+    // 2^(a + b) as two factors with half of the exponent each, as it may be beyond fp32's range.  Exponents are -125 at least, so that
+    // a half's sum is that of a normal number.  What lies between the two is between the sum and the result: nothing is lost there.
+    struct Factors {
+        int32_t one[8], two[8];   // of a column: bits of its halves
+    };
+    __device__ __forceinline__ static Factors factors(const Columns& w)
     {
-        f = g = 1.f;
-        if (!a) return;
-        const int e = max(-250, min(250, *a + *b)), h = e >> 1;
-        f = __int_as_float((h + 127) << 23);
-        g = __int_as_float((e - h + 127) << 23);
+        Factors q;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int e = (int8_t)((k < 4 ? w.x : w.y) >> (8 * (k & 3)));
+            q.one[k] = ((e >> 1) + 127) << 23;
+            q.two[k] = (e - (e >> 1) + 127) << 23;
+        }
+        return q;
+    }
+    // own: the row's exponent
+    __device__ __forceinline__ static void eight(float (&v)[8], const Factors& q, int own)
+    {
+        const int one = (own >> 1) << 23, two = (own - (own >> 1)) << 23;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = v[k] * __int_as_float(q.one[k] + one) * __int_as_float(q.two[k] + two);
+    }
+    __device__ __forceinline__ float one(float v, int batch, int r, int c) const
+    {
+        const int own = row(batch, r), e = *column(batch, c);
+        return v * power_of_two((own >> 1) + (e >> 1)) * power_of_two(own - (own >> 1) + e - (e >> 1));
     }
 };
-// An array between two products that is packed after the first: fp32 rows, and the bits of its largest finite value.
+// An array between two products that is packed after the first: fp32 rows.
 struct Between {
     float* base = nullptr;
     int64_t ld = 0, batch = 0;
@@ -104,13 +131,6 @@ struct Between {
         reinterpret_cast<float4*>(base + place)[1] = make_float4(v[4], v[5], v[6], v[7]);
     }
 };
-__device__ __forceinline__ void note_peak(int which, const float (&v)[8], int left)
-{
-    uint32_t peak = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) peak = max(peak, i < left ? finite_bits(v[i]) : 0u);
-    if (peak > block_peaks()[which]) atomicMax(block_peaks() + which, peak);
-}
 
 // g, u -> h = act(g) u as pieces (PAIRS: as fp32); g and u themselves where they are kept.
 template <class T, bool PAIRS = false>
@@ -120,33 +140,39 @@ struct GateUp {
     static constexpr int kWarps = 16;
     using T16 = typename PiecesOf<T>::type;
     static constexpr int P = PiecesOf<T>::count;
-    using Ahead = NothingAhead;
-    static constexpr int kPeaks = PAIRS ? 1 : 0;
+    using Ahead = Nothing;
     T *g, *u;
     int64_t ldg, ldu;
     std::conditional_t<PAIRS, Between, Pieces<T16>> h;
-    Exponents exponents;
-    uint32_t* peaks;
+    Exponents of_g, of_u;     // PAIRS
     int32_t m, kind, keeps, vec;
+    // Of one of the two arrays.
+    using Columns = std::conditional_t<PAIRS, Exponents::Columns, Nothing>;
 
     __device__ __forceinline__ bool wide() const { return vec; }
+    __device__ __forceinline__ Columns columns(int which, int batch, int col) const
+    {
+        if constexpr (PAIRS) return (which ? of_u : of_g).columns(batch, col);
+        else return {};
+    }
+    __device__ __forceinline__ int row(int batch, int r) const { return PAIRS ? of_g.row(batch, r) : 0; }
+    __device__ __forceinline__ static auto factors(const Columns& q)
+    {
+        if constexpr (PAIRS) return Exponents::factors(q);
+        else return q;
+    }
+    template <class Factors>
+    __device__ __forceinline__ static void scale(float (&v)[8], const Factors& f, int own)
+    {
+        if constexpr (PAIRS) Exponents::eight(v, f, own);
+    }
     __device__ __forceinline__ void keep(int which, float v, int batch, int row, int col) const
     {
-        if constexpr (PAIRS) {
-            float e, f;
-            exponents.factors(e, f);
-            v = v * e * f;
-        }
+        if constexpr (PAIRS) v = (which ? of_u : of_g).one(v, batch, row, col);
         (which ? u : g)[((int64_t)batch * m + row) * (which ? ldu : ldg) + col] = from_f32<T>(v);
     }
     __device__ __forceinline__ void eight(float (&v)[8], float (&w)[8], int batch, int row, int col, int left) const
     {
-        if constexpr (PAIRS) {
-            float e, f;
-            exponents.factors(e, f);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = v[i] * e * f, w[i] = w[i] * e * f;
-        }
         if (keeps && vec) {
             const int64_t at = (int64_t)batch * m + row;
             store8(g + at * ldg + col, left, v);
@@ -155,12 +181,10 @@ struct GateUp {
         act_values<sizeof(T) == 2>(v, kind);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] *= w[i];
-        if constexpr (PAIRS) {
-            note_peak(0, v, left);
+        if constexpr (PAIRS)
             h.store(batch * h.batch + row * h.ld + col, v);
-        } else {
+        else
             h.template store<P>(batch, row, col, v);
-        }
     }
 };
 
@@ -189,7 +213,8 @@ struct GateGrad {
     struct Ahead {
         Raw<T> g, u;
     };
-    static constexpr int kPeaks = 0;
+    using Columns = Nothing;
+    using Factors = Nothing;
     const T *g, *u;
     int64_t ldg, ldu;
     Pieces<T16> h, dg, du;
@@ -197,13 +222,15 @@ struct GateGrad {
 
     __device__ __forceinline__ bool wide() const { return true; }
     __device__ __forceinline__ void one(float, int, int, int) const {}
+    __device__ __forceinline__ Columns columns(int, int) const { return {}; }
+    __device__ __forceinline__ static Factors factors(const Columns&) { return {}; }
     __device__ __forceinline__ void load(Ahead& ahead, int batch, int row, int col, int left) const
     {
         const int64_t at = (int64_t)batch * m + row;
         ahead.g.load(g + at * ldg + col, left, vec);
         ahead.u.load(u + at * ldu + col, left, vec);
     }
-    __device__ __forceinline__ void eight(float (&dh)[8], const Ahead& now, int batch, int row, int col, int left) const
+    __device__ __forceinline__ void eight(float (&dh)[8], const Ahead& now, const Factors&, int batch, int row, int col, int left) const
     {
         float a[8], s[8], uv[8];
         now.g.values(a);
@@ -216,14 +243,18 @@ struct GateGrad {
     }
 };
 
-// acc -> an array of the caller's; batches from `split` on go to the second one.
-template <class T>
+// acc -> an array of the caller's; batches from `split` on go to the second one.  PAIRS: times the powers of two of its operands.
+template <class T, bool PAIRS = false>
 struct StoreRows {
     static constexpr bool kDual = false, kMirror = false, kPair = false;
     static constexpr double kTail = 1.0;
     static constexpr int kWarps = 8;
-    static constexpr int kPeaks = 0;
-    using Ahead = Raw<T>;
+    struct Ahead {
+        Raw<T> old;
+        int row;              // its exponent
+    };
+    using Columns = std::conditional_t<PAIRS, Exponents::Columns, Nothing>;
+    using Factors = std::conditional_t<PAIRS, Exponents::Factors, Nothing>;
     T* out[2];
     int64_t ld[2], node[2];
     Exponents exponents;
@@ -235,20 +266,30 @@ struct StoreRows {
         const int which = batch >= split;
         return {out[which] + (batch - which * split) * node[which], ld[which], 1.f, accumulate != 0};
     }
-    __device__ __forceinline__ void load(Ahead& old, int batch, int row, int col, int left) const { rows(batch).ahead(old, row, col, left); }
-    __device__ __forceinline__ void eight(float (&v)[8], const Ahead& old, int batch, int row, int col, int left) const
+    __device__ __forceinline__ void load(Ahead& ahead, int batch, int row, int col, int left) const
     {
-        float e, f;
-        exponents.factors(e, f);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = v[i] * e * f;
-        rows(batch).eight(v, old, row, col, left);
+        if constexpr (PAIRS) ahead.row = exponents.row(batch, row);
+        rows(batch).ahead(ahead.old, row, col, left);
+    }
+    __device__ __forceinline__ Columns columns(int batch, int col) const
+    {
+        if constexpr (PAIRS) return exponents.columns(batch, col);
+        else return {};
+    }
+    __device__ __forceinline__ static Factors factors(const Columns& q)
+    {
+        if constexpr (PAIRS) return Exponents::factors(q);
+        else return {};
+    }
+    __device__ __forceinline__ void eight(float (&v)[8], const Ahead& now, const Factors& f, int batch, int row, int col, int left) const
+    {
+        if constexpr (PAIRS) Exponents::eight(v, f, now.row);
+        rows(batch).eight(v, now.old, row, col, left);
     }
     __device__ __forceinline__ void one(float v, int batch, int row, int col) const
     {
-        float e, f;
-        exponents.factors(e, f);
-        rows(batch).one(v * e * f, row, col);
+        if constexpr (PAIRS) v = exponents.one(v, batch, row, col);
+        rows(batch).one(v, row, col);
     }
 };
 
@@ -258,8 +299,8 @@ inline bool rows_on_16(const void* p, int64_t ld, int64_t rows, int64_t node, in
 }
 
 // The sums of a product left in parts: [batch][part][m][ld], added in the order of k.  A thread takes eight columns.
-template <class T>
-__global__ void __launch_bounds__(256) sum_parts_kernel(const float* sums, int parts, int m, int n, int64_t ld, int64_t chunks, const __grid_constant__ StoreRows<T> out)
+template <class T, bool PAIRS>
+__global__ void __launch_bounds__(256) sum_parts_kernel(const float* sums, int parts, int m, int n, int64_t ld, int64_t chunks, const __grid_constant__ StoreRows<T, PAIRS> out)
 {
     grid_launch_dependents();
     grid_dependency_wait();
@@ -267,7 +308,7 @@ __global__ void __launch_bounds__(256) sum_parts_kernel(const float* sums, int p
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < chunks; i += (int64_t)gridDim.x * 256) {
         const int64_t r = i / per;
         const int col = (int)(i - r * per) * 8, batch = (int)(r / m), row = (int)(r - (int64_t)batch * m);
-        Raw<T> old;
+        typename StoreRows<T, PAIRS>::Ahead old;
         if (out.wide()) out.load(old, batch, row, col, n - col);
         const float* from = sums + ((int64_t)batch * parts * m + row) * ld + col;
         float v[8] = {};
@@ -279,7 +320,7 @@ __global__ void __launch_bounds__(256) sum_parts_kernel(const float* sums, int p
             for (int k = 0; k < 8; ++k) v[k] += z[k];
         }
         if (out.wide()) {
-            out.eight(v, old, batch, row, col, n - col);
+            out.eight(v, old, out.factors(out.columns(batch, col)), batch, row, col, n - col);
         } else {
 #pragma unroll
             for (int k = 0; k < 8; ++k)
@@ -308,7 +349,7 @@ int64_t parts_bytes(int64_t m, int64_t n, int64_t k, int64_t batch, int pairs, i
 template <class T, int P>
 cudaError_t store_product(const GemmPlan& g, const Matrix& out, int64_t rows, const Matrix* second, bool accumulate, const Exponents& exponents, float* sums, cudaStream_t stream)
 {
-    StoreRows<T> e;
+    StoreRows<T, P == 2> e;
     e.exponents = exponents;
     const Matrix& o2 = second ? *second : out;
     e.out[0] = static_cast<T*>(out.p);
@@ -324,7 +365,6 @@ cudaError_t store_product(const GemmPlan& g, const Matrix& out, int64_t rows, co
     if (parts == 1) return launch_gemm<P>(g, e, stream);
     StoreRows<float> to;
     const int64_t ld = (g.n + 7) / 8 * 8, chunks = g.batch * g.m * (ld / 8);
-    to.exponents = Exponents();
     to.out[0] = to.out[1] = sums;
     to.ld[0] = to.ld[1] = ld;
     to.node[0] = to.node[1] = g.m * ld;
@@ -334,7 +374,7 @@ cudaError_t store_product(const GemmPlan& g, const Matrix& out, int64_t rows, co
     const cudaError_t r = launch_gemm_as<Variant<2, 256, P, 8, false, true>>(g, parts, 0, 0, to, stream);
     if (r != cudaSuccess) return r;
     const dim3 blocks((unsigned)std::min<int64_t>((chunks + 255) / 256, (int64_t)sm_count() * 8));
-    return launch_after_trigger(sum_parts_kernel<T>, blocks, dim3(256), 0, stream, true, sums, parts, (int)g.m, (int)g.n, ld, chunks, e);
+    return launch_after_trigger(sum_parts_kernel<T, P == 2>, blocks, dim3(256), 0, stream, true, sums, parts, (int)g.m, (int)g.n, ld, chunks, e);
 }
 
 }  // namespace gpga

@@ -67,14 +67,13 @@ cudaError_t forward(const FeedForwardParams& p, cudaStream_t stream)
     return store_product<T, P>(g, p.y, p.nodes * p.rows, nullptr, false, Exponents(), q.sums, stream);
 }
 
-// fp32 as pairs of fp16.
+// fp32 as pairs of fp16: no row of x, gate, up, h or down is summed over, so each has a power of two of its own.
 struct PairsPlan {
     PackPlan in, between;
     Operand x, gate, up, down, h;
     float *hf, *sums;
     int64_t ldh, bytes;
-    uint32_t *parts, *peaks;     // of x, gate, up, down (kPeakParts each); of h and nothing
-    int32_t* exponents;          // of x, gate and up, up again, down, h
+    int8_t *of_x, *of_gate, *of_up, *of_down, *of_h;    // exponents
 };
 
 PairsPlan plan_pairs(const FeedForwardParams& p)
@@ -82,34 +81,31 @@ PairsPlan plan_pairs(const FeedForwardParams& p)
     PairsPlan q;
     q.in.base = q.between.base = p.scratch;
     q.in.pieces = q.between.pieces = 2;
-    ScratchPlan& s = q.in.scratch;
-    q.parts = reinterpret_cast<uint32_t*>(p.scratch + s.take(4 * kPeakParts * 4));
-    q.peaks = reinterpret_cast<uint32_t*>(p.scratch + s.take(8));
-    q.exponents = reinterpret_cast<int32_t*>(p.scratch + s.take(5 * 4));
+    q.in.by = q.between.by = PackPlan::kRows;
     q.x = q.in.operand(p.x.p, p.x.ld, p.rows * p.x.ld, p.rows, p.d, p.nodes, true, false, 2);
-    q.in.scaled(q.parts, kPeakParts, q.exponents);
+    q.of_x = q.in.powers();
     q.gate = q.in.operand(p.gate.p, p.gate.ld, p.gate.node, p.f, p.d, p.nodes, true, false, 2);
-    q.in.scaled(q.parts + kPeakParts, 2 * kPeakParts, q.exponents + 1);   // one power for both
+    q.of_gate = q.in.powers();
     q.up = q.in.operand(p.up.p, p.up.ld, p.up.node, p.f, p.d, p.nodes, true, false, 2);
-    q.in.scaled(q.parts + kPeakParts, 2 * kPeakParts, q.exponents + 2);
+    q.of_up = q.in.powers();
     q.down = q.in.operand(p.down.p, p.down.ld, p.down.node, p.d, p.f, p.nodes, true, false, 2);
-    q.in.scaled(q.parts + 3 * kPeakParts, kPeakParts, q.exponents + 3);
-    q.ldh = (p.f + 7) / 8 * 8;
+    q.of_down = q.in.powers();
+    ScratchPlan& s = q.between.scratch;
+    s = q.in.scratch;
+    q.ldh = padded(p.f);
     q.hf = reinterpret_cast<float*>(p.scratch + s.take(p.nodes * p.rows * q.ldh * 4));
-    q.between.scratch = s;
     q.h = q.between.operand(q.hf, q.ldh, p.rows * q.ldh, p.rows, p.f, p.nodes, true, false, 2);
-    q.between.scaled(q.peaks, 1, q.exponents + 4);
-    ScratchPlan all = q.between.scratch;
-    q.sums = reinterpret_cast<float*>(p.scratch + all.take(parts_bytes<2>(p.rows, p.d, p.f, p.nodes, 1, 2)));
-    q.bytes = all.bytes;
+    q.of_h = q.between.powers();
+    q.sums = reinterpret_cast<float*>(p.scratch + s.take(parts_bytes<2>(p.rows, p.d, p.f, p.nodes, 1, 2)));
+    q.bytes = s.bytes;
     return q;
 }
 
 cudaError_t forward_pairs(const FeedForwardParams& p, cudaStream_t stream)
 {
     const PairsPlan q = plan_pairs(p);
-    cudaError_t e = q.in.launch_peaks(q.parts, q.peaks, stream);
-    if (e == cudaSuccess) e = q.in.launch<__half>(stream);
+    const int32_t nodes = (int32_t)p.nodes;
+    cudaError_t e = q.in.launch_rows(false, nullptr, 0, stream);
     if (e != cudaSuccess) return e;
     GemmPlan g;
     g.half = true;
@@ -127,20 +123,20 @@ cudaError_t forward_pairs(const FeedForwardParams& p, cudaStream_t stream)
     up.ldg = p.g.ld;
     up.ldu = p.u.ld;
     up.h = {q.hf, q.ldh, p.rows * q.ldh};
-    up.exponents = {q.exponents, q.exponents + 1};
-    up.peaks = q.peaks;
+    up.of_g = {q.of_x, q.of_gate, padded(p.rows), padded(p.f), nodes};
+    up.of_u = {q.of_x, q.of_up, padded(p.rows), padded(p.f), nodes};
     up.m = (int32_t)p.rows;
     up.kind = p.activation;
     up.keeps = p.g.p != nullptr;
     up.vec = !up.keeps || (rows_on_16(p.g.p, p.g.ld, p.nodes * p.rows, 0, 1, 4) && rows_on_16(p.u.p, p.u.ld, p.nodes * p.rows, 0, 1, 4));
     e = launch_gemm<2>(g, up, stream);
-    if (e == cudaSuccess) e = q.between.launch<__half>(stream);
+    if (e == cudaSuccess) e = q.between.launch_rows(true, nullptr, 0, stream);
     if (e != cudaSuccess) return e;
     g.a[0] = q.h;
     g.b[0] = q.down;
     g.n = p.d;
     g.k = p.f;
-    return store_product<float, 2>(g, p.y, p.nodes * p.rows, nullptr, false, {q.exponents + 4, q.exponents + 3}, q.sums, stream);
+    return store_product<float, 2>(g, p.y, p.nodes * p.rows, nullptr, false, {q.of_h, q.of_down, padded(p.rows), padded(p.d), nodes}, q.sums, stream);
 }
 
 }  // namespace

@@ -328,16 +328,16 @@ constexpr int kFewRegisters = 64, kManyRegisters = 208;
 
 // Epi, for a product's row and column (bounds are the kernel's care; `left` columns are there from col on):
 //   Ahead, load(ahead, batch, row, col, left): what is read of eight columns ahead of their sums;
-//   eight(v, ahead, batch, row, col, left): eight columns.  wide() false: one(v, batch, row, col) is called instead;
-//   kDual: eight(v, w, batch, row, col, left), v of the first array's columns, w of the second's.  wide() false: keep(which, v,
+//   Columns, columns(batch, col): what is read once for the rows of eight columns; Factors, factors(columns): what becomes of it;
+//   eight(v, ahead, factors, batch, row, col, left): eight columns.  wide() false: one(v, batch, row, col) is called instead;
+//   kDual: scale(v, factors(columns(which, batch, col)), row(batch, row)) of each array, then eight(v, w, batch, row, col, left), v of the first array's columns, w of the second's.  wide() false: keep(which, v,
 //   batch, row, col) is called first for every single value.
-//   kPeaks: largest values that the block notes (block_peaks) and adds to those at `peaks` in the end.
 //   kPair: 16-bit values that are read and stored pass in whole lines of 64 columns, two warps together (wide() is true).
 //   kTail: microseconds of 128 x 256 columns, for the choice of the variant.
 //   kMirror: eight() leaves in v what it has stored; put(v, batch, row, col) stores it again at its mirror place.
 // The loops over eight columns are kept rolled: a warp goes through an epilogue once per tile, and unrolled it waits for
 // instructions (an epilogue with the activation and its slopes in fp32, 2048 x 2048 values: 147 us unrolled, 60 us rolled).
-struct NothingAhead {};
+struct Nothing {};
 
 // The kernel's shared memory from the first 1024-byte boundary on.
 __device__ __forceinline__ unsigned char* gemm_shared()
@@ -345,8 +345,6 @@ __device__ __forceinline__ unsigned char* gemm_shared()
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     return smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
 }
-// The block's largest values so far (room for two arrays); the kernel adds them to the call's when it ends.
-__device__ __forceinline__ uint32_t* block_peaks() { return reinterpret_cast<uint32_t*>(gemm_shared() + 176); }
 
 // A SPLIT tile's sums: eight columns after eight columns (the block that finishes them has them one after the other), 128 rows of
 // 32 bytes and 64 bytes between; the halves of a row change places every four rows, for the banks.
@@ -374,7 +372,7 @@ __global__ void __launch_bounds__(V::threads, 1)
 {
     unsigned char* const smem = gemm_shared();
     const uint32_t base = smem_u32(smem);
-    // head: full[8], empty[8], acc_full[2], acc_empty[2], tensor memory address, stop flag, SPLIT's copies, block_peaks
+    // head: full[8], empty[8], acc_full[2], acc_empty[2], tensor memory address, stop flag, SPLIT's copies
     const uint32_t full = base, empty = base + 64, acc_full = base + 128, acc_empty = base + 144;
     uint32_t* const tmem_at = reinterpret_cast<uint32_t*>(smem + 160);
     volatile uint32_t* const stop = reinterpret_cast<volatile uint32_t*>(smem + 164);
@@ -415,7 +413,6 @@ __global__ void __launch_bounds__(V::threads, 1)
             mbar_init(reinterpret_cast<uint64_t*>(smem + 144 + 8 * i), V::warps * CG);
         }
         *stop = 0;
-        for (int i = 0; i < Epi::kPeaks; ++i) block_peaks()[i] = 0;
         if constexpr (SPLIT) {
             mbar_init(copies, 1);
             if (p.splits > 1) mbar_arrive_expect_tx(copies, (p.splits - 1) * (16 / p.splits) * kSplitChunk);
@@ -573,11 +570,14 @@ __global__ void __launch_bounds__(V::threads, 1)
                         for (int r = 0; r < min(rows, 32); ++r) epi.one(staged1(stage, r, lane), g.batch, row0 + r, col0 + lane);
                     return;
                 }
+                const int c = col0 + lane_col;
+                typename Epi::Factors factors{};
+                if (c < p.n) factors = epi.factors(epi.columns(g.batch, c));
 #pragma unroll 1
                 for (int i = 0; i < 4; i += kAhead) {
 #pragma unroll
                     for (int j = 0; j < kAhead; ++j) {
-                        const int r = (i + j) * kRows + lane_row, c = col0 + lane_col;
+                        const int r = (i + j) * kRows + lane_row;
                         const typename Epi::Ahead now = ahead[j];
                         const bool here = i + kAhead < 4;
                         const int nr = here ? r + kRows * kAhead : j * kRows + lane_row, nc = here ? c : c + kColumns;
@@ -588,7 +588,7 @@ __global__ void __launch_bounds__(V::threads, 1)
                                 pair_staged8(stage, r, lane_col, v);
                             else
                                 staged8(stage, r, lane_col, v);
-                            epi.eight(v, now, g.batch, row0 + r, c, p.n - c);
+                            epi.eight(v, now, factors, g.batch, row0 + r, c, p.n - c);
                             if constexpr (Epi::kMirror)
                                 if (mirror) stage8(stage, r, lane_col, v);
                         }
@@ -616,6 +616,18 @@ __global__ void __launch_bounds__(V::threads, 1)
                             epi.load(ahead[j], g.batch, row0 + j * kRows + lane_row, from + lane_col, p.n - from - lane_col);
             };
             // The same of two arrays.
+            typename Epi::Columns columns2[2] = {};     // of the 32 columns that are next, of each array
+            int own[4] = {};
+            const auto start2 = [&](int col0) {
+                if constexpr (Epi::kDual) {
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+                        if (col0 + lane_col < p.n) columns2[q] = epi.columns(q, g.batch, col0 + lane_col);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (i * 8 + lane_row < rows) own[i] = epi.row(g.batch, row0 + i * 8 + lane_row);
+                }
+            };
             const auto block2 = [&](const float(&a)[32], const float(&b)[32], int col0) {
                 if constexpr (Epi::kDual) {
                 stage_rows(a, stage, lane);
@@ -623,17 +635,25 @@ __global__ void __launch_bounds__(V::threads, 1)
 #pragma unroll 1
                     for (int r = 0; r < min(rows, 32); ++r) epi.keep(0, staged1(stage, r, lane), g.batch, row0 + r, col0 + lane);
                 float v[4][8];
+                {
+                    const auto factors = epi.factors(columns2[0]);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) staged8(stage, i * 8 + lane_row, lane_col, v[i]);
+                    for (int i = 0; i < 4; ++i) {
+                        staged8(stage, i * 8 + lane_row, lane_col, v[i]);
+                        epi.scale(v[i], factors, own[i]);
+                    }
+                }
                 stage_rows(b, stage, lane);
                 if (!epi.wide() && col0 + lane < p.n)
 #pragma unroll 1
                     for (int r = 0; r < min(rows, 32); ++r) epi.keep(1, staged1(stage, r, lane), g.batch, row0 + r, col0 + lane);
+                const auto factors = epi.factors(columns2[1]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int r = i * 8 + lane_row, c = col0 + lane_col;
                     float w[8];
                     staged8(stage, r, lane_col, w);
+                    epi.scale(w, factors, own[i]);
                     if (r < rows && c < p.n) epi.eight(v[i], w, g.batch, row0 + r, c, p.n - c);
                 }
                 }
@@ -645,6 +665,7 @@ __global__ void __launch_bounds__(V::threads, 1)
                 for (int j = 0; j < slabs; ++j)
 #pragma unroll
                     for (int i = 0; i < 32; ++i) acc[j][i] = 0.f;
+                if constexpr (!SPLIT) start2(from);
                 for (int k0 = 0; k0 < kb_count; k0 += V::chunk, ++sums) {
                     const uint32_t buf = sums & 1;
                     ok = __all_sync(~0u, w.wait(acc_full + 8 * buf, (sums / 2) & 1));
@@ -677,6 +698,7 @@ __global__ void __launch_bounds__(V::threads, 1)
                     const int col0 = from + 32 * j;
                     if (col0 >= p.n) break;
                     if constexpr (Epi::kDual) {
+                        if (j) start2(col0);
                         float a[32], b[32];
 #pragma unroll
                         for (int q = 0; q < slabs / 2; ++q)
@@ -719,6 +741,7 @@ __global__ void __launch_bounds__(V::threads, 1)
                     }
                     if (rows <= 0 || col0 >= p.n) continue;
                     if constexpr (Epi::kDual) {
+                        start2(col0);
                         block2(a, b, col0);
                     } else {
                         if constexpr (PAIR)
@@ -779,13 +802,15 @@ __global__ void __launch_bounds__(V::threads, 1)
                                 epi.keep(0, v[k], g.batch, r, col + k);
                                 epi.keep(1, x[k], g.batch, r, col + k);
                             }
+                    epi.scale(v, epi.factors(epi.columns(0, g.batch, col)), epi.row(g.batch, r));
+                    epi.scale(x, epi.factors(epi.columns(1, g.batch, col)), epi.row(g.batch, r));
                     epi.eight(v, x, g.batch, r, col, left);
                 } else {
                     typename Epi::Ahead ahead;
                     if (epi.wide()) epi.load(ahead, g.batch, r, col, left);
                     total(chunk, row, v);
                     if (epi.wide()) {
-                        epi.eight(v, ahead, g.batch, r, col, left);
+                        epi.eight(v, ahead, epi.factors(epi.columns(g.batch, col)), g.batch, r, col, left);
                     } else {
 #pragma unroll
                         for (int k = 0; k < 8; ++k)
@@ -817,8 +842,6 @@ __global__ void __launch_bounds__(V::threads, 1)
     // Everybody is done, or has given up; copies in flight must land before the block goes.
     tmem_fence_before();
     __syncthreads();
-    if constexpr (Epi::kPeaks > 0)
-        if (threadIdx.x < Epi::kPeaks) atomicMax(epi.peaks + threadIdx.x, block_peaks()[threadIdx.x]);
     if (*stop && threadIdx.x == 0)
         for (uint32_t i = loaded > stages ? loaded - stages : 0; i < loaded; ++i)
             for (uint32_t tries = 0; tries < 4096 && !try_wait(full + 8 * (i % stages), (i / stages) & 1); ++tries) {

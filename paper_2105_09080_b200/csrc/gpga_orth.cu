@@ -116,8 +116,9 @@ template <int P>
 struct KeepPieces {
     static constexpr bool kDual = false, kMirror = true, kPair = false;
     static constexpr double kTail = 1.0;
-    static constexpr int kPeaks = 0;
     static constexpr int kWarps = 8;
+    using Columns = Nothing;
+    using Factors = Nothing;
     struct Ahead {
         Raw<__half> r[P];
     };
@@ -128,11 +129,13 @@ struct KeepPieces {
 
     __device__ __forceinline__ bool wide() const { return true; }
     __device__ __forceinline__ void one(float, int, int, int) const {}
+    __device__ __forceinline__ Columns columns(int, int) const { return {}; }
+    __device__ __forceinline__ static Factors factors(const Columns&) { return {}; }
     __device__ __forceinline__ void load(Ahead& ahead, int batch, int row, int col, int) const
     {
         if (with_r) r.template load<P>(batch, row, col, ahead.r);
     }
-    __device__ __forceinline__ void eight(float (&v)[8], const Ahead& now, int batch, int row, int col, int) const
+    __device__ __forceinline__ void eight(float (&v)[8], const Ahead& now, const Factors&, int batch, int row, int col, int) const
     {
         float a = factor;
         if (power) {
@@ -163,9 +166,10 @@ template <class T>
 struct LastStep {
     static constexpr bool kDual = false, kMirror = false, kPair = false;
     static constexpr double kTail = 1.0;
-    static constexpr int kPeaks = 0;
     static constexpr int kWarps = 8;
     using Ahead = Raw<T>;
+    using Columns = Nothing;
+    using Factors = Nothing;
     T* out;
     int64_t ld, node;
     const float* kappa;
@@ -178,7 +182,9 @@ struct LastStep {
         return {out + batch * node, ld, power ? factor * kappa[batch] : factor, accumulate != 0};
     }
     __device__ __forceinline__ void load(Ahead& old, int batch, int row, int col, int left) const { rows(batch).ahead(old, row, col, left); }
-    __device__ __forceinline__ void eight(float (&v)[8], const Ahead& old, int batch, int row, int col, int left) const
+    __device__ __forceinline__ Columns columns(int, int) const { return {}; }
+    __device__ __forceinline__ static Factors factors(const Columns&) { return {}; }
+    __device__ __forceinline__ void eight(float (&v)[8], const Ahead& old, const Factors&, int batch, int row, int col, int left) const
     {
         rows(batch).eight(v, old, row, col, left);
     }

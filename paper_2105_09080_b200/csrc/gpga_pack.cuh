@@ -4,28 +4,34 @@
 
 namespace gpga {
 
+// fp32 as pairs of fp16 values: times powers of two, one for each row or (where rows are summed over) for each column of a matrix,
+// so that what is far larger elsewhere takes no bits from it.
 struct PackJob {
     const void* src;
     int64_t ld, batch;        // of the source, in elements
     int64_t rows, cols, batches;
     int64_t chunks;           // ceil(cols / 8)
-    int64_t first;            // first of the launch's chunks that belongs to this job
+    int64_t first;            // first of the launch's units that belongs to this job
     int vec;                  // every source row starts on 16 bytes
     int src_f32;              // otherwise the type of the pieces
     int pieces;
     void* dst;
     int64_t dst_piece;
-    // Where the pieces are of the source times a power of two: bits of the largest values of its parts, and where the power's
-    // exponent goes, negated.
-    const uint32_t* peaks;
-    int peak_count;
-    int32_t* exponent;
+    int8_t* exponents;        // of the powers, negated: [batch][rows, padded to eight], or [batch][8 chunks]
+    uint32_t* peaks;          // by columns: bits of their largest finite values, [batch][8 chunks]
 };
 constexpr int kPackJobs = 5;
 struct PackJobs {
     PackJob job[kPackJobs];
     int count;
-    int64_t chunks;
+    int slice;                // by columns: rows of a unit
+    int64_t units;            // chunks; rows; or pieces of `slice` rows by 32 chunks
+    __device__ __forceinline__ const PackJob& of(int64_t unit) const
+    {
+        int i = 0;
+        while (i + 1 < count && unit >= job[i + 1].first) ++i;
+        return job[i];
+    }
 };
 
 __device__ __forceinline__ void pack_load(const PackJob& j, int64_t c, float (&v)[8])
@@ -37,41 +43,17 @@ __device__ __forceinline__ void pack_load(const PackJob& j, int64_t c, float (&v
     x.values(v);
 }
 
-// Largest finite value of an array, as bits.
+__host__ __device__ constexpr int64_t padded(int64_t n) { return (n + 7) / 8 * 8; }
+
+// Bits of |v|, 0 for infinities and NaN.
 __device__ __forceinline__ uint32_t finite_bits(float v)
 {
     const uint32_t b = __float_as_uint(v) & 0x7FFFFFFFu;
     return b < 0x7F800000u ? b : 0;
 }
-constexpr int kPeakParts = 128;   // blocks per array
-
-// Block x of job y: its part of the array.  `cleared`: peaks that a product of the call will find.
-template <int PARTS>
-__global__ void __launch_bounds__(256) peak_kernel(const __grid_constant__ PackJobs jobs, uint32_t* parts, uint32_t* cleared)
-{
-    const PackJob& j = jobs.job[blockIdx.y];
-    const int64_t count = j.batches * j.rows * j.chunks;
-    uint32_t peak = 0;
-#pragma unroll 4
-    for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < count; c += PARTS * 256) {
-        float v[8];
-        pack_load(j, c, v);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) peak = max(peak, finite_bits(v[k]));
-    }
-    peak = __reduce_max_sync(~0u, peak);
-    __shared__ uint32_t warps[8];
-    if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = peak;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int i = 1; i < 8; ++i) peak = max(peak, warps[i]);
-        parts[blockIdx.y * PARTS + blockIdx.x] = peak;
-        if (blockIdx.x == 0 && blockIdx.y == 0) cleared[0] = cleared[1] = 0;
-    }
-}
-
-// Exponent of the power of two that brings the largest value to 2^14 .. 2^15; an array of zeros stays as it is.
-__device__ __forceinline__ int scale_exponent(uint32_t peak) { return peak ? min(14 + 127 - (int)(peak >> 23), 120) : 0; }
+// Exponent of the power of two that brings the largest value to 2^14 .. 2^15 (as near as fp32 has one); zeros stay as they are.
+__device__ __forceinline__ int scale_exponent(uint32_t peak) { return peak ? min(14 + 127 - (int)(peak >> 23), 125) : 0; }
+__device__ __forceinline__ float power_of_two(int e) { return __int_as_float((e + 127) << 23); }
 
 // A thread takes a chunk of eight columns: one pass over the source, bound by memory (fp32 to three pieces: 4 bytes read,
 // 6 written per value).
@@ -79,33 +61,12 @@ template <class T16>
 __global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackJobs jobs)
 {
     grid_launch_dependents();
-    __shared__ float scale[kPackJobs];
-    if (jobs.job[0].peaks) {
-        const int i = threadIdx.x >> 5;
-        if (i < jobs.count) {
-            const PackJob& j = jobs.job[i];
-            uint32_t peak = 0;
-            for (int k = threadIdx.x & 31; k < j.peak_count; k += 32) peak = max(peak, j.peaks[k]);
-            peak = __reduce_max_sync(~0u, peak);
-            const int e = scale_exponent(peak);
-            if ((threadIdx.x & 31) == 0) {
-                scale[i] = __int_as_float((e + 127) << 23);
-                if (blockIdx.x == 0) *j.exponent = -e;
-            }
-        }
-        __syncthreads();
-    }
-    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < jobs.chunks; at += (int64_t)gridDim.x * 256) {
-        int i = 0;
-        while (i + 1 < jobs.count && at >= jobs.job[i + 1].first) ++i;
-        const PackJob& j = jobs.job[i];
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < jobs.units; at += (int64_t)gridDim.x * 256) {
+        const PackJob& j = jobs.of(at);
         const int64_t c = at - j.first;
         float v[8];
         if (j.src_f32) {
             pack_load(j, c, v);
-            if (j.peaks)
-#pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] *= scale[i];
         } else {
             const int64_t row = c / j.chunks, b = row / j.rows, r = row - b * j.rows;
             const int col = (int)(c - row * j.chunks) * 8;
@@ -123,6 +84,172 @@ __global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackJ
     }
 }
 
+namespace {
+
+// fp32 rows to pairs, a power of two for each row.  A warp takes a row: it holds 2048 columns, so that they are read once; of
+// longer rows the rest comes from L2 again.  cleared: 16-byte words that later launches find zero.
+constexpr int kHeldChunks = 8;
+__global__ void __launch_bounds__(256) pack_rows_kernel(const __grid_constant__ PackJobs jobs, uint4* cleared, int64_t clear)
+{
+    grid_launch_dependents();
+    grid_dependency_wait();
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < clear; i += (int64_t)gridDim.x * 256) cleared[i] = make_uint4(0, 0, 0, 0);
+    const int lane = threadIdx.x & 31;
+    for (int64_t at = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); at < jobs.units; at += (int64_t)gridDim.x * 8) {
+        const PackJob& j = jobs.of(at);
+        const int64_t row = at - j.first, b = row / j.rows, r = row - b * j.rows;
+        const float* const from = static_cast<const float*>(j.src) + b * j.batch + r * j.ld;
+        const int chunks = (int)j.chunks, cols = (int)j.cols;
+        Raw<float> held[kHeldChunks];
+        uint32_t peak = 0;
+        const auto largest = [&](const Raw<float>& x) {
+            float v[8];
+            x.values(v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) peak = max(peak, finite_bits(v[k]));
+        };
+#pragma unroll
+        for (int q = 0; q < kHeldChunks; ++q) {
+            const int c = lane + 32 * q;
+            if (c < chunks) held[q].load(from + 8 * c, cols - 8 * c, j.vec);
+        }
+#pragma unroll
+        for (int q = 0; q < kHeldChunks; ++q)
+            if (lane + 32 * q < chunks) largest(held[q]);
+        for (int c = lane + 32 * kHeldChunks; c < chunks; c += 32) {
+            Raw<float> x;
+            x.load(from + 8 * c, cols - 8 * c, j.vec);
+            largest(x);
+        }
+        const int e = scale_exponent(__reduce_max_sync(~0u, peak));
+        const float scale = power_of_two(e);
+        if (lane == 0) j.exponents[b * padded(j.rows) + r] = (int8_t)-e;
+        const Pieces<__half> dst{static_cast<__half*>(j.dst) + row * chunks * 8, j.dst_piece, 0, 0};
+        const auto put = [&](const Raw<float>& x, int c) {
+            float v[8];
+            x.values(v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] *= scale;
+            dst.template store_at<2>(8 * c, v);
+        };
+#pragma unroll
+        for (int q = 0; q < kHeldChunks; ++q)
+            if (lane + 32 * q < chunks) put(held[q], lane + 32 * q);
+        for (int c = lane + 32 * kHeldChunks; c < chunks; c += 32) {
+            Raw<float> x;
+            x.load(from + 8 * c, cols - 8 * c, j.vec);
+            put(x, c);
+        }
+    }
+}
+
+// Where a thread of a block is in a unit of `slice` rows by 32 chunks (fewer where rows are shorter; a power of two of threads
+// lies along a row): chunk `chunk`, if the row has it, of the rows first + group, first + group + step, ... below end.
+struct StripPlace {
+    int64_t batch, first, end;
+    int lanes, chunk, strip, group, step;
+};
+__device__ __forceinline__ StripPlace strip_place(int64_t unit, int64_t rows, int64_t chunks, int slice)
+{
+    StripPlace s;
+    const int64_t strips = (chunks + 31) / 32, slices = (rows + slice - 1) / slice, t = unit / strips;
+    s.strip = (int)(unit - t * strips);
+    s.batch = t / slices;
+    s.lanes = chunks > 16 ? 32 : chunks > 8 ? 16 : chunks > 4 ? 8 : chunks > 2 ? 4 : (int)chunks;
+    s.chunk = s.strip * 32 + (threadIdx.x & (s.lanes - 1));
+    s.first = (t - s.batch * slices) * slice;
+    s.group = threadIdx.x / s.lanes;
+    s.step = 256 / s.lanes;
+    s.end = min(s.first + slice, rows);
+    return s;
+}
+// Rows of a unit: enough units for the device, and no more adding up of their largest values than that takes.
+inline int slice_rows(int64_t rows, int64_t chunks, int64_t batches, int sms)
+{
+    int slice = 64;
+    while (slice < 1024 && batches * ((rows + slice - 1) / slice) * ((chunks + 31) / 32) > (int64_t)sms * 16) slice *= 2;
+    return slice;
+}
+
+// Largest finite values of columns, added to what `peaks` holds.
+__global__ void __launch_bounds__(256) column_peaks_kernel(const __grid_constant__ PackJobs jobs)
+{
+    grid_launch_dependents();
+    __shared__ uint32_t peaks[256];
+    for (int64_t at = blockIdx.x; at < jobs.units; at += gridDim.x) {
+        const PackJob& j = jobs.of(at);
+        const StripPlace s = strip_place(at - j.first, j.rows, j.chunks, jobs.slice);
+        peaks[threadIdx.x] = 0;
+        __syncthreads();
+        uint32_t p[8] = {};
+        if (s.chunk < j.chunks) {
+            const float* const from = static_cast<const float*>(j.src) + s.batch * j.batch + 8 * s.chunk;
+            const int left = (int)j.cols - 8 * s.chunk;
+#pragma unroll 4
+            for (int64_t r = s.first + s.group; r < s.end; r += s.step) {
+                Raw<float> x;
+                float v[8];
+                x.load(from + r * j.ld, left, j.vec);
+                x.values(v);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) p[k] = max(p[k], finite_bits(v[k]));
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) atomicMax(&peaks[(threadIdx.x & (s.lanes - 1)) * 8 + k], p[k]);
+        }
+        __syncthreads();
+        if (at == blockIdx.x) grid_dependency_wait();    // the launch before this one clears them and reads what this one reads
+        const int64_t column = s.strip * 256 + threadIdx.x;
+        if (column < j.chunks * 8 && peaks[threadIdx.x]) atomicMax(j.peaks + s.batch * j.chunks * 8 + column, peaks[threadIdx.x]);
+        __syncthreads();
+    }
+}
+
+// Powers of two of eight columns, and their exponents, negated, to `exponents` where there is one to keep them.
+__device__ __forceinline__ void column_scales(const uint32_t* peaks, float (&scale)[8], int8_t* exponents)
+{
+    const uint4 p = reinterpret_cast<const uint4*>(peaks)[0], q = reinterpret_cast<const uint4*>(peaks)[1];
+    const uint32_t peak[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int e = scale_exponent(peak[k]);
+        scale[k] = power_of_two(e);
+        w[k >> 2] |= ((uint32_t)-e & 0xFFu) << (8 * (k & 3));
+    }
+    if (exponents) *reinterpret_cast<uint2*>(exponents) = make_uint2(w[0], w[1]);
+}
+
+// fp32 to pairs, a power of two for each column.
+__global__ void __launch_bounds__(256) pack_columns_kernel(const __grid_constant__ PackJobs jobs)
+{
+    grid_launch_dependents();
+    grid_dependency_wait();
+    for (int64_t at = blockIdx.x; at < jobs.units; at += gridDim.x) {
+        const PackJob& j = jobs.of(at);
+        const StripPlace s = strip_place(at - j.first, j.rows, j.chunks, jobs.slice);
+        if (s.chunk >= j.chunks) continue;
+        float scale[8];
+        const int64_t place = (s.batch * j.chunks + s.chunk) * 8;
+        column_scales(j.peaks + place, scale, s.first == 0 && s.group == 0 ? j.exponents + place : nullptr);
+        const float* const from = static_cast<const float*>(j.src) + s.batch * j.batch + 8 * s.chunk;
+        const int left = (int)j.cols - 8 * s.chunk;
+        const Pieces<__half> dst{static_cast<__half*>(j.dst) + s.batch * j.rows * j.chunks * 8 + 8 * s.chunk, j.dst_piece, 0, 0};
+#pragma unroll 4
+        for (int64_t r = s.first + s.group; r < s.end; r += s.step) {
+            Raw<float> x;
+            float v[8];
+            x.load(from + r * j.ld, left, j.vec);
+            x.values(v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] *= scale[k];
+            dst.template store_at<2>(r * j.chunks * 8, v);
+        }
+    }
+}
+
+}  // namespace
+
 // Scratch handed out from the front, on 256 bytes.
 struct ScratchPlan {
     int64_t bytes = 0;
@@ -136,7 +263,9 @@ struct ScratchPlan {
 
 // An operand that a tiled copy can read: where it lies, or packed into scratch by the launch that `jobs` collects.
 struct PackPlan {
+    enum By { kChunks, kRows, kColumns };
     PackJobs jobs{};
+    By by = kChunks;          // units of the launch; by rows and by columns: pairs times powers of two
     ScratchPlan scratch;
     char* base = nullptr;     // nullptr: only the sizes are wanted
     int pieces = 1;           // of activations
@@ -175,14 +304,14 @@ struct PackPlan {
         j.cols = cols;
         j.batches = batches;
         j.chunks = chunks;
-        j.first = jobs.chunks;
+        j.first = jobs.units;
         j.vec = (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (rows == 1 || ld * size % 16 == 0) && (batches == 1 || batch * size % 16 == 0);
         j.src_f32 = f32;
         j.pieces = pieces;
         j.dst = base + at;
         j.dst_piece = o.piece;
         ++jobs.count;
-        jobs.chunks += batches * rows * chunks;
+        jobs.units += batches * (by == kChunks ? rows * chunks : by == kRows ? rows : (rows + jobs.slice - 1) / jobs.slice * ((chunks + 31) / 32));
         return o;
     }
     // An array of pieces in scratch that a kernel of the call writes.
@@ -200,26 +329,31 @@ struct PackPlan {
         o.base = base + scratch.take(pieces * o.piece * 2);
         return o;
     }
-    // The last operand is packed times a power of two.
-    void scaled(const uint32_t* peaks, int count, int32_t* exponent)
+    // Exponents of the last operand's powers of two.
+    int8_t* powers()
     {
         PackJob& j = jobs.job[jobs.count - 1];
-        j.peaks = peaks;
-        j.peak_count = count;
-        j.exponent = exponent;
-    }
-    cudaError_t launch_peaks(uint32_t* parts, uint32_t* cleared, cudaStream_t stream) const
-    {
-        peak_kernel<kPeakParts><<<dim3(kPeakParts, jobs.count), 256, 0, stream>>>(jobs, parts, cleared);
-        return cudaGetLastError();
+        j.exponents = reinterpret_cast<int8_t*>(base + scratch.take(j.batches * padded(by == kRows ? j.rows : j.cols)));
+        return j.exponents;
     }
     template <class T16>
     cudaError_t launch(cudaStream_t stream) const
     {
         if (!jobs.count) return cudaSuccess;
-        const int64_t blocks = std::min<int64_t>((jobs.chunks + 255) / 256, (int64_t)sm_count() * 8);
+        const int64_t blocks = std::min<int64_t>((jobs.units + 255) / 256, (int64_t)sm_count() * 8);
         pack_kernel<T16><<<(unsigned)blocks, 256, 0, stream>>>(jobs);
         return cudaGetLastError();
+    }
+    // after: the kernel before it on the stream is one of the same call.
+    cudaError_t launch_rows(bool after, void* cleared, int64_t clear_bytes, cudaStream_t stream) const
+    {
+        const dim3 blocks((unsigned)std::min<int64_t>((jobs.units + 7) / 8, (int64_t)sm_count() * 8));
+        return launch_after_trigger(pack_rows_kernel, blocks, dim3(256), 0, stream, after, jobs, static_cast<uint4*>(cleared), clear_bytes / 16);
+    }
+    cudaError_t launch_columns(bool pack, cudaStream_t stream) const
+    {
+        const dim3 blocks((unsigned)std::min<int64_t>(jobs.units, (int64_t)sm_count() * 16));
+        return launch_after_trigger(pack ? pack_columns_kernel : column_peaks_kernel, blocks, dim3(256), 0, stream, true, jobs);
     }
 };
 template <class T16>
