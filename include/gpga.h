@@ -630,7 +630,8 @@ int64_t gpga_layer_norm_scratch_bytes(int64_t nodes, int64_t rows, int64_t d);
  *    among fp32 operands may give NaN in what it reaches.
  *    16-bit operands are taken as they are, fp32 weights beside them as the sum of two values of their type (16 significant bits
  *    for bfloat16; for fp16 22, and 2^-25 at least).  Sums are fp32.  What passes from one product to the next (h, dg, du) has
- *    the activations' type (forward calls of up to eight tokens per node: 16 bits more).
+ *    the activations' type (forward calls of up to eight tokens per node: 16 bits more).  With fp16,
+ *    what passes is infinite from 65520 on; an fp32 weight beside it has 13 bits above 65504 and is infinite from 131024 on.
  *  - Scratch: the _scratch_bytes function of an entry, given the entry's own argument struct (its scratch members are not
  *    looked at), says how much it needs; 0 also where the arguments are wrong.
  *  - Waits inside the kernels are bounded.  One that gives up (which takes seconds and does not happen in a sound run) ends

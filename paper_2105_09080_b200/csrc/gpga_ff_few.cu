@@ -54,7 +54,7 @@ __device__ __forceinline__ void as_pairs(const Raw<W>& r, uint32_t (&o)[Q][4])
         } else {
             const float x = __uint_as_float(r.w[2 * i]), y = __uint_as_float(r.w[2 * i + 1]);
             float a, b;
-            o[0][i] = pack16(x, y, T());
+            o[0][i] = pack16_finite(x, y, T());
             unpack16(o[0][i], a, b, T());
             o[1][i] = pack16(x - a, y - b, T());
         }
@@ -76,7 +76,10 @@ __device__ __forceinline__ void finish(const FewParams& p, int node, int token, 
         const float h = v[0] * b;
         H* const at = static_cast<H*>(p.out) + t * p.ldo + row;
         *at = from_f32<H>(h);
-        if (sizeof(H) == 2 && p.lo) at[p.lo] = from_f32<H>(h - to_f32(*at));
+        if (sizeof(H) == 2 && p.lo) {
+            const float rounded = to_f32(*at);    // no rest beside an infinity: it could be NaN
+            at[p.lo] = from_f32<H>(fabsf(rounded) <= 3.4028234e38f ? h - rounded : 0.f);
+        }
     } else {
         static_cast<T*>(p.out)[t * p.ldo + row] = from_f32<T>(a);
     }

@@ -245,9 +245,25 @@ __device__ __forceinline__ void store8(T* p, int n, const float (&v)[8])
     }
 }
 
+// Rounded to 16 bits as pack16 does, but infinities and what is beyond the range become the largest values: the first of two that
+// stand for one value.  The second has what is left, an infinity too, and so neither makes NaN of the other.
+__device__ __forceinline__ uint32_t pack16_finite(float lo, float hi, __half)
+{
+    uint32_t w;
+    asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
+    return w;
+}
+__device__ __forceinline__ uint32_t pack16_finite(float lo, float hi, __nv_bfloat16)
+{
+    uint32_t w;
+    asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
+    return w;
+}
+
 // Where the pieces of an array of rows are (piece, batch, row, column; rows start on 16 bytes and are padded to eight).
 // bfloat16, P = 3: the upper 16 bits, the upper 16 of the rest, and what is left of it, which has eight significant bits:
-// the sum is exact (an infinity's rest is NaN).  half, P = 2: rounded, then the rounded rest: 22 bits.  P = 1: rounded.
+// the sum is exact (an infinity's rest is NaN).  P = 2: rounded, then the rounded rest: 22 bits of
+// half, 16 of bfloat16.  P = 1: rounded.
 template <class T16>
 struct Pieces {
     T16* base;
@@ -276,7 +292,7 @@ struct Pieces {
                     }
                 }
             } else {
-                w[0][i] = pack16(x, y, T16());
+                w[0][i] = P == 2 ? pack16_finite(x, y, T16()) : pack16(x, y, T16());
                 if constexpr (P == 2) {
                     float hx, hy;
                     unpack16(w[0][i], hx, hy, T16());
