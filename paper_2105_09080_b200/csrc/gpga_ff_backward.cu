@@ -80,7 +80,7 @@ cudaError_t backward(const FeedForwardParams& p, cudaStream_t stream)
     grad.m = (int32_t)p.rows;
     grad.kind = p.activation;
     grad.vec = rows_on_16(p.g.p, p.g.ld, p.nodes * p.rows, 0, 1, sizeof(T)) && rows_on_16(p.u.p, p.u.ld, p.nodes * p.rows, 0, 1, sizeof(T));
-    if ((e = launch_gemm<P>(g, grad, stream)) != cudaSuccess) return e;
+    if ((e = launch_gemm<P, T>(g, grad, stream)) != cudaSuccess) return e;
 
     g.after = true;                     // dWd = dy^T h
     g.a[0] = q.dy;

@@ -362,7 +362,7 @@ cudaError_t store_product(const GemmPlan& g, const Matrix& out, int64_t rows, co
     e.accumulate = accumulate;
     e.vec = rows_on_16(out.p, out.ld, rows, out.node, g.batch, sizeof(T)) && rows_on_16(o2.p, o2.ld, rows, o2.node, g.batch, sizeof(T));
     const int parts = gemm_parts(g, P * (P + 1) / 2, StoreRows<float>::kTail);
-    if (parts == 1) return launch_gemm<P>(g, e, stream);
+    if (parts == 1) return launch_gemm<P, T>(g, e, stream);
     StoreRows<float> to;
     const int64_t ld = (g.n + 7) / 8 * 8, chunks = g.batch * g.m * (ld / 8);
     to.out[0] = to.out[1] = sums;
@@ -371,7 +371,7 @@ cudaError_t store_product(const GemmPlan& g, const Matrix& out, int64_t rows, co
     to.split = INT32_MAX;
     to.accumulate = 0;
     to.vec = 1;
-    const cudaError_t r = launch_gemm_as<Variant<2, 256, P, 8, false, true>>(g, parts, 0, 0, to, stream);
+    const cudaError_t r = launch_gemm_up_to<Variant<2, 256, P, 8, false, true>>(most_kblocks<T>, (gemm_kblocks(g) + parts - 1) / parts, g, parts, 0, 0, to, stream);
     if (r != cudaSuccess) return r;
     const dim3 blocks((unsigned)std::min<int64_t>((chunks + 255) / 256, (int64_t)sm_count() * 8));
     return launch_after_trigger(sum_parts_kernel<T, P == 2>, blocks, dim3(256), 0, stream, true, sums, parts, (int)g.m, (int)g.n, ld, chunks, e);

@@ -57,7 +57,7 @@ cudaError_t forward(const FeedForwardParams& p, cudaStream_t stream)
     up.kind = p.activation;
     up.keeps = p.g.p != nullptr;
     up.vec = !up.keeps || (rows_on_16(p.g.p, p.g.ld, p.nodes * p.rows, 0, 1, sizeof(T)) && rows_on_16(p.u.p, p.u.ld, p.nodes * p.rows, 0, 1, sizeof(T)));
-    e = launch_gemm<P>(g, up, stream);
+    e = launch_gemm<P, T>(g, up, stream);
     if (e != cudaSuccess) return e;
     g.after = true;
     g.a[0] = q.h;
@@ -129,7 +129,7 @@ cudaError_t forward_pairs(const FeedForwardParams& p, cudaStream_t stream)
     up.kind = p.activation;
     up.keeps = p.g.p != nullptr;
     up.vec = !up.keeps || (rows_on_16(p.g.p, p.g.ld, p.nodes * p.rows, 0, 1, 4) && rows_on_16(p.u.p, p.u.ld, p.nodes * p.rows, 0, 1, 4));
-    e = launch_gemm<2>(g, up, stream);
+    e = launch_gemm<2, float>(g, up, stream);
     if (e == cudaSuccess) e = q.between.launch_rows(true, nullptr, 0, stream);
     if (e != cudaSuccess) return e;
     g.a[0] = q.h;

@@ -15,9 +15,11 @@
 // ring of stages, each one piece of A and one of B, 64 deep in k.
 //
 // CHUNKED (operands in pieces, P > 1): the matrix unit cuts what it adds to its fp32 accumulator off, it does not round, so
-// that a sum drifts towards zero by about 2^-26 of itself per instruction (K = 256 in 96 instructions: 1.6e-6 of the
-// result).  Where the result is to be as good as fp32 gives, the sum is cut into chunks of 64 or 128, the small products of
+// that a sum drifts towards zero: by about 2^-26 of itself per instruction where terms have both signs (K = 256 in 96 instructions:
+// 1.6e-6 of the result), by up to 2^-23 of the result where they have one (2^15 terms of 16 bits in 2048 instructions: 2e-4).  Where
+// the result is to be as good as fp32 gives, the sum is cut into chunks of 64 or 128, the small products of
 // a chunk come first, and the epilogue's threads, which then have most of the block's registers, add the chunks' sums.
+// LONG: so do long sums of 16-bit operands, in chunks of 512 (most_kblocks).
 //
 // SPLIT: where there are fewer tiles than SMs, a cluster of blocks takes parts of k of one 128 x 128 tile each.  Every block
 // has a part of the columns to finish: it gets the others' sums for them by bulk copies between shared memories, and adds
@@ -367,19 +369,22 @@ __device__ __forceinline__ unsigned char* gemm_shared()
 constexpr int kSplitChunk = 128 * 32 + 64;
 __device__ __forceinline__ uint32_t split_place(int chunk, int row, int half) { return chunk * kSplitChunk + row * 32 + ((half ^ (row >> 2 & 1)) << 4); }
 
+constexpr int kLongChunk = 8;   // k-blocks
+
 // What a variant of the kernel has: tile columns (of a pair of blocks, where CG = 2), pieces, warps of the epilogue, stages.
 // PARTS: batch b of the epilogue is part b % splits of the sums of batch b / splits.
-template <int CG_, int BN_, int P_, int WARPS_ = 8, bool SPLIT_ = false, bool PARTS_ = false>
+template <int CG_, int BN_, int P_, int WARPS_ = 8, bool SPLIT_ = false, bool PARTS_ = false, bool LONG_ = false>
 struct Variant {
     static constexpr int CG = CG_, BN = BN_, P = P_, warps = WARPS_, threads = 128 + 32 * warps;
-    static constexpr bool chunked = P > 1, split = SPLIT_, parts = PARTS_;
+    static constexpr bool chunked = P > 1 || LONG_, split = SPLIT_, parts = PARTS_;
     static constexpr int staging = split ? 16 * kSplitChunk : warps * kStagingWarp;   // split: the other blocks' sums
     static constexpr bool split_registers = chunked && warps == 8;    // sixteen have few enough sums each
     static_assert(!split || (CG == 1 && BN == 128 && warps == 8), "a SPLIT tile is 128 x 128");
     static constexpr uint32_t a_bytes = 128 * kTileK * 2, b_bytes = BN / CG * kTileK * 2, stage_bytes = a_bytes + b_bytes;
     static constexpr uint32_t room = (kGemmSmem - 1024 - kGemmHead - staging) / stage_bytes;
     static constexpr uint32_t stages = room < 8 ? room : 8;
-    static constexpr int chunk = P == 3 ? 1 : 2;   // k-blocks of a chunk
+    static constexpr int chunk = LONG_ ? kLongChunk : P == 3 ? 1 : 2;   // k-blocks of a chunk
+    using Long = Variant<CG, BN, P, warps, split, parts, P == 1>;
 };
 
 template <class V, class Epi>
@@ -1045,19 +1050,35 @@ inline GemmChoice choose_gemm(const GemmPlan& g, int64_t n, int64_t kblocks, int
 }
 inline int64_t gemm_kblocks(const GemmPlan& g) { return (g.k + kTileK - 1) / kTileK * g.pairs * (g.b[0].pieces - g.a[0].pieces + 1); }
 
+// K-blocks of 16-bit operands that one accumulator may sum, for a result of type T: fp32 a chunk (32 instructions, 2^-18 at worst);
+// 16 bits a sixteenth of the type's half step at worst (bfloat16 1024 instructions, fp16 256).
+template <class T> constexpr int64_t most_kblocks = kLongChunk;
+template <> constexpr int64_t most_kblocks<__nv_bfloat16> = 256;
+template <> constexpr int64_t most_kblocks<__half> = 64;
+
+// V, or where its accumulators (`per` k-blocks each) would sum more than `most`, its LONG form.
+template <class V, class Epi>
+cudaError_t launch_gemm_up_to(int64_t most, int64_t per, const GemmPlan& g, int splits, int64_t tile0, int64_t tile1, const Epi& epi, cudaStream_t stream)
+{
+    if (V::P == 1 && per > most) return launch_gemm_as<typename V::Long>(g, splits, tile0, tile1, epi, stream);
+    return launch_gemm_as<V>(g, splits, tile0, tile1, epi, stream);
+}
+
 // Where whole waves of large tiles leave a few over, those may go to clusters of blocks in a second launch (3 us): X X^T of
 // 8 x 1024 x 2816, fp32, has 80 tiles for 74 pairs of SMs (all five steps of its orthogonalisation: 1378 us without, 1211 us with).
-template <int P, class Epi>
+// T: the type of the result.
+template <int P, class T, class Epi>
 cudaError_t launch_gemm(const GemmPlan& g, const Epi& epi, cudaStream_t stream)
 {
-    const GemmChoice c = choose_gemm(g, Epi::kDual ? 2 * g.n : g.n, gemm_kblocks(g), P * (P + 1) / 2, Epi::kTail);
+    const int64_t kblocks = gemm_kblocks(g), most = most_kblocks<T>;
+    const GemmChoice c = choose_gemm(g, Epi::kDual ? 2 * g.n : g.n, kblocks, P * (P + 1) / 2, Epi::kTail);
     GemmPlan rest = g;
     if (c.large) {
-        const cudaError_t e = launch_gemm_as<Variant<2, 256, P, P <= 2 ? Epi::kWarps : 8>>(g, 1, 0, c.large, epi, stream);
+        const cudaError_t e = launch_gemm_up_to<Variant<2, 256, P, P <= 2 ? Epi::kWarps : 8>>(most, kblocks, g, 1, 0, c.large, epi, stream);
         if (e != cudaSuccess || !c.splits) return e;
         rest.after = true;
     }
-    return launch_gemm_as<Variant<1, 128, P, 8, true>>(rest, c.splits, c.small, 0, epi, stream);
+    return launch_gemm_up_to<Variant<1, 128, P, 8, true>>(most, (kblocks + c.splits - 1) / c.splits, rest, c.splits, c.small, 0, epi, stream);
 }
 
 // Parts that the sums of a product with few large tiles are cut into, so that all pairs of SMs have some; a second launch adds

@@ -548,7 +548,7 @@ cudaError_t orth(const OrthParams& p, cudaStream_t stream)
         keep.beta = keep.diagonal = 0.f;
         keep.power = first ? 2 : 0;
         keep.with_r = 0;
-        if ((e = launch_gemm<P>(g, keep, stream)) != cudaSuccess) return e;
+        if ((e = launch_gemm<P, __half>(g, keep, stream)) != cudaSuccess) return e;
         g.a[0] = g.b[0] = q.a;                          // B = a I + b A + c A A
         g.a[0].mn_major = g.b[0].mn_major = false;
         g.k = s;
@@ -558,7 +558,7 @@ cudaError_t orth(const OrthParams& p, cudaStream_t stream)
         keep.diagonal = (float)(p.c1 * kScale);
         keep.power = 0;
         keep.with_r = 1;
-        if ((e = launch_gemm<P>(g, keep, stream)) != cudaSuccess) return e;
+        if ((e = launch_gemm<P, __half>(g, keep, stream)) != cudaSuccess) return e;
         g.a[0] = tall ? x : q.b;                        // B X or X B
         g.b[0] = tall ? q.b : x;
         g.a[0].mn_major = false;
@@ -572,7 +572,7 @@ cudaError_t orth(const OrthParams& p, cudaStream_t stream)
             keep.factor = 1.f / kScale;
             keep.power = first;
             keep.with_r = 0;
-            if ((e = launch_gemm<P>(g, keep, stream)) != cudaSuccess) return e;
+            if ((e = launch_gemm<P, __half>(g, keep, stream)) != cudaSuccess) return e;
         } else {
             LastStep<T> last;
             last.out = static_cast<T*>(p.out);
@@ -583,7 +583,7 @@ cudaError_t orth(const OrthParams& p, cudaStream_t stream)
             last.power = first;
             last.accumulate = p.accumulate;
             last.vec = on_16(p.out, p.ldo, p.r, p.node_ldo, p.nodes, sizeof(T));
-            if ((e = launch_gemm<P>(g, last, stream)) != cudaSuccess) return e;
+            if ((e = launch_gemm<P, T>(g, last, stream)) != cudaSuccess) return e;
         }
     }
     return cudaSuccess;
