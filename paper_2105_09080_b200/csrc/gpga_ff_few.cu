@@ -100,6 +100,11 @@ __device__ __forceinline__ void ask_ahead(const W* w, int64_t ld, int row0, int 
 }
 
 constexpr int kFewWarps = 8;
+// Terms that the matrix instructions add to one sum (they cut off what they add, see gpga_gemm.cuh): 256 instructions, whose
+// drift is at most a sixteenth of fp16's half step.  LONG: where a warp has more, they are added to its own in fp32 (in a kernel of
+// its own: 24 tokens, 2048 x 5632, fp32 weights 38.4 us, 41.1 us with that in the same loop).
+constexpr int kFewSum = 4096;
+inline bool few_long(int k) { return k > kFewWarps * kFewSum; }
 
 // Sum of value i of every warp of the cluster, in the order of k.  sums: this block's [warp][count].
 __device__ __forceinline__ float cluster_sum(const float* sums, int i, int count, uint32_t blocks)
@@ -118,7 +123,7 @@ __device__ __forceinline__ float cluster_sum(const float* sums, int i, int count
 }
 
 // NT tiles of eight tokens; XP = 2: x is h with the rests of its rounding.
-template <class T, class W, int NT, bool GATE, int XP>
+template <class T, class W, int NT, bool GATE, int XP, bool LONG>
 __global__ void __launch_bounds__(kFewWarps * 32) few_tokens_kernel(const __grid_constant__ FewParams p)
 {
     constexpr int M = GATE ? 2 : 1, R = 16, N = 8 * NT;
@@ -153,7 +158,15 @@ __global__ void __launch_bounds__(kFewWarps * 32) few_tokens_kernel(const __grid
         for (int h = 0; h < 2; ++h) wr[m][h] = w[m] + min(row0 + 8 * h + group, p.rows - 1) * ld[m] + place;
 #pragma unroll
     for (int n = 0; n < NT; ++n) xr[n] = x + min(8 * n + group, p.tokens - 1) * p.ldx + place;
-    float acc[M][NT][4] = {};
+    float acc[M][NT][4] = {}, whole[LONG ? M : 1][NT][4] = {};
+    const auto add_up = [&] {
+#pragma unroll
+        for (int m = 0; m < M; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) whole[LONG ? m : 0][n][e] += acc[m][n][e], acc[m][n][e] = 0.f;
+    };
     const auto multiply = [&](const Raw<W>(&wv)[M][2], const Raw<T>(&xv)[XP][NT]) {
 #pragma unroll
         for (int m = 0; m < M; ++m) {
@@ -192,13 +205,16 @@ __global__ void __launch_bounds__(kFewWarps * 32) few_tokens_kernel(const __grid
 #pragma unroll
             for (int n = 0; n < NT; ++n) xv[z][n].load(xr[n] + z * p.lo + k, left, p.vec_x);
         multiply(wv, xv);
+        if constexpr (LONG)
+            if ((k - k0 + 32) % kFewSum == 0) add_up();
     }
+    if constexpr (LONG) add_up();
 #pragma unroll
     for (int m = 0; m < M; ++m)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sums[((warp * M + m) * N + 8 * n + 2 * (lane & 3) + (e & 1)) * S + 8 * (e >> 1) + group] = acc[m][n][e];
+            for (int e = 0; e < 4; ++e) sums[((warp * M + m) * N + 8 * n + 2 * (lane & 3) + (e & 1)) * S + 8 * (e >> 1) + group] = LONG ? whole[LONG ? m : 0][n][e] : acc[m][n][e];
     cluster_barrier();
     for (int i = (int)rank * kFewWarps * 32 + threadIdx.x; i < R * N; i += p.blocks * kFewWarps * 32) {
         const int r = i % R, n = i / R;
@@ -216,7 +232,7 @@ constexpr int kStreamK = 64;
 template <class W> constexpr int kStreamStages = sizeof(W) == 4 ? 4 : 8;
 template <class W> constexpr int kStreamStage = 16 * kStreamK * (int)sizeof(W);   // bytes
 
-template <class T, class W, int NT, bool GATE, int XP>
+template <class T, class W, int NT, bool GATE, int XP, bool LONG>
 __global__ void __launch_bounds__(kFewWarps * 32) few_streamed_kernel(const __grid_constant__ FewParams p)
 {
     constexpr int N = 8 * NT, S = 16 + 4, stages = kStreamStages<W>, stage_bytes = kStreamStage<W>;
@@ -265,7 +281,13 @@ __global__ void __launch_bounds__(kFewWarps * 32) few_streamed_kernel(const __gr
     int slot = 0, turn = 0;
 #pragma unroll 1
     for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x, turn ^= 1) {
-        float acc[NT][4] = {};
+        float acc[NT][4] = {}, whole[NT][4] = {};
+        const auto add_up = [&] {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) whole[n][e] += acc[n][e], acc[n][e] = 0.f;
+        };
 #pragma unroll 1
         for (int step = 0; step < mine; ++step) {
             const int k0 = (s0 + step) * kStreamK;
@@ -323,12 +345,15 @@ __global__ void __launch_bounds__(kFewWarps * 32) few_streamed_kernel(const __gr
                     }
             }
             __syncwarp();
+            if constexpr (LONG)
+                if ((step + 1) % (kFewSum / kStreamK) == 0) add_up();
         }
+        if constexpr (LONG) add_up();
         float* const here = sums + turn * kFewWarps * N * S;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) here[(warp * N + 8 * n + 2 * quad + (e & 1)) * S + 8 * (e >> 1) + group] = acc[n][e];
+            for (int e = 0; e < 4; ++e) here[(warp * N + 8 * n + 2 * quad + (e & 1)) * S + 8 * (e >> 1) + group] = LONG ? whole[n][e] : acc[n][e];
         __syncthreads();
         constexpr int R = GATE ? 8 : 16;
         for (int i = threadIdx.x; i < R * N; i += kFewWarps * 32) {
@@ -346,11 +371,11 @@ __global__ void __launch_bounds__(kFewWarps * 32) few_streamed_kernel(const __gr
     asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
-template <class T, class W, int NT, bool GATE, int XP = 1>
+template <class T, class W, int NT, bool GATE, int XP, bool LONG>
 cudaError_t launch_streamed(FewParams p, int64_t nodes, cudaStream_t stream)
 {
     constexpr int bytes = kFewWarps * (kStreamStages<W> * kStreamStage<W> + 2 * 8 * NT * 20 * 4);
-    const auto kernel = few_streamed_kernel<T, W, NT, GATE, XP>;
+    const auto kernel = few_streamed_kernel<T, W, NT, GATE, XP, LONG>;
     static std::atomic<unsigned long long> limit_set{0};
     const cudaError_t e = ensure_smem_limit(kernel, bytes, limit_set);
     if (e != cudaSuccess) return e;
@@ -469,15 +494,23 @@ cudaError_t launch_clusters(void (*kernel)(FewParams), FewParams p, int rows, in
     return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
-template <class T, class W, bool GATE>
-cudaError_t few16(const FewParams& p, int64_t nodes, cudaStream_t stream)
+template <class T, class W, bool GATE, bool LONG>
+cudaError_t few16_as(const FewParams& p, int64_t nodes, cudaStream_t stream)
 {
     constexpr int XP = GATE ? 1 : 2;   // up to eight tokens h comes with the rests of its rounding
     if (p.vec_w && p.vec_x)
-        return p.tokens <= 8 ? launch_streamed<T, W, 1, GATE, XP>(p, nodes, stream) : p.tokens <= 16 ? launch_streamed<T, W, 2, GATE>(p, nodes, stream)
-                                                                                                    : launch_streamed<T, W, 4, GATE>(p, nodes, stream);
-    const auto kernel = p.tokens <= 8 ? few_tokens_kernel<T, W, 1, GATE, XP> : p.tokens <= 16 ? few_tokens_kernel<T, W, 2, GATE, 1> : few_tokens_kernel<T, W, 4, GATE, 1>;
+        return p.tokens <= 8    ? launch_streamed<T, W, 1, GATE, XP, LONG>(p, nodes, stream)
+               : p.tokens <= 16 ? launch_streamed<T, W, 2, GATE, 1, LONG>(p, nodes, stream)
+                                : launch_streamed<T, W, 4, GATE, 1, LONG>(p, nodes, stream);
+    const auto kernel = p.tokens <= 8    ? few_tokens_kernel<T, W, 1, GATE, XP, LONG>
+                        : p.tokens <= 16 ? few_tokens_kernel<T, W, 2, GATE, 1, LONG>
+                                         : few_tokens_kernel<T, W, 4, GATE, 1, LONG>;
     return launch_clusters(kernel, p, 16, 32, nodes, stream);
+}
+template <class T, class W, bool GATE>
+cudaError_t few16(const FewParams& p, int64_t nodes, cudaStream_t stream)
+{
+    return few_long(p.k) ? few16_as<T, W, GATE, true>(p, nodes, stream) : few16_as<T, W, GATE, false>(p, nodes, stream);
 }
 
 template <bool GATE>

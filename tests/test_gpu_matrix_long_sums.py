@@ -90,3 +90,27 @@ def test_gram_matrix_of_long_rows():
     want = (z @ z.T) @ z
     e = (got - want) / want
     assert e.mean().abs() <= bound(c, F16) + 2.0 ** -12
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("wtype", [None, F32], ids=["16-bit weights", "fp32 weights"])
+@pytest.mark.parametrize("rows", [4, 12, 24])
+@pytest.mark.parametrize("long", [1 << 20, (1 << 20) - 3], ids=["rows on 16 bytes", "off them"])
+def test_few_tokens_of_long_rows(long, rows, wtype, dtype):
+    """Eight warps of a block take a part of the row each, 2^17 terms; a sum takes 4096 terms, 256 instructions, before it is added to
+    the warp's.  g over a long x; y over a long h, whose values are exact."""
+    wtype = wtype or dtype
+    x, gate = positive((1, rows, long), dtype, 1) * 2.0 ** -5, (positive((1, 40, long), dtype, 2) * 2.0 ** -12).to(wtype)
+    down = torch.zeros((1, long, 40), dtype=wtype, device="cuda")
+    _, g, _ = pkg.feed_forward_forward(x, gate, gate, down, activation="relu")
+    off = 256 * 2.0 ** -23 + (2 ** 17 / 4096 + 18) * 2.0 ** -24
+    held(g, x.double() @ gate.double().mT, off, dtype)
+    del x, gate, down
+    x = torch.zeros((1, rows, 16), dtype=dtype, device="cuda")
+    x[..., 0], x[..., 1] = 1.0, 2.0 ** -8
+    gate, up = (torch.zeros((1, long, 16), dtype=wtype, device="cuda") for _ in range(2))
+    gate[..., 0], up[..., 1] = 1.0, positive((1, long), dtype, 3).to(wtype)
+    down = (positive((1, 16, long), dtype, 4) * 2.0 ** -10).to(wtype)
+    y, *_ = pkg.feed_forward_forward(x, gate, up, down, activation="relu")
+    h = up[..., 1].double() * 2.0 ** -8
+    held(y, (h @ down[0].double().T)[:, None].expand(1, rows, 16), off, dtype)
