@@ -153,16 +153,21 @@ def batch(n, T, vocab, k, seed, device="cuda"):
 
 def train(name, topology, H, n=8, T=512, vocab=256, dim=128, iters=400, every=50, gamma=1.0, p=0.1, seed=20210509, dtype=None,
           hidden=0, update="plain"):
+    from .token_ops import token_status
     m = TokenModel(n, vocab, dim, topology, H, seed, dtype=dtype, hidden=hidden, update=update)
     test = batch(n, 2 * T, vocab, 0, seed + 1)
     traj = []
-    for k in range(iters):
-        loss = m.gradient(k, *batch(n, T, vocab, k, seed), p)
-        m.step(k, gamma)
-        if (k + 1) % every == 0 or k + 1 == iters:
-            traj.append({"k": k + 1, "loss": loss.mean().item(), "average_loss": m.average_loss(*test),
-                         "consensus": m.mixer.consensus_distance()})
-    m.close()
+    try:
+        for k in range(iters):
+            loss = m.gradient(k, *batch(n, T, vocab, k, seed), p)
+            m.step(k, gamma)
+            if (k + 1) % every == 0 or k + 1 == iters:
+                traj.append({"k": k + 1, "loss": loss.mean().item(), "average_loss": m.average_loss(*test),
+                             "consensus": m.mixer.consensus_distance()})
+                if hidden:
+                    token_status()      # the block's products report a wait that gave up here, and only here
+    finally:
+        m.close()
     return {"method": name, "H": H or "inf", "nodes": n, "tokens_per_node": T, "vocab": vocab, "dim": dim, "gamma": gamma,
             "dropout": p, "hidden": hidden, "update": update, "trajectory": traj}
 
