@@ -4,12 +4,13 @@
 //
 // Three products a step: the Gram matrix A, the polynomial B = a I + b A + c A A, and B X.  A and B are symmetric, so every
 // operand is read as it lies.  The matrices are held as S times their value in fp16: with |X| about 1 their entries lie
-// between 1 / columns and a few units, for which fp16 has its full 11 bits (S = 2^11 moves its range down to 2^-25 and
-// leaves 2^5 above one).  fp32 and fp16 updates take two fp16 values for each (22 bits and more) and three products of fp16
-// for one, summed as fp32 would be.  bfloat16 updates of more than 128 rows and columns take one value and one product, a
-// third of the time: the result is off by 1.2 to 1.4 times its own rounding.  Smaller ones, in which the rounding of X on
-// the way weighs more (500 x 33: 2 times), are computed like fp32.  X_0 is M times a power of two (nothing is lost), the
-// rest of the norm, kappa in [1, 2), is a factor in the first step's epilogues.
+// between 1 / columns and a few units, for which fp16 has its full 11 bits.  S = 2^11 for X and B moves its range down to 2^-25
+// and leaves 2^5 above one; A has 2^9, as its entries are up to 64 where singular values are up to 8.  fp32 and fp16 updates take
+// two fp16 values for each (22 bits) and three products of fp16 for one, summed as fp32 would be.  bfloat16 updates of more
+// than 128 rows and columns take one value and one product, a third of the time: the result is off by 1.2 to 1.4 times its own
+// rounding.  Smaller ones, in which the rounding of X on the way weighs more (500 x 33: 2 times), are computed like fp32.
+// X_0 is M times a power of two (nothing is lost, unless the norm is far below eps), the rest of the norm, kappa in [1, 2), is a
+// factor in the first step's epilogues.
 #include "gpga_orth.cuh"
 
 #include <type_traits>
@@ -21,7 +22,7 @@ namespace gpga {
 namespace {
 
 constexpr int GPGA_BF16 = 1;     // the type's code
-constexpr float kScale = 2048.f;
+constexpr float kScale = 2048.f, kGramScale = 512.f;   // of X and B; of A
 constexpr int kSmallSide = 128;
 constexpr int kNormParts = 1024;  // blocks of the sum of squares, over all matrices
 
@@ -410,7 +411,7 @@ __global__ void __launch_bounds__(256, 1) orth_small_kernel(const __grid_constan
             for (int j = 0; j < 32; j += 8) {
                 float o[8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) o[k] = v[j + k] * (1.f / kScale);
+                for (int k = 0; k < 8; ++k) o[k] = v[j + k] * (kGramScale / (kScale * kScale));
                 put8(a, a_piece, row, c + j, o);
             }
         }
@@ -430,7 +431,7 @@ __global__ void __launch_bounds__(256, 1) orth_small_kernel(const __grid_constan
                 float o[8];
                 get8(a, a_piece, row, c + j, o);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) o[k] = p.c5 * (1.f / kScale) * v[j + k] + p.c3 * o[k] + (row == c + j + k ? p.c1 * kScale : 0.f);
+                for (int k = 0; k < 8; ++k) o[k] = p.c5 * (kScale / (kGramScale * kGramScale)) * v[j + k] + p.c3 * (kScale / kGramScale) * o[k] + (row == c + j + k ? p.c1 * kScale : 0.f);
                 put8(a, a_piece, row, c + j, o);
             }
         }
@@ -544,7 +545,7 @@ cudaError_t orth(const OrthParams& p, cudaStream_t stream)
         g.k = std::max(p.r, p.c);
         g.symmetric = true;
         keep.out = keep.r = pieces_of<__half>(q.a);
-        keep.factor = 1.f / kScale;
+        keep.factor = kGramScale / (kScale * kScale);
         keep.beta = keep.diagonal = 0.f;
         keep.power = first ? 2 : 0;
         keep.with_r = 0;
@@ -553,8 +554,8 @@ cudaError_t orth(const OrthParams& p, cudaStream_t stream)
         g.a[0].mn_major = g.b[0].mn_major = false;
         g.k = s;
         keep.out = pieces_of<__half>(q.b);
-        keep.factor = (float)(p.c5 / kScale);
-        keep.beta = (float)p.c3;
+        keep.factor = (float)(p.c5 * (kScale / (kGramScale * kGramScale)));
+        keep.beta = (float)(p.c3 * (kScale / kGramScale));
         keep.diagonal = (float)(p.c1 * kScale);
         keep.power = 0;
         keep.with_r = 1;
