@@ -681,7 +681,7 @@ int64_t gpga_feed_forward_backward_scratch_bytes(const gpga_feed_forward_backwar
  * must keep p(s) and c1 + c3 s^2 + c5 s^4 within [-8, 8] on the way (fp16 range of the products).  M and out have type dtype.
  * fp32 and fp16 are computed with 22 significant bits and fp32 sums; so is bfloat16 where a side has at most 128 rows or
  * columns, and with 11 bits otherwise (the result is off by 1.2 to 1.4 times its own rounding).  X is held to 2^-36 besides, so
- * an update whose norm is below 2^-12 eps keeps fewer bits.  Zero gives zero; an infinity or NaN in M makes its node NaN.
+ * an update whose norm is small beside eps keeps fewer bits.  Zero gives zero; an infinity or NaN in M makes its node NaN.
  * 1 <= r, c <= 2^20, nodes * r * c <= 2^40, 1 <= steps <= 1000.  out may be M itself.
  */
 typedef struct gpga_orthogonalize_args {

@@ -293,11 +293,6 @@ struct StoreRows {
     }
 };
 
-inline bool rows_on_16(const void* p, int64_t ld, int64_t rows, int64_t node, int64_t nodes, int size)
-{
-    return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (rows <= 1 || ld * size % 16 == 0) && (nodes <= 1 || node * size % 16 == 0);
-}
-
 // The sums of a product left in parts: [batch][part][m][ld], added in the order of k.  A thread takes eight columns.
 template <class T, bool PAIRS>
 __global__ void __launch_bounds__(256) sum_parts_kernel(const float* sums, int parts, int m, int n, int64_t ld, int64_t chunks, const __grid_constant__ StoreRows<T, PAIRS> out)

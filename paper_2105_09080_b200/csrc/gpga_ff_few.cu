@@ -62,7 +62,7 @@ __device__ __forceinline__ void as_pairs(const Raw<W>& r, uint32_t (&o)[Q][4])
 }
 
 // What is done with a finished sum of both projections (or of the one): g, u, h, or y.
-template <class T, class H, bool GATE>
+template <class T, bool GATE>
 __device__ __forceinline__ void finish(const FewParams& p, int node, int token, int row, float a, float b)
 {
     const int64_t t = (int64_t)node * p.tokens + token;
@@ -74,11 +74,11 @@ __device__ __forceinline__ void finish(const FewParams& p, int node, int token, 
         float v[1] = {a};
         act_values<sizeof(T) == 2>(v, p.kind);
         const float h = v[0] * b;
-        H* const at = static_cast<H*>(p.out) + t * p.ldo + row;
-        *at = from_f32<H>(h);
-        if (sizeof(H) == 2 && p.lo) {
+        T* const at = static_cast<T*>(p.out) + t * p.ldo + row;
+        *at = from_f32<T>(h);
+        if (sizeof(T) == 2 && p.lo) {
             const float rounded = to_f32(*at);    // no rest beside an infinity: it could be NaN
-            at[p.lo] = from_f32<H>(fabsf(rounded) <= 3.4028234e38f ? h - rounded : 0.f);
+            at[p.lo] = from_f32<T>(fabsf(rounded) <= 3.4028234e38f ? h - rounded : 0.f);
         }
     } else {
         static_cast<T*>(p.out)[t * p.ldo + row] = from_f32<T>(a);
@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(kFewWarps * 32) few_tokens_kernel(const __grid
         float s[M];
 #pragma unroll
         for (int m = 0; m < M; ++m) s[m] = cluster_sum(sums, (m * N + n) * S + r, M * N * S, p.blocks);
-        finish<T, T, GATE>(p, node, n, row0 + r, s[0], s[M - 1]);
+        finish<T, GATE>(p, node, n, row0 + r, s[0], s[M - 1]);
     }
     cluster_farewell();   // nobody goes while its sums are read
 }
@@ -365,7 +365,7 @@ __global__ void __launch_bounds__(kFewWarps * 32) few_streamed_kernel(const __gr
                 a += here[(v * N + n) * S + r];
                 if constexpr (GATE) b += here[(v * N + n) * S + r + 8];
             }
-            finish<T, T, GATE>(p, node, n, row, a, b);
+            finish<T, GATE>(p, node, n, row, a, b);
         }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
@@ -466,7 +466,7 @@ __global__ void __launch_bounds__(kFewWarps * 32) few_tokens_f32_kernel(const __
             float s[M];
 #pragma unroll
             for (int m = 0; m < M; ++m) s[m] = cluster_sum(sums, (m * R + r) * N + n, M * R * N, p.blocks);
-            finish<float, float, GATE>(p, node, n, row0 + r, s[0], s[M - 1]);
+            finish<float, GATE>(p, node, n, row0 + r, s[0], s[M - 1]);
         }
     }
     cluster_barrier();

@@ -192,11 +192,6 @@ struct LastStep {
     __device__ __forceinline__ void one(float v, int batch, int row, int col) const { rows(batch).one(v, row, col); }
 };
 
-bool on_16(const void* p, int64_t ld, int64_t rows, int64_t node, int64_t nodes, int size)
-{
-    return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (rows <= 1 || ld * size % 16 == 0) && (nodes <= 1 || node * size % 16 == 0);
-}
-
 // fp16 values that a matrix is held in.
 int pieces_for(const OrthParams& p) { return p.dtype == GPGA_BF16 && std::min(p.r, p.c) > kSmallSide ? 1 : 2; }
 
@@ -506,7 +501,7 @@ cudaError_t orth_small(const OrthParams& p, cudaStream_t stream)
     q.c = (int32_t)p.c;
     q.steps = (int32_t)p.steps;
     q.accumulate = p.accumulate;
-    q.vec = on_16(p.m, p.ldm, p.r, p.node_ldm, p.nodes, sizeof(T));
+    q.vec = rows_on_16(p.m, p.ldm, p.r, p.node_ldm, p.nodes, sizeof(T));
     static std::atomic<unsigned long long> limit_set{0};
     const cudaError_t e = ensure_smem_limit(orth_small_kernel<T>, kGemmSmem, limit_set);
     if (e != cudaSuccess) return e;
@@ -519,7 +514,7 @@ cudaError_t orth(const OrthParams& p, cudaStream_t stream)
 {
     const OrthPlan q = plan_orth(p);
     const T* m = static_cast<const T*>(p.m);
-    const int vec = on_16(p.m, p.ldm, p.r, p.node_ldm, p.nodes, sizeof(T));
+    const int vec = rows_on_16(p.m, p.ldm, p.r, p.node_ldm, p.nodes, sizeof(T));
     square_sum_kernel<T><<<dim3(q.count_parts, (unsigned)p.nodes), 256, 0, stream>>>(m, p.ldm, p.node_ldm, p.r, p.c, vec, q.parts);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
@@ -583,7 +578,7 @@ cudaError_t orth(const OrthParams& p, cudaStream_t stream)
             last.factor = (float)(p.scale / ((double)kScale * kScale));
             last.power = first;
             last.accumulate = p.accumulate;
-            last.vec = on_16(p.out, p.ldo, p.r, p.node_ldo, p.nodes, sizeof(T));
+            last.vec = rows_on_16(p.out, p.ldo, p.r, p.node_ldo, p.nodes, sizeof(T));
             if ((e = launch_gemm<P, T>(g, last, stream)) != cudaSuccess) return e;
         }
     }

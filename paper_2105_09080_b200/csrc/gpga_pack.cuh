@@ -250,6 +250,12 @@ __global__ void __launch_bounds__(256) pack_columns_kernel(const __grid_constant
 
 }  // namespace
 
+// Whether all rows of a matrix per node start on 16 bytes.
+inline bool rows_on_16(const void* p, int64_t ld, int64_t rows, int64_t node, int64_t nodes, int size)
+{
+    return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (rows <= 1 || ld * size % 16 == 0) && (nodes <= 1 || node * size % 16 == 0);
+}
+
 // Scratch handed out from the front, on 256 bytes.
 struct ScratchPlan {
     int64_t bytes = 0;
@@ -305,7 +311,7 @@ struct PackPlan {
         j.batches = batches;
         j.chunks = chunks;
         j.first = jobs.units;
-        j.vec = (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (rows == 1 || ld * size % 16 == 0) && (batches == 1 || batch * size % 16 == 0);
+        j.vec = rows_on_16(p, ld, rows, batch, batches, size);
         j.src_f32 = f32;
         j.pieces = pieces;
         j.dst = base + at;

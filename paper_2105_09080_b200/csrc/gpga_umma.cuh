@@ -147,16 +147,6 @@ __device__ __forceinline__ void tmem_load32(uint32_t at, float (&v)[32])
         : "r"(at));
 }
 
-__device__ __forceinline__ void tmem_load16(uint32_t at, float (&v)[16])
-{
-    uint32_t* r = reinterpret_cast<uint32_t*>(v);
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
-          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(at));
-}
-
 // Descriptor of an operand tile in shared memory with the 128-byte swizzle (rows of 128 bytes, eight of them a 1024-byte
 // atom; the tile starts on 1024 bytes).  Rows run along the sum's axis (mn_major: the other way round, in chunks of 64 rows
 // or columns that lie chunk_bytes apart).
