@@ -10,6 +10,7 @@ import pytest
 import torch
 
 import paper_2105_09080_b200 as pkg
+import test_gpu_matrix_ops as block
 from test_gpu_matrix_ops import ACT, F32, TINY, U, block_bound, normal, normal_inputs, slope, sums
 
 pytestmark = pytest.mark.gpu
@@ -103,3 +104,36 @@ def test_gradient_of_values_far_apart(size, what, far):
     got = pkg.feed_forward_backward(dy, x, g, u, gate, up, down)
     for name, a, (want, bound) in zip(("dx", "dgate", "dup", "ddown"), got, gradient_bound(dy, x, g, u, gate, up, down, "silu")):
         assert ((a.double() - want).abs() <= bound).all(), name
+
+
+# 5, 3, 2 and 1 chunks of eight columns to a row; many nodes; rows that are longer than what a warp holds
+NARROW = [(1, 60000, 40, 900), (1, 60001, 901, 39), (1, 100000, 20, 1050), (1, 130000, 16, 1010), (2, 130000, 8, 1010), (64, 300, 130, 900), (1, 300, 3001, 2500)]
+
+
+@pytest.mark.parametrize("size", NARROW, ids=str)
+def test_narrow_and_long_rows_in_pairs_are_exact(size):
+    """Whole numbers, whose sums are exact in fp32 whatever their order."""
+    x, gate, up, down = block.whole_inputs(*size, F32, F32, seed=50)
+    gen = block.generator(51)
+    dy = block.whole(x.shape, gen, F32)
+    want = block.whole_forward(x, gate, up, down)
+    y, g, u = pkg.feed_forward_forward(x, gate, up, down, activation="relu")
+    assert all(torch.equal(a, b) for a, b in zip((y, g, u), want))
+    want = [v.float() for v in block.whole_backward(dy, x, g, u, gate, up, down)]
+    got = pkg.feed_forward_backward(dy, x, g, u, gate, up, down, activation="relu")
+    for name, a, b in zip(("dx", "dgate", "dup", "ddown"), got, want):
+        assert torch.equal(a, b), name
+    pkg.token_status()
+
+
+@pytest.mark.parametrize("size", NARROW, ids=str)
+def test_gradient_of_narrow_and_long_rows_in_pairs(size):
+    """Tokens 2^30 apart, each element within its own bound."""
+    args = normal_inputs(*size, F32, F32, seed=52)
+    n, t, d, f = size
+    gen = block.generator(53)
+    dy, g, u = normal((n, t, d), gen, F32), normal((n, t, f), gen, F32, 1.5), normal((n, t, f), gen, F32)
+    dy[:, ::6] *= FAR
+    got = pkg.feed_forward_backward(dy, args[0], g, u, *args[1:])
+    for name, a, (want, off) in zip(("dx", "dgate", "dup", "ddown"), got, gradient_bound(dy, args[0], g, u, *args[1:], "silu")):
+        assert ((a.double() - want).abs() <= off).all(), name
