@@ -623,7 +623,7 @@ int64_t gpga_layer_norm_scratch_bytes(int64_t nodes, int64_t rows, int64_t d);
  *  - A matrix of node i is row-major and starts at p + i * node_p, its rows ld_p apart (elements).  Weights are fp32 (slices of
  *    X) or of the activations' type.
  *  - fp32 operands (all of a call with fp32 activations) are taken as exact sums of three bfloat16 values, or, in calls of
- *    4e9 operations or more (gradients: 24e9), as the sum of two fp16 values times a power of two, one for each row of a factor of
+ *    4e9 operations or more (gradients: 10e9), as the sum of two fp16 values times a power of two, one for each row of a factor of
  *    a product that sums over columns and one for each column of one that sums over rows (the columns of gate and up share
  *    theirs in dx).  In such a sum a value is 2^-23 of itself off, or 2^-40 of the largest finite value that shares its power if
  *    that is more; nodes, and rows and columns that are not summed over, are as independent as in fp32 arithmetic.  An infinity

@@ -30,11 +30,11 @@ inline bool ff_few(const FeedForwardParams& p)
 // Whether fp32 operands are taken as pairs of fp16 values (three products of pieces, with passes for the powers of two of rows and
 // columns) and not as three bfloat16 values (six products): where the products take long enough for the passes.  Measured with
 // three values and with pairs: forward 442 x 221 x 602 on 3 nodes 41 us and 54 us, 4096 x 256 x 688 56 us and 57 us, 700 x 700 x
-// 1500 60 us and 53 us, 1151 x 743 x 1901 118 us and 102 us; gradient 1151 x 743 x 1901 182 us and 198 us, 1024 x 1024 x 1024 on 2
-// nodes 184 us and 175 us, 2048 x 768 x 2048 229 us and 197 us.
+// 1500 60 us and 53 us, 1151 x 743 x 1901 118 us and 102 us; gradient 1024 x 512 x 1024 74 us and 79 us, 700 x 700 x 1500
+// 100 us and 101 us, 1536 x 768 x 768 105 us and 101 us, 2048 x 768 x 2048 229 us and 197 us.
 inline bool ff_pairs(const FeedForwardParams& p, bool backward)
 {
-    return p.dtype == 0 && (double)p.nodes * p.rows * p.d * p.f * (backward ? 12 : 6) >= (backward ? 24e9 : 4e9);
+    return p.dtype == 0 && (double)p.nodes * p.rows * p.d * p.f * (backward ? 12 : 6) >= (backward ? 10e9 : 4e9);
 }
 int64_t ff_few_scratch_bytes(const FeedForwardParams& p);
 cudaError_t launch_ff_few(const FeedForwardParams& p, cudaStream_t stream);

@@ -163,11 +163,14 @@ __device__ __forceinline__ StripPlace strip_place(int64_t unit, int64_t rows, in
     s.end = min(s.first + slice, rows);
     return s;
 }
-// Rows of a unit: enough units for the device, and no more adding up of their largest values than that takes.
+// Rows of a unit: few where there would be too few units for the device otherwise (a thread goes through its rows one after the
+// other), and no more adding up of their largest values than that takes.  Gradient of 1024 x 512 x 1024: 79 us, 97 us with 64 rows
+// throughout.
 inline int slice_rows(int64_t rows, int64_t chunks, int64_t batches, int sms)
 {
-    int slice = 64;
-    while (slice < 1024 && batches * ((rows + slice - 1) / slice) * ((chunks + 31) / 32) > (int64_t)sms * 16) slice *= 2;
+    int slice = 8;
+    const auto units = [&] { return batches * ((rows + slice - 1) / slice) * ((chunks + 31) / 32); };
+    while ((slice < 64 && units() > (int64_t)sms * 5 / 2) || (slice < 1024 && units() > (int64_t)sms * 16)) slice *= 2;
     return slice;
 }
 

@@ -9,8 +9,11 @@ CSRC = Path(__file__).resolve().parent.parent / "paper_2105_09080_b200" / "csrc"
 
 
 def slice_rows(rows, chunks, batches, sms=148):
-    piece = 64
-    while piece < 1024 and batches * -(-rows // piece) * -(-chunks // 32) > sms * 16:
+    piece = 8
+    while piece < 1024:
+        units = batches * -(-rows // piece) * -(-chunks // 32)
+        if not (piece < 64 and units > sms * 5 // 2 or units > sms * 16):
+            break
         piece *= 2
     return piece
 
