@@ -20,8 +20,10 @@ struct FeedForwardParams {
 };
 
 // Whether the forward pass reads the weights where they lie, without the tensor memory path: for few tokens its time is
-// that of reading them.  Measured with either: 32 tokens, 2048 x 5632, 16-bit weights 30 us and 33 us, fp32 weights 38 us
-// and 94 us; 24 tokens, 4096 x 11008, 16-bit weights 94 us and 81 us, 16 tokens 81 us and 81 us.
+// that of reading them.  Measured with either: 32 tokens, 2048 x 5632, 16-bit weights 30 us and 33 us, fp32 weights 39 us
+// and 97 us; 24 tokens, 4096 x 11008, 16-bit weights 94 us and 81 us, 16 tokens 81 us and 81 us; 8 tokens in fp32, 1024 x 2816 36 us and
+// 48 us, 2048 x 5632 98 us and 157 us.  The form ends at 32 tokens (8 in fp32), where fp32 weights would still gain by it; 16-bit
+// ones do not from 17 tokens on where they are large: 20e6 lies between the two sizes above.
 inline bool ff_few(const FeedForwardParams& p)
 {
     if (p.dtype == 0) return p.rows <= 8;

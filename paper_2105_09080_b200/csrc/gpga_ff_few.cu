@@ -8,8 +8,8 @@
 // are not what bounds.  A block's warps take a part of k each and add up through shared memory, in a fixed order.
 //
 // Rows on 16 bytes are streamed: every warp has 12 to 14 KB of its part on the way to its own ring in shared memory all the time,
-// across the tiles that a block goes through (24 tokens, 2048 x 5632, fp32 weights, 138 MB: 45 us with loads to registers,
-// 36 us streamed; one token 27.2 us, 5.1 TB/s).  With more tokens the reading of x for every tile (from L2) adds 3 us for
+// across the tiles that a block goes through (24 tokens, 2048 x 5632, fp32 weights, 138 MB: 38.5 us; 9 us more with loads to
+// registers; one token 29 us, 4.8 TB/s).  With more tokens the reading of x for every tile (from L2) adds 3 us for
 // each eight of them.
 // Others are loaded as they lie, on clusters of blocks where there are few tiles.  fp32 activations: fp32 arithmetic.  The
 // second launch begins to read its weights while the first runs.

@@ -990,10 +990,12 @@ inline int64_t gemm_tiles(const GemmPlan& g, int64_t n, int side)
     return g.symmetric ? tm * (tm + 1) / 2 : tm * tn;
 }
 
-// Microseconds that 256 x 256 tiles take on pairs of SMs (splits = 0), or 128 x 128 tiles on clusters of `splits` blocks:
-// waves of tiles, k-blocks of a tile, and what a tile costs besides.  A k-block of a 256 x 256 tile
-// takes 0.27 us per product of pieces, one of a 128 x 128 tile on its one SM 0.25 us (a quarter of the work on half of the
-// SMs: each operand byte is used half as often); a 128 x 128 tile is a block's only one, so nothing hides its start and
+// Weight of 256 x 256 tiles on pairs of SMs (splits = 0), or of 128 x 128 tiles on clusters of `splits` blocks, for the choice between
+// them: microseconds of waves of tiles, k-blocks of a tile, and what a tile costs besides.  A k-block of a 256 x 256 tile counts
+// 0.27 us per product of pieces, one of a 128 x 128 tile on its one SM 0.25 us (a quarter of the work on half of the
+// SMs: each operand byte is used half as often), which is the matrix unit's time at its highest clock.  They take longer, more so with all SMs at
+// work, but alike: 0.34 and 0.37 us one tile alone, 0.62 and 0.49 to 0.58 us (16 bits) or 0.36 to 0.39 and 0.40 to 0.44 us (each of three
+// products of two pieces) on all SMs.  A 128 x 128 tile is a block's only one, so nothing hides its start and
 // end.  tail: the epilogue of a block's 128 x 256 part of the last tile.  Measured, all of a call with either: 512 x 512 fp32,
 // two steps, 117 us and (4 blocks) 60 us; 8 x 1024 x 2816 bfloat16 255 us and (1 block) 456 us; gradient of 8000 tokens x
 // 128 x 300, bf16, 145 us and (4 blocks) 84 us.
@@ -1065,7 +1067,8 @@ cudaError_t launch_gemm_up_to(int64_t most, int64_t per, const GemmPlan& g, int 
 }
 
 // Where whole waves of large tiles leave a few over, those may go to clusters of blocks in a second launch (3 us): X X^T of
-// 8 x 1024 x 2816, fp32, has 80 tiles for 74 pairs of SMs (all five steps of its orthogonalisation: 1378 us without, 1211 us with).
+// 8 x 1024 x 2816, fp32, has 80 tiles for 74 pairs of SMs (all five steps of its orthogonalisation, replays of a graph: 1378 us
+// without, 1211 us with).
 // T: the type of the result.
 template <int P, class T, class Epi>
 cudaError_t launch_gemm(const GemmPlan& g, const Epi& epi, cudaStream_t stream)
