@@ -132,7 +132,7 @@ PairsPlan plan_pairs(const FeedForwardParams& p)
     PairsPlan q;
     q.rows.base = q.columns.base = p.scratch;
     q.rows.pieces = q.columns.pieces = 2;
-    q.rows.by = PackPlan::kRows;
+    q.rows.by = PackPlan::rows(p.d);
     q.columns.by = PackPlan::kColumns;
     ScratchPlan& s = q.columns.scratch;
     const int64_t d8 = padded(p.d), f8 = padded(p.f), n = p.nodes;
@@ -263,7 +263,10 @@ __global__ void __launch_bounds__(256) slopes_kernel(const __grid_constant__ Slo
                 }
             }
             if constexpr (!PACK) {
-                for (int o = s.lanes / 2; o; o >>= 1) most = max(most, __shfl_xor_sync(~0u, most, o));
+                if (s.lanes == 32)
+                    most = __reduce_max_sync(~0u, most);
+                else
+                    for (int o = s.lanes / 2; o; o >>= 1) most = max(most, __shfl_xor_sync(~0u, most, o));
                 if ((threadIdx.x & (s.lanes - 1)) == 0 && most) atomicMax(p.peaks_rows + s.batch * padded(p.rows) + r, most);
             }
         }

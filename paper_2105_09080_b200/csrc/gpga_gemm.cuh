@@ -198,6 +198,11 @@ struct Raw {
             for (int i = 0; i < 4; ++i) w[i] = (2 * i < n ? h[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)h[2 * i + 1] << 16 : 0u);
         }
     }
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int i = 0; i < 2 * (int)sizeof(T); ++i) w[i] = 0;
+    }
     __device__ __forceinline__ void set(const float (&v)[8])
     {
         if constexpr (sizeof(T) == 4) {

@@ -25,7 +25,7 @@ struct PackJobs {
     PackJob job[kPackJobs];
     int count;
     int slice;                // by columns: rows of a unit
-    int64_t units;            // chunks; rows; or pieces of `slice` rows by 32 chunks
+    int64_t units;            // chunks; what a block holds of rows; or pieces of `slice` rows by 32 chunks
     __device__ __forceinline__ const PackJob& of(int64_t unit) const
     {
         int i = 0;
@@ -86,10 +86,126 @@ __global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackJ
 
 namespace {
 
-// fp32 rows to pairs, a power of two for each row.  A warp takes a row: it holds 2048 columns, so that they are read once; of
-// longer rows the rest comes from L2 again.  cleared: 16-byte words that later launches find zero.
-constexpr int kHeldChunks = 8;
+// Threads that lie along a row of chunks: a power of two, `most` at most.
+__host__ __device__ inline int row_threads(int64_t chunks, int most)
+{
+    int n = 1;
+    while (n < most && n < chunks) n *= 2;
+    return n;
+}
+// A unit of pack_rows_kernel: each thread holds kHeldChunks chunks, `slots` of them of one row.
+constexpr int kHeldChunks = 4;
+__host__ __device__ inline int row_slots(int64_t chunks) { return chunks > 512 ? 4 : chunks > 256 ? 2 : 1; }
+__host__ __device__ inline int rows_of_unit(int64_t chunks) { return kHeldChunks / row_slots(chunks) * (256 / row_threads(chunks, 256)); }
+
+// fp32 rows to pairs, a power of two for each row; bound by memory.  A block takes as many rows as it holds (8192 columns), so
+// that they are read once and their reads are under way together; of longer rows the rest comes from L2 again.  A row for each warp,
+// one after the other, took 114 us for the operands of 64 x 300 x 130 x 900.  cleared: 16-byte words that later launches find zero.
 __global__ void __launch_bounds__(256) pack_rows_kernel(const __grid_constant__ PackJobs jobs, uint4* cleared, int64_t clear)
+{
+    grid_launch_dependents();
+    grid_dependency_wait();
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < clear; i += (int64_t)gridDim.x * 256) cleared[i] = make_uint4(0, 0, 0, 0);
+    __shared__ uint32_t of_warp[2][kHeldChunks][8];    // of units in turn: one's are read while the next one's are written
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int turn = 0;
+    for (int64_t unit = blockIdx.x; unit < jobs.units; unit += gridDim.x, turn ^= 1) {
+        const PackJob& j = jobs.of(unit);
+        const int chunks = (int)j.chunks, cols = (int)j.cols, threads = row_threads(chunks, 256), slots = row_slots(chunks), side = 256 / threads;
+        const int own = threadIdx.x & (threads - 1);
+        const int64_t first = (unit - j.first) * rows_of_unit(chunks) + threadIdx.x / threads, rows = j.batches * j.rows;
+        const auto largest = [](const Raw<float>& x) {
+            float v[8];
+            uint32_t p = 0;
+            x.values(v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) p = max(p, finite_bits(v[k]));
+            return p;
+        };
+        const auto place = [&](int64_t row, int64_t& b) {      // of a row in the source
+            b = row >> 31 ? row / j.rows : (int64_t)((uint32_t)row / (uint32_t)j.rows);
+            return static_cast<const float*>(j.src) + b * j.batch + (row - b * j.rows) * j.ld;
+        };
+        Raw<float> held[kHeldChunks];
+        uint32_t peak[kHeldChunks];
+#pragma unroll
+        for (int q = 0; q < kHeldChunks; ++q) {
+            const int64_t row = first + q / slots * side;
+            const int c = own + threads * (q & (slots - 1));
+            int64_t b;
+            if (row < rows && c < chunks)
+                held[q].load(place(row, b) + 8 * c, cols - 8 * c, j.vec);
+            else
+                held[q].zero();
+        }
+#pragma unroll
+        for (int q = 0; q < kHeldChunks; ++q) peak[q] = largest(held[q]);
+        const bool longer = chunks > 256 * kHeldChunks;      // one row
+        if (longer) {
+            int64_t b;
+            const float* const from = place(first, b);
+            for (int c = own + 256 * kHeldChunks; c < chunks; c += 256) {
+                Raw<float> x;
+                x.load(from + 8 * c, cols - 8 * c, j.vec);
+                peak[0] = max(peak[0], largest(x));
+            }
+        }
+        if (slots > 1) peak[0] = peak[1] = max(peak[0], peak[1]), peak[2] = peak[3] = max(peak[2], peak[3]);
+        if (slots > 2) peak[0] = peak[1] = peak[2] = peak[3] = max(peak[0], peak[2]);
+#pragma unroll
+        for (int q = 0; q < kHeldChunks; ++q) {
+            if (threads >= 32)
+                peak[q] = __reduce_max_sync(~0u, peak[q]);
+            else
+                for (int o = threads / 2; o; o >>= 1) peak[q] = max(peak[q], __shfl_xor_sync(~0u, peak[q], o));
+        }
+        if (threads > 32) {
+            const int warps = threads / 32, from = warp & ~(warps - 1);
+            if (lane == 0)
+#pragma unroll
+                for (int q = 0; q < kHeldChunks; ++q) of_warp[turn][q][warp] = peak[q];
+            __syncthreads();
+            for (int i = 0; i < warps; ++i)
+#pragma unroll
+                for (int q = 0; q < kHeldChunks; ++q) peak[q] = max(peak[q], of_warp[turn][q][from + i]);
+        }
+        const Pieces<__half> dst{static_cast<__half*>(j.dst), j.dst_piece, 0, 0};
+        const auto put = [&](const Raw<float>& x, int64_t row, int c, float scale) {
+            float v[8];
+            x.values(v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] *= scale;
+            dst.template store_at<2>((row * chunks + c) * 8, v);
+        };
+#pragma unroll
+        for (int q = 0; q < kHeldChunks; ++q) {
+            const int64_t row = first + q / slots * side;
+            const int c = own + threads * (q & (slots - 1)), e = scale_exponent(peak[q]);
+            if (row >= rows) continue;
+            if (c == 0) {
+                int64_t b;
+                place(row, b);
+                j.exponents[b * padded(j.rows) + row - b * j.rows] = (int8_t)-e;
+            }
+            if (c < chunks) put(held[q], row, c, power_of_two(e));
+        }
+        if (longer) {
+            int64_t b;
+            const float* const from = place(first, b);
+            const float scale = power_of_two(scale_exponent(peak[0]));
+            for (int c = own + 256 * kHeldChunks; c < chunks; c += 256) {
+                Raw<float> x;
+                x.load(from + 8 * c, cols - 8 * c, j.vec);
+                put(x, first, c, scale);
+            }
+        }
+    }
+}
+
+// The same, a warp to a row: it holds 2048 columns.  For long rows, where the block's barriers cost more than rows that are read one
+// after the other (long_rows).
+constexpr int kWarpChunks = 8;
+__global__ void __launch_bounds__(256) pack_long_rows_kernel(const __grid_constant__ PackJobs jobs, uint4* cleared, int64_t clear)
 {
     grid_launch_dependents();
     grid_dependency_wait();
@@ -100,7 +216,7 @@ __global__ void __launch_bounds__(256) pack_rows_kernel(const __grid_constant__ 
         const int64_t row = at - j.first, b = row / j.rows, r = row - b * j.rows;
         const float* const from = static_cast<const float*>(j.src) + b * j.batch + r * j.ld;
         const int chunks = (int)j.chunks, cols = (int)j.cols;
-        Raw<float> held[kHeldChunks];
+        Raw<float> held[kWarpChunks];
         uint32_t peak = 0;
         const auto largest = [&](const Raw<float>& x) {
             float v[8];
@@ -109,14 +225,14 @@ __global__ void __launch_bounds__(256) pack_rows_kernel(const __grid_constant__ 
             for (int k = 0; k < 8; ++k) peak = max(peak, finite_bits(v[k]));
         };
 #pragma unroll
-        for (int q = 0; q < kHeldChunks; ++q) {
+        for (int q = 0; q < kWarpChunks; ++q) {
             const int c = lane + 32 * q;
             if (c < chunks) held[q].load(from + 8 * c, cols - 8 * c, j.vec);
         }
 #pragma unroll
-        for (int q = 0; q < kHeldChunks; ++q)
+        for (int q = 0; q < kWarpChunks; ++q)
             if (lane + 32 * q < chunks) largest(held[q]);
-        for (int c = lane + 32 * kHeldChunks; c < chunks; c += 32) {
+        for (int c = lane + 32 * kWarpChunks; c < chunks; c += 32) {
             Raw<float> x;
             x.load(from + 8 * c, cols - 8 * c, j.vec);
             largest(x);
@@ -133,15 +249,19 @@ __global__ void __launch_bounds__(256) pack_rows_kernel(const __grid_constant__ 
             dst.template store_at<2>(8 * c, v);
         };
 #pragma unroll
-        for (int q = 0; q < kHeldChunks; ++q)
+        for (int q = 0; q < kWarpChunks; ++q)
             if (lane + 32 * q < chunks) put(held[q], lane + 32 * q);
-        for (int c = lane + 32 * kHeldChunks; c < chunks; c += 32) {
+        for (int c = lane + 32 * kWarpChunks; c < chunks; c += 32) {
             Raw<float> x;
             x.load(from + 8 * c, cols - 8 * c, j.vec);
             put(x, c);
         }
     }
 }
+
+// Whether rows of so many columns go to warps.  Measured with warps and with blocks, all of a forward call: 4096 x 768 x 2048 168 us and
+// 173 us, 64 x 300 x 130 x 900 324 us and 298 us, 20000 x 64 x 1024 152 us and 148 us.
+inline bool long_rows(int64_t cols) { return cols >= 512; }
 
 // Where a thread of a block is in a unit of `slice` rows by 32 chunks (fewer where rows are shorter; a power of two of threads
 // lies along a row): chunk `chunk`, if the row has it, of the rows first + group, first + group + step, ... below end.
@@ -155,7 +275,7 @@ __device__ __forceinline__ StripPlace strip_place(int64_t unit, int64_t rows, in
     const int64_t strips = (chunks + 31) / 32, slices = (rows + slice - 1) / slice, t = unit / strips;
     s.strip = (int)(unit - t * strips);
     s.batch = t / slices;
-    s.lanes = chunks > 16 ? 32 : chunks > 8 ? 16 : chunks > 4 ? 8 : chunks > 2 ? 4 : (int)chunks;
+    s.lanes = row_threads(chunks, 32);
     s.chunk = s.strip * 32 + (threadIdx.x & (s.lanes - 1));
     s.first = (t - s.batch * slices) * slice;
     s.group = threadIdx.x / s.lanes;
@@ -272,9 +392,10 @@ struct ScratchPlan {
 
 // An operand that a tiled copy can read: where it lies, or packed into scratch by the launch that `jobs` collects.
 struct PackPlan {
-    enum By { kChunks, kRows, kColumns };
+    enum By { kChunks, kRows, kLongRows, kColumns };
+    static By rows(int64_t cols) { return long_rows(cols) ? kLongRows : kRows; }
     PackJobs jobs{};
-    By by = kChunks;          // units of the launch; by rows and by columns: pairs times powers of two
+    By by = kChunks;          // units of the launch; by rows (blocks or warps) and by columns: pairs times powers of two
     ScratchPlan scratch;
     char* base = nullptr;     // nullptr: only the sizes are wanted
     int pieces = 1;           // of activations
@@ -320,7 +441,10 @@ struct PackPlan {
         j.dst = base + at;
         j.dst_piece = o.piece;
         ++jobs.count;
-        jobs.units += batches * (by == kChunks ? rows * chunks : by == kRows ? rows : (rows + jobs.slice - 1) / jobs.slice * ((chunks + 31) / 32));
+        jobs.units += by == kChunks ? batches * rows * chunks
+                      : by == kLongRows ? batches * rows
+                      : by == kRows ? (batches * rows + rows_of_unit(chunks) - 1) / rows_of_unit(chunks)
+                                    : batches * ((rows + jobs.slice - 1) / jobs.slice) * ((chunks + 31) / 32);
         return o;
     }
     // An array of pieces in scratch that a kernel of the call writes.
@@ -342,7 +466,7 @@ struct PackPlan {
     int8_t* powers()
     {
         PackJob& j = jobs.job[jobs.count - 1];
-        j.exponents = reinterpret_cast<int8_t*>(base + scratch.take(j.batches * padded(by == kRows ? j.rows : j.cols)));
+        j.exponents = reinterpret_cast<int8_t*>(base + scratch.take(j.batches * padded(by == kColumns ? j.cols : j.rows)));
         return j.exponents;
     }
     template <class T16>
@@ -356,8 +480,9 @@ struct PackPlan {
     // after: the kernel before it on the stream is one of the same call.
     cudaError_t launch_rows(bool after, void* cleared, int64_t clear_bytes, cudaStream_t stream) const
     {
-        const dim3 blocks((unsigned)std::min<int64_t>((jobs.units + 7) / 8, (int64_t)sm_count() * 8));
-        return launch_after_trigger(pack_rows_kernel, blocks, dim3(256), 0, stream, after, jobs, static_cast<uint4*>(cleared), clear_bytes / 16);
+        const bool warps = by == kLongRows;
+        const dim3 blocks((unsigned)std::min<int64_t>(warps ? (jobs.units + 7) / 8 : jobs.units, (int64_t)sm_count() * 8));
+        return launch_after_trigger(warps ? pack_long_rows_kernel : pack_rows_kernel, blocks, dim3(256), 0, stream, after, jobs, static_cast<uint4*>(cleared), clear_bytes / 16);
     }
     cudaError_t launch_columns(bool pack, cudaStream_t stream) const
     {

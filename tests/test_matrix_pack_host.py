@@ -58,3 +58,29 @@ def test_exponents_are_those_of_normal_numbers():
             assert field - bias - e == low
     halves = [h for e in kept for h in (e >> 1, e - (e >> 1))]
     assert min(halves) * 2 >= -126 and max(halves) * 2 <= 127
+
+
+def row_units(rows, chunks):
+    """(row, chunk) that the 256 threads of a block hold of each unit of short rows: four chunks each."""
+    threads = 1
+    while threads < 256 and threads < chunks:
+        threads *= 2
+    slots = 4 if chunks > 512 else 2 if chunks > 256 else 1
+    per = 4 // slots * (256 // threads)
+    for unit in range(-(-rows // per)):
+        for thread in range(256):
+            for q in range(4):
+                row, chunk = unit * per + thread // threads + q // slots * (256 // threads), (thread & (threads - 1)) + threads * (q & (slots - 1))
+                if row < rows and chunk < chunks:
+                    yield row, chunk
+        if chunks > 1024:       # the rest of the one row
+            for thread in range(256):
+                for chunk in range(thread + 1024, chunks, 256):
+                    yield unit, chunk
+
+
+@pytest.mark.parametrize("rows,chunks", [(1, 1), (1025, 1), (700, 2), (300, 3), (130, 17), (65, 33), (33, 64), (9, 200), (5, 256), (5, 257), (3, 512), (3, 513), (2, 1024),
+                                         (2, 1025), (3, 1700)])
+def test_every_chunk_of_short_rows_is_taken_once(rows, chunks):
+    seen = list(row_units(rows, chunks))
+    assert len(seen) == rows * chunks and len(set(seen)) == rows * chunks
