@@ -132,7 +132,7 @@ PairsPlan plan_pairs(const FeedForwardParams& p)
     PairsPlan q;
     q.rows.base = q.columns.base = p.scratch;
     q.rows.pieces = q.columns.pieces = 2;
-    q.rows.by = PackPlan::rows(p.d);
+    q.rows.by_rows(p.d);
     q.columns.by = PackPlan::kColumns;
     ScratchPlan& s = q.columns.scratch;
     const int64_t d8 = padded(p.d), f8 = padded(p.f), n = p.nodes;

@@ -81,8 +81,8 @@ PairsPlan plan_pairs(const FeedForwardParams& p)
     PairsPlan q;
     q.in.base = q.between.base = p.scratch;
     q.in.pieces = q.between.pieces = 2;
-    q.in.by = PackPlan::rows(std::min(p.d, p.f));
-    q.between.by = PackPlan::rows(p.f);
+    q.in.by_rows(std::min(p.d, p.f));
+    q.between.by_rows(p.f);
     q.x = q.in.operand(p.x.p, p.x.ld, p.rows * p.x.ld, p.rows, p.d, p.nodes, true, false, 2);
     q.of_x = q.in.powers();
     q.gate = q.in.operand(p.gate.p, p.gate.ld, p.gate.node, p.f, p.d, p.nodes, true, false, 2);

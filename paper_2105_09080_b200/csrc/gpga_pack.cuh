@@ -393,7 +393,7 @@ struct ScratchPlan {
 // An operand that a tiled copy can read: where it lies, or packed into scratch by the launch that `jobs` collects.
 struct PackPlan {
     enum By { kChunks, kRows, kLongRows, kColumns };
-    static By rows(int64_t cols) { return long_rows(cols) ? kLongRows : kRows; }
+    void by_rows(int64_t cols) { by = long_rows(cols) ? kLongRows : kRows; }    // of `cols` columns at least
     PackJobs jobs{};
     By by = kChunks;          // units of the launch; by rows (blocks or warps) and by columns: pairs times powers of two
     ScratchPlan scratch;
