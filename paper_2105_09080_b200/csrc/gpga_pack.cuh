@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(256) pack_rows_kernel(const __grid_constant__ 
     __shared__ uint32_t of_warp[2][kHeldChunks][8];    // of units in turn: one's are read while the next one's are written
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     int turn = 0;
-    for (int64_t unit = blockIdx.x; unit < jobs.units; unit += gridDim.x, turn ^= 1) {
+    for (int64_t unit = blockIdx.x; unit < jobs.units; unit += gridDim.x) {
         const PackJob& j = jobs.of(unit);
         const int chunks = (int)j.chunks, cols = (int)j.cols, threads = row_threads(chunks, 256), slots = row_slots(chunks), side = 256 / threads;
         const int own = threadIdx.x & (threads - 1);
@@ -168,6 +168,7 @@ __global__ void __launch_bounds__(256) pack_rows_kernel(const __grid_constant__ 
             for (int i = 0; i < warps; ++i)
 #pragma unroll
                 for (int q = 0; q < kHeldChunks; ++q) peak[q] = max(peak[q], of_warp[turn][q][from + i]);
+            turn ^= 1;      // with the barrier: units without one may lie between
         }
         const Pieces<__half> dst{static_cast<__half*>(j.dst), j.dst_piece, 0, 0};
         const auto put = [&](const Raw<float>& x, int64_t row, int c, float scale) {
